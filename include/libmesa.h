@@ -71,9 +71,12 @@
 extern "C" {
 #endif
 
-/* Element type of q, k and v. */
+/* Element type of q, k and v; of the tensors of the recurrence, the checkpoints and the
+ * gradients of the layer's ends.  MESA_DTYPE_Q8, where a call says so: an 8-bit checkpoint
+ * (mesa_checkpoint_pack) in the place of a tensor. */
 #define MESA_DTYPE_F32 0
 #define MESA_DTYPE_BF16 1
+#define MESA_DTYPE_Q8 2
 
 /* Arithmetic of the matrix products inside CG and the read-out.
  *   MESA_PREC_AUTO  : MESA_PREC_BF16X3 for bf16 inputs at chunk 64 (fp32-accurate
@@ -383,6 +386,137 @@ int mesa_backward(const void* k, const void* v, const float* gamma, const float*
                   int64_t d_v, int dtype, int n_cg, int precision, const float* qstar,
                   const float* dout, float* dq, float* dk, float* dv, float* dgamma, float* dbeta,
                   float* dlambda, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Activation checkpoints in 8 bits: what a training forward keeps for its backward pass.
+ * A row of `width` values is held in groups of MESA_CHECKPOINT_GROUP channels; a group has
+ * one power of two 2^E, E the least number >= -126 for which every rint(x / 2^E) (half to
+ * even) lies in [-127, 127], and those codes.  A value comes back as code * 2^E, so its
+ * error is at most 2^E / 2 <= max|x| / 127 over its group, and exactly that in fp32 or bf16.
+ * A group that holds a NaN or an infinity comes back as NaN throughout; magnitudes above
+ * 63.5 * 2^122 come back as 63 * 2^122.
+ * A checkpoint of rows x width is one buffer of mesa_checkpoint_bytes(rows, width) bytes,
+ * 16-byte aligned: the codes int8 [rows, width], then, from the next multiple of 16 bytes,
+ * the exponent bytes uint8 [rows, ceil(width / MESA_CHECKPOINT_GROUP)] (E + 127, or 255 for a
+ * group that is not finite).  Returns 0 for empty or negative sizes.
+ *
+ * mesa_checkpoint_pack: x [rows, width] of dtype (MESA_DTYPE_F32, MESA_DTYPE_BF16), row i at
+ *   element i * stride (stride >= width), into the buffer.
+ * mesa_checkpoint_unpack: the buffer into x, of the same layout.
+ * x aligned to its elements; a fully dense x of whole groups on 16-byte aligned memory runs
+ * fastest.  x and the buffer must not overlap (MESA_ERR_ARG).  One kernel launch. */
+#define MESA_CHECKPOINT_GROUP 32
+size_t mesa_checkpoint_bytes(int64_t rows, int64_t width);
+int mesa_checkpoint_pack(const void* x, int64_t rows, int64_t width, int64_t stride, int dtype, void* checkpoint,
+                         void* stream);
+int mesa_checkpoint_unpack(const void* checkpoint, int64_t rows, int64_t width, int64_t stride, int dtype, void* x,
+                           void* stream);
+
+/* The gated linear recurrence of a Hawk layer, the other layer of the paper's Hawk-Mesa
+ * hybrid: a state per channel instead of the Mesa layer's matrices.  For every sequence b
+ * and channel w, with sigma(x) = 1 / (1 + exp(-x)):
+ *     l_t = -decay softplus(theta) sigma(r_t),  a_t = exp(l_t),  m_t = sqrt(1 - a_t^2)
+ *     h_t = a_t h_{t-1} + m_t sigma(i_t) x_t,   y_t = h_t
+ *   x, r, i  [batch, seq_len, width] dtype (MESA_DTYPE_F32, MESA_DTYPE_BF16): the input and
+ *            the pre-activations of the recurrence and input gates; token (b, t) at element
+ *            (b * seq_len + t) * stride of each (stride >= width: the three may be slices of
+ *            one fused projection)
+ *   theta    [width] fp32;  decay finite and > 0 (8 is usual)
+ *   reset    uint8 [batch, seq_len], or NULL: a token whose byte is not 0 starts a new
+ *            document: a_t = 0, m_t = 1, and neither r_t nor anything before t is read into it
+ *   h0       [batch, width] fp32, or NULL for zeros
+ *   y        [batch, seq_len, width] dtype
+ *   final_h  [batch, width] fp32, or NULL: h after the last token (h0 if there is none)
+ *   states   [batch, ceil(seq_len / MESA_RECURRENCE_BLOCK), width] fp32, or NULL: the states
+ *            entering every block of tokens, which the backward pass starts from
+ *   kept_x, kept_r, kept_i  all three or none: checkpoints of x, r and i
+ *            (mesa_checkpoint_bytes(batch * seq_len, width) bytes each, 16-byte aligned),
+ *            written on the way, the same bytes as mesa_checkpoint_pack's
+ *   workspace / workspace_bytes: at least mesa_recurrence_workspace_bytes(...) (0 for short
+ *            sequences: then it may be NULL), 16-byte aligned
+ * Any width, length and element alignment; the state and every product are fp32.  Outputs
+ * must overlap neither an input nor each other (MESA_ERR_ARG).  At most two kernel launches. */
+#define MESA_RECURRENCE_BLOCK 128
+size_t mesa_recurrence_workspace_bytes(int64_t batch, int64_t seq_len, int64_t width);
+int mesa_recurrence(const void* x, const void* r, const void* i, const float* theta, float decay,
+                    const uint8_t* reset, const float* h0, int64_t batch, int64_t seq_len, int64_t width,
+                    int64_t stride, int dtype, void* y, float* final_h, float* states, void* kept_x, void* kept_r,
+                    void* kept_i, void* workspace, size_t workspace_bytes, void* stream);
+
+/* One token of the recurrence for `batch` independent sequences (decoding).
+ *   state      [batch, width] fp32: h_{t-1};  state_out [batch, width] fp32: h_t, which may be
+ *              `state` itself (in place) and must not overlap it otherwise
+ *   x, r, i    [batch, width] dtype, sequence b at element b * stride;  y [batch, width] dtype
+ *   reset      uint8 [batch], or NULL: sequences that start with this token
+ * One kernel launch. */
+int mesa_recurrence_step(const float* state, const void* x, const void* r, const void* i, const float* theta,
+                         float decay, const uint8_t* reset, int64_t batch, int64_t width, int64_t stride, int dtype,
+                         float* state_out, void* y, void* stream);
+
+/* Backward pass of the recurrence: with dy = dL/dy and dfinal = dL/dh_T (c_{T+1} = dfinal),
+ *     g_t = dy_t + c_{t+1},  c_t = a_t g_t,  dh0 = c_1
+ *     dx = g m sigma(i),  di = dx x (1 - sigma(i))
+ *     dl = g (a h_{t-1} - (a^2 / m) sigma(i) x),  dr = dl l (1 - sigma(r))
+ *     dtheta = -decay sigma(theta) sum_{b,t} dl sigma(r)
+ * (a reset token has dl = 0; where m_t = 0, its term of dl, whose limit in dr is 0, is left out).
+ *   x, r, i    as in mesa_recurrence; with dtype MESA_DTYPE_Q8 the checkpoints that the forward
+ *              or mesa_checkpoint_pack wrote (stride is then not used)
+ *   theta, decay, reset, states: as given to and kept by the forward.  Inside a block the
+ *              states are rebuilt from the one that enters it
+ *   dy         [batch, seq_len, width] grad_dtype;  dfinal [batch, width] fp32 or NULL (zeros)
+ *   dx, dr, di grad_dtype (MESA_DTYPE_F32, MESA_DTYPE_BF16), token (b, t) at element
+ *              (b * seq_len + t) * grad_stride (grad_stride >= width; the three may be slices
+ *              of one array)
+ *   dtheta     [width] fp32;  dh0 [batch, width] fp32 or NULL
+ *   workspace / workspace_bytes: at least mesa_recurrence_backward_workspace_bytes(...),
+ *              16-byte aligned
+ * Every sum is fp32 and in a fixed order.  Outputs must overlap neither an input nor each
+ * other (MESA_ERR_ARG).  With no token dtheta is 0 and dh0 = dfinal.  At most three launches. */
+size_t mesa_recurrence_backward_workspace_bytes(int64_t batch, int64_t seq_len, int64_t width);
+int mesa_recurrence_backward(const void* x, const void* r, const void* i, const float* theta, float decay,
+                             const uint8_t* reset, const float* states, const void* dy, const float* dfinal,
+                             int64_t batch, int64_t seq_len, int64_t width, int64_t stride, int dtype, int grad_dtype,
+                             int64_t grad_stride, void* dx, void* dr, void* di, float* dtheta, float* dh0,
+                             void* workspace, size_t workspace_bytes, void* stream);
+
+/* Backward pass of mesa_frontend: from the gradients of its outputs (dq .. dlambda, as
+ * mesa_backward writes them) those of its inputs.
+ *   qp, kp, vp, conv_q, conv_k, conv_v, a_gamma, a_beta, theta, gamma_cap, l2_eps: as given to
+ *              mesa_frontend (conv_v NULL: the values passed through, and vp may be NULL); with
+ *              dtype MESA_DTYPE_Q8 qp, kp, vp are checkpoints of [batch * seq_len, heads * d]
+ *   dq, dk     [batch, heads, seq_len, d_k] fp32;  dv [batch, heads, seq_len, d_v] fp32
+ *   dgamma, dbeta [batch, heads, seq_len] fp32;  dlambda [heads, d_k] fp32
+ *   dqp, dkp   [batch, seq_len, heads, d_k], dvp [batch, seq_len, heads, d_v]: grad_dtype
+ *              (MESA_DTYPE_F32, MESA_DTYPE_BF16)
+ *   dconv_q, dconv_k [heads * d_k, 4], dconv_v [heads * d_v, 4] (NULL with conv_v): fp32
+ *   da_gamma, da_beta [batch, seq_len, heads] fp32;  dtheta [heads, d_k] fp32
+ *   workspace / workspace_bytes: at least mesa_frontend_backward_workspace_bytes(...)
+ * The projections, filters, dq, dk, dv, dqp, dkp, dvp and the workspace must be 16-byte
+ * aligned, the other arrays 4-byte aligned; outputs must overlap neither an input nor each
+ * other (MESA_ERR_ARG).  batch or seq_len 0 writes the dconv_* (zeros) and dtheta only; heads 0
+ * is a no-op.  Sums are fp32 and in a fixed order.  Two kernel launches. */
+size_t mesa_frontend_backward_workspace_bytes(int64_t batch, int64_t heads, int64_t seq_len, int64_t d_k, int64_t d_v);
+int mesa_frontend_backward(const void* qp, const void* kp, const void* vp, const float* conv_q, const float* conv_k,
+                           const float* conv_v, const float* a_gamma, const float* a_beta, const float* theta,
+                           float gamma_cap, float l2_eps, int64_t batch, int64_t heads, int64_t seq_len, int64_t d_k,
+                           int64_t d_v, int dtype, const float* dq, const float* dk, const float* dv,
+                           const float* dgamma, const float* dbeta, const float* dlambda, int grad_dtype, void* dqp,
+                           void* dkp, void* dvp, float* dconv_q, float* dconv_k, float* dconv_v, float* da_gamma,
+                           float* da_beta, float* dtheta, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Backward pass of mesa_output_norm: with n = 1 / sqrt(mean(o^2) + eps) and z = dy weight,
+ *     do = n (z - n^2 o mean(z o)),  dweight = sum_{b,t} dy o n
+ *   o       [batch, heads, seq_len, d_v]: MESA_DTYPE_F32, or MESA_DTYPE_Q8: a checkpoint of
+ *           [batch * heads * seq_len, d_v]
+ *   dy      [batch, seq_len, heads, d_v] grad_dtype (MESA_DTYPE_F32, MESA_DTYPE_BF16)
+ *   d_o     [batch, heads, seq_len, d_v] fp32 (the dout of mesa_backward)
+ *   dweight [heads, d_v] fp32 (zeros with no token)
+ *   workspace / workspace_bytes: at least mesa_output_norm_backward_workspace_bytes(...)
+ * o, weight, dy, d_o and the workspace 16-byte aligned; outputs must overlap neither an input
+ * nor each other (MESA_ERR_ARG).  Two kernel launches. */
+size_t mesa_output_norm_backward_workspace_bytes(int64_t batch, int64_t heads, int64_t seq_len, int64_t d_v);
+int mesa_output_norm_backward(const void* o, const float* weight, float eps, const void* dy, int64_t batch,
+                              int64_t heads, int64_t seq_len, int64_t d_v, int dtype, int grad_dtype, float* d_o,
+                              float* dweight, void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -128,3 +128,55 @@ def output_norm(o, weight, eps=1e-6):
     o, weight = _f64(o), _f64(weight)
     y = o / np.sqrt(np.mean(o * o, axis=-1, keepdims=True) + eps) * weight[None, :, None, :]
     return np.ascontiguousarray(y.transpose(0, 2, 1, 3))
+
+
+def _silu_grad(u):
+    s = sigmoid(u)
+    return s * (1.0 + u * sigmoid(-_f64(u)))
+
+
+def _short_conv_grad(x, w, du):
+    """Gradients of short_conv: dx_t = sum_i w_i du_{t+i}, dw_i = sum_t du_t x_{t-i}."""
+    T = x.shape[-2]
+    dx, dw = np.zeros_like(x), np.zeros_like(_f64(w))
+    for i in range(min(4, T)):
+        dx[..., :T - i, :] += w[:, i] * du[..., i:, :]
+        dw[:, i] = np.sum(du[..., i:, :] * x[..., :T - i, :], axis=tuple(range(x.ndim - 1)))
+    return dx, dw
+
+
+def frontend_backward(qp, kp, vp, conv_q, conv_k, conv_v, a_gamma, a_beta, theta, dq, dk, dv, dgamma, dbeta, dlam,
+                      gamma_cap=0.9975, l2_eps=1e-6):
+    """Gradients of frontend()'s inputs from those of its outputs, by the chain rule: a dict with
+    dqp, dkp, dvp, dconv_q, dconv_k, dconv_v (None without conv_v), da_gamma, da_beta, dtheta."""
+    out = {}
+    for n, p, w, g in (("q", qp, conv_q, dq), ("k", kp, conv_k, dk), ("v", vp, conv_v, dv)):
+        p, g = _f64(p), _f64(g).transpose(0, 2, 1, 3)
+        B, T, H, d = p.shape
+        if w is None:
+            out["d" + n + "p"], out["dconv_" + n] = np.ascontiguousarray(g), None
+            continue
+        w = _f64(w)
+        u = short_conv(p.reshape(B, T, H * d), w).reshape(B, T, H, d)
+        if n != "v":
+            f = silu(u)
+            size = np.sqrt(np.sum(f * f, axis=-1, keepdims=True) + l2_eps)
+            g = g / size - f * np.sum(f * g, axis=-1, keepdims=True) / size ** 3
+        dp, dw = _short_conv_grad(p.reshape(B, T, H * d), w, (g * _silu_grad(u)).reshape(B, T, H * d))
+        out["d" + n + "p"], out["dconv_" + n] = dp.reshape(B, T, H, d), dw
+    open_, shut, beta = sigmoid(a_gamma), sigmoid(-_f64(a_gamma)), sigmoid(a_beta)
+    dgamma, dbeta = _f64(dgamma).transpose(0, 2, 1), _f64(dbeta).transpose(0, 2, 1)
+    cut = 1.0 - float(gamma_cap)
+    out["da_gamma"] = dgamma * (1.0 - cut * beta ** 2) * open_ * shut
+    out["da_beta"] = (dbeta - 2.0 * cut * dgamma * open_ * beta) * beta * sigmoid(-_f64(a_beta))
+    out["dtheta"] = _f64(dlam) * sigmoid(theta)
+    return out
+
+
+def output_norm_backward(o, weight, dy, eps=1e-6):
+    """Gradients of output_norm(): do [B, H, T, d_v], dweight [H, d_v] from dy [B, T, H, d_v]."""
+    o, weight, dy = _f64(o), _f64(weight), _f64(dy).transpose(0, 2, 1, 3)
+    size = np.sqrt(np.mean(o * o, axis=-1, keepdims=True) + eps)
+    z = dy * weight[None, :, None, :]
+    do = z / size - o * np.mean(z * o, axis=-1, keepdims=True) / size ** 3
+    return do, np.sum(dy * o / size, axis=(0, 2))

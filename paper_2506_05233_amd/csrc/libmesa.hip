@@ -12,43 +12,21 @@
 #include <initializer_list>
 #include <mutex>
 
+#include "mesa_abi.hpp"
 #include "mesa_kernels.hpp"
 
 namespace {
 
+using mesa::finish;
 using mesa::ForwardShape;
+using mesa::overlaps;
+using mesa::Range;
+using mesa::range_of;
 
 bool dim_ok(int64_t d) { return d == 64 || d == 128; }
 bool chunk_ok(int c) { return c == 16 || c == 32 || c == 64; }
 
 int64_t n_chunks_of(int64_t seq_len, int chunk) { return (seq_len + chunk - 1) / chunk; }
-
-// Byte range [p, p + n) of a device array, for overlap checks.
-struct Range {
-    uintptr_t lo, hi;
-};
-Range range_of(const void* p, int64_t bytes) { return {uintptr_t(p), uintptr_t(p) + uintptr_t(bytes)}; }
-bool overlaps(Range a, Range b) { return a.lo < b.hi && b.lo < a.hi; }
-
-// MESA_SYNC_AFTER_LAUNCH (read once, at the first call): when set to anything but
-// "" or "0", every entry point synchronises its stream after its launches and turns
-// an execution error into MESA_ERR_HIP.
-bool sync_after_launch()
-{
-    static const bool on = [] {
-        const char* e = getenv("MESA_SYNC_AFTER_LAUNCH");
-        return e != nullptr && e[0] != '\0' && strcmp(e, "0") != 0;
-    }();
-    return on;
-}
-
-// The status an entry point returns once its launches are enqueued on `stream`.
-int finish(int status, void* stream)
-{
-    if (status != MESA_OK || !sync_after_launch()) return status;
-    if (hipStreamSynchronize(static_cast<hipStream_t>(stream)) != hipSuccess) return MESA_ERR_HIP;
-    return hipGetLastError() == hipSuccess ? MESA_OK : MESA_ERR_HIP;
-}
 
 // MESA_CHECK_FINITE (read once, at the first call): when set to anything but "" or
 // "0", the forward and decode calls check the values of their inputs before their

@@ -26,6 +26,7 @@ constexpr int kDppRowShr4 = 0x114;
 constexpr int kDppRowShr8 = 0x118;
 constexpr int kDppRowRor4 = 0x124;
 constexpr int kDppRowRor8 = 0x128;
+constexpr int kDppRowHalfMirror = 0x141;  // lane i of every eight takes lane 7 - i
 constexpr int kDppRowBcast15 = 0x142;  // last lane of a row to the whole next row
 constexpr int kDppRowBcast31 = 0x143;  // lane 31 to rows 2 and 3
 

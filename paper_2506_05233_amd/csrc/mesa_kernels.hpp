@@ -186,6 +186,123 @@ struct NormArgs {
 };
 hipError_t launch_output_norm(const NormArgs& a, hipStream_t stream);
 
+// Element types of the calls below (MESA_DTYPE_*).
+constexpr int kF32 = 0, kBf16 = 1, kQ8 = 2;
+
+// An 8-bit checkpoint of rows x width values: the int8 codes [rows, width], then, from the
+// next multiple of 16 bytes, the exponent bytes [rows, ceil(width / 32)].
+__host__ __device__ inline int64_t checkpoint_exponents_at(int64_t rows, int64_t width) { return (rows * width + 15) / 16 * 16; }
+
+// pack: x [rows, stride >= width] (fp32 or bf16) -> codes, exponents; else the other way.
+struct CheckpointArgs {
+    const void* x;
+    int64_t rows, width, stride;
+    bool bf16;
+    int8_t* codes;
+    uint8_t* exponents;
+};
+hipError_t launch_checkpoint(const CheckpointArgs& a, bool pack, hipStream_t stream);
+
+// The gated recurrence over [batch, seq_len, width]: token (b, t) of x, r, i at element
+// (b * seq_len + t) * stride, of y at (b * seq_len + t) * width.
+constexpr int kRecurrenceBlock = 128;  // tokens between the states that `states` keeps
+struct RecurrenceArgs {
+    int64_t batch, seq_len, width, stride;
+    int dtype;                // kF32 or kBf16: x, r, i and y
+    const void* x;
+    const void* r;
+    const void* i;
+    const float* theta;       // [width]
+    float decay;
+    const uint8_t* reset;     // [batch, seq_len] ([batch] for a step) or null
+    const float* h0;          // [batch, width]; null: zeros (a step always has it)
+    void* y;
+    float* final_h;           // [batch, width] or null
+    float* states;            // [batch, ceil(seq_len / kRecurrenceBlock), width] or null
+    uint8_t* kept_x;          // checkpoints of x, r, i, all three or null
+    uint8_t* kept_r;
+    uint8_t* kept_i;
+    int tiles;                // recurrence_tiles(seq_len)
+    float2* spans;            // [batch, tiles, width]
+};
+int64_t recurrence_tiles(int64_t seq_len);
+hipError_t launch_recurrence(const RecurrenceArgs& a, hipStream_t stream);
+hipError_t launch_recurrence_step(const RecurrenceArgs& a, float* state_out, hipStream_t stream);
+
+struct RecurrenceGradArgs {
+    int64_t batch, seq_len, width, stride, grad_stride;
+    int dtype, grad_dtype;    // x, r, i (kQ8: checkpoints); dy, dx, dr, di
+    const void* x;
+    const void* r;
+    const void* i;
+    const float* theta;
+    float decay;
+    const uint8_t* reset;
+    const float* states;
+    const void* dy;           // [batch, seq_len, width]
+    const float* dfinal;      // [batch, width] or null
+    void* dx;                 // token (b, t) at element (b * seq_len + t) * grad_stride
+    void* dr;
+    void* di;
+    float* dtheta;            // [width]
+    float* dh0;               // [batch, width] or null
+    int tiles;                // ceil(seq_len / kRecurrenceBlock)
+    float2* spans;            // [batch, tiles, width]
+    float* partial;           // [batch, tiles, width]
+};
+hipError_t launch_recurrence_backward(const RecurrenceGradArgs& a, hipStream_t stream);
+
+// Gradients of the layer's front end (see FrontArgs).
+struct FrontGradArgs {
+    int64_t batch, heads, seq_len;
+    int d_k, d_v;
+    int dtype, grad_dtype;    // qp, kp, vp (kQ8: checkpoints of [batch * seq_len, heads * d]); dqp, dkp, dvp
+    const void* qp;
+    const void* kp;
+    const void* vp;
+    const float* conv_q;
+    const float* conv_k;
+    const float* conv_v;      // or null: the values pass through
+    const float* a_gamma;
+    const float* a_beta;
+    const float* theta;
+    float gamma_cap, l2_eps;
+    const float* dq;          // [batch, heads, seq_len, d]
+    const float* dk;
+    const float* dv;
+    const float* dgamma;      // [batch, heads, seq_len]
+    const float* dbeta;
+    const float* dlambda;     // [heads, d_k]
+    void* dqp;                // [batch, seq_len, heads, d]
+    void* dkp;
+    void* dvp;
+    float* dconv_q;           // [heads * d, 4]
+    float* dconv_k;
+    float* dconv_v;
+    float* da_gamma;          // [batch, seq_len, heads]
+    float* da_beta;
+    float* dtheta;            // [heads, d_k]
+    float* partial;           // front_grad_partial_floats
+};
+int64_t front_grad_partial_floats(int64_t batch, int64_t heads, int64_t seq_len, int d_k, int d_v);
+hipError_t launch_frontend_backward(const FrontGradArgs& a, hipStream_t stream);
+
+// Gradients of the back end (see NormArgs).
+struct NormGradArgs {
+    int64_t batch, heads, seq_len;
+    int d_v;
+    int dtype, grad_dtype;    // o (kF32, or kQ8: a checkpoint of [batch * heads * seq_len, d_v]); dy
+    const void* o;
+    const float* weight;
+    float eps;
+    const void* dy;           // [batch, seq_len, heads, d_v]
+    float* d_o;               // [batch, heads, seq_len, d_v]
+    float* dweight;           // [heads, d_v]
+    float* partial;           // norm_grad_partial_floats
+};
+int64_t norm_grad_partial_floats(int64_t batch, int64_t heads, int64_t seq_len, int d_v);
+hipError_t launch_output_norm_backward(const NormGradArgs& a, hipStream_t stream);
+
 // Compute units of the current device (queried once per device), for the persistent
 // kernels that launch one workgroup per unit.
 int device_compute_units();

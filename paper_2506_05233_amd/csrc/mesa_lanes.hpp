@@ -1,0 +1,164 @@
+// Device helpers of the elementwise and scan kernels: four consecutive channels of a token
+// per lane, held as fp32, bf16 or an 8-bit checkpoint, and the gate functions.
+#pragma once
+
+#include "mesa_device.hpp"
+
+namespace mesa {
+
+constexpr float kLog2e = 1.44269504088896341f;
+constexpr float kLn2 = 0.69314718055994531f;
+
+// Element tag of an 8-bit checkpoint (see the layout at launch_checkpoint_pack): int8 codes
+// and, for every group of kGroup channels of a row, the exponent byte of their common scale.
+struct q8_t {
+    int8_t code;
+};
+constexpr int kGroup = 32;
+
+// The exponent byte of a group whose largest magnitude is amax: E + 127 for the least E >=
+// -126 with rint(amax 2^-E) <= 127; 255 if amax is not finite.  127.5 = 1.9921875 * 2^6 is
+// the first magnitude that no longer fits at E = 0, so adding 1/128 to the significand
+// carries into the exponent exactly there.
+__device__ __forceinline__ uint32_t group_exponent(float amax)
+{
+    const uint32_t u = __float_as_uint(amax);
+    const int e = int((u + 0x10000u) >> 23) - 6;
+    return u >= 0x7F800000u ? 255u : uint32_t(max(e, 1));
+}
+// 2^E, and infinity for byte 255, which turns every code of that group (all 0) into NaN
+__device__ __forceinline__ float group_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
+// 2^-E for the bytes 1..249 (for byte 255 no matter what: group_most brings every code to 0)
+__device__ __forceinline__ float group_inverse(uint32_t byte) { return __uint_as_float(((254u - byte) & 0xFFu) << 23); }
+// Codes of a group are at most 127; at the largest exponent 63, since 64 * 2^122 is past fp32.
+__device__ __forceinline__ float group_most(uint32_t byte) { return byte == 255u ? 0.0f : byte >= 249u ? 63.0f : 127.0f; }
+
+// x 2^-E is exact (or rounds to a magnitude far below 1/2), so the only rounding is rint,
+// half to even; a NaN element (its group has byte 255) becomes 0.
+__device__ __forceinline__ int group_code(float x, float inv, float most)
+{
+    const float c = __builtin_rintf(x * inv);
+    return int(fminf(fmaxf(c, -most), most));
+}
+__device__ __forceinline__ uint32_t pack_codes(const int (&c)[4])
+{
+    return (uint32_t(c[0]) & 0xFFu) | ((uint32_t(c[1]) & 0xFFu) << 8) | ((uint32_t(c[2]) & 0xFFu) << 16) | (uint32_t(c[3]) << 24);
+}
+
+// max |x| with a NaN or an infinity coming out as infinity (fmaxf would drop a NaN): the
+// bits of |x| order as the values do, NaNs above infinity.
+__device__ __forceinline__ uint32_t abs_bits(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
+
+// Two fp32 values rounded to bf16 (nearest even, NaN stays NaN), packed low to high.
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
+{
+    const f32x2_t v = {lo, hi};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2_t));
+}
+
+// Four channels of one token.  Vec: the address is aligned to the four elements and all four
+// exist; otherwise n (0..4) of them are read or written one by one, the others read as 0.
+template <typename T>
+struct Lane4;
+
+template <>
+struct Lane4<float> {
+    using Raw = float4;
+    template <bool Vec>
+    __device__ static Raw load(const void* base, int64_t at, int n)
+    {
+        const float* p = static_cast<const float*>(base) + at;
+        if constexpr (Vec) return n > 0 ? *reinterpret_cast<const float4*>(p) : make_float4(0.f, 0.f, 0.f, 0.f);
+        return make_float4(n > 0 ? p[0] : 0.f, n > 1 ? p[1] : 0.f, n > 2 ? p[2] : 0.f, n > 3 ? p[3] : 0.f);
+    }
+    __device__ static void widen(const Raw& r, float (&x)[4]) { x[0] = r.x, x[1] = r.y, x[2] = r.z, x[3] = r.w; }
+    template <bool Vec>
+    __device__ static void store(void* base, int64_t at, int n, const float (&y)[4])
+    {
+        float* p = static_cast<float*>(base) + at;
+        if constexpr (Vec) {
+            if (n > 0) *reinterpret_cast<float4*>(p) = make_float4(y[0], y[1], y[2], y[3]);
+        } else {
+#pragma unroll
+            for (int v = 0; v < 4; ++v)
+                if (v < n) p[v] = y[v];
+        }
+    }
+};
+
+template <>
+struct Lane4<bf16_t> {
+    using Raw = uint2;
+    template <bool Vec>
+    __device__ static Raw load(const void* base, int64_t at, int n)
+    {
+        const uint16_t* p = static_cast<const uint16_t*>(base) + at;
+        if constexpr (Vec) return n > 0 ? *reinterpret_cast<const uint2*>(p) : make_uint2(0u, 0u);
+        const uint32_t a = n > 0 ? p[0] : 0u, b = n > 1 ? p[1] : 0u, c = n > 2 ? p[2] : 0u, d = n > 3 ? p[3] : 0u;
+        return make_uint2(a | (b << 16), c | (d << 16));
+    }
+    __device__ static void widen(const Raw& r, float (&x)[4])
+    {
+        x[0] = __uint_as_float(r.x << 16), x[1] = __uint_as_float(r.x & 0xFFFF0000u);
+        x[2] = __uint_as_float(r.y << 16), x[3] = __uint_as_float(r.y & 0xFFFF0000u);
+    }
+    template <bool Vec>
+    __device__ static void store(void* base, int64_t at, int n, const float (&y)[4])
+    {
+        uint16_t* p = static_cast<uint16_t*>(base) + at;
+        const uint2 w = make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
+        if constexpr (Vec) {
+            if (n > 0) *reinterpret_cast<uint2*>(p) = w;
+        } else {
+            if (n > 0) p[0] = uint16_t(w.x);
+            if (n > 1) p[1] = uint16_t(w.x >> 16);
+            if (n > 2) p[2] = uint16_t(w.y);
+            if (n > 3) p[3] = uint16_t(w.y >> 16);
+        }
+    }
+};
+
+// Codes of four channels and their group's exponent byte.
+struct Q8Raw {
+    uint32_t codes, byte;
+};
+__device__ __forceinline__ void widen_q8(uint32_t codes, float scale, float (&x)[4])
+{
+#pragma unroll
+    for (int v = 0; v < 4; ++v) x[v] = float(int8_t(codes >> (8 * v))) * scale;
+}
+__device__ __forceinline__ uint32_t load_codes_scalar(const int8_t* p, int n)
+{
+    uint32_t w = 0;
+#pragma unroll
+    for (int v = 0; v < 4; ++v)
+        if (v < n) w |= uint32_t(uint8_t(p[v])) << (8 * v);
+    return w;
+}
+template <bool Vec>
+__device__ __forceinline__ uint32_t load_codes(const int8_t* p, int n)
+{
+    if constexpr (Vec) return n > 0 ? *reinterpret_cast<const uint32_t*>(p) : 0u;
+    return load_codes_scalar(p, n);
+}
+
+// sigma(x); exp(-x) = inf gives 0
+__device__ __forceinline__ float sigmoid_fast(float x) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * x)); }
+// sigma(x) and 1 - sigma(x), each to fp32 accuracy relative to itself
+__device__ __forceinline__ float sigmoid_both(float x, float& rest)
+{
+    const float e = __builtin_amdgcn_exp2f(-kLog2e * x);
+    const float s = __builtin_amdgcn_rcpf(1.0f + e);
+    rest = x > 0.0f ? e * s : 1.0f - s;
+    return s;
+}
+// log(1 + exp(x)) = max(x, 0) + log(1 + exp(-|x|)); a NaN stays one
+__device__ __forceinline__ float softplus_both(float x)
+{
+    const float tail = log1pf(expf(-fabsf(x)));
+    return x > 0.0f ? x + tail : tail;
+}
+
+}  // namespace mesa

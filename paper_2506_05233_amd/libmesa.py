@@ -15,6 +15,7 @@ LIB_PATH = os.path.join(HERE, "_lib", "libmesa.so")
 
 MESA_DTYPE_F32 = 0
 MESA_DTYPE_BF16 = 1
+MESA_DTYPE_Q8 = 2
 MESA_PREC_AUTO = 0
 MESA_PREC_F32 = 1
 MESA_PREC_BF16 = 2
@@ -29,12 +30,19 @@ MESA_ERR_HIP = 6
 MESA_ERR_NONFINITE = 7
 MESA_MAX_NCG = 1024
 MESA_NOALLOC_SCRATCH_BYTES = 64 << 20
+MESA_CHECKPOINT_GROUP = 32
+MESA_RECURRENCE_BLOCK = 128
 
 EXPORTED = ("mesa_forward", "mesa_forward_ex", "mesa_forward_states", "mesa_forward_solve",
             "mesa_forward_tol", "mesa_forward_workspace_bytes", "mesa_decode_step",
             "mesa_decode_step_tol", "mesa_decode_step_packed", "mesa_pack_state", "mesa_unpack_state",
             "mesa_backward", "mesa_backward_workspace_bytes", "mesa_forward_noalloc",
             "mesa_frontend", "mesa_output_norm",
+            "mesa_checkpoint_bytes", "mesa_checkpoint_pack", "mesa_checkpoint_unpack",
+            "mesa_recurrence", "mesa_recurrence_workspace_bytes", "mesa_recurrence_step",
+            "mesa_recurrence_backward", "mesa_recurrence_backward_workspace_bytes",
+            "mesa_frontend_backward", "mesa_frontend_backward_workspace_bytes",
+            "mesa_output_norm_backward", "mesa_output_norm_backward_workspace_bytes",
             "mesa_status_string", "mesa_version")
 
 _lib = None
@@ -95,6 +103,30 @@ def load():
     lib.mesa_frontend.restype = ci
     lib.mesa_output_norm.argtypes = [fp, fp, cf, i64, i64, i64, i64, ci, vp, vp]
     lib.mesa_output_norm.restype = ci
+    lib.mesa_checkpoint_bytes.argtypes = [i64, i64]
+    lib.mesa_checkpoint_bytes.restype = sz
+    lib.mesa_checkpoint_pack.argtypes = lib.mesa_checkpoint_unpack.argtypes = [vp, i64, i64, i64, ci, vp, vp]
+    lib.mesa_checkpoint_pack.restype = lib.mesa_checkpoint_unpack.restype = ci
+    lib.mesa_recurrence_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.mesa_recurrence_workspace_bytes.restype = sz
+    lib.mesa_recurrence.argtypes = [vp, vp, vp, fp, cf, vp, fp, i64, i64, i64, i64, ci, vp, fp, fp, vp, vp, vp, vp, sz, vp]
+    lib.mesa_recurrence.restype = ci
+    lib.mesa_recurrence_step.argtypes = [fp, vp, vp, vp, fp, cf, vp, i64, i64, i64, ci, fp, vp, vp]
+    lib.mesa_recurrence_step.restype = ci
+    lib.mesa_recurrence_backward_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.mesa_recurrence_backward_workspace_bytes.restype = sz
+    lib.mesa_recurrence_backward.argtypes = [vp, vp, vp, fp, cf, vp, fp, vp, fp, i64, i64, i64, i64, ci, ci, i64,
+                                             vp, vp, vp, fp, fp, vp, sz, vp]
+    lib.mesa_recurrence_backward.restype = ci
+    lib.mesa_frontend_backward_workspace_bytes.argtypes = [i64, i64, i64, i64, i64]
+    lib.mesa_frontend_backward_workspace_bytes.restype = sz
+    lib.mesa_frontend_backward.argtypes = ([vp, vp, vp, fp, fp, fp, fp, fp, fp, cf, cf, i64, i64, i64, i64, i64, ci]
+                                           + [fp] * 6 + [ci] + [vp] * 3 + [fp] * 6 + [vp, sz, vp])
+    lib.mesa_frontend_backward.restype = ci
+    lib.mesa_output_norm_backward_workspace_bytes.argtypes = [i64, i64, i64, i64]
+    lib.mesa_output_norm_backward_workspace_bytes.restype = sz
+    lib.mesa_output_norm_backward.argtypes = [vp, fp, cf, vp, i64, i64, i64, i64, ci, ci, fp, fp, vp, sz, vp]
+    lib.mesa_output_norm_backward.restype = ci
     lib.mesa_status_string.argtypes = [ci]
     lib.mesa_status_string.restype = ctypes.c_char_p
     lib.mesa_version.argtypes = []
@@ -506,3 +538,377 @@ def decode_step(state_H, state_G, q, k, v, gamma, beta, lam, n_cg, out=None, eps
     if st != MESA_OK:
         raise MesaError(st, "mesa_decode_step")
     return out
+
+
+# ---------------------------------------------------------------- 8-bit checkpoints
+def _row_stride(t, name):
+    """Elements between the rows of t [..., width]: its last dimension dense, the leading ones
+    one even run of rows."""
+    if t.is_contiguous():
+        return t.shape[-1]
+    shape, stride = t.shape, t.stride()
+    if shape[-1] > 1 and stride[-1] != 1:
+        raise ValueError("%s must be dense along its last dimension" % name)
+    row = span = None
+    for n, st in zip(reversed(shape[:-1]), reversed(stride[:-1])):
+        if n == 1:
+            continue
+        if row is None:
+            row = st
+        elif st != span:
+            raise ValueError("%s must have evenly spaced rows" % name)
+        span = st * n
+    if row is None:
+        return shape[-1]
+    if row < shape[-1]:
+        raise ValueError("%s must not overlap itself" % name)
+    return row
+
+
+def _check_rows(t, name, shape, dtype, device):
+    """As _check, for a tensor whose rows may be spaced; returns their stride."""
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
+    if t.dtype != dtype:
+        raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
+    if t.device != device:
+        raise ValueError("%s is on %s, expected %s" % (name, t.device, device))
+    return _row_stride(t, name)
+
+
+def _float_code(dtype, name):
+    torch = _torch()
+    if dtype == torch.float32:
+        return MESA_DTYPE_F32
+    if dtype == torch.bfloat16:
+        return MESA_DTYPE_BF16
+    raise TypeError("%s must be float32 or bfloat16, got %s" % (name, dtype))
+
+
+def _on_device(t, name):
+    if not isinstance(t, _torch().Tensor):
+        raise TypeError("%s must be a torch.Tensor" % name)
+    if not t.is_cuda:
+        raise ValueError("%s must be a device tensor" % name)
+    return t.device
+
+
+def _workspace(workspace, need, device):
+    """A caller's workspace, when it is given and large enough, or a new one."""
+    if need == 0:
+        return None
+    if workspace is not None and workspace.device == device and workspace.numel() * workspace.element_size() >= need:
+        return workspace
+    return _torch().empty(need, dtype=_torch().uint8, device=device)
+
+
+def checkpoint_bytes(rows, width) -> int:
+    return load().mesa_checkpoint_bytes(rows, width)
+
+
+class Checkpoint:
+    """An 8-bit checkpoint of a tensor of `shape` ([..., width]): the device buffer that
+    mesa_checkpoint_pack writes, about 1.03 bytes a value."""
+
+    __slots__ = ("buffer", "shape")
+
+    def __init__(self, buffer, shape):
+        torch = _torch()
+        self.shape = tuple(int(n) for n in shape)
+        _on_device(buffer, "buffer")
+        if buffer.dtype != torch.uint8 or not buffer.is_contiguous() or buffer.numel() < checkpoint_bytes(self.rows, self.width):
+            raise ValueError("buffer must be a contiguous uint8 tensor of %d bytes" % checkpoint_bytes(self.rows, self.width))
+        self.buffer = buffer
+
+    @classmethod
+    def empty(cls, shape, device):
+        torch = _torch()
+        rows = 1
+        for n in shape[:-1]:
+            rows *= n
+        return cls(torch.empty(checkpoint_bytes(rows, shape[-1]), dtype=torch.uint8, device=device), shape)
+
+    @property
+    def width(self):
+        return self.shape[-1]
+
+    @property
+    def rows(self):
+        n = 1
+        for k in self.shape[:-1]:
+            n *= k
+        return n
+
+    @property
+    def device(self):
+        return self.buffer.device
+
+    @property
+    def codes(self):
+        """int8 [rows, width]"""
+        n = self.rows * self.width
+        return self.buffer[:n].view(_torch().int8).view(self.rows, self.width)
+
+    @property
+    def exponents(self):
+        """uint8 [rows, ceil(width / 32)]: E + 127 of each group, 255 for one that is not finite"""
+        at = -(-self.rows * self.width // 16) * 16
+        groups = -(-self.width // MESA_CHECKPOINT_GROUP)
+        return self.buffer[at:at + self.rows * groups].view(self.rows, groups)
+
+
+def checkpoint_pack(x):
+    """mesa_checkpoint_pack: x [..., width] fp32 or bf16 (rows evenly spaced, so a slice of a
+    fused projection will do) as a Checkpoint."""
+    lib = load()
+    dev = _on_device(x, "x")
+    code = _float_code(x.dtype, "x")
+    stride = _row_stride(x, "x")
+    ck = Checkpoint.empty(x.shape, dev)
+    st = lib.mesa_checkpoint_pack(_ptr(x), ck.rows, ck.width, stride, code, _ptr(ck.buffer), _stream(dev))
+    if st != MESA_OK:
+        raise MesaError(st, "mesa_checkpoint_pack")
+    return ck
+
+
+def checkpoint_unpack(ck, dtype=None, out=None):
+    """mesa_checkpoint_unpack: the values of a Checkpoint, as dtype (torch.bfloat16 by default,
+    which holds them exactly) or into out (rows evenly spaced)."""
+    torch = _torch()
+    lib = load()
+    dev = ck.device
+    if out is None:
+        out = torch.empty(ck.shape, dtype=torch.bfloat16 if dtype is None else dtype, device=dev)
+    stride = _check_rows(out, "out", ck.shape, out.dtype if dtype is None else dtype, dev)
+    st = lib.mesa_checkpoint_unpack(_ptr(ck.buffer), ck.rows, ck.width, stride, _float_code(out.dtype, "out"), _ptr(out),
+                                    _stream(dev))
+    if st != MESA_OK:
+        raise MesaError(st, "mesa_checkpoint_unpack")
+    return out
+
+
+# ---------------------------------------------------------------- the gated recurrence
+def _common_stride(x, r, i, shape, dtype, device):
+    strides = [_check_rows(t, n, shape, dtype, device) for t, n in ((x, "x"), (r, "r"), (i, "i"))]
+    if strides[0] != strides[1] or strides[0] != strides[2]:
+        raise ValueError("x, r and i must have their rows equally spaced, got %s" % (strides,))
+    return strides[0]
+
+
+def recurrence_workspace_bytes(batch, seq_len, width) -> int:
+    return load().mesa_recurrence_workspace_bytes(batch, seq_len, width)
+
+
+def recurrence(x, r, i, theta, decay=8.0, reset=None, h0=None, want_final=False, want_states=False,
+               want_checkpoints=False, out=None, workspace=None):
+    """mesa_recurrence: the gated linear recurrence over x, r, i [B,T,W] (fp32 or bf16, rows
+    evenly spaced alike, e.g. slices of one projection), theta [W] fp32, reset [B,T] uint8 or
+    None (a token that starts a document), h0 [B,W] fp32 or None.  Returns y [B,T,W] of x's
+    dtype, or a dict with "y" and, if asked, "h" [B,W] fp32 (the state after the last token),
+    "states" [B,ceil(T/128),W] fp32 (for recurrence_backward) and the checkpoints "x", "r", "i"
+    of the inputs."""
+    torch = _torch()
+    lib = load()
+    dev = _on_device(x, "x")
+    B, T, W = x.shape
+    f32 = torch.float32
+    stride = _common_stride(x, r, i, (B, T, W), x.dtype, dev)
+    code = _float_code(x.dtype, "x")
+    _check(theta, "theta", (W,), f32, dev)
+    if reset is not None:
+        _check(reset, "reset", (B, T), torch.uint8, dev)
+    if h0 is not None:
+        _check(h0, "h0", (B, W), f32, dev)
+    if out is None:
+        out = torch.empty((B, T, W), dtype=x.dtype, device=dev)
+    else:
+        _check(out, "out", (B, T, W), x.dtype, dev)
+    need = lib.mesa_recurrence_workspace_bytes(B, T, W)
+    workspace = _workspace(workspace, need, dev)
+    res = {"y": out}
+    if want_final:
+        res["h"] = torch.empty((B, W), dtype=f32, device=dev)
+    if want_states:
+        res["states"] = torch.empty((B, -(-T // MESA_RECURRENCE_BLOCK), W), dtype=f32, device=dev)
+    kept = (None, None, None)
+    if want_checkpoints:
+        for n in ("x", "r", "i"):
+            res[n] = Checkpoint.empty((B, T, W), dev)
+        kept = tuple(res[n].buffer for n in ("x", "r", "i"))
+    st = lib.mesa_recurrence(_ptr(x), _ptr(r), _ptr(i), _ptr(theta), float(decay), _ptr(reset), _ptr(h0), B, T, W, stride,
+                             code, _ptr(out), _ptr(res.get("h")), _ptr(res.get("states")), _ptr(kept[0]), _ptr(kept[1]),
+                             _ptr(kept[2]), _ptr(workspace), need, _stream(dev))
+    if st != MESA_OK:
+        raise MesaError(st, "mesa_recurrence")
+    return res if len(res) > 1 else out
+
+
+def recurrence_step(state, x, r, i, theta, decay=8.0, reset=None, state_out=None, out=None):
+    """mesa_recurrence_step: one token of the recurrence.  state [B,W] fp32, updated in place
+    unless state_out is given; x, r, i [B,W] fp32 or bf16 (rows evenly spaced alike); theta [W];
+    reset [B] uint8 or None.  Returns y [B,W] of x's dtype."""
+    torch = _torch()
+    lib = load()
+    dev = _on_device(x, "x")
+    B, W = x.shape
+    stride = _common_stride(x, r, i, (B, W), x.dtype, dev)
+    _check(state, "state", (B, W), torch.float32, dev)
+    _check(theta, "theta", (W,), torch.float32, dev)
+    if reset is not None:
+        _check(reset, "reset", (B,), torch.uint8, dev)
+    if state_out is None:
+        state_out = state
+    else:
+        _check(state_out, "state_out", (B, W), torch.float32, dev)
+    if out is None:
+        out = torch.empty((B, W), dtype=x.dtype, device=dev)
+    else:
+        _check(out, "out", (B, W), x.dtype, dev)
+    st = lib.mesa_recurrence_step(_ptr(state), _ptr(x), _ptr(r), _ptr(i), _ptr(theta), float(decay), _ptr(reset), B, W,
+                                  stride, _float_code(x.dtype, "x"), _ptr(state_out), _ptr(out), _stream(dev))
+    if st != MESA_OK:
+        raise MesaError(st, "mesa_recurrence_step")
+    return out
+
+
+def recurrence_backward_workspace_bytes(batch, seq_len, width) -> int:
+    return load().mesa_recurrence_backward_workspace_bytes(batch, seq_len, width)
+
+
+def recurrence_backward(x, r, i, theta, states, dy, dfinal=None, decay=8.0, reset=None, out=None, workspace=None):
+    """mesa_recurrence_backward: gradients of the recurrence.  x, r, i [B,T,W] as given to
+    recurrence(), or the three Checkpoints it kept; states as it returned them; dy [B,T,W]
+    fp32 or bf16; dfinal [B,W] fp32 or None (no gradient of the last state).  Returns a dict:
+    "dx", "dr", "di" [B,T,W] of dy's dtype (out: three tensors to write them to, rows evenly
+    spaced alike, e.g. slices of one gradient), "dtheta" [W] and "dh0" [B,W] fp32."""
+    torch = _torch()
+    lib = load()
+    B, T, W = shape = tuple(x.shape)
+    f32 = torch.float32
+    if isinstance(x, Checkpoint):
+        dev, code, stride = x.device, MESA_DTYPE_Q8, W
+        for t, n in ((r, "r"), (i, "i")):
+            if not isinstance(t, Checkpoint) or t.shape != shape or t.device != dev:
+                raise TypeError("%s must be a Checkpoint of shape %s on %s, as x is" % (n, shape, dev))
+        x, r, i = x.buffer, r.buffer, i.buffer
+    else:
+        dev = _on_device(x, "x")
+        code = _float_code(x.dtype, "x")
+        stride = _common_stride(x, r, i, shape, x.dtype, dev)
+    _check(theta, "theta", (W,), f32, dev)
+    _check(states, "states", (B, -(-T // MESA_RECURRENCE_BLOCK), W), f32, dev)
+    _check(dy, "dy", shape, device=dev)
+    grad_code = _float_code(dy.dtype, "dy")
+    if dfinal is not None:
+        _check(dfinal, "dfinal", (B, W), f32, dev)
+    if reset is not None:
+        _check(reset, "reset", (B, T), torch.uint8, dev)
+    if out is None:
+        out = tuple(torch.empty(shape, dtype=dy.dtype, device=dev) for _ in range(3))
+        grad_stride = W
+    else:
+        grad_stride = _common_stride(*out, shape, dy.dtype, dev)
+    need = lib.mesa_recurrence_backward_workspace_bytes(B, T, W)
+    workspace = _workspace(workspace, need, dev)
+    res = {"dx": out[0], "dr": out[1], "di": out[2], "dtheta": torch.empty((W,), dtype=f32, device=dev),
+           "dh0": torch.empty((B, W), dtype=f32, device=dev)}
+    st = lib.mesa_recurrence_backward(_ptr(x), _ptr(r), _ptr(i), _ptr(theta), float(decay), _ptr(reset), _ptr(states),
+                                      _ptr(dy), _ptr(dfinal), B, T, W, stride, code, grad_code, grad_stride, _ptr(out[0]),
+                                      _ptr(out[1]), _ptr(out[2]), _ptr(res["dtheta"]), _ptr(res["dh0"]), _ptr(workspace),
+                                      need, _stream(dev))
+    if st != MESA_OK:
+        raise MesaError(st, "mesa_recurrence_backward")
+    return res
+
+
+# ---------------------------------------------------------------- gradients of the layer's ends
+def _held(t, name, shape, dtype, device):
+    """A tensor of shape and dtype, or a Checkpoint of that shape: the tensor behind it."""
+    if isinstance(t, Checkpoint):
+        if dtype is not None or t.shape != tuple(shape) or t.device != device:
+            raise TypeError("%s must be held as the others are, with shape %s on %s" % (name, tuple(shape), device))
+        return t.buffer
+    if dtype is None:
+        raise TypeError("%s must be a Checkpoint, as the others are" % name)
+    _check(t, name, shape, dtype, device)
+    return t
+
+
+def frontend_backward_workspace_bytes(batch, heads, seq_len, d_k, d_v) -> int:
+    return load().mesa_frontend_backward_workspace_bytes(batch, heads, seq_len, d_k, d_v)
+
+
+def frontend_backward(qp, kp, vp, conv_q, conv_k, conv_v, a_gamma, a_beta, theta, dq, dk, dv, dgamma, dbeta, dlam,
+                      gamma_cap=0.9975, l2_eps=1e-6, grad_dtype=None, workspace=None):
+    """mesa_frontend_backward: gradients of frontend()'s inputs from those of its outputs (dq,
+    dk [B,H,T,d_k], dv [B,H,T,d_v], dgamma, dbeta [B,H,T], dlam [H,d_k]: fp32, as backward()
+    returns them).  qp, kp, vp as given to frontend(), or Checkpoints of them.  Returns a dict:
+    "dqp", "dkp" [B,T,H,d_k], "dvp" [B,T,H,d_v] of grad_dtype (the projections' dtype by default,
+    bf16 for Checkpoints), "dconv_q", "dconv_k" [H*d_k,4], "dconv_v" [H*d_v,4] (with conv_v),
+    "da_gamma", "da_beta" [B,T,H], "dtheta" [H,d_k] (fp32)."""
+    torch = _torch()
+    lib = load()
+    B, T, H, dk_ = qp.shape
+    dv_ = vp.shape[-1]
+    f32 = torch.float32
+    q8 = isinstance(qp, Checkpoint)
+    dev = qp.device if q8 else _on_device(qp, "qp")
+    code = MESA_DTYPE_Q8 if q8 else _float_code(qp.dtype, "qp")
+    dtype = None if q8 else qp.dtype
+    if grad_dtype is None:
+        grad_dtype = torch.bfloat16 if q8 else qp.dtype
+    qp = _held(qp, "qp", (B, T, H, dk_), dtype, dev)
+    kp = _held(kp, "kp", (B, T, H, dk_), dtype, dev)
+    vp = _held(vp, "vp", (B, T, H, dv_), dtype, dev)
+    for t, n, shape in ((conv_q, "conv_q", (H * dk_, 4)), (conv_k, "conv_k", (H * dk_, 4)), (conv_v, "conv_v", (H * dv_, 4)),
+                        (a_gamma, "a_gamma", (B, T, H)), (a_beta, "a_beta", (B, T, H)), (theta, "theta", (H, dk_)),
+                        (dq, "dq", (B, H, T, dk_)), (dk, "dk", (B, H, T, dk_)), (dv, "dv", (B, H, T, dv_)),
+                        (dgamma, "dgamma", (B, H, T)), (dbeta, "dbeta", (B, H, T)), (dlam, "dlam", (H, dk_))):
+        if t is not None or n != "conv_v":
+            _check(t, n, shape, f32, dev)
+    new = lambda dt, *shape: torch.empty(shape, dtype=dt, device=dev)
+    res = {"dqp": new(grad_dtype, B, T, H, dk_), "dkp": new(grad_dtype, B, T, H, dk_), "dvp": new(grad_dtype, B, T, H, dv_),
+           "dconv_q": new(f32, H * dk_, 4), "dconv_k": new(f32, H * dk_, 4)}
+    if conv_v is not None:
+        res["dconv_v"] = new(f32, H * dv_, 4)
+    res["da_gamma"], res["da_beta"], res["dtheta"] = new(f32, B, T, H), new(f32, B, T, H), new(f32, H, dk_)
+    need = lib.mesa_frontend_backward_workspace_bytes(B, H, T, dk_, dv_)
+    workspace = _workspace(workspace, need, dev)
+    st = lib.mesa_frontend_backward(_ptr(qp), _ptr(kp), _ptr(vp), _ptr(conv_q), _ptr(conv_k), _ptr(conv_v), _ptr(a_gamma),
+                                    _ptr(a_beta), _ptr(theta), float(gamma_cap), float(l2_eps), B, H, T, dk_, dv_, code,
+                                    _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dgamma), _ptr(dbeta), _ptr(dlam),
+                                    _float_code(grad_dtype, "grad_dtype"), _ptr(res["dqp"]), _ptr(res["dkp"]),
+                                    _ptr(res["dvp"]), _ptr(res["dconv_q"]), _ptr(res["dconv_k"]), _ptr(res.get("dconv_v")),
+                                    _ptr(res["da_gamma"]), _ptr(res["da_beta"]), _ptr(res["dtheta"]), _ptr(workspace), need,
+                                    _stream(dev))
+    if st != MESA_OK:
+        raise MesaError(st, "mesa_frontend_backward")
+    return res
+
+
+def output_norm_backward_workspace_bytes(batch, heads, seq_len, d_v) -> int:
+    return load().mesa_output_norm_backward_workspace_bytes(batch, heads, seq_len, d_v)
+
+
+def output_norm_backward(o, weight, dy, eps=1e-6, workspace=None):
+    """mesa_output_norm_backward: gradients of output_norm() from dy [B,T,H,d_v] (fp32 or bf16).
+    o [B,H,T,d_v] fp32 as given to it, or a Checkpoint of it; weight [H,d_v].  Returns a dict:
+    "do" [B,H,T,d_v] (backward()'s dout) and "dweight" [H,d_v], fp32."""
+    torch = _torch()
+    lib = load()
+    B, H, T, dv_ = o.shape
+    f32 = torch.float32
+    q8 = isinstance(o, Checkpoint)
+    dev = o.device if q8 else _on_device(o, "o")
+    o = _held(o, "o", (B, H, T, dv_), None if q8 else f32, dev)
+    _check(weight, "weight", (H, dv_), f32, dev)
+    _check(dy, "dy", (B, T, H, dv_), device=dev)
+    res = {"do": torch.empty((B, H, T, dv_), dtype=f32, device=dev), "dweight": torch.empty((H, dv_), dtype=f32, device=dev)}
+    need = lib.mesa_output_norm_backward_workspace_bytes(B, H, T, dv_)
+    workspace = _workspace(workspace, need, dev)
+    st = lib.mesa_output_norm_backward(_ptr(o), _ptr(weight), float(eps), _ptr(dy), B, H, T, dv_,
+                                       MESA_DTYPE_Q8 if q8 else MESA_DTYPE_F32, _float_code(dy.dtype, "dy"), _ptr(res["do"]),
+                                       _ptr(res["dweight"]), _ptr(workspace), need, _stream(dev))
+    if st != MESA_OK:
+        raise MesaError(st, "mesa_output_norm_backward")
+    return res
