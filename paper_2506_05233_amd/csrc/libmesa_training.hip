@@ -119,9 +119,6 @@ int recurrence_sizes(int64_t batch, int64_t seq_len, int64_t width, int64_t stri
     return MESA_OK;
 }
 
-// Bytes of the spans of a walk over `tiles` tiles, none for a single tile.
-int64_t span_bytes(int64_t batch, int64_t tiles, int64_t width) { return tiles > 1 ? (batch * tiles * width * 8 + 15) / 16 * 16 : 0; }
-
 int64_t blocks_of(int64_t seq_len) { return (seq_len + MESA_RECURRENCE_BLOCK - 1) / MESA_RECURRENCE_BLOCK; }
 
 bool sizes_countable(int64_t batch, int64_t seq_len, int64_t width)
@@ -152,7 +149,7 @@ int mesa_checkpoint_unpack(const void* buffer, int64_t rows, int64_t width, int6
 size_t mesa_recurrence_workspace_bytes(int64_t batch, int64_t seq_len, int64_t width)
 {
     if (!sizes_countable(batch, seq_len, width)) return 0;
-    return size_t(span_bytes(batch, mesa::recurrence_tiles(seq_len), width));
+    return size_t(mesa::recurrence_walk_bytes(batch, mesa::recurrence_tiles(seq_len), width));
 }
 
 int mesa_recurrence(const void* x, const void* r, const void* i, const float* theta, float decay,
@@ -183,7 +180,7 @@ int mesa_recurrence(const void* x, const void* r, const void* i, const float* th
     const mesa::RecurrenceArgs a{batch, seq_len, width, stride, dtype, x, r, i, theta, decay, reset, h0, y, final_h,
                                  states, static_cast<uint8_t*>(kept_x), static_cast<uint8_t*>(kept_r),
                                  static_cast<uint8_t*>(kept_i), int(mesa::recurrence_tiles(seq_len)),
-                                 static_cast<float2*>(workspace)};
+                                 static_cast<uint64_t*>(workspace)};
     return status_of(mesa::launch_recurrence(a, static_cast<hipStream_t>(stream)), stream);
 }
 
@@ -212,7 +209,7 @@ size_t mesa_recurrence_backward_workspace_bytes(int64_t batch, int64_t seq_len, 
 {
     if (!sizes_countable(batch, seq_len, width)) return 0;
     const int64_t tiles = blocks_of(seq_len);
-    return size_t(span_bytes(batch, tiles, width) + (batch * tiles * width * 4 + 15) / 16 * 16);
+    return size_t(mesa::recurrence_walk_bytes(batch, tiles, width) + (batch * tiles * width * 4 + 15) / 16 * 16);
 }
 
 int mesa_recurrence_backward(const void* x, const void* r, const void* i, const float* theta, float decay,
@@ -248,8 +245,8 @@ int mesa_recurrence_backward(const void* x, const void* r, const void* i, const 
     char* ws = static_cast<char*>(workspace);
     const mesa::RecurrenceGradArgs a{batch, seq_len, width, stride, grad_stride, dtype, grad_dtype, x, r, i, theta,
                                      decay, reset, states, dy, dfinal, dx, dr, di, dtheta, dh0, int(tiles),
-                                     reinterpret_cast<float2*>(ws),
-                                     reinterpret_cast<float*>(ws + span_bytes(batch, tiles, width))};
+                                     reinterpret_cast<uint64_t*>(ws),
+                                     reinterpret_cast<float*>(ws + mesa::recurrence_walk_bytes(batch, tiles, width))};
     return status_of(mesa::launch_recurrence_backward(a, static_cast<hipStream_t>(stream)), stream);
 }
 

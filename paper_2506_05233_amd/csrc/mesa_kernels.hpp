@@ -223,9 +223,10 @@ struct RecurrenceArgs {
     uint8_t* kept_r;
     uint8_t* kept_i;
     int tiles;                // recurrence_tiles(seq_len)
-    float2* spans;            // [batch, tiles, width]
+    uint64_t* words;          // recurrence_walk_bytes(batch, tiles, width), 16-byte aligned
 };
 int64_t recurrence_tiles(int64_t seq_len);
+int64_t recurrence_walk_bytes(int64_t batch, int64_t tiles, int64_t width);
 hipError_t launch_recurrence(const RecurrenceArgs& a, hipStream_t stream);
 hipError_t launch_recurrence_step(const RecurrenceArgs& a, float* state_out, hipStream_t stream);
 
@@ -247,7 +248,7 @@ struct RecurrenceGradArgs {
     float* dtheta;            // [width]
     float* dh0;               // [batch, width] or null
     int tiles;                // ceil(seq_len / kRecurrenceBlock)
-    float2* spans;            // [batch, tiles, width]
+    uint64_t* words;          // recurrence_walk_bytes(batch, tiles, width), 16-byte aligned
     float* partial;           // [batch, tiles, width]
 };
 hipError_t launch_recurrence_backward(const RecurrenceGradArgs& a, hipStream_t stream);

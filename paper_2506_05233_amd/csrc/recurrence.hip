@@ -18,11 +18,11 @@
 // a lane holds kSub consecutive tokens of four channels in registers, a row of 16 lanes a
 // token's 64 channels (128 bytes of bf16), a workgroup 32 such runs in time.  The runs'
 // (A, B) are joined inside a wave by row swaps, across waves in LDS, across workgroups
-// through the workspace: a first kernel writes every tile's (A, B), a second folds those
-// before it and walks its tokens from the state that enters them.  A reset inside a span
-// is kept as the sign of A (A is never negative otherwise), since 0 times a state that is
-// not finite would not forget it.  All of it is fp32 and in a fixed order.
+// through the workspace (below), so every input is read once.  A reset inside a span is
+// kept as the sign of A (A is never negative otherwise), since 0 times a state that is not
+// finite would not forget it.  All of it is fp32 and in a fixed order.
 #include <algorithm>
+#include <type_traits>
 
 #include "mesa_kernels.hpp"
 #include "mesa_lanes.hpp"
@@ -122,6 +122,133 @@ __device__ __forceinline__ Span terms(float x, float r, float i, float rate, boo
     return {a, m * in};
 }
 
+// ---------------------------------------------------------------- the walk over tiles
+// A tile's workgroup needs the state that enters it: the spans of the tiles before it,
+// applied one after the other.  Tiles are taken in groups of kJoin: a tile publishes its span
+// as soon as it knows it, without waiting for anything; the last tile of a group publishes
+// the state that leaves the group instead, once it has it.  A tile reads the state that
+// entered its group and the spans of the (at most kJoin - 1) tiles of the group before it.
+//
+// A workgroup takes its tile by drawing a ticket when it starts, and waits only for tiles of
+// smaller tickets; those are held by workgroups that run already, and the smallest ticket
+// not yet finished waits for nothing, so every wait ends whatever the order and the number
+// of workgroups that fit the GPU.  A span and its "published" mark are one 8-byte word
+// written and read with single relaxed accesses of agent scope, so no other memory has to be
+// ordered.  The words start as kUnset, written by a fill kernel ahead on the stream.
+constexpr int kJoin = 8;
+constexpr uint64_t kUnset = ~uint64_t(0);
+constexpr int kTicketWords = 2;   // the ticket counter's 16 bytes, ahead of the spans
+
+__device__ __forceinline__ void publish(uint64_t* at, Span s)
+{
+    uint64_t w = uint64_t(__float_as_uint(s.A)) | (uint64_t(__float_as_uint(s.B)) << 32);
+    if (w == kUnset) w = 0xFFFFFFFF7FC00000ull;   // two NaNs with those very bits
+    __hip_atomic_store(at, w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// The word at `at` of every lane that wants one, once all of them are published.
+__device__ __forceinline__ Span await(const uint64_t* at, bool wanted)
+{
+    uint64_t w = 0;
+    for (;;) {
+        if (wanted) w = __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (!__any(wanted && w == kUnset)) break;
+        __builtin_amdgcn_s_sleep(2);
+    }
+    return {__uint_as_float(uint32_t(w)), __uint_as_float(uint32_t(w >> 32))};
+}
+
+__global__ __launch_bounds__(256) void recurrence_fill_kernel(ulonglong2* words, int64_t n)
+{
+    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < n; i += int64_t(gridDim.x) * 256) words[i] = make_ulonglong2(kUnset, kUnset);
+}
+
+// Shared memory of a walk: the spans of a workgroup's waves, what comes before them, and the
+// state entering every wave.
+template <int Waves>
+struct WalkShared {
+    float2 span[Waves][kCh];
+    float2 before[kJoin][kCh];
+    union {
+        float enter[Waves][kCh];
+        int ticket;              // read by all before the first barrier of the walk
+    };
+};
+
+// The workgroup's place in the call: the walk's tiles in order (the first walked first),
+// slower than the slabs of channels and the sequences, so that a tile's predecessors
+// started long before it where there are many.
+struct Place {
+    int64_t b;
+    int slab, step;
+};
+template <int Waves>
+__device__ __forceinline__ Place place_of(uint64_t* words, bool many, int64_t batch, int slabs, WalkShared<Waves>& sh)
+{
+    uint32_t id = blockIdx.x;
+    if (many) {
+        if (threadIdx.x == 0)
+            sh.ticket = int(__hip_atomic_fetch_add(reinterpret_cast<uint32_t*>(words), 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1u);
+        __syncthreads();
+        id = uint32_t(__builtin_amdgcn_readfirstlane(sh.ticket));
+    }
+    const uint32_t rows = uint32_t(batch) * uint32_t(slabs), step = id / rows, row = id - step * rows;
+    return {int64_t(row / uint32_t(slabs)), int(row % uint32_t(slabs)), int(step)};
+}
+
+// From the waves' spans (in the order of the walk, written by their first lanes and made
+// visible by a barrier) the state entering each of them, in sh.enter after the barrier at
+// the end.  `step` is the tile's place in the walk, `first` the state ahead of the whole walk.
+template <bool Reset, int Waves>
+__device__ __forceinline__ void walk(WalkShared<Waves>& sh, uint64_t* words, int64_t batch, int64_t b, int step, int steps,
+                                     int64_t width, int slab, const float* first)
+{
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int64_t ch = int64_t(slab) * kCh + lane;
+    const bool mine = ch < width;
+    const int group = step / kJoin, at = step % kJoin;
+    const int groups = steps / kJoin;
+    uint64_t* spans = words + kTicketWords + b * steps * width + ch;
+    uint64_t* leaves = words + kTicketWords + batch * steps * width + b * groups * width + ch;
+    if (wave == 0 && at != kJoin - 1 && step + 1 < steps) {
+        Span s = nothing();
+#pragma unroll
+        for (int w = 0; w < Waves; ++w) s = join<Reset>(s, {sh.span[w][lane].x, sh.span[w][lane].y});
+        if (mine) publish(spans + int64_t(step) * width, s);
+    }
+    // entry 0 is the state entering the group, entry e the span of the group's tile e - 1
+    for (int e = wave; e <= at; e += Waves) {
+        Span s;
+        if (e > 0)
+            s = await(spans + int64_t(group * kJoin + e - 1) * width, mine);
+        else if (group > 0)
+            s = await(leaves + int64_t(group - 1) * width, mine);
+        else
+            s = {-0.0f, first != nullptr && mine ? first[b * width + ch] : 0.0f};
+        sh.before[e][lane] = make_float2(s.A, s.B);
+    }
+    __syncthreads();
+    if (wave == 0) {
+        float h = sh.before[0][lane].y;
+        for (int e = 1; e <= at; ++e) h = apply<Reset>({sh.before[e][lane].x, sh.before[e][lane].y}, h);
+#pragma unroll
+        for (int w = 0; w < Waves; ++w) {
+            sh.enter[w][lane] = h;
+            h = apply<Reset>({sh.span[w][lane].x, sh.span[w][lane].y}, h);
+        }
+        if (mine && at == kJoin - 1 && step + 1 < steps) publish(leaves + int64_t(group) * width, {-0.0f, h});
+    }
+    __syncthreads();
+}
+
+// Makes a value opaque at this point: what is derived from it is derived here again, instead
+// of being kept in registers from an earlier place.
+__device__ __forceinline__ void pin(float& x) { asm volatile("" : "+v"(x)); }
+__device__ __forceinline__ void pin(uint32_t& x) { asm volatile("" : "+v"(x)); }
+__device__ __forceinline__ void pin(uint2& r) { pin(r.x), pin(r.y); }
+__device__ __forceinline__ void pin(float4& r) { pin(r.x), pin(r.y), pin(r.z), pin(r.w); }
+__device__ __forceinline__ void pin(Q8Raw& r) { pin(r.codes), pin(r.byte); }
+
 // ---------------------------------------------------------------- forward
 constexpr int kFwdSub = 8;                         // tokens of a lane
 constexpr int kFwdThreads = 512;
@@ -129,154 +256,149 @@ constexpr int kFwdWaves = kFwdThreads / kWave;
 constexpr int kFwdTile = kFwdWaves * 4 * kFwdSub;  // tokens of a workgroup
 static_assert(kFwdTile == 2 * kBlock && kBlock % kFwdSub == 0, "a state block starts at a lane's first token");
 
-// Folds spans [B, n_tiles, width] of tiles lo .. hi - 1, in that order (Back: reversed),
-// onto the state h of four channels.
-template <bool Reset, bool Vec, bool Back>
-__device__ __forceinline__ void fold_tiles(const float2* spans, int64_t width, int lo, int hi, int n, float (&h)[4])
+// A tile's rows are read and written at an address that the whole wave shares plus an offset
+// of the lane's own, in elements: 32 bits of it on the vector path, whose rows are at most
+// kNearStride apart, 64 otherwise.
+constexpr int64_t kNearStride = int64_t(1) << 22;
+template <bool Vec>
+using Offset = std::conditional_t<Vec, uint32_t, int64_t>;
+
+template <typename T, bool Vec>
+__device__ __forceinline__ typename Lane4<T>::Raw load_row(const void* base, int64_t row, Offset<Vec> off, int n)
 {
-    for (int t = 0; t < hi - lo; ++t) {
-        const float2* p = spans + int64_t(Back ? hi - 1 - t : lo + t) * width;
-#pragma unroll
-        for (int v = 0; v < 4; ++v)
-            if (v < n) {
-                const float2 s = p[v];
-                h[v] = apply<Reset>({s.x, s.y}, h[v]);
-            }
-    }
+    return Lane4<T>::template load<Vec>(static_cast<const T*>(base) + row, off, n);
 }
 
-// Spans: the tiles' (A, B) only, into a.spans.  Otherwise the outputs.
-template <typename T, bool Vec, bool Reset, bool Spans>
-__global__ __launch_bounds__(kFwdThreads) void recurrence_kernel(RecurrenceArgs a)
+// Eight lanes hold a group of 32 channels: its exponent byte and this lane's four codes.
+__device__ __forceinline__ uint32_t pack_group(const float (&x)[4], uint32_t& byte)
 {
-    __shared__ float4 wave_A[kFwdWaves][kAcross], wave_B[kFwdWaves][kAcross];
-    const int slabs = int((a.width + kCh - 1) / kCh);
-    const int slab = blockIdx.x % slabs;
-    const int tile = (blockIdx.x / slabs) % a.tiles;
-    const int64_t b = blockIdx.x / slabs / a.tiles;
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    const int row = lane / kAcross, col = lane % kAcross;
-    const int64_t ch = int64_t(slab) * kCh + col * 4;
-    const int n = int(max<int64_t>(0, min<int64_t>(4, a.width - ch)));   // channels of this lane
-    const int64_t t0 = int64_t(tile) * kFwdTile + (wave * 4 + row) * kFwdSub;
-    const int64_t at0 = (b * a.seq_len + t0) * a.stride + ch;
+    uint32_t top = max(max(abs_bits(x[0]), abs_bits(x[1])), max(abs_bits(x[2]), abs_bits(x[3])));
+    top = max(top, uint32_t(dpp_i32<kDppQuadSwap1>(int(top), int(top))));
+    top = max(top, uint32_t(dpp_i32<kDppQuadSwap2>(int(top), int(top))));
+    top = max(top, uint32_t(dpp_i32<kDppRowHalfMirror>(int(top), int(top))));
+    byte = group_exponent(__uint_as_float(top));
+    const float inv = group_inverse(byte), most = group_most(byte);
+    const int c[4] = {group_code(x[0], inv, most), group_code(x[1], inv, most), group_code(x[2], inv, most), group_code(x[3], inv, most)};
+    return pack_codes(c);
+}
 
-    // tokens past the end leave the state alone and are neither read nor written
+// Whether a lane of the wave has a reset at its token j: few waves do, and the others'
+// arithmetic is that without resets.
+template <bool Reset>
+__device__ __forceinline__ bool any_hard(bool hard)
+{
+    return Reset && __any(hard);
+}
+
+template <typename T, bool Vec, bool Reset, bool Kept>
+__global__ __launch_bounds__(kFwdThreads, 4) void recurrence_kernel(RecurrenceArgs a)
+{
+    __shared__ WalkShared<kFwdWaves> sh;
+    const int slabs = int((a.width + kCh - 1) / kCh);
+    const Place at = place_of(a.words, a.tiles > 1, a.batch, slabs, sh);
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int row = lane / kAcross, col = lane % kAcross;
+    const int64_t ch0 = int64_t(at.slab) * kCh, ch = ch0 + col * 4;
+    const int n = int(max<int64_t>(0, min<int64_t>(4, a.width - ch)));   // channels of this lane
+    const int64_t w0 = int64_t(at.step) * kFwdTile + wave * 4 * kFwdSub;  // the wave's first token
+    const int64_t token0 = at.b * a.seq_len + w0;
+    const int64_t left = a.seq_len - w0 - row * kFwdSub;                 // tokens there are from the lane's first on
+
+    // tokens past the end are neither read nor written; they come after all others, so the
+    // state that they would leave is used by nobody
     typename Lane4<T>::Raw rx[kFwdSub], rr[kFwdSub], ri[kFwdSub];
     bool hard[kFwdSub] = {};
+    const Offset<Vec> off = Offset<Vec>(row * kFwdSub) * Offset<Vec>(a.stride) + col * 4;
 #pragma unroll
     for (int j = 0; j < kFwdSub; ++j) {
-        const int m = t0 + j < a.seq_len ? n : 0;
-        rx[j] = Lane4<T>::template load<Vec>(a.x, at0 + j * a.stride, m);
-        rr[j] = Lane4<T>::template load<Vec>(a.r, at0 + j * a.stride, m);
-        ri[j] = Lane4<T>::template load<Vec>(a.i, at0 + j * a.stride, m);
-        if (Reset) hard[j] = t0 + j < a.seq_len && a.reset[b * a.seq_len + t0 + j] != 0;
+        const int m = j < left ? n : 0;
+        const int64_t at_row = (token0 + j) * a.stride + ch0;
+        rx[j] = load_row<T, Vec>(a.x, at_row, off, m);
+        rr[j] = load_row<T, Vec>(a.r, at_row, off, m);
+        ri[j] = load_row<T, Vec>(a.i, at_row, off, m);
+        if (Reset) hard[j] = j < left && a.reset[token0 + row * kFwdSub + j] != 0;
     }
     const Rates k = rates_of(a.theta, a.decay, ch, n);
-    Span e[kFwdSub][4], own[4];
+    if constexpr (Kept) {
+        uint8_t* const kept[3] = {a.kept_x, a.kept_r, a.kept_i};
+        const int64_t bytes_at = checkpoint_exponents_at(a.batch * a.seq_len, a.width), groups = (a.width + kGroup - 1) / kGroup;
+#pragma unroll
+        for (int j = 0; j < kFwdSub; ++j) {
+            const int64_t token = token0 + row * kFwdSub + j;
+#pragma unroll
+            for (int q = 0; q < 3; ++q) {
+                float x[4];
+                Lane4<T>::widen(q == 0 ? rx[j] : q == 1 ? rr[j] : ri[j], x);
+                uint32_t byte;
+                const uint32_t codes = pack_group(x, byte);
+                if (j < left && n > 0) {
+                    uint8_t* out = kept[q] + token * a.width + ch;
+                    if constexpr (Vec) {
+                        *reinterpret_cast<uint32_t*>(out) = codes;
+                    } else {
+#pragma unroll
+                        for (int v = 0; v < 4; ++v)
+                            if (v < n) out[v] = uint8_t(codes >> (8 * v));
+                    }
+                    if (col % 8 == 0) kept[q][bytes_at + token * groups + ch / kGroup] = uint8_t(byte);
+                }
+            }
+        }
+    }
+    Span e[kFwdSub][4], own[4], before[4], all[4];
 #pragma unroll
     for (int v = 0; v < 4; ++v) own[v] = nothing();
 #pragma unroll
     for (int j = 0; j < kFwdSub; ++j) {
         float x[4], r[4], i[4];
+        pin(rx[j]), pin(rr[j]), pin(ri[j]);
         Lane4<T>::widen(rx[j], x);
         Lane4<T>::widen(rr[j], r);
         Lane4<T>::widen(ri[j], i);
-        const bool there = t0 + j < a.seq_len;
 #pragma unroll
-        for (int v = 0; v < 4; ++v) {
-            e[j][v] = there ? terms<Reset>(x[v], r[v], i[v], k.v[v], hard[j]) : nothing();
-            own[v] = join<Reset>(own[v], e[j][v]);
+        for (int v = 0; v < 4; ++v) e[j][v] = terms<false>(x[v], r[v], i[v], k.v[v], false);
+        if (any_hard<Reset>(hard[j])) {
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                if (hard[j]) e[j][v] = terms<true>(x[v], r[v], i[v], k.v[v], true);
+                own[v] = join<true>(own[v], e[j][v]);
+            }
+        } else {
+#pragma unroll
+            for (int v = 0; v < 4; ++v) own[v] = {own[v].A * e[j][v].A, apply<false>(e[j][v], own[v].B)};
         }
     }
-    Span before[4], all[4];
 #pragma unroll
     for (int v = 0; v < 4; ++v) join_rows<Reset, false>(own[v], row, before[v], all[v]);
     if (row == 0) {
-        wave_A[wave][col] = make_float4(all[0].A, all[1].A, all[2].A, all[3].A);
-        wave_B[wave][col] = make_float4(all[0].B, all[1].B, all[2].B, all[3].B);
+        float4* out = reinterpret_cast<float4*>(&sh.span[wave][col * 4]);
+        out[0] = make_float4(all[0].A, all[0].B, all[1].A, all[1].B);
+        out[1] = make_float4(all[2].A, all[2].B, all[3].A, all[3].B);
     }
     __syncthreads();
-    if constexpr (Spans) {
-        if (wave == 0 && row == 0 && n > 0) {
-            Span s[4];
+    walk<Reset>(sh, a.words, a.batch, at.b, at.step, a.tiles, a.width, at.slab, a.h0);
+    const float4 enter = *reinterpret_cast<const float4*>(&sh.enter[wave][col * 4]);
+    float h[4] = {enter.x, enter.y, enter.z, enter.w};
 #pragma unroll
-            for (int v = 0; v < 4; ++v) s[v] = nothing();
-            for (int w = 0; w < kFwdWaves; ++w) {
-                const float4 A = wave_A[w][col], B = wave_B[w][col];
-                const Span t[4] = {{A.x, B.x}, {A.y, B.y}, {A.z, B.z}, {A.w, B.w}};
+    for (int v = 0; v < 4; ++v) h[v] = apply<Reset>(before[v], h[v]);
+    const int64_t t0 = w0 + row * kFwdSub;
+    if (a.states != nullptr && t0 % kBlock == 0 && left > 0)
+        Lane4<float>::store<false>(a.states, (at.b * ((a.seq_len + kBlock - 1) / kBlock) + t0 / kBlock) * a.width + ch, n, h);
+    T* y = static_cast<T*>(a.y) + token0 * a.width + ch0;
+    const Offset<Vec> y_off = Offset<Vec>(row * kFwdSub) * Offset<Vec>(a.width) + col * 4;
+    float* final_h = a.final_h != nullptr ? a.final_h + at.b * a.width + ch : nullptr;
 #pragma unroll
-                for (int v = 0; v < 4; ++v) s[v] = join<Reset>(s[v], t[v]);
-            }
-            float2* out = a.spans + (b * a.tiles + tile) * a.width + ch;
+    for (int j = 0; j < kFwdSub; ++j) {
+        if (any_hard<Reset>(hard[j])) {
 #pragma unroll
-            for (int v = 0; v < 4; ++v)
-                if (v < n) out[v] = make_float2(s[v].A, s[v].B);
+            for (int v = 0; v < 4; ++v) h[v] = apply<true>(e[j][v], h[v]);
+        } else {
+#pragma unroll
+            for (int v = 0; v < 4; ++v) h[v] = apply<false>(e[j][v], h[v]);
         }
-    } else {
-        float h[4];
-#pragma unroll
-        for (int v = 0; v < 4; ++v) h[v] = a.h0 != nullptr && v < n ? a.h0[b * a.width + ch + v] : 0.0f;
-        fold_tiles<Reset, Vec, false>(a.spans + b * a.tiles * a.width + ch, a.width, 0, tile, n, h);
-        for (int w = 0; w < wave; ++w) {
-            const float4 A = wave_A[w][col], B = wave_B[w][col];
-            h[0] = apply<Reset>({A.x, B.x}, h[0]);
-            h[1] = apply<Reset>({A.y, B.y}, h[1]);
-            h[2] = apply<Reset>({A.z, B.z}, h[2]);
-            h[3] = apply<Reset>({A.w, B.w}, h[3]);
-        }
-#pragma unroll
-        for (int v = 0; v < 4; ++v) h[v] = apply<Reset>(before[v], h[v]);
-        if (a.states != nullptr && t0 % kBlock == 0 && t0 < a.seq_len)
-            Lane4<float>::store<false>(a.states, (b * ((a.seq_len + kBlock - 1) / kBlock) + t0 / kBlock) * a.width + ch, n, h);
-        const int64_t y0 = (b * a.seq_len + t0) * a.width + ch;
-#pragma unroll
-        for (int j = 0; j < kFwdSub; ++j) {
-#pragma unroll
-            for (int v = 0; v < 4; ++v) h[v] = apply<Reset>(e[j][v], h[v]);
-            if (t0 + j < a.seq_len) {
-                Lane4<T>::template store<Vec>(a.y, y0 + j * a.width, n, h);
-                if (t0 + j == a.seq_len - 1 && a.final_h != nullptr) Lane4<float>::store<false>(a.final_h, b * a.width + ch, n, h);
-            }
-        }
-        if (a.kept_x != nullptr) {
-            // the checkpoint of this tile's inputs: eight lanes are a group of 32 channels
-            const int64_t groups = (a.width + kGroup - 1) / kGroup;
-            uint8_t* const kept[3] = {a.kept_x, a.kept_r, a.kept_i};
-            const int64_t bytes_at = checkpoint_exponents_at(a.batch * a.seq_len, a.width);
-#pragma unroll
-            for (int j = 0; j < kFwdSub; ++j) {
-                float val[3][4];
-                Lane4<T>::widen(rx[j], val[0]);
-                Lane4<T>::widen(rr[j], val[1]);
-                Lane4<T>::widen(ri[j], val[2]);
-                const int64_t token = b * a.seq_len + t0 + j;
-#pragma unroll
-                for (int q = 0; q < 3; ++q) {
-                    uint32_t top = 0;
-#pragma unroll
-                    for (int v = 0; v < 4; ++v) top = max(top, abs_bits(val[q][v]));
-                    top = max(top, uint32_t(dpp_i32<kDppQuadSwap1>(int(top), int(top))));
-                    top = max(top, uint32_t(dpp_i32<kDppQuadSwap2>(int(top), int(top))));
-                    top = max(top, uint32_t(dpp_i32<kDppRowHalfMirror>(int(top), int(top))));
-                    const uint32_t byte = group_exponent(__uint_as_float(top));
-                    const float inv = group_inverse(byte), most = group_most(byte);
-                    int c[4];
-#pragma unroll
-                    for (int v = 0; v < 4; ++v) c[v] = group_code(val[q][v], inv, most);
-                    if (t0 + j < a.seq_len && n > 0) {
-                        uint8_t* out = kept[q] + token * a.width + ch;
-                        if constexpr (Vec) {
-                            *reinterpret_cast<uint32_t*>(out) = pack_codes(c);
-                        } else {
-#pragma unroll
-                            for (int v = 0; v < 4; ++v)
-                                if (v < n) out[v] = uint8_t(c[v]);
-                        }
-                        if (col % 8 == 0) kept[q][bytes_at + token * groups + ch / kGroup] = uint8_t(byte);
-                    }
-                }
-            }
+        if (j < left) {
+            Lane4<T>::template store<Vec>(y + j * a.width, y_off, n, h);
+            if (j == left - 1 && final_h != nullptr) Lane4<float>::store<false>(final_h, 0, n, h);
         }
     }
 }
@@ -310,14 +432,15 @@ constexpr int kBwdWaves = kBwdThreads / kWave;
 constexpr int kBwdTile = kBwdWaves * 4 * kBwdSub;
 static_assert(kBwdTile == kBlock, "a tile of the backward pass starts at a kept state");
 
-// x, r or i of the backward pass: a tensor of T, or a checkpoint.
+// x, r or i of the backward pass: a tensor of T, or a checkpoint.  `token` is the wave's
+// token, `row` the lane's tokens from there.
 template <typename T>
 struct Source {
     using Raw = typename Lane4<T>::Raw;
     template <bool Vec>
-    __device__ static Raw load(const void* base, const RecurrenceGradArgs& a, int64_t token, int64_t ch, int n)
+    __device__ static Raw load(const void* base, const RecurrenceGradArgs& a, int64_t token, int row, int64_t ch0, int col, int n)
     {
-        return Lane4<T>::template load<Vec>(base, token * a.stride + ch, n);
+        return load_row<T, Vec>(base, token * a.stride + ch0, Offset<Vec>(row) * Offset<Vec>(a.stride) + col * 4, n);
     }
     __device__ static void widen(const Raw& r, float (&x)[4]) { Lane4<T>::widen(r, x); }
 };
@@ -325,209 +448,250 @@ template <>
 struct Source<q8_t> {
     using Raw = Q8Raw;
     template <bool Vec>
-    __device__ static Raw load(const void* base, const RecurrenceGradArgs& a, int64_t token, int64_t ch, int n)
+    __device__ static Raw load(const void* base, const RecurrenceGradArgs& a, int64_t token, int row, int64_t ch0, int col, int n)
     {
         if (n <= 0) return {0u, 0u};
-        const uint8_t* bytes = static_cast<const uint8_t*>(base) + checkpoint_exponents_at(a.batch * a.seq_len, a.width);
-        return {load_codes<Vec>(static_cast<const int8_t*>(base) + token * a.width + ch, n),
-                bytes[token * ((a.width + kGroup - 1) / kGroup) + ch / kGroup]};
+        const int64_t groups = (a.width + kGroup - 1) / kGroup;
+        const int8_t* codes = static_cast<const int8_t*>(base) + token * a.width + ch0;
+        const uint8_t* bytes = static_cast<const uint8_t*>(base) + checkpoint_exponents_at(a.batch * a.seq_len, a.width) + token * groups + ch0 / kGroup;
+        return {load_codes<Vec>(codes + Offset<Vec>(row) * Offset<Vec>(a.width) + col * 4, n), bytes[Offset<Vec>(row) * Offset<Vec>(groups) + col / 8]};
     }
     __device__ static void widen(const Raw& r, float (&x)[4]) { widen_q8(r.codes, group_scale(r.byte), x); }
 };
 
-// Spans: every tile's (A, B) of c -> A c + B, the walk from its last token to its first.
-template <typename T, typename Tg, bool Vec, bool Reset, bool Spans>
-__global__ __launch_bounds__(kBwdThreads) void recurrence_grad_kernel(RecurrenceGradArgs a)
+// sigma(x) and 1 - sigma(x) in one register, each to its own accuracy: the smaller of the two,
+// the second with its sign set.
+__device__ __forceinline__ float fold_gate(float x)
 {
-    __shared__ float4 fwd_A[kBwdWaves][kAcross], fwd_B[kBwdWaves][kAcross];
-    __shared__ float4 bwd_A[kBwdWaves][kAcross], bwd_B[kBwdWaves][kAcross];
+    const float e = __builtin_amdgcn_exp2f(-kLog2e * x);
+    const float s = __builtin_amdgcn_rcpf(1.0f + e);
+    return x > 0.0f ? -(e * s) : s;
+}
+__device__ __forceinline__ float gate_of(float f) { return signbit(f) ? 1.0f + f : f; }
+__device__ __forceinline__ float rest_of(float f) { return signbit(f) ? -f : 1.0f - f; }
+
+// What the walk back needs of an element, all that is kept of it in between.
+struct Kept {
+    float a, hp, m, s, i;   // hp: the state's input at first, then the state before the token; s, i folded gates
+};
+
+// Lean: 16-bit gradients of 8- or 16-bit inputs run two workgroups a compute unit, with 128
+// registers a lane, and keep m and the spans ahead of a lane's own in LDS.  With fp32 arrays one
+// workgroup of up to 256 registers is as fast as those would be with spills.
+template <typename T, typename Tg>
+constexpr bool kLean = sizeof(T) <= 2 && sizeof(Tg) == 2;
+
+template <bool Lean>
+struct BackwardShared {
+    WalkShared<kBwdWaves> walk;          // the walk back: its first wave is the workgroup's last
+    float2 span[kBwdWaves][kCh];         // the waves' spans on the way forward
+    float enter[kBwdWaves][kCh];
+};
+template <>
+struct BackwardShared<true> : BackwardShared<false> {
+    float4 m[kBwdSub][kBwdThreads];
+    float4 ahead[4][kBwdThreads];
+};
+
+__device__ __forceinline__ float4 to_float4(const float (&x)[4]) { return make_float4(x[0], x[1], x[2], x[3]); }
+__device__ __forceinline__ void from_float4(const float4& f, float (&x)[4]) { x[0] = f.x, x[1] = f.y, x[2] = f.z, x[3] = f.w; }
+
+template <typename T, typename Tg, bool Vec, bool Reset>
+__global__ __launch_bounds__(kBwdThreads, (kLean<T, Tg> ? 4 : 2)) void recurrence_grad_kernel(RecurrenceGradArgs a)
+{
+    constexpr bool Lean = kLean<T, Tg>;
+    __shared__ BackwardShared<Lean> sh;
     const int slabs = int((a.width + kCh - 1) / kCh);
-    const int slab = blockIdx.x % slabs;
-    const int tile = (blockIdx.x / slabs) % a.tiles;
-    const int64_t b = blockIdx.x / slabs / a.tiles;
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const Place at = place_of(a.words, a.tiles > 1, a.batch, slabs, sh.walk);
+    const int64_t tile = a.tiles - 1 - at.step;
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int row = lane / kAcross, col = lane % kAcross;
-    const int64_t ch = int64_t(slab) * kCh + col * 4;
+    const int64_t ch0 = int64_t(at.slab) * kCh, ch = ch0 + col * 4;
     const int n = int(max<int64_t>(0, min<int64_t>(4, a.width - ch)));
-    const int64_t t0 = int64_t(tile) * kBwdTile + (wave * 4 + row) * kBwdSub;
-    const int64_t token0 = b * a.seq_len + t0;
+    const int64_t w0 = tile * kBwdTile + wave * 4 * kBwdSub;
+    const int64_t token0 = at.b * a.seq_len + w0;
+    const int64_t left = a.seq_len - w0 - row * kBwdSub;
 
     typename Source<T>::Raw rx[kBwdSub], rr[kBwdSub], ri[kBwdSub];
     typename Lane4<Tg>::Raw rd[kBwdSub];
     bool hard[kBwdSub] = {};
+    const Offset<Vec> d_off = Offset<Vec>(row * kBwdSub) * Offset<Vec>(a.width) + col * 4;
 #pragma unroll
     for (int j = 0; j < kBwdSub; ++j) {
-        const int m = t0 + j < a.seq_len ? n : 0;
-        rr[j] = Source<T>::template load<Vec>(a.r, a, token0 + j, ch, m);
-        rd[j] = Lane4<Tg>::template load<Vec>(a.dy, (token0 + j) * a.width + ch, m);
-        if (!Spans) {
-            rx[j] = Source<T>::template load<Vec>(a.x, a, token0 + j, ch, m);
-            ri[j] = Source<T>::template load<Vec>(a.i, a, token0 + j, ch, m);
-        }
-        if (Reset) hard[j] = t0 + j < a.seq_len && a.reset[token0 + j] != 0;
+        const int m = j < left ? n : 0;
+        rr[j] = Source<T>::template load<Vec>(a.r, a, token0 + j, row * kBwdSub, ch0, col, m);
+        rx[j] = Source<T>::template load<Vec>(a.x, a, token0 + j, row * kBwdSub, ch0, col, m);
+        ri[j] = Source<T>::template load<Vec>(a.i, a, token0 + j, row * kBwdSub, ch0, col, m);
+        rd[j] = load_row<Tg, Vec>(a.dy, (token0 + j) * a.width + ch0, d_off, m);
+        if (Reset) hard[j] = j < left && a.reset[token0 + row * kBwdSub + j] != 0;
     }
     const Rates k = rates_of(a.theta, a.decay, ch, n);
-    float ea[kBwdSub][4];
-    Span fwd[4], bwd[4];
+    // the lane's tokens: their factors, and what they do together to the state and, on the way
+    // back, to its gradient
+    Kept e[kBwdSub][4];
+    Span fwd[4], bwd[4], all[4];
 #pragma unroll
     for (int v = 0; v < 4; ++v) fwd[v] = bwd[v] = nothing();
 #pragma unroll
     for (int j = 0; j < kBwdSub; ++j) {
-        float x[4], r[4], i[4];
+        float x[4], r[4], i[4], m[4];
+        pin(rx[j]), pin(rr[j]), pin(ri[j]);
+        Source<T>::widen(rx[j], x);
         Source<T>::widen(rr[j], r);
-        if (!Spans) {
-            Source<T>::widen(rx[j], x);
-            Source<T>::widen(ri[j], i);
-        }
-        const bool there = t0 + j < a.seq_len;
+        Source<T>::widen(ri[j], i);
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
-            if constexpr (Spans) {
-                const float z = k.v[v] * sigmoid_fast(r[v]);
-                ea[j][v] = !there ? 1.0f : Reset && hard[j] ? -0.0f : __builtin_amdgcn_exp2f(z);
-            } else {
-                const Span s = there ? terms<Reset>(x[v], r[v], i[v], k.v[v], hard[j]) : nothing();
-                ea[j][v] = s.A;
-                fwd[v] = join<Reset>(fwd[v], s);
-            }
+            Kept& q = e[j][v];
+            q.s = fold_gate(r[v]);
+            q.i = fold_gate(i[v]);
+            const float z = k.v[v] * gate_of(q.s);
+            q.a = __builtin_amdgcn_exp2f(z);
+            m[v] = __builtin_amdgcn_sqrtf(one_minus_square(z, q.a));
+        }
+        const bool cut = any_hard<Reset>(hard[j]);
+        if (cut && hard[j]) {
+#pragma unroll
+            for (int v = 0; v < 4; ++v) e[j][v].a = -0.0f, m[v] = 1.0f;
+        }
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            Kept& q = e[j][v];
+            q.hp = m[v] * gate_of(q.i) * x[v];
+            if (!Lean) q.m = m[v];
+            pin(q.s), pin(q.i);
+        }
+        if constexpr (Lean) sh.m[j][threadIdx.x] = to_float4(m);
+        if (cut) {
+#pragma unroll
+            for (int v = 0; v < 4; ++v) fwd[v] = join<true>(fwd[v], {e[j][v].a, e[j][v].hp});
+        } else {
+#pragma unroll
+            for (int v = 0; v < 4; ++v) fwd[v] = {fwd[v].A * e[j][v].a, fmaf(e[j][v].a, fwd[v].B, e[j][v].hp)};
         }
     }
 #pragma unroll
     for (int j = kBwdSub - 1; j >= 0; --j) {
         float d[4];
+        pin(rd[j]);
         Lane4<Tg>::widen(rd[j], d);
+        if (j < left) {   // a token past the end leaves the gradient alone
 #pragma unroll
-        for (int v = 0; v < 4; ++v) {
-            // c -> a (dy + c); a reset's c is 0 whatever comes after
-            const bool cut = Reset && signbit(ea[j][v]);
-            bwd[v] = cut ? Span{-0.0f, 0.0f} : Span{bwd[v].A * ea[j][v], ea[j][v] * (bwd[v].B + d[v])};
-        }
-    }
-    Span fbefore[4], fall[4], bbefore[4], ball[4];
+            for (int v = 0; v < 4; ++v) bwd[v] = {bwd[v].A * e[j][v].a, e[j][v].a * (bwd[v].B + d[v])};   // c -> a (dy + c)
+            if (Reset && hard[j]) {
 #pragma unroll
-    for (int v = 0; v < 4; ++v) {
-        if (!Spans) join_rows<Reset, false>(fwd[v], row, fbefore[v], fall[v]);
-        join_rows<Reset, true>(bwd[v], row, bbefore[v], ball[v]);
-    }
-    if (row == 0) {
-        if (!Spans) {
-            fwd_A[wave][col] = make_float4(fall[0].A, fall[1].A, fall[2].A, fall[3].A);
-            fwd_B[wave][col] = make_float4(fall[0].B, fall[1].B, fall[2].B, fall[3].B);
-        }
-        bwd_A[wave][col] = make_float4(ball[0].A, ball[1].A, ball[2].A, ball[3].A);
-        bwd_B[wave][col] = make_float4(ball[0].B, ball[1].B, ball[2].B, ball[3].B);
-    }
-    __syncthreads();
-    if constexpr (Spans) {
-        if (wave == 0 && row == 0 && n > 0) {
-            Span s[4];
-#pragma unroll
-            for (int v = 0; v < 4; ++v) s[v] = nothing();
-            for (int w = kBwdWaves - 1; w >= 0; --w) {
-                const float4 A = bwd_A[w][col], B = bwd_B[w][col];
-                const Span t[4] = {{A.x, B.x}, {A.y, B.y}, {A.z, B.z}, {A.w, B.w}};
-#pragma unroll
-                for (int v = 0; v < 4; ++v) s[v] = join<Reset>(s[v], t[v]);
+                for (int v = 0; v < 4; ++v) bwd[v] = {-0.0f, 0.0f};   // a reset's c is 0 whatever comes after
             }
-            float2* out = a.spans + (b * a.tiles + tile) * a.width + ch;
-#pragma unroll
-            for (int v = 0; v < 4; ++v)
-                if (v < n) out[v] = make_float2(s[v].A, s[v].B);
         }
-        return;
     }
-    float h[4], c[4];
+    Span fahead[4], bahead[4];
+#pragma unroll
+    for (int v = 0; v < 4; ++v) join_rows<Reset, false>(fwd[v], row, fahead[v], all[v]);
+    if (row == 0) {
+        float4* out = reinterpret_cast<float4*>(&sh.span[wave][col * 4]);
+        out[0] = make_float4(all[0].A, all[0].B, all[1].A, all[1].B);
+        out[1] = make_float4(all[2].A, all[2].B, all[3].A, all[3].B);
+    }
+    if constexpr (Lean) {
+        sh.ahead[0][threadIdx.x] = make_float4(fahead[0].A, fahead[1].A, fahead[2].A, fahead[3].A);
+        sh.ahead[1][threadIdx.x] = make_float4(fahead[0].B, fahead[1].B, fahead[2].B, fahead[3].B);
+    }
+#pragma unroll
+    for (int v = 0; v < 4; ++v) join_rows<Reset, true>(bwd[v], row, bahead[v], all[v]);
+    if (row == 0) {
+        float4* out = reinterpret_cast<float4*>(&sh.walk.span[kBwdWaves - 1 - wave][col * 4]);
+        out[0] = make_float4(all[0].A, all[0].B, all[1].A, all[1].B);
+        out[1] = make_float4(all[2].A, all[2].B, all[3].A, all[3].B);
+    }
+    if constexpr (Lean) {
+        sh.ahead[2][threadIdx.x] = make_float4(bahead[0].A, bahead[1].A, bahead[2].A, bahead[3].A);
+        sh.ahead[3][threadIdx.x] = make_float4(bahead[0].B, bahead[1].B, bahead[2].B, bahead[3].B);
+    }
+    const int64_t my = ch0 + lane;
+    float state = 0.0f;      // wave 1: the state entering the tile, a channel a lane
+    if (wave == 1 && my < a.width) state = a.states[(at.b * a.tiles + tile) * a.width + my];
+    __syncthreads();
+    if (wave == 1) {
+#pragma unroll
+        for (int w = 0; w < kBwdWaves; ++w) {
+            sh.enter[w][lane] = state;
+            state = apply<Reset>({sh.span[w][lane].x, sh.span[w][lane].y}, state);
+        }
+    }
+    walk<Reset>(sh.walk, a.words, a.batch, at.b, at.step, a.tiles, a.width, at.slab, a.dfinal);
+    float h[4], c[4], dth[4] = {0.f, 0.f, 0.f, 0.f};
+    from_float4(*reinterpret_cast<const float4*>(&sh.enter[wave][col * 4]), h);
+    from_float4(*reinterpret_cast<const float4*>(&sh.walk.enter[kBwdWaves - 1 - wave][col * 4]), c);
+    if constexpr (Lean) {
+        float f[4][4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) from_float4(sh.ahead[q][threadIdx.x], f[q]);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) fahead[v] = {f[0][v], f[1][v]}, bahead[v] = {f[2][v], f[3][v]};
+    }
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
-        h[v] = v < n ? a.states[(b * a.tiles + tile) * a.width + ch + v] : 0.0f;
-        c[v] = v < n && a.dfinal != nullptr ? a.dfinal[b * a.width + ch + v] : 0.0f;
-    }
-    fold_tiles<Reset, Vec, true>(a.spans + b * a.tiles * a.width + ch, a.width, tile + 1, a.tiles, n, c);
-    for (int w = 0; w < wave; ++w) {
-        const float4 A = fwd_A[w][col], B = fwd_B[w][col];
-        h[0] = apply<Reset>({A.x, B.x}, h[0]);
-        h[1] = apply<Reset>({A.y, B.y}, h[1]);
-        h[2] = apply<Reset>({A.z, B.z}, h[2]);
-        h[3] = apply<Reset>({A.w, B.w}, h[3]);
-    }
-    for (int w = kBwdWaves - 1; w > wave; --w) {
-        const float4 A = bwd_A[w][col], B = bwd_B[w][col];
-        c[0] = apply<Reset>({A.x, B.x}, c[0]);
-        c[1] = apply<Reset>({A.y, B.y}, c[1]);
-        c[2] = apply<Reset>({A.z, B.z}, c[2]);
-        c[3] = apply<Reset>({A.w, B.w}, c[3]);
-    }
-    // the states before each of the lane's tokens, then the walk back
-    float hp[kBwdSub][4];
-#pragma unroll
-    for (int v = 0; v < 4; ++v) {
-        h[v] = apply<Reset>(fbefore[v], h[v]);
-        c[v] = apply<Reset>(bbefore[v], c[v]);
+        h[v] = apply<Reset>(fahead[v], h[v]);
+        c[v] = apply<Reset>(bahead[v], c[v]);
     }
 #pragma unroll
     for (int j = 0; j < kBwdSub; ++j) {
-        float x[4], r[4], i[4];
-        Source<T>::widen(rx[j], x);
-        Source<T>::widen(rr[j], r);
-        Source<T>::widen(ri[j], i);
+        const bool cut = any_hard<Reset>(hard[j]);
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
-            hp[j][v] = h[v];
-            h[v] = apply<Reset>(terms<Reset>(x[v], r[v], i[v], k.v[v], hard[j]), h[v]);
+            const Span in = {e[j][v].a, e[j][v].hp};
+            e[j][v].hp = h[v];
+            h[v] = cut ? apply<true>(in, h[v]) : apply<false>(in, h[v]);
         }
     }
-    float dth[4] = {0.f, 0.f, 0.f, 0.f};
+    const int64_t g0 = token0 * a.grad_stride + ch0;
+    const Offset<Vec> g_off = Offset<Vec>(row * kBwdSub) * Offset<Vec>(a.grad_stride) + col * 4;
+    Tg* const dx = static_cast<Tg*>(a.dx) + g0;
+    Tg* const dr = static_cast<Tg*>(a.dr) + g0;
+    Tg* const di = static_cast<Tg*>(a.di) + g0;
 #pragma unroll
     for (int j = kBwdSub - 1; j >= 0; --j) {
-        float x[4], r[4], i[4], d[4], gx[4], gr[4], gi[4];
+        if (j >= left) continue;
+        float x[4], d[4], m[4], gx[4], gr[4], gi[4];
+        pin(rx[j]), pin(rd[j]);
         Source<T>::widen(rx[j], x);
-        Source<T>::widen(rr[j], r);
-        Source<T>::widen(ri[j], i);
         Lane4<Tg>::widen(rd[j], d);
-        const bool there = t0 + j < a.seq_len;
+        if constexpr (Lean) {
+            from_float4(sh.m[j][threadIdx.x], m);
+        } else {
+#pragma unroll
+            for (int v = 0; v < 4; ++v) m[v] = e[j][v].m;
+        }
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
+            const Kept& q = e[j][v];
             const bool cut = Reset && hard[j];
-            float s_rest, i_rest;
-            const float s = sigmoid_both(r[v], s_rest), si = sigmoid_both(i[v], i_rest);
-            const float z = k.v[v] * s;
-            const float at = __builtin_amdgcn_exp2f(z);
-            const float m2 = one_minus_square(z, at);
-            const float inv = m2 < kMinNormal ? 0.0f : __builtin_amdgcn_rsqf(m2);   // NaN for a NaN
-            const float m = cut ? 1.0f : m2 * inv;
+            const float s = gate_of(q.s), si = gate_of(q.i);
+            const float inv = m[v] > 0.0f ? __builtin_amdgcn_rcpf(m[v]) : m[v];   // 0 at m = 0, NaN for a NaN
             const float g = d[v] + c[v];
-            const float ix = si * x[v];
-            gx[v] = g * m * si;
-            gi[v] = gx[v] * x[v] * i_rest;
-            const float dl = g * fmaf(at, hp[j][v], -at * at * inv * ix);
-            gr[v] = cut ? 0.0f : dl * (z * kLn2) * s_rest;
-            if (there && !cut) dth[v] = fmaf(dl, s, dth[v]);
-            c[v] = cut ? 0.0f : there ? at * g : c[v];
+            gx[v] = g * m[v] * si;
+            gi[v] = gx[v] * x[v] * rest_of(q.i);
+            const float dl = g * q.a * fmaf(-q.a * inv, si * x[v], q.hp);
+            gr[v] = cut ? 0.0f : dl * (k.v[v] * kLn2 * s * rest_of(q.s));
+            dth[v] = cut ? dth[v] : fmaf(dl, s, dth[v]);
+            c[v] = cut ? 0.0f : q.a * g;
         }
-        if (there) {
-            const int64_t at = (token0 + j) * a.grad_stride + ch;
-            Lane4<Tg>::template store<Vec>(a.dx, at, n, gx);
-            Lane4<Tg>::template store<Vec>(a.dr, at, n, gr);
-            Lane4<Tg>::template store<Vec>(a.di, at, n, gi);
-        }
+        const int64_t step = j * a.grad_stride;
+        Lane4<Tg>::template store<Vec>(dx + step, g_off, n, gx);
+        Lane4<Tg>::template store<Vec>(dr + step, g_off, n, gr);
+        Lane4<Tg>::template store<Vec>(di + step, g_off, n, gi);
     }
-    if (a.dh0 != nullptr && t0 == 0) Lane4<float>::store<false>(a.dh0, b * a.width + ch, n, c);
+    if (a.dh0 != nullptr && tile == 0 && wave == 0 && row == 0) Lane4<float>::store<false>(a.dh0, at.b * a.width + ch, n, c);
     // dtheta: the tile's sum of dl s, one row of the partial sums
-    __syncthreads();
 #pragma unroll
-    for (int v = 0; v < 4; ++v) {
-        dth[v] = row_pair_sums(dth[v]);
-    }
-    if (row == 0) fwd_A[wave][col] = make_float4(dth[0], dth[1], dth[2], dth[3]);
+    for (int v = 0; v < 4; ++v) dth[v] = row_pair_sums(dth[v]);
     __syncthreads();
-    if (wave == 0 && row == 0 && n > 0) {
-        float4 s = fwd_A[0][col];
-        for (int w = 1; w < kBwdWaves; ++w) {
-            const float4 q = fwd_A[w][col];
-            s.x += q.x, s.y += q.y, s.z += q.z, s.w += q.w;
-        }
-        const float o[4] = {s.x, s.y, s.z, s.w};
-        Lane4<float>::store<false>(a.partial, (b * a.tiles + tile) * a.width + ch, n, o);
+    if (row == 0) *reinterpret_cast<float4*>(&sh.enter[wave][col * 4]) = to_float4(dth);
+    __syncthreads();
+    if (wave == 0 && my < a.width) {
+        float s = sh.enter[0][lane];
+#pragma unroll
+        for (int w = 1; w < kBwdWaves; ++w) s += sh.enter[w][lane];
+        a.partial[(at.b * a.tiles + tile) * a.width + my] = s;
     }
 }
 
@@ -564,12 +728,24 @@ hipError_t copy_state(const float* from, float* to, int64_t n, hipStream_t strea
     return hipGetLastError();
 }
 
+// Marks every word of a walk as not yet published.
+hipError_t clear_walk(uint64_t* words, int64_t batch, int64_t tiles, int64_t width, hipStream_t stream)
+{
+    const int64_t n = recurrence_walk_bytes(batch, tiles, width) / 16;
+    if (n == 0) return hipSuccess;
+    hipLaunchKernelGGL(recurrence_fill_kernel, dim3(unsigned(std::min<int64_t>((n + 255) / 256, 1024))), dim3(256), 0, stream,
+                       reinterpret_cast<ulonglong2*>(words), n);
+    return hipGetLastError();
+}
+
 template <typename T, bool Vec, bool Reset>
 hipError_t launch_forward(const RecurrenceArgs& a, int64_t blocks, hipStream_t stream)
 {
     const dim3 grid{unsigned(blocks)}, block{kFwdThreads};
-    if (a.tiles > 1) hipLaunchKernelGGL((recurrence_kernel<T, Vec, Reset, true>), grid, block, 0, stream, a);
-    hipLaunchKernelGGL((recurrence_kernel<T, Vec, Reset, false>), grid, block, 0, stream, a);
+    if (a.kept_x != nullptr)
+        hipLaunchKernelGGL((recurrence_kernel<T, Vec, Reset, true>), grid, block, 0, stream, a);
+    else
+        hipLaunchKernelGGL((recurrence_kernel<T, Vec, Reset, false>), grid, block, 0, stream, a);
     return hipGetLastError();
 }
 
@@ -578,9 +754,10 @@ hipError_t launch_forward_type(const RecurrenceArgs& a, hipStream_t stream)
 {
     const int64_t blocks = a.batch * a.tiles * ((a.width + kCh - 1) / kCh);
     if (blocks > INT32_MAX) return hipErrorInvalidValue;
+    if (hipError_t e = clear_walk(a.words, a.batch, a.tiles, a.width, stream); e != hipSuccess) return e;
     constexpr int bytes = 4 * int(sizeof(T));
-    const bool vec = a.width % 4 == 0 && a.stride % 4 == 0 && aligned(a.x, bytes) && aligned(a.r, bytes) &&
-                     aligned(a.i, bytes) && aligned(a.y, bytes);
+    const bool vec = a.width % 4 == 0 && a.stride % 4 == 0 && a.stride <= kNearStride && aligned(a.x, bytes) &&
+                     aligned(a.r, bytes) && aligned(a.i, bytes) && aligned(a.y, bytes);
     if (a.reset != nullptr)
         return vec ? launch_forward<T, true, true>(a, blocks, stream) : launch_forward<T, false, true>(a, blocks, stream);
     return vec ? launch_forward<T, true, false>(a, blocks, stream) : launch_forward<T, false, false>(a, blocks, stream);
@@ -601,32 +778,37 @@ hipError_t launch_step_type(const RecurrenceArgs& a, float* state_out, hipStream
     return hipGetLastError();
 }
 
-template <typename T, typename Tg, bool Vec, bool Reset>
-hipError_t launch_backward(const RecurrenceGradArgs& a, int64_t blocks, hipStream_t stream)
-{
-    const dim3 grid{unsigned(blocks)}, block{kBwdThreads};
-    if (a.tiles > 1) hipLaunchKernelGGL((recurrence_grad_kernel<T, Tg, Vec, Reset, true>), grid, block, 0, stream, a);
-    hipLaunchKernelGGL((recurrence_grad_kernel<T, Tg, Vec, Reset, false>), grid, block, 0, stream, a);
-    return hipGetLastError();
-}
-
 template <typename T, typename Tg>
 hipError_t launch_backward_types(const RecurrenceGradArgs& a, hipStream_t stream)
 {
     const int64_t blocks = a.batch * a.tiles * ((a.width + kCh - 1) / kCh);
     if (blocks > INT32_MAX) return hipErrorInvalidValue;
+    if (hipError_t e = clear_walk(a.words, a.batch, a.tiles, a.width, stream); e != hipSuccess) return e;
     constexpr int in = 4 * int(sizeof(T)), out = 4 * int(sizeof(Tg));
-    const bool vec = a.width % 4 == 0 && a.stride % 4 == 0 && a.grad_stride % 4 == 0 && aligned(a.x, in) &&
-                     aligned(a.r, in) && aligned(a.i, in) && aligned(a.dy, out) && aligned(a.dx, out) &&
-                     aligned(a.dr, out) && aligned(a.di, out);
-    if (a.reset != nullptr)
-        return vec ? launch_backward<T, Tg, true, true>(a, blocks, stream) : launch_backward<T, Tg, false, true>(a, blocks, stream);
-    return vec ? launch_backward<T, Tg, true, false>(a, blocks, stream) : launch_backward<T, Tg, false, false>(a, blocks, stream);
+    const bool vec = a.width % 4 == 0 && a.stride % 4 == 0 && a.grad_stride % 4 == 0 && a.stride <= kNearStride &&
+                     a.grad_stride <= kNearStride && aligned(a.x, in) && aligned(a.r, in) && aligned(a.i, in) &&
+                     aligned(a.dy, out) && aligned(a.dx, out) && aligned(a.dr, out) && aligned(a.di, out);
+    const dim3 grid{unsigned(blocks)}, block{kBwdThreads};
+    if (vec && a.reset != nullptr)
+        hipLaunchKernelGGL((recurrence_grad_kernel<T, Tg, true, true>), grid, block, 0, stream, a);
+    else if (vec)
+        hipLaunchKernelGGL((recurrence_grad_kernel<T, Tg, true, false>), grid, block, 0, stream, a);
+    else if (a.reset != nullptr)
+        hipLaunchKernelGGL((recurrence_grad_kernel<T, Tg, false, true>), grid, block, 0, stream, a);
+    else
+        hipLaunchKernelGGL((recurrence_grad_kernel<T, Tg, false, false>), grid, block, 0, stream, a);
+    return hipGetLastError();
 }
 
 }  // namespace
 
 int64_t recurrence_tiles(int64_t seq_len) { return (seq_len + kFwdTile - 1) / kFwdTile; }
+
+int64_t recurrence_walk_bytes(int64_t batch, int64_t tiles, int64_t width)
+{
+    if (tiles <= 1) return 0;
+    return (kTicketWords + batch * (tiles + tiles / kJoin) * width + 1) / 2 * 16;
+}
 
 hipError_t launch_recurrence(const RecurrenceArgs& a, hipStream_t stream)
 {
