@@ -154,10 +154,13 @@ __device__ __forceinline__ float sigmoid_both(float x, float& rest)
     rest = x > 0.0f ? e * s : 1.0f - s;
     return s;
 }
-// log(1 + exp(x)) = max(x, 0) + log(1 + exp(-|x|)); a NaN stays one
-__device__ __forceinline__ float softplus_both(float x)
+// log(1 + exp(x)) = max(x, 0) + log(1 + e), e = exp(-|x|).  With u = 1 + e as rounded, log(u) e / (u - 1)
+// is log(1 + e) to fp32 accuracy however small e is, and e itself where u is 1.  A NaN stays one.
+__device__ __forceinline__ float softplus_fast(float x)
 {
-    const float tail = log1pf(expf(-fabsf(x)));
+    const float e = __builtin_amdgcn_exp2f(-kLog2e * fabsf(x));
+    const float u = 1.0f + e, d = u - 1.0f;
+    const float tail = d == 0.0f ? e : kLn2 * __builtin_amdgcn_logf(u) * e * __builtin_amdgcn_rcpf(d);
     return x > 0.0f ? x + tail : tail;
 }
 

@@ -9,10 +9,7 @@
 //     dtheta = -decay sigma(theta) sum_{b,t} dl s
 // A reset token has a_t = 0 and m_t = 1 and nothing before it is read.
 //
-// 1 - a^2 is -expm1(2 l): its series for a small argument, 1 - a a otherwise (the
-// difference then keeps all but two bits).  l / m, which multiplies dl in dr, tends to 0
-// with l although 1 / m does not stay finite, so the reciprocal root is formed once and
-// is 0 where 1 - a^2 is.
+// 1 - a^2 is -expm1(2 l): its series for a small argument, 1 - a a otherwise.
 //
 // A span of tokens acts on the state as h -> A h + B, and spans compose, so time is cut:
 // a lane holds kSub consecutive tokens of four channels in registers, a row of 16 lanes a
@@ -92,22 +89,23 @@ __device__ __forceinline__ Rates rates_of(const float* theta, float decay, int64
 {
     Rates k;
 #pragma unroll
-    for (int v = 0; v < 4; ++v) k.v[v] = v < n ? -decay * kLog2e * softplus_both(theta[ch + v]) : 0.0f;
+    for (int v = 0; v < 4; ++v) k.v[v] = v < n ? -decay * kLog2e * softplus_fast(theta[ch + v]) : 0.0f;
     return k;
 }
 
-// a = 2^z and 1 - a^2 for z <= 0
-__device__ __forceinline__ float one_minus_square(float z, float a)
+// 1 - a^2 = 1 - 4^z for z <= 0 and a = 2^z as rounded: for u = -2 ln 2 z below 1/8 the series
+// u - u^2/2 + u^3/6 - u^4/24 + u^5/120, written in z (what is left out is below u^6/720, 5e-8 of
+// the sum); above, 1 - a a keeps all but three bits.
+// `least` is added to the former.
+__device__ __forceinline__ float one_minus_square(float z, float a, float least = 0.0f)
 {
-    const float u = -2.0f * kLn2 * z;   // a^2 = exp(-u)
-    float p = 1.0f / 5040.0f;
-    p = fmaf(p, u, -1.0f / 720.0f);
-    p = fmaf(p, u, 1.0f / 120.0f);
-    p = fmaf(p, u, -1.0f / 24.0f);
-    p = fmaf(p, u, 1.0f / 6.0f);
-    p = fmaf(p, u, -0.5f);
-    p = fmaf(p, u, 1.0f);
-    return u < 0.35f ? u * p : fmaf(-a, a, 1.0f);   // first term left out: u^7 / 8! < 2e-8
+    constexpr float w = -2.0f * kLn2;
+    float p = w * w * w * w * w / 120.0f;
+    p = fmaf(p, z, -w * w * w * w / 24.0f);
+    p = fmaf(p, z, w * w * w / 6.0f);
+    p = fmaf(p, z, -w * w / 2.0f);
+    p = fmaf(p, z, w);
+    return z > 0.125f / w ? fmaf(p, z, least) : fmaf(-a, a, 1.0f);
 }
 
 // One element's a and b (the state's input); hard: a reset token, a = -0
@@ -269,10 +267,15 @@ __device__ __forceinline__ typename Lane4<T>::Raw load_row(const void* base, int
     return Lane4<T>::template load<Vec>(static_cast<const T*>(base) + row, off, n);
 }
 
-// Eight lanes hold a group of 32 channels: its exponent byte and this lane's four codes.
-__device__ __forceinline__ uint32_t pack_group(const float (&x)[4], uint32_t& byte)
+// How many of `most` tokens exist when n are left (which may be none or fewer).
+__device__ __forceinline__ int there_are(int64_t n, int most) { return int(max<int64_t>(0, min<int64_t>(n, most))); }
+
+// Eight lanes hold a group of 32 channels: its exponent byte and this lane's four codes.  A lane
+// past the last channel (not mine) has no part in it.
+__device__ __forceinline__ uint32_t pack_group(const float (&x)[4], bool mine, uint32_t& byte)
 {
     uint32_t top = max(max(abs_bits(x[0]), abs_bits(x[1])), max(abs_bits(x[2]), abs_bits(x[3])));
+    top = mine ? top : 0u;
     top = max(top, uint32_t(dpp_i32<kDppQuadSwap1>(int(top), int(top))));
     top = max(top, uint32_t(dpp_i32<kDppQuadSwap2>(int(top), int(top))));
     top = max(top, uint32_t(dpp_i32<kDppRowHalfMirror>(int(top), int(top))));
@@ -302,21 +305,31 @@ __global__ __launch_bounds__(kFwdThreads, 4) void recurrence_kernel(RecurrenceAr
     const int n = int(max<int64_t>(0, min<int64_t>(4, a.width - ch)));   // channels of this lane
     const int64_t w0 = int64_t(at.step) * kFwdTile + wave * 4 * kFwdSub;  // the wave's first token
     const int64_t token0 = at.b * a.seq_len + w0;
-    const int64_t left = a.seq_len - w0 - row * kFwdSub;                 // tokens there are from the lane's first on
+    const int left = there_are(a.seq_len - w0 - row * kFwdSub, kFwdSub);  // of the lane's tokens
 
-    // tokens past the end are neither read nor written; they come after all others, so the
-    // state that they would leave is used by nobody
+    // Tokens past the end come after all others, so the state that they would leave is used by
+    // nobody.  A wave whose tokens all exist reads without asking; its lanes past the last
+    // channel read the slab's first, for nothing.
     typename Lane4<T>::Raw rx[kFwdSub], rr[kFwdSub], ri[kFwdSub];
     bool hard[kFwdSub] = {};
-    const Offset<Vec> off = Offset<Vec>(row * kFwdSub) * Offset<Vec>(a.stride) + col * 4;
+    auto load_all = [&](int c4, auto count) {
+        const Offset<Vec> off = Offset<Vec>(row * kFwdSub) * Offset<Vec>(a.stride) + c4 * 4;
 #pragma unroll
-    for (int j = 0; j < kFwdSub; ++j) {
-        const int m = j < left ? n : 0;
-        const int64_t at_row = (token0 + j) * a.stride + ch0;
-        rx[j] = load_row<T, Vec>(a.x, at_row, off, m);
-        rr[j] = load_row<T, Vec>(a.r, at_row, off, m);
-        ri[j] = load_row<T, Vec>(a.i, at_row, off, m);
-        if (Reset) hard[j] = j < left && a.reset[token0 + row * kFwdSub + j] != 0;
+        for (int j = 0; j < kFwdSub; ++j) {
+            const int m = count(j);
+            const int64_t at_row = (token0 + j) * a.stride + ch0;
+            rx[j] = load_row<T, Vec>(a.x, at_row, off, m);
+            rr[j] = load_row<T, Vec>(a.r, at_row, off, m);
+            ri[j] = load_row<T, Vec>(a.i, at_row, off, m);
+        }
+    };
+    if (Vec && w0 + 4 * kFwdSub <= a.seq_len)
+        load_all(n > 0 ? col : 0, [](int) { return 4; });
+    else
+        load_all(col, [&](int j) { return j < left ? n : 0; });
+    if constexpr (Reset) {
+#pragma unroll
+        for (int j = 0; j < kFwdSub; ++j) hard[j] = j < left && a.reset[token0 + row * kFwdSub + j] != 0;
     }
     const Rates k = rates_of(a.theta, a.decay, ch, n);
     if constexpr (Kept) {
@@ -330,7 +343,7 @@ __global__ __launch_bounds__(kFwdThreads, 4) void recurrence_kernel(RecurrenceAr
                 float x[4];
                 Lane4<T>::widen(q == 0 ? rx[j] : q == 1 ? rr[j] : ri[j], x);
                 uint32_t byte;
-                const uint32_t codes = pack_group(x, byte);
+                const uint32_t codes = pack_group(x, n > 0, byte);
                 if (j < left && n > 0) {
                     uint8_t* out = kept[q] + token * a.width + ch;
                     if constexpr (Vec) {
@@ -398,7 +411,7 @@ __global__ __launch_bounds__(kFwdThreads, 4) void recurrence_kernel(RecurrenceAr
         }
         if (j < left) {
             Lane4<T>::template store<Vec>(y + j * a.width, y_off, n, h);
-            if (j == left - 1 && final_h != nullptr) Lane4<float>::store<false>(final_h, 0, n, h);
+            if (final_h != nullptr && w0 + row * kFwdSub + j == a.seq_len - 1) Lane4<float>::store<false>(final_h, 0, n, h);
         }
     }
 }
@@ -442,7 +455,13 @@ struct Source {
     {
         return load_row<T, Vec>(base, token * a.stride + ch0, Offset<Vec>(row) * Offset<Vec>(a.stride) + col * 4, n);
     }
-    __device__ static void widen(const Raw& r, float (&x)[4]) { Lane4<T>::widen(r, x); }
+    // the values times `by`
+    __device__ static void widen(const Raw& r, float by, float (&x)[4])
+    {
+        Lane4<T>::widen(r, x);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) x[v] *= by;
+    }
 };
 template <>
 struct Source<q8_t> {
@@ -456,23 +475,19 @@ struct Source<q8_t> {
         const uint8_t* bytes = static_cast<const uint8_t*>(base) + checkpoint_exponents_at(a.batch * a.seq_len, a.width) + token * groups + ch0 / kGroup;
         return {load_codes<Vec>(codes + Offset<Vec>(row) * Offset<Vec>(a.width) + col * 4, n), bytes[Offset<Vec>(row) * Offset<Vec>(groups) + col / 8]};
     }
-    __device__ static void widen(const Raw& r, float (&x)[4]) { widen_q8(r.codes, group_scale(r.byte), x); }
+    __device__ static void widen(const Raw& r, float by, float (&x)[4]) { widen_q8(r.codes, group_scale(r.byte) * by, x); }
 };
 
-// sigma(x) and 1 - sigma(x) in one register, each to its own accuracy: the smaller of the two,
-// the second with its sign set.
-__device__ __forceinline__ float fold_gate(float x)
-{
-    const float e = __builtin_amdgcn_exp2f(-kLog2e * x);
-    const float s = __builtin_amdgcn_rcpf(1.0f + e);
-    return x > 0.0f ? -(e * s) : s;
-}
-__device__ __forceinline__ float gate_of(float f) { return signbit(f) ? 1.0f + f : f; }
-__device__ __forceinline__ float rest_of(float f) { return signbit(f) ? -f : 1.0f - f; }
+// From e = exp(-x): sigma(x), and 1 - sigma(x) = e sigma(x) to its own accuracy.  Where e is
+// infinite the product counts as 0 (a multiplication that takes 0 times anything as 0) instead
+// of the 1 that it is: it only ever multiplies sigma(x), which is 0 there.
+__device__ __forceinline__ float gate_of(float e) { return __builtin_amdgcn_rcpf(1.0f + e); }
+__device__ float mul_zero_wins(float x, float y) __asm("llvm.amdgcn.fmul.legacy");
+__device__ __forceinline__ float rest_of(float e, float s) { return mul_zero_wins(e, s); }
 
 // What the walk back needs of an element, all that is kept of it in between.
 struct Kept {
-    float a, hp, m, s, i;   // hp: the state's input at first, then the state before the token; s, i folded gates
+    float a, hp, m, er, ei;   // hp: the state's input at first, then the state before the token; exp(-r), exp(-i)
 };
 
 // Lean: 16-bit gradients of 8- or 16-bit inputs run two workgroups a compute unit, with 128
@@ -510,20 +525,29 @@ __global__ __launch_bounds__(kBwdThreads, (kLean<T, Tg> ? 4 : 2)) void recurrenc
     const int n = int(max<int64_t>(0, min<int64_t>(4, a.width - ch)));
     const int64_t w0 = tile * kBwdTile + wave * 4 * kBwdSub;
     const int64_t token0 = at.b * a.seq_len + w0;
-    const int64_t left = a.seq_len - w0 - row * kBwdSub;
+    const int left = there_are(a.seq_len - w0 - row * kBwdSub, kBwdSub);
 
     typename Source<T>::Raw rx[kBwdSub], rr[kBwdSub], ri[kBwdSub];
     typename Lane4<Tg>::Raw rd[kBwdSub];
     bool hard[kBwdSub] = {};
-    const Offset<Vec> d_off = Offset<Vec>(row * kBwdSub) * Offset<Vec>(a.width) + col * 4;
+    auto load_all = [&](int c4, auto count) {
+        const Offset<Vec> d_off = Offset<Vec>(row * kBwdSub) * Offset<Vec>(a.width) + c4 * 4;
 #pragma unroll
-    for (int j = 0; j < kBwdSub; ++j) {
-        const int m = j < left ? n : 0;
-        rr[j] = Source<T>::template load<Vec>(a.r, a, token0 + j, row * kBwdSub, ch0, col, m);
-        rx[j] = Source<T>::template load<Vec>(a.x, a, token0 + j, row * kBwdSub, ch0, col, m);
-        ri[j] = Source<T>::template load<Vec>(a.i, a, token0 + j, row * kBwdSub, ch0, col, m);
-        rd[j] = load_row<Tg, Vec>(a.dy, (token0 + j) * a.width + ch0, d_off, m);
-        if (Reset) hard[j] = j < left && a.reset[token0 + row * kBwdSub + j] != 0;
+        for (int j = 0; j < kBwdSub; ++j) {
+            const int m = count(j);
+            rr[j] = Source<T>::template load<Vec>(a.r, a, token0 + j, row * kBwdSub, ch0, c4, m);
+            rx[j] = Source<T>::template load<Vec>(a.x, a, token0 + j, row * kBwdSub, ch0, c4, m);
+            ri[j] = Source<T>::template load<Vec>(a.i, a, token0 + j, row * kBwdSub, ch0, c4, m);
+            rd[j] = load_row<Tg, Vec>(a.dy, (token0 + j) * a.width + ch0, d_off, m);
+        }
+    };
+    if (Vec && w0 + 4 * kBwdSub <= a.seq_len)
+        load_all(n > 0 ? col : 0, [](int) { return 4; });
+    else
+        load_all(col, [&](int j) { return j < left ? n : 0; });
+    if constexpr (Reset) {
+#pragma unroll
+        for (int j = 0; j < kBwdSub; ++j) hard[j] = j < left && a.reset[token0 + row * kBwdSub + j] != 0;
     }
     const Rates k = rates_of(a.theta, a.decay, ch, n);
     // the lane's tokens: their factors, and what they do together to the state and, on the way
@@ -534,19 +558,22 @@ __global__ __launch_bounds__(kBwdThreads, (kLean<T, Tg> ? 4 : 2)) void recurrenc
     for (int v = 0; v < 4; ++v) fwd[v] = bwd[v] = nothing();
 #pragma unroll
     for (int j = 0; j < kBwdSub; ++j) {
-        float x[4], r[4], i[4], m[4];
+        float x[4], r[4], i[4], m[4], in[4];
         pin(rx[j]), pin(rr[j]), pin(ri[j]);
-        Source<T>::widen(rx[j], x);
-        Source<T>::widen(rr[j], r);
-        Source<T>::widen(ri[j], i);
+        Source<T>::widen(rx[j], 1.0f, x);
+        Source<T>::widen(rr[j], -kLog2e, r);
+        Source<T>::widen(ri[j], -kLog2e, i);
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
             Kept& q = e[j][v];
-            q.s = fold_gate(r[v]);
-            q.i = fold_gate(i[v]);
-            const float z = k.v[v] * gate_of(q.s);
+            q.er = __builtin_amdgcn_exp2f(r[v]);
+            q.ei = __builtin_amdgcn_exp2f(i[v]);
+            const float z = k.v[v] * gate_of(q.er);
             q.a = __builtin_amdgcn_exp2f(z);
-            m[v] = __builtin_amdgcn_sqrtf(one_minus_square(z, q.a));
+            // at least 2^-60, so that 1 / m is finite: where 1 - a^2 is less, its share of every
+            // gradient is below fp32's resolution of the others
+            m[v] = __builtin_amdgcn_sqrtf(one_minus_square(z, q.a, 0x1p-120f));
+            in[v] = gate_of(q.ei) * x[v];
         }
         const bool cut = any_hard<Reset>(hard[j]);
         if (cut && hard[j]) {
@@ -556,9 +583,9 @@ __global__ __launch_bounds__(kBwdThreads, (kLean<T, Tg> ? 4 : 2)) void recurrenc
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
             Kept& q = e[j][v];
-            q.hp = m[v] * gate_of(q.i) * x[v];
+            q.hp = m[v] * in[v];
             if (!Lean) q.m = m[v];
-            pin(q.s), pin(q.i);
+            pin(q.er), pin(q.ei);
         }
         if constexpr (Lean) sh.m[j][threadIdx.x] = to_float4(m);
         if (cut) {
@@ -653,7 +680,7 @@ __global__ __launch_bounds__(kBwdThreads, (kLean<T, Tg> ? 4 : 2)) void recurrenc
         if (j >= left) continue;
         float x[4], d[4], m[4], gx[4], gr[4], gi[4];
         pin(rx[j]), pin(rd[j]);
-        Source<T>::widen(rx[j], x);
+        Source<T>::widen(rx[j], 1.0f, x);
         Lane4<Tg>::widen(rd[j], d);
         if constexpr (Lean) {
             from_float4(sh.m[j][threadIdx.x], m);
@@ -665,15 +692,14 @@ __global__ __launch_bounds__(kBwdThreads, (kLean<T, Tg> ? 4 : 2)) void recurrenc
         for (int v = 0; v < 4; ++v) {
             const Kept& q = e[j][v];
             const bool cut = Reset && hard[j];
-            const float s = gate_of(q.s), si = gate_of(q.i);
-            const float inv = m[v] > 0.0f ? __builtin_amdgcn_rcpf(m[v]) : m[v];   // 0 at m = 0, NaN for a NaN
-            const float g = d[v] + c[v];
+            const float s = gate_of(q.er), si = gate_of(q.ei);
+            const float g = d[v] + c[v], ag = q.a * g;
             gx[v] = g * m[v] * si;
-            gi[v] = gx[v] * x[v] * rest_of(q.i);
-            const float dl = g * q.a * fmaf(-q.a * inv, si * x[v], q.hp);
-            gr[v] = cut ? 0.0f : dl * (k.v[v] * kLn2 * s * rest_of(q.s));
+            gi[v] = gx[v] * x[v] * rest_of(q.ei, si);
+            const float dl = ag * fmaf(-q.a * __builtin_amdgcn_rcpf(m[v]), si * x[v], q.hp);
+            gr[v] = cut ? 0.0f : dl * (k.v[v] * kLn2 * s * rest_of(q.er, s));
             dth[v] = cut ? dth[v] : fmaf(dl, s, dth[v]);
-            c[v] = cut ? 0.0f : q.a * g;
+            c[v] = cut ? 0.0f : ag;
         }
         const int64_t step = j * a.grad_stride;
         Lane4<Tg>::template store<Vec>(dx + step, g_off, n, gx);
