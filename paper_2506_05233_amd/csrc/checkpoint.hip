@@ -113,18 +113,15 @@ __global__ __launch_bounds__(kThreads) void checkpoint_pack_kernel(CheckpointArg
         top = max(top, uint32_t(dpp_i32<kDppQuadSwap1>(int(top), int(top))));
         top = max(top, uint32_t(dpp_i32<kDppQuadSwap2>(int(top), int(top))));
         const uint32_t byte = group_exponent(__uint_as_float(top));
-        const float inv = group_inverse(byte), most = group_most(byte);
-        int c[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) c[e] = group_code(v[k][e], inv, most);
+        const float lo[4] = {v[k][0], v[k][1], v[k][2], v[k][3]}, hi[4] = {v[k][4], v[k][5], v[k][6], v[k][7]};
+        const uint32_t w[2] = {pack_codes(lo, byte), pack_codes(hi, byte)};
         int8_t* out = a.codes + at[k].code;
         if constexpr (Flat) {
-            const int lo[4] = {c[0], c[1], c[2], c[3]}, hi[4] = {c[4], c[5], c[6], c[7]};
-            *reinterpret_cast<uint2*>(out) = make_uint2(pack_codes(lo), pack_codes(hi));
+            *reinterpret_cast<uint2*>(out) = make_uint2(w[0], w[1]);
         } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                if (e < at[k].n) out[e] = int8_t(c[e]);
+                if (e < at[k].n) out[e] = int8_t(w[e / 4] >> (8 * (e % 4)));
         }
         if ((threadIdx.x & 3) == 0) a.exponents[at[k].byte] = uint8_t(byte);
     }

@@ -28,21 +28,38 @@ __device__ __forceinline__ uint32_t group_exponent(float amax)
 }
 // 2^E, and infinity for byte 255, which turns every code of that group (all 0) into NaN
 __device__ __forceinline__ float group_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
-// 2^-E for the bytes 1..249 (for byte 255 no matter what: group_most brings every code to 0)
+// 2^-E for the bytes 1..249 (byte 255: no matter what, its codes are set to 0)
 __device__ __forceinline__ float group_inverse(uint32_t byte) { return __uint_as_float(((254u - byte) & 0xFFu) << 23); }
-// Codes of a group are at most 127; at the largest exponent 63, since 64 * 2^122 is past fp32.
-__device__ __forceinline__ float group_most(uint32_t byte) { return byte == 255u ? 0.0f : byte >= 249u ? 63.0f : 127.0f; }
+// Codes of a group are at most 127 by the choice of E, but for the bytes from kRareByte on: at
+// the largest exponent they stop at 63, since 64 * 2^122 is past fp32, and a group that is
+// not finite has codes 0.
+constexpr uint32_t kRareByte = 249;
+__device__ __forceinline__ float group_most(uint32_t byte) { return byte == 255u ? 0.0f : 63.0f; }
 
-// x 2^-E is exact (or rounds to a magnitude far below 1/2), so the only rounding is rint,
-// half to even; a NaN element (its group has byte 255) becomes 0.
-__device__ __forceinline__ int group_code(float x, float inv, float most)
+// rint(x 2^-E), half to even, in the low byte: x 2^-E is exact (or rounds to a magnitude far
+// below 1/2), and adding 1.5 * 2^23 leaves an integer's two's complement in the low bits.
+__device__ __forceinline__ uint32_t group_code(float x, float inv) { return __float_as_uint(fmaf(x, inv, 12582912.0f)); }
+// the same for a group with byte >= kRareByte
+__device__ __forceinline__ uint32_t group_code_rare(float x, float inv, float most)
 {
     const float c = __builtin_rintf(x * inv);
-    return int(fminf(fmaxf(c, -most), most));
+    return uint32_t(int(fminf(fmaxf(c, -most), most)));
 }
-__device__ __forceinline__ uint32_t pack_codes(const int (&c)[4])
+// the low bytes of four words, first to last
+__device__ __forceinline__ uint32_t pack_codes(uint32_t a, uint32_t b, uint32_t c, uint32_t d)
 {
-    return (uint32_t(c[0]) & 0xFFu) | ((uint32_t(c[1]) & 0xFFu) << 8) | ((uint32_t(c[2]) & 0xFFu) << 16) | (uint32_t(c[3]) << 24);
+    const uint32_t lo = __builtin_amdgcn_perm(b, a, 0x0C0C0400u), hi = __builtin_amdgcn_perm(d, c, 0x04000C0Cu);
+    return lo | hi;
+}
+__device__ __forceinline__ uint32_t pack_codes(const float (&x)[4], uint32_t byte)
+{
+    const float inv = group_inverse(byte);
+    if (__any(byte >= kRareByte)) {
+        const float most = byte >= kRareByte ? group_most(byte) : 127.0f;
+        return pack_codes(group_code_rare(x[0], inv, most), group_code_rare(x[1], inv, most), group_code_rare(x[2], inv, most),
+                          group_code_rare(x[3], inv, most));
+    }
+    return pack_codes(group_code(x[0], inv), group_code(x[1], inv), group_code(x[2], inv), group_code(x[3], inv));
 }
 
 // max |x| with a NaN or an infinity coming out as infinity (fmaxf would drop a NaN): the

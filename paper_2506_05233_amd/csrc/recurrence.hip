@@ -25,6 +25,10 @@
 #include "mesa_lanes.hpp"
 
 namespace mesa {
+
+// The multiplication that takes 0 times anything as 0.
+__device__ float mul_zero_wins(float x, float y) __asm("llvm.amdgcn.fmul.legacy");
+
 namespace {
 
 constexpr int kAcross = 16;            // lanes across a token's channels
@@ -128,14 +132,15 @@ __device__ __forceinline__ Span terms(float x, float r, float i, float rate, boo
 // entered its group and the spans of the (at most kJoin - 1) tiles of the group before it.
 //
 // A workgroup takes its tile by drawing a ticket when it starts, and waits only for tiles of
-// smaller tickets; those are held by workgroups that run already, and the smallest ticket
+// smaller tickets of its slab; those are held by workgroups that run already, and the smallest ticket
 // not yet finished waits for nothing, so every wait ends whatever the order and the number
 // of workgroups that fit the GPU.  A span and its "published" mark are one 8-byte word
 // written and read with single relaxed accesses of agent scope, so no other memory has to be
 // ordered.  The words start as kUnset, written by a fill kernel ahead on the stream.
-constexpr int kJoin = 8;
+constexpr int kJoinOn = 32, kJoinBack = 8;   // forward; backward, whose shared memory is full
 constexpr uint64_t kUnset = ~uint64_t(0);
-constexpr int kTicketWords = 2;   // the ticket counter's 16 bytes, ahead of the spans
+// 64-bit words of the ticket counters (32 bits for each slab of channels), ahead of the spans
+__host__ __device__ inline int64_t ticket_words(int64_t width) { return (width + 2 * kCh - 1) / (2 * kCh); }
 
 __device__ __forceinline__ void publish(uint64_t* at, Span s)
 {
@@ -163,7 +168,7 @@ __global__ __launch_bounds__(256) void recurrence_fill_kernel(ulonglong2* words,
 
 // Shared memory of a walk: the spans of a workgroup's waves, what comes before them, and the
 // state entering every wave.
-template <int Waves>
+template <int Waves, int kJoin>
 struct WalkShared {
     float2 span[Waves][kCh];
     float2 before[kJoin][kCh];
@@ -173,32 +178,37 @@ struct WalkShared {
     };
 };
 
-// The workgroup's place in the call: the walk's tiles in order (the first walked first),
-// slower than the slabs of channels and the sequences, so that a tile's predecessors
-// started long before it where there are many.
+// The workgroup's place in the call.  Its slab of channels goes by its index, so that the
+// channels' constants are on their way while the ticket is drawn (a counter for each slab);
+// the ticket gives the sequence and the step of the walk, steps slower than sequences, so
+// that a tile's predecessors started long before it where there are many sequences.
 struct Place {
     int64_t b;
-    int slab, step;
+    int step;
 };
-template <int Waves>
-__device__ __forceinline__ Place place_of(uint64_t* words, bool many, int64_t batch, int slabs, WalkShared<Waves>& sh)
+__device__ __forceinline__ int draw_ticket(uint64_t* words, bool many, int slab, int slabs)
 {
-    uint32_t id = blockIdx.x;
+    if (!many) return int(blockIdx.x) / slabs;
+    if (threadIdx.x != 0) return 0;
+    return int(__hip_atomic_fetch_add(reinterpret_cast<uint32_t*>(words) + slab, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1u);
+}
+template <class Shared>
+__device__ __forceinline__ Place place_of(int ticket, bool many, int64_t batch, Shared& sh)
+{
     if (many) {
-        if (threadIdx.x == 0)
-            sh.ticket = int(__hip_atomic_fetch_add(reinterpret_cast<uint32_t*>(words), 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1u);
+        if (threadIdx.x == 0) sh.ticket = ticket;
         __syncthreads();
-        id = uint32_t(__builtin_amdgcn_readfirstlane(sh.ticket));
+        ticket = sh.ticket;
     }
-    const uint32_t rows = uint32_t(batch) * uint32_t(slabs), step = id / rows, row = id - step * rows;
-    return {int64_t(row / uint32_t(slabs)), int(row % uint32_t(slabs)), int(step)};
+    const uint32_t id = uint32_t(__builtin_amdgcn_readfirstlane(ticket)), step = id / uint32_t(batch);
+    return {int64_t(id - step * uint32_t(batch)), int(step)};
 }
 
 // From the waves' spans (in the order of the walk, written by their first lanes and made
 // visible by a barrier) the state entering each of them, in sh.enter after the barrier at
 // the end.  `step` is the tile's place in the walk, `first` the state ahead of the whole walk.
-template <bool Reset, int Waves>
-__device__ __forceinline__ void walk(WalkShared<Waves>& sh, uint64_t* words, int64_t batch, int64_t b, int step, int steps,
+template <bool Reset, int Waves, int kJoin>
+__device__ __forceinline__ void walk(WalkShared<Waves, kJoin>& sh, uint64_t* words, int64_t batch, int64_t b, int step, int steps,
                                      int64_t width, int slab, const float* first)
 {
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -206,8 +216,8 @@ __device__ __forceinline__ void walk(WalkShared<Waves>& sh, uint64_t* words, int
     const bool mine = ch < width;
     const int group = step / kJoin, at = step % kJoin;
     const int groups = steps / kJoin;
-    uint64_t* spans = words + kTicketWords + b * steps * width + ch;
-    uint64_t* leaves = words + kTicketWords + batch * steps * width + b * groups * width + ch;
+    uint64_t* spans = words + ticket_words(width) + b * steps * width + ch;
+    uint64_t* leaves = words + ticket_words(width) + batch * steps * width + b * groups * width + ch;
     if (wave == 0 && at != kJoin - 1 && step + 1 < steps) {
         Span s = nothing();
 #pragma unroll
@@ -227,6 +237,7 @@ __device__ __forceinline__ void walk(WalkShared<Waves>& sh, uint64_t* words, int
     }
     __syncthreads();
     if (wave == 0) {
+        __builtin_amdgcn_s_setprio(3);   // the others wait for it
         float h = sh.before[0][lane].y;
         for (int e = 1; e <= at; ++e) h = apply<Reset>({sh.before[e][lane].x, sh.before[e][lane].y}, h);
 #pragma unroll
@@ -235,6 +246,7 @@ __device__ __forceinline__ void walk(WalkShared<Waves>& sh, uint64_t* words, int
             h = apply<Reset>({sh.span[w][lane].x, sh.span[w][lane].y}, h);
         }
         if (mine && at == kJoin - 1 && step + 1 < steps) publish(leaves + int64_t(group) * width, {-0.0f, h});
+        __builtin_amdgcn_s_setprio(0);
     }
     __syncthreads();
 }
@@ -280,29 +292,44 @@ __device__ __forceinline__ uint32_t pack_group(const float (&x)[4], bool mine, u
     top = max(top, uint32_t(dpp_i32<kDppQuadSwap2>(int(top), int(top))));
     top = max(top, uint32_t(dpp_i32<kDppRowHalfMirror>(int(top), int(top))));
     byte = group_exponent(__uint_as_float(top));
-    const float inv = group_inverse(byte), most = group_most(byte);
-    const int c[4] = {group_code(x[0], inv, most), group_code(x[1], inv, most), group_code(x[2], inv, most), group_code(x[3], inv, most)};
-    return pack_codes(c);
+    return pack_codes(x, byte);
 }
 
-// Whether a lane of the wave has a reset at its token j: few waves do, and the others'
-// arithmetic is that without resets.
-template <bool Reset>
-__device__ __forceinline__ bool any_hard(bool hard)
-{
-    return Reset && __any(hard);
-}
+// The resets of a wave's tokens, bit t for its token t, the same in every lane; few waves have
+// any, and the others' arithmetic is that without resets.  Lane row `row` of Sub tokens:
+// whether its token j is one, and whether token j of any row is.
+template <bool Reset, int Sub>
+struct Cuts {
+    uint32_t all, mine;
+    __device__ Cuts(const uint8_t* reset, int64_t left, int row)
+    {
+        const int lane = threadIdx.x % kWave;
+        all = mine = 0;
+        if constexpr (Reset) {
+            all = uint32_t(__ballot(lane < 4 * Sub && lane < left && reset[lane] != 0));
+            mine = all >> (row * Sub);
+        }
+    }
+    __device__ bool lane(int j) const { return Reset && ((mine >> j) & 1u) != 0; }
+    __device__ bool any(int j) const
+    {
+        constexpr uint32_t rows = 1u | (1u << Sub) | (1u << (2 * Sub)) | (1u << (3 * Sub));
+        return Reset && (all & (rows << j)) != 0;
+    }
+};
 
 template <typename T, bool Vec, bool Reset, bool Kept>
-__global__ __launch_bounds__(kFwdThreads, 4) void recurrence_kernel(RecurrenceArgs a)
+__global__ __launch_bounds__(kFwdThreads, (Vec ? 4 : 2)) void recurrence_kernel(RecurrenceArgs a)
 {
-    __shared__ WalkShared<kFwdWaves> sh;
+    __shared__ WalkShared<kFwdWaves, kJoinOn> sh;
     const int slabs = int((a.width + kCh - 1) / kCh);
-    const Place at = place_of(a.words, a.tiles > 1, a.batch, slabs, sh);
+    const int slab = int(blockIdx.x) % slabs, ticket = draw_ticket(a.words, a.tiles > 1, slab, slabs);
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int row = lane / kAcross, col = lane % kAcross;
-    const int64_t ch0 = int64_t(at.slab) * kCh, ch = ch0 + col * 4;
+    const int64_t ch0 = int64_t(slab) * kCh, ch = ch0 + col * 4;
     const int n = int(max<int64_t>(0, min<int64_t>(4, a.width - ch)));   // channels of this lane
+    const Rates k = rates_of(a.theta, a.decay, ch, n);
+    const Place at = place_of(ticket, a.tiles > 1, a.batch, sh);
     const int64_t w0 = int64_t(at.step) * kFwdTile + wave * 4 * kFwdSub;  // the wave's first token
     const int64_t token0 = at.b * a.seq_len + w0;
     const int left = there_are(a.seq_len - w0 - row * kFwdSub, kFwdSub);  // of the lane's tokens
@@ -311,7 +338,6 @@ __global__ __launch_bounds__(kFwdThreads, 4) void recurrence_kernel(RecurrenceAr
     // nobody.  A wave whose tokens all exist reads without asking; its lanes past the last
     // channel read the slab's first, for nothing.
     typename Lane4<T>::Raw rx[kFwdSub], rr[kFwdSub], ri[kFwdSub];
-    bool hard[kFwdSub] = {};
     auto load_all = [&](int c4, auto count) {
         const Offset<Vec> off = Offset<Vec>(row * kFwdSub) * Offset<Vec>(a.stride) + c4 * 4;
 #pragma unroll
@@ -327,33 +353,38 @@ __global__ __launch_bounds__(kFwdThreads, 4) void recurrence_kernel(RecurrenceAr
         load_all(n > 0 ? col : 0, [](int) { return 4; });
     else
         load_all(col, [&](int j) { return j < left ? n : 0; });
-    if constexpr (Reset) {
-#pragma unroll
-        for (int j = 0; j < kFwdSub; ++j) hard[j] = j < left && a.reset[token0 + row * kFwdSub + j] != 0;
-    }
-    const Rates k = rates_of(a.theta, a.decay, ch, n);
+    const Cuts<Reset, kFwdSub> cuts(a.reset + token0, a.seq_len - w0, row);
     if constexpr (Kept) {
         uint8_t* const kept[3] = {a.kept_x, a.kept_r, a.kept_i};
-        const int64_t bytes_at = checkpoint_exponents_at(a.batch * a.seq_len, a.width), groups = (a.width + kGroup - 1) / kGroup;
+        const int64_t groups = (a.width + kGroup - 1) / kGroup;
+        const int64_t codes_at = token0 * a.width + ch0;
+        const int64_t bytes_at = checkpoint_exponents_at(a.batch * a.seq_len, a.width) + token0 * groups + ch0 / kGroup;
+        const Offset<Vec> c_off = Offset<Vec>(row * kFwdSub) * Offset<Vec>(a.width) + col * 4;
+        const Offset<Vec> b_off = Offset<Vec>(row * kFwdSub) * Offset<Vec>(groups) + col / 8;
 #pragma unroll
         for (int j = 0; j < kFwdSub; ++j) {
-            const int64_t token = token0 + row * kFwdSub + j;
+            uint32_t codes[3], byte[3];
 #pragma unroll
             for (int q = 0; q < 3; ++q) {
                 float x[4];
                 Lane4<T>::widen(q == 0 ? rx[j] : q == 1 ? rr[j] : ri[j], x);
-                uint32_t byte;
-                const uint32_t codes = pack_group(x, n > 0, byte);
-                if (j < left && n > 0) {
-                    uint8_t* out = kept[q] + token * a.width + ch;
+                codes[q] = pack_group(x, n > 0, byte[q]);
+            }
+            if (j < left && n > 0) {
+#pragma unroll
+                for (int q = 0; q < 3; ++q) {
+                    uint8_t* out = kept[q] + codes_at + j * a.width + c_off;
                     if constexpr (Vec) {
-                        *reinterpret_cast<uint32_t*>(out) = codes;
+                        *reinterpret_cast<uint32_t*>(out) = codes[q];
                     } else {
 #pragma unroll
                         for (int v = 0; v < 4; ++v)
-                            if (v < n) out[v] = uint8_t(codes >> (8 * v));
+                            if (v < n) out[v] = uint8_t(codes[q] >> (8 * v));
                     }
-                    if (col % 8 == 0) kept[q][bytes_at + token * groups + ch / kGroup] = uint8_t(byte);
+                }
+                if (col % 8 == 0) {
+#pragma unroll
+                    for (int q = 0; q < 3; ++q) kept[q][bytes_at + j * groups + b_off] = uint8_t(byte[q]);
                 }
             }
         }
@@ -370,10 +401,10 @@ __global__ __launch_bounds__(kFwdThreads, 4) void recurrence_kernel(RecurrenceAr
         Lane4<T>::widen(ri[j], i);
 #pragma unroll
         for (int v = 0; v < 4; ++v) e[j][v] = terms<false>(x[v], r[v], i[v], k.v[v], false);
-        if (any_hard<Reset>(hard[j])) {
+        if (cuts.any(j)) {
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
-                if (hard[j]) e[j][v] = terms<true>(x[v], r[v], i[v], k.v[v], true);
+                if (cuts.lane(j)) e[j][v] = terms<true>(x[v], r[v], i[v], k.v[v], true);
                 own[v] = join<true>(own[v], e[j][v]);
             }
         } else {
@@ -389,7 +420,7 @@ __global__ __launch_bounds__(kFwdThreads, 4) void recurrence_kernel(RecurrenceAr
         out[1] = make_float4(all[2].A, all[2].B, all[3].A, all[3].B);
     }
     __syncthreads();
-    walk<Reset>(sh, a.words, a.batch, at.b, at.step, a.tiles, a.width, at.slab, a.h0);
+    walk<Reset>(sh, a.words, a.batch, at.b, at.step, a.tiles, a.width, slab, a.h0);
     const float4 enter = *reinterpret_cast<const float4*>(&sh.enter[wave][col * 4]);
     float h[4] = {enter.x, enter.y, enter.z, enter.w};
 #pragma unroll
@@ -402,7 +433,7 @@ __global__ __launch_bounds__(kFwdThreads, 4) void recurrence_kernel(RecurrenceAr
     float* final_h = a.final_h != nullptr ? a.final_h + at.b * a.width + ch : nullptr;
 #pragma unroll
     for (int j = 0; j < kFwdSub; ++j) {
-        if (any_hard<Reset>(hard[j])) {
+        if (cuts.any(j)) {
 #pragma unroll
             for (int v = 0; v < 4; ++v) h[v] = apply<true>(e[j][v], h[v]);
         } else {
@@ -479,10 +510,8 @@ struct Source<q8_t> {
 };
 
 // From e = exp(-x): sigma(x), and 1 - sigma(x) = e sigma(x) to its own accuracy.  Where e is
-// infinite the product counts as 0 (a multiplication that takes 0 times anything as 0) instead
-// of the 1 that it is: it only ever multiplies sigma(x), which is 0 there.
+// infinite the product counts as 0 instead of the 1 that it is: it only ever multiplies sigma(x), which is 0 there.
 __device__ __forceinline__ float gate_of(float e) { return __builtin_amdgcn_rcpf(1.0f + e); }
-__device__ float mul_zero_wins(float x, float y) __asm("llvm.amdgcn.fmul.legacy");
 __device__ __forceinline__ float rest_of(float e, float s) { return mul_zero_wins(e, s); }
 
 // What the walk back needs of an element, all that is kept of it in between.
@@ -498,7 +527,7 @@ constexpr bool kLean = sizeof(T) <= 2 && sizeof(Tg) == 2;
 
 template <bool Lean>
 struct BackwardShared {
-    WalkShared<kBwdWaves> walk;          // the walk back: its first wave is the workgroup's last
+    WalkShared<kBwdWaves, kJoinBack> walk;          // the walk back: its first wave is the workgroup's last
     float2 span[kBwdWaves][kCh];         // the waves' spans on the way forward
     float enter[kBwdWaves][kCh];
 };
@@ -517,19 +546,20 @@ __global__ __launch_bounds__(kBwdThreads, (kLean<T, Tg> ? 4 : 2)) void recurrenc
     constexpr bool Lean = kLean<T, Tg>;
     __shared__ BackwardShared<Lean> sh;
     const int slabs = int((a.width + kCh - 1) / kCh);
-    const Place at = place_of(a.words, a.tiles > 1, a.batch, slabs, sh.walk);
-    const int64_t tile = a.tiles - 1 - at.step;
+    const int slab = int(blockIdx.x) % slabs, ticket = draw_ticket(a.words, a.tiles > 1, slab, slabs);
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int row = lane / kAcross, col = lane % kAcross;
-    const int64_t ch0 = int64_t(at.slab) * kCh, ch = ch0 + col * 4;
+    const int64_t ch0 = int64_t(slab) * kCh, ch = ch0 + col * 4;
     const int n = int(max<int64_t>(0, min<int64_t>(4, a.width - ch)));
+    const Rates k = rates_of(a.theta, a.decay, ch, n);
+    const Place at = place_of(ticket, a.tiles > 1, a.batch, sh.walk);
+    const int64_t tile = a.tiles - 1 - at.step;
     const int64_t w0 = tile * kBwdTile + wave * 4 * kBwdSub;
     const int64_t token0 = at.b * a.seq_len + w0;
     const int left = there_are(a.seq_len - w0 - row * kBwdSub, kBwdSub);
 
     typename Source<T>::Raw rx[kBwdSub], rr[kBwdSub], ri[kBwdSub];
     typename Lane4<Tg>::Raw rd[kBwdSub];
-    bool hard[kBwdSub] = {};
     auto load_all = [&](int c4, auto count) {
         const Offset<Vec> d_off = Offset<Vec>(row * kBwdSub) * Offset<Vec>(a.width) + c4 * 4;
 #pragma unroll
@@ -545,11 +575,7 @@ __global__ __launch_bounds__(kBwdThreads, (kLean<T, Tg> ? 4 : 2)) void recurrenc
         load_all(n > 0 ? col : 0, [](int) { return 4; });
     else
         load_all(col, [&](int j) { return j < left ? n : 0; });
-    if constexpr (Reset) {
-#pragma unroll
-        for (int j = 0; j < kBwdSub; ++j) hard[j] = j < left && a.reset[token0 + row * kBwdSub + j] != 0;
-    }
-    const Rates k = rates_of(a.theta, a.decay, ch, n);
+    const Cuts<Reset, kBwdSub> cuts(a.reset + token0, a.seq_len - w0, row);
     // the lane's tokens: their factors, and what they do together to the state and, on the way
     // back, to its gradient
     Kept e[kBwdSub][4];
@@ -575,8 +601,8 @@ __global__ __launch_bounds__(kBwdThreads, (kLean<T, Tg> ? 4 : 2)) void recurrenc
             m[v] = __builtin_amdgcn_sqrtf(one_minus_square(z, q.a, 0x1p-120f));
             in[v] = gate_of(q.ei) * x[v];
         }
-        const bool cut = any_hard<Reset>(hard[j]);
-        if (cut && hard[j]) {
+        const bool cut = cuts.any(j);
+        if (cut && cuts.lane(j)) {
 #pragma unroll
             for (int v = 0; v < 4; ++v) e[j][v].a = -0.0f, m[v] = 1.0f;
         }
@@ -604,7 +630,7 @@ __global__ __launch_bounds__(kBwdThreads, (kLean<T, Tg> ? 4 : 2)) void recurrenc
         if (j < left) {   // a token past the end leaves the gradient alone
 #pragma unroll
             for (int v = 0; v < 4; ++v) bwd[v] = {bwd[v].A * e[j][v].a, e[j][v].a * (bwd[v].B + d[v])};   // c -> a (dy + c)
-            if (Reset && hard[j]) {
+            if (cuts.any(j) && cuts.lane(j)) {
 #pragma unroll
                 for (int v = 0; v < 4; ++v) bwd[v] = {-0.0f, 0.0f};   // a reset's c is 0 whatever comes after
             }
@@ -644,7 +670,7 @@ __global__ __launch_bounds__(kBwdThreads, (kLean<T, Tg> ? 4 : 2)) void recurrenc
             state = apply<Reset>({sh.span[w][lane].x, sh.span[w][lane].y}, state);
         }
     }
-    walk<Reset>(sh.walk, a.words, a.batch, at.b, at.step, a.tiles, a.width, at.slab, a.dfinal);
+    walk<Reset>(sh.walk, a.words, a.batch, at.b, at.step, a.tiles, a.width, slab, a.dfinal);
     float h[4], c[4], dth[4] = {0.f, 0.f, 0.f, 0.f};
     from_float4(*reinterpret_cast<const float4*>(&sh.enter[wave][col * 4]), h);
     from_float4(*reinterpret_cast<const float4*>(&sh.walk.enter[kBwdWaves - 1 - wave][col * 4]), c);
@@ -662,7 +688,7 @@ __global__ __launch_bounds__(kBwdThreads, (kLean<T, Tg> ? 4 : 2)) void recurrenc
     }
 #pragma unroll
     for (int j = 0; j < kBwdSub; ++j) {
-        const bool cut = any_hard<Reset>(hard[j]);
+        const bool cut = cuts.any(j);
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
             const Span in = {e[j][v].a, e[j][v].hp};
@@ -691,7 +717,7 @@ __global__ __launch_bounds__(kBwdThreads, (kLean<T, Tg> ? 4 : 2)) void recurrenc
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
             const Kept& q = e[j][v];
-            const bool cut = Reset && hard[j];
+            const bool cut = cuts.lane(j);
             const float s = gate_of(q.er), si = gate_of(q.ei);
             const float g = d[v] + c[v], ag = q.a * g;
             gx[v] = g * m[v] * si;
@@ -833,7 +859,7 @@ int64_t recurrence_tiles(int64_t seq_len) { return (seq_len + kFwdTile - 1) / kF
 int64_t recurrence_walk_bytes(int64_t batch, int64_t tiles, int64_t width)
 {
     if (tiles <= 1) return 0;
-    return (kTicketWords + batch * (tiles + tiles / kJoin) * width + 1) / 2 * 16;
+    return (ticket_words(width) + batch * (tiles + tiles / kJoinBack) * width + 1) / 2 * 16;   // kJoinBack is the smaller
 }
 
 hipError_t launch_recurrence(const RecurrenceArgs& a, hipStream_t stream)
