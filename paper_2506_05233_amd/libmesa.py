@@ -8,6 +8,7 @@ fallback.  Loading fails loudly when the built library is missing.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -173,6 +174,9 @@ def _dtype_code(t):
 
 def _check(t, name, shape, dtype=None, device=None):
     torch = _torch()
+    if (isinstance(t, torch.Tensor) and t.is_cuda and t.shape == shape and (dtype is None or t.dtype is dtype)
+            and (device is None or t.device == device) and t.is_contiguous()):
+        return
     if not isinstance(t, torch.Tensor):
         raise TypeError("%s must be a torch.Tensor" % name)
     if tuple(t.shape) != tuple(shape):
@@ -188,12 +192,21 @@ def _check(t, name, shape, dtype=None, device=None):
 
 
 def _ptr(t):
-    return None if t is None else ctypes.c_void_p(t.data_ptr())
+    return None if t is None else t.data_ptr()
+
+
+_raw_stream = None
 
 
 def _stream(device):
-    torch = _torch()
-    return ctypes.c_void_p(torch.cuda.current_stream(device).cuda_stream)
+    """torch's current HIP stream of the device, as the C ABI takes it."""
+    global _raw_stream
+    if _raw_stream is None:
+        torch = _torch()
+        # the handle itself: building a torch.cuda.Stream around it takes longer than a short call
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+            lambda index: torch.cuda.current_stream(index).cuda_stream)
+    return _raw_stream(device.index)
 
 
 def forward(q, k, v, gamma, beta, lam, n_cg, chunk=64, precision=MESA_PREC_AUTO, want_qstar=False,
@@ -565,22 +578,32 @@ def _row_stride(t, name):
     return row
 
 
+def _check_all(dtype, device, *items):
+    """_check of several (tensor, name, shape) of one dtype in one go."""
+    Tensor = _torch().Tensor
+    for t, name, shape in items:
+        if not (isinstance(t, Tensor) and t.shape == shape and t.dtype is dtype and t.device == device and t.is_contiguous()):
+            _check(t, name, shape, dtype, device)
+
+
 def _check_rows(t, name, shape, dtype, device):
     """As _check, for a tensor whose rows may be spaced; returns their stride."""
-    if tuple(t.shape) != tuple(shape):
+    if not isinstance(t, _torch().Tensor):
+        raise TypeError("%s must be a torch.Tensor" % name)
+    if t.shape != shape:
         raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
     if t.device != device:
         raise ValueError("%s is on %s, expected %s" % (name, t.device, device))
-    return _row_stride(t, name)
+    return shape[-1] if t.is_contiguous() else _row_stride(t, name)
 
 
 def _float_code(dtype, name):
     torch = _torch()
-    if dtype == torch.float32:
+    if dtype is torch.float32:
         return MESA_DTYPE_F32
-    if dtype == torch.bfloat16:
+    if dtype is torch.bfloat16:
         return MESA_DTYPE_BF16
     raise TypeError("%s must be float32 or bfloat16, got %s" % (name, dtype))
 
@@ -599,7 +622,8 @@ def _workspace(workspace, need, device):
         return None
     if workspace is not None and workspace.device == device and workspace.numel() * workspace.element_size() >= need:
         return workspace
-    return _torch().empty(need, dtype=_torch().uint8, device=device)
+    torch = _torch()
+    return torch.empty(need, dtype=torch.uint8, device=device)
 
 
 def checkpoint_bytes(rows, width) -> int:
@@ -610,34 +634,27 @@ class Checkpoint:
     """An 8-bit checkpoint of a tensor of `shape` ([..., width]): the device buffer that
     mesa_checkpoint_pack writes, about 1.03 bytes a value."""
 
-    __slots__ = ("buffer", "shape")
+    __slots__ = ("buffer", "shape", "rows", "width")
 
     def __init__(self, buffer, shape):
         torch = _torch()
-        self.shape = tuple(int(n) for n in shape)
+        self.shape = shape = tuple(int(n) for n in shape)
+        self.rows, self.width = math.prod(shape[:-1]), shape[-1]
         _on_device(buffer, "buffer")
-        if buffer.dtype != torch.uint8 or not buffer.is_contiguous() or buffer.numel() < checkpoint_bytes(self.rows, self.width):
-            raise ValueError("buffer must be a contiguous uint8 tensor of %d bytes" % checkpoint_bytes(self.rows, self.width))
+        need = checkpoint_bytes(self.rows, self.width)
+        if buffer.dtype != torch.uint8 or not buffer.is_contiguous() or buffer.numel() < need:
+            raise ValueError("buffer must be a contiguous uint8 tensor of %d bytes" % need)
         self.buffer = buffer
 
     @classmethod
     def empty(cls, shape, device):
+        """A checkpoint of that shape with nothing in it yet."""
         torch = _torch()
-        rows = 1
-        for n in shape[:-1]:
-            rows *= n
-        return cls(torch.empty(checkpoint_bytes(rows, shape[-1]), dtype=torch.uint8, device=device), shape)
-
-    @property
-    def width(self):
-        return self.shape[-1]
-
-    @property
-    def rows(self):
-        n = 1
-        for k in self.shape[:-1]:
-            n *= k
-        return n
+        ck = cls.__new__(cls)
+        ck.shape = shape = tuple(shape)
+        ck.rows, ck.width = math.prod(shape[:-1]), shape[-1]
+        ck.buffer = torch.empty(checkpoint_bytes(ck.rows, ck.width), dtype=torch.uint8, device=device)
+        return ck
 
     @property
     def device(self):
@@ -689,10 +706,10 @@ def checkpoint_unpack(ck, dtype=None, out=None):
 
 # ---------------------------------------------------------------- the gated recurrence
 def _common_stride(x, r, i, shape, dtype, device):
-    strides = [_check_rows(t, n, shape, dtype, device) for t, n in ((x, "x"), (r, "r"), (i, "i"))]
-    if strides[0] != strides[1] or strides[0] != strides[2]:
-        raise ValueError("x, r and i must have their rows equally spaced, got %s" % (strides,))
-    return strides[0]
+    stride = _check_rows(x, "x", shape, dtype, device)
+    if _check_rows(r, "r", shape, dtype, device) != stride or _check_rows(i, "i", shape, dtype, device) != stride:
+        raise ValueError("x, r and i must have their rows equally spaced")
+    return stride
 
 
 def recurrence_workspace_bytes(batch, seq_len, width) -> int:
@@ -752,13 +769,12 @@ def recurrence_step(state, x, r, i, theta, decay=8.0, reset=None, state_out=None
     dev = _on_device(x, "x")
     B, W = x.shape
     stride = _common_stride(x, r, i, (B, W), x.dtype, dev)
-    _check(state, "state", (B, W), torch.float32, dev)
-    _check(theta, "theta", (W,), torch.float32, dev)
+    _check_all(torch.float32, dev, (state, "state", (B, W)), (theta, "theta", (W,)))
     if reset is not None:
         _check(reset, "reset", (B,), torch.uint8, dev)
     if state_out is None:
         state_out = state
-    else:
+    elif state_out is not state:
         _check(state_out, "state_out", (B, W), torch.float32, dev)
     if out is None:
         out = torch.empty((B, W), dtype=x.dtype, device=dev)
@@ -795,8 +811,7 @@ def recurrence_backward(x, r, i, theta, states, dy, dfinal=None, decay=8.0, rese
         dev = _on_device(x, "x")
         code = _float_code(x.dtype, "x")
         stride = _common_stride(x, r, i, shape, x.dtype, dev)
-    _check(theta, "theta", (W,), f32, dev)
-    _check(states, "states", (B, -(-T // MESA_RECURRENCE_BLOCK), W), f32, dev)
+    _check_all(f32, dev, (theta, "theta", (W,)), (states, "states", (B, -(-T // MESA_RECURRENCE_BLOCK), W)))
     _check(dy, "dy", shape, device=dev)
     grad_code = _float_code(dy.dtype, "dy")
     if dfinal is not None:
@@ -804,13 +819,13 @@ def recurrence_backward(x, r, i, theta, states, dy, dfinal=None, decay=8.0, rese
     if reset is not None:
         _check(reset, "reset", (B, T), torch.uint8, dev)
     if out is None:
-        out = tuple(torch.empty(shape, dtype=dy.dtype, device=dev) for _ in range(3))
+        out = (torch.empty_like(dy), torch.empty_like(dy), torch.empty_like(dy))
         grad_stride = W
     else:
         grad_stride = _common_stride(*out, shape, dy.dtype, dev)
     need = lib.mesa_recurrence_backward_workspace_bytes(B, T, W)
     workspace = _workspace(workspace, need, dev)
-    res = {"dx": out[0], "dr": out[1], "di": out[2], "dtheta": torch.empty((W,), dtype=f32, device=dev),
+    res = {"dx": out[0], "dr": out[1], "di": out[2], "dtheta": torch.empty_like(theta),
            "dh0": torch.empty((B, W), dtype=f32, device=dev)}
     st = lib.mesa_recurrence_backward(_ptr(x), _ptr(r), _ptr(i), _ptr(theta), float(decay), _ptr(reset), _ptr(states),
                                       _ptr(dy), _ptr(dfinal), B, T, W, stride, code, grad_code, grad_stride, _ptr(out[0]),
@@ -860,18 +875,21 @@ def frontend_backward(qp, kp, vp, conv_q, conv_k, conv_v, a_gamma, a_beta, theta
     qp = _held(qp, "qp", (B, T, H, dk_), dtype, dev)
     kp = _held(kp, "kp", (B, T, H, dk_), dtype, dev)
     vp = _held(vp, "vp", (B, T, H, dv_), dtype, dev)
-    for t, n, shape in ((conv_q, "conv_q", (H * dk_, 4)), (conv_k, "conv_k", (H * dk_, 4)), (conv_v, "conv_v", (H * dv_, 4)),
-                        (a_gamma, "a_gamma", (B, T, H)), (a_beta, "a_beta", (B, T, H)), (theta, "theta", (H, dk_)),
-                        (dq, "dq", (B, H, T, dk_)), (dk, "dk", (B, H, T, dk_)), (dv, "dv", (B, H, T, dv_)),
-                        (dgamma, "dgamma", (B, H, T)), (dbeta, "dbeta", (B, H, T)), (dlam, "dlam", (H, dk_))):
-        if t is not None or n != "conv_v":
-            _check(t, n, shape, f32, dev)
-    new = lambda dt, *shape: torch.empty(shape, dtype=dt, device=dev)
-    res = {"dqp": new(grad_dtype, B, T, H, dk_), "dkp": new(grad_dtype, B, T, H, dk_), "dvp": new(grad_dtype, B, T, H, dv_),
-           "dconv_q": new(f32, H * dk_, 4), "dconv_k": new(f32, H * dk_, 4)}
+    gates, outs = (B, T, H), (B, H, T)
+    _check_all(f32, dev, (conv_q, "conv_q", (H * dk_, 4)), (conv_k, "conv_k", (H * dk_, 4)), (a_gamma, "a_gamma", gates),
+               (a_beta, "a_beta", gates), (theta, "theta", (H, dk_)), (dq, "dq", (B, H, T, dk_)), (dk, "dk", (B, H, T, dk_)),
+               (dv, "dv", (B, H, T, dv_)), (dgamma, "dgamma", outs), (dbeta, "dbeta", outs), (dlam, "dlam", (H, dk_)))
     if conv_v is not None:
-        res["dconv_v"] = new(f32, H * dv_, 4)
-    res["da_gamma"], res["da_beta"], res["dtheta"] = new(f32, B, T, H), new(f32, B, T, H), new(f32, H, dk_)
+        _check_all(f32, dev, (conv_v, "conv_v", (H * dv_, 4)))
+    like = torch.empty_like     # quicker than torch.empty, and every gradient has its input's shape
+    if q8:
+        grads = [torch.empty(t, dtype=grad_dtype, device=dev) for t in ((B, T, H, dk_), (B, T, H, dk_), (B, T, H, dv_))]
+    else:
+        grads = [like(t, dtype=grad_dtype) for t in (qp, kp, vp)]
+    res = {"dqp": grads[0], "dkp": grads[1], "dvp": grads[2], "dconv_q": like(conv_q), "dconv_k": like(conv_k)}
+    if conv_v is not None:
+        res["dconv_v"] = like(conv_v)
+    res["da_gamma"], res["da_beta"], res["dtheta"] = like(a_gamma), like(a_beta), like(theta)
     need = lib.mesa_frontend_backward_workspace_bytes(B, H, T, dk_, dv_)
     workspace = _workspace(workspace, need, dev)
     st = lib.mesa_frontend_backward(_ptr(qp), _ptr(kp), _ptr(vp), _ptr(conv_q), _ptr(conv_k), _ptr(conv_v), _ptr(a_gamma),
@@ -903,7 +921,8 @@ def output_norm_backward(o, weight, dy, eps=1e-6, workspace=None):
     o = _held(o, "o", (B, H, T, dv_), None if q8 else f32, dev)
     _check(weight, "weight", (H, dv_), f32, dev)
     _check(dy, "dy", (B, T, H, dv_), device=dev)
-    res = {"do": torch.empty((B, H, T, dv_), dtype=f32, device=dev), "dweight": torch.empty((H, dv_), dtype=f32, device=dev)}
+    res = {"do": torch.empty((B, H, T, dv_), dtype=f32, device=dev) if q8 else torch.empty_like(o),
+           "dweight": torch.empty_like(weight)}
     need = lib.mesa_output_norm_backward_workspace_bytes(B, H, T, dv_)
     workspace = _workspace(workspace, need, dev)
     st = lib.mesa_output_norm_backward(_ptr(o), _ptr(weight), float(eps), _ptr(dy), B, H, T, dv_,
