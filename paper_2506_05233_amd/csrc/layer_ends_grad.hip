@@ -45,11 +45,19 @@ int64_t blocks_of(int64_t seq_len, int d, int run)
     return (seq_len + per - 1) / per;
 }
 
+// Sum over the 16 or 32 consecutive lanes of a group; every lane of it receives the sum.
 template <int L>
 __device__ __forceinline__ float group_sum(float v)
 {
-#pragma unroll
-    for (int m = L / 2; m >= 1; m /= 2) v += __shfl_xor(v, m);
+    static_assert(L == 16 || L == 32, "a row of lanes, or two");
+    v += dpp_f32<kDppQuadSwap1>(v, v);
+    v += dpp_f32<kDppQuadSwap2>(v, v);
+    v += dpp_f32<kDppRowRor4>(v, v);
+    v += dpp_f32<kDppRowRor8>(v, v);
+    if constexpr (L == 32) {
+        const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(s[0]) + __uint_as_float(s[1]);
+    }
     return v;
 }
 
@@ -66,7 +74,7 @@ struct Held<q8_t> {
     using Raw = Q8Raw;
     __device__ static Raw load(const void* base, int64_t bytes, int64_t at)
     {
-        return {load_codes<true>(static_cast<const int8_t*>(base) + at, 4), static_cast<const uint8_t*>(base)[bytes + at / kGroup]};
+        return {*reinterpret_cast<const uint32_t*>(static_cast<const int8_t*>(base) + at), static_cast<const uint8_t*>(base)[bytes + at / kGroup]};
     }
     __device__ static void widen(const Raw& r, float (&x)[4]) { widen_q8(r.codes, group_scale(r.byte), x); }
 };

@@ -77,6 +77,9 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
 
 // Four channels of one token.  Vec: the address is aligned to the four elements and all four
 // exist; otherwise n (0..4) of them are read or written one by one, the others read as 0.
+// load_near reads channels ch .. ch + 3 of the row at element `row`, the row's last channel
+// in the place of those past it (and, with Vec, its slab's first four, ch0, in the place of
+// four that are), so that it asks nothing.
 template <typename T>
 struct Lane4;
 
@@ -89,6 +92,13 @@ struct Lane4<float> {
         const float* p = static_cast<const float*>(base) + at;
         if constexpr (Vec) return n > 0 ? *reinterpret_cast<const float4*>(p) : make_float4(0.f, 0.f, 0.f, 0.f);
         return make_float4(n > 0 ? p[0] : 0.f, n > 1 ? p[1] : 0.f, n > 2 ? p[2] : 0.f, n > 3 ? p[3] : 0.f);
+    }
+    template <bool Vec>
+    __device__ static Raw load_near(const void* base, int64_t row, int64_t ch, int64_t ch0, int64_t last)
+    {
+        const float* p = static_cast<const float*>(base) + row;
+        if constexpr (Vec) return *reinterpret_cast<const float4*>(p + (ch <= last ? ch : ch0));
+        return make_float4(p[min(ch, last)], p[min(ch + 1, last)], p[min(ch + 2, last)], p[min(ch + 3, last)]);
     }
     __device__ static void widen(const Raw& r, float (&x)[4]) { x[0] = r.x, x[1] = r.y, x[2] = r.z, x[3] = r.w; }
     template <bool Vec>
@@ -115,6 +125,14 @@ struct Lane4<bf16_t> {
         if constexpr (Vec) return n > 0 ? *reinterpret_cast<const uint2*>(p) : make_uint2(0u, 0u);
         const uint32_t a = n > 0 ? p[0] : 0u, b = n > 1 ? p[1] : 0u, c = n > 2 ? p[2] : 0u, d = n > 3 ? p[3] : 0u;
         return make_uint2(a | (b << 16), c | (d << 16));
+    }
+    template <bool Vec>
+    __device__ static Raw load_near(const void* base, int64_t row, int64_t ch, int64_t ch0, int64_t last)
+    {
+        const uint16_t* p = static_cast<const uint16_t*>(base) + row;
+        if constexpr (Vec) return *reinterpret_cast<const uint2*>(p + (ch <= last ? ch : ch0));
+        return make_uint2(p[min(ch, last)] | (uint32_t(p[min(ch + 1, last)]) << 16),
+                          p[min(ch + 2, last)] | (uint32_t(p[min(ch + 3, last)]) << 16));
     }
     __device__ static void widen(const Raw& r, float (&x)[4])
     {
@@ -155,10 +173,11 @@ __device__ __forceinline__ uint32_t load_codes_scalar(const int8_t* p, int n)
     return w;
 }
 template <bool Vec>
-__device__ __forceinline__ uint32_t load_codes(const int8_t* p, int n)
+__device__ __forceinline__ uint32_t load_codes_near(const int8_t* p, int64_t ch, int64_t ch0, int64_t last)
 {
-    if constexpr (Vec) return n > 0 ? *reinterpret_cast<const uint32_t*>(p) : 0u;
-    return load_codes_scalar(p, n);
+    if constexpr (Vec) return *reinterpret_cast<const uint32_t*>(p + (ch <= last ? ch : ch0));
+    return uint8_t(p[min(ch, last)]) | (uint32_t(uint8_t(p[min(ch + 1, last)])) << 8) | (uint32_t(uint8_t(p[min(ch + 2, last)])) << 16) |
+           (uint32_t(uint8_t(p[min(ch + 3, last)])) << 24);
 }
 
 // sigma(x); exp(-x) = inf gives 0

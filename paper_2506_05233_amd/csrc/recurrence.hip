@@ -273,10 +273,10 @@ constexpr int64_t kNearStride = int64_t(1) << 22;
 template <bool Vec>
 using Offset = std::conditional_t<Vec, uint32_t, int64_t>;
 
-template <typename T, bool Vec>
-__device__ __forceinline__ typename Lane4<T>::Raw load_row(const void* base, int64_t row, Offset<Vec> off, int n)
+template <typename T>
+__device__ __forceinline__ typename Lane4<T>::Raw load_row(const void* base, int64_t row, int64_t off)
 {
-    return Lane4<T>::template load<Vec>(static_cast<const T*>(base) + row, off, n);
+    return Lane4<T>::template load<true>(static_cast<const T*>(base) + row, off, 4);
 }
 
 // How many of `most` tokens exist when n are left (which may be none or fewer).
@@ -335,24 +335,26 @@ __global__ __launch_bounds__(kFwdThreads, (Vec ? 4 : 2)) void recurrence_kernel(
     const int left = there_are(a.seq_len - w0 - row * kFwdSub, kFwdSub);  // of the lane's tokens
 
     // Tokens past the end come after all others, so the state that they would leave is used by
-    // nobody.  A wave whose tokens all exist reads without asking; its lanes past the last
-    // channel read the slab's first, for nothing.
+    // nobody: they and channels past the last are read as copies of existing ones.
     typename Lane4<T>::Raw rx[kFwdSub], rr[kFwdSub], ri[kFwdSub];
-    auto load_all = [&](int c4, auto count) {
-        const Offset<Vec> off = Offset<Vec>(row * kFwdSub) * Offset<Vec>(a.stride) + c4 * 4;
+    if (Vec && w0 + 4 * kFwdSub <= a.seq_len) {
+        const Offset<Vec> off = Offset<Vec>(row * kFwdSub) * Offset<Vec>(a.stride) + (n > 0 ? col * 4 : 0);
 #pragma unroll
         for (int j = 0; j < kFwdSub; ++j) {
-            const int m = count(j);
             const int64_t at_row = (token0 + j) * a.stride + ch0;
-            rx[j] = load_row<T, Vec>(a.x, at_row, off, m);
-            rr[j] = load_row<T, Vec>(a.r, at_row, off, m);
-            ri[j] = load_row<T, Vec>(a.i, at_row, off, m);
+            rx[j] = load_row<T>(a.x, at_row, off);
+            rr[j] = load_row<T>(a.r, at_row, off);
+            ri[j] = load_row<T>(a.i, at_row, off);
         }
-    };
-    if (Vec && w0 + 4 * kFwdSub <= a.seq_len)
-        load_all(n > 0 ? col : 0, [](int) { return 4; });
-    else
-        load_all(col, [&](int j) { return j < left ? n : 0; });
+    } else {
+#pragma unroll
+        for (int j = 0; j < kFwdSub; ++j) {
+            const int64_t at_row = (at.b * a.seq_len + min<int64_t>(w0 + row * kFwdSub + j, a.seq_len - 1)) * a.stride;
+            rx[j] = Lane4<T>::template load_near<Vec>(a.x, at_row, ch, ch0, a.width - 1);
+            rr[j] = Lane4<T>::template load_near<Vec>(a.r, at_row, ch, ch0, a.width - 1);
+            ri[j] = Lane4<T>::template load_near<Vec>(a.i, at_row, ch, ch0, a.width - 1);
+        }
+    }
     const Cuts<Reset, kFwdSub> cuts(a.reset + token0, a.seq_len - w0, row);
     if constexpr (Kept) {
         uint8_t* const kept[3] = {a.kept_x, a.kept_r, a.kept_i};
@@ -476,15 +478,19 @@ constexpr int kBwdWaves = kBwdThreads / kWave;
 constexpr int kBwdTile = kBwdWaves * 4 * kBwdSub;
 static_assert(kBwdTile == kBlock, "a tile of the backward pass starts at a kept state");
 
-// x, r or i of the backward pass: a tensor of T, or a checkpoint.  `token` is the wave's
-// token, `row` the lane's tokens from there.
+// x, r or i of the backward pass: a tensor of T, or a checkpoint.  load: the token `row` tokens
+// from the wave's own, at 4 c4 channels from the slab's first; load_near: any token.
 template <typename T>
 struct Source {
     using Raw = typename Lane4<T>::Raw;
-    template <bool Vec>
-    __device__ static Raw load(const void* base, const RecurrenceGradArgs& a, int64_t token, int row, int64_t ch0, int col, int n)
+    __device__ static Raw load(const void* base, const RecurrenceGradArgs& a, int64_t token, int row, int64_t ch0, int c4)
     {
-        return load_row<T, Vec>(base, token * a.stride + ch0, Offset<Vec>(row) * Offset<Vec>(a.stride) + col * 4, n);
+        return load_row<T>(base, token * a.stride + ch0, uint32_t(row) * uint32_t(a.stride) + c4 * 4);
+    }
+    template <bool Vec>
+    __device__ static Raw load_near(const void* base, const RecurrenceGradArgs& a, int64_t token, int64_t ch, int64_t ch0)
+    {
+        return Lane4<T>::template load_near<Vec>(base, token * a.stride, ch, ch0, a.width - 1);
     }
     // the values times `by`
     __device__ static void widen(const Raw& r, float by, float (&x)[4])
@@ -497,14 +503,20 @@ struct Source {
 template <>
 struct Source<q8_t> {
     using Raw = Q8Raw;
-    template <bool Vec>
-    __device__ static Raw load(const void* base, const RecurrenceGradArgs& a, int64_t token, int row, int64_t ch0, int col, int n)
+    __device__ static Raw load(const void* base, const RecurrenceGradArgs& a, int64_t token, int row, int64_t ch0, int c4)
     {
-        if (n <= 0) return {0u, 0u};
         const int64_t groups = (a.width + kGroup - 1) / kGroup;
         const int8_t* codes = static_cast<const int8_t*>(base) + token * a.width + ch0;
         const uint8_t* bytes = static_cast<const uint8_t*>(base) + checkpoint_exponents_at(a.batch * a.seq_len, a.width) + token * groups + ch0 / kGroup;
-        return {load_codes<Vec>(codes + Offset<Vec>(row) * Offset<Vec>(a.width) + col * 4, n), bytes[Offset<Vec>(row) * Offset<Vec>(groups) + col / 8]};
+        return {*reinterpret_cast<const uint32_t*>(codes + (uint32_t(row) * uint32_t(a.width) + c4 * 4)), bytes[uint32_t(row) * uint32_t(groups) + c4 / 8]};
+    }
+    template <bool Vec>
+    __device__ static Raw load_near(const void* base, const RecurrenceGradArgs& a, int64_t token, int64_t ch, int64_t ch0)
+    {
+        const int64_t groups = (a.width + kGroup - 1) / kGroup;
+        const uint8_t* bytes = static_cast<const uint8_t*>(base) + checkpoint_exponents_at(a.batch * a.seq_len, a.width);
+        return {load_codes_near<Vec>(static_cast<const int8_t*>(base) + token * a.width, ch, ch0, a.width - 1),
+                bytes[token * groups + min(ch, a.width - 1) / kGroup]};
     }
     __device__ static void widen(const Raw& r, float by, float (&x)[4]) { widen_q8(r.codes, group_scale(r.byte) * by, x); }
 };
@@ -560,21 +572,26 @@ __global__ __launch_bounds__(kBwdThreads, (kLean<T, Tg> ? 4 : 2)) void recurrenc
 
     typename Source<T>::Raw rx[kBwdSub], rr[kBwdSub], ri[kBwdSub];
     typename Lane4<Tg>::Raw rd[kBwdSub];
-    auto load_all = [&](int c4, auto count) {
-        const Offset<Vec> d_off = Offset<Vec>(row * kBwdSub) * Offset<Vec>(a.width) + c4 * 4;
+    if (Vec && w0 + 4 * kBwdSub <= a.seq_len) {
+        const int c4 = n > 0 ? col : 0;
 #pragma unroll
         for (int j = 0; j < kBwdSub; ++j) {
-            const int m = count(j);
-            rr[j] = Source<T>::template load<Vec>(a.r, a, token0 + j, row * kBwdSub, ch0, c4, m);
-            rx[j] = Source<T>::template load<Vec>(a.x, a, token0 + j, row * kBwdSub, ch0, c4, m);
-            ri[j] = Source<T>::template load<Vec>(a.i, a, token0 + j, row * kBwdSub, ch0, c4, m);
-            rd[j] = load_row<Tg, Vec>(a.dy, (token0 + j) * a.width + ch0, d_off, m);
+            rr[j] = Source<T>::load(a.r, a, token0 + j, row * kBwdSub, ch0, c4);
+            rx[j] = Source<T>::load(a.x, a, token0 + j, row * kBwdSub, ch0, c4);
+            ri[j] = Source<T>::load(a.i, a, token0 + j, row * kBwdSub, ch0, c4);
+            rd[j] = load_row<Tg>(a.dy, (token0 + j) * a.width + ch0, uint32_t(row * kBwdSub) * uint32_t(a.width) + c4 * 4);
         }
-    };
-    if (Vec && w0 + 4 * kBwdSub <= a.seq_len)
-        load_all(n > 0 ? col : 0, [](int) { return 4; });
-    else
-        load_all(col, [&](int j) { return j < left ? n : 0; });
+    } else {
+        // tokens past the end and channels past the last are read as copies of existing ones
+#pragma unroll
+        for (int j = 0; j < kBwdSub; ++j) {
+            const int64_t token = at.b * a.seq_len + min<int64_t>(w0 + row * kBwdSub + j, a.seq_len - 1);
+            rr[j] = Source<T>::template load_near<Vec>(a.r, a, token, ch, ch0);
+            rx[j] = Source<T>::template load_near<Vec>(a.x, a, token, ch, ch0);
+            ri[j] = Source<T>::template load_near<Vec>(a.i, a, token, ch, ch0);
+            rd[j] = Lane4<Tg>::template load_near<Vec>(a.dy, token * a.width, ch, ch0, a.width - 1);
+        }
+    }
     const Cuts<Reset, kBwdSub> cuts(a.reset + token0, a.seq_len - w0, row);
     // the lane's tokens: their factors, and what they do together to the state and, on the way
     // back, to its gradient
