@@ -107,7 +107,7 @@ __device__ void stream_grad(const FrontGradArgs& a, int kind, int64_t bh, int64_
             for (int u = 0; u < kBatch; ++u) {
                 const int64_t t = t0 + s + u;
                 const float y[4] = {g[u].x, g[u].y, g[u].z, g[u].w};
-                if (t < t1) Lane4<Tg>::template store<true>(dst, at0 + t * stride, 4, y);
+                if (t < t1) stream_store(static_cast<Tg*>(dst) + at0 + t * stride, Lane4<Tg>::narrow(y));
             }
         }
         return;
@@ -181,7 +181,8 @@ __device__ void stream_grad(const FrontGradArgs& a, int kind, int64_t bh, int64_
                 du[c][2] = du[c][1], du[c][1] = du[c][0], du[c][0] = d;
                 prev[c][2] = prev[c][1], prev[c][1] = prev[c][0], prev[c][0] = x[c];
             }
-            if (t - kHalo >= t0 && t - kHalo < t1) Lane4<Tg>::template store<true>(dst, at0 + (t - kHalo) * stride, 4, dp);
+            if (t - kHalo >= t0 && t - kHalo < t1)
+                stream_store(static_cast<Tg*>(dst) + at0 + (t - kHalo) * stride, Lane4<Tg>::narrow(dp));
         }
     }
     // the workgroup's runs added: red[group][channel][tap]

@@ -169,4 +169,28 @@ __device__ __forceinline__ T load_at(const void* base, uint32_t byte_off)
     return *reinterpret_cast<const T*>(static_cast<const char*>(base) + byte_off);
 }
 
+// A store of 4, 8 or 16 bytes that passes through the L2 without staying there.  For results
+// written a piece of a row at a time, which otherwise wait for the L2's write-backs (three 67 MB
+// gradients in pieces of 128 bytes: 133 us, 106 with these); where a workgroup writes one run
+// of memory ordinary stores are the faster (a 134 MB gradient: 42 us, 50 with these).
+template <typename T>
+__device__ __forceinline__ void stream_store(void* p, const T& x)
+{
+    static_assert(sizeof(T) == 4 || sizeof(T) == 8 || sizeof(T) == 16, "a register or two or four");
+    typedef uint32_t words __attribute__((ext_vector_type(sizeof(T) / 4)));
+    __builtin_nontemporal_store(__builtin_bit_cast(words, x), static_cast<words*>(p));
+}
+
+// load_at's counterpart, streaming (a byte: an ordinary store).
+template <typename T>
+__device__ __forceinline__ void store_at(void* base, uint32_t byte_off, const T& x)
+{
+    asm volatile("" : "+v"(byte_off));
+    void* const p = static_cast<char*>(base) + byte_off;
+    if constexpr (sizeof(T) == 1)
+        *static_cast<T*>(p) = x;
+    else
+        stream_store(p, x);
+}
+
 }  // namespace mesa

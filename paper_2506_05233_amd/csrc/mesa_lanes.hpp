@@ -101,6 +101,7 @@ struct Lane4<float> {
         return make_float4(p[min(ch, last)], p[min(ch + 1, last)], p[min(ch + 2, last)], p[min(ch + 3, last)]);
     }
     __device__ static void widen(const Raw& r, float (&x)[4]) { x[0] = r.x, x[1] = r.y, x[2] = r.z, x[3] = r.w; }
+    __device__ static float4 narrow(const float (&y)[4]) { return make_float4(y[0], y[1], y[2], y[3]); }
     template <bool Vec>
     __device__ static void store(void* base, int64_t at, int n, const float (&y)[4])
     {
@@ -139,6 +140,7 @@ struct Lane4<bf16_t> {
         x[0] = __uint_as_float(r.x << 16), x[1] = __uint_as_float(r.x & 0xFFFF0000u);
         x[2] = __uint_as_float(r.y << 16), x[3] = __uint_as_float(r.y & 0xFFFF0000u);
     }
+    __device__ static uint2 narrow(const float (&y)[4]) { return make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])); }
     template <bool Vec>
     __device__ static void store(void* base, int64_t at, int n, const float (&y)[4])
     {

@@ -14,8 +14,8 @@
 // A span of tokens acts on the state as h -> A h + B, and spans compose, so time is cut:
 // a lane holds kSub consecutive tokens of four channels in registers, a row of 16 lanes a
 // token's 64 channels (128 bytes of bf16), a workgroup 32 such runs in time.  The runs'
-// (A, B) are joined inside a wave by row swaps, across waves in LDS, across workgroups
-// through the workspace (below), so every input is read once.  A reset inside a span is
+// (A, B) meet in LDS, where one wave passes through them with a channel in each lane, and
+// across workgroups in the workspace (below), so every input is read once.  A reset inside a span is
 // kept as the sign of A (A is never negative otherwise), since 0 times a state that is not
 // finite would not forget it.  All of it is fp32 and in a fixed order.
 #include <algorithm>
@@ -33,6 +33,9 @@ namespace {
 
 constexpr int kAcross = 16;            // lanes across a token's channels
 constexpr int kCh = 4 * kAcross;       // channels of a workgroup
+constexpr int kWaveRows = kWave / kAcross;   // runs of tokens of a wave, one to a row of lanes
+constexpr int kRows = 32;                    // of a workgroup
+constexpr int kWaves = kRows / kWaveRows, kThreads = kWaves * kWave;
 constexpr int kBlock = kRecurrenceBlock;
 
 // What a span of tokens does to the state.
@@ -53,37 +56,6 @@ __device__ __forceinline__ Span join(Span lo, Span hi)
     return {hard ? hi.A : lo.A * hi.A, apply<Reset>(hi, lo.B)};
 }
 __device__ __forceinline__ Span nothing() { return {1.0f, 0.0f}; }
-
-// Rows (16 lanes) r of a wave: out lo[r] = v[r & ~1], hi[r] = v[r | 1]; and for pairs of rows.
-__device__ __forceinline__ void swap_rows(float v, float& lo, float& hi)
-{
-    const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    lo = __uint_as_float(s[0]), hi = __uint_as_float(s[1]);
-}
-__device__ __forceinline__ void swap_halves(float v, float& lo, float& hi)
-{
-    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    lo = __uint_as_float(s[0]), hi = __uint_as_float(s[1]);
-}
-
-// Joins the spans of a wave's four rows in time order (Back: from the last row to the
-// first): `before` the span of the rows that come before the lane's own, `all` that of all.
-template <bool Reset, bool Back>
-__device__ __forceinline__ void join_rows(Span own, int row, Span& before, Span& all)
-{
-    Span lo, hi;
-    swap_rows(own.A, lo.A, hi.A);
-    swap_rows(own.B, lo.B, hi.B);
-    const bool second = Back ? (row & 1) == 0 : (row & 1) != 0;
-    before = second ? (Back ? hi : lo) : nothing();
-    const Span pair = Back ? join<Reset>(hi, lo) : join<Reset>(lo, hi);
-    Span plo, phi;
-    swap_halves(pair.A, plo.A, phi.A);
-    swap_halves(pair.B, plo.B, phi.B);
-    const bool later = Back ? row < 2 : row >= 2;
-    if (later) before = join<Reset>(Back ? phi : plo, before);
-    all = Back ? join<Reset>(phi, plo) : join<Reset>(plo, phi);
-}
 
 // The per-channel constants: log2 a_t = rate * s_t.
 struct Rates {
@@ -137,10 +109,12 @@ __device__ __forceinline__ Span terms(float x, float r, float i, float rate, boo
 // of workgroups that fit the GPU.  A span and its "published" mark are one 8-byte word
 // written and read with single relaxed accesses of agent scope, so no other memory has to be
 // ordered.  The words start as kUnset, written by a fill kernel ahead on the stream.
-constexpr int kJoinOn = 32, kJoinBack = 8;   // forward; backward, whose shared memory is full
+constexpr int kJoinOn = 32, kJoinBack = 16;   // forward; backward, with less shared memory to spare
 constexpr uint64_t kUnset = ~uint64_t(0);
-// 64-bit words of the ticket counters (32 bits for each slab of channels), ahead of the spans
-__host__ __device__ inline int64_t ticket_words(int64_t width) { return (width + 2 * kCh - 1) / (2 * kCh); }
+// Ticket counters, one for each slab of channels, ahead of the spans: each in a cache line of
+// its own (the GPU's dies draw from one line one at a time), in 64-bit words.
+constexpr int kCounterWords = 16;
+__host__ __device__ inline int64_t ticket_words(int64_t width) { return (width + kCh - 1) / kCh * kCounterWords; }
 
 __device__ __forceinline__ void publish(uint64_t* at, Span s)
 {
@@ -166,16 +140,49 @@ __global__ __launch_bounds__(256) void recurrence_fill_kernel(ulonglong2* words,
     for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < n; i += int64_t(gridDim.x) * 256) words[i] = make_ulonglong2(kUnset, kUnset);
 }
 
-// Shared memory of a walk: the spans of a workgroup's waves, what comes before them, and the
-// state entering every wave.
-template <int Waves, int kJoin>
+// Shared memory of a walk: the spans of the lane rows (four to a wave) of a workgroup in
+// planes of A and B, in the order of the walk, and the spans of the tiles before it.  The
+// state entering a row takes the place of its B.
+struct RowSpans {
+    float A[kRows][kCh], B[kRows][kCh];
+
+    __device__ void put(int r, int col, const Span (&s)[4])
+    {
+        *reinterpret_cast<float4*>(&A[r][col * 4]) = make_float4(s[0].A, s[1].A, s[2].A, s[3].A);
+        *reinterpret_cast<float4*>(&B[r][col * 4]) = make_float4(s[0].B, s[1].B, s[2].B, s[3].B);
+    }
+    __device__ void entering(int r, int col, float (&h)[4]) const
+    {
+        const float4 f = *reinterpret_cast<const float4*>(&B[r][col * 4]);
+        h[0] = f.x, h[1] = f.y, h[2] = f.z, h[3] = f.w;
+    }
+    // for a wave whose lanes take a channel each: all rows together, and from the state ahead
+    // of them the one that enters each; returns the one that leaves them
+    template <bool Reset>
+    __device__ Span all(int lane) const
+    {
+        Span s = nothing();
+#pragma unroll 8
+        for (int r = 0; r < kRows; ++r) s = join<Reset>(s, {A[r][lane], B[r][lane]});
+        return s;
+    }
+    template <bool Reset>
+    __device__ float pass(int lane, float h)
+    {
+#pragma unroll 8
+        for (int r = 0; r < kRows; ++r) {
+            const Span s = {A[r][lane], B[r][lane]};
+            B[r][lane] = h;
+            h = apply<Reset>(s, h);
+        }
+        return h;
+    }
+};
+template <int kJoin>
 struct WalkShared {
-    float2 span[Waves][kCh];
+    RowSpans rows;
     float2 before[kJoin][kCh];
-    union {
-        float enter[Waves][kCh];
-        int ticket;              // read by all before the first barrier of the walk
-    };
+    int ticket;
 };
 
 // The workgroup's place in the call.  Its slab of channels goes by its index, so that the
@@ -190,7 +197,7 @@ __device__ __forceinline__ int draw_ticket(uint64_t* words, bool many, int slab,
 {
     if (!many) return int(blockIdx.x) / slabs;
     if (threadIdx.x != 0) return 0;
-    return int(__hip_atomic_fetch_add(reinterpret_cast<uint32_t*>(words) + slab, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1u);
+    return int(__hip_atomic_fetch_add(reinterpret_cast<uint32_t*>(words + slab * kCounterWords), 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1u);
 }
 template <class Shared>
 __device__ __forceinline__ Place place_of(int ticket, bool many, int64_t batch, Shared& sh)
@@ -204,28 +211,30 @@ __device__ __forceinline__ Place place_of(int ticket, bool many, int64_t batch, 
     return {int64_t(id - step * uint32_t(batch)), int(step)};
 }
 
-// From the waves' spans (in the order of the walk, written by their first lanes and made
-// visible by a barrier) the state entering each of them, in sh.enter after the barrier at
-// the end.  `step` is the tile's place in the walk, `first` the state ahead of the whole walk.
-template <bool Reset, int Waves, int kJoin>
-__device__ __forceinline__ void walk(WalkShared<Waves, kJoin>& sh, uint64_t* words, int64_t batch, int64_t b, int step, int steps,
+// From the rows' spans (made visible by a barrier) the state entering each of them, after the
+// barrier at the end.  `step` is the tile's place in the walk, `first` the state ahead of the
+// whole walk.  The first wave passes through the rows; the others' time is the compute unit's
+// second workgroup's.
+template <bool Reset, int kJoin>
+__device__ __forceinline__ void walk(WalkShared<kJoin>& sh, uint64_t* words, int64_t batch, int64_t b, int step, int steps,
                                      int64_t width, int slab, const float* first)
 {
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int64_t ch = int64_t(slab) * kCh + lane;
-    const bool mine = ch < width;
+    const bool mine = lane < kCh && ch < width;
     const int group = step / kJoin, at = step % kJoin;
     const int groups = steps / kJoin;
     uint64_t* spans = words + ticket_words(width) + b * steps * width + ch;
     uint64_t* leaves = words + ticket_words(width) + batch * steps * width + b * groups * width + ch;
-    if (wave == 0 && at != kJoin - 1 && step + 1 < steps) {
-        Span s = nothing();
-#pragma unroll
-        for (int w = 0; w < Waves; ++w) s = join<Reset>(s, {sh.span[w][lane].x, sh.span[w][lane].y});
+    if (wave == 0 && lane < kCh && at != kJoin - 1 && step + 1 < steps) {
+        __builtin_amdgcn_s_setprio(3);   // other workgroups wait for it
+        const Span s = sh.rows.template all<Reset>(lane);
         if (mine) publish(spans + int64_t(step) * width, s);
+        __builtin_amdgcn_s_setprio(0);
     }
-    // entry 0 is the state entering the group, entry e the span of the group's tile e - 1
-    for (int e = wave; e <= at; e += Waves) {
+    // entry 0 is the state entering the group, entry e the span of the group's tile e - 1; the
+    // first wave, which publishes, comes last
+    for (int e = kWaves - 1 - wave; e <= at; e += kWaves) {
         Span s;
         if (e > 0)
             s = await(spans + int64_t(group * kJoin + e - 1) * width, mine);
@@ -233,18 +242,14 @@ __device__ __forceinline__ void walk(WalkShared<Waves, kJoin>& sh, uint64_t* wor
             s = await(leaves + int64_t(group - 1) * width, mine);
         else
             s = {-0.0f, first != nullptr && mine ? first[b * width + ch] : 0.0f};
-        sh.before[e][lane] = make_float2(s.A, s.B);
+        if (lane < kCh) sh.before[e][lane] = make_float2(s.A, s.B);
     }
     __syncthreads();
-    if (wave == 0) {
+    if (wave == 0 && lane < kCh) {
         __builtin_amdgcn_s_setprio(3);   // the others wait for it
         float h = sh.before[0][lane].y;
         for (int e = 1; e <= at; ++e) h = apply<Reset>({sh.before[e][lane].x, sh.before[e][lane].y}, h);
-#pragma unroll
-        for (int w = 0; w < Waves; ++w) {
-            sh.enter[w][lane] = h;
-            h = apply<Reset>({sh.span[w][lane].x, sh.span[w][lane].y}, h);
-        }
+        h = sh.rows.template pass<Reset>(lane, h);
         if (mine && at == kJoin - 1 && step + 1 < steps) publish(leaves + int64_t(group) * width, {-0.0f, h});
         __builtin_amdgcn_s_setprio(0);
     }
@@ -261,22 +266,26 @@ __device__ __forceinline__ void pin(Q8Raw& r) { pin(r.codes), pin(r.byte); }
 
 // ---------------------------------------------------------------- forward
 constexpr int kFwdSub = 8;                         // tokens of a lane
-constexpr int kFwdThreads = 512;
-constexpr int kFwdWaves = kFwdThreads / kWave;
-constexpr int kFwdTile = kFwdWaves * 4 * kFwdSub;  // tokens of a workgroup
+constexpr int kFwdTile = kRows * kFwdSub;           // tokens of a workgroup
 static_assert(kFwdTile == 2 * kBlock && kBlock % kFwdSub == 0, "a state block starts at a lane's first token");
 
-// A tile's rows are read and written at an address that the whole wave shares plus an offset
-// of the lane's own, in elements: 32 bits of it on the vector path, whose rows are at most
-// kNearStride apart, 64 otherwise.
+// A tile's rows are read and written, on the vector path, at an address that the whole wave
+// shares plus an offset of the lane's own in 32 bits (rows at most kNearStride elements apart).
 constexpr int64_t kNearStride = int64_t(1) << 22;
-template <bool Vec>
-using Offset = std::conditional_t<Vec, uint32_t, int64_t>;
 
 template <typename T>
-__device__ __forceinline__ typename Lane4<T>::Raw load_row(const void* base, int64_t row, int64_t off)
+__device__ __forceinline__ typename Lane4<T>::Raw load_row(const void* base, int64_t row, uint32_t off)
 {
-    return Lane4<T>::template load<true>(static_cast<const T*>(base) + row, off, 4);
+    return load_at<typename Lane4<T>::Raw>(static_cast<const T*>(base) + row, off * uint32_t(sizeof(T)));
+}
+template <typename T, bool Vec>
+__device__ __forceinline__ void store_row(void* base, int64_t row, int64_t lane_rows, int64_t stride, int col, int n, const float (&y)[4])
+{
+    if constexpr (Vec) {
+        if (n > 0) store_at(static_cast<T*>(base) + row, (uint32_t(lane_rows) * uint32_t(stride) + col * 4) * uint32_t(sizeof(T)), Lane4<T>::narrow(y));
+    } else {
+        Lane4<T>::template store<false>(base, row + lane_rows * stride + col * 4, n, y);
+    }
 }
 
 // How many of `most` tokens exist when n are left (which may be none or fewer).
@@ -300,28 +309,31 @@ __device__ __forceinline__ uint32_t pack_group(const float (&x)[4], bool mine, u
 // whether its token j is one, and whether token j of any row is.
 template <bool Reset, int Sub>
 struct Cuts {
-    uint32_t all, mine;
+    uint64_t all;
+    uint32_t mine;
     __device__ Cuts(const uint8_t* reset, int64_t left, int row)
     {
         const int lane = threadIdx.x % kWave;
         all = mine = 0;
         if constexpr (Reset) {
-            all = uint32_t(__ballot(lane < 4 * Sub && lane < left && reset[lane] != 0));
-            mine = all >> (row * Sub);
+            all = __ballot(lane < kWaveRows * Sub && lane < left && reset[lane] != 0);
+            mine = uint32_t(all >> (row * Sub));
         }
     }
     __device__ bool lane(int j) const { return Reset && ((mine >> j) & 1u) != 0; }
     __device__ bool any(int j) const
     {
-        constexpr uint32_t rows = 1u | (1u << Sub) | (1u << (2 * Sub)) | (1u << (3 * Sub));
+        uint64_t rows = 0;
+#pragma unroll
+        for (int r = 0; r < kWaveRows; ++r) rows |= uint64_t(1) << (r * Sub);
         return Reset && (all & (rows << j)) != 0;
     }
 };
 
 template <typename T, bool Vec, bool Reset, bool Kept>
-__global__ __launch_bounds__(kFwdThreads, (Vec ? 4 : 2)) void recurrence_kernel(RecurrenceArgs a)
+__global__ __launch_bounds__(kThreads, (Vec ? 4 : 2)) void recurrence_kernel(RecurrenceArgs a)
 {
-    __shared__ WalkShared<kFwdWaves, kJoinOn> sh;
+    __shared__ WalkShared<kJoinOn> sh;
     const int slabs = int((a.width + kCh - 1) / kCh);
     const int slab = int(blockIdx.x) % slabs, ticket = draw_ticket(a.words, a.tiles > 1, slab, slabs);
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -330,15 +342,15 @@ __global__ __launch_bounds__(kFwdThreads, (Vec ? 4 : 2)) void recurrence_kernel(
     const int n = int(max<int64_t>(0, min<int64_t>(4, a.width - ch)));   // channels of this lane
     const Rates k = rates_of(a.theta, a.decay, ch, n);
     const Place at = place_of(ticket, a.tiles > 1, a.batch, sh);
-    const int64_t w0 = int64_t(at.step) * kFwdTile + wave * 4 * kFwdSub;  // the wave's first token
+    const int64_t w0 = int64_t(at.step) * kFwdTile + wave * kWaveRows * kFwdSub;  // the wave's first token
     const int64_t token0 = at.b * a.seq_len + w0;
     const int left = there_are(a.seq_len - w0 - row * kFwdSub, kFwdSub);  // of the lane's tokens
 
     // Tokens past the end come after all others, so the state that they would leave is used by
     // nobody: they and channels past the last are read as copies of existing ones.
     typename Lane4<T>::Raw rx[kFwdSub], rr[kFwdSub], ri[kFwdSub];
-    if (Vec && w0 + 4 * kFwdSub <= a.seq_len) {
-        const Offset<Vec> off = Offset<Vec>(row * kFwdSub) * Offset<Vec>(a.stride) + (n > 0 ? col * 4 : 0);
+    if (Vec && w0 + kWaveRows * kFwdSub <= a.seq_len) {
+        const uint32_t off = uint32_t(row * kFwdSub) * uint32_t(a.stride) + (n > 0 ? col * 4 : 0);
 #pragma unroll
         for (int j = 0; j < kFwdSub; ++j) {
             const int64_t at_row = (token0 + j) * a.stride + ch0;
@@ -361,8 +373,7 @@ __global__ __launch_bounds__(kFwdThreads, (Vec ? 4 : 2)) void recurrence_kernel(
         const int64_t groups = (a.width + kGroup - 1) / kGroup;
         const int64_t codes_at = token0 * a.width + ch0;
         const int64_t bytes_at = checkpoint_exponents_at(a.batch * a.seq_len, a.width) + token0 * groups + ch0 / kGroup;
-        const Offset<Vec> c_off = Offset<Vec>(row * kFwdSub) * Offset<Vec>(a.width) + col * 4;
-        const Offset<Vec> b_off = Offset<Vec>(row * kFwdSub) * Offset<Vec>(groups) + col / 8;
+        const uint32_t c_off = uint32_t(row * kFwdSub) * uint32_t(a.width) + col * 4, b_off = uint32_t(row * kFwdSub) * uint32_t(groups) + col / 8;
 #pragma unroll
         for (int j = 0; j < kFwdSub; ++j) {
             uint32_t codes[3], byte[3];
@@ -375,10 +386,10 @@ __global__ __launch_bounds__(kFwdThreads, (Vec ? 4 : 2)) void recurrence_kernel(
             if (j < left && n > 0) {
 #pragma unroll
                 for (int q = 0; q < 3; ++q) {
-                    uint8_t* out = kept[q] + codes_at + j * a.width + c_off;
                     if constexpr (Vec) {
-                        *reinterpret_cast<uint32_t*>(out) = codes[q];
+                        store_at(kept[q] + codes_at + j * a.width, c_off, codes[q]);
                     } else {
+                        uint8_t* out = kept[q] + codes_at + (row * kFwdSub + j) * a.width + col * 4;
 #pragma unroll
                         for (int v = 0; v < 4; ++v)
                             if (v < n) out[v] = uint8_t(codes[q] >> (8 * v));
@@ -386,12 +397,17 @@ __global__ __launch_bounds__(kFwdThreads, (Vec ? 4 : 2)) void recurrence_kernel(
                 }
                 if (col % 8 == 0) {
 #pragma unroll
-                    for (int q = 0; q < 3; ++q) kept[q][bytes_at + j * groups + b_off] = uint8_t(byte[q]);
+                    for (int q = 0; q < 3; ++q) {
+                        if constexpr (Vec)
+                            store_at(kept[q] + bytes_at + j * groups, b_off, uint8_t(byte[q]));
+                        else
+                            kept[q][bytes_at + (row * kFwdSub + j) * groups + col / 8] = uint8_t(byte[q]);
+                    }
                 }
             }
         }
     }
-    Span e[kFwdSub][4], own[4], before[4], all[4];
+    Span e[kFwdSub][4], own[4];
 #pragma unroll
     for (int v = 0; v < 4; ++v) own[v] = nothing();
 #pragma unroll
@@ -414,24 +430,14 @@ __global__ __launch_bounds__(kFwdThreads, (Vec ? 4 : 2)) void recurrence_kernel(
             for (int v = 0; v < 4; ++v) own[v] = {own[v].A * e[j][v].A, apply<false>(e[j][v], own[v].B)};
         }
     }
-#pragma unroll
-    for (int v = 0; v < 4; ++v) join_rows<Reset, false>(own[v], row, before[v], all[v]);
-    if (row == 0) {
-        float4* out = reinterpret_cast<float4*>(&sh.span[wave][col * 4]);
-        out[0] = make_float4(all[0].A, all[0].B, all[1].A, all[1].B);
-        out[1] = make_float4(all[2].A, all[2].B, all[3].A, all[3].B);
-    }
+    sh.rows.put(wave * kWaveRows + row, col, own);
     __syncthreads();
     walk<Reset>(sh, a.words, a.batch, at.b, at.step, a.tiles, a.width, slab, a.h0);
-    const float4 enter = *reinterpret_cast<const float4*>(&sh.enter[wave][col * 4]);
-    float h[4] = {enter.x, enter.y, enter.z, enter.w};
-#pragma unroll
-    for (int v = 0; v < 4; ++v) h[v] = apply<Reset>(before[v], h[v]);
+    float h[4];
+    sh.rows.entering(wave * kWaveRows + row, col, h);
     const int64_t t0 = w0 + row * kFwdSub;
     if (a.states != nullptr && t0 % kBlock == 0 && left > 0)
         Lane4<float>::store<false>(a.states, (at.b * ((a.seq_len + kBlock - 1) / kBlock) + t0 / kBlock) * a.width + ch, n, h);
-    T* y = static_cast<T*>(a.y) + token0 * a.width + ch0;
-    const Offset<Vec> y_off = Offset<Vec>(row * kFwdSub) * Offset<Vec>(a.width) + col * 4;
     float* final_h = a.final_h != nullptr ? a.final_h + at.b * a.width + ch : nullptr;
 #pragma unroll
     for (int j = 0; j < kFwdSub; ++j) {
@@ -443,7 +449,7 @@ __global__ __launch_bounds__(kFwdThreads, (Vec ? 4 : 2)) void recurrence_kernel(
             for (int v = 0; v < 4; ++v) h[v] = apply<false>(e[j][v], h[v]);
         }
         if (j < left) {
-            Lane4<T>::template store<Vec>(y + j * a.width, y_off, n, h);
+            store_row<T, Vec>(a.y, (token0 + j) * a.width + ch0, row * kFwdSub, a.width, col, n, h);
             if (final_h != nullptr && w0 + row * kFwdSub + j == a.seq_len - 1) Lane4<float>::store<false>(final_h, 0, n, h);
         }
     }
@@ -473,9 +479,7 @@ __global__ __launch_bounds__(256) void recurrence_step_kernel(RecurrenceArgs a, 
 
 // ---------------------------------------------------------------- backward
 constexpr int kBwdSub = 4;
-constexpr int kBwdThreads = 512;
-constexpr int kBwdWaves = kBwdThreads / kWave;
-constexpr int kBwdTile = kBwdWaves * 4 * kBwdSub;
+constexpr int kBwdTile = kRows * kBwdSub;
 static_assert(kBwdTile == kBlock, "a tile of the backward pass starts at a kept state");
 
 // x, r or i of the backward pass: a tensor of T, or a checkpoint.  load: the token `row` tokens
@@ -508,7 +512,7 @@ struct Source<q8_t> {
         const int64_t groups = (a.width + kGroup - 1) / kGroup;
         const int8_t* codes = static_cast<const int8_t*>(base) + token * a.width + ch0;
         const uint8_t* bytes = static_cast<const uint8_t*>(base) + checkpoint_exponents_at(a.batch * a.seq_len, a.width) + token * groups + ch0 / kGroup;
-        return {*reinterpret_cast<const uint32_t*>(codes + (uint32_t(row) * uint32_t(a.width) + c4 * 4)), bytes[uint32_t(row) * uint32_t(groups) + c4 / 8]};
+        return {load_at<uint32_t>(codes, uint32_t(row) * uint32_t(a.width) + c4 * 4), load_at<uint8_t>(bytes, uint32_t(row) * uint32_t(groups) + c4 / 8)};
     }
     template <bool Vec>
     __device__ static Raw load_near(const void* base, const RecurrenceGradArgs& a, int64_t token, int64_t ch, int64_t ch0)
@@ -539,21 +543,19 @@ constexpr bool kLean = sizeof(T) <= 2 && sizeof(Tg) == 2;
 
 template <bool Lean>
 struct BackwardShared {
-    WalkShared<kBwdWaves, kJoinBack> walk;          // the walk back: its first wave is the workgroup's last
-    float2 span[kBwdWaves][kCh];         // the waves' spans on the way forward
-    float enter[kBwdWaves][kCh];
+    WalkShared<kJoinBack> back;          // the walk back: its first row is the workgroup's last
+    RowSpans on;                         // the rows on the way forward
 };
 template <>
 struct BackwardShared<true> : BackwardShared<false> {
-    float4 m[kBwdSub][kBwdThreads];
-    float4 ahead[4][kBwdThreads];
+    float4 m[kBwdSub][kThreads];
 };
 
 __device__ __forceinline__ float4 to_float4(const float (&x)[4]) { return make_float4(x[0], x[1], x[2], x[3]); }
 __device__ __forceinline__ void from_float4(const float4& f, float (&x)[4]) { x[0] = f.x, x[1] = f.y, x[2] = f.z, x[3] = f.w; }
 
 template <typename T, typename Tg, bool Vec, bool Reset>
-__global__ __launch_bounds__(kBwdThreads, (kLean<T, Tg> ? 4 : 2)) void recurrence_grad_kernel(RecurrenceGradArgs a)
+__global__ __launch_bounds__(kThreads, (kLean<T, Tg> ? 4 : 2)) void recurrence_grad_kernel(RecurrenceGradArgs a)
 {
     constexpr bool Lean = kLean<T, Tg>;
     __shared__ BackwardShared<Lean> sh;
@@ -564,15 +566,15 @@ __global__ __launch_bounds__(kBwdThreads, (kLean<T, Tg> ? 4 : 2)) void recurrenc
     const int64_t ch0 = int64_t(slab) * kCh, ch = ch0 + col * 4;
     const int n = int(max<int64_t>(0, min<int64_t>(4, a.width - ch)));
     const Rates k = rates_of(a.theta, a.decay, ch, n);
-    const Place at = place_of(ticket, a.tiles > 1, a.batch, sh.walk);
+    const Place at = place_of(ticket, a.tiles > 1, a.batch, sh.back);
     const int64_t tile = a.tiles - 1 - at.step;
-    const int64_t w0 = tile * kBwdTile + wave * 4 * kBwdSub;
+    const int64_t w0 = tile * kBwdTile + wave * kWaveRows * kBwdSub;
     const int64_t token0 = at.b * a.seq_len + w0;
     const int left = there_are(a.seq_len - w0 - row * kBwdSub, kBwdSub);
 
     typename Source<T>::Raw rx[kBwdSub], rr[kBwdSub], ri[kBwdSub];
     typename Lane4<Tg>::Raw rd[kBwdSub];
-    if (Vec && w0 + 4 * kBwdSub <= a.seq_len) {
+    if (Vec && w0 + kWaveRows * kBwdSub <= a.seq_len) {
         const int c4 = n > 0 ? col : 0;
 #pragma unroll
         for (int j = 0; j < kBwdSub; ++j) {
@@ -596,7 +598,7 @@ __global__ __launch_bounds__(kBwdThreads, (kLean<T, Tg> ? 4 : 2)) void recurrenc
     // the lane's tokens: their factors, and what they do together to the state and, on the way
     // back, to its gradient
     Kept e[kBwdSub][4];
-    Span fwd[4], bwd[4], all[4];
+    Span fwd[4], bwd[4];
 #pragma unroll
     for (int v = 0; v < 4; ++v) fwd[v] = bwd[v] = nothing();
 #pragma unroll
@@ -653,56 +655,18 @@ __global__ __launch_bounds__(kBwdThreads, (kLean<T, Tg> ? 4 : 2)) void recurrenc
             }
         }
     }
-    Span fahead[4], bahead[4];
-#pragma unroll
-    for (int v = 0; v < 4; ++v) join_rows<Reset, false>(fwd[v], row, fahead[v], all[v]);
-    if (row == 0) {
-        float4* out = reinterpret_cast<float4*>(&sh.span[wave][col * 4]);
-        out[0] = make_float4(all[0].A, all[0].B, all[1].A, all[1].B);
-        out[1] = make_float4(all[2].A, all[2].B, all[3].A, all[3].B);
-    }
-    if constexpr (Lean) {
-        sh.ahead[0][threadIdx.x] = make_float4(fahead[0].A, fahead[1].A, fahead[2].A, fahead[3].A);
-        sh.ahead[1][threadIdx.x] = make_float4(fahead[0].B, fahead[1].B, fahead[2].B, fahead[3].B);
-    }
-#pragma unroll
-    for (int v = 0; v < 4; ++v) join_rows<Reset, true>(bwd[v], row, bahead[v], all[v]);
-    if (row == 0) {
-        float4* out = reinterpret_cast<float4*>(&sh.walk.span[kBwdWaves - 1 - wave][col * 4]);
-        out[0] = make_float4(all[0].A, all[0].B, all[1].A, all[1].B);
-        out[1] = make_float4(all[2].A, all[2].B, all[3].A, all[3].B);
-    }
-    if constexpr (Lean) {
-        sh.ahead[2][threadIdx.x] = make_float4(bahead[0].A, bahead[1].A, bahead[2].A, bahead[3].A);
-        sh.ahead[3][threadIdx.x] = make_float4(bahead[0].B, bahead[1].B, bahead[2].B, bahead[3].B);
-    }
+    const int my_row = wave * kWaveRows + row, my_back = kRows - 1 - my_row;
+    sh.on.put(my_row, col, fwd);
+    sh.back.rows.put(my_back, col, bwd);
     const int64_t my = ch0 + lane;
     float state = 0.0f;      // wave 1: the state entering the tile, a channel a lane
-    if (wave == 1 && my < a.width) state = a.states[(at.b * a.tiles + tile) * a.width + my];
+    if (wave == 1 && lane < kCh && my < a.width) state = a.states[(at.b * a.tiles + tile) * a.width + my];
     __syncthreads();
-    if (wave == 1) {
-#pragma unroll
-        for (int w = 0; w < kBwdWaves; ++w) {
-            sh.enter[w][lane] = state;
-            state = apply<Reset>({sh.span[w][lane].x, sh.span[w][lane].y}, state);
-        }
-    }
-    walk<Reset>(sh.walk, a.words, a.batch, at.b, at.step, a.tiles, a.width, slab, a.dfinal);
+    if (wave == 1 && lane < kCh) sh.on.template pass<Reset>(lane, state);
+    walk<Reset>(sh.back, a.words, a.batch, at.b, at.step, a.tiles, a.width, slab, a.dfinal);
     float h[4], c[4], dth[4] = {0.f, 0.f, 0.f, 0.f};
-    from_float4(*reinterpret_cast<const float4*>(&sh.enter[wave][col * 4]), h);
-    from_float4(*reinterpret_cast<const float4*>(&sh.walk.enter[kBwdWaves - 1 - wave][col * 4]), c);
-    if constexpr (Lean) {
-        float f[4][4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) from_float4(sh.ahead[q][threadIdx.x], f[q]);
-#pragma unroll
-        for (int v = 0; v < 4; ++v) fahead[v] = {f[0][v], f[1][v]}, bahead[v] = {f[2][v], f[3][v]};
-    }
-#pragma unroll
-    for (int v = 0; v < 4; ++v) {
-        h[v] = apply<Reset>(fahead[v], h[v]);
-        c[v] = apply<Reset>(bahead[v], c[v]);
-    }
+    sh.on.entering(my_row, col, h);
+    sh.back.rows.entering(my_back, col, c);
 #pragma unroll
     for (int j = 0; j < kBwdSub; ++j) {
         const bool cut = cuts.any(j);
@@ -713,11 +677,6 @@ __global__ __launch_bounds__(kBwdThreads, (kLean<T, Tg> ? 4 : 2)) void recurrenc
             h[v] = cut ? apply<true>(in, h[v]) : apply<false>(in, h[v]);
         }
     }
-    const int64_t g0 = token0 * a.grad_stride + ch0;
-    const Offset<Vec> g_off = Offset<Vec>(row * kBwdSub) * Offset<Vec>(a.grad_stride) + col * 4;
-    Tg* const dx = static_cast<Tg*>(a.dx) + g0;
-    Tg* const dr = static_cast<Tg*>(a.dr) + g0;
-    Tg* const di = static_cast<Tg*>(a.di) + g0;
 #pragma unroll
     for (int j = kBwdSub - 1; j >= 0; --j) {
         if (j >= left) continue;
@@ -744,23 +703,21 @@ __global__ __launch_bounds__(kBwdThreads, (kLean<T, Tg> ? 4 : 2)) void recurrenc
             dth[v] = cut ? dth[v] : fmaf(dl, s, dth[v]);
             c[v] = cut ? 0.0f : ag;
         }
-        const int64_t step = j * a.grad_stride;
-        Lane4<Tg>::template store<Vec>(dx + step, g_off, n, gx);
-        Lane4<Tg>::template store<Vec>(dr + step, g_off, n, gr);
-        Lane4<Tg>::template store<Vec>(di + step, g_off, n, gi);
+        const int64_t at_row = (token0 + j) * a.grad_stride + ch0;
+        store_row<Tg, Vec>(a.dx, at_row, row * kBwdSub, a.grad_stride, col, n, gx);
+        store_row<Tg, Vec>(a.dr, at_row, row * kBwdSub, a.grad_stride, col, n, gr);
+        store_row<Tg, Vec>(a.di, at_row, row * kBwdSub, a.grad_stride, col, n, gi);
     }
     if (a.dh0 != nullptr && tile == 0 && wave == 0 && row == 0) Lane4<float>::store<false>(a.dh0, at.b * a.width + ch, n, c);
-    // dtheta: the tile's sum of dl s, one row of the partial sums
-#pragma unroll
-    for (int v = 0; v < 4; ++v) dth[v] = row_pair_sums(dth[v]);
+    // dtheta: the tile's sum of dl s, one row of the partial sums; the rows' sums take the place
+    // of their entering states
+    *reinterpret_cast<float4*>(&sh.on.B[my_row][col * 4]) = to_float4(dth);
     __syncthreads();
-    if (row == 0) *reinterpret_cast<float4*>(&sh.enter[wave][col * 4]) = to_float4(dth);
-    __syncthreads();
-    if (wave == 0 && my < a.width) {
-        float s = sh.enter[0][lane];
-#pragma unroll
-        for (int w = 1; w < kBwdWaves; ++w) s += sh.enter[w][lane];
-        a.partial[(at.b * a.tiles + tile) * a.width + my] = s;
+    if (wave == 0 && lane < kCh) {
+        float s = 0.0f;
+#pragma unroll 8
+        for (int r = 0; r < kRows; ++r) s += sh.on.B[r][lane];
+        if (my < a.width) a.partial[(at.b * a.tiles + tile) * a.width + my] = s;
     }
 }
 
@@ -810,7 +767,7 @@ hipError_t clear_walk(uint64_t* words, int64_t batch, int64_t tiles, int64_t wid
 template <typename T, bool Vec, bool Reset>
 hipError_t launch_forward(const RecurrenceArgs& a, int64_t blocks, hipStream_t stream)
 {
-    const dim3 grid{unsigned(blocks)}, block{kFwdThreads};
+    const dim3 grid{unsigned(blocks)}, block{kThreads};
     if (a.kept_x != nullptr)
         hipLaunchKernelGGL((recurrence_kernel<T, Vec, Reset, true>), grid, block, 0, stream, a);
     else
@@ -857,7 +814,7 @@ hipError_t launch_backward_types(const RecurrenceGradArgs& a, hipStream_t stream
     const bool vec = a.width % 4 == 0 && a.stride % 4 == 0 && a.grad_stride % 4 == 0 && a.stride <= kNearStride &&
                      a.grad_stride <= kNearStride && aligned(a.x, in) && aligned(a.r, in) && aligned(a.i, in) &&
                      aligned(a.dy, out) && aligned(a.dx, out) && aligned(a.dr, out) && aligned(a.di, out);
-    const dim3 grid{unsigned(blocks)}, block{kBwdThreads};
+    const dim3 grid{unsigned(blocks)}, block{kThreads};
     if (vec && a.reset != nullptr)
         hipLaunchKernelGGL((recurrence_grad_kernel<T, Tg, true, true>), grid, block, 0, stream, a);
     else if (vec)
