@@ -107,14 +107,14 @@ int checkpoint(const void* x, int64_t rows, int64_t width, int64_t stride, int d
     return status_of(mesa::launch_checkpoint(a, pack, static_cast<hipStream_t>(stream)), stream);
 }
 
-// Sizes shared by the recurrence's calls; a grid of one workgroup a 64-channel slab of 128 tokens
+// Sizes shared by the recurrence's calls; a grid of one workgroup a 32-channel slab of 128 tokens
 // must be countable in 31 bits.
 int recurrence_sizes(int64_t batch, int64_t seq_len, int64_t width, int64_t stride, float decay)
 {
     if (batch < 0 || seq_len < 0 || width < 0 || seq_len > kMostElements || width > kMostElements) return MESA_ERR_SHAPE;
     if (!(isfinite(decay) && decay > 0.0f)) return MESA_ERR_ARG;
     if (batch > 0 && seq_len > 0 && stride < width) return MESA_ERR_SHAPE;
-    const int64_t blocks = (seq_len + MESA_RECURRENCE_BLOCK - 1) / MESA_RECURRENCE_BLOCK, slabs = (width + 63) / 64;
+    const int64_t blocks = (seq_len + MESA_RECURRENCE_BLOCK - 1) / MESA_RECURRENCE_BLOCK, slabs = (width + 31) / 32;
     if (!product_ok({batch, blocks, slabs}) || batch * blocks * slabs > INT32_MAX) return MESA_ERR_SHAPE;
     return MESA_OK;
 }

@@ -31,11 +31,12 @@ __device__ float mul_zero_wins(float x, float y) __asm("llvm.amdgcn.fmul.legacy"
 
 namespace {
 
-constexpr int kAcross = 16;            // lanes across a token's channels
-constexpr int kCh = 4 * kAcross;       // channels of a workgroup
-constexpr int kWaveRows = kWave / kAcross;   // runs of tokens of a wave, one to a row of lanes
-constexpr int kRows = 32;                    // of a workgroup
-constexpr int kWaves = kRows / kWaveRows, kThreads = kWaves * kWave;
+constexpr int kRows = 32;              // runs of tokens of a workgroup, one to a row of lanes
+// A workgroup of rows of Across lanes, four channels in each.
+template <int Across>
+struct Form {
+    static constexpr int kAcross = Across, kCh = 4 * Across, kWaveRows = kWave / Across, kWaves = kRows / kWaveRows, kThreads = kWaves * kWave;
+};
 constexpr int kBlock = kRecurrenceBlock;
 
 // What a span of tokens does to the state.
@@ -114,7 +115,7 @@ constexpr uint64_t kUnset = ~uint64_t(0);
 // Ticket counters, one for each slab of channels, ahead of the spans: each in a cache line of
 // its own (the GPU's dies draw from one line one at a time), in 64-bit words.
 constexpr int kCounterWords = 16;
-__host__ __device__ inline int64_t ticket_words(int64_t width) { return (width + kCh - 1) / kCh * kCounterWords; }
+__host__ __device__ inline int64_t ticket_words(int64_t slabs) { return slabs * kCounterWords; }
 
 __device__ __forceinline__ void publish(uint64_t* at, Span s)
 {
@@ -143,6 +144,7 @@ __global__ __launch_bounds__(256) void recurrence_fill_kernel(ulonglong2* words,
 // Shared memory of a walk: the spans of the lane rows (four to a wave) of a workgroup in
 // planes of A and B, in the order of the walk, and the spans of the tiles before it.  The
 // state entering a row takes the place of its B.
+template <int kCh>
 struct RowSpans {
     float A[kRows][kCh], B[kRows][kCh];
 
@@ -178,9 +180,9 @@ struct RowSpans {
         return h;
     }
 };
-template <int kJoin>
+template <int kCh, int kJoin>
 struct WalkShared {
-    RowSpans rows;
+    RowSpans<kCh> rows;
     float2 before[kJoin][kCh];
     int ticket;
 };
@@ -215,18 +217,19 @@ __device__ __forceinline__ Place place_of(int ticket, bool many, int64_t batch, 
 // barrier at the end.  `step` is the tile's place in the walk, `first` the state ahead of the
 // whole walk.  The first wave passes through the rows; the others' time is the compute unit's
 // second workgroup's.
-template <bool Reset, int kJoin>
-__device__ __forceinline__ void walk(WalkShared<kJoin>& sh, uint64_t* words, int64_t batch, int64_t b, int step, int steps,
+template <bool Reset, class F, int kJoin>
+__device__ __forceinline__ void walk(WalkShared<F::kCh, kJoin>& sh, uint64_t* words, int64_t batch, int64_t b, int step, int steps,
                                      int64_t width, int slab, const float* first)
 {
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int64_t ch = int64_t(slab) * kCh + lane;
-    const bool mine = lane < kCh && ch < width;
+    const int64_t ch = int64_t(slab) * F::kCh + lane;
+    const bool mine = lane < F::kCh && ch < width;
     const int group = step / kJoin, at = step % kJoin;
     const int groups = steps / kJoin;
-    uint64_t* spans = words + ticket_words(width) + b * steps * width + ch;
-    uint64_t* leaves = words + ticket_words(width) + batch * steps * width + b * groups * width + ch;
-    if (wave == 0 && lane < kCh && at != kJoin - 1 && step + 1 < steps) {
+    const int64_t slabs = (width + F::kCh - 1) / F::kCh;
+    uint64_t* spans = words + ticket_words(slabs) + b * steps * width + ch;
+    uint64_t* leaves = words + ticket_words(slabs) + batch * steps * width + b * groups * width + ch;
+    if (wave == 0 && lane < F::kCh && at != kJoin - 1 && step + 1 < steps) {
         __builtin_amdgcn_s_setprio(3);   // other workgroups wait for it
         const Span s = sh.rows.template all<Reset>(lane);
         if (mine) publish(spans + int64_t(step) * width, s);
@@ -234,7 +237,7 @@ __device__ __forceinline__ void walk(WalkShared<kJoin>& sh, uint64_t* words, int
     }
     // entry 0 is the state entering the group, entry e the span of the group's tile e - 1; the
     // first wave, which publishes, comes last
-    for (int e = kWaves - 1 - wave; e <= at; e += kWaves) {
+    for (int e = F::kWaves - 1 - wave; e <= at; e += F::kWaves) {
         Span s;
         if (e > 0)
             s = await(spans + int64_t(group * kJoin + e - 1) * width, mine);
@@ -242,10 +245,10 @@ __device__ __forceinline__ void walk(WalkShared<kJoin>& sh, uint64_t* words, int
             s = await(leaves + int64_t(group - 1) * width, mine);
         else
             s = {-0.0f, first != nullptr && mine ? first[b * width + ch] : 0.0f};
-        if (lane < kCh) sh.before[e][lane] = make_float2(s.A, s.B);
+        if (lane < F::kCh) sh.before[e][lane] = make_float2(s.A, s.B);
     }
     __syncthreads();
-    if (wave == 0 && lane < kCh) {
+    if (wave == 0 && lane < F::kCh) {
         __builtin_amdgcn_s_setprio(3);   // the others wait for it
         float h = sh.before[0][lane].y;
         for (int e = 1; e <= at; ++e) h = apply<Reset>({sh.before[e][lane].x, sh.before[e][lane].y}, h);
@@ -307,16 +310,16 @@ __device__ __forceinline__ uint32_t pack_group(const float (&x)[4], bool mine, u
 // The resets of a wave's tokens, bit t for its token t, the same in every lane; few waves have
 // any, and the others' arithmetic is that without resets.  Lane row `row` of Sub tokens:
 // whether its token j is one, and whether token j of any row is.
-template <bool Reset, int Sub>
+template <bool Reset, class F, int Sub>
 struct Cuts {
     uint64_t all;
     uint32_t mine;
-    __device__ Cuts(const uint8_t* reset, int64_t left, int row)
+    __device__ Cuts(const uint8_t* reset, int64_t at, int64_t left, int row)
     {
         const int lane = threadIdx.x % kWave;
         all = mine = 0;
         if constexpr (Reset) {
-            all = __ballot(lane < kWaveRows * Sub && lane < left && reset[lane] != 0);
+            if (reset != nullptr) all = __ballot(lane < F::kWaveRows * Sub && lane < left && reset[at + lane] != 0);
             mine = uint32_t(all >> (row * Sub));
         }
     }
@@ -325,15 +328,16 @@ struct Cuts {
     {
         uint64_t rows = 0;
 #pragma unroll
-        for (int r = 0; r < kWaveRows; ++r) rows |= uint64_t(1) << (r * Sub);
+        for (int r = 0; r < F::kWaveRows; ++r) rows |= uint64_t(1) << (r * Sub);
         return Reset && (all & (rows << j)) != 0;
     }
 };
 
-template <typename T, bool Vec, bool Reset, bool Kept>
-__global__ __launch_bounds__(kThreads, (Vec ? 4 : 2)) void recurrence_kernel(RecurrenceArgs a)
+template <typename T, bool Vec, bool Reset, bool Kept, class F>
+__global__ __launch_bounds__(F::kThreads, (Vec ? 4 : 2)) void recurrence_kernel(RecurrenceArgs a)
 {
-    __shared__ WalkShared<kJoinOn> sh;
+    constexpr int kAcross = F::kAcross, kCh = F::kCh, kWaveRows = F::kWaveRows;
+    __shared__ WalkShared<kCh, kJoinOn> sh;
     const int slabs = int((a.width + kCh - 1) / kCh);
     const int slab = int(blockIdx.x) % slabs, ticket = draw_ticket(a.words, a.tiles > 1, slab, slabs);
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -367,7 +371,7 @@ __global__ __launch_bounds__(kThreads, (Vec ? 4 : 2)) void recurrence_kernel(Rec
             ri[j] = Lane4<T>::template load_near<Vec>(a.i, at_row, ch, ch0, a.width - 1);
         }
     }
-    const Cuts<Reset, kFwdSub> cuts(a.reset + token0, a.seq_len - w0, row);
+    const Cuts<Reset, F, kFwdSub> cuts(a.reset, token0, a.seq_len - w0, row);
     if constexpr (Kept) {
         uint8_t* const kept[3] = {a.kept_x, a.kept_r, a.kept_i};
         const int64_t groups = (a.width + kGroup - 1) / kGroup;
@@ -432,7 +436,7 @@ __global__ __launch_bounds__(kThreads, (Vec ? 4 : 2)) void recurrence_kernel(Rec
     }
     sh.rows.put(wave * kWaveRows + row, col, own);
     __syncthreads();
-    walk<Reset>(sh, a.words, a.batch, at.b, at.step, a.tiles, a.width, slab, a.h0);
+    walk<Reset, F>(sh, a.words, a.batch, at.b, at.step, a.tiles, a.width, slab, a.h0);
     float h[4];
     sh.rows.entering(wave * kWaveRows + row, col, h);
     const int64_t t0 = w0 + row * kFwdSub;
@@ -541,24 +545,25 @@ struct Kept {
 template <typename T, typename Tg>
 constexpr bool kLean = sizeof(T) <= 2 && sizeof(Tg) == 2;
 
-template <bool Lean>
+template <bool Lean, class F>
 struct BackwardShared {
-    WalkShared<kJoinBack> back;          // the walk back: its first row is the workgroup's last
-    RowSpans on;                         // the rows on the way forward
+    WalkShared<F::kCh, kJoinBack> back;          // the walk back: its first row is the workgroup's last
+    RowSpans<F::kCh> on;                         // the rows on the way forward
 };
-template <>
-struct BackwardShared<true> : BackwardShared<false> {
-    float4 m[kBwdSub][kThreads];
+template <class F>
+struct BackwardShared<true, F> : BackwardShared<false, F> {
+    float4 m[kBwdSub][F::kThreads];
 };
 
 __device__ __forceinline__ float4 to_float4(const float (&x)[4]) { return make_float4(x[0], x[1], x[2], x[3]); }
 __device__ __forceinline__ void from_float4(const float4& f, float (&x)[4]) { x[0] = f.x, x[1] = f.y, x[2] = f.z, x[3] = f.w; }
 
-template <typename T, typename Tg, bool Vec, bool Reset>
-__global__ __launch_bounds__(kThreads, (kLean<T, Tg> ? 4 : 2)) void recurrence_grad_kernel(RecurrenceGradArgs a)
+template <typename T, typename Tg, bool Vec, bool Reset, class F>
+__global__ __launch_bounds__(F::kThreads, (kLean<T, Tg> ? 4 : 2)) void recurrence_grad_kernel(RecurrenceGradArgs a)
 {
+    constexpr int kAcross = F::kAcross, kCh = F::kCh, kWaveRows = F::kWaveRows;
     constexpr bool Lean = kLean<T, Tg>;
-    __shared__ BackwardShared<Lean> sh;
+    __shared__ BackwardShared<Lean, F> sh;
     const int slabs = int((a.width + kCh - 1) / kCh);
     const int slab = int(blockIdx.x) % slabs, ticket = draw_ticket(a.words, a.tiles > 1, slab, slabs);
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -594,7 +599,7 @@ __global__ __launch_bounds__(kThreads, (kLean<T, Tg> ? 4 : 2)) void recurrence_g
             rd[j] = Lane4<Tg>::template load_near<Vec>(a.dy, token * a.width, ch, ch0, a.width - 1);
         }
     }
-    const Cuts<Reset, kBwdSub> cuts(a.reset + token0, a.seq_len - w0, row);
+    const Cuts<Reset, F, kBwdSub> cuts(a.reset, token0, a.seq_len - w0, row);
     // the lane's tokens: their factors, and what they do together to the state and, on the way
     // back, to its gradient
     Kept e[kBwdSub][4];
@@ -663,7 +668,7 @@ __global__ __launch_bounds__(kThreads, (kLean<T, Tg> ? 4 : 2)) void recurrence_g
     if (wave == 1 && lane < kCh && my < a.width) state = a.states[(at.b * a.tiles + tile) * a.width + my];
     __syncthreads();
     if (wave == 1 && lane < kCh) sh.on.template pass<Reset>(lane, state);
-    walk<Reset>(sh.back, a.words, a.batch, at.b, at.step, a.tiles, a.width, slab, a.dfinal);
+    walk<Reset, F>(sh.back, a.words, a.batch, at.b, at.step, a.tiles, a.width, slab, a.dfinal);
     float h[4], c[4], dth[4] = {0.f, 0.f, 0.f, 0.f};
     sh.on.entering(my_row, col, h);
     sh.back.rows.entering(my_back, col, c);
@@ -764,29 +769,44 @@ hipError_t clear_walk(uint64_t* words, int64_t batch, int64_t tiles, int64_t wid
     return hipGetLastError();
 }
 
-template <typename T, bool Vec, bool Reset>
-hipError_t launch_forward(const RecurrenceArgs& a, int64_t blocks, hipStream_t stream)
+// Workgroups of 64 channels read and write whole lines of memory; where there are fewer of
+// them than compute units, workgroups of half the channels finish sooner (a 777-token fp32
+// gradient of 2 x 321 channels, 84 of the wide ones: 22 us wide, 17 narrow; 2048 tokens of
+// 8 x 2048: 106 us wide, 160 narrow).  The narrow ones always look for resets.
+using Wide = Form<16>;
+using Narrow = Form<8>;
+
+template <class F>
+int64_t workgroups(int64_t batch, int64_t tiles, int64_t width) { return batch * tiles * ((width + F::kCh - 1) / F::kCh); }
+bool narrow(int64_t batch, int64_t tiles, int64_t width) { return workgroups<Wide>(batch, tiles, width) < device_compute_units(); }
+
+template <typename T, bool Vec, bool Reset, class F>
+hipError_t launch_forward(const RecurrenceArgs& a, hipStream_t stream)
 {
-    const dim3 grid{unsigned(blocks)}, block{kThreads};
+    const dim3 grid{unsigned(workgroups<F>(a.batch, a.tiles, a.width))}, block{F::kThreads};
     if (a.kept_x != nullptr)
-        hipLaunchKernelGGL((recurrence_kernel<T, Vec, Reset, true>), grid, block, 0, stream, a);
+        hipLaunchKernelGGL((recurrence_kernel<T, Vec, Reset, true, F>), grid, block, 0, stream, a);
     else
-        hipLaunchKernelGGL((recurrence_kernel<T, Vec, Reset, false>), grid, block, 0, stream, a);
+        hipLaunchKernelGGL((recurrence_kernel<T, Vec, Reset, false, F>), grid, block, 0, stream, a);
     return hipGetLastError();
+}
+
+template <typename T, bool Vec>
+hipError_t launch_forward_form(const RecurrenceArgs& a, hipStream_t stream)
+{
+    if (narrow(a.batch, a.tiles, a.width)) return launch_forward<T, Vec, true, Narrow>(a, stream);
+    return a.reset != nullptr ? launch_forward<T, Vec, true, Wide>(a, stream) : launch_forward<T, Vec, false, Wide>(a, stream);
 }
 
 template <typename T>
 hipError_t launch_forward_type(const RecurrenceArgs& a, hipStream_t stream)
 {
-    const int64_t blocks = a.batch * a.tiles * ((a.width + kCh - 1) / kCh);
-    if (blocks > INT32_MAX) return hipErrorInvalidValue;
+    if (workgroups<Narrow>(a.batch, a.tiles, a.width) > INT32_MAX) return hipErrorInvalidValue;
     if (hipError_t e = clear_walk(a.words, a.batch, a.tiles, a.width, stream); e != hipSuccess) return e;
     constexpr int bytes = 4 * int(sizeof(T));
     const bool vec = a.width % 4 == 0 && a.stride % 4 == 0 && a.stride <= kNearStride && aligned(a.x, bytes) &&
                      aligned(a.r, bytes) && aligned(a.i, bytes) && aligned(a.y, bytes);
-    if (a.reset != nullptr)
-        return vec ? launch_forward<T, true, true>(a, blocks, stream) : launch_forward<T, false, true>(a, blocks, stream);
-    return vec ? launch_forward<T, true, false>(a, blocks, stream) : launch_forward<T, false, false>(a, blocks, stream);
+    return vec ? launch_forward_form<T, true>(a, stream) : launch_forward_form<T, false>(a, stream);
 }
 
 template <typename T>
@@ -804,26 +824,31 @@ hipError_t launch_step_type(const RecurrenceArgs& a, float* state_out, hipStream
     return hipGetLastError();
 }
 
+template <typename T, typename Tg, bool Vec, bool Reset, class F>
+hipError_t launch_backward(const RecurrenceGradArgs& a, hipStream_t stream)
+{
+    hipLaunchKernelGGL((recurrence_grad_kernel<T, Tg, Vec, Reset, F>), dim3(unsigned(workgroups<F>(a.batch, a.tiles, a.width))),
+                       dim3(F::kThreads), 0, stream, a);
+    return hipGetLastError();
+}
+
+template <typename T, typename Tg, bool Vec>
+hipError_t launch_backward_form(const RecurrenceGradArgs& a, hipStream_t stream)
+{
+    if (narrow(a.batch, a.tiles, a.width)) return launch_backward<T, Tg, Vec, true, Narrow>(a, stream);
+    return a.reset != nullptr ? launch_backward<T, Tg, Vec, true, Wide>(a, stream) : launch_backward<T, Tg, Vec, false, Wide>(a, stream);
+}
+
 template <typename T, typename Tg>
 hipError_t launch_backward_types(const RecurrenceGradArgs& a, hipStream_t stream)
 {
-    const int64_t blocks = a.batch * a.tiles * ((a.width + kCh - 1) / kCh);
-    if (blocks > INT32_MAX) return hipErrorInvalidValue;
+    if (workgroups<Narrow>(a.batch, a.tiles, a.width) > INT32_MAX) return hipErrorInvalidValue;
     if (hipError_t e = clear_walk(a.words, a.batch, a.tiles, a.width, stream); e != hipSuccess) return e;
     constexpr int in = 4 * int(sizeof(T)), out = 4 * int(sizeof(Tg));
     const bool vec = a.width % 4 == 0 && a.stride % 4 == 0 && a.grad_stride % 4 == 0 && a.stride <= kNearStride &&
                      a.grad_stride <= kNearStride && aligned(a.x, in) && aligned(a.r, in) && aligned(a.i, in) &&
                      aligned(a.dy, out) && aligned(a.dx, out) && aligned(a.dr, out) && aligned(a.di, out);
-    const dim3 grid{unsigned(blocks)}, block{kThreads};
-    if (vec && a.reset != nullptr)
-        hipLaunchKernelGGL((recurrence_grad_kernel<T, Tg, true, true>), grid, block, 0, stream, a);
-    else if (vec)
-        hipLaunchKernelGGL((recurrence_grad_kernel<T, Tg, true, false>), grid, block, 0, stream, a);
-    else if (a.reset != nullptr)
-        hipLaunchKernelGGL((recurrence_grad_kernel<T, Tg, false, true>), grid, block, 0, stream, a);
-    else
-        hipLaunchKernelGGL((recurrence_grad_kernel<T, Tg, false, false>), grid, block, 0, stream, a);
-    return hipGetLastError();
+    return vec ? launch_backward_form<T, Tg, true>(a, stream) : launch_backward_form<T, Tg, false>(a, stream);
 }
 
 }  // namespace
@@ -833,7 +858,8 @@ int64_t recurrence_tiles(int64_t seq_len) { return (seq_len + kFwdTile - 1) / kF
 int64_t recurrence_walk_bytes(int64_t batch, int64_t tiles, int64_t width)
 {
     if (tiles <= 1) return 0;
-    return (ticket_words(width) + batch * (tiles + tiles / kJoinBack) * width + 1) / 2 * 16;   // kJoinBack is the smaller
+    // counters for the narrow workgroups, leaves for the shorter groups: enough for either form and way
+    return (ticket_words((width + Narrow::kCh - 1) / Narrow::kCh) + batch * (tiles + tiles / kJoinBack) * width + 1) / 2 * 16;
 }
 
 hipError_t launch_recurrence(const RecurrenceArgs& a, hipStream_t stream)

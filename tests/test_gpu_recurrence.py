@@ -142,6 +142,35 @@ def test_widths(width, dtype):
     _say("width %d %s: forward %.1e, gradients %.1e, from 8 bits %.1e" % (width, dtype, e, e2[0], e2[1]))
 
 
+@pytest.mark.parametrize("T,width,resets", [(129, 64, 0.0), (300, 65, 0.01), (520, 72, 0.0), (257, 130, 0.02), (600, 36, 0.0)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_many_sequences(T, width, resets, dtype):
+    """Enough sequences to fill the GPU with workgroups of 64 channels (fewer take half of them)."""
+    x = _inputs(140, T, width, dtype, seed=T + width, resets=resets)
+    d, f, ref, e = _check_forward(x, dtype)
+    e2 = [_check_backward(x, d, f, ref, dtype, kept8) for kept8 in (False, True)]
+    _say("140 sequences T=%d width %d %s: forward %.1e, gradients %.1e, from 8 bits %.1e" % (T, width, dtype, e, e2[0], e2[1]))
+
+
+@pytest.mark.parametrize("B", [2, 140])
+@pytest.mark.parametrize("dtype,kept8,grad", [("f32", False, "bf16"), ("bf16", False, "f32"), ("f32", True, "f32"), ("bf16", True, "f32"),
+                                              ("f32", True, "bf16")])
+def test_gradients_of_another_type(B, dtype, kept8, grad):
+    """Gradients in fp32 of bf16 or 8-bit inputs and the other way."""
+    x = _inputs(B, 270, 68, dtype, seed=B, resets=0.01)
+    x["dy"] = _round(x["dy"], "bf16")
+    d, f, ref, _ = _check_forward(x, dtype)
+    d["dy"] = d["dy"].to(_tdt(grad))
+    held = {n: (R.checkpoint(x[n].reshape(-1, 68))[2].reshape(x[n].shape) if kept8 else x[n]) for n in "xri"}
+    g = L.recurrence_backward(*((f if kept8 else d)[n] for n in "xri"), d["theta"], f["states"], d["dy"], d["dfinal"], reset=d["reset"])
+    want = R.backward(held["x"], held["r"], held["i"], x["theta"], _np(f["states"]), x["dy"], x["dfinal"], reset=x["reset"])
+    for n in ("dx", "dr", "di"):
+        assert g[n].dtype == _tdt(grad)
+        _close(g[n], want[n], grad, TOL_GRAD, n)
+    for n in ("dtheta", "dh0"):
+        _close(g[n], want[n], "f32", TOL_GRAD, n)
+
+
 def test_many_tiles():
     """One long sequence: every tile's entering state comes from all those before it."""
     x = _inputs(1, 20011, 8, "f32", seed=5, resets=0.0005)
