@@ -312,6 +312,7 @@ __device__ __forceinline__ uint32_t pack_group(const float (&x)[4], bool mine, u
 // whether its token j is one, and whether token j of any row is.
 template <bool Reset, class F, int Sub>
 struct Cuts {
+    static_assert(F::kWaveRows * Sub <= 64, "a wave's tokens are the bits of one ballot");
     uint64_t all;
     uint32_t mine;
     __device__ Cuts(const uint8_t* reset, int64_t at, int64_t left, int row)
