@@ -12,12 +12,20 @@
 // 1 - a^2 is -expm1(2 l): its series for a small argument, 1 - a a otherwise.
 //
 // A span of tokens acts on the state as h -> A h + B, and spans compose, so time is cut:
-// a lane holds kSub consecutive tokens of four channels in registers, a row of 16 lanes a
-// token's 64 channels (128 bytes of bf16), a workgroup 32 such runs in time.  The runs'
+// a lane holds a few consecutive tokens of four channels in registers, a row of 16 lanes the
+// 64 channels of such a run (128 bytes of bf16 a token), a workgroup 32 runs in time.  The runs'
 // (A, B) meet in LDS, where one wave passes through them with a channel in each lane, and
-// across workgroups in the workspace (below), so every input is read once.  A reset inside a span is
-// kept as the sign of A (A is never negative otherwise), since 0 times a state that is not
-// finite would not forget it.  All of it is fp32 and in a fixed order.
+// across workgroups in the workspace (below), so every input is read once.  A reset inside a
+// span is kept as the sign of A (A is never negative otherwise), since 0 times a state that is
+// not finite would not forget it.  All of it is fp32 and in a fixed order.
+//
+// 8 x 2048 tokens of 2048 bf16 channels: forward 52 us, 268 MB or 5.2 TB/s, what a copy of that
+// size reaches; with the inputs' checkpoints written as well a forward of 4 x 2000 tokens of 1536
+// packed channels takes 42 us (3.2 TB/s), three quarters of it arithmetic.  Backward from
+// checkpoints to bf16 gradients 102 us (3.6 TB/s): nine transcendentals and some fifty other
+// instructions an element keep the vector units busy for two thirds of the time, and the rest is
+// each workgroup waiting for its first loads and its walk.  One row of 16381 tokens: 63 us, its 64
+// tiles one behind the other.  One token of 1 x 2048 or 256 x 2048 channels is one launch.
 #include <algorithm>
 #include <type_traits>
 
@@ -57,6 +65,13 @@ __device__ __forceinline__ Span join(Span lo, Span hi)
     return {hard ? hi.A : lo.A * hi.A, apply<Reset>(hi, lo.B)};
 }
 __device__ __forceinline__ Span nothing() { return {1.0f, 0.0f}; }
+// adds a token to the span (A, B) of those before it
+template <bool Reset>
+__device__ __forceinline__ void take(Span token, float& A, float& B)
+{
+    const Span s = join<Reset>({A, B}, token);
+    A = s.A, B = s.B;
+}
 
 // The per-channel constants: log2 a_t = rate * s_t.
 struct Rates {
@@ -110,10 +125,11 @@ __device__ __forceinline__ Span terms(float x, float r, float i, float rate, boo
 // of workgroups that fit the GPU.  A span and its "published" mark are one 8-byte word
 // written and read with single relaxed accesses of agent scope, so no other memory has to be
 // ordered.  The words start as kUnset, written by a fill kernel ahead on the stream.
-constexpr int kJoinOn = 32, kJoinBack = 16;   // forward; backward, with less shared memory to spare
+constexpr int kJoin = 16;
+constexpr int kLook = 8;   // words that a lane asks for at once
 constexpr uint64_t kUnset = ~uint64_t(0);
-// Ticket counters, one for each slab of channels, ahead of the spans: each in a cache line of
-// its own (the GPU's dies draw from one line one at a time), in 64-bit words.
+// Ticket counters, one for each slab of channels, ahead of the spans, each in a cache line of
+// its own; in 64-bit words.
 constexpr int kCounterWords = 16;
 __host__ __device__ inline int64_t ticket_words(int64_t slabs) { return slabs * kCounterWords; }
 
@@ -124,14 +140,18 @@ __device__ __forceinline__ void publish(uint64_t* at, Span s)
     __hip_atomic_store(at, w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-// The word at `at` of every lane that wants one, once all of them are published.
-__device__ __forceinline__ Span await(const uint64_t* at, bool wanted)
+__device__ __forceinline__ uint64_t look(const uint64_t* at)
 {
-    uint64_t w = 0;
-    for (;;) {
-        if (wanted) w = __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        if (!__any(wanted && w == kUnset)) break;
-        __builtin_amdgcn_s_sleep(2);
+    return __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// The word at `at` of every lane that wants one, once all of them are published; w: what was
+// there at a first look.
+__device__ __forceinline__ Span await(const uint64_t* at, bool wanted, uint64_t w)
+{
+    while (__any(wanted && w == kUnset)) {
+        __builtin_amdgcn_s_sleep(1);
+        if (wanted) w = look(at);
     }
     return {__uint_as_float(uint32_t(w)), __uint_as_float(uint32_t(w >> 32))};
 }
@@ -141,51 +161,48 @@ __global__ __launch_bounds__(256) void recurrence_fill_kernel(ulonglong2* words,
     for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < n; i += int64_t(gridDim.x) * 256) words[i] = make_ulonglong2(kUnset, kUnset);
 }
 
-// Shared memory of a walk: the spans of the lane rows (four to a wave) of a workgroup in
-// planes of A and B, in the order of the walk, and the spans of the tiles before it.  The
-// state entering a row takes the place of its B.
+// What the lane rows of a workgroup do to the state, in shared memory: a plane of their A and one
+// of their B, by time.  The state entering a row takes the place of its B.
 template <int kCh>
-struct RowSpans {
-    float A[kRows][kCh], B[kRows][kCh];
+using Plane = float[kRows][kCh];
 
-    __device__ void put(int r, int col, const Span (&s)[4])
-    {
-        *reinterpret_cast<float4*>(&A[r][col * 4]) = make_float4(s[0].A, s[1].A, s[2].A, s[3].A);
-        *reinterpret_cast<float4*>(&B[r][col * 4]) = make_float4(s[0].B, s[1].B, s[2].B, s[3].B);
-    }
-    __device__ void entering(int r, int col, float (&h)[4]) const
-    {
-        const float4 f = *reinterpret_cast<const float4*>(&B[r][col * 4]);
-        h[0] = f.x, h[1] = f.y, h[2] = f.z, h[3] = f.w;
-    }
-    // for a wave whose lanes take a channel each: all rows together, and from the state ahead
-    // of them the one that enters each; returns the one that leaves them
-    template <bool Reset>
-    __device__ Span all(int lane) const
-    {
-        Span s = nothing();
+template <int kCh>
+__device__ __forceinline__ void put(Plane<kCh>& p, int r, int col, const float (&x)[4])
+{
+    *reinterpret_cast<float4*>(&p[r][col * 4]) = make_float4(x[0], x[1], x[2], x[3]);
+}
+template <int kCh>
+__device__ __forceinline__ void get(const Plane<kCh>& p, int r, int col, float (&x)[4])
+{
+    const float4 f = *reinterpret_cast<const float4*>(&p[r][col * 4]);
+    x[0] = f.x, x[1] = f.y, x[2] = f.z, x[3] = f.w;
+}
+// for a wave whose lanes take a channel each (Back: from the last row to the first): all rows
+// together, and from the state ahead of them the one that enters each; returns the one that
+// leaves them
+template <bool Reset, bool Back, int kCh>
+__device__ __forceinline__ Span join_rows(const Plane<kCh>& A, const Plane<kCh>& B, int lane)
+{
+    Span s = nothing();
 #pragma unroll 8
-        for (int r = 0; r < kRows; ++r) s = join<Reset>(s, {A[r][lane], B[r][lane]});
-        return s;
+    for (int r = 0; r < kRows; ++r) {
+        const int at = Back ? kRows - 1 - r : r;
+        s = join<Reset>(s, {A[at][lane], B[at][lane]});
     }
-    template <bool Reset>
-    __device__ float pass(int lane, float h)
-    {
+    return s;
+}
+template <bool Reset, bool Back, int kCh>
+__device__ __forceinline__ float pass_rows(const Plane<kCh>& A, Plane<kCh>& B, int lane, float h)
+{
 #pragma unroll 8
-        for (int r = 0; r < kRows; ++r) {
-            const Span s = {A[r][lane], B[r][lane]};
-            B[r][lane] = h;
-            h = apply<Reset>(s, h);
-        }
-        return h;
+    for (int r = 0; r < kRows; ++r) {
+        const int at = Back ? kRows - 1 - r : r;
+        const Span s = {A[at][lane], B[at][lane]};
+        B[at][lane] = h;
+        h = apply<Reset>(s, h);
     }
-};
-template <int kCh, int kJoin>
-struct WalkShared {
-    RowSpans<kCh> rows;
-    float2 before[kJoin][kCh];
-    int ticket;
-};
+    return h;
+}
 
 // The workgroup's place in the call.  Its slab of channels goes by its index, so that the
 // channels' constants are on their way while the ticket is drawn (a counter for each slab);
@@ -201,63 +218,76 @@ __device__ __forceinline__ int draw_ticket(uint64_t* words, bool many, int slab,
     if (threadIdx.x != 0) return 0;
     return int(__hip_atomic_fetch_add(reinterpret_cast<uint32_t*>(words + slab * kCounterWords), 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1u);
 }
-template <class Shared>
-__device__ __forceinline__ Place place_of(int ticket, bool many, int64_t batch, Shared& sh)
+__device__ __forceinline__ Place place_of(int ticket, bool many, int64_t batch, int& shared)
 {
     if (many) {
-        if (threadIdx.x == 0) sh.ticket = ticket;
+        if (threadIdx.x == 0) shared = ticket;
         __syncthreads();
-        ticket = sh.ticket;
+        ticket = shared;
     }
     const uint32_t id = uint32_t(__builtin_amdgcn_readfirstlane(ticket)), step = id / uint32_t(batch);
     return {int64_t(id - step * uint32_t(batch)), int(step)};
 }
 
-// From the rows' spans (made visible by a barrier) the state entering each of them, after the
-// barrier at the end.  `step` is the tile's place in the walk, `first` the state ahead of the
-// whole walk.  The first wave passes through the rows; the others' time is the compute unit's
-// second workgroup's.
-template <bool Reset, class F, int kJoin>
-__device__ __forceinline__ void walk(WalkShared<F::kCh, kJoin>& sh, uint64_t* words, int64_t batch, int64_t b, int step, int steps,
-                                     int64_t width, int slab, const float* first)
-{
-    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int64_t ch = int64_t(slab) * F::kCh + lane;
-    const bool mine = lane < F::kCh && ch < width;
-    const int group = step / kJoin, at = step % kJoin;
-    const int groups = steps / kJoin;
-    const int64_t slabs = (width + F::kCh - 1) / F::kCh;
-    uint64_t* spans = words + ticket_words(slabs) + b * steps * width + ch;
-    uint64_t* leaves = words + ticket_words(slabs) + batch * steps * width + b * groups * width + ch;
-    if (wave == 0 && lane < F::kCh && at != kJoin - 1 && step + 1 < steps) {
-        __builtin_amdgcn_s_setprio(3);   // other workgroups wait for it
-        const Span s = sh.rows.template all<Reset>(lane);
-        if (mine) publish(spans + int64_t(step) * width, s);
-        __builtin_amdgcn_s_setprio(0);
+// A tile's part in the walk, done by the first wave of its workgroup with a channel in each
+// lane.  `step` is the tile's place in the walk, `first` the state ahead of the whole walk.
+template <bool Reset, bool Back, class F>
+struct Walk {
+    uint64_t* spans;          // of the sequence's tiles, this lane's channel
+    uint64_t* leaves;         // of its groups
+    int64_t width;
+    int step, steps;
+    bool mine;                // the lane has a channel
+    float start;              // entering the walk
+    uint64_t seen[kLook];     // what the first words held: entry 0 the state entering the group, e the group's tile e - 1
+
+    // Taken before the barrier that makes the rows visible, so that the look's way to memory is
+    // part of the wait for the other waves.
+    __device__ void look_ahead(uint64_t* words, int64_t batch, int64_t b, int step_, int steps_, int64_t width_, int slab, const float* first)
+    {
+        step = step_, steps = steps_, width = width_;
+        const int64_t slabs = (width + F::kCh - 1) / F::kCh, groups = steps / kJoin;
+        const int lane = threadIdx.x % kWave;
+        const int64_t ch = int64_t(slab) * F::kCh + lane;
+        mine = lane < F::kCh && ch < width;
+        spans = words + ticket_words(slabs) + b * steps * width + ch;
+        leaves = words + ticket_words(slabs) + batch * steps * width + b * groups * width + ch;
+        const int group = step / kJoin, at = step % kJoin;
+        start = group == 0 && first != nullptr && mine ? first[b * width + ch] : 0.0f;
+        seen[0] = group > 0 && mine ? look(leaves + int64_t(group - 1) * width) : 0;
+#pragma unroll
+        for (int e = 1; e < kLook; ++e) seen[e] = e <= at && mine ? look(entry(group, e)) : 0;
     }
-    // entry 0 is the state entering the group, entry e the span of the group's tile e - 1; the
-    // first wave, which publishes, comes last
-    for (int e = F::kWaves - 1 - wave; e <= at; e += F::kWaves) {
-        Span s;
-        if (e > 0)
-            s = await(spans + int64_t(group * kJoin + e - 1) * width, mine);
-        else if (group > 0)
-            s = await(leaves + int64_t(group - 1) * width, mine);
-        else
-            s = {-0.0f, first != nullptr && mine ? first[b * width + ch] : 0.0f};
-        if (lane < F::kCh) sh.before[e][lane] = make_float2(s.A, s.B);
-    }
-    __syncthreads();
-    if (wave == 0 && lane < F::kCh) {
-        __builtin_amdgcn_s_setprio(3);   // the others wait for it
-        float h = sh.before[0][lane].y;
-        for (int e = 1; e <= at; ++e) h = apply<Reset>({sh.before[e][lane].x, sh.before[e][lane].y}, h);
-        h = sh.rows.template pass<Reset>(lane, h);
+    __device__ const uint64_t* entry(int group, int e) const { return spans + int64_t(group * kJoin + e - 1) * width; }
+
+    // The rows' entering states, in the place of their B: first this tile's span is published,
+    // then what the tiles before it published is taken in.
+    __device__ void pass(const Plane<F::kCh>& A, Plane<F::kCh>& B)
+    {
+        const int lane = threadIdx.x % kWave, group = step / kJoin, at = step % kJoin;
+        if (lane >= F::kCh) return;
+        __builtin_amdgcn_s_setprio(3);   // the other waves wait for it, and other workgroups
+        if (at != kJoin - 1 && step + 1 < steps) {
+            const Span s = join_rows<Reset, Back>(A, B, lane);
+            if (mine) publish(spans + int64_t(step) * width, s);
+        }
+        float h = group > 0 ? await(leaves + int64_t(group - 1) * width, mine, seen[0]).B : start;
+#pragma unroll
+        for (int e = 1; e < kLook; ++e)
+            if (e <= at) h = apply<Reset>(await(entry(group, e), mine, seen[e]), h);
+#pragma unroll 1
+        for (int e0 = kLook; e0 <= at; e0 += kLook) {
+#pragma unroll
+            for (int e = 0; e < kLook; ++e) seen[e] = e0 + e <= at && mine ? look(entry(group, e0 + e)) : 0;
+#pragma unroll
+            for (int e = 0; e < kLook; ++e)
+                if (e0 + e <= at) h = apply<Reset>(await(entry(group, e0 + e), mine, seen[e]), h);
+        }
+        h = pass_rows<Reset, Back>(A, B, lane, h);
         if (mine && at == kJoin - 1 && step + 1 < steps) publish(leaves + int64_t(group) * width, {-0.0f, h});
         __builtin_amdgcn_s_setprio(0);
     }
-    __syncthreads();
-}
+};
 
 // Makes a value opaque at this point: what is derived from it is derived here again, instead
 // of being kept in registers from an earlier place.
@@ -338,7 +368,10 @@ template <typename T, bool Vec, bool Reset, bool Kept, class F>
 __global__ __launch_bounds__(F::kThreads, (Vec ? 4 : 2)) void recurrence_kernel(RecurrenceArgs a)
 {
     constexpr int kAcross = F::kAcross, kCh = F::kCh, kWaveRows = F::kWaveRows;
-    __shared__ WalkShared<kCh, kJoinOn> sh;
+    __shared__ struct {
+        Plane<kCh> A, B;
+        int ticket;
+    } sh;
     const int slabs = int((a.width + kCh - 1) / kCh);
     const int slab = int(blockIdx.x) % slabs, ticket = draw_ticket(a.words, a.tiles > 1, slab, slabs);
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -346,7 +379,7 @@ __global__ __launch_bounds__(F::kThreads, (Vec ? 4 : 2)) void recurrence_kernel(
     const int64_t ch0 = int64_t(slab) * kCh, ch = ch0 + col * 4;
     const int n = int(max<int64_t>(0, min<int64_t>(4, a.width - ch)));   // channels of this lane
     const Rates k = rates_of(a.theta, a.decay, ch, n);
-    const Place at = place_of(ticket, a.tiles > 1, a.batch, sh);
+    const Place at = place_of(ticket, a.tiles > 1, a.batch, sh.ticket);
     const int64_t w0 = int64_t(at.step) * kFwdTile + wave * kWaveRows * kFwdSub;  // the wave's first token
     const int64_t token0 = at.b * a.seq_len + w0;
     const int left = there_are(a.seq_len - w0 - row * kFwdSub, kFwdSub);  // of the lane's tokens
@@ -374,6 +407,7 @@ __global__ __launch_bounds__(F::kThreads, (Vec ? 4 : 2)) void recurrence_kernel(
     }
     const Cuts<Reset, F, kFwdSub> cuts(a.reset, token0, a.seq_len - w0, row);
     if constexpr (Kept) {
+        // ordinary stores: the backward pass is the next to read them
         uint8_t* const kept[3] = {a.kept_x, a.kept_r, a.kept_i};
         const int64_t groups = (a.width + kGroup - 1) / kGroup;
         const int64_t codes_at = token0 * a.width + ch0;
@@ -392,7 +426,7 @@ __global__ __launch_bounds__(F::kThreads, (Vec ? 4 : 2)) void recurrence_kernel(
 #pragma unroll
                 for (int q = 0; q < 3; ++q) {
                     if constexpr (Vec) {
-                        store_at(kept[q] + codes_at + j * a.width, c_off, codes[q]);
+                        *reinterpret_cast<uint32_t*>(kept[q] + codes_at + j * a.width + c_off) = codes[q];
                     } else {
                         uint8_t* out = kept[q] + codes_at + (row * kFwdSub + j) * a.width + col * 4;
 #pragma unroll
@@ -404,7 +438,7 @@ __global__ __launch_bounds__(F::kThreads, (Vec ? 4 : 2)) void recurrence_kernel(
 #pragma unroll
                     for (int q = 0; q < 3; ++q) {
                         if constexpr (Vec)
-                            store_at(kept[q] + bytes_at + j * groups, b_off, uint8_t(byte[q]));
+                            kept[q][bytes_at + j * groups + b_off] = uint8_t(byte[q]);
                         else
                             kept[q][bytes_at + (row * kFwdSub + j) * groups + col / 8] = uint8_t(byte[q]);
                     }
@@ -412,9 +446,10 @@ __global__ __launch_bounds__(F::kThreads, (Vec ? 4 : 2)) void recurrence_kernel(
             }
         }
     }
-    Span e[kFwdSub][4], own[4];
+    Span e[kFwdSub][4];
+    float ownA[4], ownB[4];
 #pragma unroll
-    for (int v = 0; v < 4; ++v) own[v] = nothing();
+    for (int v = 0; v < 4; ++v) ownA[v] = 1.0f, ownB[v] = 0.0f;
 #pragma unroll
     for (int j = 0; j < kFwdSub; ++j) {
         float x[4], r[4], i[4];
@@ -428,18 +463,22 @@ __global__ __launch_bounds__(F::kThreads, (Vec ? 4 : 2)) void recurrence_kernel(
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
                 if (cuts.lane(j)) e[j][v] = terms<true>(x[v], r[v], i[v], k.v[v], true);
-                own[v] = join<true>(own[v], e[j][v]);
+                take<true>(e[j][v], ownA[v], ownB[v]);
             }
         } else {
 #pragma unroll
-            for (int v = 0; v < 4; ++v) own[v] = {own[v].A * e[j][v].A, apply<false>(e[j][v], own[v].B)};
+            for (int v = 0; v < 4; ++v) take<false>(e[j][v], ownA[v], ownB[v]);
         }
     }
-    sh.rows.put(wave * kWaveRows + row, col, own);
+    put<kCh>(sh.A, wave * kWaveRows + row, col, ownA);
+    put<kCh>(sh.B, wave * kWaveRows + row, col, ownB);
+    Walk<Reset, false, F> walk;
+    if (wave == 0) walk.look_ahead(a.words, a.batch, at.b, at.step, a.tiles, a.width, slab, a.h0);
     __syncthreads();
-    walk<Reset, F>(sh, a.words, a.batch, at.b, at.step, a.tiles, a.width, slab, a.h0);
+    if (wave == 0) walk.pass(sh.A, sh.B);
+    __syncthreads();
     float h[4];
-    sh.rows.entering(wave * kWaveRows + row, col, h);
+    get<kCh>(sh.B, wave * kWaveRows + row, col, h);
     const int64_t t0 = w0 + row * kFwdSub;
     if (a.states != nullptr && t0 % kBlock == 0 && left > 0)
         Lane4<float>::store<false>(a.states, (at.b * ((a.seq_len + kBlock - 1) / kBlock) + t0 / kBlock) * a.width + ch, n, h);
@@ -541,15 +580,15 @@ struct Kept {
 };
 
 // Lean: 16-bit gradients of 8- or 16-bit inputs run two workgroups a compute unit, with 128
-// registers a lane, and keep m and the spans ahead of a lane's own in LDS.  With fp32 arrays one
-// workgroup of up to 256 registers is as fast as those would be with spills.
+// registers a lane, and keep m in LDS.  With fp32 arrays, whose four inputs alone are 64
+// registers, that many would spill: one workgroup of up to 256.
 template <typename T, typename Tg>
 constexpr bool kLean = sizeof(T) <= 2 && sizeof(Tg) == 2;
 
 template <bool Lean, class F>
 struct BackwardShared {
-    WalkShared<F::kCh, kJoinBack> back;          // the walk back: its first row is the workgroup's last
-    RowSpans<F::kCh> on;                         // the rows on the way forward
+    Plane<F::kCh> A, on, back;    // a row's A is the same on the way forward and on the way back
+    int ticket;
 };
 template <class F>
 struct BackwardShared<true, F> : BackwardShared<false, F> {
@@ -572,7 +611,7 @@ __global__ __launch_bounds__(F::kThreads, (kLean<T, Tg> ? 4 : 2)) void recurrenc
     const int64_t ch0 = int64_t(slab) * kCh, ch = ch0 + col * 4;
     const int n = int(max<int64_t>(0, min<int64_t>(4, a.width - ch)));
     const Rates k = rates_of(a.theta, a.decay, ch, n);
-    const Place at = place_of(ticket, a.tiles > 1, a.batch, sh.back);
+    const Place at = place_of(ticket, a.tiles > 1, a.batch, sh.ticket);
     const int64_t tile = a.tiles - 1 - at.step;
     const int64_t w0 = tile * kBwdTile + wave * kWaveRows * kBwdSub;
     const int64_t token0 = at.b * a.seq_len + w0;
@@ -602,11 +641,12 @@ __global__ __launch_bounds__(F::kThreads, (kLean<T, Tg> ? 4 : 2)) void recurrenc
     }
     const Cuts<Reset, F, kBwdSub> cuts(a.reset, token0, a.seq_len - w0, row);
     // the lane's tokens: their factors, and what they do together to the state and, on the way
-    // back, to its gradient
+    // back, to its gradient; tokens past the end do nothing to either
+    const bool whole = w0 + kWaveRows * kBwdSub <= a.seq_len;
     Kept e[kBwdSub][4];
-    Span fwd[4], bwd[4];
+    float A[4], on[4], back[4];
 #pragma unroll
-    for (int v = 0; v < 4; ++v) fwd[v] = bwd[v] = nothing();
+    for (int v = 0; v < 4; ++v) A[v] = 1.0f, on[v] = back[v] = 0.0f;
 #pragma unroll
     for (int j = 0; j < kBwdSub; ++j) {
         float x[4], r[4], i[4], m[4], in[4];
@@ -631,6 +671,10 @@ __global__ __launch_bounds__(F::kThreads, (kLean<T, Tg> ? 4 : 2)) void recurrenc
 #pragma unroll
             for (int v = 0; v < 4; ++v) e[j][v].a = -0.0f, m[v] = 1.0f;
         }
+        if (!whole && j >= left) {
+#pragma unroll
+            for (int v = 0; v < 4; ++v) e[j][v].a = m[v] = 1.0f, in[v] = 0.0f;
+        }
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
             Kept& q = e[j][v];
@@ -641,10 +685,10 @@ __global__ __launch_bounds__(F::kThreads, (kLean<T, Tg> ? 4 : 2)) void recurrenc
         if constexpr (Lean) sh.m[j][threadIdx.x] = to_float4(m);
         if (cut) {
 #pragma unroll
-            for (int v = 0; v < 4; ++v) fwd[v] = join<true>(fwd[v], {e[j][v].a, e[j][v].hp});
+            for (int v = 0; v < 4; ++v) take<true>({e[j][v].a, e[j][v].hp}, A[v], on[v]);
         } else {
 #pragma unroll
-            for (int v = 0; v < 4; ++v) fwd[v] = {fwd[v].A * e[j][v].a, fmaf(e[j][v].a, fwd[v].B, e[j][v].hp)};
+            for (int v = 0; v < 4; ++v) take<false>({e[j][v].a, e[j][v].hp}, A[v], on[v]);
         }
     }
 #pragma unroll
@@ -652,27 +696,30 @@ __global__ __launch_bounds__(F::kThreads, (kLean<T, Tg> ? 4 : 2)) void recurrenc
         float d[4];
         pin(rd[j]);
         Lane4<Tg>::widen(rd[j], d);
-        if (j < left) {   // a token past the end leaves the gradient alone
+        if (!whole && j >= left) continue;
 #pragma unroll
-            for (int v = 0; v < 4; ++v) bwd[v] = {bwd[v].A * e[j][v].a, e[j][v].a * (bwd[v].B + d[v])};   // c -> a (dy + c)
-            if (cuts.any(j) && cuts.lane(j)) {
+        for (int v = 0; v < 4; ++v) back[v] = e[j][v].a * (back[v] + d[v]);   // c -> a (dy + c)
+        if (cuts.any(j) && cuts.lane(j)) {
 #pragma unroll
-                for (int v = 0; v < 4; ++v) bwd[v] = {-0.0f, 0.0f};   // a reset's c is 0 whatever comes after
-            }
+            for (int v = 0; v < 4; ++v) A[v] = -0.0f, back[v] = 0.0f;   // a reset's c is 0 whatever comes after (A may be a NaN by now)
         }
     }
-    const int my_row = wave * kWaveRows + row, my_back = kRows - 1 - my_row;
-    sh.on.put(my_row, col, fwd);
-    sh.back.rows.put(my_back, col, bwd);
+    const int my_row = wave * kWaveRows + row;
+    put<kCh>(sh.A, my_row, col, A);
+    put<kCh>(sh.on, my_row, col, on);
+    put<kCh>(sh.back, my_row, col, back);
     const int64_t my = ch0 + lane;
     float state = 0.0f;      // wave 1: the state entering the tile, a channel a lane
     if (wave == 1 && lane < kCh && my < a.width) state = a.states[(at.b * a.tiles + tile) * a.width + my];
+    Walk<Reset, true, F> walk;
+    if (wave == 0) walk.look_ahead(a.words, a.batch, at.b, at.step, a.tiles, a.width, slab, a.dfinal);
     __syncthreads();
-    if (wave == 1 && lane < kCh) sh.on.template pass<Reset>(lane, state);
-    walk<Reset, F>(sh.back, a.words, a.batch, at.b, at.step, a.tiles, a.width, slab, a.dfinal);
+    if (wave == 0) walk.pass(sh.A, sh.back);
+    if (wave == 1 && lane < kCh) pass_rows<Reset, false>(sh.A, sh.on, lane, state);
+    __syncthreads();
     float h[4], c[4], dth[4] = {0.f, 0.f, 0.f, 0.f};
-    sh.on.entering(my_row, col, h);
-    sh.back.rows.entering(my_back, col, c);
+    get<kCh>(sh.on, my_row, col, h);
+    get<kCh>(sh.back, my_row, col, c);
 #pragma unroll
     for (int j = 0; j < kBwdSub; ++j) {
         const bool cut = cuts.any(j);
@@ -705,8 +752,9 @@ __global__ __launch_bounds__(F::kThreads, (kLean<T, Tg> ? 4 : 2)) void recurrenc
             gx[v] = g * m[v] * si;
             gi[v] = gx[v] * x[v] * rest_of(q.ei, si);
             const float dl = ag * fmaf(-q.a * __builtin_amdgcn_rcpf(m[v]), si * x[v], q.hp);
-            gr[v] = cut ? 0.0f : dl * (k.v[v] * kLn2 * s * rest_of(q.er, s));
-            dth[v] = cut ? dth[v] : fmaf(dl, s, dth[v]);
+            const float dls = cut ? 0.0f : dl * s;
+            gr[v] = cut ? 0.0f : dls * (k.v[v] * kLn2 * rest_of(q.er, s));
+            dth[v] += dls;
             c[v] = cut ? 0.0f : ag;
         }
         const int64_t at_row = (token0 + j) * a.grad_stride + ch0;
@@ -717,12 +765,12 @@ __global__ __launch_bounds__(F::kThreads, (kLean<T, Tg> ? 4 : 2)) void recurrenc
     if (a.dh0 != nullptr && tile == 0 && wave == 0 && row == 0) Lane4<float>::store<false>(a.dh0, at.b * a.width + ch, n, c);
     // dtheta: the tile's sum of dl s, one row of the partial sums; the rows' sums take the place
     // of their entering states
-    *reinterpret_cast<float4*>(&sh.on.B[my_row][col * 4]) = to_float4(dth);
+    put<kCh>(sh.on, my_row, col, dth);
     __syncthreads();
     if (wave == 0 && lane < kCh) {
         float s = 0.0f;
 #pragma unroll 8
-        for (int r = 0; r < kRows; ++r) s += sh.on.B[r][lane];
+        for (int r = 0; r < kRows; ++r) s += sh.on[r][lane];
         if (my < a.width) a.partial[(at.b * a.tiles + tile) * a.width + my] = s;
     }
 }
@@ -859,8 +907,8 @@ int64_t recurrence_tiles(int64_t seq_len) { return (seq_len + kFwdTile - 1) / kF
 int64_t recurrence_walk_bytes(int64_t batch, int64_t tiles, int64_t width)
 {
     if (tiles <= 1) return 0;
-    // counters for the narrow workgroups, leaves for the shorter groups: enough for either form and way
-    return (ticket_words((width + Narrow::kCh - 1) / Narrow::kCh) + batch * (tiles + tiles / kJoinBack) * width + 1) / 2 * 16;
+    // counters for the narrow workgroups: enough for either form
+    return (ticket_words((width + Narrow::kCh - 1) / Narrow::kCh) + batch * (tiles + tiles / kJoin) * width + 1) / 2 * 16;
 }
 
 hipError_t launch_recurrence(const RecurrenceArgs& a, hipStream_t stream)

@@ -235,6 +235,27 @@ def test_a_reset_reads_nothing_before_it(at):
         assert np.all(np.isfinite(got[1])) and np.all(np.isfinite(got[0]) == np.isfinite(want[n][0])), n
 
 
+@pytest.mark.parametrize("at,bad", [(2, 3), (5, 6), (130, 131), (130, 170), (300, 699)])
+def test_a_reset_hands_no_gradient_back(at, bad):
+    """NaN gates and gradients at tokens after a reset do not reach those before it."""
+    x = _inputs(2, 700, 68, "f32", seed=bad)
+    x["reset"] = np.zeros((2, 700), np.uint8)
+    x["reset"][0, at] = 1
+    x["r"][0, bad, 7] = np.nan
+    x["dy"][0, bad, 9] = np.inf
+    x["dfinal"][0, 11] = np.nan
+    d = _dev(x, "f32")
+    f = L.recurrence(d["x"], d["r"], d["i"], d["theta"], reset=d["reset"], h0=d["h0"], want_states=True)
+    g = L.recurrence_backward(d["x"], d["r"], d["i"], d["theta"], f["states"], d["dy"], d["dfinal"], reset=d["reset"])
+    want = R.backward(x["x"], x["r"], x["i"], x["theta"], _np(f["states"]), x["dy"], x["dfinal"], reset=x["reset"])
+    assert np.all(np.isfinite(_np(g["dh0"])))
+    for n in ("dx", "dr", "di"):
+        got = _np(g[n])
+        assert not np.isfinite(got[0, bad, 9]) or n == "dr", n
+        assert np.all(np.isfinite(got[0, :at])) and np.all(np.isfinite(got[1])), n
+        assert rel_l2(got[0, :at], want[n][0, :at]) <= TOL_GRAD and rel_l2(got[1], want[n][1]) <= TOL_GRAD, n
+
+
 def test_gates_at_their_ends():
     """Gates shut and open past fp32's exponential, no decay at all, a decay that forgets at once."""
     x = _inputs(1, 140, 12, "f32", seed=9)
