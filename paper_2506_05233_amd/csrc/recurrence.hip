@@ -192,13 +192,13 @@ __device__ __forceinline__ Span join_rows(const Plane<kCh>& A, const Plane<kCh>&
     return s;
 }
 template <bool Reset, bool Back, int kCh>
-__device__ __forceinline__ float pass_rows(const Plane<kCh>& A, Plane<kCh>& B, int lane, float h)
+__device__ __forceinline__ float pass_rows(const Plane<kCh>& A, const Plane<kCh>& B, Plane<kCh>& in, int lane, float h)
 {
 #pragma unroll 8
     for (int r = 0; r < kRows; ++r) {
         const int at = Back ? kRows - 1 - r : r;
         const Span s = {A[at][lane], B[at][lane]};
-        B[at][lane] = h;
+        in[at][lane] = h;
         h = apply<Reset>(s, h);
     }
     return h;
@@ -243,7 +243,7 @@ struct Walk {
 
     // Taken before the barrier that makes the rows visible, so that the look's way to memory is
     // part of the wait for the other waves.
-    __device__ void look_ahead(uint64_t* words, int64_t batch, int64_t b, int step_, int steps_, int64_t width_, int slab, const float* first)
+    __device__ void find(uint64_t* words, int64_t batch, int64_t b, int step_, int steps_, int64_t width_, int slab)
     {
         step = step_, steps = steps_, width = width_;
         const int64_t slabs = (width + F::kCh - 1) / F::kCh, groups = steps / kJoin;
@@ -252,8 +252,11 @@ struct Walk {
         mine = lane < F::kCh && ch < width;
         spans = words + ticket_words(slabs) + b * steps * width + ch;
         leaves = words + ticket_words(slabs) + batch * steps * width + b * groups * width + ch;
+    }
+    __device__ void look_ahead(const float* first, int64_t b, int slab)
+    {
         const int group = step / kJoin, at = step % kJoin;
-        start = group == 0 && first != nullptr && mine ? first[b * width + ch] : 0.0f;
+        start = group == 0 && first != nullptr && mine ? first[b * width + int64_t(slab) * F::kCh + threadIdx.x % kWave] : 0.0f;
         seen[0] = group > 0 && mine ? look(leaves + int64_t(group - 1) * width) : 0;
 #pragma unroll
         for (int e = 1; e < kLook; ++e) seen[e] = e <= at && mine ? look(entry(group, e)) : 0;
@@ -262,15 +265,20 @@ struct Walk {
 
     // The rows' entering states, in the place of their B: first this tile's span is published,
     // then what the tiles before it published is taken in.
-    __device__ void pass(const Plane<F::kCh>& A, Plane<F::kCh>& B)
+    __device__ void tell(const Plane<F::kCh>& A, const Plane<F::kCh>& B)
+    {
+        const int lane = threadIdx.x % kWave;
+        if (lane >= F::kCh || step % kJoin == kJoin - 1 || step + 1 >= steps) return;
+        __builtin_amdgcn_s_setprio(3);   // other workgroups wait for it
+        const Span s = join_rows<Reset, Back>(A, B, lane);
+        if (mine) publish(spans + int64_t(step) * width, s);
+        __builtin_amdgcn_s_setprio(0);
+    }
+    __device__ void pass(const Plane<F::kCh>& A, const Plane<F::kCh>& B, Plane<F::kCh>& in)
     {
         const int lane = threadIdx.x % kWave, group = step / kJoin, at = step % kJoin;
         if (lane >= F::kCh) return;
         __builtin_amdgcn_s_setprio(3);   // the other waves wait for it, and other workgroups
-        if (at != kJoin - 1 && step + 1 < steps) {
-            const Span s = join_rows<Reset, Back>(A, B, lane);
-            if (mine) publish(spans + int64_t(step) * width, s);
-        }
         float h = group > 0 ? await(leaves + int64_t(group - 1) * width, mine, seen[0]).B : start;
 #pragma unroll
         for (int e = 1; e < kLook; ++e)
@@ -283,7 +291,7 @@ struct Walk {
             for (int e = 0; e < kLook; ++e)
                 if (e0 + e <= at) h = apply<Reset>(await(entry(group, e0 + e), mine, seen[e]), h);
         }
-        h = pass_rows<Reset, Back>(A, B, lane, h);
+        h = pass_rows<Reset, Back>(A, B, in, lane, h);
         if (mine && at == kJoin - 1 && step + 1 < steps) publish(leaves + int64_t(group) * width, {-0.0f, h});
         __builtin_amdgcn_s_setprio(0);
     }
@@ -345,14 +353,16 @@ struct Cuts {
     static_assert(F::kWaveRows * Sub <= 64, "a wave's tokens are the bits of one ballot");
     uint64_t all;
     uint32_t mine;
-    __device__ Cuts(const uint8_t* reset, int64_t at, int64_t left, int row)
+    // The mark of the wave's token `lane`, asked for ahead of the tiles: loads return in order.
+    __device__ static uint32_t ask(const uint8_t* reset, int64_t at, int64_t left)
     {
         const int lane = threadIdx.x % kWave;
-        all = mine = 0;
-        if constexpr (Reset) {
-            if (reset != nullptr) all = __ballot(lane < F::kWaveRows * Sub && lane < left && reset[at + lane] != 0);
-            mine = uint32_t(all >> (row * Sub));
-        }
+        return Reset && reset != nullptr && lane < F::kWaveRows * Sub && lane < left ? reset[at + lane] : 0u;
+    }
+    __device__ Cuts(uint32_t mark, int row)
+    {
+        all = Reset ? __ballot(mark != 0) : 0;
+        mine = uint32_t(all >> (row * Sub));
     }
     __device__ bool lane(int j) const { return Reset && ((mine >> j) & 1u) != 0; }
     __device__ bool any(int j) const
@@ -383,6 +393,7 @@ __global__ __launch_bounds__(F::kThreads, (Vec ? 4 : 2)) void recurrence_kernel(
     const int64_t w0 = int64_t(at.step) * kFwdTile + wave * kWaveRows * kFwdSub;  // the wave's first token
     const int64_t token0 = at.b * a.seq_len + w0;
     const int left = there_are(a.seq_len - w0 - row * kFwdSub, kFwdSub);  // of the lane's tokens
+    const uint32_t mark = Cuts<Reset, F, kFwdSub>::ask(a.reset, token0, a.seq_len - w0);
 
     // Tokens past the end come after all others, so the state that they would leave is used by
     // nobody: they and channels past the last are read as copies of existing ones.
@@ -405,7 +416,7 @@ __global__ __launch_bounds__(F::kThreads, (Vec ? 4 : 2)) void recurrence_kernel(
             ri[j] = Lane4<T>::template load_near<Vec>(a.i, at_row, ch, ch0, a.width - 1);
         }
     }
-    const Cuts<Reset, F, kFwdSub> cuts(a.reset, token0, a.seq_len - w0, row);
+    const Cuts<Reset, F, kFwdSub> cuts(mark, row);
     if constexpr (Kept) {
         // ordinary stores: the backward pass is the next to read them
         uint8_t* const kept[3] = {a.kept_x, a.kept_r, a.kept_i};
@@ -473,9 +484,9 @@ __global__ __launch_bounds__(F::kThreads, (Vec ? 4 : 2)) void recurrence_kernel(
     put<kCh>(sh.A, wave * kWaveRows + row, col, ownA);
     put<kCh>(sh.B, wave * kWaveRows + row, col, ownB);
     Walk<Reset, false, F> walk;
-    if (wave == 0) walk.look_ahead(a.words, a.batch, at.b, at.step, a.tiles, a.width, slab, a.h0);
+    if (wave == 0) walk.find(a.words, a.batch, at.b, at.step, a.tiles, a.width, slab), walk.look_ahead(a.h0, at.b, slab);
     __syncthreads();
-    if (wave == 0) walk.pass(sh.A, sh.B);
+    if (wave == 0) walk.tell(sh.A, sh.B), walk.pass(sh.A, sh.B, sh.B);
     __syncthreads();
     float h[4];
     get<kCh>(sh.B, wave * kWaveRows + row, col, h);
@@ -587,7 +598,7 @@ constexpr bool kLean = sizeof(T) <= 2 && sizeof(Tg) == 2;
 
 template <bool Lean, class F>
 struct BackwardShared {
-    Plane<F::kCh> A, on, back;    // a row's A is the same on the way forward and on the way back
+    Plane<F::kCh> A, on, back, in;    // a row's A is the same on the way forward and on the way back
     int ticket;
 };
 template <class F>
@@ -616,6 +627,7 @@ __global__ __launch_bounds__(F::kThreads, (kLean<T, Tg> ? 4 : 2)) void recurrenc
     const int64_t w0 = tile * kBwdTile + wave * kWaveRows * kBwdSub;
     const int64_t token0 = at.b * a.seq_len + w0;
     const int left = there_are(a.seq_len - w0 - row * kBwdSub, kBwdSub);
+    const uint32_t mark = Cuts<Reset, F, kBwdSub>::ask(a.reset, token0, a.seq_len - w0);
 
     typename Source<T>::Raw rx[kBwdSub], rr[kBwdSub], ri[kBwdSub];
     typename Lane4<Tg>::Raw rd[kBwdSub];
@@ -639,7 +651,7 @@ __global__ __launch_bounds__(F::kThreads, (kLean<T, Tg> ? 4 : 2)) void recurrenc
             rd[j] = Lane4<Tg>::template load_near<Vec>(a.dy, token * a.width, ch, ch0, a.width - 1);
         }
     }
-    const Cuts<Reset, F, kBwdSub> cuts(a.reset, token0, a.seq_len - w0, row);
+    const Cuts<Reset, F, kBwdSub> cuts(mark, row);
     // the lane's tokens: their factors, and what they do together to the state and, on the way
     // back, to its gradient; tokens past the end do nothing to either
     const bool whole = w0 + kWaveRows * kBwdSub <= a.seq_len;
@@ -712,28 +724,36 @@ __global__ __launch_bounds__(F::kThreads, (kLean<T, Tg> ? 4 : 2)) void recurrenc
     float state = 0.0f;      // wave 1: the state entering the tile, a channel a lane
     if (wave == 1 && lane < kCh && my < a.width) state = a.states[(at.b * a.tiles + tile) * a.width + my];
     Walk<Reset, true, F> walk;
-    if (wave == 0) walk.look_ahead(a.words, a.batch, at.b, at.step, a.tiles, a.width, slab, a.dfinal);
+    if (wave == 0 || wave == 2) walk.find(a.words, a.batch, at.b, at.step, a.tiles, a.width, slab);
+    if (wave == 0) walk.look_ahead(a.dfinal, at.b, slab);
     __syncthreads();
-    if (wave == 0) walk.pass(sh.A, sh.back);
-    if (wave == 1 && lane < kCh) pass_rows<Reset, false>(sh.A, sh.on, lane, state);
+    if (wave == 0) walk.pass(sh.A, sh.back, sh.in);
+    if (wave == 2) walk.tell(sh.A, sh.back);
+    if (wave == 1 && lane < kCh) {
+        __builtin_amdgcn_s_setprio(3);
+        pass_rows<Reset, false>(sh.A, sh.on, sh.on, lane, state);
+        __builtin_amdgcn_s_setprio(0);
+    }
     __syncthreads();
     float h[4], c[4], dth[4] = {0.f, 0.f, 0.f, 0.f};
     get<kCh>(sh.on, my_row, col, h);
-    get<kCh>(sh.back, my_row, col, c);
+    get<kCh>(sh.in, my_row, col, c);
 #pragma unroll
     for (int j = 0; j < kBwdSub; ++j) {
-        const bool cut = cuts.any(j);
+        float after[4];
 #pragma unroll
-        for (int v = 0; v < 4; ++v) {
-            const Span in = {e[j][v].a, e[j][v].hp};
-            e[j][v].hp = h[v];
-            h[v] = cut ? apply<true>(in, h[v]) : apply<false>(in, h[v]);
+        for (int v = 0; v < 4; ++v) after[v] = apply<false>({e[j][v].a, e[j][v].hp}, h[v]);
+        if (cuts.any(j)) {
+#pragma unroll
+            for (int v = 0; v < 4; ++v) after[v] = apply<true>({e[j][v].a, e[j][v].hp}, h[v]);
         }
+#pragma unroll
+        for (int v = 0; v < 4; ++v) e[j][v].hp = h[v], h[v] = after[v];
     }
 #pragma unroll
     for (int j = kBwdSub - 1; j >= 0; --j) {
         if (j >= left) continue;
-        float x[4], d[4], m[4], gx[4], gr[4], gi[4];
+        float x[4], d[4], m[4], gx[4], gr[4], gi[4], dls[4];
         pin(rx[j]), pin(rd[j]);
         Source<T>::widen(rx[j], 1.0f, x);
         Lane4<Tg>::widen(rd[j], d);
@@ -746,17 +766,21 @@ __global__ __launch_bounds__(F::kThreads, (kLean<T, Tg> ? 4 : 2)) void recurrenc
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
             const Kept& q = e[j][v];
-            const bool cut = cuts.lane(j);
             const float s = gate_of(q.er), si = gate_of(q.ei);
             const float g = d[v] + c[v], ag = q.a * g;
             gx[v] = g * m[v] * si;
             gi[v] = gx[v] * x[v] * rest_of(q.ei, si);
             const float dl = ag * fmaf(-q.a * __builtin_amdgcn_rcpf(m[v]), si * x[v], q.hp);
-            const float dls = cut ? 0.0f : dl * s;
-            gr[v] = cut ? 0.0f : dls * (k.v[v] * kLn2 * rest_of(q.er, s));
-            dth[v] += dls;
-            c[v] = cut ? 0.0f : ag;
+            dls[v] = dl * s;
+            gr[v] = dls[v] * (k.v[v] * kLn2 * rest_of(q.er, s));
+            c[v] = ag;
         }
+        if (cuts.any(j) && cuts.lane(j)) {
+#pragma unroll
+            for (int v = 0; v < 4; ++v) dls[v] = gr[v] = c[v] = 0.0f;
+        }
+#pragma unroll
+        for (int v = 0; v < 4; ++v) dth[v] += dls[v];
         const int64_t at_row = (token0 + j) * a.grad_stride + ch0;
         store_row<Tg, Vec>(a.dx, at_row, row * kBwdSub, a.grad_stride, col, n, gx);
         store_row<Tg, Vec>(a.dr, at_row, row * kBwdSub, a.grad_stride, col, n, gr);
