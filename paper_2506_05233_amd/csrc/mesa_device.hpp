@@ -181,12 +181,4 @@ __device__ __forceinline__ void stream_store(void* p, const T& x)
     __builtin_nontemporal_store(__builtin_bit_cast(words, x), static_cast<words*>(p));
 }
 
-// load_at's counterpart, streaming.
-template <typename T>
-__device__ __forceinline__ void store_at(void* base, uint32_t byte_off, const T& x)
-{
-    asm volatile("" : "+v"(byte_off));
-    stream_store(static_cast<char*>(base) + byte_off, x);
-}
-
 }  // namespace mesa

@@ -222,7 +222,7 @@ struct RecurrenceArgs {
     uint8_t* kept_x;          // checkpoints of x, r, i, all three or null
     uint8_t* kept_r;
     uint8_t* kept_i;
-    int tiles;                // recurrence_tiles(seq_len)
+    int tiles;                // recurrence_tiles(seq_len) or fewer: the launch sets it
     uint64_t* words;          // recurrence_walk_bytes(batch, tiles, width), 16-byte aligned
 };
 int64_t recurrence_tiles(int64_t seq_len);

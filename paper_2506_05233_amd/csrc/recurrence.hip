@@ -19,12 +19,12 @@
 // span is kept as the sign of A (A is never negative otherwise), since 0 times a state that is
 // not finite would not forget it.  All of it is fp32 and in a fixed order.
 //
-// 8 x 2048 tokens of 2048 bf16 channels: forward 52 us, 268 MB or 5.2 TB/s, what a copy of that
+// 8 x 2048 tokens of 2048 bf16 channels: forward 51 us, 268 MB or 5.2 TB/s, what a copy of that
 // size reaches; with the inputs' checkpoints written as well a forward of 4 x 2000 tokens of 1536
-// packed channels takes 42 us (3.2 TB/s), three quarters of it arithmetic.  Backward from
-// checkpoints to bf16 gradients 102 us (3.6 TB/s): nine transcendentals and some fifty other
-// instructions an element keep the vector units busy for two thirds of the time, and the rest is
-// each workgroup waiting for its first loads and its walk.  One row of 16381 tokens: 63 us, its 64
+// packed channels takes 40 us (3.4 TB/s), three quarters of it arithmetic.  Backward from
+// checkpoints to bf16 gradients 93 us (4.0 TB/s): ten transcendentals and some sixty other
+// instructions an element keep the vector units busy for four fifths of the time, and the rest is
+// each workgroup waiting for its first loads and its walk.  One row of 16381 tokens: 60 us, its 64
 // tiles one behind the other.  One token of 1 x 2048 or 256 x 2048 channels is one launch.
 #include <algorithm>
 #include <type_traits>
@@ -73,16 +73,18 @@ __device__ __forceinline__ void take(Span token, float& A, float& B)
     A = s.A, B = s.B;
 }
 
-// The per-channel constants: log2 a_t = rate * s_t.
-struct Rates {
-    float v[4];
-};
-__device__ __forceinline__ Rates rates_of(const float* theta, float decay, int64_t ch, int n)
+// The four theta of a lane whose first channel is channel c of a slab of cols; a channel past the
+// last takes the last one's.
+__device__ __forceinline__ void load_theta(const float* slab, int c, int cols, float (&t)[4])
 {
-    Rates k;
 #pragma unroll
-    for (int v = 0; v < 4; ++v) k.v[v] = v < n ? -decay * kLog2e * softplus_fast(theta[ch + v]) : 0.0f;
-    return k;
+    for (int v = 0; v < 4; ++v) t[v] = slab[uint32_t(min(c + v, cols - 1))];
+}
+// The per-channel constants: by = -decay: log a_t = k s_t; by = -decay log2(e): log2 a_t = k s_t.
+__device__ __forceinline__ void rates_of(const float (&t)[4], float by, float (&k)[4])
+{
+#pragma unroll
+    for (int v = 0; v < 4; ++v) k[v] = by * softplus_fast(t[v]);
 }
 
 // 1 - a^2 = 1 - 4^z for z <= 0 and a = 2^z as rounded: for u = -2 ln 2 z below 1/8 the series
@@ -303,34 +305,56 @@ __device__ __forceinline__ void pin(float& x) { asm volatile("" : "+v"(x)); }
 __device__ __forceinline__ void pin(uint32_t& x) { asm volatile("" : "+v"(x)); }
 __device__ __forceinline__ void pin(uint2& r) { pin(r.x), pin(r.y); }
 __device__ __forceinline__ void pin(float4& r) { pin(r.x), pin(r.y), pin(r.z), pin(r.w); }
-__device__ __forceinline__ void pin(Q8Raw& r) { pin(r.codes), pin(r.byte); }
+__device__ __forceinline__ void pin(Q8Raw& r) { pin(r.codes); }
 
 // ---------------------------------------------------------------- forward
-constexpr int kFwdSub = 8;                         // tokens of a lane
-constexpr int kFwdTile = kRows * kFwdSub;           // tokens of a workgroup
-static_assert(kFwdTile == 2 * kBlock && kBlock % kFwdSub == 0, "a state block starts at a lane's first token");
+// Tokens of a lane: eight where nothing but the state leaves the tile (8 x 2048 tokens of 2048
+// bf16: 51 us, 58 with four); four where the inputs' codes do as well (4 x 2000 of 1536: 42 us
+// with eight, 40 with four) and in the narrow form, whose calls are short (2 x 100 tokens of 768
+// fp32: 7.6 us with eight, 6.0 with four).
+template <class F, bool Kept>
+constexpr int kFwdSub = F::kAcross == 16 && !Kept ? 8 : 4;
+template <class F, bool Kept>
+constexpr int kFwdTile = kRows * kFwdSub<F, Kept>;   // tokens of a workgroup
 
 // A tile's rows are read and written, on the vector path, at an address that the whole wave
-// shares plus an offset of the lane's own in 32 bits (rows at most kNearStride elements apart).
+// shares plus an offset of the lane's own in 32 bits (rows at most kNearStride elements apart),
+// made opaque at each use so that no 64-bit addresses are formed ahead and held.
 constexpr int64_t kNearStride = int64_t(1) << 22;
 
-template <typename T>
-__device__ __forceinline__ typename Lane4<T>::Raw load_row(const void* base, int64_t row, uint32_t off)
+template <typename R>
+__device__ __forceinline__ R load_off(const void* base, uint32_t& off)
 {
-    return load_at<typename Lane4<T>::Raw>(static_cast<const T*>(base) + row, off * uint32_t(sizeof(T)));
+    pin(off);
+    return *reinterpret_cast<const R*>(static_cast<const char*>(base) + off);
 }
+template <typename T>
+__device__ __forceinline__ typename Lane4<T>::Raw load_row(const void* base, int64_t row, uint32_t& off)
+{
+    return load_off<typename Lane4<T>::Raw>(static_cast<const T*>(base) + row, off);
+}
+// Four channels of a token: on the vector path at the row's element `row` and off bytes from
+// there, otherwise at element `at` of that row, n of them.
 template <typename T, bool Vec>
-__device__ __forceinline__ void store_row(void* base, int64_t row, int64_t lane_rows, int64_t stride, int col, int n, const float (&y)[4])
+__device__ __forceinline__ void store_row(void* base, int64_t row, uint32_t& off, int64_t at, int n, const float (&y)[4])
 {
     if constexpr (Vec) {
-        if (n > 0) store_at(static_cast<T*>(base) + row, (uint32_t(lane_rows) * uint32_t(stride) + col * 4) * uint32_t(sizeof(T)), Lane4<T>::narrow(y));
+        pin(off);
+        if (n > 0) stream_store(reinterpret_cast<char*>(static_cast<T*>(base) + row) + off, Lane4<T>::narrow(y));
     } else {
-        Lane4<T>::template store<false>(base, row + lane_rows * stride + col * 4, n, y);
+        Lane4<T>::template store<false>(base, row + at, n, y);
     }
 }
 
-// How many of `most` tokens exist when n are left (which may be none or fewer).
-__device__ __forceinline__ int there_are(int64_t n, int most) { return int(max<int64_t>(0, min<int64_t>(n, most))); }
+// A wave's token w0 and those after it: how many of a run of Sub tokens, the row-th of the wave, exist.
+template <class F, int Sub>
+__device__ __forceinline__ int there_are(int64_t seq_len, int64_t w0, int row)
+{
+    const int wave = int(max<int64_t>(0, min<int64_t>(seq_len - w0, F::kWaveRows * Sub)));
+    return min(max(wave - row * Sub, 0), Sub);
+}
+// How many of a lane's four channels exist, from channel c of a slab of cols.
+__device__ __forceinline__ int channels_of(int c, int cols) { return min(max(cols - c, 0), 4); }
 
 // Eight lanes hold a group of 32 channels: its exponent byte and this lane's four codes.  A lane
 // past the last channel (not mine) has no part in it.
@@ -377,7 +401,8 @@ struct Cuts {
 template <typename T, bool Vec, bool Reset, bool Kept, class F>
 __global__ __launch_bounds__(F::kThreads, (Vec ? 4 : 2)) void recurrence_kernel(RecurrenceArgs a)
 {
-    constexpr int kAcross = F::kAcross, kCh = F::kCh, kWaveRows = F::kWaveRows;
+    constexpr int kAcross = F::kAcross, kCh = F::kCh, kWaveRows = F::kWaveRows, kSub = kFwdSub<F, Kept>, kTile = kFwdTile<F, Kept>;
+    static_assert(kTile % kBlock == 0 && kBlock % kSub == 0, "a state block starts at a lane's first token");
     __shared__ struct {
         Plane<kCh> A, B;
         int ticket;
@@ -387,21 +412,24 @@ __global__ __launch_bounds__(F::kThreads, (Vec ? 4 : 2)) void recurrence_kernel(
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int row = lane / kAcross, col = lane % kAcross;
     const int64_t ch0 = int64_t(slab) * kCh, ch = ch0 + col * 4;
-    const int n = int(max<int64_t>(0, min<int64_t>(4, a.width - ch)));   // channels of this lane
-    const Rates k = rates_of(a.theta, a.decay, ch, n);
+    const int cols = int(min<int64_t>(a.width - ch0, kCh)), n = channels_of(col * 4, cols);
+    float theta[4], k[4];
+    load_theta(a.theta + ch0, col * 4, cols, theta);
     const Place at = place_of(ticket, a.tiles > 1, a.batch, sh.ticket);
-    const int64_t w0 = int64_t(at.step) * kFwdTile + wave * kWaveRows * kFwdSub;  // the wave's first token
+#pragma unroll
+    for (int v = 0; v < 4; ++v) pin(theta[v]);   // here before the tile is asked for, or it would be waited for with it
+    const int64_t w0 = int64_t(at.step) * kTile + wave * kWaveRows * kSub;  // the wave's first token
     const int64_t token0 = at.b * a.seq_len + w0;
-    const int left = there_are(a.seq_len - w0 - row * kFwdSub, kFwdSub);  // of the lane's tokens
-    const uint32_t mark = Cuts<Reset, F, kFwdSub>::ask(a.reset, token0, a.seq_len - w0);
+    const int left = there_are<F, kSub>(a.seq_len, w0, row);  // of the lane's tokens
+    const uint32_t mark = Cuts<Reset, F, kSub>::ask(a.reset, token0, a.seq_len - w0);
 
     // Tokens past the end come after all others, so the state that they would leave is used by
     // nobody: they and channels past the last are read as copies of existing ones.
-    typename Lane4<T>::Raw rx[kFwdSub], rr[kFwdSub], ri[kFwdSub];
-    if (Vec && w0 + kWaveRows * kFwdSub <= a.seq_len) {
-        const uint32_t off = uint32_t(row * kFwdSub) * uint32_t(a.stride) + (n > 0 ? col * 4 : 0);
+    typename Lane4<T>::Raw rx[kSub], rr[kSub], ri[kSub];
+    if (Vec && w0 + kWaveRows * kSub <= a.seq_len) {
+        uint32_t off = (uint32_t(row * kSub) * uint32_t(a.stride) + (n > 0 ? col * 4 : 0)) * uint32_t(sizeof(T));
 #pragma unroll
-        for (int j = 0; j < kFwdSub; ++j) {
+        for (int j = 0; j < kSub; ++j) {
             const int64_t at_row = (token0 + j) * a.stride + ch0;
             rx[j] = load_row<T>(a.x, at_row, off);
             rr[j] = load_row<T>(a.r, at_row, off);
@@ -409,23 +437,24 @@ __global__ __launch_bounds__(F::kThreads, (Vec ? 4 : 2)) void recurrence_kernel(
         }
     } else {
 #pragma unroll
-        for (int j = 0; j < kFwdSub; ++j) {
-            const int64_t at_row = (at.b * a.seq_len + min<int64_t>(w0 + row * kFwdSub + j, a.seq_len - 1)) * a.stride;
+        for (int j = 0; j < kSub; ++j) {
+            const int64_t at_row = (at.b * a.seq_len + min<int64_t>(w0 + row * kSub + j, a.seq_len - 1)) * a.stride;
             rx[j] = Lane4<T>::template load_near<Vec>(a.x, at_row, ch, ch0, a.width - 1);
             rr[j] = Lane4<T>::template load_near<Vec>(a.r, at_row, ch, ch0, a.width - 1);
             ri[j] = Lane4<T>::template load_near<Vec>(a.i, at_row, ch, ch0, a.width - 1);
         }
     }
-    const Cuts<Reset, F, kFwdSub> cuts(mark, row);
+    const Cuts<Reset, F, kSub> cuts(mark, row);
+    rates_of(theta, -a.decay * kLog2e, k);
     if constexpr (Kept) {
         // ordinary stores: the backward pass is the next to read them
         uint8_t* const kept[3] = {a.kept_x, a.kept_r, a.kept_i};
         const int64_t groups = (a.width + kGroup - 1) / kGroup;
         const int64_t codes_at = token0 * a.width + ch0;
         const int64_t bytes_at = checkpoint_exponents_at(a.batch * a.seq_len, a.width) + token0 * groups + ch0 / kGroup;
-        const uint32_t c_off = uint32_t(row * kFwdSub) * uint32_t(a.width) + col * 4, b_off = uint32_t(row * kFwdSub) * uint32_t(groups) + col / 8;
+        const uint32_t c_off = uint32_t(row * kSub) * uint32_t(a.width) + col * 4, b_off = uint32_t(row * kSub) * uint32_t(groups) + col / 8;
 #pragma unroll
-        for (int j = 0; j < kFwdSub; ++j) {
+        for (int j = 0; j < kSub; ++j) {
             uint32_t codes[3], byte[3];
 #pragma unroll
             for (int q = 0; q < 3; ++q) {
@@ -439,7 +468,7 @@ __global__ __launch_bounds__(F::kThreads, (Vec ? 4 : 2)) void recurrence_kernel(
                     if constexpr (Vec) {
                         *reinterpret_cast<uint32_t*>(kept[q] + codes_at + j * a.width + c_off) = codes[q];
                     } else {
-                        uint8_t* out = kept[q] + codes_at + (row * kFwdSub + j) * a.width + col * 4;
+                        uint8_t* out = kept[q] + codes_at + (row * kSub + j) * a.width + col * 4;
 #pragma unroll
                         for (int v = 0; v < 4; ++v)
                             if (v < n) out[v] = uint8_t(codes[q] >> (8 * v));
@@ -451,29 +480,29 @@ __global__ __launch_bounds__(F::kThreads, (Vec ? 4 : 2)) void recurrence_kernel(
                         if constexpr (Vec)
                             kept[q][bytes_at + j * groups + b_off] = uint8_t(byte[q]);
                         else
-                            kept[q][bytes_at + (row * kFwdSub + j) * groups + col / 8] = uint8_t(byte[q]);
+                            kept[q][bytes_at + (row * kSub + j) * groups + col / 8] = uint8_t(byte[q]);
                     }
                 }
             }
         }
     }
-    Span e[kFwdSub][4];
+    Span e[kSub][4];
     float ownA[4], ownB[4];
 #pragma unroll
     for (int v = 0; v < 4; ++v) ownA[v] = 1.0f, ownB[v] = 0.0f;
 #pragma unroll
-    for (int j = 0; j < kFwdSub; ++j) {
+    for (int j = 0; j < kSub; ++j) {
         float x[4], r[4], i[4];
         pin(rx[j]), pin(rr[j]), pin(ri[j]);
         Lane4<T>::widen(rx[j], x);
         Lane4<T>::widen(rr[j], r);
         Lane4<T>::widen(ri[j], i);
 #pragma unroll
-        for (int v = 0; v < 4; ++v) e[j][v] = terms<false>(x[v], r[v], i[v], k.v[v], false);
+        for (int v = 0; v < 4; ++v) e[j][v] = terms<false>(x[v], r[v], i[v], k[v], false);
         if (cuts.any(j)) {
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
-                if (cuts.lane(j)) e[j][v] = terms<true>(x[v], r[v], i[v], k.v[v], true);
+                if (cuts.lane(j)) e[j][v] = terms<true>(x[v], r[v], i[v], k[v], true);
                 take<true>(e[j][v], ownA[v], ownB[v]);
             }
         } else {
@@ -490,12 +519,13 @@ __global__ __launch_bounds__(F::kThreads, (Vec ? 4 : 2)) void recurrence_kernel(
     __syncthreads();
     float h[4];
     get<kCh>(sh.B, wave * kWaveRows + row, col, h);
-    const int64_t t0 = w0 + row * kFwdSub;
+    const int64_t t0 = w0 + row * kSub;
     if (a.states != nullptr && t0 % kBlock == 0 && left > 0)
         Lane4<float>::store<false>(a.states, (at.b * ((a.seq_len + kBlock - 1) / kBlock) + t0 / kBlock) * a.width + ch, n, h);
+    uint32_t y_off = (uint32_t(row * kSub) * uint32_t(a.width) + col * 4) * uint32_t(sizeof(T));
     float* final_h = a.final_h != nullptr ? a.final_h + at.b * a.width + ch : nullptr;
 #pragma unroll
-    for (int j = 0; j < kFwdSub; ++j) {
+    for (int j = 0; j < kSub; ++j) {
         if (cuts.any(j)) {
 #pragma unroll
             for (int v = 0; v < 4; ++v) h[v] = apply<true>(e[j][v], h[v]);
@@ -504,8 +534,8 @@ __global__ __launch_bounds__(F::kThreads, (Vec ? 4 : 2)) void recurrence_kernel(
             for (int v = 0; v < 4; ++v) h[v] = apply<false>(e[j][v], h[v]);
         }
         if (j < left) {
-            store_row<T, Vec>(a.y, (token0 + j) * a.width + ch0, row * kFwdSub, a.width, col, n, h);
-            if (final_h != nullptr && w0 + row * kFwdSub + j == a.seq_len - 1) Lane4<float>::store<false>(final_h, 0, n, h);
+            store_row<T, Vec>(a.y, (token0 + j) * a.width + ch0, y_off, row * kSub * a.width + col * 4, n, h);
+            if (final_h != nullptr && w0 + row * kSub + j == a.seq_len - 1) Lane4<float>::store<false>(final_h, 0, n, h);
         }
     }
 }
@@ -525,9 +555,11 @@ __global__ __launch_bounds__(256) void recurrence_step_kernel(RecurrenceArgs a, 
     Lane4<T>::widen(Lane4<T>::template load<Vec>(a.i, b * a.stride + ch, Per), i);
     Lane4<float>::widen(Lane4<float>::load<Vec>(a.h0, b * a.width + ch, Per), h);
     const bool hard = a.reset != nullptr && a.reset[b] != 0;
-    const Rates k = rates_of(a.theta, a.decay, ch, Per);
+    float theta[4], k[4];
+    load_theta(a.theta + ch, 0, Per, theta);
+    rates_of(theta, -a.decay * kLog2e, k);
 #pragma unroll
-    for (int v = 0; v < Per; ++v) h[v] = apply<true>(terms<true>(x[v], r[v], i[v], k.v[v], hard), h[v]);
+    for (int v = 0; v < Per; ++v) h[v] = apply<true>(terms<true>(x[v], r[v], i[v], k[v], hard), h[v]);
     Lane4<float>::store<Vec>(state_out, b * a.width + ch, Per, h);
     Lane4<T>::template store<Vec>(a.y, b * a.width + ch, Per, h);
 }
@@ -537,14 +569,19 @@ constexpr int kBwdSub = 4;
 constexpr int kBwdTile = kRows * kBwdSub;
 static_assert(kBwdTile == kBlock, "a tile of the backward pass starts at a kept state");
 
-// x, r or i of the backward pass: a tensor of T, or a checkpoint.  load: the token `row` tokens
-// from the wave's own, at 4 c4 channels from the slab's first; load_near: any token.
+// x, r or i of the backward pass: a tensor of T, or a checkpoint.  load: a token `row` tokens
+// and four channels c4 groups of four past the one that the wave shares, which is what Off holds;
+// load_near: any token.
 template <typename T>
 struct Source {
     using Raw = typename Lane4<T>::Raw;
-    __device__ static Raw load(const void* base, const RecurrenceGradArgs& a, int64_t token, int row, int64_t ch0, int c4)
+    struct Off {
+        uint32_t at;
+        __device__ Off(const RecurrenceGradArgs& a, int row, int c4) : at((uint32_t(row) * uint32_t(a.stride) + c4 * 4) * uint32_t(sizeof(T))) {}
+    };
+    __device__ static Raw load(const void* base, const RecurrenceGradArgs& a, int64_t token, int64_t ch0, Off& off)
     {
-        return load_row<T>(base, token * a.stride + ch0, uint32_t(row) * uint32_t(a.stride) + c4 * 4);
+        return load_row<T>(base, token * a.stride + ch0, off.at);
     }
     template <bool Vec>
     __device__ static Raw load_near(const void* base, const RecurrenceGradArgs& a, int64_t token, int64_t ch, int64_t ch0)
@@ -562,12 +599,17 @@ struct Source {
 template <>
 struct Source<q8_t> {
     using Raw = Q8Raw;
-    __device__ static Raw load(const void* base, const RecurrenceGradArgs& a, int64_t token, int row, int64_t ch0, int c4)
+    struct Off {
+        uint32_t code, byte;
+        __device__ Off(const RecurrenceGradArgs& a, int row, int c4)
+            : code(uint32_t(row) * uint32_t(a.width) + c4 * 4), byte(uint32_t(row) * uint32_t((a.width + kGroup - 1) / kGroup) + c4 / 8) {}
+    };
+    __device__ static Raw load(const void* base, const RecurrenceGradArgs& a, int64_t token, int64_t ch0, Off& off)
     {
         const int64_t groups = (a.width + kGroup - 1) / kGroup;
         const int8_t* codes = static_cast<const int8_t*>(base) + token * a.width + ch0;
         const uint8_t* bytes = static_cast<const uint8_t*>(base) + checkpoint_exponents_at(a.batch * a.seq_len, a.width) + token * groups + ch0 / kGroup;
-        return {load_at<uint32_t>(codes, uint32_t(row) * uint32_t(a.width) + c4 * 4), load_at<uint8_t>(bytes, uint32_t(row) * uint32_t(groups) + c4 / 8)};
+        return {load_off<uint32_t>(codes, off.code), load_off<uint8_t>(bytes, off.byte)};
     }
     template <bool Vec>
     __device__ static Raw load_near(const void* base, const RecurrenceGradArgs& a, int64_t token, int64_t ch, int64_t ch0)
@@ -620,25 +662,29 @@ __global__ __launch_bounds__(F::kThreads, (kLean<T, Tg> ? 4 : 2)) void recurrenc
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int row = lane / kAcross, col = lane % kAcross;
     const int64_t ch0 = int64_t(slab) * kCh, ch = ch0 + col * 4;
-    const int n = int(max<int64_t>(0, min<int64_t>(4, a.width - ch)));
-    const Rates k = rates_of(a.theta, a.decay, ch, n);
+    const int cols = int(min<int64_t>(a.width - ch0, kCh)), n = channels_of(col * 4, cols);
+    float theta[4], k[4];
+    load_theta(a.theta + ch0, col * 4, cols, theta);
     const Place at = place_of(ticket, a.tiles > 1, a.batch, sh.ticket);
+#pragma unroll
+    for (int v = 0; v < 4; ++v) pin(theta[v]);   // here before the tile is asked for, or it would be waited for with it
     const int64_t tile = a.tiles - 1 - at.step;
     const int64_t w0 = tile * kBwdTile + wave * kWaveRows * kBwdSub;
     const int64_t token0 = at.b * a.seq_len + w0;
-    const int left = there_are(a.seq_len - w0 - row * kBwdSub, kBwdSub);
+    const int left = there_are<F, kBwdSub>(a.seq_len, w0, row);
     const uint32_t mark = Cuts<Reset, F, kBwdSub>::ask(a.reset, token0, a.seq_len - w0);
 
     typename Source<T>::Raw rx[kBwdSub], rr[kBwdSub], ri[kBwdSub];
     typename Lane4<Tg>::Raw rd[kBwdSub];
     if (Vec && w0 + kWaveRows * kBwdSub <= a.seq_len) {
-        const int c4 = n > 0 ? col : 0;
+        typename Source<T>::Off off(a, row * kBwdSub, n > 0 ? col : 0);
+        uint32_t d_off = (uint32_t(row * kBwdSub) * uint32_t(a.width) + (n > 0 ? col * 4 : 0)) * uint32_t(sizeof(Tg));
 #pragma unroll
         for (int j = 0; j < kBwdSub; ++j) {
-            rr[j] = Source<T>::load(a.r, a, token0 + j, row * kBwdSub, ch0, c4);
-            rx[j] = Source<T>::load(a.x, a, token0 + j, row * kBwdSub, ch0, c4);
-            ri[j] = Source<T>::load(a.i, a, token0 + j, row * kBwdSub, ch0, c4);
-            rd[j] = load_row<Tg>(a.dy, (token0 + j) * a.width + ch0, uint32_t(row * kBwdSub) * uint32_t(a.width) + c4 * 4);
+            rr[j] = Source<T>::load(a.r, a, token0 + j, ch0, off);
+            rx[j] = Source<T>::load(a.x, a, token0 + j, ch0, off);
+            ri[j] = Source<T>::load(a.i, a, token0 + j, ch0, off);
+            rd[j] = load_row<Tg>(a.dy, (token0 + j) * a.width + ch0, d_off);
         }
     } else {
         // tokens past the end and channels past the last are read as copies of existing ones
@@ -652,6 +698,7 @@ __global__ __launch_bounds__(F::kThreads, (kLean<T, Tg> ? 4 : 2)) void recurrenc
         }
     }
     const Cuts<Reset, F, kBwdSub> cuts(mark, row);
+    rates_of(theta, -a.decay, k);
     // the lane's tokens: their factors, and what they do together to the state and, on the way
     // back, to its gradient; tokens past the end do nothing to either
     const bool whole = w0 + kWaveRows * kBwdSub <= a.seq_len;
@@ -671,7 +718,7 @@ __global__ __launch_bounds__(F::kThreads, (kLean<T, Tg> ? 4 : 2)) void recurrenc
             Kept& q = e[j][v];
             q.er = __builtin_amdgcn_exp2f(r[v]);
             q.ei = __builtin_amdgcn_exp2f(i[v]);
-            const float z = k.v[v] * gate_of(q.er);
+            const float z = k[v] * __builtin_amdgcn_rcpf(fmaf(q.er, kLn2, kLn2));   // s / ln 2
             q.a = __builtin_amdgcn_exp2f(z);
             // at least 2^-60, so that 1 / m is finite: where 1 - a^2 is less, its share of every
             // gradient is below fp32's resolution of the others
@@ -750,6 +797,7 @@ __global__ __launch_bounds__(F::kThreads, (kLean<T, Tg> ? 4 : 2)) void recurrenc
 #pragma unroll
         for (int v = 0; v < 4; ++v) e[j][v].hp = h[v], h[v] = after[v];
     }
+    uint32_t g_off = (uint32_t(row * kBwdSub) * uint32_t(a.grad_stride) + col * 4) * uint32_t(sizeof(Tg));
 #pragma unroll
     for (int j = kBwdSub - 1; j >= 0; --j) {
         if (j >= left) continue;
@@ -772,7 +820,7 @@ __global__ __launch_bounds__(F::kThreads, (kLean<T, Tg> ? 4 : 2)) void recurrenc
             gi[v] = gx[v] * x[v] * rest_of(q.ei, si);
             const float dl = ag * fmaf(-q.a * __builtin_amdgcn_rcpf(m[v]), si * x[v], q.hp);
             dls[v] = dl * s;
-            gr[v] = dls[v] * (k.v[v] * kLn2 * rest_of(q.er, s));
+            gr[v] = dls[v] * (k[v] * rest_of(q.er, s));
             c[v] = ag;
         }
         if (cuts.any(j) && cuts.lane(j)) {
@@ -781,10 +829,10 @@ __global__ __launch_bounds__(F::kThreads, (kLean<T, Tg> ? 4 : 2)) void recurrenc
         }
 #pragma unroll
         for (int v = 0; v < 4; ++v) dth[v] += dls[v];
-        const int64_t at_row = (token0 + j) * a.grad_stride + ch0;
-        store_row<Tg, Vec>(a.dx, at_row, row * kBwdSub, a.grad_stride, col, n, gx);
-        store_row<Tg, Vec>(a.dr, at_row, row * kBwdSub, a.grad_stride, col, n, gr);
-        store_row<Tg, Vec>(a.di, at_row, row * kBwdSub, a.grad_stride, col, n, gi);
+        const int64_t at_row = (token0 + j) * a.grad_stride + ch0, at = row * kBwdSub * a.grad_stride + col * 4;
+        store_row<Tg, Vec>(a.dx, at_row, g_off, at, n, gx);
+        store_row<Tg, Vec>(a.dr, at_row, g_off, at, n, gr);
+        store_row<Tg, Vec>(a.di, at_row, g_off, at, n, gi);
     }
     if (a.dh0 != nullptr && tile == 0 && wave == 0 && row == 0) Lane4<float>::store<false>(a.dh0, at.b * a.width + ch, n, c);
     // dtheta: the tile's sum of dl s, one row of the partial sums; the rows' sums take the place
@@ -851,35 +899,36 @@ using Narrow = Form<8>;
 
 template <class F>
 int64_t workgroups(int64_t batch, int64_t tiles, int64_t width) { return batch * tiles * ((width + F::kCh - 1) / F::kCh); }
+template <class F, bool Kept>
+int64_t tiles_of(int64_t seq_len) { return (seq_len + kFwdTile<F, Kept> - 1) / kFwdTile<F, Kept>; }
 bool narrow(int64_t batch, int64_t tiles, int64_t width) { return workgroups<Wide>(batch, tiles, width) < device_compute_units(); }
 
-template <typename T, bool Vec, bool Reset, class F>
-hipError_t launch_forward(const RecurrenceArgs& a, hipStream_t stream)
+template <typename T, bool Vec, bool Reset, bool Kept, class F>
+hipError_t launch_forward(RecurrenceArgs a, hipStream_t stream)
 {
-    const dim3 grid{unsigned(workgroups<F>(a.batch, a.tiles, a.width))}, block{F::kThreads};
-    if (a.kept_x != nullptr)
-        hipLaunchKernelGGL((recurrence_kernel<T, Vec, Reset, true, F>), grid, block, 0, stream, a);
-    else
-        hipLaunchKernelGGL((recurrence_kernel<T, Vec, Reset, false, F>), grid, block, 0, stream, a);
+    a.tiles = tiles_of<F, Kept>(a.seq_len);
+    if (hipError_t e = clear_walk(a.words, a.batch, a.tiles, a.width, stream); e != hipSuccess) return e;
+    hipLaunchKernelGGL((recurrence_kernel<T, Vec, Reset, Kept, F>), dim3(unsigned(workgroups<F>(a.batch, a.tiles, a.width))),
+                       dim3(F::kThreads), 0, stream, a);
     return hipGetLastError();
 }
 
-template <typename T, bool Vec>
+template <typename T, bool Vec, bool Kept>
 hipError_t launch_forward_form(const RecurrenceArgs& a, hipStream_t stream)
 {
-    if (narrow(a.batch, a.tiles, a.width)) return launch_forward<T, Vec, true, Narrow>(a, stream);
-    return a.reset != nullptr ? launch_forward<T, Vec, true, Wide>(a, stream) : launch_forward<T, Vec, false, Wide>(a, stream);
+    if (narrow(a.batch, tiles_of<Wide, Kept>(a.seq_len), a.width)) return launch_forward<T, Vec, true, Kept, Narrow>(a, stream);
+    return a.reset != nullptr ? launch_forward<T, Vec, true, Kept, Wide>(a, stream) : launch_forward<T, Vec, false, Kept, Wide>(a, stream);
 }
 
 template <typename T>
 hipError_t launch_forward_type(const RecurrenceArgs& a, hipStream_t stream)
 {
-    if (workgroups<Narrow>(a.batch, a.tiles, a.width) > INT32_MAX) return hipErrorInvalidValue;
-    if (hipError_t e = clear_walk(a.words, a.batch, a.tiles, a.width, stream); e != hipSuccess) return e;
+    if (workgroups<Narrow>(a.batch, tiles_of<Narrow, false>(a.seq_len), a.width) > INT32_MAX) return hipErrorInvalidValue;
     constexpr int bytes = 4 * int(sizeof(T));
     const bool vec = a.width % 4 == 0 && a.stride % 4 == 0 && a.stride <= kNearStride && aligned(a.x, bytes) &&
                      aligned(a.r, bytes) && aligned(a.i, bytes) && aligned(a.y, bytes);
-    return vec ? launch_forward_form<T, true>(a, stream) : launch_forward_form<T, false>(a, stream);
+    if (a.kept_x != nullptr) return vec ? launch_forward_form<T, true, true>(a, stream) : launch_forward_form<T, false, true>(a, stream);
+    return vec ? launch_forward_form<T, true, false>(a, stream) : launch_forward_form<T, false, false>(a, stream);
 }
 
 template <typename T>
@@ -926,7 +975,8 @@ hipError_t launch_backward_types(const RecurrenceGradArgs& a, hipStream_t stream
 
 }  // namespace
 
-int64_t recurrence_tiles(int64_t seq_len) { return (seq_len + kFwdTile - 1) / kFwdTile; }
+// the most that a forward pass of either form has
+int64_t recurrence_tiles(int64_t seq_len) { return tiles_of<Narrow, true>(seq_len); }
 
 int64_t recurrence_walk_bytes(int64_t batch, int64_t tiles, int64_t width)
 {
