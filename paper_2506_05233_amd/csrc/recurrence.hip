@@ -164,7 +164,7 @@ __global__ __launch_bounds__(256) void recurrence_fill_kernel(ulonglong2* words,
 }
 
 // What the lane rows of a workgroup do to the state, in shared memory: a plane of their A and one
-// of their B, by time.  The state entering a row takes the place of its B.
+// of their B, by time.
 template <int kCh>
 using Plane = float[kRows][kCh];
 
@@ -231,8 +231,11 @@ __device__ __forceinline__ Place place_of(int ticket, bool many, int64_t batch, 
     return {int64_t(id - step * uint32_t(batch)), int(step)};
 }
 
-// A tile's part in the walk, done by the first wave of its workgroup with a channel in each
-// lane.  `step` is the tile's place in the walk, `first` the state ahead of the whole walk.
+// A tile's part in the walk, by waves with a channel in each lane.  `step` is the tile's place in
+// the walk, `first` the state ahead of the whole walk.  The forward's first wave does all of it;
+// in the backward pass, whose workgroups have longer to wait, a second one publishes meanwhile
+// (gradients from checkpoints of 8 x 2048 tokens of 2048 102 us and 98; the forward, which would
+// need a plane more for it, 52 and 55).
 template <bool Reset, bool Back, class F>
 struct Walk {
     uint64_t* spans;          // of the sequence's tiles, this lane's channel
@@ -243,8 +246,6 @@ struct Walk {
     float start;              // entering the walk
     uint64_t seen[kLook];     // what the first words held: entry 0 the state entering the group, e the group's tile e - 1
 
-    // Taken before the barrier that makes the rows visible, so that the look's way to memory is
-    // part of the wait for the other waves.
     __device__ void find(uint64_t* words, int64_t batch, int64_t b, int step_, int steps_, int64_t width_, int slab)
     {
         step = step_, steps = steps_, width = width_;
@@ -255,6 +256,8 @@ struct Walk {
         spans = words + ticket_words(slabs) + b * steps * width + ch;
         leaves = words + ticket_words(slabs) + batch * steps * width + b * groups * width + ch;
     }
+    // Taken before the barrier that makes the rows visible, so that the look's way to memory is
+    // part of the wait for the other waves.
     __device__ void look_ahead(const float* first, int64_t b, int slab)
     {
         const int group = step / kJoin, at = step % kJoin;
@@ -265,8 +268,7 @@ struct Walk {
     }
     __device__ const uint64_t* entry(int group, int e) const { return spans + int64_t(group * kJoin + e - 1) * width; }
 
-    // The rows' entering states, in the place of their B: first this tile's span is published,
-    // then what the tiles before it published is taken in.
+    // Publishes this tile's span.  It waits for nothing, so nobody waits for it in a circle.
     __device__ void tell(const Plane<F::kCh>& A, const Plane<F::kCh>& B)
     {
         const int lane = threadIdx.x % kWave;
@@ -276,6 +278,8 @@ struct Walk {
         if (mine) publish(spans + int64_t(step) * width, s);
         __builtin_amdgcn_s_setprio(0);
     }
+    // The rows' entering states into the plane `in` (which may be B, once told): takes in what the
+    // tiles before this one published, and passes through the rows.
     __device__ void pass(const Plane<F::kCh>& A, const Plane<F::kCh>& B, Plane<F::kCh>& in)
     {
         const int lane = threadIdx.x % kWave, group = step / kJoin, at = step % kJoin;
