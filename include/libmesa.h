@@ -403,7 +403,12 @@ int mesa_backward(const void* k, const void* v, const float* gamma, const float*
  *   element i * stride (stride >= width), into the buffer.
  * mesa_checkpoint_unpack: the buffer into x, of the same layout.
  * x aligned to its elements; a fully dense x of whole groups on 16-byte aligned memory runs
- * fastest.  x and the buffer must not overlap (MESA_ERR_ARG).  One kernel launch. */
+ * fastest.  x and the buffer must not overlap (MESA_ERR_ARG).  One kernel launch.
+ *
+ * Here and in the calls below a size whose launch would have 2^32 threads or more is refused with
+ * MESA_ERR_SHAPE and nothing runs: a thread takes a row's 32 channels of a checkpoint, 512 threads
+ * 64 channels and 128 tokens (forward: 128 or 256) of a sequence of the recurrence, a thread four
+ * channels or one of its step, 256 threads 128 tokens or more of a head of the layer's ends. */
 #define MESA_CHECKPOINT_GROUP 32
 size_t mesa_checkpoint_bytes(int64_t rows, int64_t width);
 int mesa_checkpoint_pack(const void* x, int64_t rows, int64_t width, int64_t stride, int dtype, void* checkpoint,

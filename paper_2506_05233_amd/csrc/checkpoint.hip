@@ -169,7 +169,7 @@ hipError_t launch(const CheckpointArgs& a, bool pack, hipStream_t stream)
     const bool flat = a.width % kGroup == 0 && a.stride == a.width && uintptr_t(a.x) % 16 == 0;
     const int64_t pieces = a.rows * ((a.width + kGroup - 1) / kGroup) * (kGroup / kPer);
     const int64_t blocks = (pieces + kThreads * kIter - 1) / (kThreads * kIter);
-    if (blocks > INT32_MAX) return hipErrorInvalidValue;
+    if (!grid_fits(blocks, kThreads)) return hipErrorInvalidConfiguration;
     const dim3 grid{unsigned(blocks)}, block{kThreads};
     if (pack && flat)
         hipLaunchKernelGGL((checkpoint_pack_kernel<T, true>), grid, block, 0, stream, a, pieces);

@@ -259,13 +259,14 @@ __global__ __launch_bounds__(kThreads) void frontend_grad_kernel(FrontGradArgs a
 }
 
 // out[c] = sum of rows of partial [rows, cols], for up to three arrays in one launch.
+constexpr int kSumThreads = 1024;
 struct Sums {
     const float* partial[3];
     float* out[3];
     int64_t rows[3], cols[3];
     int64_t blocks[3];
 };
-__global__ __launch_bounds__(1024) void partial_sum_kernel(Sums s)
+__global__ __launch_bounds__(kSumThreads) void partial_sum_kernel(Sums s)
 {
     __shared__ float part[16][kWave];
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
@@ -283,12 +284,12 @@ __global__ __launch_bounds__(1024) void partial_sum_kernel(Sums s)
     s.out[q][c] = v;
 }
 
+int64_t blocks_of(const Sums& s) { return s.blocks[0] + s.blocks[1] + s.blocks[2]; }
 hipError_t launch_sums(const Sums& s, hipStream_t stream)
 {
-    const int64_t blocks = s.blocks[0] + s.blocks[1] + s.blocks[2];
+    const int64_t blocks = blocks_of(s);
     if (blocks == 0) return hipSuccess;
-    if (blocks > INT32_MAX) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(partial_sum_kernel, dim3(unsigned(blocks)), dim3(1024), 0, stream, s);
+    hipLaunchKernelGGL(partial_sum_kernel, dim3(unsigned(blocks)), dim3(kSumThreads), 0, stream, s);
     return hipGetLastError();
 }
 
@@ -298,15 +299,15 @@ hipError_t launch_front(const FrontGradArgs& a, hipStream_t stream)
     const FrontPlan p = front_plan(a.batch, a.heads, a.seq_len, DK, DV);
     const int64_t bh = a.batch * a.heads;
     const int64_t blocks = bh * (2 * p.blocks_k + p.blocks_v) + p.gate_blocks + (a.heads * DK + kThreads - 1) / kThreads;
-    if (blocks > INT32_MAX) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((frontend_grad_kernel<T, Tg, DK, DV>), dim3(unsigned(blocks)), dim3(kThreads), 0, stream, a, p);
-    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     const int64_t ck = a.heads * DK * 4, cv = a.conv_v != nullptr ? a.heads * DV * 4 : 0;
     const Sums s{{a.partial, a.partial + p.part_k, a.partial + 2 * p.part_k},
                  {a.dconv_q, a.dconv_k, a.dconv_v},
                  {a.batch * p.blocks_k, a.batch * p.blocks_k, a.batch * p.blocks_v},
                  {ck, ck, cv},
                  {(ck + kWave - 1) / kWave, (ck + kWave - 1) / kWave, (cv + kWave - 1) / kWave}};
+    if (!grid_fits(blocks, kThreads) || !grid_fits(blocks_of(s), kSumThreads)) return hipErrorInvalidConfiguration;
+    hipLaunchKernelGGL((frontend_grad_kernel<T, Tg, DK, DV>), dim3(unsigned(blocks)), dim3(kThreads), 0, stream, a, p);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     return launch_sums(s, stream);
 }
 
@@ -379,14 +380,15 @@ hipError_t launch_norm(const NormGradArgs& a, hipStream_t stream)
 {
     const int run = run_of(a.batch * a.heads, a.seq_len, D);
     const int64_t per = blocks_of(a.seq_len, D, run), blocks = a.batch * a.heads * per;
-    if (blocks > INT32_MAX) return hipErrorInvalidValue;
+    const int64_t cols = a.heads * D;
+    const Sums s{{a.partial, nullptr, nullptr}, {a.dweight, nullptr, nullptr}, {a.batch * per, 0, 0}, {cols, 0, 0},
+                 {(cols + kWave - 1) / kWave, 0, 0}};
+    if (!grid_fits(blocks, kThreads) || !grid_fits(blocks_of(s), kSumThreads)) return hipErrorInvalidConfiguration;
     if (blocks > 0) {
         hipLaunchKernelGGL((output_norm_grad_kernel<T, Tg, D>), dim3(unsigned(blocks)), dim3(kThreads), 0, stream, a, run, per);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
-    const int64_t cols = a.heads * D;
-    return launch_sums({{a.partial, nullptr, nullptr}, {a.dweight, nullptr, nullptr}, {a.batch * per, 0, 0}, {cols, 0, 0},
-                        {(cols + kWave - 1) / kWave, 0, 0}}, stream);
+    return launch_sums(s, stream);
 }
 
 template <typename T, typename Tg>

@@ -89,7 +89,11 @@ bool clash(std::initializer_list<Rows> ins, std::initializer_list<Rows> outs)
     return false;
 }
 
-int status_of(hipError_t e, void* stream) { return finish(e == hipSuccess ? MESA_OK : MESA_ERR_HIP, stream); }
+// A launch's own refusal of a grid past 32 bits of threads comes before anything is enqueued.
+int status_of(hipError_t e, void* stream)
+{
+    return finish(e == hipSuccess ? MESA_OK : e == hipErrorInvalidConfiguration ? MESA_ERR_SHAPE : MESA_ERR_HIP, stream);
+}
 
 int checkpoint(const void* x, int64_t rows, int64_t width, int64_t stride, int dtype, const void* buffer, bool pack,
                void* stream)
@@ -107,8 +111,8 @@ int checkpoint(const void* x, int64_t rows, int64_t width, int64_t stride, int d
     return status_of(mesa::launch_checkpoint(a, pack, static_cast<hipStream_t>(stream)), stream);
 }
 
-// Sizes shared by the recurrence's calls; a grid of one workgroup a 32-channel slab of 128 tokens
-// must be countable in 31 bits.
+// Sizes shared by the recurrence's calls; tickets and tiles are counted in 32 bits, one of a slab
+// of 32 channels and 128 tokens.
 int recurrence_sizes(int64_t batch, int64_t seq_len, int64_t width, int64_t stride, float decay)
 {
     if (batch < 0 || seq_len < 0 || width < 0 || seq_len > kMostElements || width > kMostElements) return MESA_ERR_SHAPE;

@@ -304,6 +304,11 @@ struct NormGradArgs {
 int64_t norm_grad_partial_floats(int64_t batch, int64_t heads, int64_t seq_len, int d_v);
 hipError_t launch_output_norm_backward(const NormGradArgs& a, hipStream_t stream);
 
+// Whether `blocks` workgroups of `threads` can be launched at once.  The runtime counts a launch's
+// threads in 32 bits and past that starts the remainder alone, without an error (of 8388616
+// workgroups of 512 threads eight ran), so such a launch has to be refused before it is made.
+inline bool grid_fits(int64_t blocks, int threads) { return blocks <= int64_t(UINT32_MAX) / threads; }
+
 // Compute units of the current device (queried once per device), for the persistent
 // kernels that launch one workgroup per unit.
 int device_compute_units();

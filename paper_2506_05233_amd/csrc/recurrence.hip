@@ -871,8 +871,7 @@ __global__ __launch_bounds__(1024) void recurrence_dtheta_kernel(const float* pa
 // the final state of an empty sequence: the entering one
 __global__ __launch_bounds__(256) void recurrence_copy_kernel(const float* from, float* to, int64_t n)
 {
-    const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x;
-    if (i < n) to[i] = from != nullptr ? from[i] : 0.0f;
+    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < n; i += int64_t(gridDim.x) * 256) to[i] = from != nullptr ? from[i] : 0.0f;
 }
 
 bool aligned(const void* p, int bytes) { return uintptr_t(p) % uintptr_t(bytes) == 0; }
@@ -880,7 +879,7 @@ bool aligned(const void* p, int bytes) { return uintptr_t(p) % uintptr_t(bytes) 
 hipError_t copy_state(const float* from, float* to, int64_t n, hipStream_t stream)
 {
     if (to == nullptr) return hipSuccess;
-    hipLaunchKernelGGL(recurrence_copy_kernel, dim3(unsigned((n + 255) / 256)), dim3(256), 0, stream, from, to, n);
+    hipLaunchKernelGGL(recurrence_copy_kernel, dim3(unsigned(std::min<int64_t>((n + 255) / 256, 1 << 16))), dim3(256), 0, stream, from, to, n);
     return hipGetLastError();
 }
 
@@ -911,6 +910,7 @@ template <typename T, bool Vec, bool Reset, bool Kept, class F>
 hipError_t launch_forward(RecurrenceArgs a, hipStream_t stream)
 {
     a.tiles = tiles_of<F, Kept>(a.seq_len);
+    if (!grid_fits(workgroups<F>(a.batch, a.tiles, a.width), F::kThreads)) return hipErrorInvalidConfiguration;
     if (hipError_t e = clear_walk(a.words, a.batch, a.tiles, a.width, stream); e != hipSuccess) return e;
     hipLaunchKernelGGL((recurrence_kernel<T, Vec, Reset, Kept, F>), dim3(unsigned(workgroups<F>(a.batch, a.tiles, a.width))),
                        dim3(F::kThreads), 0, stream, a);
@@ -927,7 +927,6 @@ hipError_t launch_forward_form(const RecurrenceArgs& a, hipStream_t stream)
 template <typename T>
 hipError_t launch_forward_type(const RecurrenceArgs& a, hipStream_t stream)
 {
-    if (workgroups<Narrow>(a.batch, tiles_of<Narrow, false>(a.seq_len), a.width) > INT32_MAX) return hipErrorInvalidValue;
     constexpr int bytes = 4 * int(sizeof(T));
     const bool vec = a.width % 4 == 0 && a.stride % 4 == 0 && a.stride <= kNearStride && aligned(a.x, bytes) &&
                      aligned(a.r, bytes) && aligned(a.i, bytes) && aligned(a.y, bytes);
@@ -942,7 +941,7 @@ hipError_t launch_step_type(const RecurrenceArgs& a, float* state_out, hipStream
     const bool vec = a.width % 4 == 0 && a.stride % 4 == 0 && aligned(a.x, bytes) && aligned(a.r, bytes) &&
                      aligned(a.i, bytes) && aligned(a.y, bytes) && aligned(a.h0, 16) && aligned(state_out, 16);
     const int64_t threads = a.batch * (vec ? a.width / 4 : a.width), blocks = (threads + 255) / 256;
-    if (blocks > INT32_MAX) return hipErrorInvalidValue;
+    if (!grid_fits(blocks, 256)) return hipErrorInvalidConfiguration;
     if (vec)
         hipLaunchKernelGGL((recurrence_step_kernel<T, 4>), dim3(unsigned(blocks)), dim3(256), 0, stream, a, state_out);
     else
@@ -953,6 +952,8 @@ hipError_t launch_step_type(const RecurrenceArgs& a, float* state_out, hipStream
 template <typename T, typename Tg, bool Vec, bool Reset, class F>
 hipError_t launch_backward(const RecurrenceGradArgs& a, hipStream_t stream)
 {
+    if (!grid_fits(workgroups<F>(a.batch, a.tiles, a.width), F::kThreads)) return hipErrorInvalidConfiguration;
+    if (hipError_t e = clear_walk(a.words, a.batch, a.tiles, a.width, stream); e != hipSuccess) return e;
     hipLaunchKernelGGL((recurrence_grad_kernel<T, Tg, Vec, Reset, F>), dim3(unsigned(workgroups<F>(a.batch, a.tiles, a.width))),
                        dim3(F::kThreads), 0, stream, a);
     return hipGetLastError();
@@ -968,8 +969,6 @@ hipError_t launch_backward_form(const RecurrenceGradArgs& a, hipStream_t stream)
 template <typename T, typename Tg>
 hipError_t launch_backward_types(const RecurrenceGradArgs& a, hipStream_t stream)
 {
-    if (workgroups<Narrow>(a.batch, a.tiles, a.width) > INT32_MAX) return hipErrorInvalidValue;
-    if (hipError_t e = clear_walk(a.words, a.batch, a.tiles, a.width, stream); e != hipSuccess) return e;
     constexpr int in = 4 * int(sizeof(T)), out = 4 * int(sizeof(Tg));
     const bool vec = a.width % 4 == 0 && a.stride % 4 == 0 && a.grad_stride % 4 == 0 && a.stride <= kNearStride &&
                      a.grad_stride <= kNearStride && aligned(a.x, in) && aligned(a.r, in) && aligned(a.i, in) &&
@@ -1005,6 +1004,8 @@ hipError_t launch_recurrence_step(const RecurrenceArgs& a, float* state_out, hip
 hipError_t launch_recurrence_backward(const RecurrenceGradArgs& a, hipStream_t stream)
 {
     if (a.width == 0) return hipSuccess;
+    const int64_t sums = (a.width + kWave - 1) / kWave;
+    if (!grid_fits(sums, 1024)) return hipErrorInvalidConfiguration;
     if (a.batch * a.seq_len > 0) {
         hipError_t e;
         if (a.dtype == kQ8)
@@ -1019,8 +1020,8 @@ hipError_t launch_recurrence_backward(const RecurrenceGradArgs& a, hipStream_t s
         if (e != hipSuccess) return e;
     }
     const int64_t rows = a.seq_len > 0 ? a.batch * a.tiles : 0;
-    hipLaunchKernelGGL(recurrence_dtheta_kernel, dim3(unsigned((a.width + kWave - 1) / kWave)), dim3(1024), 0, stream,
-                       a.partial, rows, a.theta, a.decay, a.width, a.dtheta);
+    hipLaunchKernelGGL(recurrence_dtheta_kernel, dim3(unsigned(sums)), dim3(1024), 0, stream, a.partial, rows, a.theta,
+                       a.decay, a.width, a.dtheta);
     return hipGetLastError();
 }
 
