@@ -104,7 +104,8 @@ extern "C" {
 /* Status codes. */
 #define MESA_OK 0
 #define MESA_ERR_NULL 1          /* a required pointer is NULL                         */
-#define MESA_ERR_SHAPE 2         /* a size is negative or the sizes are inconsistent  */
+#define MESA_ERR_SHAPE 2         /* a size is negative or the sizes are inconsistent,
+                                  * or a launch would need 2^32 threads or more        */
 #define MESA_ERR_UNSUPPORTED 3   /* d_k, d_v, chunk, dtype or precision not supported */
 #define MESA_ERR_ARG 4           /* n_cg or eps out of range, misaligned, overlapping  */
 #define MESA_ERR_WORKSPACE 5     /* workspace too small                                */

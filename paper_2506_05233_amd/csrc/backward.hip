@@ -27,6 +27,7 @@
 // product over tokens or features is a dense contraction of fp32 operands and runs
 // on the matrix cores in fp32 (v_mfma_f32_16x16x4f32: exact fp32 products, fp32
 // accumulation), 16 x 16 output tiles per wave.
+#include <algorithm>
 #include <type_traits>
 
 #include "mesa_device.hpp"
@@ -1486,6 +1487,9 @@ hipError_t launch_bwd_dims(const BwdArgs& a, hipStream_t stream, int stage)
     const int64_t bh = a.s.batch * a.s.heads;
     const unsigned chunks = unsigned(bh * a.s.n_chunks);
     constexpr bool kSplit = std::is_same<Tin, bf16_t>::value;  // the bf16 route's split products
+    // one workgroup a chunk, or a few for each (sequence, head); the adjoint's totals are looked at below
+    if (!grid_fits(bh * a.s.n_chunks, std::max(kThreads, kGradThreads)) || !grid_fits(bh * ((DK + DV) / kAdjRows), kThreads))
+        return hipErrorInvalidConfiguration;
     switch (stage) {
         case 0:
             hipLaunchKernelGGL((bwd_rhs_kernel<Tin, DK, DV>), dim3(chunks), dim3(kThreads), 0, stream, a);
@@ -1513,6 +1517,7 @@ hipError_t launch_bwd_dims(const BwdArgs& a, hipStream_t stream, int stage)
             const int64_t rounds = (bh * NTILE * (nc - 1) + resident - 1) / resident;
             if (nc > 1 && bytes + 11000000 < (walk - rounds) * 12000000) {
                 AdjSeg p1{1, nc, 1, nc - 1, true, nullptr, a.u, true};
+                if (!grid_fits(bh * NTILE * (nc - 1), kThreads)) return hipErrorInvalidConfiguration;
                 hipLaunchKernelGGL((bwd_adjoint_kernel<DK, DV, kSplit>), dim3(unsigned(bh * NTILE * (nc - 1))), dim3(kThreads), 0,
                                    stream, a, p1);
                 const hipError_t e = hipGetLastError();

@@ -538,6 +538,7 @@ template <typename Tin, int DK>
 hipError_t launch_mma(const CgArgs& a, hipStream_t stream)
 {
     const unsigned blocks = unsigned(a.s.batch * a.s.heads * a.s.n_chunks);
+    if (!grid_fits(blocks, kThreads)) return hipErrorInvalidConfiguration;
     if (a.s.d_v == 64)
         hipLaunchKernelGGL((chunk_cg_f32_mma_kernel<Tin, DK, 64>), dim3(blocks), dim3(kThreads), 0, stream, a);
     else
@@ -555,6 +556,7 @@ hipError_t launch_dk(const CgArgs& a, hipStream_t stream)
         else return launch_mma<Tin, DK>(a, stream);
     }
     const unsigned blocks = unsigned(a.s.batch * a.s.heads * a.s.n_chunks);
+    if (!grid_fits(blocks, kThreads)) return hipErrorInvalidConfiguration;
     switch (a.s.chunk) {
         case 16: hipLaunchKernelGGL((chunk_cg_f32_kernel<Tin, DK, 16>), dim3(blocks), dim3(kThreads), 0, stream, a); break;
         case 32: hipLaunchKernelGGL((chunk_cg_f32_kernel<Tin, DK, 32>), dim3(blocks), dim3(kThreads), 0, stream, a); break;

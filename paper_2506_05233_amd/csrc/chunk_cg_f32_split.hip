@@ -608,6 +608,7 @@ template <typename Tin>
 hipError_t launch_tin(const CgArgs& a, hipStream_t stream)
 {
     const unsigned blocks = unsigned(a.s.batch * a.s.heads * a.s.n_chunks);
+    if (!grid_fits(blocks, kThreads)) return hipErrorInvalidConfiguration;
     if (a.s.d_v == 64)
         hipLaunchKernelGGL((chunk_cg_f32_split_kernel<Tin, 64>), dim3(blocks), dim3(kThreads), 0, stream, a);
     else

@@ -1014,15 +1014,18 @@ hipError_t launch_scan(const StateArgs& a, int64_t part2, hipStream_t stream)
 {
     const int64_t bh = a.s.batch * a.s.heads;
     const int per = a.s.d_k * (a.s.d_k + a.s.d_v) / (MODE == kScanPlain ? 4 : 8);
+    if (!grid_fits(bh * (per / kThreads), kThreads)) return hipErrorInvalidConfiguration;
     hipLaunchKernelGGL(chunk_scan_kernel<MODE>, dim3(unsigned(bh * (per / kThreads))), dim3(kThreads), 0, stream, a, part2);
     return hipGetLastError();
 }
 
 template <int DK, int DV, bool STORE, bool SPLIT, bool PLAIN = false, bool X3 = false>
-void launch_wide_kernel(const StateArgs& a, const SegPlan& sg, int64_t bh, hipStream_t stream)
+hipError_t launch_wide_kernel(const StateArgs& a, const SegPlan& sg, int64_t bh, hipStream_t stream)
 {
-    const unsigned blocks = unsigned(bh * 2 * sg.count);
-    hipLaunchKernelGGL((chunk_state_wide_kernel<DK, DV, STORE, SPLIT, PLAIN, X3>), dim3(blocks), dim3(kWideThreads), 0, stream, a, sg);
+    const int64_t blocks = bh * 2 * sg.count;
+    if (!grid_fits(blocks, kWideThreads)) return hipErrorInvalidConfiguration;
+    hipLaunchKernelGGL((chunk_state_wide_kernel<DK, DV, STORE, SPLIT, PLAIN, X3>), dim3(unsigned(blocks)), dim3(kWideThreads), 0, stream, a, sg);
+    return hipGetLastError();
 }
 
 template <int DK, int DV>
@@ -1052,8 +1055,7 @@ hipError_t launch_wide(const StateArgs& a, hipStream_t stream)
         const int64_t part2 = a.x3 ? g_plane : mode == kScanFrag ? reinterpret_cast<char*>(a.seg_ws) - static_cast<char*>(a.Hs) : 0;
         if (mode != kScanFrag || (a.seg_ws && a.seg_bytes >= size_t(bh * nc * int64_t(DK) * (DK + DV) * 2))) {
             const SegPlan p1{1, nc, nc - 1, true, 0, nullptr, nullptr, mode, part2};
-            launch_wide_kernel<DK, DV, false, true>(a, p1, bh, stream);
-            const hipError_t e = hipGetLastError();
+            const hipError_t e = launch_wide_kernel<DK, DV, false, true>(a, p1, bh, stream);
             if (e != hipSuccess) return e;
             return mode == kScanX3 ? launch_scan<kScanX3>(a, part2, stream)
                  : mode == kScanBoth ? launch_scan<kScanBoth>(a, part2, stream) : launch_scan<kScanFrag>(a, part2, stream);
@@ -1061,10 +1063,10 @@ hipError_t launch_wide(const StateArgs& a, hipStream_t stream)
     }
     if (S > 1 && final_only) {
         sg.totals = true;
-        launch_wide_kernel<DK, DV, false, true>(a, sg, bh, stream);
-        hipError_t e = hipGetLastError();
+        const hipError_t e = launch_wide_kernel<DK, DV, false, true>(a, sg, bh, stream);
         if (e != hipSuccess) return e;
         constexpr int kTiles = 2 * (DK + DV) / 16 / (kWideThreads / kWave / (DK / 32));  // row x column tiles of a wave, both parts
+        if (!grid_fits(bh * kTiles, kWideThreads)) return hipErrorInvalidConfiguration;
         hipLaunchKernelGGL((segment_combine_kernel<DK, DV>), dim3(unsigned(bh * kTiles)), dim3(kWideThreads), 0, stream, a, sg);
         return hipGetLastError();
     }
@@ -1077,24 +1079,17 @@ hipError_t launch_wide(const StateArgs& a, hipStream_t stream)
         SegPlan p1 = sg;
         p1.count = S - 1;
         p1.totals = true;
-        if (a.store_chunks && single && !fin)
-            launch_wide_kernel<DK, DV, false, false>(a, p1, bh, stream);
-        else
-            launch_wide_kernel<DK, DV, false, true>(a, p1, bh, stream);
-        const hipError_t e = hipGetLastError();
+        const hipError_t e = a.store_chunks && single && !fin ? launch_wide_kernel<DK, DV, false, false>(a, p1, bh, stream)
+                                                              : launch_wide_kernel<DK, DV, false, true>(a, p1, bh, stream);
         if (e != hipSuccess) return e;
     }
     if (a.store_chunks && a.x3)  // fp32 H_c fragments, G_c high and low planes, fp32-accurate
-        launch_wide_kernel<DK, DV, true, true, false, true>(a, sg, bh, stream);
-    else if (a.store_chunks && a.frag && a.Hs32)  // fragments and fp32 plain states, fp32-accurate
-        launch_wide_kernel<DK, DV, true, true, true>(a, sg, bh, stream);
-    else if (a.store_chunks && a.frag && !fin)
-        launch_wide_kernel<DK, DV, true, false>(a, sg, bh, stream);
-    else if (a.store_chunks && a.frag)
-        launch_wide_kernel<DK, DV, true, true>(a, sg, bh, stream);
-    else
-        launch_wide_kernel<DK, DV, false, true>(a, sg, bh, stream);
-    return hipGetLastError();
+        return launch_wide_kernel<DK, DV, true, true, false, true>(a, sg, bh, stream);
+    if (a.store_chunks && a.frag && a.Hs32)  // fragments and fp32 plain states, fp32-accurate
+        return launch_wide_kernel<DK, DV, true, true, true>(a, sg, bh, stream);
+    if (a.store_chunks && a.frag && !fin) return launch_wide_kernel<DK, DV, true, false>(a, sg, bh, stream);
+    if (a.store_chunks && a.frag) return launch_wide_kernel<DK, DV, true, true>(a, sg, bh, stream);
+    return launch_wide_kernel<DK, DV, false, true>(a, sg, bh, stream);
 }
 
 __global__ __launch_bounds__(kThreads) void fill_zero_kernel(float* dst, int64_t n)
@@ -1128,25 +1123,29 @@ hipError_t launch_chunk_state(const StateArgs& a, hipStream_t stream)
         return a.s.d_v == 64 ? launch_wide<128, 64>(a, stream) : launch_wide<128, 128>(a, stream);
     }
     if (!a.s.bf16 && a.s.chunk == 64) {
-        const unsigned blocks = unsigned(bh * ((a.s.d_k + a.s.d_v) / 16) * (a.s.d_k / 64));
+        const int64_t blocks = bh * ((a.s.d_k + a.s.d_v) / 16) * (a.s.d_k / 64);
         const int nc = a.s.n_chunks;
         if (a.store_chunks && !a.final_H && !a.final_G && f32_takes_scan(bh, nc, a.s.d_k, a.s.d_v)) {
+            if (!grid_fits(blocks * (nc - 1), kThreads)) return hipErrorInvalidConfiguration;
             auto one = a.s.d_k == 64 ? chunk_state_f32_kernel<64, 2> : chunk_state_f32_kernel<128, 2>;
-            hipLaunchKernelGGL(one, dim3(blocks * unsigned(nc - 1)), dim3(kThreads), 0, stream, a);
+            hipLaunchKernelGGL(one, dim3(unsigned(blocks * (nc - 1))), dim3(kThreads), 0, stream, a);
             const hipError_t e = hipGetLastError();
             return e != hipSuccess ? e : launch_scan<kScanPlain>(a, 0, stream);
         }
         auto kern = a.s.d_k == 64 ? (a.store_chunks ? chunk_state_f32_kernel<64, 1> : chunk_state_f32_kernel<64, 0>)
                                   : (a.store_chunks ? chunk_state_f32_kernel<128, 1> : chunk_state_f32_kernel<128, 0>);
-        hipLaunchKernelGGL(kern, dim3(blocks), dim3(kThreads), 0, stream, a);
+        if (!grid_fits(blocks, kThreads)) return hipErrorInvalidConfiguration;
+        hipLaunchKernelGGL(kern, dim3(unsigned(blocks)), dim3(kThreads), 0, stream, a);
         return hipGetLastError();
     }
     if (a.s.bf16 && a.s.chunk == 64) {
-        const unsigned blocks = unsigned(bh * ((a.s.d_k + a.s.d_v) / 64) * (a.s.d_k / 32));
-        hipLaunchKernelGGL(chunk_state_mfma_kernel, dim3(blocks), dim3(kThreads), 0, stream, a);
+        const int64_t blocks = bh * ((a.s.d_k + a.s.d_v) / 64) * (a.s.d_k / 32);
+        if (!grid_fits(blocks, kThreads)) return hipErrorInvalidConfiguration;
+        hipLaunchKernelGGL(chunk_state_mfma_kernel, dim3(unsigned(blocks)), dim3(kThreads), 0, stream, a);
         return hipGetLastError();
     }
     const int64_t blocks = bh * ((a.s.d_k + a.s.d_v) / kTileRows);
+    if (!grid_fits(blocks, kThreads)) return hipErrorInvalidConfiguration;
     if (a.s.bf16)
         hipLaunchKernelGGL(chunk_state_kernel<bf16_t>, dim3(unsigned(blocks)), dim3(kThreads), 0,
                            stream, a);

@@ -19,6 +19,7 @@
 //      writes it back, and the row sums of G diag(x) are reduced across lanes
 //      and waves.
 // All arithmetic is fp32.  Few pairs take a kernel of their own (decode_few_kernel below).
+#include <algorithm>
 #include <type_traits>
 
 #include "mesa_device.hpp"
@@ -505,6 +506,7 @@ template <typename Tin, int DK, bool PACKED>
 hipError_t launch_dk(const DecodeArgs& a, hipStream_t stream)
 {
     const unsigned blocks = unsigned(a.batch * a.heads);
+    if (!grid_fits(blocks, DK)) return hipErrorInvalidConfiguration;   // the few-pairs kernel's are few
     // Up to two workgroups of the few-pairs kernel per compute unit at d_k = 128 (four at
     // 64) its shorter chain wins, beyond that the kernel above, which keeps more pairs in flight
     // (us per step, 15 CG steps, few-pairs kernel against the one above; packed in brackets):
@@ -536,36 +538,39 @@ hipError_t launch_dk(const DecodeArgs& a, hipStream_t stream)
     return hipGetLastError();
 }
 
-// full <-> packed symmetric state (one thread per stored element; the packed
+// full <-> packed symmetric state (one thread per stored element, up to what one launch holds; the packed
 // element HP[k][i] is H[i][(i + k) mod d_k], so unpacking writes it to (i, i + k)
 // and (i + k, i))
 __global__ __launch_bounds__(256) void pack_state_kernel(const float* H, float* HP, int64_t pairs, int dk)
 {
     const int64_t per = int64_t(dk / 2 + 1) * dk;
-    const int64_t idx = int64_t(blockIdx.x) * 256 + threadIdx.x;
-    if (idx >= pairs * per) return;
-    const int64_t pr = idx / per;
-    const int e = int(idx % per), k = e / dk, i = e % dk;
-    HP[idx] = H[pr * dk * dk + int64_t(i) * dk + ((i + k) & (dk - 1))];
+    for (int64_t idx = int64_t(blockIdx.x) * 256 + threadIdx.x; idx < pairs * per; idx += int64_t(gridDim.x) * 256) {
+        const int64_t pr = idx / per;
+        const int e = int(idx % per), k = e / dk, i = e % dk;
+        HP[idx] = H[pr * dk * dk + int64_t(i) * dk + ((i + k) & (dk - 1))];
+    }
 }
 
 __global__ __launch_bounds__(256) void unpack_state_kernel(const float* HP, float* H, int64_t pairs, int dk)
 {
-    const int64_t idx = int64_t(blockIdx.x) * 256 + threadIdx.x;
-    if (idx >= pairs * dk * dk) return;
-    const int64_t pr = idx / (int64_t(dk) * dk);
-    const int e = int(idx % (int64_t(dk) * dk)), i = e / dk, j = e % dk;
-    // H[i][j] is stored as HP[k][i] with k = (j - i) mod d_k when k <= d_k/2, else as
-    // HP[(i - j) mod d_k][j]; on the last diagonal the copy at the smaller index of
-    // {i, j} mod d_k/2 is the stored one
-    int k = (j - i) & (dk - 1), at = i;
-    if (k > dk / 2) {
-        k = (i - j) & (dk - 1);
-        at = j;
+    for (int64_t idx = int64_t(blockIdx.x) * 256 + threadIdx.x; idx < pairs * dk * dk; idx += int64_t(gridDim.x) * 256) {
+        const int64_t pr = idx / (int64_t(dk) * dk);
+        const int e = int(idx % (int64_t(dk) * dk)), i = e / dk, j = e % dk;
+        // H[i][j] is stored as HP[k][i] with k = (j - i) mod d_k when k <= d_k/2, else as
+        // HP[(i - j) mod d_k][j]; on the last diagonal the copy at the smaller index of
+        // {i, j} mod d_k/2 is the stored one
+        int k = (j - i) & (dk - 1), at = i;
+        if (k > dk / 2) {
+            k = (i - j) & (dk - 1);
+            at = j;
+        }
+        if (k == dk / 2) at = i % (dk / 2);
+        H[idx] = HP[pr * (dk / 2 + 1) * dk + int64_t(k) * dk + at];
     }
-    if (k == dk / 2) at = i % (dk / 2);
-    H[idx] = HP[pr * (dk / 2 + 1) * dk + int64_t(k) * dk + at];
 }
+
+// workgroups for n elements; past 2^30 threads each takes several
+unsigned convert_blocks(int64_t n) { return unsigned(std::min<int64_t>((n + 255) / 256, 1 << 22)); }
 
 template <typename Tin>
 hipError_t launch_tin(const DecodeArgs& a, hipStream_t stream)
@@ -585,7 +590,7 @@ hipError_t launch_pack_state(const float* H, float* HP, int64_t pairs, int d_k, 
 {
     const int64_t n = pairs * (d_k / 2 + 1) * d_k;
     if (n == 0) return hipSuccess;
-    hipLaunchKernelGGL(pack_state_kernel, dim3(unsigned((n + 255) / 256)), dim3(256), 0, stream, H, HP, pairs, d_k);
+    hipLaunchKernelGGL(pack_state_kernel, dim3(convert_blocks(n)), dim3(256), 0, stream, H, HP, pairs, d_k);
     return hipGetLastError();
 }
 
@@ -593,7 +598,7 @@ hipError_t launch_unpack_state(const float* HP, float* H, int64_t pairs, int d_k
 {
     const int64_t n = pairs * int64_t(d_k) * d_k;
     if (n == 0) return hipSuccess;
-    hipLaunchKernelGGL(unpack_state_kernel, dim3(unsigned((n + 255) / 256)), dim3(256), 0, stream, HP, H, pairs, d_k);
+    hipLaunchKernelGGL(unpack_state_kernel, dim3(convert_blocks(n)), dim3(256), 0, stream, HP, H, pairs, d_k);
     return hipGetLastError();
 }
 

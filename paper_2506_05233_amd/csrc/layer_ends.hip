@@ -290,7 +290,7 @@ hipError_t launch_front(const FrontArgs& a, hipStream_t stream)
     const int64_t gbk = (bh * a.seq_len + kThreads - 1) / kThreads;
     const int64_t lbk = (a.heads * DK + kThreads - 1) / kThreads;
     const int64_t blocks = 2 * nqk + nv + gbk + lbk;
-    if (blocks > INT32_MAX) return hipErrorInvalidValue;
+    if (!grid_fits(blocks, kThreads)) return hipErrorInvalidConfiguration;
     hipLaunchKernelGGL((frontend_kernel<Tin, DK, DV>), dim3(unsigned(blocks)), dim3(kThreads), 0, stream, a, nqk, nv, gbk);
     return hipGetLastError();
 }
@@ -309,7 +309,7 @@ hipError_t launch_norm(const NormArgs& a, hipStream_t stream)
     const int64_t items = a.batch * a.heads * ((a.seq_len + WT - 1) / WT);
     const int64_t per = kThreads / kWave;
     const int64_t blocks = (items + per - 1) / per;
-    if (blocks > INT32_MAX) return hipErrorInvalidValue;
+    if (!grid_fits(blocks, kThreads)) return hipErrorInvalidConfiguration;
     hipLaunchKernelGGL((output_norm_kernel<Tout, DV>), dim3(unsigned(blocks)), dim3(kThreads), 0, stream, a);
     return hipGetLastError();
 }

@@ -19,6 +19,7 @@ namespace {
 
 using mesa::finish;
 using mesa::ForwardShape;
+using mesa::launch_status;
 using mesa::overlaps;
 using mesa::Range;
 using mesa::range_of;
@@ -294,7 +295,7 @@ int launch_states(const FwdCall& c, bool store_chunks, hipStream_t s)
             sa.seg_bytes = full - states;
         }
     }
-    return mesa::launch_chunk_state(sa, s) == hipSuccess ? MESA_OK : MESA_ERR_HIP;
+    return launch_status(mesa::launch_chunk_state(sa, s));
 }
 
 int launch_solve(const FwdCall& c, hipStream_t s)
@@ -307,7 +308,7 @@ int launch_solve(const FwdCall& c, hipStream_t s)
     const hipError_t e = prec == MESA_PREC_BF16     ? mesa::launch_chunk_cg_bf16(ca, s)
                          : prec == MESA_PREC_BF16X3 ? mesa::launch_chunk_cg_x3(ca, s)
                                                     : mesa::launch_chunk_cg_f32(ca, s);
-    return e == hipSuccess ? MESA_OK : MESA_ERR_HIP;
+    return launch_status(e);
 }
 
 }  // namespace
@@ -461,8 +462,7 @@ int decode_step(float* state_H, float* state_G, const void* q, const void* k, co
     if (st != MESA_OK) return st;
     mesa::DecodeArgs da{batch, heads, int(d_k), int(d_v), b16, state_H, state_G,
                         q, k, v, gamma, beta, lambda, max_cg, out, eps * eps, steps_out, packed};
-    st = finish(mesa::launch_decode_step(da, static_cast<hipStream_t>(stream)) == hipSuccess ? MESA_OK : MESA_ERR_HIP,
-                stream);
+    st = finish(launch_status(mesa::launch_decode_step(da, static_cast<hipStream_t>(stream))), stream);
     if (st != MESA_OK) return st;
     return check_values({{out, pairs * d_v, false, -kFinite, kFinite}, {state_H, h_elems, false, -kFinite, kFinite},
                          {state_G, g_elems, false, -kFinite, kFinite}},
@@ -654,17 +654,17 @@ int backward_launch(const void* k, const void* v, const float* gamma, const floa
         fa.Gs32 = f32_at(L.gs);
         fa.seg_ws = f32_at(L.sh);
         fa.seg_bytes = size_t(L.u - L.sh);
-        if (mesa::launch_chunk_state(fa, s) != hipSuccess) return MESA_ERR_HIP;
+        if (const int e = launch_status(mesa::launch_chunk_state(fa, s)); e != MESA_OK) return e;
     } else {
         mesa::StateArgs sa{shape, k, v, gamma, beta, f32_at(L.hs), f32_at(L.gs), nullptr, nullptr, true, false};
-        if (mesa::launch_chunk_state(sa, s) != hipSuccess) return MESA_ERR_HIP;
+        if (const int e = launch_status(mesa::launch_chunk_state(sa, s)); e != MESA_OK) return e;
     }
     mesa::BwdArgs ba{shape, k, v, gamma, beta, qstar, dout, dq, f32_at(L.hs), f32_at(L.gs), f32_at(L.sh),
                      f32_at(L.ag), f32_at(L.u), use_bf16 ? u16_at(L.u16) : nullptr, dk, dv, dgamma, dbeta,
                      f32_at(L.dl), dlambda};
     // u_t = G_t^T e_t, then e*_t = (H_t + Lambda)^{-1} u_t into dq: on the matrix cores
     // (bf16 operands, u rounded to bf16, no read-out) or with fp32 products
-    if (mesa::launch_backward_stage(ba, 0, s) != hipSuccess) return MESA_ERR_HIP;
+    if (const int e = launch_status(mesa::launch_backward_stage(ba, 0, s)); e != MESA_OK) return e;
     if (use_bf16) {
         mesa::CgArgs ca{shape, u16_at(L.u16), k, v, gamma, beta, lambda, u16_at(L.fh), u16_at(L.fg), n_cg,
                         nullptr, dq, 0.0f, nullptr};
@@ -672,10 +672,10 @@ int backward_launch(const void* k, const void* v, const float* gamma, const floa
     } else {
         mesa::CgArgs ca{shape, nullptr, k, v, gamma, beta, lambda, f32_at(L.hs), f32_at(L.gs), n_cg, nullptr, dq,
                         0.0f, nullptr, f32_at(L.u)};
-        if (mesa::launch_chunk_cg_f32(ca, s) != hipSuccess) return MESA_ERR_HIP;
+        if (const int e = launch_status(mesa::launch_chunk_cg_f32(ca, s)); e != MESA_OK) return e;
     }
     for (int stage = 1; stage <= 3; ++stage)
-        if (mesa::launch_backward_stage(ba, stage, s) != hipSuccess) return MESA_ERR_HIP;
+        if (const int e = launch_status(mesa::launch_backward_stage(ba, stage, s)); e != MESA_OK) return e;
     return MESA_OK;
 }
 
@@ -812,7 +812,7 @@ int mesa_frontend(const void* qp, const void* kp, const void* vp, const float* c
                        conv_q, conv_k, conv_v, a_gamma, a_beta, theta, gamma_cap, l2_eps, q, k, v, gamma,
                        beta, lambda};
     const hipError_t e = mesa::launch_frontend(fa, static_cast<hipStream_t>(stream));
-    return finish(e == hipSuccess ? MESA_OK : MESA_ERR_HIP, stream);
+    return finish(launch_status(e), stream);
 }
 
 int mesa_output_norm(const float* o, const float* weight, float eps, int64_t batch, int64_t heads,
@@ -832,7 +832,7 @@ int mesa_output_norm(const float* o, const float* weight, float eps, int64_t bat
         return MESA_ERR_ARG;
     mesa::NormArgs na{batch, heads, seq_len, int(d_v), out_dtype == MESA_DTYPE_BF16, o, weight, eps, y};
     const hipError_t e = mesa::launch_output_norm(na, static_cast<hipStream_t>(stream));
-    return finish(e == hipSuccess ? MESA_OK : MESA_ERR_HIP, stream);
+    return finish(launch_status(e), stream);
 }
 
 }  // extern "C"

@@ -11,6 +11,7 @@
 namespace {
 
 using mesa::finish;
+using mesa::launch_status;
 using mesa::overlaps;
 using mesa::Range;
 using mesa::range_of;
@@ -89,11 +90,7 @@ bool clash(std::initializer_list<Rows> ins, std::initializer_list<Rows> outs)
     return false;
 }
 
-// A launch's own refusal of a grid past 32 bits of threads comes before anything is enqueued.
-int status_of(hipError_t e, void* stream)
-{
-    return finish(e == hipSuccess ? MESA_OK : e == hipErrorInvalidConfiguration ? MESA_ERR_SHAPE : MESA_ERR_HIP, stream);
-}
+int status_of(hipError_t e, void* stream) { return finish(launch_status(e), stream); }
 
 int checkpoint(const void* x, int64_t rows, int64_t width, int64_t stride, int dtype, const void* buffer, bool pack,
                void* stream)

@@ -30,6 +30,12 @@ inline bool sync_after_launch()
     return on;
 }
 
+// A launch's error as a status; a grid that one launch cannot hold is refused as a size.
+inline int launch_status(hipError_t e)
+{
+    return e == hipSuccess ? MESA_OK : e == hipErrorInvalidConfiguration ? MESA_ERR_SHAPE : MESA_ERR_HIP;
+}
+
 // The status an entry point returns once its launches are enqueued on `stream`.
 inline int finish(int status, void* stream)
 {

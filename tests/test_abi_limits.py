@@ -58,3 +58,14 @@ def test_ends_past_one_launch(lib):
                                       None) == L.MESA_ERR_SHAPE
     assert lib.mesa_output_norm_backward(P[0], P[1], 1e-6, P[2], 1 << 24, 1, 1, 64, 0, 0, P[3], P[4], P[5], 1 << 43,
                                          None) == L.MESA_ERR_SHAPE
+
+
+# The Mesa layer's own calls: workgroups of 256 threads, several for each (sequence, head).
+def test_mesa_layer_past_one_launch(lib):
+    P = [(k + 1) << 46 for k in range(20)]
+    big = 1 << 45
+    for dtype, BH in ((0, 1 << 21), (1, 1 << 23)):      # states: a workgroup for 16 rows in fp32, two in all for bf16
+        assert lib.mesa_forward(*P[:6], BH, 1, 1, 64, 64, dtype, 5, 64, P[6], P[7], big, None) == L.MESA_ERR_SHAPE
+        assert lib.mesa_backward(*P[:5], BH, 1, 1, 64, 64, dtype, 5, 0, P[5], P[6], *P[7:13], P[13], big, None) == L.MESA_ERR_SHAPE
+    assert lib.mesa_frontend(*P[:9], 0.99, 1e-6, 1 << 22, 8, 1, 64, 64, 0, *P[9:15], None) == L.MESA_ERR_SHAPE
+    assert lib.mesa_output_norm(P[0], P[1], 1e-6, 1 << 22, 16, 1, 64, 0, P[2], None) == L.MESA_ERR_SHAPE

@@ -40,3 +40,19 @@ def test_state_of_an_empty_sequence_past_32_bits():
                                   None, None, 0, torch.cuda.current_stream().cuda_stream)
     assert st == L.MESA_OK
     assert not bool(final.view(-1, W).any(dim=1).any())
+
+
+def test_packed_states_past_32_bits():
+    """More state elements than a launch has threads: the last pairs are converted as the first."""
+    pairs, d = (1 << 18) + 3, 128
+    full = torch.zeros((pairs, 1, d, d), device="cuda")
+    for p in (0, 1, pairs - 2, pairs - 1):
+        a = torch.randn((d, d), generator=torch.Generator().manual_seed(p)).cuda()
+        full[p, 0] = a + a.T
+    packed = L.pack_state(full)
+    few = torch.cat([full[:2], full[-2:]])
+    want = L.pack_state(few)
+    assert torch.equal(torch.cat([packed[:2], packed[-2:]]), want) and not bool(packed[2:-2].any())
+    del full
+    back = L.unpack_state(packed)
+    assert torch.equal(torch.cat([back[:2], back[-2:]]), few) and not bool(back[2:-2].any())
