@@ -116,7 +116,8 @@ int recurrence_sizes(int64_t batch, int64_t seq_len, int64_t width, int64_t stri
     if (!(isfinite(decay) && decay > 0.0f)) return MESA_ERR_ARG;
     if (batch > 0 && seq_len > 0 && stride < width) return MESA_ERR_SHAPE;
     const int64_t blocks = (seq_len + MESA_RECURRENCE_BLOCK - 1) / MESA_RECURRENCE_BLOCK, slabs = (width + 31) / 32;
-    if (!product_ok({batch, blocks, slabs}) || batch * blocks * slabs > INT32_MAX) return MESA_ERR_SHAPE;
+    // the states are batch x width, however few the tokens
+    if (!product_ok({batch, width}) || !product_ok({batch, blocks, slabs}) || batch * blocks * slabs > INT32_MAX) return MESA_ERR_SHAPE;
     return MESA_OK;
 }
 

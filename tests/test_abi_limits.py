@@ -69,3 +69,13 @@ def test_mesa_layer_past_one_launch(lib):
         assert lib.mesa_backward(*P[:5], BH, 1, 1, 64, 64, dtype, 5, 0, P[5], P[6], *P[7:13], P[13], big, None) == L.MESA_ERR_SHAPE
     assert lib.mesa_frontend(*P[:9], 0.99, 1e-6, 1 << 22, 8, 1, 64, 64, 0, *P[9:15], None) == L.MESA_ERR_SHAPE
     assert lib.mesa_output_norm(P[0], P[1], 1e-6, 1 << 22, 16, 1, 64, 0, P[2], None) == L.MESA_ERR_SHAPE
+
+
+# With no token the states are still batch x width: their size is checked as any other's.
+@pytest.mark.parametrize("B,W", [(1 << 50, 1 << 20), ((1 << 40) + 1, 1), (1 << 40, 2), (1 << 21, 1 << 20)])
+def test_states_of_empty_sequences_too_large(lib, B, W):
+    f = FAR
+    assert lib.mesa_recurrence(None, None, None, None, 8.0, None, f["x"], B, 0, W, W, 0, None, f["y"], None, None, None, None, None, 0,
+                               None) == L.MESA_ERR_SHAPE
+    assert lib.mesa_recurrence_backward(None, None, None, f["th"], 8.0, None, None, None, f["dy"], B, 0, W, W, 0, 0, W, None, None, None,
+                                        f["dth"], f["dx"], None, 0, None) == L.MESA_ERR_SHAPE
