@@ -822,8 +822,9 @@ __global__ __launch_bounds__(F::kThreads, (kLean<T, Tg> ? 4 : 2)) void recurrenc
             const float g = d[v] + c[v], ag = q.a * g;
             gx[v] = g * m[v] * si;
             gi[v] = gx[v] * x[v] * rest_of(q.ei, si);
-            const float dl = ag * fmaf(-q.a * __builtin_amdgcn_rcpf(m[v]), si * x[v], q.hp);
-            dls[v] = dl * s;
+            // dl s, with s / m first: it is at most m / (2 decay softplus(theta)), where 1 / m beside
+            // a large x would overflow and then meet an s of 0
+            dls[v] = ag * fmaf(-q.a * (s * __builtin_amdgcn_rcpf(m[v])), si * x[v], s * q.hp);
             gr[v] = dls[v] * (k[v] * rest_of(q.er, s));
             c[v] = ag;
         }

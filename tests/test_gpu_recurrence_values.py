@@ -1,0 +1,69 @@
+"""Gradients of the recurrence where a gate is shut beside an input of any finite size.
+
+What a shut gate costs.  The kernel's m' = sqrt(m^2 + 2^-120) is off by at most 2^-60.  So dx = g m sigma(i) is
+off by 2^-60 |g| and di by 2^-60 |g x|.  With K = decay softplus(theta) and m^2 <= 2 K s, the second term of
+dl s, s a^2 / m sigma(i) x, is off by s (1 / m - 1 / m') |g x| <= m (1 - m / m') |g x| / (2 K) <= 2^-60 |g x| / (6 K),
+hence dr = dl l (1 - s) by 2^-60 |g x| / 6 and dtheta by that times the number of shut tokens and decay sigma(theta) / K
+<= 1.  |g| is at most the sum of the magnitudes of the column's dy.  To that comes 2e-5 of an array's column, as
+for any gradient."""
+import numpy as np
+import pytest
+
+from oracle import recurrence as R
+from paper_2506_05233_amd import libmesa as L
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+TOL_GRAD = 2e-5
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    L.load()
+    yield
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("size", [1e19, 1e21, 1e25, 1e30])
+def test_a_shut_gate_beside_a_large_input(size, dtype):
+    T, W, at = 140, 8, 50
+    rng = np.random.default_rng(0)
+    x, r, i, dy = (torch.from_numpy(rng.standard_normal((1, T, W)).astype(np.float32)).to(dtype) for _ in range(4))
+    th = np.full(W, -4.0, np.float32)
+    r[0, at] = torch.tensor([-200.0, -100.0, -90.0, -80.0, -60.0, -30.0, 0.0, 40.0]).to(dtype)
+    x[0, at] = torch.tensor(size).to(dtype)
+    f64 = [t.double().numpy() for t in (x, r, i, dy)]
+    ref = R.forward(*f64[:3], th)
+    states = ref["states"].astype(np.float32)
+    want = R.backward(*f64[:3], th, states, f64[3])
+    d = [t.cuda() for t in (x, r, i)]
+    g = L.recurrence_backward(*d, torch.from_numpy(th).cuda(), torch.from_numpy(states).cuda(), dy.cuda())
+    bound = 2.0 ** -60 * np.abs(f64[3][0]).sum(axis=0)
+    rounding = 2.0 ** -8 if dtype is torch.bfloat16 else 0.0
+    for n in ("dx", "dr", "di", "dtheta"):
+        got, ref_n = g[n].double().cpu().numpy().reshape(-1, W), want[n].reshape(-1, W)
+        assert np.all(np.isfinite(got)), n
+        for c in range(W):
+            off = bound[c] * (1.0 if n == "dx" else float(f64[0][0, at, c]))
+            col = want["dtheta_size"][c] if n == "dtheta" else np.linalg.norm(ref_n[:, c])
+            err = np.linalg.norm(got[:, c] - ref_n[:, c])
+            assert err <= (TOL_GRAD + rounding) * col + off, (n, c, err, col, off)
+
+
+def test_a_gate_shut_for_good():
+    """r = -infinity: the token leaves the state as it is, and its gate has no gradient."""
+    T, W = 140, 4
+    rng = np.random.default_rng(1)
+    x, r, i, dy = (torch.from_numpy(rng.standard_normal((1, T, W)).astype(np.float32)).cuda() for _ in range(4))
+    r[0, 50] = -float("inf")
+    x[0, 50, 1:] = torch.tensor([1e10, 1e21, 3e38], device="cuda")
+    th = torch.full((W,), -4.0, device="cuda")
+    f = L.recurrence(x, r, i, th, want_states=True)
+    assert torch.equal(f["y"][0, 50], f["y"][0, 49])
+    g = L.recurrence_backward(x, r, i, th, f["states"], dy)
+    assert all(bool(torch.isfinite(g[n]).all()) for n in g) and not g["dr"][0, 50].any()
