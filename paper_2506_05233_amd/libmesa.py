@@ -191,6 +191,22 @@ def _check(t, name, shape, dtype=None, device=None):
         raise ValueError("%s must be contiguous" % name)
 
 
+def _workspace(workspace, need, device):
+    """A caller's workspace, when it is given, on the device and large enough, or a new one.  It
+    must be contiguous: a kernel writes the bytes that it counts, one after the other."""
+    if need == 0:
+        return None
+    torch = _torch()
+    if workspace is not None:
+        if not isinstance(workspace, torch.Tensor):
+            raise TypeError("workspace must be a torch.Tensor")
+        if workspace.device == device and workspace.numel() * workspace.element_size() >= need:
+            if not workspace.is_contiguous():
+                raise ValueError("workspace must be contiguous")
+            return workspace
+    return torch.empty(need, dtype=torch.uint8, device=device)
+
+
 def _ptr(t):
     return None if t is None else t.data_ptr()
 
@@ -234,8 +250,7 @@ def forward(q, k, v, gamma, beta, lam, n_cg, chunk=64, precision=MESA_PREC_AUTO,
         out = torch.empty((B, H, T, dv), dtype=torch.float32, device=dev)
     _check(out, "out", (B, H, T, dv), torch.float32, dev)
     need = lib.mesa_forward_workspace_bytes(B, H, T, dk, dv, chunk)
-    if workspace is None or workspace.numel() * workspace.element_size() < need:
-        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=dev)
+    workspace = _workspace(workspace, max(need, 1), dev)
     qstar = torch.empty((B, H, T, dk), dtype=torch.float32, device=dev) if want_qstar else None
     if eps is not None or want_steps:
         if want_states:
@@ -430,8 +445,7 @@ def backward(k, v, gamma, beta, lam, qstar, dout, n_cg, precision=MESA_PREC_AUTO
     _check(qstar, "qstar", (B, H, T, dk), torch.float32, dev)
     _check(dout, "dout", (B, H, T, dv), torch.float32, dev)
     need = lib.mesa_backward_workspace_bytes(B, H, T, dk, dv)
-    if workspace is None or workspace.numel() * workspace.element_size() < need:
-        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=dev)
+    workspace = _workspace(workspace, max(need, 1), dev)
     f32 = dict(dtype=torch.float32, device=dev)
     res = {"dq": torch.empty((B, H, T, dk), **f32), "dk": torch.empty((B, H, T, dk), **f32),
            "dv": torch.empty((B, H, T, dv), **f32), "dgamma": torch.empty((B, H, T), **f32),
@@ -614,16 +628,6 @@ def _on_device(t, name):
     if not t.is_cuda:
         raise ValueError("%s must be a device tensor" % name)
     return t.device
-
-
-def _workspace(workspace, need, device):
-    """A caller's workspace, when it is given and large enough, or a new one."""
-    if need == 0:
-        return None
-    if workspace is not None and workspace.device == device and workspace.numel() * workspace.element_size() >= need:
-        return workspace
-    torch = _torch()
-    return torch.empty(need, dtype=torch.uint8, device=device)
 
 
 def checkpoint_bytes(rows, width) -> int:
