@@ -861,14 +861,17 @@ def frontend_backward(qp, kp, vp, conv_q, conv_k, conv_v, a_gamma, a_beta, theta
                       gamma_cap=0.9975, l2_eps=1e-6, grad_dtype=None, workspace=None):
     """mesa_frontend_backward: gradients of frontend()'s inputs from those of its outputs (dq,
     dk [B,H,T,d_k], dv [B,H,T,d_v], dgamma, dbeta [B,H,T], dlam [H,d_k]: fp32, as backward()
-    returns them).  qp, kp, vp as given to frontend(), or Checkpoints of them.  Returns a dict:
+    returns them).  qp, kp, vp as given to frontend(), or Checkpoints of them; without conv_v vp
+    is not read and may be None.  Returns a dict:
     "dqp", "dkp" [B,T,H,d_k], "dvp" [B,T,H,d_v] of grad_dtype (the projections' dtype by default,
     bf16 for Checkpoints), "dconv_q", "dconv_k" [H*d_k,4], "dconv_v" [H*d_v,4] (with conv_v),
     "da_gamma", "da_beta" [B,T,H], "dtheta" [H,d_k] (fp32)."""
     torch = _torch()
     lib = load()
     B, T, H, dk_ = qp.shape
-    dv_ = vp.shape[-1]
+    if vp is None and conv_v is not None:
+        raise TypeError("vp must be given with conv_v")
+    dv_ = (dv if vp is None else vp).shape[-1]
     f32 = torch.float32
     q8 = isinstance(qp, Checkpoint)
     dev = qp.device if q8 else _on_device(qp, "qp")
@@ -878,7 +881,8 @@ def frontend_backward(qp, kp, vp, conv_q, conv_k, conv_v, a_gamma, a_beta, theta
         grad_dtype = torch.bfloat16 if q8 else qp.dtype
     qp = _held(qp, "qp", (B, T, H, dk_), dtype, dev)
     kp = _held(kp, "kp", (B, T, H, dk_), dtype, dev)
-    vp = _held(vp, "vp", (B, T, H, dv_), dtype, dev)
+    if vp is not None:
+        vp = _held(vp, "vp", (B, T, H, dv_), dtype, dev)
     gates, outs = (B, T, H), (B, H, T)
     _check_all(f32, dev, (conv_q, "conv_q", (H * dk_, 4)), (conv_k, "conv_k", (H * dk_, 4)), (a_gamma, "a_gamma", gates),
                (a_beta, "a_beta", gates), (theta, "theta", (H, dk_)), (dq, "dq", (B, H, T, dk_)), (dk, "dk", (B, H, T, dk_)),
@@ -886,7 +890,7 @@ def frontend_backward(qp, kp, vp, conv_q, conv_k, conv_v, a_gamma, a_beta, theta
     if conv_v is not None:
         _check_all(f32, dev, (conv_v, "conv_v", (H * dv_, 4)))
     like = torch.empty_like     # quicker than torch.empty, and every gradient has its input's shape
-    if q8:
+    if q8 or vp is None:
         grads = [torch.empty(t, dtype=grad_dtype, device=dev) for t in ((B, T, H, dk_), (B, T, H, dk_), (B, T, H, dv_))]
     else:
         grads = [like(t, dtype=grad_dtype) for t in (qp, kp, vp)]
