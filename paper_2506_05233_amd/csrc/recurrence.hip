@@ -44,6 +44,7 @@ constexpr int kRows = 32;              // runs of tokens of a workgroup, one to 
 template <int Across>
 struct Form {
     static constexpr int kAcross = Across, kCh = 4 * Across, kWaveRows = kWave / Across, kWaves = kRows / kWaveRows, kThreads = kWaves * kWave;
+    static_assert(kCh <= kWave, "the walk has a channel in each lane");
 };
 constexpr int kBlock = kRecurrenceBlock;
 
@@ -660,6 +661,7 @@ __global__ __launch_bounds__(F::kThreads, (kLean<T, Tg> ? 4 : 2)) void recurrenc
 {
     constexpr int kAcross = F::kAcross, kCh = F::kCh, kWaveRows = F::kWaveRows;
     constexpr bool Lean = kLean<T, Tg>;
+    static_assert(F::kWaves >= 3, "a wave for each: the pass back, the states, and publishing, which later tiles wait for");
     __shared__ BackwardShared<Lean, F> sh;
     const int slabs = int((a.width + kCh - 1) / kCh);
     const int slab = int(blockIdx.x) % slabs, ticket = draw_ticket(a.words, a.tiles > 1, slab, slabs);
