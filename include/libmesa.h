@@ -391,10 +391,11 @@ int mesa_backward(const void* k, const void* v, const float* gamma, const float*
 /* Activation checkpoints in 8 bits: what a training forward keeps for its backward pass.
  * A row of `width` values is held in groups of MESA_CHECKPOINT_GROUP channels; a group has
  * one power of two 2^E, E the least number >= -126 for which every rint(x / 2^E) (half to
- * even) lies in [-127, 127], and those codes.  A value comes back as code * 2^E, so its
- * error is at most 2^E / 2 <= max|x| / 127 over its group, and exactly that in fp32 or bf16.
- * A group that holds a NaN or an infinity comes back as NaN throughout; magnitudes above
- * 63.5 * 2^122 come back as 63 * 2^122.
+ * even) lies in [-127, 127], and those codes.  A value comes back as code * 2^E, exactly that in
+ * fp32 or bf16, so its error is at most 2^E / 2, which is at most max(max|x| / 127, 2^-127) over its
+ * group (below a largest magnitude of 2^-120 the latter, up to the whole value).  A group that
+ * holds a NaN or an infinity comes back as NaN throughout.  A group that reaches 63.75 * 2^122 has
+ * E = 122 and codes to 63: its magnitudes above 63.5 * 2^122 come back as 63 * 2^122.
  * A checkpoint of rows x width is one buffer of mesa_checkpoint_bytes(rows, width) bytes,
  * 16-byte aligned: the codes int8 [rows, width], then, from the next multiple of 16 bytes,
  * the exponent bytes uint8 [rows, ceil(width / MESA_CHECKPOINT_GROUP)] (E + 127, or 255 for a

@@ -4,7 +4,8 @@
 // A power of two makes both directions exact but for the one rounding: x 2^-E and code 2^E
 // are exact products, the codes are the same however they are computed, restoring to bf16
 // loses nothing (seven bits fit its eight), and the scale is one byte for 32 values.  The
-// error of a value is at most 2^E / 2 <= amax / 127; a free scale amax / 127 would halve
+// error of a value is at most 2^E / 2 <= amax / 127 (2^-127 where E stops at -126, and up to 2^E for
+// magnitudes that the largest exponent's codes stop short of); a free scale amax / 127 would halve
 // that at best, at four bytes a group and with codes that hang on the rounding of a quotient.
 //
 // Both kernels are HBM-bound: 3.03 (bf16) or 5.03 (fp32) bytes an element each way.  A lane
