@@ -440,7 +440,9 @@ int mesa_checkpoint_unpack(const void* checkpoint, int64_t rows, int64_t width, 
  *            written on the way, the same bytes as mesa_checkpoint_pack's
  *   workspace / workspace_bytes: at least mesa_recurrence_workspace_bytes(...) (0 for up
  *            to MESA_RECURRENCE_BLOCK tokens: then it may be NULL), 16-byte aligned
- * Any width, length and element alignment; the state and every product are fp32.  Outputs
+ * Any width, length and element alignment; the state and every product are fp32.  A state that
+ * is not finite stays so until a reset, but not always the same: runs of tokens are joined by the
+ * product of their a_t, and an infinity times one that has underflowed is a NaN.  Outputs
  * must overlap neither an input nor each other (MESA_ERR_ARG).  At most two kernel launches. */
 #define MESA_RECURRENCE_BLOCK 128
 size_t mesa_recurrence_workspace_bytes(int64_t batch, int64_t seq_len, int64_t width);

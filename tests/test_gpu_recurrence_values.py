@@ -67,3 +67,22 @@ def test_a_gate_shut_for_good():
     assert torch.equal(f["y"][0, 50], f["y"][0, 49])
     g = L.recurrence_backward(x, r, i, th, f["states"], dy)
     assert all(bool(torch.isfinite(g[n]).all()) for n in g) and not g["dr"][0, 50].any()
+
+
+@pytest.mark.parametrize("T", [5, 130, 700, 2500])
+def test_an_infinite_state_stays_not_finite_until_a_reset(T):
+    """Whatever the tokens' products underflow to, no later token of the document comes out finite, and all of the
+    next one do; the other channels and the other sequence are untouched."""
+    rng = np.random.default_rng(T)
+    x, r, i = (torch.from_numpy(rng.standard_normal((2, T, 36)).astype(np.float32)).cuda() for _ in range(3))
+    th = torch.from_numpy(rng.uniform(-8.0, 2.0, 36).astype(np.float32)).cuda()      # from slow to underflowing at once
+    clean = L.recurrence(x, r, i, th, want_final=True)
+    x[0, 2, ::2] = float("inf")
+    f = L.recurrence(x, r, i, th, want_final=True)
+    y = f["y"]
+    assert not torch.isfinite(y[0, 2:, ::2]).any() and not torch.isfinite(f["h"][0, ::2]).any()
+    assert torch.equal(y[0, :, 1::2], clean["y"][0, :, 1::2]) and torch.equal(y[1], clean["y"][1]) and torch.equal(y[0, :2], clean["y"][0, :2])
+    reset = torch.zeros((2, T), dtype=torch.uint8, device="cuda")
+    reset[0, T - 2] = 1
+    y = L.recurrence(x, r, i, th, reset=reset)
+    assert not torch.isfinite(y[0, 2:T - 2, ::2]).any() and torch.isfinite(y[0, T - 2:]).all()
