@@ -65,6 +65,16 @@ __device__ __forceinline__ float group_sum(float v)
     return v;
 }
 
+// 1 / sqrt(x) of a square sum and an eps.  The instruction takes a subnormal as 0, which it can be if
+// nothing is added to tiny rows; Small: as the forward then, where it counts.
+template <bool Small>
+__device__ __forceinline__ float rsq(float x)
+{
+    return Small ? rsqrtf(x) : __builtin_amdgcn_rsqf(x);
+}
+// Whether an eps leaves subnormal sums as they are.
+__host__ __device__ __forceinline__ bool small_eps(float eps) { return eps < 0x1p-126f; }
+
 // Four channels at element `at` of a dense array of T, or of a checkpoint whose exponent
 // bytes start at `bytes` (its width is a multiple of 32, so element e has byte e / 32).
 template <typename T>
@@ -85,7 +95,7 @@ struct Held<q8_t> {
 
 // One stream (kind 0 q, 1 k, 2 v) of one (sequence, head): `blk` its workgroup among those
 // of the sequence.
-template <typename T, typename Tg, int D>
+template <typename T, typename Tg, int D, bool Small>
 __device__ void stream_grad(const FrontGradArgs& a, int kind, int64_t bh, int64_t blk, int64_t blocks, int run, float* partial,
                             float (&red)[kThreads * 16])
 {
@@ -166,8 +176,8 @@ __device__ void stream_grad(const FrontGradArgs& a, int kind, int64_t bh, int64_
             }
             float n = 1.0f, pull = 0.0f;
             if (kind < 2) {
-                n = __builtin_amdgcn_rsqf(group_sum<LPT>(ss) + a.l2_eps);
-                pull = n * n * group_sum<LPT>(dot);
+                n = rsq<Small>(group_sum<LPT>(ss) + a.l2_eps);
+                pull = n * (n * group_sum<LPT>(dot));
             }
             float dp[4];
 #pragma unroll
@@ -232,12 +242,17 @@ __global__ __launch_bounds__(kThreads) void frontend_grad_kernel(FrontGradArgs a
     if (id < 2 * nk) {
         const int kind = id < nk ? 0 : 1;
         id -= kind * nk;
-        stream_grad<T, Tg, DK>(a, kind, id / p.blocks_k, id % p.blocks_k, p.blocks_k, p.run_k, a.partial + kind * p.part_k, red);
+        float* partial = a.partial + kind * p.part_k;
+        // a form of its own, since the few instructions more cost both ends 200 us of 195 at the size above
+        if (small_eps(a.l2_eps))
+            stream_grad<T, Tg, DK, true>(a, kind, id / p.blocks_k, id % p.blocks_k, p.blocks_k, p.run_k, partial, red);
+        else
+            stream_grad<T, Tg, DK, false>(a, kind, id / p.blocks_k, id % p.blocks_k, p.blocks_k, p.run_k, partial, red);
         return;
     }
     id -= 2 * nk;
     if (id < nv) {
-        stream_grad<T, Tg, DV>(a, 2, id / p.blocks_v, id % p.blocks_v, p.blocks_v, p.run_v, a.partial + 2 * p.part_k, red);
+        stream_grad<T, Tg, DV, false>(a, 2, id / p.blocks_v, id % p.blocks_v, p.blocks_v, p.run_v, a.partial + 2 * p.part_k, red);
         return;
     }
     id -= nv;
@@ -356,8 +371,9 @@ __global__ __launch_bounds__(kThreads) void output_norm_grad_kernel(NormGradArgs
                 ss = fmaf(o[c], o[c], ss);
                 dot = fmaf(z[c], o[c], dot);
             }
-            const float n = __builtin_amdgcn_rsqf(group_sum<LPT>(ss) * (1.0f / D) + a.eps);
-            const float pull = n * n * group_sum<LPT>(dot) * (1.0f / D);
+            // n^2 of a small row would overflow, n times the mean of z o is of z's order
+            const float n = rsq<true>(group_sum<LPT>(ss) * (1.0f / D) + a.eps);   // no slower here
+            const float pull = n * (n * (group_sum<LPT>(dot) * (1.0f / D)));
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 out[c] = n * fmaf(-pull, o[c], z[c]);
