@@ -11,8 +11,11 @@
 // Both kernels are HBM-bound: 3.03 (bf16) or 5.03 (fp32) bytes an element each way.  A lane
 // moves eight consecutive values (16 bytes of bf16), so a group is four lanes and its
 // maximum two exchanges inside a quad.  16384 rows of 2048 bf16: 17.7 us to pack, 16.0 to
-// unpack (102 MB, 5.7 and 6.4 TB/s, part of it out of the last-level cache).  Rows of 1000 or
-// at odd addresses go element by element: 33 of them 7 and 8 us, all latency.
+// unpack (102 MB, 5.7 and 6.4 TB/s, part of it out of the last-level cache), 8192 rows of fp32 13.5
+// and 16.8 (101 MB).  Anything but dense rows of whole groups on aligned memory goes element by
+// element, three to four times as long: the same 16384 rows as thirds of rows of 6144 52 and 59 us, the
+// fp32 ones 37 and 52, 33554 bf16 rows of 1000 or of 1001 57 and 64.  33 fp32 rows of 1000 take 7 and 8
+// us, all latency.
 #include "mesa_kernels.hpp"
 #include "mesa_lanes.hpp"
 
@@ -166,7 +169,7 @@ template <typename T>
 hipError_t launch(const CheckpointArgs& a, bool pack, hipStream_t stream)
 {
     // dense rows of whole groups on aligned memory are one run of groups: no division, 16
-    // bytes a lane
+    // bytes a lane (both forms' times above)
     const bool flat = a.width % kGroup == 0 && a.stride == a.width && uintptr_t(a.x) % 16 == 0;
     const int64_t pieces = a.rows * ((a.width + kGroup - 1) / kGroup) * (kGroup / kPer);
     const int64_t blocks = (pieces + kThreads * kIter - 1) / (kThreads * kIter);

@@ -19,8 +19,9 @@
 // partial row; a second small kernel adds the rows in order.
 //
 // Both are HBM-bound.  8 sequences of 16 heads of 128 channels, 2048 tokens, from checkpoints to
-// bf16: front end 145 us (714 MB, 4.9 TB/s; its vector units are busy for two thirds of that),
-// back end 43 us (236 MB, 5.5 TB/s), each with 5 us for the sums of the partial rows.
+// bf16, no filter on the values: front end 145 to 148 us (680 MB, 4.6 TB/s; its vector units are busy
+// for seven tenths of that), back end 43 us (236 MB, 5.5 TB/s), each with 5 us for the sums of the
+// partial rows.
 #include "mesa_kernels.hpp"
 #include "mesa_lanes.hpp"
 
@@ -34,7 +35,11 @@ constexpr int kHalo = 3;
 constexpr int groups_of(int d) { return kThreads / (d / 4); }  // runs of a workgroup
 
 // Tokens of a run: long runs repeat the three halo tokens less often, short ones give
-// enough workgroups when there are few tokens.
+// enough workgroups when there are few tokens.  With runs of 64, 32 and 16, sequences of 16 heads of
+// 2048 tokens of 128 channels from 8 bits: front end 1 sequence 36, 24, 23 us, 2 42, 36, 38, 4 72, 75,
+// 81, 8 147, 149, 157, 16 300, 310, 353; back end 24, 14, 10, 24, 16, 14, 37, 26, 25, 48, 43, 45 and 81, 88,
+// 82.  2 x 4 heads of 777 fp32 tokens of 64 channels: 29, 17, 11 and 17, 10, 7.  The rule takes 16, 16,
+// 16, 32, 64 and 16: the front end of 4 sequences alone would take longer ones.
 int run_of(int64_t sequences, int64_t seq_len, int d)
 {
     for (int run : {64, 32}) {

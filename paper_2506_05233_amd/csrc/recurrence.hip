@@ -21,11 +21,13 @@
 //
 // 8 x 2048 tokens of 2048 bf16 channels: forward 51 us, 268 MB or 5.2 TB/s, what a copy of that
 // size reaches; with the inputs' checkpoints written as well a forward of 4 x 2000 tokens of 1536
-// packed channels takes 40 us (3.4 TB/s), three quarters of it arithmetic.  Backward from
-// checkpoints to bf16 gradients 93 to 96 us (3.9 TB/s): ten transcendentals and some sixty other
-// instructions an element keep the vector units busy for four fifths of the time, and the rest is
-// each workgroup waiting for its first loads and its walk.  One row of 16381 tokens: 60 us, its 64
-// tiles one behind the other.  One token of 1 x 2048 or 256 x 2048 channels is one launch.
+// packed channels takes 40 us (3.4 TB/s): 78 vector instructions an element, 45 of them for packing
+// and resets.  Backward from checkpoints to bf16 gradients 95 to 98 us (3.9 TB/s): ten
+// transcendentals and some sixty other instructions an element keep the vector units busy for four
+// fifths of the time, and the rest is each workgroup waiting for its first loads and its walk; from
+// bf16 tensors 108 us (4.4 TB/s).  fp32, 4 x 2048 tokens of 2048: forward 44 us, backward 86 us (6.1
+// and 5.5 TB/s).  One row of 16381 tokens: 60 us, its 64 tiles one behind the other.  One token of
+// 1 x 2048 or 256 x 2048 channels is one launch.
 #include <algorithm>
 #include <type_traits>
 
@@ -638,8 +640,10 @@ struct Kept {
 };
 
 // Lean: 16-bit gradients of 8- or 16-bit inputs run two workgroups a compute unit, with 128
-// registers a lane, and keep m in LDS.  With fp32 arrays, whose four inputs alone are 64
-// registers, that many would spill: one workgroup of up to 256.
+// registers a lane, and keep m in LDS.  Other types one workgroup of up to 256.  fp32 inputs, which
+// with dy are 64 registers, spill in 128 (48 bytes a lane; 4 x 2048 tokens of 2048, fp32 gradients:
+// 86 us so, 99 lean).  fp32 gradients of narrower inputs would be faster lean (from bf16 75 us so, 61
+// lean, from 8 bits 81 and 63, of which the aligned forms without resets spill up to 20 bytes).
 template <typename T, typename Tg>
 constexpr bool kLean = sizeof(T) <= 2 && sizeof(Tg) == 2;
 
@@ -897,9 +901,11 @@ hipError_t clear_walk(uint64_t* words, int64_t batch, int64_t tiles, int64_t wid
 }
 
 // Workgroups of 64 channels read and write whole lines of memory; where there are fewer of
-// them than compute units, workgroups of half the channels finish sooner (a 777-token fp32
-// gradient of 2 x 321 channels, 84 of the wide ones: 22 us wide, 17 narrow; 2048 tokens of
-// 8 x 2048: 106 us wide, 160 narrow).  The narrow ones always look for resets.
+// them than compute units, workgroups of half the channels finish sooner or as soon (777 tokens of
+// 2 x 321, fp32 gradient, 84 of the wide ones: 22.5 us wide, 16.2 narrow; 100 tokens of 2 x 768, fp32,
+// 24: 8.3 and 6.0; 2048 tokens of 2 x 192 from 8 bits, 96: 13.0 both, 2 x 384, 192: 13.4 and 14.4; not
+// from there on: 2 x 512, 256: 13.9 and 14.0, 2 x 1024 17.4 and 23.0, 8 x 2048 97 and 124, forward 50
+// and 74).  The narrow ones always look for resets.
 using Wide = Form<16>;
 using Narrow = Form<8>;
 
