@@ -322,7 +322,7 @@ const char* mesa_status_string(int status)
     switch (status) {
         case MESA_OK: return "ok";
         case MESA_ERR_NULL: return "a required pointer is NULL";
-        case MESA_ERR_SHAPE: return "a size is negative or the sizes are inconsistent";
+        case MESA_ERR_SHAPE: return "a size is negative, or the sizes are inconsistent or past what one launch holds";
         case MESA_ERR_UNSUPPORTED: return "d_k, d_v, chunk, dtype or precision not supported";
         case MESA_ERR_ARG: return "n_cg or eps out of range, a misaligned pointer, or an output overlapping an input";
         case MESA_ERR_WORKSPACE: return "workspace too small";

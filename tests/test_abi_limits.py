@@ -79,3 +79,7 @@ def test_states_of_empty_sequences_too_large(lib, B, W):
                                None) == L.MESA_ERR_SHAPE
     assert lib.mesa_recurrence_backward(None, None, None, f["th"], 8.0, None, None, None, f["dy"], B, 0, W, W, 0, 0, W, None, None, None,
                                         f["dth"], f["dx"], None, 0, None) == L.MESA_ERR_SHAPE
+
+
+def test_the_status_says_so(lib):
+    assert b"launch" in lib.mesa_status_string(L.MESA_ERR_SHAPE)
