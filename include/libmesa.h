@@ -527,6 +527,67 @@ int mesa_output_norm_backward(const void* o, const float* weight, float eps, con
                               int64_t heads, int64_t seq_len, int64_t d_v, int dtype, int grad_dtype, float* d_o,
                               float* dweight, void* workspace, size_t workspace_bytes, void* stream);
 
+/* The two ends of a language model built from these layers (the paper's backbone: one table
+ * [vocab, width] that embeds the tokens, scaled by sqrt(width), and, tied, makes the logits, held
+ * within a soft cap of 30).  In the calls below
+ *   - `token` and `target` are int32 (token_bytes 4) or int64 (token_bytes 8) [rows]; a number
+ *     outside [0, vocab) stands for no token (padding, a target that does not count);
+ *   - the rows of table, h, dy and of the outputs out, dtable and dh lie `*_stride` elements apart
+ *     (>= width), on memory aligned to their elements.  Rows of a multiple of 8 (cross entropy:
+ *     64) channels on 16-byte boundaries are moved fastest; others cost a copy or narrower accesses;
+ *   - rows <= 2^24, width <= 2^16, vocab < 2^31 - 1024, and no array of 2^40 elements
+ *     (MESA_ERR_SHAPE otherwise, as for a launch of 2^32 threads or more);
+ *   - outputs and workspaces must overlap neither an input nor each other (MESA_ERR_ARG; slices of
+ *     one array with the same stride may interleave); workspaces are 16-byte aligned and hold at
+ *     least what the call's *_workspace_bytes says;
+ *   - sums are fp32 and in a fixed order: the same inputs give the same bits.
+ *
+ * mesa_embedding: out_n = scale E[token_n], a row of zeros where there is no token; dtype is the
+ *   table's, out_dtype out's (MESA_DTYPE_F32, MESA_DTYPE_BF16).  One kernel launch; rows 0 is a no-op.
+ * mesa_embedding_backward: dE_v = scale sum over n with token_n = v of dy_n (zeros where there is
+ *   none), added in the order of n; with `accumulate` not 0 it is added to what dtable holds
+ *   (rows of tokens that do not occur are then not touched).  dy of grad_dtype, dtable of
+ *   table_dtype.  Rows of dy that have no token are not read.  Three kernel launches up to 2048 rows,
+ *   else six or eight (more from a vocabulary of 2^18 on). */
+int mesa_embedding(const void* table, const void* token, int token_bytes, float scale, int64_t rows, int64_t vocab,
+                   int64_t width, int64_t table_stride, int dtype, int out_dtype, int64_t out_stride, void* out,
+                   void* stream);
+size_t mesa_embedding_backward_workspace_bytes(int64_t rows, int64_t vocab, int64_t width);
+int mesa_embedding_backward(const void* token, int token_bytes, const void* dy, float scale, int64_t rows,
+                            int64_t vocab, int64_t width, int64_t dy_stride, int grad_dtype, int table_dtype,
+                            int64_t dtable_stride, int accumulate, void* dtable, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
+/* Softmax cross entropy of h [rows, width] against the table's rows, without keeping the logits:
+ *     z_nv = h_n . E_v,  l = cap tanh(z / cap) (cap 0: l = z),  lse_n = log sum_v exp(l_nv)
+ *     loss_n = lse_n - l_n,target  (0 where the target does not count)
+ *     best_n = the lowest v whose z_nv is the largest (-1 where every one is a NaN)
+ *   h, table   dtype (MESA_DTYPE_F32, MESA_DTYPE_BF16): products of bf16 are exact, those of fp32 are formed
+ *              from three bf16 parts of each factor (24 bits); both are summed in fp32
+ *   target, loss [rows] fp32: both or neither (then only lse and best are computed)
+ *   lse [rows] fp32;  best int32 [rows], or NULL
+ *   cap        finite and >= 0
+ * rows 0 is a no-op; vocab and width must be positive.  Two kernel launches, and one or two more for
+ * each 64 MiB of a table that has to be copied (fp32, or spaced or aligned otherwise).
+ *
+ * mesa_cross_entropy_backward: gradients for a given dloss [rows] fp32 and the lse of the forward
+ *     dz_nv = dloss_n (exp(l_nv - lse_n) - [v = target_n]) (1 - (l_nv / cap)^2), 0 where the target does not count
+ *     dh_n = sum_v dz_nv E_v,  dE_v = sum_n dz_nv h_n
+ *   dh [rows, width], dtable [vocab, width]: dtype; either may be NULL.  Rows of h, lse and dloss
+ *   whose target does not count may hold anything.  dz, formed a piece of the vocabulary at a time
+ *   (the workspace holds at most 256 MiB of it, or 256 columns), is rounded to bf16 for bf16 inputs.  With rows 0
+ *   dtable is zeros.  Up to five kernel launches a piece, and a few more. */
+size_t mesa_cross_entropy_workspace_bytes(int64_t rows, int64_t vocab, int64_t width, int dtype);
+int mesa_cross_entropy(const void* h, const void* table, const void* target, int token_bytes, float cap, int64_t rows,
+                       int64_t vocab, int64_t width, int64_t h_stride, int64_t table_stride, int dtype, float* loss,
+                       float* lse, int32_t* best, void* workspace, size_t workspace_bytes, void* stream);
+size_t mesa_cross_entropy_backward_workspace_bytes(int64_t rows, int64_t vocab, int64_t width, int dtype);
+int mesa_cross_entropy_backward(const void* h, const void* table, const void* target, int token_bytes,
+                                const float* lse, const float* dloss, float cap, int64_t rows, int64_t vocab,
+                                int64_t width, int64_t h_stride, int64_t table_stride, int dtype, int64_t dh_stride,
+                                int64_t dtable_stride, void* dh, void* dtable, void* workspace,
+                                size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

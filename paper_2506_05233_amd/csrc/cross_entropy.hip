@@ -1,0 +1,844 @@
+// Softmax cross entropy over a vocabulary with a soft cap on the logits, and its gradient, without
+// ever keeping the logits of all rows and the whole vocabulary:
+//     z = h . E_v,  l = cap tanh(z / cap),  lse = log sum_v exp(l),  loss = lse - l_target
+//     dz = dloss (exp(l - lse) - [v = target]) (1 - (l / cap)^2),  dh = sum_v dz E_v,  dE_v = sum_n dz h_n
+//
+// Three matrix products (2 rows vocab width operations each; the logits' one twice, since they are
+// formed again for the gradient), on the bf16 matrix cores (bf16_product.hpp).
+#include <algorithm>
+
+#include "bf16_product.hpp"
+#include "mesa_kernels.hpp"
+#include "mesa_lanes.hpp"
+#include "vocab.hpp"
+
+namespace mesa {
+namespace {
+
+constexpr float kInf = __builtin_inff();
+
+using Wide = TileShape<256, 256, 2, 4>;
+using Middle = TileShape<128, 128, 2, 2>;
+using Narrow = TileShape<64, 64, 2, 2>;      // tokens are the second size
+using Thin = TileShape<64, 32, 4, 1>;
+
+int64_t ceil_to(int64_t x, int64_t n) { return (x + n - 1) / n * n; }
+int64_t ceil_div(int64_t x, int64_t n) { return (x + n - 1) / n; }
+
+// ------------------------------------------------------------------ operands in bf16 planes
+constexpr int kPackThreads = 256;
+
+struct PackArgs {
+    const void* x;           // [rows] rows of width, stride apart
+    int64_t rows, width, stride;
+    Tokens targets;          // p null: every row counts; else rows whose target is none come out as zeros
+    int64_t vocab;
+    uint16_t* out;           // planes of [out_rows, ld]
+    int64_t out_rows, ld, plane;
+    uint16_t* zeros;         // kZeroBytes of zeros, or null
+};
+constexpr int64_t kZeroBytes = 256;
+
+// The three parts of an fp32 value, whose sum it is: each the nearest bf16 to what the parts before
+// leave, which are exact differences (the first cut off where the nearest would be an infinity).  The
+// products of parts that are left out are below 2^-25 of the whole.  An infinity or a NaN stays in the
+// first part alone.
+__device__ __forceinline__ void three_parts(float x, uint32_t (&p)[3])
+{
+    const bool finite = (__float_as_uint(x) & 0x7F800000u) != 0x7F800000u;
+    p[0] = pack_bf16(x, 0.0f);
+    if (finite && (p[0] & 0x7F80u) == 0x7F80u) p[0] = __float_as_uint(x) >> 16;
+    const float a = finite ? x - __uint_as_float(p[0] << 16) : 0.0f;
+    p[1] = pack_bf16(a, 0.0f);
+    p[2] = pack_bf16(a - __uint_as_float(p[1] << 16), 0.0f);
+}
+
+// Eight consecutive channels a thread, out_rows x ld of them; what x does not hold is zero.
+template <typename T>
+__global__ void __launch_bounds__(kPackThreads) pack_planes_kernel(PackArgs a)
+{
+    const int64_t i = int64_t(blockIdx.x) * kPackThreads + threadIdx.x;
+    const int64_t per = a.ld / 8;
+    if (a.zeros != nullptr && i < kZeroBytes / 16) reinterpret_cast<uint4*>(a.zeros)[i] = make_uint4(0, 0, 0, 0);
+    if (i >= a.out_rows * per) return;
+    const int64_t row = i / per, c = i % per * 8;
+    float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    bool counts = row < a.rows;
+    if (counts && a.targets.p != nullptr) {
+        const int64_t t = token_at(a.targets, row);
+        counts = t >= 0 && t < a.vocab;
+    }
+    if (counts) {
+        const T* src = static_cast<const T*>(a.x) + row * a.stride + c;
+        if (c + 8 <= a.width && uintptr_t(src) % 16 == 0) {
+            float lo[4], hi[4];
+            Lane4<T>::widen(Lane4<T>::template load<true>(src, 0, 4), lo);
+            Lane4<T>::widen(Lane4<T>::template load<true>(src, 4, 4), hi);
+#pragma unroll
+            for (int v = 0; v < 4; ++v) x[v] = lo[v], x[v + 4] = hi[v];
+        } else {
+#pragma unroll
+            for (int v = 0; v < 8; ++v)
+                if (c + v < a.width) x[v] = to_f32(src[v]);
+        }
+    }
+    uint16_t* dst = a.out + row * a.ld + c;
+    if constexpr (sizeof(T) == 2) {
+        uint32_t w[4];
+#pragma unroll
+        for (int v = 0; v < 4; ++v) w[v] = __float_as_uint(x[2 * v]) >> 16 | (__float_as_uint(x[2 * v + 1]) & 0xFFFF0000u);
+        *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
+    } else {
+        uint32_t w[3][4];
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            uint32_t p[3], q[3];
+            three_parts(x[2 * v], p);
+            three_parts(x[2 * v + 1], q);
+#pragma unroll
+            for (int k = 0; k < 3; ++k) w[k][v] = p[k] | q[k] << 16;
+        }
+#pragma unroll
+        for (int k = 0; k < 3; ++k) *reinterpret_cast<uint4*>(dst + k * a.plane) = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
+    }
+}
+
+hipError_t pack_planes(const PackArgs& a, int dtype, hipStream_t stream)
+{
+    const int64_t blocks = ceil_div(a.out_rows * (a.ld / 8), kPackThreads);
+    if (!grid_fits(blocks, kPackThreads)) return hipErrorInvalidConfiguration;
+    if (dtype == kBf16)
+        hipLaunchKernelGGL((pack_planes_kernel<bf16_t>), dim3(unsigned(blocks)), dim3(kPackThreads), 0, stream, a);
+    else
+        hipLaunchKernelGGL((pack_planes_kernel<float>), dim3(unsigned(blocks)), dim3(kPackThreads), 0, stream, a);
+    return hipGetLastError();
+}
+
+// ------------------------------------------------------------------ the logits
+// tanh(x) and 1 - tanh(x)^2, each to fp32 accuracy relative to itself: with e = exp(-2 |x|) they are
+// (1 - e) / (1 + e) and 4 e / (1 + e)^2; near 0, where 1 - e cancels, the series of tanh.
+__device__ __forceinline__ float tanh_of(float x, float& slope)
+{
+    const float y = fabsf(x), e = __builtin_amdgcn_exp2f(-2.0f * kLog2e * y), q = __builtin_amdgcn_rcpf(1.0f + e);
+    slope = 4.0f * e * q * q;
+    const float s = x * x;
+    const float series = y * fmaf(s, fmaf(s, fmaf(s, fmaf(s, 62.0f / 2835.0f, -17.0f / 315.0f), 2.0f / 15.0f), -1.0f / 3.0f), 1.0f);
+    return copysignf(y < 0.3f ? series : (1.0f - e) * q, x);
+}
+
+// max over the four 16-lane rows: every lane receives that of its column position
+__device__ __forceinline__ float row_pair_max(float v)
+{
+    const auto s16 = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fmaxf(__uint_as_float(s16[0]), __uint_as_float(s16[1]));
+    const auto s32 = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(s32[0]), __uint_as_float(s32[1]));
+}
+__device__ __forceinline__ int row_pair_min(int v)
+{
+    const auto s16 = __builtin_amdgcn_permlane16_swap(uint32_t(v), uint32_t(v), false, false);
+    v = min(int(s16[0]), int(s16[1]));
+    const auto s32 = __builtin_amdgcn_permlane32_swap(uint32_t(v), uint32_t(v), false, false);
+    return min(int(s32[0]), int(s32[1]));
+}
+
+struct LogitsArgs {
+    Matrix table, h;          // from the piece's first row of the table on
+    int pairs;
+    int64_t steps;            // of 64 channels
+    int64_t first, vocab;     // the piece's first row; rows of the whole table
+    int64_t piece;            // rows of the piece
+    int64_t rows;
+    int64_t tiles_m, tiles_n;
+    Tokens targets;
+    float cap;
+    // forward: of each tile of the vocabulary, [tile][row]
+    float2* part;             // largest logit, sum of exp(logit - that)
+    float* best_z;            // largest product and the lowest v that has it, or null
+    int32_t* best_v;
+    int64_t tile0;            // the piece's first tile
+    float* at;                // [rows]: the target's logit
+    // gradient
+    const float* lse;
+    const float* dloss;
+    uint16_t* dz;             // planes of [row][piece], dz_ld elements a row
+    int64_t dz_ld, dz_plane, dz_rows;
+};
+
+// One tile of the vocabulary against one of the rows; of every row the tile's largest logit and its
+// sum of exponentials to that, which the next kernel joins over the tiles.
+template <class S>
+__global__ void __launch_bounds__(S::kThreads) logits_kernel(LogitsArgs a)
+{
+    __shared__ __attribute__((aligned(16))) uint16_t lds[S::kLds];
+    int64_t tm, tn;
+    tile_of(a.tiles_m, a.tiles_n, tm, tn);
+    const int64_t m0 = tm * S::M, n0 = tn * S::N;
+    f32x4 acc[S::MT][S::NT];
+    Product<S, true, true>::run(a.table, m0, a.h, n0, 0, a.steps * kStepK, a.pairs, nullptr, lds, acc);
+
+    const int lane = int(threadIdx.x) % kWave, g = lane / 16, n = lane % 16;
+    const int wave = int(threadIdx.x) / kWave, wm = wave / S::WN, wn = wave % S::WN;
+    const int64_t v0 = a.first + m0 + wm * S::MT * 16;      // the wave's first row of the table
+    const int here = int(min(a.first + a.piece - v0, int64_t(S::MT * 16)));     // its rows that exist (0 or less: none)
+    float* red_m = reinterpret_cast<float*>(lds);           // [WM][N]
+    float* red_s = red_m + S::WM * S::N;
+    float* red_z = red_s + S::WM * S::N;
+    int* red_v = reinterpret_cast<int*>(red_z + S::WM * S::N);
+
+    if (a.best_z != nullptr) {
+#pragma unroll
+        for (int j = 0; j < S::NT; ++j) {
+            float top = -kInf;
+#pragma unroll
+            for (int i = 0; i < S::MT; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) top = fmaxf(top, 16 * i + 4 * g + r < here ? acc[i][j][r] : -kInf);
+            top = row_pair_max(top);
+            int who = INT32_MAX;
+#pragma unroll
+            for (int i = 0; i < S::MT; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int v = 16 * i + 4 * g + r;
+                    if (v < here && acc[i][j][r] == top) who = min(who, v);
+                }
+            who = row_pair_min(who);
+            if (g == 0) {
+                red_z[wm * S::N + (wn * S::NT + j) * 16 + n] = top;
+                red_v[wm * S::N + (wn * S::NT + j) * 16 + n] = who == INT32_MAX ? who : int(v0) + who;
+            }
+        }
+    }
+    if (a.cap > 0.0f) {
+        const float inv = 1.0f / a.cap;
+        float slope;
+#pragma unroll
+        for (int i = 0; i < S::MT; ++i)
+#pragma unroll
+            for (int j = 0; j < S::NT; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) acc[i][j][r] = a.cap * tanh_of(acc[i][j][r] * inv, slope);
+    }
+#pragma unroll
+    for (int j = 0; j < S::NT; ++j) {
+        const int64_t row = n0 + (wn * S::NT + j) * 16 + n;
+        if (a.at != nullptr) {
+            const int64_t t = row < a.rows ? token_at(a.targets, row) - v0 : -1;
+            if (__any(t >= 0 && t < here)) {
+#pragma unroll
+                for (int i = 0; i < S::MT; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (16 * i + 4 * g + r == t && t < here) a.at[row] = acc[i][j][r];
+            }
+        }
+        float top = -kInf;
+        if (here < S::MT * 16) {
+#pragma unroll
+            for (int i = 0; i < S::MT; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (16 * i + 4 * g + r >= here) acc[i][j][r] = -kInf;
+        }
+#pragma unroll
+        for (int i = 0; i < S::MT; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) top = fmaxf(top, acc[i][j][r]);
+        top = row_pair_max(top);
+        // where every logit is -infinity (or there is none) the sum is 0, whatever they are taken to
+        const float base = top == -kInf ? 0.0f : top;
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < S::MT; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) sum += __builtin_amdgcn_exp2f((acc[i][j][r] - base) * kLog2e);
+        sum = row_pair_sums(sum);
+        if (g == 0) {
+            red_m[wm * S::N + (wn * S::NT + j) * 16 + n] = top;
+            red_s[wm * S::N + (wn * S::NT + j) * 16 + n] = sum;
+        }
+    }
+    __syncthreads();
+    const int t = int(threadIdx.x);
+    if (t < S::N && n0 + t < a.rows) {
+        float top = red_m[t];
+#pragma unroll
+        for (int w = 1; w < S::WM; ++w) top = fmaxf(top, red_m[w * S::N + t]);
+        float sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < S::WM; ++w) {
+            const float m = red_m[w * S::N + t];
+            sum += red_s[w * S::N + t] * (m == top ? 1.0f : __builtin_amdgcn_exp2f((m - top) * kLog2e));
+        }
+        const int64_t to = (a.tile0 + tm) * a.rows + n0 + t;
+        a.part[to] = make_float2(top, sum);
+        if (a.best_z != nullptr) {
+            float z = red_z[t];
+            int v = red_v[t];
+#pragma unroll
+            for (int w = 1; w < S::WM; ++w) {
+                const float zw = red_z[w * S::N + t];
+                const int vw = red_v[w * S::N + t];
+                if (zw > z || (zw == z && vw < v)) z = zw, v = vw;
+            }
+            a.best_z[to] = z;
+            a.best_v[to] = v;
+        }
+    }
+}
+
+// The tiles' sums joined: 16 rows a workgroup, 16 threads for the tiles of each.
+struct JoinArgs {
+    const float2* part;
+    const float* best_z;
+    const int32_t* best_v;
+    const float* at;
+    Tokens targets;
+    int64_t rows, vocab, tiles;
+    float* loss;
+    float* lse;
+    int32_t* best;
+};
+constexpr int kJoinRows = 16, kJoinSlices = 16;
+
+__global__ void __launch_bounds__(kJoinRows* kJoinSlices) join_kernel(JoinArgs a)
+{
+    __shared__ float2 red[kJoinSlices][kJoinRows];
+    __shared__ float red_z[kJoinSlices][kJoinRows];
+    __shared__ int red_v[kJoinSlices][kJoinRows];
+    const int r = int(threadIdx.x) % kJoinRows, slice = int(threadIdx.x) / kJoinRows;
+    const int64_t row = int64_t(blockIdx.x) * kJoinRows + r;
+    float top = -kInf, sum = 0.0f, z = -kInf;
+    int v = INT32_MAX;
+    auto add = [&](float2 p) {
+        const float m = fmaxf(top, p.x);
+        if (m == -kInf) {
+            sum += p.y;
+            return;
+        }
+        sum = sum * (top == m ? 1.0f : __builtin_amdgcn_exp2f((top - m) * kLog2e)) +
+              p.y * (p.x == m ? 1.0f : __builtin_amdgcn_exp2f((p.x - m) * kLog2e));
+        top = m;
+    };
+    if (row < a.rows) {
+#pragma unroll 4
+        for (int64_t t = slice; t < a.tiles; t += kJoinSlices) {
+            add(a.part[t * a.rows + row]);
+            if (a.best != nullptr) {
+                const float zt = a.best_z[t * a.rows + row];
+                const int vt = a.best_v[t * a.rows + row];
+                if (zt > z || (zt == z && vt < v)) z = zt, v = vt;
+            }
+        }
+    }
+    red[slice][r] = make_float2(top, sum);
+    red_z[slice][r] = z;
+    red_v[slice][r] = v;
+    __syncthreads();
+    if (slice != 0 || row >= a.rows) return;
+#pragma unroll
+    for (int s = 1; s < kJoinSlices; ++s) {
+        add(red[s][r]);
+        if (red_z[s][r] > z || (red_z[s][r] == z && red_v[s][r] < v)) z = red_z[s][r], v = red_v[s][r];
+    }
+    const float lse = top + kLn2 * __builtin_amdgcn_logf(sum);
+    a.lse[row] = lse;
+    if (a.loss != nullptr) {
+        const int64_t t = token_at(a.targets, row);
+        a.loss[row] = t >= 0 && t < a.vocab ? lse - a.at[row] : 0.0f;
+    }
+    if (a.best != nullptr) a.best[row] = v == INT32_MAX ? -1 : v;
+}
+
+// ------------------------------------------------------------------ the gradient
+// The logits of one tile again, and from them dz in bf16 (three planes of it for fp32 operands).
+template <class S>
+__global__ void __launch_bounds__(S::kThreads) logits_grad_kernel(LogitsArgs a)
+{
+    __shared__ __attribute__((aligned(16))) uint16_t lds[S::kLds];
+    int64_t tm, tn;
+    tile_of(a.tiles_m, a.tiles_n, tm, tn);
+    const int64_t m0 = tm * S::M, n0 = tn * S::N;
+    f32x4 acc[S::MT][S::NT];
+    Product<S, true, true>::run(a.table, m0, a.h, n0, 0, a.steps * kStepK, a.pairs, nullptr, lds, acc);
+
+    const int lane = int(threadIdx.x) % kWave, g = lane / 16, n = lane % 16;
+    const int wave = int(threadIdx.x) / kWave, wm = wave / S::WN, wn = wave % S::WN;
+    const int64_t c0 = m0 + wm * S::MT * 16;                // the wave's first column of dz
+    const int here = int(min(a.piece - c0, int64_t(S::MT * 16)));
+    const float inv = a.cap > 0.0f ? 1.0f / a.cap : 0.0f;
+#pragma unroll
+    for (int j = 0; j < S::NT; ++j) {
+        const int64_t row = n0 + (wn * S::NT + j) * 16 + n;
+        int64_t t = -1;
+        float lse = 0.0f, up = 0.0f;
+        if (row < a.rows) {
+            t = token_at(a.targets, row);
+            lse = a.lse[row];
+            up = a.dloss[row];
+        }
+        const bool counts = t >= 0 && t < a.vocab;
+        const int mine = counts ? int(max(min(t - a.first - c0, int64_t(INT32_MAX)), int64_t(-1))) : -1;
+        if (row >= a.dz_rows) continue;
+        uint16_t* dst = a.dz + row * a.dz_ld + c0;
+#pragma unroll
+        for (int i = 0; i < S::MT; ++i) {
+            float d[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int v = 16 * i + 4 * g + r;
+                float l = acc[i][j][r], slope = 1.0f;
+                if (a.cap > 0.0f) l = a.cap * tanh_of(l * inv, slope);
+                const float p = __builtin_amdgcn_exp2f((l - lse) * kLog2e);
+                d[r] = (v == mine ? p - 1.0f : p) * slope * up;
+                if (!counts || v >= here) d[r] = 0.0f;
+            }
+            // rounded to bf16 once for both products: 2^-8 of an element at most, at random over the sums
+            if (a.pairs == 1) {
+                *reinterpret_cast<uint2*>(dst + 16 * i + 4 * g) = make_uint2(pack_bf16(d[0], d[1]), pack_bf16(d[2], d[3]));
+            } else {
+                uint32_t p[4][3];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) three_parts(d[r], p[r]);
+#pragma unroll
+                for (int k = 0; k < 3; ++k)
+                    *reinterpret_cast<uint2*>(dst + k * a.dz_plane + 16 * i + 4 * g) =
+                        make_uint2(p[0][k] | p[1][k] << 16, p[2][k] | p[3][k] << 16);
+            }
+        }
+    }
+}
+
+// out[n][m] = sum_k A(m, k) B(n, k): m a channel, n a row of dh or of the table's gradient.
+struct GradArgs {
+    Matrix a, b;
+    int pairs;
+    int64_t k, k_split;       // k of one launch layer, a multiple of 64 (blockIdx.y of them)
+    const void* zeros;
+    int64_t tiles_m, tiles_n;
+    int64_t width, n;         // of the result
+    // fp32 sums on the way: [layer][n][slab_ld], written (first) or added to; null: none
+    float* slab;
+    int64_t slab_ld, slab_layer;
+    bool first;
+    // the result, or null (then the slab is written): rows out_stride apart; rows whose target is
+    // none are 0 (targets.p null: every row counts)
+    void* out;
+    int64_t out_stride;
+    Tokens targets;
+    int64_t vocab;
+};
+
+template <typename T>
+__device__ __forceinline__ void put4(T* p, int n, bool wide, const f32x4& y)
+{
+    const float x[4] = {y[0], y[1], y[2], y[3]};
+    if (wide)
+        Lane4<T>::template store<true>(p, 0, n, x);
+    else
+        Lane4<T>::template store<false>(p, 0, n, x);
+}
+
+template <class S, bool AlongB, typename T>
+__global__ void __launch_bounds__(S::kThreads) grad_kernel(GradArgs a)
+{
+    __shared__ __attribute__((aligned(16))) uint16_t lds[S::kLds];
+    int64_t tm, tn;
+    tile_of(a.tiles_m, a.tiles_n, tm, tn);
+    const int64_t m0 = tm * S::M, n0 = tn * S::N, k0 = int64_t(blockIdx.y) * a.k_split;
+    f32x4 acc[S::MT][S::NT];
+    Product<S, false, AlongB>::run(a.a, m0, a.b, n0, k0, min(k0 + a.k_split, a.k), a.pairs, a.zeros, lds, acc);
+
+    const int lane = int(threadIdx.x) % kWave, g = lane / 16, n = lane % 16;
+    const int wave = int(threadIdx.x) / kWave, wm = wave / S::WN, wn = wave % S::WN;
+    // four channels in one access: the rows' pitch and the base allow it (the slab's always do)
+    const bool wide = a.out != nullptr && (a.out_stride * int64_t(sizeof(T))) % (4 * sizeof(T)) == 0 && uintptr_t(a.out) % (4 * sizeof(T)) == 0;
+    float* slab = a.slab == nullptr ? nullptr : a.slab + int64_t(blockIdx.y) * a.slab_layer;
+#pragma unroll
+    for (int j = 0; j < S::NT; ++j) {
+        const int64_t row = n0 + (wn * S::NT + j) * 16 + n;
+        if (row >= a.n) continue;
+        bool counts = true;
+        if (a.out != nullptr && a.targets.p != nullptr) {
+            const int64_t t = token_at(a.targets, row);
+            counts = t >= 0 && t < a.vocab;
+        }
+#pragma unroll
+        for (int i = 0; i < S::MT; ++i) {
+            const int64_t m = m0 + (wm * S::MT + i) * 16 + 4 * g;
+            if (m >= a.width) continue;
+            f32x4 y = acc[i][j];
+            float* s = slab + row * a.slab_ld + m;
+            if (slab != nullptr && !a.first) y += *reinterpret_cast<const f32x4*>(s);
+            if (a.out == nullptr) {
+                *reinterpret_cast<f32x4*>(s) = y;
+            } else {
+                if (!counts) y = f32x4{0.f, 0.f, 0.f, 0.f};
+                const int left = int(min(a.width - m, int64_t(4)));
+                put4(static_cast<T*>(a.out) + row * a.out_stride + m, left, wide && left == 4, y);
+            }
+        }
+    }
+}
+
+// The layers of a slab added in order.
+struct SumArgs {
+    const float* slab;
+    int64_t slab_ld, slab_layer, layers;
+    int64_t n, width;
+    void* out;
+    int64_t out_stride;
+    Tokens targets;
+    int64_t vocab;
+};
+constexpr int kSumThreads = 256;
+
+template <typename T>
+__global__ void __launch_bounds__(kSumThreads) layer_sum_kernel(SumArgs a)
+{
+    const int64_t per = a.slab_ld / 4, i = int64_t(blockIdx.x) * kSumThreads + threadIdx.x;
+    if (i >= a.n * per) return;
+    const int64_t row = i / per, m = i % per * 4;
+    if (m >= a.width) return;
+    f32x4 y = {0.f, 0.f, 0.f, 0.f};
+    bool counts = true;
+    if (a.targets.p != nullptr) {
+        const int64_t t = token_at(a.targets, row);
+        counts = t >= 0 && t < a.vocab;
+    }
+    if (counts) {
+        const float* s = a.slab + row * a.slab_ld + m;
+#pragma unroll 4
+        for (int64_t l = 0; l < a.layers; ++l) y += *reinterpret_cast<const f32x4*>(s + l * a.slab_layer);
+    }
+    T* p = static_cast<T*>(a.out) + row * a.out_stride + m;
+    const int left = int(min(a.width - m, int64_t(4)));
+    put4(p, left, left == 4 && uintptr_t(p) % (4 * sizeof(T)) == 0, y);
+}
+
+// ------------------------------------------------------------------ plans
+// Which tile a product of m by n takes: the largest that still gives every compute unit work.
+enum Shape { kWideShape, kMiddleShape, kNarrowShape, kThinShape };
+constexpr int64_t kShapeM[] = {Wide::M, Middle::M, Narrow::M, Thin::M}, kShapeN[] = {Wide::N, Middle::N, Narrow::N, Thin::N};
+
+Shape shape_of(int64_t m, int64_t n, int64_t layers)
+{
+    if (n <= 32) return kThinShape;
+    if (n <= 64) return kNarrowShape;
+    if (ceil_div(m, 256) * ceil_div(n, 256) * layers >= 224) return kWideShape;
+    return ceil_div(m, 128) * ceil_div(n, 128) * layers >= 192 ? kMiddleShape : kNarrowShape;
+}
+
+template <typename F>
+hipError_t with_shape(Shape s, F f)
+{
+    switch (s) {
+        case kWideShape: return f(Wide{});
+        case kMiddleShape: return f(Middle{});
+        case kNarrowShape: return f(Narrow{});
+        default: return f(Thin{});
+    }
+}
+
+// A table or h that the products read where it lies: bf16 rows of whole steps in 16-byte pieces.
+bool direct(const void* p, int64_t stride, int64_t width, int dtype)
+{
+    return dtype == kBf16 && width % kStepK == 0 && stride % 8 == 0 && stride < (int64_t(1) << 22) && uintptr_t(p) % 16 == 0;
+}
+
+constexpr int64_t kCopyBytes = int64_t(64) << 20;      // of the table's rows in bf16 planes at a time, forward
+constexpr int64_t kPieceBytes = int64_t(256) << 20;    // of dz at a time
+constexpr int64_t kSlabBytes = int64_t(256) << 20;     // of fp32 layers of one product, at most (or one layer)
+
+constexpr int64_t kUnits = 256;                        // compute units of the card
+
+int planes_of(int dtype) { return dtype == kBf16 ? 1 : 3; }
+
+// Rows of the table in a piece of the forward, where it has to be copied.
+int64_t copy_rows(int64_t vocab, int64_t width, int dtype)
+{
+    const int64_t row = ceil_to(width, kStepK) * 2 * planes_of(dtype);
+    return std::min(ceil_to(vocab, 256), std::max<int64_t>(256, kCopyBytes / row / 256 * 256));
+}
+
+struct Carve {      // the workspace, piece after piece of 256 bytes
+    int64_t at = 0;
+    int64_t take(int64_t bytes)
+    {
+        const int64_t p = at;
+        at += ceil_to(bytes, 256);
+        return p;
+    }
+};
+
+struct ForwardPlan {
+    int64_t part, best_z, best_v, at, h, table, bytes, tiles;
+    ForwardPlan(int64_t rows, int64_t vocab, int64_t width, int dtype)
+    {
+        // whether the table is copied hangs on its address, so there is room for either way's tiles
+        const int64_t copied = copy_rows(vocab, width, dtype);
+        tiles = std::max(ceil_div(vocab, kShapeM[shape_of(vocab, rows, 1)]), ceil_div(vocab, kShapeM[shape_of(copied, rows, 1)]));
+        Carve c;
+        const int64_t row = ceil_to(width, kStepK) * 2 * planes_of(dtype);
+        part = c.take(tiles * rows * 8);
+        best_z = c.take(tiles * rows * 4);
+        best_v = c.take(tiles * rows * 4);
+        at = c.take(rows * 4);
+        h = c.take(rows * row);
+        table = c.take(copied * row);
+        bytes = c.at;
+    }
+};
+
+struct GradPlan {
+    int64_t piece, dz, dz_rows, dz_ld, h, table, zeros, slab_h, slab_e, bytes, ld;
+    int64_t h_layers, e_layers;
+    Shape logits, dh, de;
+    GradPlan(int64_t rows, int64_t vocab, int64_t width, int dtype)
+    {
+        const int64_t planes = planes_of(dtype);
+        ld = ceil_to(width, kStepK);
+        dz_rows = ceil_to(rows, 64);
+        piece = std::min(ceil_to(vocab, 256), std::max<int64_t>(256, kPieceBytes / (dz_rows * 2 * planes) / 256 * 256));
+        // pieces of about the same size
+        piece = ceil_to(ceil_div(vocab, ceil_div(vocab, piece)), 256);
+        dz_ld = piece;
+        logits = shape_of(piece, rows, 1);
+        h_layers = layers(width, rows, piece, dh);
+        e_layers = layers(width, piece, rows, de);
+        Carve c;
+        zeros = c.take(kZeroBytes);
+        h = c.take(dz_rows * ld * 2 * planes);
+        table = c.take(piece * ld * 2 * planes);
+        dz = c.take(dz_rows * dz_ld * 2 * planes);
+        slab_h = h_layers > 1 || piece < vocab ? c.take(h_layers * rows * ld * 4) : 0;
+        slab_e = e_layers > 1 ? c.take(e_layers * piece * ld * 4) : 0;
+        bytes = c.at;
+    }
+    // Into how many layers of k a product of m by n is cut: enough for two workgroups a compute unit,
+    // each of at least eight steps.
+    static int64_t layers(int64_t m, int64_t n, int64_t k, Shape& shape)
+    {
+        const int64_t most = std::max<int64_t>(1, std::min(ceil_div(k, kStepK) / 8, kSlabBytes / (ceil_to(m, kStepK) * n * 4)));
+        shape = shape_of(m, n, most);
+        const int64_t tiles = ceil_div(m, kShapeM[shape]) * ceil_div(n, kShapeN[shape]);
+        return std::min(most, std::max<int64_t>(1, 2 * kUnits / tiles));
+    }
+};
+
+}  // namespace
+
+int64_t cross_entropy_bytes(int64_t rows, int64_t vocab, int64_t width, int dtype) { return ForwardPlan(rows, vocab, width, dtype).bytes; }
+
+int64_t cross_entropy_grad_bytes(int64_t rows, int64_t vocab, int64_t width, int dtype)
+{
+    return GradPlan(rows, vocab, width, dtype).bytes;
+}
+
+hipError_t launch_cross_entropy(const CrossEntropyArgs& a, hipStream_t stream)
+{
+    const ForwardPlan plan(a.rows, a.vocab, a.width, a.dtype);
+    const int planes = planes_of(a.dtype);
+    const int64_t ld = ceil_to(a.width, kStepK);
+    LogitsArgs k{};
+    k.pairs = planes == 1 ? 1 : 6;
+    k.steps = ld / kStepK;
+    k.vocab = a.vocab;
+    k.rows = a.rows;
+    k.targets = a.targets;
+    k.cap = a.cap;
+    k.part = reinterpret_cast<float2*>(a.workspace + plan.part);
+    k.best_z = a.best == nullptr ? nullptr : reinterpret_cast<float*>(a.workspace + plan.best_z);
+    k.best_v = reinterpret_cast<int32_t*>(a.workspace + plan.best_v);
+    k.at = a.targets.p == nullptr ? nullptr : reinterpret_cast<float*>(a.workspace + plan.at);
+    if (direct(a.h, a.h_stride, a.width, a.dtype)) {
+        k.h = Matrix{static_cast<const uint16_t*>(a.h), a.h_stride, 0, a.rows, a.width};
+    } else {
+        uint16_t* copy = reinterpret_cast<uint16_t*>(a.workspace + plan.h);
+        k.h = Matrix{copy, ld, a.rows * ld, a.rows, ld};
+        const PackArgs p{a.h, a.rows, a.width, a.h_stride, Tokens{}, 0, copy, a.rows, ld, a.rows * ld, nullptr};
+        if (hipError_t e = pack_planes(p, a.dtype, stream); e != hipSuccess) return e;
+    }
+    const bool as_is = direct(a.table, a.table_stride, a.width, a.dtype);
+    const int64_t most = as_is ? a.vocab : copy_rows(a.vocab, a.width, a.dtype);
+    const Shape shape = shape_of(most, a.rows, 1);
+    k.tiles_n = ceil_div(a.rows, kShapeN[shape]);
+    for (int64_t first = 0; first < a.vocab; first += most) {
+        k.first = first;
+        k.piece = std::min(most, a.vocab - first);
+        k.tile0 = first / kShapeM[shape];
+        k.tiles_m = ceil_div(k.piece, kShapeM[shape]);
+        if (as_is) {
+            k.table = Matrix{static_cast<const uint16_t*>(a.table), a.table_stride, 0, a.vocab, a.width};
+        } else {
+            uint16_t* copy = reinterpret_cast<uint16_t*>(a.workspace + plan.table);
+            k.table = Matrix{copy, ld, most * ld, k.piece, ld};
+            const char* src = static_cast<const char*>(a.table) + first * a.table_stride * (planes == 1 ? 2 : 4);
+            const PackArgs p{src, k.piece, a.width, a.table_stride, Tokens{}, 0, copy, k.piece, ld, most * ld, nullptr};
+            if (hipError_t e = pack_planes(p, a.dtype, stream); e != hipSuccess) return e;
+        }
+        const hipError_t e = with_shape(shape, [&](auto s) {
+            using S = decltype(s);
+            if (!grid_fits(k.tiles_m * k.tiles_n, S::kThreads)) return hipErrorInvalidConfiguration;
+            hipLaunchKernelGGL((logits_kernel<S>), dim3(unsigned(k.tiles_m * k.tiles_n)), dim3(S::kThreads), 0, stream, k);
+            return hipGetLastError();
+        });
+        if (e != hipSuccess) return e;
+    }
+    const JoinArgs j{k.part, k.best_z, k.best_v, k.at, a.targets, a.rows, a.vocab,
+                     ceil_div(a.vocab, kShapeM[shape]), a.targets.p == nullptr ? nullptr : a.loss, a.lse, a.best};
+    const int64_t blocks = ceil_div(a.rows, kJoinRows);
+    if (!grid_fits(blocks, kJoinRows * kJoinSlices)) return hipErrorInvalidConfiguration;
+    hipLaunchKernelGGL(join_kernel, dim3(unsigned(blocks)), dim3(kJoinRows * kJoinSlices), 0, stream, j);
+    return hipGetLastError();
+}
+
+namespace {
+
+template <bool AlongB>
+hipError_t launch_grad(const GradArgs& k, Shape shape, int64_t layers, int dtype, hipStream_t stream)
+{
+    return with_shape(shape, [&](auto s) {
+        using S = decltype(s);
+        if (!grid_fits(k.tiles_m * k.tiles_n, S::kThreads)) return hipErrorInvalidConfiguration;
+        const dim3 grid(unsigned(k.tiles_m * k.tiles_n), unsigned(layers)), block(S::kThreads);
+        if (dtype == kBf16)
+            hipLaunchKernelGGL((grad_kernel<S, AlongB, bf16_t>), grid, block, 0, stream, k);
+        else
+            hipLaunchKernelGGL((grad_kernel<S, AlongB, float>), grid, block, 0, stream, k);
+        return hipGetLastError();
+    });
+}
+
+hipError_t launch_sum(const SumArgs& a, int dtype, hipStream_t stream)
+{
+    const int64_t blocks = ceil_div(a.n * (a.slab_ld / 4), kSumThreads);
+    if (!grid_fits(blocks, kSumThreads)) return hipErrorInvalidConfiguration;
+    if (dtype == kBf16)
+        hipLaunchKernelGGL((layer_sum_kernel<bf16_t>), dim3(unsigned(blocks)), dim3(kSumThreads), 0, stream, a);
+    else
+        hipLaunchKernelGGL((layer_sum_kernel<float>), dim3(unsigned(blocks)), dim3(kSumThreads), 0, stream, a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_cross_entropy_grad(const CrossEntropyGradArgs& a, hipStream_t stream)
+{
+    if (a.rows == 0) {      // the table's gradient is the sum of nothing
+        if (a.dtable == nullptr) return hipSuccess;
+        const SumArgs none{nullptr, ceil_to(a.width, 4), 0, 0, a.vocab, a.width, a.dtable, a.dtable_stride, Tokens{}, 0};
+        return launch_sum(none, a.dtype, stream);
+    }
+    const GradPlan plan(a.rows, a.vocab, a.width, a.dtype);
+    const int planes = planes_of(a.dtype);
+    const int pairs = planes == 1 ? 1 : 6;
+    const int64_t ld = plan.ld, es = planes == 1 ? 2 : 4;
+    char* ws = a.workspace;
+    uint16_t* h = reinterpret_cast<uint16_t*>(ws + plan.h);
+    uint16_t* zeros = reinterpret_cast<uint16_t*>(ws + plan.zeros);
+    uint16_t* dz = reinterpret_cast<uint16_t*>(ws + plan.dz);
+    // h is copied always: rows that do not count may hold anything, and the products over rows would meet it
+    const PackArgs ph{a.h, a.rows, a.width, a.h_stride, a.targets, a.vocab, h, plan.dz_rows, ld, plan.dz_rows * ld, zeros};
+    if (hipError_t e = pack_planes(ph, a.dtype, stream); e != hipSuccess) return e;
+    const bool as_is = direct(a.table, a.table_stride, a.width, a.dtype);
+    const int64_t dz_plane = plan.dz_rows * plan.dz_ld;
+
+    for (int64_t first = 0; first < a.vocab; first += plan.piece) {
+        const int64_t piece = std::min(plan.piece, a.vocab - first);
+        const bool last = first + piece == a.vocab;
+        const char* src = static_cast<const char*>(a.table) + first * a.table_stride * es;
+        Matrix table;
+        if (as_is) {
+            table = Matrix{reinterpret_cast<const uint16_t*>(src), a.table_stride, 0, piece, a.width};
+        } else {
+            uint16_t* copy = reinterpret_cast<uint16_t*>(ws + plan.table);
+            table = Matrix{copy, ld, plan.piece * ld, piece, ld};
+            const PackArgs p{src, piece, a.width, a.table_stride, Tokens{}, 0, copy, piece, ld, plan.piece * ld, nullptr};
+            if (hipError_t e = pack_planes(p, a.dtype, stream); e != hipSuccess) return e;
+        }
+        LogitsArgs k{};
+        k.table = table;
+        k.h = Matrix{h, ld, plan.dz_rows * ld, plan.dz_rows, ld};
+        k.pairs = pairs;
+        k.steps = ld / kStepK;
+        k.first = first;
+        k.vocab = a.vocab;
+        k.piece = piece;
+        k.rows = a.rows;
+        k.targets = a.targets;
+        k.cap = a.cap;
+        k.lse = a.lse;
+        k.dloss = a.dloss;
+        k.dz = dz;
+        k.dz_ld = plan.dz_ld;
+        k.dz_plane = dz_plane;
+        k.dz_rows = plan.dz_rows;
+        k.tiles_m = ceil_div(piece, kShapeM[plan.logits]);
+        k.tiles_n = ceil_div(plan.dz_rows, kShapeN[plan.logits]);
+        hipError_t e = with_shape(plan.logits, [&](auto s) {
+            using S = decltype(s);
+            if (!grid_fits(k.tiles_m * k.tiles_n, S::kThreads)) return hipErrorInvalidConfiguration;
+            hipLaunchKernelGGL((logits_grad_kernel<S>), dim3(unsigned(k.tiles_m * k.tiles_n)), dim3(S::kThreads), 0, stream, k);
+            return hipGetLastError();
+        });
+        if (e != hipSuccess) return e;
+        const Matrix dz_rows{dz, plan.dz_ld, dz_plane, plan.dz_rows, plan.dz_ld};
+        if (a.dh != nullptr) {
+            const bool slab = plan.h_layers > 1 || plan.piece < a.vocab;
+            GradArgs d{};
+            d.a = table;
+            d.b = dz_rows;
+            d.pairs = pairs;
+            d.k = piece;
+            d.k_split = ceil_to(ceil_div(plan.piece, plan.h_layers), kStepK);
+            d.zeros = zeros;
+            d.tiles_m = ceil_div(a.width, kShapeM[plan.dh]);
+            d.tiles_n = ceil_div(a.rows, kShapeN[plan.dh]);
+            d.width = a.width;
+            d.n = a.rows;
+            d.slab = slab ? reinterpret_cast<float*>(ws + plan.slab_h) : nullptr;
+            d.slab_ld = ld;
+            d.slab_layer = a.rows * ld;
+            d.first = first == 0;
+            d.out = plan.h_layers == 1 && last ? a.dh : nullptr;
+            d.out_stride = a.dh_stride;
+            d.targets = a.targets;
+            d.vocab = a.vocab;
+            if (e = launch_grad<true>(d, plan.dh, plan.h_layers, a.dtype, stream); e != hipSuccess) return e;
+            if (last && plan.h_layers > 1) {
+                const SumArgs s{d.slab, ld, d.slab_layer, plan.h_layers, a.rows, a.width, a.dh, a.dh_stride, a.targets, a.vocab};
+                if (e = launch_sum(s, a.dtype, stream); e != hipSuccess) return e;
+            }
+        }
+        if (a.dtable != nullptr) {
+            GradArgs d{};
+            d.a = k.h;
+            d.b = dz_rows;
+            d.pairs = pairs;
+            d.k = plan.dz_rows;
+            d.k_split = ceil_to(ceil_div(plan.dz_rows, plan.e_layers), kStepK);
+            d.zeros = zeros;
+            d.tiles_m = ceil_div(a.width, kShapeM[plan.de]);
+            d.tiles_n = ceil_div(piece, kShapeN[plan.de]);
+            d.width = a.width;
+            d.n = piece;
+            d.slab = plan.e_layers > 1 ? reinterpret_cast<float*>(ws + plan.slab_e) : nullptr;
+            d.slab_ld = ld;
+            d.slab_layer = plan.piece * ld;
+            d.first = true;
+            void* out = static_cast<char*>(a.dtable) + first * a.dtable_stride * es;
+            d.out = plan.e_layers == 1 ? out : nullptr;
+            d.out_stride = a.dtable_stride;
+            if (e = launch_grad<false>(d, plan.de, plan.e_layers, a.dtype, stream); e != hipSuccess) return e;
+            if (plan.e_layers > 1) {
+                const SumArgs s{d.slab, ld, d.slab_layer, plan.e_layers, piece, a.width, out, a.dtable_stride, Tokens{}, 0};
+                if (e = launch_sum(s, a.dtype, stream); e != hipSuccess) return e;
+            }
+        }
+    }
+    return hipSuccess;
+}
+
+}  // namespace mesa

@@ -3,94 +3,33 @@
 // of every entry point is documented in include/libmesa.h.
 #include <math.h>
 
-#include <initializer_list>
-
 #include "mesa_abi.hpp"
 #include "mesa_kernels.hpp"
 
 namespace {
 
-using mesa::finish;
-using mesa::launch_status;
-using mesa::overlaps;
-using mesa::Range;
-using mesa::range_of;
+using mesa::aligned;
+using mesa::all_aligned;
+using mesa::any_null;
+using mesa::bytes_of;
+using mesa::clash;
+using mesa::dense;
+using mesa::float_type;
+using mesa::kMostElements;
+using mesa::product_ok;
+using mesa::Rows;
+using mesa::status_of;
+using mesa::tokens;
+using mesa::touch;
 
 static_assert(MESA_RECURRENCE_BLOCK == mesa::kRecurrenceBlock, "the header's block of tokens");
 static_assert(MESA_DTYPE_F32 == mesa::kF32 && MESA_DTYPE_BF16 == mesa::kBf16 && MESA_DTYPE_Q8 == mesa::kQ8, "the header's types");
-
-constexpr int64_t kMostElements = int64_t(1) << 40;   // of one array: byte offsets stay far inside 64 bits
-
-// Whether the product of non-negative factors stays within kMostElements.
-bool product_ok(std::initializer_list<int64_t> factors)
-{
-    int64_t p = 1;
-    for (int64_t f : factors) {
-        if (f == 0) return true;
-        if (f > kMostElements / p) return false;
-        p *= f;
-    }
-    return true;
-}
-
-bool float_type(int dtype) { return dtype == MESA_DTYPE_F32 || dtype == MESA_DTYPE_BF16; }
-int64_t bytes_of(int dtype) { return dtype == MESA_DTYPE_BF16 ? 2 : dtype == MESA_DTYPE_Q8 ? 1 : 4; }
-bool aligned(const void* p, int64_t bytes) { return uintptr_t(p) % uintptr_t(bytes) == 0; }
-bool all_aligned(std::initializer_list<const void*> ptrs, int64_t bytes)
-{
-    for (const void* p : ptrs)
-        if (!aligned(p, bytes)) return false;
-    return true;
-}
-bool any_null(std::initializer_list<const void*> ptrs)
-{
-    for (const void* p : ptrs)
-        if (p == nullptr) return true;
-    return false;
-}
 
 size_t checkpoint_bytes(int64_t rows, int64_t width)
 {
     const int64_t groups = (width + MESA_CHECKPOINT_GROUP - 1) / MESA_CHECKPOINT_GROUP;
     return size_t((mesa::checkpoint_exponents_at(rows, width) + rows * groups + 15) / 16 * 16);
 }
-
-// A device array as `rows` pieces of `bytes`, `pitch` apart (absent: a null pointer or no bytes).
-struct Rows {
-    const void* p;
-    int64_t rows, bytes, pitch;
-    bool empty() const { return p == nullptr || rows <= 0 || bytes <= 0; }
-    Range span() const { return range_of(p, (rows - 1) * pitch + bytes); }
-};
-Rows dense(const void* p, int64_t bytes) { return {p, 1, bytes, bytes}; }
-Rows tokens(const void* p, int64_t n, int64_t width, int64_t stride, int dtype)
-{
-    return {p, n, width * bytes_of(dtype), stride * bytes_of(dtype)};
-}
-
-// Whether two arrays share a byte.  Slices of one array (the same pitch) interleave freely.
-bool touch(const Rows& a, const Rows& b)
-{
-    if (a.empty() || b.empty() || !overlaps(a.span(), b.span())) return false;
-    if (a.pitch != b.pitch || a.rows == 1 || b.rows == 1) return true;
-    int64_t d = (int64_t(uintptr_t(b.p)) - int64_t(uintptr_t(a.p))) % a.pitch;
-    if (d < 0) d += a.pitch;
-    return d < a.bytes || a.pitch - d < b.bytes;
-}
-
-// Outputs must overlap neither an input nor each other.
-bool clash(std::initializer_list<Rows> ins, std::initializer_list<Rows> outs)
-{
-    for (const Rows* o = outs.begin(); o != outs.end(); ++o) {
-        for (const Rows& i : ins)
-            if (touch(*o, i)) return true;
-        for (const Rows* q = o + 1; q != outs.end(); ++q)
-            if (touch(*o, *q)) return true;
-    }
-    return false;
-}
-
-int status_of(hipError_t e, void* stream) { return finish(launch_status(e), stream); }
 
 int checkpoint(const void* x, int64_t rows, int64_t width, int64_t stride, int dtype, const void* buffer, bool pack,
                void* stream)

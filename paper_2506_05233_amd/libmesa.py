@@ -44,6 +44,9 @@ EXPORTED = ("mesa_forward", "mesa_forward_ex", "mesa_forward_states", "mesa_forw
             "mesa_recurrence_backward", "mesa_recurrence_backward_workspace_bytes",
             "mesa_frontend_backward", "mesa_frontend_backward_workspace_bytes",
             "mesa_output_norm_backward", "mesa_output_norm_backward_workspace_bytes",
+            "mesa_embedding", "mesa_embedding_backward", "mesa_embedding_backward_workspace_bytes",
+            "mesa_cross_entropy", "mesa_cross_entropy_workspace_bytes",
+            "mesa_cross_entropy_backward", "mesa_cross_entropy_backward_workspace_bytes",
             "mesa_status_string", "mesa_version")
 
 _lib = None
@@ -128,6 +131,20 @@ def load():
     lib.mesa_output_norm_backward_workspace_bytes.restype = sz
     lib.mesa_output_norm_backward.argtypes = [vp, fp, cf, vp, i64, i64, i64, i64, ci, ci, fp, fp, vp, sz, vp]
     lib.mesa_output_norm_backward.restype = ci
+    lib.mesa_embedding.argtypes = [vp, vp, ci, cf, i64, i64, i64, i64, ci, ci, i64, vp, vp]
+    lib.mesa_embedding.restype = ci
+    lib.mesa_embedding_backward_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.mesa_embedding_backward_workspace_bytes.restype = sz
+    lib.mesa_embedding_backward.argtypes = [vp, ci, vp, cf, i64, i64, i64, i64, ci, ci, i64, ci, vp, vp, sz, vp]
+    lib.mesa_embedding_backward.restype = ci
+    lib.mesa_cross_entropy_workspace_bytes.argtypes = [i64, i64, i64, ci]
+    lib.mesa_cross_entropy_workspace_bytes.restype = sz
+    lib.mesa_cross_entropy.argtypes = [vp, vp, vp, ci, cf, i64, i64, i64, i64, i64, ci, fp, fp, vp, vp, sz, vp]
+    lib.mesa_cross_entropy.restype = ci
+    lib.mesa_cross_entropy_backward_workspace_bytes.argtypes = [i64, i64, i64, ci]
+    lib.mesa_cross_entropy_backward_workspace_bytes.restype = sz
+    lib.mesa_cross_entropy_backward.argtypes = [vp, vp, vp, ci, fp, fp, cf, i64, i64, i64, i64, i64, ci, i64, i64, vp, vp, vp, sz, vp]
+    lib.mesa_cross_entropy_backward.restype = ci
     lib.mesa_status_string.argtypes = [ci]
     lib.mesa_status_string.restype = ctypes.c_char_p
     lib.mesa_version.argtypes = []
@@ -938,4 +955,149 @@ def output_norm_backward(o, weight, dy, eps=1e-6, workspace=None):
                                        _ptr(res["dweight"]), _ptr(workspace), need, _stream(dev))
     if st != MESA_OK:
         raise MesaError(st, "mesa_output_norm_backward")
+    return res
+
+
+# ---------------------------------------------------------------- a language model's two ends
+def _token_bytes(t, name, device):
+    """Bytes of a token number of t, a dense int32 or int64 tensor on the device."""
+    torch = _torch()
+    if not isinstance(t, torch.Tensor):
+        raise TypeError("%s must be a torch.Tensor" % name)
+    if t.dtype is not torch.int64 and t.dtype is not torch.int32:
+        raise TypeError("%s must be int32 or int64, got %s" % (name, t.dtype))
+    if t.device != device:
+        raise ValueError("%s is on %s, expected %s" % (name, t.device, device))
+    if not t.is_contiguous():
+        raise ValueError("%s must be contiguous" % name)
+    return 8 if t.dtype is torch.int64 else 4
+
+
+def _table_rows(t, name, width=None):
+    """Device, type code and row stride of a table [vocab, width]."""
+    dev = _on_device(t, name)
+    if t.dim() != 2 or (width is not None and t.shape[1] != width):
+        raise ValueError("%s has shape %s, expected [vocab, %s]" % (name, tuple(t.shape), "width" if width is None else width))
+    return dev, _float_code(t.dtype, name), _row_stride(t, name)
+
+
+def embedding(table, tokens, scale=1.0, out_dtype=None, out=None):
+    """mesa_embedding: scale * table[tokens] for table [V,W] (fp32 or bf16, rows evenly spaced) and
+    tokens [...] int32 or int64; a token outside [0, V) gives a row of zeros.  Returns [...,W] of
+    out_dtype (the table's by default), or writes out (rows evenly spaced)."""
+    torch = _torch()
+    lib = load()
+    dev, code, stride = _table_rows(table, "table")
+    size = _token_bytes(tokens, "tokens", dev)
+    V, W = table.shape
+    shape = tokens.shape + (W,)
+    if out is None:
+        out = torch.empty(shape, dtype=table.dtype if out_dtype is None else out_dtype, device=dev)
+    out_stride = _check_rows(out, "out", shape, out.dtype if out_dtype is None else out_dtype, dev)
+    st = lib.mesa_embedding(_ptr(table), _ptr(tokens), size, float(scale), tokens.numel(), V, W, stride, code,
+                            _float_code(out.dtype, "out"), out_stride, _ptr(out), _stream(dev))
+    if st != MESA_OK:
+        raise MesaError(st, "mesa_embedding")
+    return out
+
+
+def embedding_backward_workspace_bytes(rows, vocab, width) -> int:
+    return load().mesa_embedding_backward_workspace_bytes(rows, vocab, width)
+
+
+def embedding_backward(tokens, dy, vocab, scale=1.0, grad_dtype=None, out=None, accumulate=False, workspace=None):
+    """mesa_embedding_backward: the gradient [vocab,W] of embedding()'s table from tokens [...] and
+    dy [...,W] (fp32 or bf16, rows evenly spaced), of grad_dtype (dy's by default); or into out
+    [vocab,W] (rows evenly spaced), added to what it holds with accumulate.  Tokens that occur more
+    than once are added in their order, in fp32."""
+    torch = _torch()
+    lib = load()
+    dev = _on_device(dy, "dy")
+    size = _token_bytes(tokens, "tokens", dev)
+    W = dy.shape[-1] if dy.dim() else 0
+    dy_stride = _check_rows(dy, "dy", tokens.shape + (W,), dy.dtype, dev)
+    code = _float_code(dy.dtype, "dy")
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate needs out")
+        out = torch.empty((vocab, W), dtype=dy.dtype if grad_dtype is None else grad_dtype, device=dev)
+    out_stride = _check_rows(out, "out", (vocab, W), out.dtype if grad_dtype is None else grad_dtype, dev)
+    rows = tokens.numel()
+    need = lib.mesa_embedding_backward_workspace_bytes(rows, vocab, W)
+    workspace = _workspace(workspace, need, dev)
+    st = lib.mesa_embedding_backward(_ptr(tokens), size, _ptr(dy), float(scale), rows, vocab, W, dy_stride, code,
+                                     _float_code(out.dtype, "out"), out_stride, int(bool(accumulate)), _ptr(out),
+                                     _ptr(workspace), need, _stream(dev))
+    if st != MESA_OK:
+        raise MesaError(st, "mesa_embedding_backward")
+    return out
+
+
+def cross_entropy_workspace_bytes(rows, vocab, width, dtype) -> int:
+    return load().mesa_cross_entropy_workspace_bytes(rows, vocab, width, dtype)
+
+
+def cross_entropy(h, table, targets=None, cap=0.0, want_best=False, workspace=None):
+    """mesa_cross_entropy: of h [...,W] against table [V,W] (fp32 or bf16, one dtype, rows evenly
+    spaced), with the logits held within cap (0: as they are).  targets [...] int32 or int64, or
+    None.  Returns a dict of [...] tensors: "lse" fp32 (log of the sum of the logits'
+    exponentials), with targets "loss" fp32 (0 where the target lies outside [0, V)), and, if asked,
+    "best" int32 (the token with the largest logit, the lowest of several)."""
+    torch = _torch()
+    lib = load()
+    W = h.shape[-1]
+    dev, code, table_stride = _table_rows(table, "table", W)
+    shape = h.shape[:-1]
+    h_stride = _check_rows(h, "h", shape + (W,), table.dtype, dev)
+    size = 0
+    res = {"lse": torch.empty(shape, dtype=torch.float32, device=dev)}
+    if targets is not None:
+        size = _token_bytes(targets, "targets", dev)
+        if targets.shape != shape:
+            raise ValueError("targets has shape %s, expected %s" % (tuple(targets.shape), tuple(shape)))
+        res["loss"] = torch.empty(shape, dtype=torch.float32, device=dev)
+    if want_best:
+        res["best"] = torch.empty(shape, dtype=torch.int32, device=dev)
+    rows = res["lse"].numel()
+    need = lib.mesa_cross_entropy_workspace_bytes(rows, table.shape[0], W, code)
+    workspace = _workspace(workspace, need, dev)
+    st = lib.mesa_cross_entropy(_ptr(h), _ptr(table), _ptr(targets), size, float(cap), rows, table.shape[0], W, h_stride,
+                                table_stride, code, _ptr(res.get("loss")), _ptr(res["lse"]), _ptr(res.get("best")),
+                                _ptr(workspace), need, _stream(dev))
+    if st != MESA_OK:
+        raise MesaError(st, "mesa_cross_entropy")
+    return res
+
+
+def cross_entropy_backward_workspace_bytes(rows, vocab, width, dtype) -> int:
+    return load().mesa_cross_entropy_backward_workspace_bytes(rows, vocab, width, dtype)
+
+
+def cross_entropy_backward(h, table, targets, lse, dloss, cap=0.0, want_dh=True, want_dtable=True, workspace=None):
+    """mesa_cross_entropy_backward: gradients of cross_entropy() for dloss [...] fp32 (the gradient of
+    each row's loss), from what was given to it and the lse that it returned.  Returns a dict, of
+    h's dtype: "dh" [...,W] and "dtable" [V,W], each unless it is not wanted."""
+    torch = _torch()
+    lib = load()
+    W = h.shape[-1]
+    dev, code, table_stride = _table_rows(table, "table", W)
+    shape = h.shape[:-1]
+    h_stride = _check_rows(h, "h", shape + (W,), table.dtype, dev)
+    size = _token_bytes(targets, "targets", dev)
+    if targets.shape != shape:
+        raise ValueError("targets has shape %s, expected %s" % (tuple(targets.shape), tuple(shape)))
+    _check_all(torch.float32, dev, (lse, "lse", shape), (dloss, "dloss", shape))
+    res = {}
+    if want_dh:
+        res["dh"] = torch.empty(shape + (W,), dtype=h.dtype, device=dev)
+    if want_dtable:
+        res["dtable"] = torch.empty(table.shape, dtype=h.dtype, device=dev)
+    rows, V = lse.numel(), table.shape[0]
+    need = lib.mesa_cross_entropy_backward_workspace_bytes(rows, V, W, code)
+    workspace = _workspace(workspace, need, dev)
+    st = lib.mesa_cross_entropy_backward(_ptr(h), _ptr(table), _ptr(targets), size, _ptr(lse), _ptr(dloss), float(cap), rows, V, W,
+                                         h_stride, table_stride, code, W, W, _ptr(res.get("dh")), _ptr(res.get("dtable")),
+                                         _ptr(workspace), need, _stream(dev))
+    if st != MESA_OK:
+        raise MesaError(st, "mesa_cross_entropy_backward")
     return res
