@@ -35,9 +35,7 @@ struct PackArgs {
     int64_t vocab;
     uint16_t* out;           // planes of [out_rows, ld]
     int64_t out_rows, ld, plane;
-    uint16_t* zeros;         // kZeroBytes of zeros, or null
 };
-constexpr int64_t kZeroBytes = 256;
 
 // The three parts of an fp32 value, whose sum it is: each the nearest bf16 to what the parts before
 // leave, which are exact differences (the first cut off where the nearest would be an infinity).  The
@@ -59,7 +57,6 @@ __global__ void __launch_bounds__(kPackThreads) pack_planes_kernel(PackArgs a)
 {
     const int64_t i = int64_t(blockIdx.x) * kPackThreads + threadIdx.x;
     const int64_t per = a.ld / 8;
-    if (a.zeros != nullptr && i < kZeroBytes / 16) reinterpret_cast<uint4*>(a.zeros)[i] = make_uint4(0, 0, 0, 0);
     if (i >= a.out_rows * per) return;
     const int64_t row = i / per, c = i % per * 8;
     float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
@@ -126,6 +123,37 @@ __device__ __forceinline__ float tanh_of(float x, float& slope)
     return copysignf(y < 0.3f ? series : (1.0f - e) * q, x);
 }
 
+// The same for |x| <= kNear as x P(x^2), P of degree four: 2^-24.5 of itself by its coefficients (a
+// fit that levels the largest relative error), 2^-22.7 as evaluated.  A third of the instructions of the
+// general form, and none of the slow ones.  A soft cap is there to hold the few far logits, so waves
+// whose logits are all near are the rule; the others take the general form for a column at a time.
+constexpr float kNear = 0.5625f;
+struct NearTanh {
+    float c[5];      // for z in the place of x = z / cap
+    float edge;      // largest |z|
+    __device__ explicit NearTanh(float cap)
+    {
+        const float inv = cap > 0.0f ? 1.0f / cap : 0.0f, q = inv * inv;
+        c[0] = 0.99999996002f * inv;
+        c[1] = -0.33332697360f * inv * q;
+        c[2] = 0.13316993368f * inv * q * q;
+        c[3] = -0.05247611788f * inv * q * q * q;
+        c[4] = 0.01610694871f * inv * q * q * q * q;
+        edge = kNear * cap;
+        // powers of a far cap that leave fp32's range, up or down, take the general form
+        const float last = inv * q * q * q * q;
+        if (!(last > 1e-30f && last < 1e30f)) edge = -1.0f;
+    }
+    __device__ __forceinline__ float operator()(float z) const
+    {
+        const float s = z * z;
+        return z * fmaf(s, fmaf(s, fmaf(s, fmaf(s, c[4], c[3]), c[2]), c[1]), c[0]);
+    }
+};
+
+// Up to this cap exp(l) and sums of them stay far inside fp32's range, whatever l is.
+constexpr float kPlainCap = 60.0f;
+
 // max over the four 16-lane rows: every lane receives that of its column position
 __device__ __forceinline__ float row_pair_max(float v)
 {
@@ -175,7 +203,7 @@ __global__ void __launch_bounds__(S::kThreads) logits_kernel(LogitsArgs a)
     tile_of(a.tiles_m, a.tiles_n, tm, tn);
     const int64_t m0 = tm * S::M, n0 = tn * S::N;
     f32x4 acc[S::MT][S::NT];
-    Product<S, true, true>::run(a.table, m0, a.h, n0, 0, a.steps * kStepK, a.pairs, nullptr, lds, acc);
+    Product<S, true, true>::run(a.table, m0, a.h, n0, 0, a.steps * kStepK, a.pairs, lds, acc);
 
     const int lane = int(threadIdx.x) % kWave, g = lane / 16, n = lane % 16;
     const int wave = int(threadIdx.x) / kWave, wm = wave / S::WN, wn = wave % S::WN;
@@ -210,19 +238,31 @@ __global__ void __launch_bounds__(S::kThreads) logits_kernel(LogitsArgs a)
             }
         }
     }
-    if (a.cap > 0.0f) {
-        const float inv = 1.0f / a.cap;
-        float slope;
-#pragma unroll
-        for (int i = 0; i < S::MT; ++i)
-#pragma unroll
-            for (int j = 0; j < S::NT; ++j)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) acc[i][j][r] = a.cap * tanh_of(acc[i][j][r] * inv, slope);
-    }
+    const NearTanh near(a.cap);
+    const float inv = a.cap > 0.0f ? 1.0f / a.cap : 0.0f;
+    const bool plain = a.cap > 0.0f && a.cap <= kPlainCap;      // then nothing has to be taken off the logits
 #pragma unroll
     for (int j = 0; j < S::NT; ++j) {
         const int64_t row = n0 + (wn * S::NT + j) * 16 + n;
+        if (a.cap > 0.0f) {
+            float far = 0.0f;
+#pragma unroll
+            for (int i = 0; i < S::MT; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) far = fmaxf(far, fabsf(acc[i][j][r]));
+            if (!__any(far > near.edge)) {
+#pragma unroll
+                for (int i = 0; i < S::MT; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) acc[i][j][r] = a.cap * near(acc[i][j][r]);
+            } else {
+                float slope;
+#pragma unroll
+                for (int i = 0; i < S::MT; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) acc[i][j][r] = a.cap * tanh_of(acc[i][j][r] * inv, slope);
+            }
+        }
         if (a.at != nullptr) {
             const int64_t t = row < a.rows ? token_at(a.targets, row) - v0 : -1;
             if (__any(t >= 0 && t < here)) {
@@ -233,7 +273,6 @@ __global__ void __launch_bounds__(S::kThreads) logits_kernel(LogitsArgs a)
                         if (16 * i + 4 * g + r == t && t < here) a.at[row] = acc[i][j][r];
             }
         }
-        float top = -kInf;
         if (here < S::MT * 16) {
 #pragma unroll
             for (int i = 0; i < S::MT; ++i)
@@ -241,18 +280,26 @@ __global__ void __launch_bounds__(S::kThreads) logits_kernel(LogitsArgs a)
                 for (int r = 0; r < 4; ++r)
                     if (16 * i + 4 * g + r >= here) acc[i][j][r] = -kInf;
         }
+        float top = 0.0f, sum = 0.0f;
+        if (plain) {
 #pragma unroll
-        for (int i = 0; i < S::MT; ++i)
+            for (int i = 0; i < S::MT; ++i)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) top = fmaxf(top, acc[i][j][r]);
-        top = row_pair_max(top);
-        // where every logit is -infinity (or there is none) the sum is 0, whatever they are taken to
-        const float base = top == -kInf ? 0.0f : top;
-        float sum = 0.0f;
+                for (int r = 0; r < 4; ++r) sum += __builtin_amdgcn_exp2f(acc[i][j][r] * kLog2e);
+        } else {
+            top = -kInf;
 #pragma unroll
-        for (int i = 0; i < S::MT; ++i)
+            for (int i = 0; i < S::MT; ++i)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) sum += __builtin_amdgcn_exp2f((acc[i][j][r] - base) * kLog2e);
+                for (int r = 0; r < 4; ++r) top = fmaxf(top, acc[i][j][r]);
+            top = row_pair_max(top);
+            // where every logit is -infinity (or there is none) the sum is 0, whatever they are taken to
+            const float base = top == -kInf ? 0.0f : top;
+#pragma unroll
+            for (int i = 0; i < S::MT; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) sum += __builtin_amdgcn_exp2f((acc[i][j][r] - base) * kLog2e);
+        }
         sum = row_pair_sums(sum);
         if (g == 0) {
             red_m[wm * S::N + (wn * S::NT + j) * 16 + n] = top;
@@ -288,7 +335,7 @@ __global__ void __launch_bounds__(S::kThreads) logits_kernel(LogitsArgs a)
     }
 }
 
-// The tiles' sums joined: 16 rows a workgroup, 16 threads for the tiles of each.
+// The tiles' sums joined, in a fixed order: Rows rows a workgroup, 256 / Rows threads for the tiles of each.
 struct JoinArgs {
     const float2* part;
     const float* best_z;
@@ -300,48 +347,57 @@ struct JoinArgs {
     float* lse;
     int32_t* best;
 };
-constexpr int kJoinRows = 16, kJoinSlices = 16;
+constexpr int kJoinThreads = 256, kJoinDepth = 4;
 
-__global__ void __launch_bounds__(kJoinRows* kJoinSlices) join_kernel(JoinArgs a)
+template <int Rows>
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(JoinArgs a)
 {
-    __shared__ float2 red[kJoinSlices][kJoinRows];
-    __shared__ float red_z[kJoinSlices][kJoinRows];
-    __shared__ int red_v[kJoinSlices][kJoinRows];
-    const int r = int(threadIdx.x) % kJoinRows, slice = int(threadIdx.x) / kJoinRows;
-    const int64_t row = int64_t(blockIdx.x) * kJoinRows + r;
+    constexpr int kSlices = kJoinThreads / Rows;
+    __shared__ float2 red[kJoinThreads];
+    __shared__ float red_z[kJoinThreads];
+    __shared__ int red_v[kJoinThreads];
+    const int r = int(threadIdx.x) % Rows, slice = int(threadIdx.x) / Rows;
+    const int64_t row = int64_t(blockIdx.x) * Rows + r;
     float top = -kInf, sum = 0.0f, z = -kInf;
     int v = INT32_MAX;
     auto add = [&](float2 p) {
         const float m = fmaxf(top, p.x);
-        if (m == -kInf) {
-            sum += p.y;
-            return;
-        }
-        sum = sum * (top == m ? 1.0f : __builtin_amdgcn_exp2f((top - m) * kLog2e)) +
-              p.y * (p.x == m ? 1.0f : __builtin_amdgcn_exp2f((p.x - m) * kLog2e));
+        // of what is all -infinity the sums are 0, or NaN
+        const float before = top == m ? 1.0f : __builtin_amdgcn_exp2f((top - m) * kLog2e);
+        sum = sum * before + p.y * (p.x == m ? 1.0f : __builtin_amdgcn_exp2f((p.x - m) * kLog2e));
         top = m;
     };
+    auto better = [&](float zt, int vt) {
+        if (zt > z || (zt == z && vt < v)) z = zt, v = vt;
+    };
     if (row < a.rows) {
-#pragma unroll 4
-        for (int64_t t = slice; t < a.tiles; t += kJoinSlices) {
-            add(a.part[t * a.rows + row]);
+        for (int64_t t = slice; t < a.tiles; t += kSlices * kJoinDepth) {
+            float2 p[kJoinDepth];
+#pragma unroll
+            for (int k = 0; k < kJoinDepth; ++k) p[k] = t + k * kSlices < a.tiles ? a.part[(t + k * kSlices) * a.rows + row] : make_float2(-kInf, 0.0f);
+#pragma unroll
+            for (int k = 0; k < kJoinDepth; ++k) add(p[k]);
             if (a.best != nullptr) {
-                const float zt = a.best_z[t * a.rows + row];
-                const int vt = a.best_v[t * a.rows + row];
-                if (zt > z || (zt == z && vt < v)) z = zt, v = vt;
+#pragma unroll
+                for (int k = 0; k < kJoinDepth; ++k)
+                    if (t + k * kSlices < a.tiles) better(a.best_z[(t + k * kSlices) * a.rows + row], a.best_v[(t + k * kSlices) * a.rows + row]);
             }
         }
     }
-    red[slice][r] = make_float2(top, sum);
-    red_z[slice][r] = z;
-    red_v[slice][r] = v;
-    __syncthreads();
-    if (slice != 0 || row >= a.rows) return;
 #pragma unroll
-    for (int s = 1; s < kJoinSlices; ++s) {
-        add(red[s][r]);
-        if (red_z[s][r] > z || (red_z[s][r] == z && red_v[s][r] < v)) z = red_z[s][r], v = red_v[s][r];
+    for (int half = kSlices / 2; half > 0; half /= 2) {
+        red[threadIdx.x] = make_float2(top, sum);
+        red_z[threadIdx.x] = z;
+        red_v[threadIdx.x] = v;
+        __syncthreads();
+        if (slice < half) {
+            const int other = int(threadIdx.x) + half * Rows;
+            add(red[other]);
+            better(red_z[other], red_v[other]);
+        }
+        __syncthreads();
     }
+    if (slice != 0 || row >= a.rows) return;
     const float lse = top + kLn2 * __builtin_amdgcn_logf(sum);
     a.lse[row] = lse;
     if (a.loss != nullptr) {
@@ -352,6 +408,21 @@ __global__ void __launch_bounds__(kJoinRows* kJoinSlices) join_kernel(JoinArgs a
 }
 
 // ------------------------------------------------------------------ the gradient
+// dz of a column of near logits, none of them a target's: tanh, its slope 1 - tanh^2 (at least 0.74, so
+// nothing cancels), exp and two products.
+template <class S>
+__device__ __forceinline__ void grads_near(f32x4 (&acc)[S::MT][S::NT], int j, const NearTanh& near, float scale, float lse2, float up)
+{
+#pragma unroll
+    for (int i = 0; i < S::MT; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const float y = near(acc[i][j][r]);
+            const float p = __builtin_amdgcn_exp2f(fmaf(y, scale, -lse2));
+            acc[i][j][r] = p * fmaf(-y, y, 1.0f) * up;
+        }
+}
+
 // The logits of one tile again, and from them dz in bf16 (three planes of it for fp32 operands).
 template <class S>
 __global__ void __launch_bounds__(S::kThreads) logits_grad_kernel(LogitsArgs a)
@@ -361,50 +432,76 @@ __global__ void __launch_bounds__(S::kThreads) logits_grad_kernel(LogitsArgs a)
     tile_of(a.tiles_m, a.tiles_n, tm, tn);
     const int64_t m0 = tm * S::M, n0 = tn * S::N;
     f32x4 acc[S::MT][S::NT];
-    Product<S, true, true>::run(a.table, m0, a.h, n0, 0, a.steps * kStepK, a.pairs, nullptr, lds, acc);
+    Product<S, true, true>::run(a.table, m0, a.h, n0, 0, a.steps * kStepK, a.pairs, lds, acc);
 
     const int lane = int(threadIdx.x) % kWave, g = lane / 16, n = lane % 16;
     const int wave = int(threadIdx.x) / kWave, wm = wave / S::WN, wn = wave % S::WN;
     const int64_t c0 = m0 + wm * S::MT * 16;                // the wave's first column of dz
     const int here = int(min(a.piece - c0, int64_t(S::MT * 16)));
-    const float inv = a.cap > 0.0f ? 1.0f / a.cap : 0.0f;
+    const float inv = a.cap > 0.0f ? 1.0f / a.cap : 0.0f, scale = a.cap * kLog2e;
+    const NearTanh near(a.cap);
 #pragma unroll
     for (int j = 0; j < S::NT; ++j) {
         const int64_t row = n0 + (wn * S::NT + j) * 16 + n;
         int64_t t = -1;
-        float lse = 0.0f, up = 0.0f;
+        // a row that does not count has products of 0 (h is copied so) and takes exp(-far) times 0
+        float lse2 = 1e30f, up = 0.0f;
         if (row < a.rows) {
             t = token_at(a.targets, row);
-            lse = a.lse[row];
-            up = a.dloss[row];
+            if (t >= 0 && t < a.vocab) lse2 = a.lse[row] * kLog2e, up = a.dloss[row];
         }
-        const bool counts = t >= 0 && t < a.vocab;
-        const int mine = counts ? int(max(min(t - a.first - c0, int64_t(INT32_MAX)), int64_t(-1))) : -1;
+        const int64_t to = t - a.first - c0;
+        const int mine = t < a.vocab && to >= 0 && to < here ? int(to) : -1;
+        float far = 0.0f;
+#pragma unroll
+        for (int i = 0; i < S::MT; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) far = fmaxf(far, fabsf(acc[i][j][r]));
+        const bool all_near = a.cap > 0.0f && !__any(far > near.edge), target = __any(mine >= 0);
+        // dz in the place of z; the target's element, where it is one of the wave's, gets its -1 in place
+        auto grads = [&](auto logit) {
+#pragma unroll
+            for (int i = 0; i < S::MT; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    float slope;
+                    const float p = __builtin_amdgcn_exp2f(logit(acc[i][j][r], slope) - lse2);
+                    acc[i][j][r] = (target && 16 * i + 4 * g + r == mine ? p - 1.0f : p) * (slope * up);
+                }
+        };
+        if (all_near && !target) {
+            grads_near<S>(acc, j, near, scale, lse2, up);
+        } else if (a.cap > 0.0f) {
+            grads([&](float z, float& slope) { return scale * tanh_of(z * inv, slope); });
+        } else {
+            grads([&](float z, float& slope) {
+                slope = 1.0f;
+                return z * kLog2e;
+            });
+        }
+        if (here < S::MT * 16) {
+#pragma unroll
+            for (int i = 0; i < S::MT; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (16 * i + 4 * g + r >= here) acc[i][j][r] = 0.0f;
+        }
         if (row >= a.dz_rows) continue;
-        uint16_t* dst = a.dz + row * a.dz_ld + c0;
+        uint16_t* dst = a.dz + row * a.dz_ld + c0 + 4 * g;
+        // rounded to bf16 once for both products: 2^-8 of an element at most, at random over the sums
+        if (a.pairs == 1) {
 #pragma unroll
-        for (int i = 0; i < S::MT; ++i) {
-            float d[4];
+            for (int i = 0; i < S::MT; ++i)
+                *reinterpret_cast<uint2*>(dst + 16 * i) = make_uint2(pack_bf16(acc[i][j][0], acc[i][j][1]), pack_bf16(acc[i][j][2], acc[i][j][3]));
+        } else {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int v = 16 * i + 4 * g + r;
-                float l = acc[i][j][r], slope = 1.0f;
-                if (a.cap > 0.0f) l = a.cap * tanh_of(l * inv, slope);
-                const float p = __builtin_amdgcn_exp2f((l - lse) * kLog2e);
-                d[r] = (v == mine ? p - 1.0f : p) * slope * up;
-                if (!counts || v >= here) d[r] = 0.0f;
-            }
-            // rounded to bf16 once for both products: 2^-8 of an element at most, at random over the sums
-            if (a.pairs == 1) {
-                *reinterpret_cast<uint2*>(dst + 16 * i + 4 * g) = make_uint2(pack_bf16(d[0], d[1]), pack_bf16(d[2], d[3]));
-            } else {
+            for (int i = 0; i < S::MT; ++i) {
                 uint32_t p[4][3];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) three_parts(d[r], p[r]);
+                for (int r = 0; r < 4; ++r) three_parts(acc[i][j][r], p[r]);
 #pragma unroll
                 for (int k = 0; k < 3; ++k)
-                    *reinterpret_cast<uint2*>(dst + k * a.dz_plane + 16 * i + 4 * g) =
-                        make_uint2(p[0][k] | p[1][k] << 16, p[2][k] | p[3][k] << 16);
+                    *reinterpret_cast<uint2*>(dst + k * a.dz_plane + 16 * i) = make_uint2(p[0][k] | p[1][k] << 16, p[2][k] | p[3][k] << 16);
             }
         }
     }
@@ -415,7 +512,6 @@ struct GradArgs {
     Matrix a, b;
     int pairs;
     int64_t k, k_split;       // k of one launch layer, a multiple of 64 (blockIdx.y of them)
-    const void* zeros;
     int64_t tiles_m, tiles_n;
     int64_t width, n;         // of the result
     // fp32 sums on the way: [layer][n][slab_ld], written (first) or added to; null: none
@@ -448,7 +544,7 @@ __global__ void __launch_bounds__(S::kThreads) grad_kernel(GradArgs a)
     tile_of(a.tiles_m, a.tiles_n, tm, tn);
     const int64_t m0 = tm * S::M, n0 = tn * S::N, k0 = int64_t(blockIdx.y) * a.k_split;
     f32x4 acc[S::MT][S::NT];
-    Product<S, false, AlongB>::run(a.a, m0, a.b, n0, k0, min(k0 + a.k_split, a.k), a.pairs, a.zeros, lds, acc);
+    Product<S, false, AlongB, AlongB>::run(a.a, m0, a.b, n0, k0, min(k0 + a.k_split, a.k), a.pairs, lds, acc);
 
     const int lane = int(threadIdx.x) % kWave, g = lane / 16, n = lane % 16;
     const int wave = int(threadIdx.x) / kWave, wm = wave / S::WN, wn = wave % S::WN;
@@ -592,7 +688,7 @@ struct ForwardPlan {
 };
 
 struct GradPlan {
-    int64_t piece, dz, dz_rows, dz_ld, h, table, zeros, slab_h, slab_e, bytes, ld;
+    int64_t piece, dz, dz_rows, dz_ld, h, table, slab_h, slab_e, bytes, ld;
     int64_t h_layers, e_layers;
     Shape logits, dh, de;
     GradPlan(int64_t rows, int64_t vocab, int64_t width, int dtype)
@@ -608,7 +704,6 @@ struct GradPlan {
         h_layers = layers(width, rows, piece, dh);
         e_layers = layers(width, piece, rows, de);
         Carve c;
-        zeros = c.take(kZeroBytes);
         h = c.take(dz_rows * ld * 2 * planes);
         table = c.take(piece * ld * 2 * planes);
         dz = c.take(dz_rows * dz_ld * 2 * planes);
@@ -657,7 +752,7 @@ hipError_t launch_cross_entropy(const CrossEntropyArgs& a, hipStream_t stream)
     } else {
         uint16_t* copy = reinterpret_cast<uint16_t*>(a.workspace + plan.h);
         k.h = Matrix{copy, ld, a.rows * ld, a.rows, ld};
-        const PackArgs p{a.h, a.rows, a.width, a.h_stride, Tokens{}, 0, copy, a.rows, ld, a.rows * ld, nullptr};
+        const PackArgs p{a.h, a.rows, a.width, a.h_stride, Tokens{}, 0, copy, a.rows, ld, a.rows * ld};
         if (hipError_t e = pack_planes(p, a.dtype, stream); e != hipSuccess) return e;
     }
     const bool as_is = direct(a.table, a.table_stride, a.width, a.dtype);
@@ -675,7 +770,7 @@ hipError_t launch_cross_entropy(const CrossEntropyArgs& a, hipStream_t stream)
             uint16_t* copy = reinterpret_cast<uint16_t*>(a.workspace + plan.table);
             k.table = Matrix{copy, ld, most * ld, k.piece, ld};
             const char* src = static_cast<const char*>(a.table) + first * a.table_stride * (planes == 1 ? 2 : 4);
-            const PackArgs p{src, k.piece, a.width, a.table_stride, Tokens{}, 0, copy, k.piece, ld, most * ld, nullptr};
+            const PackArgs p{src, k.piece, a.width, a.table_stride, Tokens{}, 0, copy, k.piece, ld, most * ld};
             if (hipError_t e = pack_planes(p, a.dtype, stream); e != hipSuccess) return e;
         }
         const hipError_t e = with_shape(shape, [&](auto s) {
@@ -688,9 +783,13 @@ hipError_t launch_cross_entropy(const CrossEntropyArgs& a, hipStream_t stream)
     }
     const JoinArgs j{k.part, k.best_z, k.best_v, k.at, a.targets, a.rows, a.vocab,
                      ceil_div(a.vocab, kShapeM[shape]), a.targets.p == nullptr ? nullptr : a.loss, a.lse, a.best};
-    const int64_t blocks = ceil_div(a.rows, kJoinRows);
-    if (!grid_fits(blocks, kJoinRows * kJoinSlices)) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL(join_kernel, dim3(unsigned(blocks)), dim3(kJoinRows * kJoinSlices), 0, stream, j);
+    // a workgroup for each of few rows; sixteen neighbours, whose sums lie side by side, of many
+    const int64_t blocks = a.rows <= 1024 ? a.rows : ceil_div(a.rows, 16);
+    if (!grid_fits(blocks, kJoinThreads)) return hipErrorInvalidConfiguration;
+    if (a.rows <= 1024)
+        hipLaunchKernelGGL((join_kernel<1>), dim3(unsigned(blocks)), dim3(kJoinThreads), 0, stream, j);
+    else
+        hipLaunchKernelGGL((join_kernel<16>), dim3(unsigned(blocks)), dim3(kJoinThreads), 0, stream, j);
     return hipGetLastError();
 }
 
@@ -737,10 +836,9 @@ hipError_t launch_cross_entropy_grad(const CrossEntropyGradArgs& a, hipStream_t 
     const int64_t ld = plan.ld, es = planes == 1 ? 2 : 4;
     char* ws = a.workspace;
     uint16_t* h = reinterpret_cast<uint16_t*>(ws + plan.h);
-    uint16_t* zeros = reinterpret_cast<uint16_t*>(ws + plan.zeros);
     uint16_t* dz = reinterpret_cast<uint16_t*>(ws + plan.dz);
     // h is copied always: rows that do not count may hold anything, and the products over rows would meet it
-    const PackArgs ph{a.h, a.rows, a.width, a.h_stride, a.targets, a.vocab, h, plan.dz_rows, ld, plan.dz_rows * ld, zeros};
+    const PackArgs ph{a.h, a.rows, a.width, a.h_stride, a.targets, a.vocab, h, plan.dz_rows, ld, plan.dz_rows * ld};
     if (hipError_t e = pack_planes(ph, a.dtype, stream); e != hipSuccess) return e;
     const bool as_is = direct(a.table, a.table_stride, a.width, a.dtype);
     const int64_t dz_plane = plan.dz_rows * plan.dz_ld;
@@ -755,7 +853,7 @@ hipError_t launch_cross_entropy_grad(const CrossEntropyGradArgs& a, hipStream_t 
         } else {
             uint16_t* copy = reinterpret_cast<uint16_t*>(ws + plan.table);
             table = Matrix{copy, ld, plan.piece * ld, piece, ld};
-            const PackArgs p{src, piece, a.width, a.table_stride, Tokens{}, 0, copy, piece, ld, plan.piece * ld, nullptr};
+            const PackArgs p{src, piece, a.width, a.table_stride, Tokens{}, 0, copy, piece, ld, plan.piece * ld};
             if (hipError_t e = pack_planes(p, a.dtype, stream); e != hipSuccess) return e;
         }
         LogitsArgs k{};
@@ -793,7 +891,6 @@ hipError_t launch_cross_entropy_grad(const CrossEntropyGradArgs& a, hipStream_t 
             d.pairs = pairs;
             d.k = piece;
             d.k_split = ceil_to(ceil_div(plan.piece, plan.h_layers), kStepK);
-            d.zeros = zeros;
             d.tiles_m = ceil_div(a.width, kShapeM[plan.dh]);
             d.tiles_n = ceil_div(a.rows, kShapeN[plan.dh]);
             d.width = a.width;
@@ -819,7 +916,6 @@ hipError_t launch_cross_entropy_grad(const CrossEntropyGradArgs& a, hipStream_t 
             d.pairs = pairs;
             d.k = plan.dz_rows;
             d.k_split = ceil_to(ceil_div(plan.dz_rows, plan.e_layers), kStepK);
-            d.zeros = zeros;
             d.tiles_m = ceil_div(a.width, kShapeM[plan.de]);
             d.tiles_n = ceil_div(piece, kShapeN[plan.de]);
             d.width = a.width;
