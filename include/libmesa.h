@@ -547,8 +547,8 @@ int mesa_output_norm_backward(const void* o, const float* weight, float eps, con
  * mesa_embedding_backward: dE_v = scale sum over n with token_n = v of dy_n (zeros where there is
  *   none), added in the order of n; with `accumulate` not 0 it is added to what dtable holds
  *   (rows of tokens that do not occur are then not touched).  dy of grad_dtype, dtable of
- *   table_dtype.  Rows of dy that have no token are not read.  Three kernel launches up to 2048 rows,
- *   else six or eight (more from a vocabulary of 2^18 on). */
+ *   table_dtype.  Rows of dy that have no token are not read.  Three kernel launches up to 16384
+ *   rows, else six or seven (more from a vocabulary of 2^18 on). */
 int mesa_embedding(const void* table, const void* token, int token_bytes, float scale, int64_t rows, int64_t vocab,
                    int64_t width, int64_t table_stride, int dtype, int out_dtype, int64_t out_stride, void* out,
                    void* stream);

@@ -1,11 +1,13 @@
 // Token embedding, y_n = scale E[t_n], and the gradient of its table, dE_v = scale sum_{n: t_n = v} dy_n.
 //
 // The look-up is a copy.  The gradient sorts the tokens (least significant digits first, stable), so
-// that the rows of one token follow each other in the order in which they came, and every row of the
-// table is then written once, by one group of lanes, which adds its token's rows in that order: no
-// atomics on values, the same bits every time.  A token that fills whole pieces of 32 sorted
-// positions has their sums from a launch before (and those of 32 such pieces from another), so that
-// no group walks more than about a hundred rows, however frequent a token is.
+// that the rows of one token follow each other in the order in which they came.  Then every piece of 16
+// sorted positions is added up by one group of lanes, in order: tokens that begin and end in the piece
+// are written to the table, and the sums of the piece's first and last token, where those go on past it,
+// are kept; a last launch adds those up along each such token (of many rows over whole runs of 32 pieces).
+// No atomics on values, the same bits every time, and no group walks far, however frequent a token is.
+// The sort keeps a few compute units busy for some 30 us; the others fill the gradient with zeros in the
+// same launches, which is most of its traffic.
 #include <algorithm>
 
 #include "mesa_kernels.hpp"
@@ -52,13 +54,38 @@ __device__ __forceinline__ void store_channels(T* p, const float (&y)[V])
     }
 }
 
+// V consecutive channels as they lie in memory, until they are added.
+template <typename T, int V>
+struct Row {
+    typename Lane4<T>::Raw lo, hi;
+    __device__ __forceinline__ void load(const T* p)
+    {
+        lo = reinterpret_cast<const typename Lane4<T>::Raw*>(p)[0];
+        hi = reinterpret_cast<const typename Lane4<T>::Raw*>(p)[1];
+    }
+    __device__ __forceinline__ void add(float (&sum)[V]) const
+    {
+        float x[4], y[4];
+        Lane4<T>::widen(lo, x);
+        Lane4<T>::widen(hi, y);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) sum[v] += x[v], sum[v + 4] += y[v];
+    }
+};
+template <typename T>
+struct Row<T, 1> {
+    T x;
+    __device__ __forceinline__ void load(const T* p) { x = *p; }
+    __device__ __forceinline__ void add(float (&sum)[1]) const { sum[0] += to_f32(x); }
+};
+
 // A row's lanes: a power of two, as many as it has pieces of V channels, at most the workgroup.
 struct Lanes {
     int log2;
     __host__ __device__ int rows() const { return kThreads >> log2; }     // rows a workgroup takes at once
     __device__ int row() const { return int(threadIdx.x) >> log2; }
     __device__ int lane() const { return int(threadIdx.x) & ((1 << log2) - 1); }
-    __device__ int count() const { return 1 << log2; }
+    __host__ __device__ int count() const { return 1 << log2; }
 };
 Lanes lanes_for(int64_t width, int v)
 {
@@ -115,11 +142,11 @@ hipError_t lookup(const EmbeddingArgs& a, hipStream_t stream)
 }
 
 // ------------------------------------------------------------------ the tokens in order
-constexpr int kTile = 2048;            // tokens a workgroup sorts
+constexpr int kTile = 1024;            // tokens a workgroup sorts
 constexpr int kWaves = kThreads / kWave;
 constexpr int kRounds = kTile / kThreads;
 constexpr int kDigitBits = 9, kBins = 1 << kDigitBits;
-constexpr int kPiece = 32;             // sorted positions of a piece, pieces of a run of pieces
+constexpr int kPiece = 16, kRun = 32;  // sorted positions of a piece; pieces of a run
 
 // A token's key: itself, or vocab for one that does not count, which comes last.
 __device__ __forceinline__ uint32_t key_of(const Tokens& t, int64_t i, int64_t vocab)
@@ -128,26 +155,42 @@ __device__ __forceinline__ uint32_t key_of(const Tokens& t, int64_t i, int64_t v
     return v >= 0 && v < vocab ? uint32_t(v) : uint32_t(vocab);
 }
 
-// Ranks of a tile's keys by one digit.  Wave w has keys w 512 + 64 k + lane; count[w][d] ends as the
-// number of its keys with digit d and rank[k] as how many of them come before the lane's k-th.
-__device__ __forceinline__ void digit_ranks(const uint32_t (&digit)[kRounds], const bool (&active)[kRounds], int bits,
-                                            volatile uint32_t (*count)[kBins], uint32_t (&rank)[kRounds])
+// Ranks of a workgroup's keys by one digit.  Wave w has keys w 64 Rounds + 64 k + lane; count[w][d] ends
+// as the number of its keys with digit d and rank[k] as how many of them come before the lane's k-th
+// (bit k of live: it exists).
+template <int Rounds>
+__device__ __forceinline__ void digit_ranks(const uint32_t (&key)[Rounds], uint32_t live, int shift, uint32_t mask,
+                                            volatile uint32_t (*count)[kBins], uint32_t (&rank)[Rounds])
 {
     const int lane = int(threadIdx.x) % kWave, wave = int(threadIdx.x) / kWave;
     for (int i = lane; i < kBins; i += kWave) count[wave][i] = 0;
 #pragma unroll
-    for (int k = 0; k < kRounds; ++k) {
-        uint64_t same = __ballot(active[k]);
-        for (int b = 0; b < bits; ++b) {
-            const bool bit = (digit[k] >> b) & 1;
+    for (int k = 0; k < Rounds; ++k) {
+        const bool active = (live >> k) & 1;
+        const uint32_t digit = (key[k] >> shift) & mask;
+        uint64_t same = __ballot(active);
+#pragma unroll
+        for (int b = 0; b < kDigitBits; ++b) {      // bits past the digit's are 0 everywhere
+            const bool bit = (digit >> b) & 1;
             const uint64_t with = __ballot(bit);
             same &= bit ? with : ~with;
         }
-        const uint32_t before = active[k] ? count[wave][digit[k]] : 0;
+        const uint32_t before = active ? count[wave][digit] : 0;
         const int lower = __popcll(same & ((uint64_t(1) << lane) - 1));
         rank[k] = before + uint32_t(lower);
-        if (active[k] && lower == 0) count[wave][digit[k]] = before + uint32_t(__popcll(same));
+        if (active && lower == 0) count[wave][digit] = before + uint32_t(__popcll(same));
     }
+}
+
+// Inclusive prefix sum over the lanes of a wave.
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x, int lane)
+{
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) {
+        const uint32_t o = uint32_t(__shfl_up(int(x), d));
+        if (lane >= d) x += o;
+    }
+    return x;
 }
 
 struct SortArgs {
@@ -160,22 +203,48 @@ struct SortArgs {
     uint32_t* hist;                // [tiles][kBins]
     int64_t tiles;
     int shift, bits;
-    uint2* spans;                  // [vocab], cleared on the way when not null
-    int digits;                    // of a whole key (a single tile sorts by all of them)
+    int digits;                    // of a whole key (a single workgroup sorts by all of them)
 };
 
-// Clears the spans, by workgroups tiles .. gridDim.x - 1.
-__device__ __forceinline__ void clear_spans(uint2* spans, int64_t vocab, int64_t first)
+// Zeros for rows of the table's gradient, in a launch's workgroups from `first` on.
+struct Fill {
+    char* p;
+    int64_t rows, bytes, pitch;      // bytes of a row, and between rows
+    int piece;                       // bytes of an access: 16, 4 or 2
+};
+__device__ __forceinline__ void fill_rows(const Fill& f, int64_t first)
 {
-    for (int64_t v = (int64_t(blockIdx.x) - first) * kThreads + threadIdx.x; v < vocab; v += (int64_t(gridDim.x) - first) * kThreads)
-        spans[v] = make_uint2(0u, 0u);
+    const int64_t block = int64_t(blockIdx.x) - first, blocks = int64_t(gridDim.x) - first;
+    if (f.bytes == f.pitch) {        // dense rows are one run
+        const int64_t n = f.rows * f.bytes / f.piece, step = blocks * blockDim.x;
+        for (int64_t i = block * blockDim.x + threadIdx.x; i < n; i += step) {
+            if (f.piece == 16)
+                reinterpret_cast<uint4*>(f.p)[i] = make_uint4(0, 0, 0, 0);
+            else if (f.piece == 4)
+                reinterpret_cast<uint32_t*>(f.p)[i] = 0;
+            else
+                reinterpret_cast<uint16_t*>(f.p)[i] = 0;
+        }
+        return;
+    }
+    for (int64_t row = block; row < f.rows; row += blocks) {
+        char* p = f.p + row * f.pitch;
+        for (int64_t i = threadIdx.x; i < f.bytes / f.piece; i += blockDim.x) {
+            if (f.piece == 16)
+                reinterpret_cast<uint4*>(p)[i] = make_uint4(0, 0, 0, 0);
+            else if (f.piece == 4)
+                reinterpret_cast<uint32_t*>(p)[i] = 0;
+            else
+                reinterpret_cast<uint16_t*>(p)[i] = 0;
+        }
+    }
 }
 
 // How many keys of a tile have each value of a digit.
-__global__ void __launch_bounds__(kThreads) token_histogram_kernel(SortArgs a)
+__global__ void __launch_bounds__(kThreads) token_histogram_kernel(SortArgs a, Fill fill)
 {
     if (int64_t(blockIdx.x) >= a.tiles) {
-        clear_spans(a.spans, a.vocab, a.tiles);
+        fill_rows(fill, a.tiles);
         return;
     }
     __shared__ uint32_t bins[kBins];
@@ -199,12 +268,7 @@ __device__ __forceinline__ void scan_bins(uint32_t* x, uint32_t* wave_total)
 {
     const int t = int(threadIdx.x), lane = t % kWave, wave = t / kWave;
     const uint32_t a = x[2 * t], b = x[2 * t + 1];
-    uint32_t s = a + b;
-#pragma unroll
-    for (int d = 1; d < kWave; d *= 2) {
-        const uint32_t o = uint32_t(__shfl_up(int(s), d));
-        if (lane >= d) s += o;
-    }
+    const uint32_t s = wave_scan(a + b, lane);
     if (lane == kWave - 1) wave_total[wave] = s;
     __syncthreads();
     uint32_t base = 0;
@@ -216,21 +280,25 @@ __device__ __forceinline__ void scan_bins(uint32_t* x, uint32_t* wave_total)
 static_assert(kBins == 2 * kThreads, "two bins a thread");
 
 // A tile's keys to their places by one digit.
-__global__ void __launch_bounds__(kThreads) token_scatter_kernel(SortArgs a)
+__global__ void __launch_bounds__(kThreads) token_scatter_kernel(SortArgs a, Fill fill)
 {
+    if (int64_t(blockIdx.x) >= a.tiles) {
+        fill_rows(fill, a.tiles);
+        return;
+    }
     __shared__ uint32_t count[kWaves][kBins];
     __shared__ uint32_t base[kBins], before[kBins], wave_total[kWaves];
     const int lane = int(threadIdx.x) % kWave, wave = int(threadIdx.x) / kWave;
     const int64_t first = int64_t(blockIdx.x) * kTile + wave * (kTile / kWaves) + lane;
-    uint32_t key[kRounds], place[kRounds], digit[kRounds], rank[kRounds];
-    bool active[kRounds];
+    const uint32_t mask = (1u << a.bits) - 1u;
+    uint32_t key[kRounds], place[kRounds], rank[kRounds], live = 0;
 #pragma unroll
     for (int k = 0; k < kRounds; ++k) {
         const int64_t i = first + k * kWave;
-        active[k] = i < a.rows;
-        key[k] = !active[k] ? 0u : a.keys_in == nullptr ? key_of(a.tokens, i, a.vocab) : a.keys_in[i];
-        place[k] = !active[k] ? 0u : a.keys_in == nullptr ? uint32_t(i) : a.places_in[i];
-        digit[k] = (key[k] >> a.shift) & ((1u << a.bits) - 1u);
+        const bool active = i < a.rows;
+        live |= uint32_t(active) << k;
+        key[k] = !active ? 0u : a.keys_in == nullptr ? key_of(a.tokens, i, a.vocab) : a.keys_in[i];
+        place[k] = !active ? 0u : a.keys_in == nullptr ? uint32_t(i) : a.places_in[i];
     }
     // keys of a smaller digit, and of the same digit in earlier tiles
     for (int d = int(threadIdx.x); d < kBins; d += kThreads) {
@@ -244,7 +312,7 @@ __global__ void __launch_bounds__(kThreads) token_scatter_kernel(SortArgs a)
         base[d] = all;
         before[d] = early;
     }
-    digit_ranks(digit, active, a.bits, count, rank);
+    digit_ranks<kRounds>(key, live, a.shift, mask, count, rank);
     __syncthreads();
     scan_bins(base, wave_total);
     for (int d = int(threadIdx.x); d < kBins; d += kThreads) {
@@ -258,72 +326,89 @@ __global__ void __launch_bounds__(kThreads) token_scatter_kernel(SortArgs a)
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < kRounds; ++k)
-        if (active[k]) {
-            const uint32_t at = count[wave][digit[k]] + rank[k];
+        if ((live >> k) & 1) {
+            const uint32_t at = count[wave][(key[k] >> a.shift) & mask] + rank[k];
             a.keys_out[at] = key[k];
             a.places_out[at] = place[k];
         }
 }
 
-// All digits of at most one tile of tokens, by one workgroup; the others clear the spans.
-__global__ void __launch_bounds__(kThreads) token_sort_kernel(SortArgs a)
+// All digits of up to 2048 tokens by one workgroup of 16 waves, Rounds keys a thread, which pass through
+// LDS once a digit: 5.7 us for 777 tokens of 5003, where the launches by digit take 4 times 5 or more.
+// (16 keys a thread, 16384 tokens, would take 54 against 30.)
+constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / kWave, kSortRounds = 2;
+
+template <int Rounds>
+__global__ void __launch_bounds__(kSortThreads) token_sort_kernel(SortArgs a, Fill fill)
 {
     if (blockIdx.x > 0) {
-        clear_spans(a.spans, a.vocab, 1);
+        fill_rows(fill, 1);
         return;
     }
-    __shared__ uint32_t count[kWaves][kBins];
-    __shared__ uint32_t base[kBins], wave_total[kWaves];
-    __shared__ uint32_t keys[kTile], places[kTile];
+    __shared__ uint32_t count[kSortWaves][kBins];
+    __shared__ uint32_t total[kBins / kWave];
+    __shared__ uint32_t pass[Rounds * kSortThreads];
     const int lane = int(threadIdx.x) % kWave, wave = int(threadIdx.x) / kWave;
-    const int first = wave * (kTile / kWaves) + lane;
-    uint32_t key[kRounds], place[kRounds], digit[kRounds], rank[kRounds];
-    bool active[kRounds];
+    const int first = wave * (Rounds * kWave) + lane;
+    const uint32_t mask = (1u << a.bits) - 1u;
+    uint32_t key[Rounds], place[Rounds], rank[Rounds], live = 0;
 #pragma unroll
-    for (int k = 0; k < kRounds; ++k) {
+    for (int k = 0; k < Rounds; ++k) {
         const int i = first + k * kWave;
-        active[k] = i < a.rows;
-        key[k] = active[k] ? key_of(a.tokens, i, a.vocab) : 0u;
+        live |= uint32_t(i < a.rows) << k;
+        key[k] = i < a.rows ? key_of(a.tokens, i, a.vocab) : 0u;
         place[k] = uint32_t(i);
     }
     for (int s = 0; s < a.digits; ++s) {
+        const int shift = s * a.bits;
+        digit_ranks<Rounds>(key, live, shift, mask, count, rank);
+        __syncthreads();
+        // bin d: its keys in each wave come after those of smaller digits and of earlier waves
+        const int d = int(threadIdx.x);
+        uint32_t mine[kSortWaves], sum = 0;
+        if (d < kBins) {
 #pragma unroll
-        for (int k = 0; k < kRounds; ++k) digit[k] = (key[k] >> (s * a.bits)) & ((1u << a.bits) - 1u);
-        digit_ranks(digit, active, a.bits, count, rank);
-        __syncthreads();
-        for (int d = int(threadIdx.x); d < kBins; d += kThreads) {
-            uint32_t n = 0;
-            for (int w = 0; w < kWaves; ++w) n += count[w][d];
-            base[d] = n;
-        }
-        __syncthreads();
-        scan_bins(base, wave_total);
-        for (int d = int(threadIdx.x); d < kBins; d += kThreads) {
-            uint32_t at = base[d];
-            for (int w = 0; w < kWaves; ++w) {
-                const uint32_t n = count[w][d];
-                count[w][d] = at;
-                at += n;
+            for (int w = 0; w < kSortWaves; ++w) mine[w] = count[w][d];
+#pragma unroll
+            for (int w = 0; w < kSortWaves; ++w) {
+                const uint32_t n = mine[w];
+                mine[w] = sum;
+                sum += n;
             }
         }
+        const uint32_t upto = wave_scan(sum, lane);
+        if (d < kBins && lane == kWave - 1) total[wave] = upto;
+        __syncthreads();
+        if (d < kBins) {
+            uint32_t at = upto - sum;
+            for (int w = 0; w < wave; ++w) at += total[w];
+#pragma unroll
+            for (int w = 0; w < kSortWaves; ++w) count[w][d] = at + mine[w];
+        }
+        __syncthreads();
+        // the keys that exist fill the front again, so the same lanes stay active
+#pragma unroll
+        for (int k = 0; k < Rounds; ++k) rank[k] += count[wave][(key[k] >> shift) & mask];
+#pragma unroll
+        for (int k = 0; k < Rounds; ++k)
+            if ((live >> k) & 1) pass[rank[k]] = key[k];
         __syncthreads();
 #pragma unroll
-        for (int k = 0; k < kRounds; ++k)
-            if (active[k]) {
-                const uint32_t at = count[wave][digit[k]] + rank[k];
-                keys[at] = key[k];
-                places[at] = place[k];
-            }
+        for (int k = 0; k < Rounds; ++k)
+            if ((live >> k) & 1) key[k] = pass[first + k * kWave];
         __syncthreads();
-        // the keys that exist fill the front again, so the same lanes are active
 #pragma unroll
-        for (int k = 0; k < kRounds; ++k)
-            if (active[k]) key[k] = keys[first + k * kWave], place[k] = places[first + k * kWave];
+        for (int k = 0; k < Rounds; ++k)
+            if ((live >> k) & 1) pass[rank[k]] = place[k];
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < Rounds; ++k)
+            if ((live >> k) & 1) place[k] = pass[first + k * kWave];
         __syncthreads();
     }
 #pragma unroll
-    for (int k = 0; k < kRounds; ++k)
-        if (active[k]) {
+    for (int k = 0; k < Rounds; ++k)
+        if ((live >> k) & 1) {
             a.keys_out[first + k * kWave] = key[k];
             a.places_out[first + k * kWave] = place[k];
         }
@@ -337,62 +422,94 @@ struct SumArgs {
     bool accumulate;
     const uint32_t* keys;          // sorted, with the rows that they came from
     const uint32_t* places;
-    uint2* spans;                  // [vocab]: first and past the last of a token's sorted positions
-    float* pieces;                 // [rows / 32][ld]: sums of whole pieces of one token
-    float* runs;                   // [rows / 1024][ld]: of 32 pieces
+    float* entered;                // [pieces][ld]: of each piece its part of a token that begins before it
+    float* left;                   // [pieces][ld]: and of one that begins in it and goes on after it
+    float* runs;                   // [pieces / kRun][ld]: sums of kRun of `entered`, all of one token
     void* dtable;
 };
 
-constexpr int kDepth = 4;          // rows asked for together
+constexpr int kDepth = 16;         // sums asked for together
+constexpr uint32_t kNoKey = 0xFFFFFFFFu;
+// Past so many rows there are runs of pieces.  Up to there a token that is everywhere has 1024 pieces at most,
+// which one group adds in some 100 us; a launch for everyone's runs costs 5.
+constexpr int64_t kRunRows = 16384;
 
-// Writes every token's span, and the sum of each piece that lies within one.
-template <typename T, int V>
-__global__ void __launch_bounds__(kThreads) token_piece_kernel(SumArgs a)
+template <typename O, int V>
+__device__ __forceinline__ void write_row(const SumArgs& a, uint32_t token, int64_t c, float (&sum)[V])
 {
-    const int64_t first = int64_t(blockIdx.x) * kPiece;
-    const int t = int(threadIdx.x);
-    if (t < kPiece && first + t < a.rows) {
-        const int64_t i = first + t;
-        const uint32_t k = a.keys[i];
-        if (k < uint32_t(a.vocab)) {
-            if (i == 0 || a.keys[i - 1] != k) a.spans[k].x = uint32_t(i);
-            if (i + 1 == a.rows || a.keys[i + 1] != k) a.spans[k].y = uint32_t(i + 1);
-        }
-    }
-    if (first + kPiece > a.rows) return;
-    const uint32_t k = a.keys[first];
-    if (k != a.keys[first + kPiece - 1] || k >= uint32_t(a.vocab)) return;
-    for (int64_t c = int64_t(t) * V; c < a.width; c += kThreads * V) {
-        float sum[V];
+    O* dst = static_cast<O*>(a.dtable) + int64_t(token) * a.table_stride + c;
+    float x[V];
 #pragma unroll
-        for (int v = 0; v < V; ++v) sum[v] = 0.0f;
-        for (int r = 0; r < kPiece; r += kDepth) {
-            float x[kDepth][V];
+    for (int v = 0; v < V; ++v) x[v] = 0.0f;
+    if (a.accumulate) load_channels<O, V>(dst, x);
 #pragma unroll
-            for (int e = 0; e < kDepth; ++e) load_channels<T, V>(static_cast<const T*>(a.dy) + int64_t(a.places[first + r + e]) * a.dy_stride + c, x[e]);
-#pragma unroll
-            for (int e = 0; e < kDepth; ++e)
-#pragma unroll
-                for (int v = 0; v < V; ++v) sum[v] += x[e][v];
-        }
-        store_channels<float, V>(a.pieces + int64_t(blockIdx.x) * a.ld + c, sum);
-    }
+    for (int v = 0; v < V; ++v) x[v] += a.scale * sum[v];
+    store_channels<O, V>(dst, x);
 }
 
-// Sums of 32 pieces that lie within one token's span.
+// Each piece of sorted positions: its tokens' sums.
+template <typename T, typename O, int V>
+__global__ void __launch_bounds__(kThreads) token_piece_kernel(SumArgs a, Lanes lanes)
+{
+    const int64_t piece = int64_t(blockIdx.x) * lanes.rows() + lanes.row(), first = piece * kPiece;
+    if (first >= a.rows) return;
+    const int64_t c = (int64_t(blockIdx.y) * lanes.count() + lanes.lane()) * V;
+    if (c >= a.width) return;
+    const int n = int(min(int64_t(kPiece), a.rows - first));
+    const uint32_t vocab = uint32_t(a.vocab);
+    uint32_t key[kPiece], place[kPiece];
+#pragma unroll
+    for (int e = 0; e < kPiece; ++e) {
+        const int64_t i = min(first + e, a.rows - 1);
+        key[e] = e < n ? a.keys[i] : kNoKey;
+        place[e] = a.places[i];
+    }
+    const uint32_t before = first > 0 ? a.keys[first - 1] : kNoKey, after = first + n < a.rows ? a.keys[first + n] : kNoKey;
+    if (key[0] >= vocab) return;      // only rows that do not count from here on
+    // every row of the piece is asked for before the first is added (in the place of a row that does not count,
+    // all of which come last, the first one again, for a sum that is not kept)
+    Row<T, V> x[kPiece];
+#pragma unroll
+    for (int e = 0; e < kPiece; ++e) x[e].load(static_cast<const T*>(a.dy) + int64_t(key[e] < vocab ? place[e] : place[0]) * a.dy_stride + c);
+    uint32_t token = key[0];
+    bool begins = token != before;
+    float sum[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) sum[v] = 0.0f;
+    auto flush = [&](bool ends) {
+        if (begins && ends)
+            write_row<O, V>(a, token, c, sum);
+        else
+            store_channels<float, V>((begins ? a.left : a.entered) + piece * a.ld + c, sum);
+    };
+#pragma unroll
+    for (int e = 0; e < kPiece; ++e) {
+        if (key[e] != token) {
+            if (token < vocab) flush(true);
+            token = key[e];
+            begins = true;
+#pragma unroll
+            for (int v = 0; v < V; ++v) sum[v] = 0.0f;
+        }
+        x[e].add(sum);
+    }
+    if (token < vocab) flush(token != after);
+}
+
+// Sums of the runs of pieces that lie within one token's rows, the first of which come before them.
 template <int V>
 __global__ void __launch_bounds__(kThreads) token_run_kernel(SumArgs a)
 {
-    const int64_t first = int64_t(blockIdx.x) * kPiece * kPiece;
-    if (first + kPiece * kPiece > a.rows) return;
-    const uint32_t k = a.keys[first];
-    if (k != a.keys[first + kPiece * kPiece - 1] || k >= uint32_t(a.vocab)) return;
-    const float* src = a.pieces + int64_t(blockIdx.x) * kPiece * a.ld;
+    const int64_t first = int64_t(blockIdx.x) * kPiece * kRun;
+    if (first == 0 || first + kPiece * kRun > a.rows) return;
+    const uint32_t k = a.keys[first - 1];
+    if (k != a.keys[first + kPiece * kRun - 1] || k >= uint32_t(a.vocab)) return;
+    const float* src = a.entered + int64_t(blockIdx.x) * kRun * a.ld;
     for (int64_t c = int64_t(threadIdx.x) * V; c < a.width; c += kThreads * V) {
         float sum[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) sum[v] = 0.0f;
-        for (int r = 0; r < kPiece; r += kDepth) {
+        for (int r = 0; r < kRun; r += kDepth) {
             float x[kDepth][V];
 #pragma unroll
             for (int e = 0; e < kDepth; ++e) load_channels<float, V>(src + (r + e) * a.ld + c, x[e]);
@@ -405,77 +522,93 @@ __global__ void __launch_bounds__(kThreads) token_run_kernel(SumArgs a)
     }
 }
 
-// Adds `n` rows at row(i) to the sum, several loads under way at a time, in order.
-template <typename T, int V, typename Row>
-__device__ __forceinline__ void add_rows(float (&sum)[V], int64_t n, Row row)
+// Adds rows lo .. hi - 1 of fp32 sums, several loads under way at a time, in order.
+template <int V>
+__device__ __forceinline__ void add_rows(float (&sum)[V], const float* rows, int64_t ld, int64_t lo, int64_t hi)
 {
-    int64_t i = 0;
-    for (; i + kDepth <= n; i += kDepth) {
+    for (int64_t i = lo; i < hi; i += kDepth) {
         float x[kDepth][V];
 #pragma unroll
-        for (int e = 0; e < kDepth; ++e) load_channels<T, V>(row(i + e), x[e]);
+        for (int e = 0; e < kDepth; ++e) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) x[e][v] = 0.0f;
+            if (i + e < hi) load_channels<float, V>(rows + (i + e) * ld, x[e]);
+        }
 #pragma unroll
         for (int e = 0; e < kDepth; ++e)
 #pragma unroll
             for (int v = 0; v < V; ++v) sum[v] += x[e][v];
     }
-    for (; i < n; ++i) {
-        float x[V];
-        load_channels<T, V>(row(i), x);
-#pragma unroll
-        for (int v = 0; v < V; ++v) sum[v] += x[v];
+}
+
+// Past the last of the sorted positions from `at` on that have the same key.
+__device__ __forceinline__ int64_t end_of(const uint32_t* keys, int64_t at, int64_t rows)
+{
+    const uint32_t key = keys[at];
+    int64_t lo = at, hi = rows;      // keys[lo] is the token's, keys[hi] is not (or there is none)
+    for (int64_t step = kPiece; lo + step < rows; step *= 4) {
+        if (keys[lo + step] != key) {
+            hi = lo + step;
+            break;
+        }
+        lo += step;
+    }
+    while (hi - lo > 1) {
+        const int64_t mid = (lo + hi) / 2;
+        if (keys[mid] == key)
+            lo = mid;
+        else
+            hi = mid;
+    }
+    return hi;
+}
+
+// Past the last of the pieces that a token enters which goes on after position `last`, the end of a piece.
+// A piece is entered where it begins with the token; a whole wave of one group looks at 64 of them at once.
+__device__ __forceinline__ int64_t pieces_entered(const SumArgs& a, uint32_t token, int64_t last, const Lanes& lanes)
+{
+    if (lanes.log2 < 6) return (end_of(a.keys, last, a.rows) + kPiece - 1) / kPiece;
+    const int64_t pieces = (a.rows + kPiece - 1) / kPiece;
+    for (int64_t p = last / kPiece + 1;; p += kWave) {
+        const int64_t mine = p + int(threadIdx.x) % kWave;
+        const uint64_t off = __ballot(mine >= pieces || a.keys[min(mine, pieces - 1) * kPiece] != token);
+        if (off != 0) return p + __builtin_ctzll(off);
     }
 }
 
-// Rows of the table's gradient, one a group of lanes.
-template <typename T, typename O, int V>
-__global__ void __launch_bounds__(kThreads) token_row_kernel(SumArgs a, Lanes lanes)
+// The tokens that begin in a piece and go on after it, one a group of lanes.
+template <typename O, int V>
+__global__ void __launch_bounds__(kThreads) token_join_kernel(SumArgs a, Lanes lanes)
 {
-    const int64_t v0 = int64_t(blockIdx.x) * lanes.rows() + lanes.row();
-    if (v0 >= a.vocab) return;
-    const uint2 span = a.spans[v0];
-    if (a.accumulate && span.x == span.y) return;
-    // rows up to a piece's start, pieces up to a run's, runs, pieces, rows
-    const int64_t lo = span.x, hi = span.y;
-    const int64_t p0 = (lo + kPiece - 1) / kPiece, p1 = hi / kPiece;
-    const bool pieces = p0 < p1;
-    const int64_t head = pieces ? p0 * kPiece : hi;
-    const int64_t r0 = (p0 + kPiece - 1) / kPiece, r1 = p1 / kPiece;
-    const bool runs = pieces && r0 < r1;
-    const int64_t mid = runs ? r0 * kPiece : p1;
-    const T* dy = static_cast<const T*>(a.dy);
-    for (int64_t c = int64_t(lanes.lane()) * V; c < a.width; c += int64_t(lanes.count()) * V) {
-        float sum[V];
-#pragma unroll
-        for (int v = 0; v < V; ++v) sum[v] = 0.0f;
-        add_rows<T, V>(sum, head - lo, [&](int64_t i) { return dy + int64_t(a.places[lo + i]) * a.dy_stride + c; });
-        if (pieces) {
-            add_rows<float, V>(sum, mid - p0, [&](int64_t i) { return a.pieces + (p0 + i) * a.ld + c; });
-            if (runs) {
-                add_rows<float, V>(sum, r1 - r0, [&](int64_t i) { return a.runs + (r0 + i) * a.ld + c; });
-                add_rows<float, V>(sum, p1 - r1 * kPiece, [&](int64_t i) { return a.pieces + (r1 * kPiece + i) * a.ld + c; });
-            }
-            add_rows<T, V>(sum, hi - p1 * kPiece, [&](int64_t i) { return dy + int64_t(a.places[p1 * kPiece + i]) * a.dy_stride + c; });
-        }
-        O* dst = static_cast<O*>(a.dtable) + v0 * a.table_stride + c;
-        if (a.accumulate) {
-            float x[V];
-            load_channels<O, V>(dst, x);
-#pragma unroll
-            for (int v = 0; v < V; ++v) sum[v] = x[v] + a.scale * sum[v];
-        } else {
-#pragma unroll
-            for (int v = 0; v < V; ++v) sum[v] = span.x == span.y ? 0.0f : a.scale * sum[v];
-        }
-        store_channels<O, V>(dst, sum);
+    const int64_t piece = int64_t(blockIdx.x) * lanes.rows() + lanes.row(), first = piece * kPiece, last = first + kPiece - 1;
+    if (last + 1 >= a.rows) return;
+    const uint32_t token = a.keys[last];
+    if (token >= uint32_t(a.vocab) || a.keys[last + 1] != token) return;
+    if (first > 0 && a.keys[first - 1] == token) return;      // it begins before
+    const int64_t p0 = piece + 1, p1 = pieces_entered(a, token, last, lanes);
+    const int64_t c = (int64_t(blockIdx.y) * lanes.count() + lanes.lane()) * V;
+    if (c >= a.width) return;
+    float sum[V];
+    load_channels<float, V>(a.left + piece * a.ld + c, sum);
+    const int64_t r0 = (p0 + kRun - 1) / kRun, r1 = p1 / kRun;
+    // a run is whole, the last one only if the token goes on to its end
+    const bool runs = a.rows > kRunRows && r0 < r1;
+    const int64_t r2 = runs && (r1 * kRun * kPiece > a.rows || a.keys[r1 * kRun * kPiece - 1] != token) ? r1 - 1 : r1;
+    if (runs && r0 < r2) {
+        add_rows<V>(sum, a.entered + c, a.ld, p0, r0 * kRun);
+        add_rows<V>(sum, a.runs + c, a.ld, r0, r2);
+        add_rows<V>(sum, a.entered + c, a.ld, r2 * kRun, p1);
+    } else {
+        add_rows<V>(sum, a.entered + c, a.ld, p0, p1);
     }
+    write_row<O, V>(a, token, c, sum);
 }
 
 int64_t ceil_to(int64_t x, int64_t n) { return (x + n - 1) / n * n; }
 
 struct GradLayout {
-    int64_t tiles, ld, hist, keys[2], places[2], spans, pieces, runs, bytes;
-    GradLayout(int64_t rows, int64_t vocab, int64_t width)
+    int64_t tiles, ld, hist, keys[2], places[2], entered, left, runs, bytes;
+    GradLayout(int64_t rows, int64_t width)
     {
         tiles = (rows + kTile - 1) / kTile;
         ld = ceil_to(width, 8);
@@ -487,9 +620,10 @@ struct GradLayout {
         };
         hist = take(tiles * kBins * 4);
         for (int k = 0; k < 2; ++k) keys[k] = take(rows * 4), places[k] = take(rows * 4);
-        spans = take(vocab * 8);
-        pieces = take(rows / kPiece * ld * 4);
-        runs = take(rows / (kPiece * kPiece) * ld * 4);
+        const int64_t pieces = (rows + kPiece - 1) / kPiece;
+        entered = take(pieces * ld * 4);
+        left = take(pieces * ld * 4);
+        runs = rows <= kRunRows ? 0 : take(pieces / kRun * ld * 4);
         bytes = at;
     }
 };
@@ -497,13 +631,15 @@ struct GradLayout {
 template <typename T, typename O, int V>
 hipError_t sums(const SumArgs& a, hipStream_t stream)
 {
-    const int64_t pieces = (a.rows + kPiece - 1) / kPiece, runs = a.rows / (kPiece * kPiece);
+    const int64_t pieces = (a.rows + kPiece - 1) / kPiece, runs = a.rows <= kRunRows ? 0 : pieces / kRun;
     const Lanes lanes = lanes_for(a.width, V);
-    const int64_t blocks = (a.vocab + lanes.rows() - 1) / lanes.rows();
-    if (!grid_fits(blocks, kThreads) || !grid_fits(pieces, kThreads)) return hipErrorInvalidConfiguration;
-    if (pieces > 0) hipLaunchKernelGGL((token_piece_kernel<T, V>), dim3(unsigned(pieces)), dim3(kThreads), 0, stream, a);
+    const int64_t blocks = (pieces + lanes.rows() - 1) / lanes.rows();
+    // a workgroup's lanes side by side, and along the second dimension of the grid
+    const unsigned slabs = unsigned((a.width + lanes.count() * V - 1) / (lanes.count() * V));
+    if (!grid_fits(blocks, kThreads) || !grid_fits(runs, kThreads)) return hipErrorInvalidConfiguration;
+    hipLaunchKernelGGL((token_piece_kernel<T, O, V>), dim3(unsigned(blocks), slabs), dim3(kThreads), 0, stream, a, lanes);
     if (runs > 0) hipLaunchKernelGGL((token_run_kernel<V>), dim3(unsigned(runs)), dim3(kThreads), 0, stream, a);
-    hipLaunchKernelGGL((token_row_kernel<T, O, V>), dim3(unsigned(blocks)), dim3(kThreads), 0, stream, a, lanes);
+    if (pieces > 1) hipLaunchKernelGGL((token_join_kernel<O, V>), dim3(unsigned(blocks), slabs), dim3(kThreads), 0, stream, a, lanes);
     return hipGetLastError();
 }
 
@@ -518,11 +654,11 @@ hipError_t launch_embedding(const EmbeddingArgs& a, hipStream_t stream)
     return wide ? lookup<float, float, 8>(a, stream) : lookup<float, float, 1>(a, stream);
 }
 
-int64_t embedding_grad_bytes(int64_t rows, int64_t vocab, int64_t width) { return GradLayout(rows, vocab, width).bytes; }
+int64_t embedding_grad_bytes(int64_t rows, int64_t width) { return GradLayout(rows, width).bytes; }
 
 hipError_t launch_embedding_grad(const EmbeddingGradArgs& a, hipStream_t stream)
 {
-    const GradLayout lay(a.rows, a.vocab, a.width);
+    const GradLayout lay(a.rows, a.width);
     char* ws = a.workspace;
     int key_bits = 1;
     while (key_bits < 32 && (int64_t(1) << key_bits) <= a.vocab) ++key_bits;
@@ -535,16 +671,33 @@ hipError_t launch_embedding_grad(const EmbeddingGradArgs& a, hipStream_t stream)
     s.tiles = lay.tiles;
     s.bits = (key_bits + digits - 1) / digits;
     s.digits = digits;
-    s.spans = reinterpret_cast<uint2*>(ws + lay.spans);
     uint32_t* keys[2] = {reinterpret_cast<uint32_t*>(ws + lay.keys[0]), reinterpret_cast<uint32_t*>(ws + lay.keys[1])};
     uint32_t* places[2] = {reinterpret_cast<uint32_t*>(ws + lay.places[0]), reinterpret_cast<uint32_t*>(ws + lay.places[1])};
-    const int64_t clear = std::min<int64_t>((a.vocab + 4 * kThreads - 1) / (4 * kThreads), 1024);
+    // the table's rows are filled with zeros in equal shares of the sort's launches
+    const int64_t es = a.table_dtype == kBf16 ? 2 : 4, bytes = a.width * es, pitch = a.table_stride * es;
+    const int piece = bytes % 16 == 0 && pitch % 16 == 0 && uintptr_t(a.dtable) % 16 == 0 ? 16 : int(es);
+    const int shares = a.rows <= kSortRounds * kSortThreads ? 1 : 2 * digits;
+    int share = 0;
+    int64_t blocks = 0;
+    auto next_fill = [&](int threads) {
+        const int64_t r0 = a.vocab * share / shares, r1 = a.vocab * (share + 1) / shares;
+        ++share;
+        const Fill f{static_cast<char*>(a.dtable) + r0 * pitch, a.accumulate ? 0 : r1 - r0, bytes, pitch, piece};
+        // about 64 KB a workgroup, at most eight a compute unit
+        blocks = std::min<int64_t>(ceil_to(f.rows * bytes, 65536) / 65536, 2048 * kThreads / threads);
+        return f;
+    };
     int out = 0;
-    if (!grid_fits(lay.tiles + clear, kThreads)) return hipErrorInvalidConfiguration;
-    if (lay.tiles <= 1) {
+    if (!grid_fits(lay.tiles + 2048, kThreads)) return hipErrorInvalidConfiguration;
+    if (shares == 1) {
         s.keys_out = keys[0];
         s.places_out = places[0];
-        hipLaunchKernelGGL(token_sort_kernel, dim3(unsigned(1 + clear)), dim3(kThreads), 0, stream, s);
+        const Fill fill = next_fill(kSortThreads);
+        const dim3 grid(unsigned(1 + blocks)), block(kSortThreads);
+        if (a.rows <= kSortThreads)
+            hipLaunchKernelGGL(token_sort_kernel<1>, grid, block, 0, stream, s, fill);
+        else
+            hipLaunchKernelGGL(token_sort_kernel<kSortRounds>, grid, block, 0, stream, s, fill);
     } else {
         for (int d = 0; d < digits; ++d) {
             s.shift = d * s.bits;
@@ -553,13 +706,16 @@ hipError_t launch_embedding_grad(const EmbeddingGradArgs& a, hipStream_t stream)
             out = d == 0 ? 0 : 1 - out;
             s.keys_out = keys[out];
             s.places_out = places[out];
-            hipLaunchKernelGGL(token_histogram_kernel, dim3(unsigned(lay.tiles + (d == 0 ? clear : 0))), dim3(kThreads), 0, stream, s);
-            hipLaunchKernelGGL(token_scatter_kernel, dim3(unsigned(lay.tiles)), dim3(kThreads), 0, stream, s);
+            const Fill one = next_fill(kThreads);
+            hipLaunchKernelGGL(token_histogram_kernel, dim3(unsigned(lay.tiles + blocks)), dim3(kThreads), 0, stream, s, one);
+            const Fill two = next_fill(kThreads);
+            hipLaunchKernelGGL(token_scatter_kernel, dim3(unsigned(lay.tiles + blocks)), dim3(kThreads), 0, stream, s, two);
         }
     }
-    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    if (hipError_t e = hipGetLastError(); e != hipSuccess || a.rows == 0) return e;
     const SumArgs k{a.dy, a.rows, a.vocab, a.width, a.dy_stride, a.table_stride, lay.ld, a.scale, a.accumulate, keys[out], places[out],
-                    s.spans, reinterpret_cast<float*>(ws + lay.pieces), reinterpret_cast<float*>(ws + lay.runs), a.dtable};
+                    reinterpret_cast<float*>(ws + lay.entered), reinterpret_cast<float*>(ws + lay.left),
+                    reinterpret_cast<float*>(ws + lay.runs), a.dtable};
     const bool wide = wide_rows(a.dy, a.dy_stride, a.width, a.dtype) && wide_rows(a.dtable, a.table_stride, a.width, a.table_dtype);
     if (a.dtype == kBf16 && a.table_dtype == kBf16) return wide ? sums<bf16_t, bf16_t, 8>(k, stream) : sums<bf16_t, bf16_t, 1>(k, stream);
     if (a.dtype == kBf16) return wide ? sums<bf16_t, float, 8>(k, stream) : sums<bf16_t, float, 1>(k, stream);

@@ -66,7 +66,7 @@ int mesa_embedding(const void* table, const void* token, int token_bytes, float 
 size_t mesa_embedding_backward_workspace_bytes(int64_t rows, int64_t vocab, int64_t width)
 {
     if (vocab_sizes(rows, vocab, width) != MESA_OK || vocab == 0 || width == 0) return 0;
-    return size_t(mesa::embedding_grad_bytes(rows, vocab, width));
+    return size_t(mesa::embedding_grad_bytes(rows, width));
 }
 
 int mesa_embedding_backward(const void* token, int token_bytes, const void* dy, float scale, int64_t rows, int64_t vocab, int64_t width,
@@ -78,8 +78,8 @@ int mesa_embedding_backward(const void* token, int token_bytes, const void* dy, 
     if (!isfinite(scale)) return MESA_ERR_ARG;
     if (vocab == 0 || width == 0 || (rows == 0 && accumulate != 0)) return MESA_OK;
     if (!stride_ok(rows, width, dy_stride) || !stride_ok(vocab, width, dtable_stride)) return MESA_ERR_SHAPE;
-    if (dtable == nullptr || workspace == nullptr || (rows > 0 && any_null({token, dy}))) return MESA_ERR_NULL;
     const size_t need = mesa_embedding_backward_workspace_bytes(rows, vocab, width);
+    if (dtable == nullptr || (need > 0 && workspace == nullptr) || (rows > 0 && any_null({token, dy}))) return MESA_ERR_NULL;
     if (workspace_bytes < need) return MESA_ERR_WORKSPACE;
     if (!aligned(dy, bytes_of(grad_dtype)) || !aligned(dtable, bytes_of(table_dtype)) || !aligned(token, token_bytes) || !aligned(workspace, 16))
         return MESA_ERR_ARG;

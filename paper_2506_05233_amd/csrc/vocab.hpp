@@ -33,7 +33,7 @@ struct EmbeddingGradArgs {
     void* dtable;
     char* workspace;          // embedding_grad_bytes, 16-byte aligned
 };
-int64_t embedding_grad_bytes(int64_t rows, int64_t vocab, int64_t width);
+int64_t embedding_grad_bytes(int64_t rows, int64_t width);
 hipError_t launch_embedding_grad(const EmbeddingGradArgs& a, hipStream_t stream);
 
 struct CrossEntropyArgs {

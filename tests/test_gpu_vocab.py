@@ -89,7 +89,8 @@ def test_embedding_shapes_and_values():
 # ------------------------------------------------------------------ its gradient
 @pytest.mark.parametrize("rows,vocab,width,pad", [
     (1, 1, 1, 0), (1, 5003, 64, 0), (33, 1, 8, 0), (64, 3, 40, 0), (777, 5003, 321, 0), (2048, 50, 64, 0), (2049, 50, 64, 8),
-    (2100, 600, 72, 3), (5000, 300, 16, 0), (9000, 70000, 8, 0), (3000, 2, 24, 0), (70, 140000, 4, 0), (4100, 270000, 8, 0)])
+    (2100, 600, 72, 3), (5000, 300, 16, 0), (9000, 70000, 8, 0), (3000, 2, 24, 0), (70, 140000, 4, 0), (4100, 270000, 8, 0),
+    (16384, 40, 8, 0), (16385, 1000, 8, 0), (40000, 300, 9, 1)])
 @pytest.mark.parametrize("dtype,out", [(F32, F32), (BF16, BF16), (BF16, F32), (F32, BF16)])
 def test_embedding_backward(rows, vocab, width, pad, dtype, out):
     rng = np.random.default_rng(rows + vocab)
@@ -116,9 +117,9 @@ def test_embedding_backward(rows, vocab, width, pad, dtype, out):
     assert torch.equal(room[quiet], base[quiet]) and torch.equal(room[:, width:], base[:, width:])
 
 
-@pytest.mark.parametrize("rows", [31, 32, 33, 1023, 1024, 1025, 3000, 5000])
+@pytest.mark.parametrize("rows", [15, 16, 17, 511, 512, 513, 3000, 5000, 16384, 16385, 17000, 33793, 40000])
 def test_one_token_everywhere(rows):
-    """Every row the same token, at lengths around whole pieces of 32 and of 1024 sorted positions."""
+    """Every row the same token, at lengths around whole pieces of 16 and runs of 512 sorted positions."""
     rng = np.random.default_rng(rows)
     dy = _table(rng, rows, 40, F32)
     t = np.full(rows, 2)
