@@ -6,6 +6,7 @@
 // Three matrix products (2 rows vocab width operations each; the logits' one twice, since they are
 // formed again for the gradient), on the bf16 matrix cores (bf16_product.hpp).
 #include <algorithm>
+#include <type_traits>
 
 #include "bf16_product.hpp"
 #include "mesa_kernels.hpp"
@@ -17,10 +18,24 @@ namespace {
 
 constexpr float kInf = __builtin_inff();
 
-using Wide = TileShape<256, 256, 2, 4>;
-using Middle = TileShape<128, 128, 2, 2>;
-using Narrow = TileShape<64, 64, 2, 2>;      // tokens are the second size
-using Thin = TileShape<64, 32, 4, 1>;
+// Tiles of the three products: rows of the table or channels by rows of h or of the table.
+template <int Planes>
+struct Shapes;
+template <>
+struct Shapes<1> {
+    using Wide = TileShape<1, 256, 256, 2, 4>;
+    using Middle = TileShape<1, 128, 128, 2, 2>;
+    using Narrow = TileShape<1, 64, 64, 2, 2>;
+    using Thin = TileShape<1, 64, 32, 4, 1>;
+};
+template <>
+struct Shapes<3> {
+    using Wide = TileShape<3, 128, 256, 2, 4>;
+    using Middle = TileShape<3, 128, 128, 2, 4>;
+    using Narrow = TileShape<3, 64, 64, 2, 2>;
+    using Thin = Narrow;
+};
+constexpr int kStepK = 64;      // rows that the products read are filled up to a multiple of this
 
 int64_t ceil_to(int64_t x, int64_t n) { return (x + n - 1) / n * n; }
 int64_t ceil_div(int64_t x, int64_t n) { return (x + n - 1) / n; }
@@ -51,11 +66,14 @@ __device__ __forceinline__ void three_parts(float x, uint32_t (&p)[3])
     p[2] = pack_bf16(a - __uint_as_float(p[1] << 16), 0.0f);
 }
 
-// Eight consecutive channels a thread, out_rows x ld of them; what x does not hold is zero.
+// Eight consecutive channels a thread, out_rows x ld of them; what x does not hold is zero.  One or two
+// matrices a launch.
 template <typename T>
-__global__ void __launch_bounds__(kPackThreads) pack_planes_kernel(PackArgs a)
+__global__ void __launch_bounds__(kPackThreads) pack_planes_kernel(PackArgs one, PackArgs two, unsigned blocks_one)
 {
-    const int64_t i = int64_t(blockIdx.x) * kPackThreads + threadIdx.x;
+    const bool first = blockIdx.x < blocks_one;
+    const PackArgs& a = first ? one : two;
+    const int64_t i = int64_t(blockIdx.x - (first ? 0 : blocks_one)) * kPackThreads + threadIdx.x;
     const int64_t per = a.ld / 8;
     if (i >= a.out_rows * per) return;
     const int64_t row = i / per, c = i % per * 8;
@@ -100,14 +118,17 @@ __global__ void __launch_bounds__(kPackThreads) pack_planes_kernel(PackArgs a)
     }
 }
 
-hipError_t pack_planes(const PackArgs& a, int dtype, hipStream_t stream)
+// Either may have no rows.
+hipError_t pack_planes(const PackArgs& one, const PackArgs& two, int dtype, hipStream_t stream)
 {
-    const int64_t blocks = ceil_div(a.out_rows * (a.ld / 8), kPackThreads);
-    if (!grid_fits(blocks, kPackThreads)) return hipErrorInvalidConfiguration;
+    const int64_t b1 = ceil_div(one.out_rows * (one.ld / 8), kPackThreads), b2 = ceil_div(two.out_rows * (two.ld / 8), kPackThreads);
+    if (b1 + b2 == 0) return hipSuccess;
+    if (!grid_fits(b1 + b2, kPackThreads)) return hipErrorInvalidConfiguration;
+    const dim3 grid(unsigned(b1 + b2)), block(kPackThreads);
     if (dtype == kBf16)
-        hipLaunchKernelGGL((pack_planes_kernel<bf16_t>), dim3(unsigned(blocks)), dim3(kPackThreads), 0, stream, a);
+        hipLaunchKernelGGL((pack_planes_kernel<bf16_t>), grid, block, 0, stream, one, two, unsigned(b1));
     else
-        hipLaunchKernelGGL((pack_planes_kernel<float>), dim3(unsigned(blocks)), dim3(kPackThreads), 0, stream, a);
+        hipLaunchKernelGGL((pack_planes_kernel<float>), grid, block, 0, stream, one, two, unsigned(b1));
     return hipGetLastError();
 }
 
@@ -172,8 +193,7 @@ __device__ __forceinline__ int row_pair_min(int v)
 
 struct LogitsArgs {
     Matrix table, h;          // from the piece's first row of the table on
-    int pairs;
-    int64_t steps;            // of 64 channels
+    int64_t width;
     int64_t first, vocab;     // the piece's first row; rows of the whole table
     int64_t piece;            // rows of the piece
     int64_t rows;
@@ -198,12 +218,12 @@ struct LogitsArgs {
 template <class S>
 __global__ void __launch_bounds__(S::kThreads) logits_kernel(LogitsArgs a)
 {
-    __shared__ __attribute__((aligned(16))) uint16_t lds[S::kLds];
+    __shared__ __attribute__((aligned(16))) uint16_t lds[S::kBuffer], odd[S::kBuffer];
     int64_t tm, tn;
-    tile_of(a.tiles_m, a.tiles_n, tm, tn);
+    tile_of(int(blockIdx.x), int(gridDim.x), a.tiles_m, a.tiles_n, tm, tn);
     const int64_t m0 = tm * S::M, n0 = tn * S::N;
     f32x4 acc[S::MT][S::NT];
-    Product<S, true, true>::run(a.table, m0, a.h, n0, 0, a.steps * kStepK, a.pairs, lds, acc);
+    Product<S, true, true>::run(a.table, m0, a.h, n0, 0, a.width, lds, odd, acc);
 
     const int lane = int(threadIdx.x) % kWave, g = lane / 16, n = lane % 16;
     const int wave = int(threadIdx.x) / kWave, wm = wave / S::WN, wn = wave % S::WN;
@@ -427,12 +447,12 @@ __device__ __forceinline__ void grads_near(f32x4 (&acc)[S::MT][S::NT], int j, co
 template <class S>
 __global__ void __launch_bounds__(S::kThreads) logits_grad_kernel(LogitsArgs a)
 {
-    __shared__ __attribute__((aligned(16))) uint16_t lds[S::kLds];
+    __shared__ __attribute__((aligned(16))) uint16_t lds[S::kBuffer], odd[S::kBuffer];
     int64_t tm, tn;
-    tile_of(a.tiles_m, a.tiles_n, tm, tn);
+    tile_of(int(blockIdx.x), int(gridDim.x), a.tiles_m, a.tiles_n, tm, tn);
     const int64_t m0 = tm * S::M, n0 = tn * S::N;
     f32x4 acc[S::MT][S::NT];
-    Product<S, true, true>::run(a.table, m0, a.h, n0, 0, a.steps * kStepK, a.pairs, lds, acc);
+    Product<S, true, true>::run(a.table, m0, a.h, n0, 0, a.width, lds, odd, acc);
 
     const int lane = int(threadIdx.x) % kWave, g = lane / 16, n = lane % 16;
     const int wave = int(threadIdx.x) / kWave, wm = wave / S::WN, wn = wave % S::WN;
@@ -489,7 +509,7 @@ __global__ void __launch_bounds__(S::kThreads) logits_grad_kernel(LogitsArgs a)
         if (row >= a.dz_rows) continue;
         uint16_t* dst = a.dz + row * a.dz_ld + c0 + 4 * g;
         // rounded to bf16 once for both products: 2^-8 of an element at most, at random over the sums
-        if (a.pairs == 1) {
+        if constexpr (S::Planes == 1) {
 #pragma unroll
             for (int i = 0; i < S::MT; ++i)
                 *reinterpret_cast<uint2*>(dst + 16 * i) = make_uint2(pack_bf16(acc[i][j][0], acc[i][j][1]), pack_bf16(acc[i][j][2], acc[i][j][3]));
@@ -510,7 +530,6 @@ __global__ void __launch_bounds__(S::kThreads) logits_grad_kernel(LogitsArgs a)
 // out[n][m] = sum_k A(m, k) B(n, k): m a channel, n a row of dh or of the table's gradient.
 struct GradArgs {
     Matrix a, b;
-    int pairs;
     int64_t k, k_split;       // k of one launch layer, a multiple of 64 (blockIdx.y of them)
     int64_t tiles_m, tiles_n;
     int64_t width, n;         // of the result
@@ -536,15 +555,16 @@ __device__ __forceinline__ void put4(T* p, int n, bool wide, const f32x4& y)
         Lane4<T>::template store<false>(p, 0, n, x);
 }
 
-template <class S, bool AlongB, typename T>
+template <class S, bool AlongB>
 __global__ void __launch_bounds__(S::kThreads) grad_kernel(GradArgs a)
 {
-    __shared__ __attribute__((aligned(16))) uint16_t lds[S::kLds];
+    using T = std::conditional_t<S::Planes == 1, bf16_t, float>;
+    __shared__ __attribute__((aligned(16))) uint16_t lds[S::kBuffer], odd[S::kBuffer];
     int64_t tm, tn;
-    tile_of(a.tiles_m, a.tiles_n, tm, tn);
+    tile_of(int(blockIdx.x), int(gridDim.x), a.tiles_m, a.tiles_n, tm, tn);
     const int64_t m0 = tm * S::M, n0 = tn * S::N, k0 = int64_t(blockIdx.y) * a.k_split;
     f32x4 acc[S::MT][S::NT];
-    Product<S, false, AlongB, AlongB>::run(a.a, m0, a.b, n0, k0, min(k0 + a.k_split, a.k), a.pairs, lds, acc);
+    Product<S, false, AlongB, AlongB>::run(a.a, m0, a.b, n0, k0, min(k0 + a.k_split, a.k), lds, odd, acc);
 
     const int lane = int(threadIdx.x) % kWave, g = lane / 16, n = lane % 16;
     const int wave = int(threadIdx.x) / kWave, wm = wave / S::WN, wn = wave % S::WN;
@@ -614,27 +634,42 @@ __global__ void __launch_bounds__(kSumThreads) layer_sum_kernel(SumArgs a)
 }
 
 // ------------------------------------------------------------------ plans
-// Which tile a product of m by n takes: the largest that still gives every compute unit work.
-enum Shape { kWideShape, kMiddleShape, kNarrowShape, kThinShape };
-constexpr int64_t kShapeM[] = {Wide::M, Middle::M, Narrow::M, Thin::M}, kShapeN[] = {Wide::N, Middle::N, Narrow::N, Thin::N};
-
-Shape shape_of(int64_t m, int64_t n, int64_t layers)
+enum Shape { kWide, kMiddle, kNarrow, kThin };
+int planes_of(int dtype) { return dtype == kBf16 ? 1 : 3; }
+template <int Planes>
+int64_t shape_size(Shape s, bool n)
 {
-    if (n <= 32) return kThinShape;
-    if (n <= 64) return kNarrowShape;
-    if (ceil_div(m, 256) * ceil_div(n, 256) * layers >= 224) return kWideShape;
-    return ceil_div(m, 128) * ceil_div(n, 128) * layers >= 192 ? kMiddleShape : kNarrowShape;
+    using P = Shapes<Planes>;
+    const int64_t m_of[] = {P::Wide::M, P::Middle::M, P::Narrow::M, P::Thin::M}, n_of[] = {P::Wide::N, P::Middle::N, P::Narrow::N, P::Thin::N};
+    return n ? n_of[s] : m_of[s];
+}
+int64_t shape_m(Shape s, int planes) { return planes == 1 ? shape_size<1>(s, false) : shape_size<3>(s, false); }
+int64_t shape_n(Shape s, int planes) { return planes == 1 ? shape_size<1>(s, true) : shape_size<3>(s, true); }
+
+// Which tile a product of m by n in `layers` of k takes: the largest that still gives most compute units work.
+Shape shape_of(int64_t m, int64_t n, int64_t layers, int planes)
+{
+    if (n <= 32) return kThin;
+    auto tiles = [&](Shape s) { return ceil_div(m, shape_m(s, planes)) * ceil_div(n, shape_n(s, planes)) * layers; };
+    if (n > 64 && tiles(kWide) >= 180) return kWide;
+    return n > 64 && tiles(kMiddle) >= 160 ? kMiddle : kNarrow;
 }
 
-template <typename F>
+template <int Planes, typename F>
 hipError_t with_shape(Shape s, F f)
 {
+    using P = Shapes<Planes>;
     switch (s) {
-        case kWideShape: return f(Wide{});
-        case kMiddleShape: return f(Middle{});
-        case kNarrowShape: return f(Narrow{});
-        default: return f(Thin{});
+        case kWide: return f(typename P::Wide{});
+        case kMiddle: return f(typename P::Middle{});
+        case kNarrow: return f(typename P::Narrow{});
+        default: return f(typename P::Thin{});
     }
+}
+template <typename F>
+hipError_t with_shape(Shape s, int planes, F f)
+{
+    return planes == 1 ? with_shape<1>(s, f) : with_shape<3>(s, f);
 }
 
 // A table or h that the products read where it lies: bf16 rows of whole steps in 16-byte pieces.
@@ -648,8 +683,6 @@ constexpr int64_t kPieceBytes = int64_t(256) << 20;    // of dz at a time
 constexpr int64_t kSlabBytes = int64_t(256) << 20;     // of fp32 layers of one product, at most (or one layer)
 
 constexpr int64_t kUnits = 256;                        // compute units of the card
-
-int planes_of(int dtype) { return dtype == kBf16 ? 1 : 3; }
 
 // Rows of the table in a piece of the forward, where it has to be copied.
 int64_t copy_rows(int64_t vocab, int64_t width, int dtype)
@@ -674,7 +707,8 @@ struct ForwardPlan {
     {
         // whether the table is copied hangs on its address, so there is room for either way's tiles
         const int64_t copied = copy_rows(vocab, width, dtype);
-        tiles = std::max(ceil_div(vocab, kShapeM[shape_of(vocab, rows, 1)]), ceil_div(vocab, kShapeM[shape_of(copied, rows, 1)]));
+        const int planes = planes_of(dtype);
+        tiles = std::max(ceil_div(vocab, shape_m(shape_of(vocab, rows, 1, planes), planes)), ceil_div(vocab, shape_m(shape_of(copied, rows, 1, planes), planes)));
         Carve c;
         const int64_t row = ceil_to(width, kStepK) * 2 * planes_of(dtype);
         part = c.take(tiles * rows * 8);
@@ -689,36 +723,45 @@ struct ForwardPlan {
 
 struct GradPlan {
     int64_t piece, dz, dz_rows, dz_ld, h, table, slab_h, slab_e, bytes, ld;
-    int64_t h_layers, e_layers;
-    Shape logits, dh, de;
+    int64_t h_layers, e_layers, e_layers_last;
+    Shape logits, dh, de, de_last;
     GradPlan(int64_t rows, int64_t vocab, int64_t width, int dtype)
     {
-        const int64_t planes = planes_of(dtype);
+        const int planes = planes_of(dtype);
         ld = ceil_to(width, kStepK);
         dz_rows = ceil_to(rows, 64);
-        piece = std::min(ceil_to(vocab, 256), std::max<int64_t>(256, kPieceBytes / (dz_rows * 2 * planes) / 256 * 256));
-        // pieces of about the same size
-        piece = ceil_to(ceil_div(vocab, ceil_div(vocab, piece)), 256);
+        piece = std::max<int64_t>(256, kPieceBytes / (dz_rows * 2 * planes) / 256 * 256);
+        // pieces whose part of the table's gradient is whole rounds of wide tiles on all compute units, where they are
+        // large enough for that; else pieces of about the same size
+        const int64_t round = std::max<int64_t>(1, kUnits / ceil_div(width, shape_m(kWide, planes))) * shape_n(kWide, planes);
+        if (vocab <= piece)
+            piece = ceil_to(vocab, 256);
+        else
+            piece = piece >= round ? piece / round * round : ceil_to(ceil_div(vocab, ceil_div(vocab, piece)), 256);
         dz_ld = piece;
-        logits = shape_of(piece, rows, 1);
-        h_layers = layers(width, rows, piece, dh);
-        e_layers = layers(width, piece, rows, de);
+        logits = shape_of(piece, rows, 1, planes);
+        h_layers = layers(width, rows, piece, planes, dh);
+        e_layers = layers(width, piece, rows, planes, de);
+        // the last piece may be much shorter, and is then cut into more layers
+        const int64_t rest = vocab - (ceil_div(vocab, piece) - 1) * piece;
+        e_layers_last = layers(width, rest, rows, planes, de_last);
         Carve c;
         h = c.take(dz_rows * ld * 2 * planes);
         table = c.take(piece * ld * 2 * planes);
         dz = c.take(dz_rows * dz_ld * 2 * planes);
         slab_h = h_layers > 1 || piece < vocab ? c.take(h_layers * rows * ld * 4) : 0;
-        slab_e = e_layers > 1 ? c.take(e_layers * piece * ld * 4) : 0;
+        slab_e = e_layers > 1 || e_layers_last > 1 ? c.take(std::max(e_layers > 1 ? e_layers * piece : 0, e_layers_last > 1 ? e_layers_last * rest : 0) * ld * 4) : 0;
         bytes = c.at;
     }
-    // Into how many layers of k a product of m by n is cut: enough for two workgroups a compute unit,
-    // each of at least eight steps.
-    static int64_t layers(int64_t m, int64_t n, int64_t k, Shape& shape)
+    // Into how many layers of k a product of m by n is cut: no more than the workgroups that run at a time
+    // (one of wide tiles a compute unit, two, four), each of at least eight steps.
+    static int64_t layers(int64_t m, int64_t n, int64_t k, int planes, Shape& shape)
     {
         const int64_t most = std::max<int64_t>(1, std::min(ceil_div(k, kStepK) / 8, kSlabBytes / (ceil_to(m, kStepK) * n * 4)));
-        shape = shape_of(m, n, most);
-        const int64_t tiles = ceil_div(m, kShapeM[shape]) * ceil_div(n, kShapeN[shape]);
-        return std::min(most, std::max<int64_t>(1, 2 * kUnits / tiles));
+        shape = shape_of(m, n, most, planes);
+        const int64_t tiles = ceil_div(m, shape_m(shape, planes)) * ceil_div(n, shape_n(shape, planes));
+        const int64_t at_once = kUnits * (shape == kWide ? 1 : shape == kMiddle ? (planes == 1 ? 2 : 1) : planes == 1 ? 4 : 3);
+        return std::min(most, std::max<int64_t>(1, at_once / tiles));
     }
 };
 
@@ -737,8 +780,7 @@ hipError_t launch_cross_entropy(const CrossEntropyArgs& a, hipStream_t stream)
     const int planes = planes_of(a.dtype);
     const int64_t ld = ceil_to(a.width, kStepK);
     LogitsArgs k{};
-    k.pairs = planes == 1 ? 1 : 6;
-    k.steps = ld / kStepK;
+    k.width = a.width;
     k.vocab = a.vocab;
     k.rows = a.rows;
     k.targets = a.targets;
@@ -747,33 +789,35 @@ hipError_t launch_cross_entropy(const CrossEntropyArgs& a, hipStream_t stream)
     k.best_z = a.best == nullptr ? nullptr : reinterpret_cast<float*>(a.workspace + plan.best_z);
     k.best_v = reinterpret_cast<int32_t*>(a.workspace + plan.best_v);
     k.at = a.targets.p == nullptr ? nullptr : reinterpret_cast<float*>(a.workspace + plan.at);
+    PackArgs h{};      // h is copied, if at all, along with the table's first piece
     if (direct(a.h, a.h_stride, a.width, a.dtype)) {
         k.h = Matrix{static_cast<const uint16_t*>(a.h), a.h_stride, 0, a.rows, a.width};
     } else {
         uint16_t* copy = reinterpret_cast<uint16_t*>(a.workspace + plan.h);
         k.h = Matrix{copy, ld, a.rows * ld, a.rows, ld};
-        const PackArgs p{a.h, a.rows, a.width, a.h_stride, Tokens{}, 0, copy, a.rows, ld, a.rows * ld};
-        if (hipError_t e = pack_planes(p, a.dtype, stream); e != hipSuccess) return e;
+        h = PackArgs{a.h, a.rows, a.width, a.h_stride, Tokens{}, 0, copy, a.rows, ld, a.rows * ld};
     }
     const bool as_is = direct(a.table, a.table_stride, a.width, a.dtype);
     const int64_t most = as_is ? a.vocab : copy_rows(a.vocab, a.width, a.dtype);
-    const Shape shape = shape_of(most, a.rows, 1);
-    k.tiles_n = ceil_div(a.rows, kShapeN[shape]);
+    const Shape shape = shape_of(most, a.rows, 1, planes);
+    k.tiles_n = ceil_div(a.rows, shape_n(shape, planes));
     for (int64_t first = 0; first < a.vocab; first += most) {
         k.first = first;
         k.piece = std::min(most, a.vocab - first);
-        k.tile0 = first / kShapeM[shape];
-        k.tiles_m = ceil_div(k.piece, kShapeM[shape]);
+        k.tile0 = first / shape_m(shape, planes);
+        k.tiles_m = ceil_div(k.piece, shape_m(shape, planes));
+        PackArgs table{};
         if (as_is) {
             k.table = Matrix{static_cast<const uint16_t*>(a.table), a.table_stride, 0, a.vocab, a.width};
         } else {
             uint16_t* copy = reinterpret_cast<uint16_t*>(a.workspace + plan.table);
             k.table = Matrix{copy, ld, most * ld, k.piece, ld};
             const char* src = static_cast<const char*>(a.table) + first * a.table_stride * (planes == 1 ? 2 : 4);
-            const PackArgs p{src, k.piece, a.width, a.table_stride, Tokens{}, 0, copy, k.piece, ld, most * ld};
-            if (hipError_t e = pack_planes(p, a.dtype, stream); e != hipSuccess) return e;
+            table = PackArgs{src, k.piece, a.width, a.table_stride, Tokens{}, 0, copy, k.piece, ld, most * ld};
         }
-        const hipError_t e = with_shape(shape, [&](auto s) {
+        if (hipError_t e = pack_planes(h, table, a.dtype, stream); e != hipSuccess) return e;
+        h = PackArgs{};
+        const hipError_t e = with_shape(shape, planes, [&](auto s) {
             using S = decltype(s);
             if (!grid_fits(k.tiles_m * k.tiles_n, S::kThreads)) return hipErrorInvalidConfiguration;
             hipLaunchKernelGGL((logits_kernel<S>), dim3(unsigned(k.tiles_m * k.tiles_n)), dim3(S::kThreads), 0, stream, k);
@@ -782,7 +826,7 @@ hipError_t launch_cross_entropy(const CrossEntropyArgs& a, hipStream_t stream)
         if (e != hipSuccess) return e;
     }
     const JoinArgs j{k.part, k.best_z, k.best_v, k.at, a.targets, a.rows, a.vocab,
-                     ceil_div(a.vocab, kShapeM[shape]), a.targets.p == nullptr ? nullptr : a.loss, a.lse, a.best};
+                     ceil_div(a.vocab, shape_m(shape, planes)), a.targets.p == nullptr ? nullptr : a.loss, a.lse, a.best};
     // a workgroup for each of few rows; sixteen neighbours, whose sums lie side by side, of many
     const int64_t blocks = a.rows <= 1024 ? a.rows : ceil_div(a.rows, 16);
     if (!grid_fits(blocks, kJoinThreads)) return hipErrorInvalidConfiguration;
@@ -796,16 +840,12 @@ hipError_t launch_cross_entropy(const CrossEntropyArgs& a, hipStream_t stream)
 namespace {
 
 template <bool AlongB>
-hipError_t launch_grad(const GradArgs& k, Shape shape, int64_t layers, int dtype, hipStream_t stream)
+hipError_t launch_grad(const GradArgs& k, Shape shape, int64_t layers, int planes, hipStream_t stream)
 {
-    return with_shape(shape, [&](auto s) {
+    return with_shape(shape, planes, [&](auto s) {
         using S = decltype(s);
         if (!grid_fits(k.tiles_m * k.tiles_n, S::kThreads)) return hipErrorInvalidConfiguration;
-        const dim3 grid(unsigned(k.tiles_m * k.tiles_n), unsigned(layers)), block(S::kThreads);
-        if (dtype == kBf16)
-            hipLaunchKernelGGL((grad_kernel<S, AlongB, bf16_t>), grid, block, 0, stream, k);
-        else
-            hipLaunchKernelGGL((grad_kernel<S, AlongB, float>), grid, block, 0, stream, k);
+        hipLaunchKernelGGL((grad_kernel<S, AlongB>), dim3(unsigned(k.tiles_m * k.tiles_n), unsigned(layers)), dim3(S::kThreads), 0, stream, k);
         return hipGetLastError();
     });
 }
@@ -832,14 +872,12 @@ hipError_t launch_cross_entropy_grad(const CrossEntropyGradArgs& a, hipStream_t 
     }
     const GradPlan plan(a.rows, a.vocab, a.width, a.dtype);
     const int planes = planes_of(a.dtype);
-    const int pairs = planes == 1 ? 1 : 6;
     const int64_t ld = plan.ld, es = planes == 1 ? 2 : 4;
     char* ws = a.workspace;
     uint16_t* h = reinterpret_cast<uint16_t*>(ws + plan.h);
     uint16_t* dz = reinterpret_cast<uint16_t*>(ws + plan.dz);
     // h is copied always: rows that do not count may hold anything, and the products over rows would meet it
-    const PackArgs ph{a.h, a.rows, a.width, a.h_stride, a.targets, a.vocab, h, plan.dz_rows, ld, plan.dz_rows * ld};
-    if (hipError_t e = pack_planes(ph, a.dtype, stream); e != hipSuccess) return e;
+    PackArgs ph{a.h, a.rows, a.width, a.h_stride, a.targets, a.vocab, h, plan.dz_rows, ld, plan.dz_rows * ld};
     const bool as_is = direct(a.table, a.table_stride, a.width, a.dtype);
     const int64_t dz_plane = plan.dz_rows * plan.dz_ld;
 
@@ -848,19 +886,20 @@ hipError_t launch_cross_entropy_grad(const CrossEntropyGradArgs& a, hipStream_t 
         const bool last = first + piece == a.vocab;
         const char* src = static_cast<const char*>(a.table) + first * a.table_stride * es;
         Matrix table;
+        PackArgs pt{};
         if (as_is) {
             table = Matrix{reinterpret_cast<const uint16_t*>(src), a.table_stride, 0, piece, a.width};
         } else {
             uint16_t* copy = reinterpret_cast<uint16_t*>(ws + plan.table);
             table = Matrix{copy, ld, plan.piece * ld, piece, ld};
-            const PackArgs p{src, piece, a.width, a.table_stride, Tokens{}, 0, copy, piece, ld, plan.piece * ld};
-            if (hipError_t e = pack_planes(p, a.dtype, stream); e != hipSuccess) return e;
+            pt = PackArgs{src, piece, a.width, a.table_stride, Tokens{}, 0, copy, piece, ld, plan.piece * ld};
         }
+        if (hipError_t e = pack_planes(ph, pt, a.dtype, stream); e != hipSuccess) return e;
+        ph = PackArgs{};
         LogitsArgs k{};
         k.table = table;
         k.h = Matrix{h, ld, plan.dz_rows * ld, plan.dz_rows, ld};
-        k.pairs = pairs;
-        k.steps = ld / kStepK;
+        k.width = a.width;
         k.first = first;
         k.vocab = a.vocab;
         k.piece = piece;
@@ -873,9 +912,9 @@ hipError_t launch_cross_entropy_grad(const CrossEntropyGradArgs& a, hipStream_t 
         k.dz_ld = plan.dz_ld;
         k.dz_plane = dz_plane;
         k.dz_rows = plan.dz_rows;
-        k.tiles_m = ceil_div(piece, kShapeM[plan.logits]);
-        k.tiles_n = ceil_div(plan.dz_rows, kShapeN[plan.logits]);
-        hipError_t e = with_shape(plan.logits, [&](auto s) {
+        k.tiles_m = ceil_div(piece, shape_m(plan.logits, planes));
+        k.tiles_n = ceil_div(plan.dz_rows, shape_n(plan.logits, planes));
+        hipError_t e = with_shape(plan.logits, planes, [&](auto s) {
             using S = decltype(s);
             if (!grid_fits(k.tiles_m * k.tiles_n, S::kThreads)) return hipErrorInvalidConfiguration;
             hipLaunchKernelGGL((logits_grad_kernel<S>), dim3(unsigned(k.tiles_m * k.tiles_n)), dim3(S::kThreads), 0, stream, k);
@@ -888,11 +927,10 @@ hipError_t launch_cross_entropy_grad(const CrossEntropyGradArgs& a, hipStream_t 
             GradArgs d{};
             d.a = table;
             d.b = dz_rows;
-            d.pairs = pairs;
             d.k = piece;
             d.k_split = ceil_to(ceil_div(plan.piece, plan.h_layers), kStepK);
-            d.tiles_m = ceil_div(a.width, kShapeM[plan.dh]);
-            d.tiles_n = ceil_div(a.rows, kShapeN[plan.dh]);
+            d.tiles_m = ceil_div(a.width, shape_m(plan.dh, planes));
+            d.tiles_n = ceil_div(a.rows, shape_n(plan.dh, planes));
             d.width = a.width;
             d.n = a.rows;
             d.slab = slab ? reinterpret_cast<float*>(ws + plan.slab_h) : nullptr;
@@ -903,33 +941,34 @@ hipError_t launch_cross_entropy_grad(const CrossEntropyGradArgs& a, hipStream_t 
             d.out_stride = a.dh_stride;
             d.targets = a.targets;
             d.vocab = a.vocab;
-            if (e = launch_grad<true>(d, plan.dh, plan.h_layers, a.dtype, stream); e != hipSuccess) return e;
+            if (e = launch_grad<true>(d, plan.dh, plan.h_layers, planes, stream); e != hipSuccess) return e;
             if (last && plan.h_layers > 1) {
                 const SumArgs s{d.slab, ld, d.slab_layer, plan.h_layers, a.rows, a.width, a.dh, a.dh_stride, a.targets, a.vocab};
                 if (e = launch_sum(s, a.dtype, stream); e != hipSuccess) return e;
             }
         }
         if (a.dtable != nullptr) {
+            const int64_t layers = last ? plan.e_layers_last : plan.e_layers;
+            const Shape shape = last ? plan.de_last : plan.de;
             GradArgs d{};
             d.a = k.h;
             d.b = dz_rows;
-            d.pairs = pairs;
             d.k = plan.dz_rows;
-            d.k_split = ceil_to(ceil_div(plan.dz_rows, plan.e_layers), kStepK);
-            d.tiles_m = ceil_div(a.width, kShapeM[plan.de]);
-            d.tiles_n = ceil_div(piece, kShapeN[plan.de]);
+            d.k_split = ceil_to(ceil_div(plan.dz_rows, layers), kStepK);
+            d.tiles_m = ceil_div(a.width, shape_m(shape, planes));
+            d.tiles_n = ceil_div(piece, shape_n(shape, planes));
             d.width = a.width;
             d.n = piece;
-            d.slab = plan.e_layers > 1 ? reinterpret_cast<float*>(ws + plan.slab_e) : nullptr;
+            d.slab = layers > 1 ? reinterpret_cast<float*>(ws + plan.slab_e) : nullptr;
             d.slab_ld = ld;
-            d.slab_layer = plan.piece * ld;
+            d.slab_layer = piece * ld;
             d.first = true;
             void* out = static_cast<char*>(a.dtable) + first * a.dtable_stride * es;
-            d.out = plan.e_layers == 1 ? out : nullptr;
+            d.out = layers == 1 ? out : nullptr;
             d.out_stride = a.dtable_stride;
-            if (e = launch_grad<false>(d, plan.de, plan.e_layers, a.dtype, stream); e != hipSuccess) return e;
-            if (plan.e_layers > 1) {
-                const SumArgs s{d.slab, ld, d.slab_layer, plan.e_layers, piece, a.width, out, a.dtable_stride, Tokens{}, 0};
+            if (e = launch_grad<false>(d, shape, layers, planes, stream); e != hipSuccess) return e;
+            if (layers > 1) {
+                const SumArgs s{d.slab, ld, d.slab_layer, layers, piece, a.width, out, a.dtable_stride, Tokens{}, 0};
                 if (e = launch_sum(s, a.dtype, stream); e != hipSuccess) return e;
             }
         }
