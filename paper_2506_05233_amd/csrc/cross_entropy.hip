@@ -218,18 +218,19 @@ struct LogitsArgs {
 template <class S>
 __global__ void __launch_bounds__(S::kThreads) logits_kernel(LogitsArgs a)
 {
-    __shared__ __attribute__((aligned(16))) uint16_t lds[S::kBuffer], odd[S::kBuffer];
-    int64_t tm, tn;
-    tile_of(int(blockIdx.x), int(gridDim.x), a.tiles_m, a.tiles_n, tm, tn);
-    const int64_t m0 = tm * S::M, n0 = tn * S::N;
+    __shared__ __attribute__((aligned(16))) uint16_t even[S::kBuffer], odd[S::kBuffer];
+    int tm, tn;
+    tile_of(int(a.tiles_m), int(a.tiles_n), tm, tn);
     f32x4 acc[S::MT][S::NT];
-    Product<S, true, true>::run(a.table, m0, a.h, n0, 0, a.width, lds, odd, acc);
+    Product<S, true, true>::run(a.table, a.h, tm, tn, 0, a.width, even, odd, acc);
 
+    float* red = reinterpret_cast<float*>(even);
+    const int64_t m0 = int64_t(tm) * S::M, n0 = int64_t(tn) * S::N;
     const int lane = int(threadIdx.x) % kWave, g = lane / 16, n = lane % 16;
     const int wave = int(threadIdx.x) / kWave, wm = wave / S::WN, wn = wave % S::WN;
     const int64_t v0 = a.first + m0 + wm * S::MT * 16;      // the wave's first row of the table
     const int here = int(min(a.first + a.piece - v0, int64_t(S::MT * 16)));     // its rows that exist (0 or less: none)
-    float* red_m = reinterpret_cast<float*>(lds);           // [WM][N]
+    float* red_m = red;           // [WM][N]
     float* red_s = red_m + S::WM * S::N;
     float* red_z = red_s + S::WM * S::N;
     int* red_v = reinterpret_cast<int*>(red_z + S::WM * S::N);
@@ -447,13 +448,13 @@ __device__ __forceinline__ void grads_near(f32x4 (&acc)[S::MT][S::NT], int j, co
 template <class S>
 __global__ void __launch_bounds__(S::kThreads) logits_grad_kernel(LogitsArgs a)
 {
-    __shared__ __attribute__((aligned(16))) uint16_t lds[S::kBuffer], odd[S::kBuffer];
-    int64_t tm, tn;
-    tile_of(int(blockIdx.x), int(gridDim.x), a.tiles_m, a.tiles_n, tm, tn);
-    const int64_t m0 = tm * S::M, n0 = tn * S::N;
+    __shared__ __attribute__((aligned(16))) uint16_t even[S::kBuffer], odd[S::kBuffer];
+    int tm, tn;
+    tile_of(int(a.tiles_m), int(a.tiles_n), tm, tn);
     f32x4 acc[S::MT][S::NT];
-    Product<S, true, true>::run(a.table, m0, a.h, n0, 0, a.width, lds, odd, acc);
+    Product<S, true, true>::run(a.table, a.h, tm, tn, 0, a.width, even, odd, acc);
 
+    const int64_t m0 = int64_t(tm) * S::M, n0 = int64_t(tn) * S::N;
     const int lane = int(threadIdx.x) % kWave, g = lane / 16, n = lane % 16;
     const int wave = int(threadIdx.x) / kWave, wm = wave / S::WN, wn = wave % S::WN;
     const int64_t c0 = m0 + wm * S::MT * 16;                // the wave's first column of dz
@@ -530,7 +531,7 @@ __global__ void __launch_bounds__(S::kThreads) logits_grad_kernel(LogitsArgs a)
 // out[n][m] = sum_k A(m, k) B(n, k): m a channel, n a row of dh or of the table's gradient.
 struct GradArgs {
     Matrix a, b;
-    int64_t k, k_split;       // k of one launch layer, a multiple of 64 (blockIdx.y of them)
+    int64_t k, k_split;       // k of a layer, a multiple of 64: blockIdx.y of them, none empty
     int64_t tiles_m, tiles_n;
     int64_t width, n;         // of the result
     // fp32 sums on the way: [layer][n][slab_ld], written (first) or added to; null: none
@@ -559,13 +560,14 @@ template <class S, bool AlongB>
 __global__ void __launch_bounds__(S::kThreads) grad_kernel(GradArgs a)
 {
     using T = std::conditional_t<S::Planes == 1, bf16_t, float>;
-    __shared__ __attribute__((aligned(16))) uint16_t lds[S::kBuffer], odd[S::kBuffer];
-    int64_t tm, tn;
-    tile_of(int(blockIdx.x), int(gridDim.x), a.tiles_m, a.tiles_n, tm, tn);
-    const int64_t m0 = tm * S::M, n0 = tn * S::N, k0 = int64_t(blockIdx.y) * a.k_split;
+    __shared__ __attribute__((aligned(16))) uint16_t even[S::kBuffer], odd[S::kBuffer];
+    int tm, tn;
+    tile_of(int(a.tiles_m), int(a.tiles_n), tm, tn);
+    const int64_t k0 = int64_t(blockIdx.y) * a.k_split;
     f32x4 acc[S::MT][S::NT];
-    Product<S, false, AlongB, AlongB>::run(a.a, m0, a.b, n0, k0, min(k0 + a.k_split, a.k), lds, odd, acc);
+    Product<S, false, AlongB, AlongB>::run(a.a, a.b, tm, tn, k0, min(k0 + a.k_split, a.k), even, odd, acc);
 
+    const int64_t m0 = int64_t(tm) * S::M, n0 = int64_t(tn) * S::N;
     const int lane = int(threadIdx.x) % kWave, g = lane / 16, n = lane % 16;
     const int wave = int(threadIdx.x) / kWave, wm = wave / S::WN, wn = wave % S::WN;
     // four channels in one access: the rows' pitch and the base allow it (the slab's always do)
@@ -634,6 +636,8 @@ __global__ void __launch_bounds__(kSumThreads) layer_sum_kernel(SumArgs a)
 }
 
 // ------------------------------------------------------------------ plans
+constexpr int64_t kUnits = 256;      // compute units of the card
+
 enum Shape { kWide, kMiddle, kNarrow, kThin };
 int planes_of(int dtype) { return dtype == kBf16 ? 1 : 3; }
 template <int Planes>
@@ -682,7 +686,6 @@ constexpr int64_t kCopyBytes = int64_t(64) << 20;      // of the table's rows in
 constexpr int64_t kPieceBytes = int64_t(256) << 20;    // of dz at a time
 constexpr int64_t kSlabBytes = int64_t(256) << 20;     // of fp32 layers of one product, at most (or one layer)
 
-constexpr int64_t kUnits = 256;                        // compute units of the card
 
 // Rows of the table in a piece of the forward, where it has to be copied.
 int64_t copy_rows(int64_t vocab, int64_t width, int dtype)
@@ -929,6 +932,7 @@ hipError_t launch_cross_entropy_grad(const CrossEntropyGradArgs& a, hipStream_t 
             d.b = dz_rows;
             d.k = piece;
             d.k_split = ceil_to(ceil_div(plan.piece, plan.h_layers), kStepK);
+            const int64_t layers = ceil_div(std::min(plan.piece, a.vocab), d.k_split);      // that hold something
             d.tiles_m = ceil_div(a.width, shape_m(plan.dh, planes));
             d.tiles_n = ceil_div(a.rows, shape_n(plan.dh, planes));
             d.width = a.width;
@@ -937,24 +941,24 @@ hipError_t launch_cross_entropy_grad(const CrossEntropyGradArgs& a, hipStream_t 
             d.slab_ld = ld;
             d.slab_layer = a.rows * ld;
             d.first = first == 0;
-            d.out = plan.h_layers == 1 && last ? a.dh : nullptr;
+            d.out = layers == 1 && last ? a.dh : nullptr;
             d.out_stride = a.dh_stride;
             d.targets = a.targets;
             d.vocab = a.vocab;
-            if (e = launch_grad<true>(d, plan.dh, plan.h_layers, planes, stream); e != hipSuccess) return e;
-            if (last && plan.h_layers > 1) {
-                const SumArgs s{d.slab, ld, d.slab_layer, plan.h_layers, a.rows, a.width, a.dh, a.dh_stride, a.targets, a.vocab};
+            if (e = launch_grad<true>(d, plan.dh, ceil_div(d.k, d.k_split), planes, stream); e != hipSuccess) return e;
+            if (last && layers > 1) {
+                const SumArgs s{d.slab, ld, d.slab_layer, layers, a.rows, a.width, a.dh, a.dh_stride, a.targets, a.vocab};
                 if (e = launch_sum(s, a.dtype, stream); e != hipSuccess) return e;
             }
         }
         if (a.dtable != nullptr) {
-            const int64_t layers = last ? plan.e_layers_last : plan.e_layers;
             const Shape shape = last ? plan.de_last : plan.de;
             GradArgs d{};
             d.a = k.h;
             d.b = dz_rows;
             d.k = plan.dz_rows;
-            d.k_split = ceil_to(ceil_div(plan.dz_rows, layers), kStepK);
+            d.k_split = ceil_to(ceil_div(plan.dz_rows, last ? plan.e_layers_last : plan.e_layers), kStepK);
+            const int64_t layers = ceil_div(d.k, d.k_split);
             d.tiles_m = ceil_div(a.width, shape_m(shape, planes));
             d.tiles_n = ceil_div(piece, shape_n(shape, planes));
             d.width = a.width;
