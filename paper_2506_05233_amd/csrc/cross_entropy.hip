@@ -66,6 +66,23 @@ __device__ __forceinline__ void three_parts(float x, uint32_t (&p)[3])
     p[2] = pack_bf16(a - __uint_as_float(p[1] << 16), 0.0f);
 }
 
+// Eight consecutive values from an address that is aligned to an element only, which vector memory
+// instructions take as well.
+__device__ __forceinline__ void load8_unaligned(const float* p, float (&x)[8])
+{
+    typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+    const f32x4_any lo = reinterpret_cast<const f32x4_any*>(p)[0], hi = reinterpret_cast<const f32x4_any*>(p)[1];
+#pragma unroll
+    for (int v = 0; v < 4; ++v) x[v] = lo[v], x[v + 4] = hi[v];
+}
+__device__ __forceinline__ void load8_unaligned(const bf16_t* p, float (&x)[8])
+{
+    typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+    const u32x4_any w = *reinterpret_cast<const u32x4_any*>(p);
+#pragma unroll
+    for (int v = 0; v < 4; ++v) x[2 * v] = __uint_as_float(w[v] << 16), x[2 * v + 1] = __uint_as_float(w[v] & 0xFFFF0000u);
+}
+
 // Eight consecutive channels a thread, out_rows x ld of them; what x does not hold is zero.  One or two
 // matrices a launch.
 template <typename T>
@@ -76,7 +93,9 @@ __global__ void __launch_bounds__(kPackThreads) pack_planes_kernel(PackArgs one,
     const int64_t i = int64_t(blockIdx.x - (first ? 0 : blocks_one)) * kPackThreads + threadIdx.x;
     const int64_t per = a.ld / 8;
     if (i >= a.out_rows * per) return;
-    const int64_t row = i / per, c = i % per * 8;
+    // fewer than 2^32 threads a launch
+    const uint32_t at = uint32_t(i), row32 = at / uint32_t(per);
+    const int64_t row = row32, c = int64_t(at - row32 * uint32_t(per)) * 8;
     float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     bool counts = row < a.rows;
     if (counts && a.targets.p != nullptr) {
@@ -85,12 +104,8 @@ __global__ void __launch_bounds__(kPackThreads) pack_planes_kernel(PackArgs one,
     }
     if (counts) {
         const T* src = static_cast<const T*>(a.x) + row * a.stride + c;
-        if (c + 8 <= a.width && uintptr_t(src) % 16 == 0) {
-            float lo[4], hi[4];
-            Lane4<T>::widen(Lane4<T>::template load<true>(src, 0, 4), lo);
-            Lane4<T>::widen(Lane4<T>::template load<true>(src, 4, 4), hi);
-#pragma unroll
-            for (int v = 0; v < 4; ++v) x[v] = lo[v], x[v + 4] = hi[v];
+        if (c + 8 <= a.width) {
+            load8_unaligned(src, x);
         } else {
 #pragma unroll
             for (int v = 0; v < 8; ++v)
@@ -650,14 +665,50 @@ int64_t shape_size(Shape s, bool n)
 int64_t shape_m(Shape s, int planes) { return planes == 1 ? shape_size<1>(s, false) : shape_size<3>(s, false); }
 int64_t shape_n(Shape s, int planes) { return planes == 1 ? shape_size<1>(s, true) : shape_size<3>(s, true); }
 
-// Which tile a product of m by n in `layers` of k takes: the largest that still gives most compute units work.
-Shape shape_of(int64_t m, int64_t n, int64_t layers, int planes)
+// What a product takes with each tile shape, in us, fitted to 73 sizes of each type (33 to 4000 rows, 1000 to
+// 50257 of the table, 320 to 2048 channels), most of them within a tenth.  A tile alone on its compute unit takes
+// `alone` + `alone_step` a step of k; with as many as share a unit it takes `shared` + `shared_step` of the
+// unit's time.  What that decides, by measurement: 16 x 7 tiles of 128 against 8 x 4 of 256 (2000 x 777 by 50257) 195 us
+// against 165, but 4 tiles of 64 against one of 256 (1000 x 64 by 2048) 13 against 45; fp32 280 tiles of 128 on 256
+// units 65, 160 wide ones 55.
+struct Cost {
+    float alone, alone_step, shared, shared_step;
+    int per_unit;
+};
+constexpr Cost kCost[2][4] = {
+    {{13.0f, 1.15f, 9.1f, 1.49f, 1}, {7.0f, 0.66f, 2.6f, 0.47f, 2}, {4.2f, 0.42f, 0.73f, 0.174f, 5}, {4.0f, 0.40f, 0.6f, 0.12f, 6}},
+    {{9.7f, 1.68f, 6.7f, 2.13f, 1}, {7.2f, 0.96f, 3.4f, 1.25f, 1}, {4.5f, 0.58f, 0.74f, 0.426f, 3}, {4.5f, 0.58f, 0.74f, 0.426f, 3}}};
+
+float cost_of(Shape s, int planes, int64_t tiles, int64_t k)
 {
-    if (n <= 32) return kThin;
-    auto tiles = [&](Shape s) { return ceil_div(m, shape_m(s, planes)) * ceil_div(n, shape_n(s, planes)) * layers; };
-    if (n > 64 && tiles(kWide) >= 180) return kWide;
-    return n > 64 && tiles(kMiddle) >= 160 ? kMiddle : kNarrow;
+    const Cost& c = kCost[planes == 1 ? 0 : 1][s];
+    const float steps = float(ceil_div(k, step_k(planes))), alone = c.alone + c.alone_step * steps, shared = c.shared + c.shared_step * steps;
+    const int64_t each = ceil_div(tiles, kUnits), rounds = each / c.per_unit, rest = each % c.per_unit;
+    return float(rounds) * std::max(alone, shared * float(c.per_unit)) + (rest > 0 ? std::max(alone, shared * float(rest)) : 0.0f);
 }
+
+// How a product of m by n over k is cut: into tiles of a shape and, up to `most`, layers of k whose sums a
+// further launch adds up.
+struct Cut {
+    Shape shape;
+    int64_t layers;
+};
+Cut cut_of(int64_t m, int64_t n, int64_t k, int planes, int64_t most)
+{
+    Cut best{kThin, 1};
+    float least = 0.0f;
+    for (Shape s : {kWide, kMiddle, kNarrow, kThin}) {
+        if (s == kThin && n > 32) continue;      // it reads the table's rows once for 32 of the others
+        const int64_t tiles = ceil_div(m, shape_m(s, planes)) * ceil_div(n, shape_n(s, planes));
+        for (int64_t l = 1; l <= most; l += l < 4 ? 1 : l / 2) {
+            const float sum = l > 1 ? 5.0f + float(l) * float(m) * float(n) * 1e-6f : 0.0f;
+            const float t = cost_of(s, planes, tiles * l, ceil_div(k, l)) + sum;
+            if (least == 0.0f || t < least) least = t, best = {s, l};
+        }
+    }
+    return best;
+}
+Shape shape_of(int64_t m, int64_t n, int64_t k, int planes) { return cut_of(m, n, k, planes, 1).shape; }
 
 template <int Planes, typename F>
 hipError_t with_shape(Shape s, F f)
@@ -711,7 +762,7 @@ struct ForwardPlan {
         // whether the table is copied hangs on its address, so there is room for either way's tiles
         const int64_t copied = copy_rows(vocab, width, dtype);
         const int planes = planes_of(dtype);
-        tiles = std::max(ceil_div(vocab, shape_m(shape_of(vocab, rows, 1, planes), planes)), ceil_div(vocab, shape_m(shape_of(copied, rows, 1, planes), planes)));
+        tiles = std::max(ceil_div(vocab, shape_m(shape_of(vocab, rows, width, planes), planes)), ceil_div(vocab, shape_m(shape_of(copied, rows, width, planes), planes)));
         Carve c;
         const int64_t row = ceil_to(width, kStepK) * 2 * planes_of(dtype);
         part = c.take(tiles * rows * 8);
@@ -726,8 +777,8 @@ struct ForwardPlan {
 
 struct GradPlan {
     int64_t piece, dz, dz_rows, dz_ld, h, table, slab_h, slab_e, bytes, ld;
-    int64_t h_layers, e_layers, e_layers_last;
-    Shape logits, dh, de, de_last;
+    Shape logits;
+    Cut dh, de, de_last;
     GradPlan(int64_t rows, int64_t vocab, int64_t width, int dtype)
     {
         const int planes = planes_of(dtype);
@@ -742,29 +793,25 @@ struct GradPlan {
         else
             piece = piece >= round ? piece / round * round : ceil_to(ceil_div(vocab, ceil_div(vocab, piece)), 256);
         dz_ld = piece;
-        logits = shape_of(piece, rows, 1, planes);
-        h_layers = layers(width, rows, piece, planes, dh);
-        e_layers = layers(width, piece, rows, planes, de);
-        // the last piece may be much shorter, and is then cut into more layers
+        logits = shape_of(piece, rows, width, planes);
+        dh = layers(width, rows, std::min(piece, vocab), planes);
+        // the last piece may be much shorter, and is then cut otherwise
         const int64_t rest = vocab - (ceil_div(vocab, piece) - 1) * piece;
-        e_layers_last = layers(width, rest, rows, planes, de_last);
+        de = layers(width, std::min(piece, vocab), rows, planes);
+        de_last = layers(width, rest, rows, planes);
         Carve c;
         h = c.take(dz_rows * ld * 2 * planes);
         table = c.take(piece * ld * 2 * planes);
         dz = c.take(dz_rows * dz_ld * 2 * planes);
-        slab_h = h_layers > 1 || piece < vocab ? c.take(h_layers * rows * ld * 4) : 0;
-        slab_e = e_layers > 1 || e_layers_last > 1 ? c.take(std::max(e_layers > 1 ? e_layers * piece : 0, e_layers_last > 1 ? e_layers_last * rest : 0) * ld * 4) : 0;
+        slab_h = dh.layers > 1 || piece < vocab ? c.take(dh.layers * rows * ld * 4) : 0;
+        const int64_t layered = std::max(de.layers > 1 ? de.layers * piece : 0, de_last.layers > 1 ? de_last.layers * rest : 0);
+        slab_e = layered > 0 ? c.take(layered * ld * 4) : 0;
         bytes = c.at;
     }
-    // Into how many layers of k a product of m by n is cut: no more than the workgroups that run at a time
-    // (one of wide tiles a compute unit, two, four), each of at least eight steps.
-    static int64_t layers(int64_t m, int64_t n, int64_t k, int planes, Shape& shape)
+    // Layers have at least eight steps of 64, and there is room for their sums.
+    static Cut layers(int64_t m, int64_t n, int64_t k, int planes)
     {
-        const int64_t most = std::max<int64_t>(1, std::min(ceil_div(k, kStepK) / 8, kSlabBytes / (ceil_to(m, kStepK) * n * 4)));
-        shape = shape_of(m, n, most, planes);
-        const int64_t tiles = ceil_div(m, shape_m(shape, planes)) * ceil_div(n, shape_n(shape, planes));
-        const int64_t at_once = kUnits * (shape == kWide ? 1 : shape == kMiddle ? (planes == 1 ? 2 : 1) : planes == 1 ? 4 : 3);
-        return std::min(most, std::max<int64_t>(1, at_once / tiles));
+        return cut_of(m, n, k, planes, std::max<int64_t>(1, std::min(ceil_div(k, kStepK) / 8, kSlabBytes / (ceil_to(m, kStepK) * n * 4))));
     }
 };
 
@@ -802,7 +849,7 @@ hipError_t launch_cross_entropy(const CrossEntropyArgs& a, hipStream_t stream)
     }
     const bool as_is = direct(a.table, a.table_stride, a.width, a.dtype);
     const int64_t most = as_is ? a.vocab : copy_rows(a.vocab, a.width, a.dtype);
-    const Shape shape = shape_of(most, a.rows, 1, planes);
+    const Shape shape = shape_of(most, a.rows, a.width, planes);
     k.tiles_n = ceil_div(a.rows, shape_n(shape, planes));
     for (int64_t first = 0; first < a.vocab; first += most) {
         k.first = first;
@@ -926,15 +973,15 @@ hipError_t launch_cross_entropy_grad(const CrossEntropyGradArgs& a, hipStream_t 
         if (e != hipSuccess) return e;
         const Matrix dz_rows{dz, plan.dz_ld, dz_plane, plan.dz_rows, plan.dz_ld};
         if (a.dh != nullptr) {
-            const bool slab = plan.h_layers > 1 || plan.piece < a.vocab;
+            const bool slab = plan.dh.layers > 1 || plan.piece < a.vocab;
             GradArgs d{};
             d.a = table;
             d.b = dz_rows;
             d.k = piece;
-            d.k_split = ceil_to(ceil_div(plan.piece, plan.h_layers), kStepK);
+            d.k_split = ceil_to(ceil_div(std::min(plan.piece, a.vocab), plan.dh.layers), kStepK);
             const int64_t layers = ceil_div(std::min(plan.piece, a.vocab), d.k_split);      // that hold something
-            d.tiles_m = ceil_div(a.width, shape_m(plan.dh, planes));
-            d.tiles_n = ceil_div(a.rows, shape_n(plan.dh, planes));
+            d.tiles_m = ceil_div(a.width, shape_m(plan.dh.shape, planes));
+            d.tiles_n = ceil_div(a.rows, shape_n(plan.dh.shape, planes));
             d.width = a.width;
             d.n = a.rows;
             d.slab = slab ? reinterpret_cast<float*>(ws + plan.slab_h) : nullptr;
@@ -945,19 +992,20 @@ hipError_t launch_cross_entropy_grad(const CrossEntropyGradArgs& a, hipStream_t 
             d.out_stride = a.dh_stride;
             d.targets = a.targets;
             d.vocab = a.vocab;
-            if (e = launch_grad<true>(d, plan.dh, ceil_div(d.k, d.k_split), planes, stream); e != hipSuccess) return e;
+            if (e = launch_grad<true>(d, plan.dh.shape, ceil_div(d.k, d.k_split), planes, stream); e != hipSuccess) return e;
             if (last && layers > 1) {
                 const SumArgs s{d.slab, ld, d.slab_layer, layers, a.rows, a.width, a.dh, a.dh_stride, a.targets, a.vocab};
                 if (e = launch_sum(s, a.dtype, stream); e != hipSuccess) return e;
             }
         }
         if (a.dtable != nullptr) {
-            const Shape shape = last ? plan.de_last : plan.de;
+            const Cut cut = last ? plan.de_last : plan.de;
+            const Shape shape = cut.shape;
             GradArgs d{};
             d.a = k.h;
             d.b = dz_rows;
             d.k = plan.dz_rows;
-            d.k_split = ceil_to(ceil_div(plan.dz_rows, last ? plan.e_layers_last : plan.e_layers), kStepK);
+            d.k_split = ceil_to(ceil_div(plan.dz_rows, cut.layers), kStepK);
             const int64_t layers = ceil_div(d.k, d.k_split);
             d.tiles_m = ceil_div(a.width, shape_m(shape, planes));
             d.tiles_n = ceil_div(piece, shape_n(shape, planes));
