@@ -19,65 +19,76 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// V consecutive channels as fp32, V 8 (16-byte pieces or two of them, aligned) or 1.
+// Sixteen bytes at an address that is aligned to an element only, which vector memory instructions take as well.
+typedef uint32_t words_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef float floats_any __attribute__((ext_vector_type(4), aligned(4)));
+
+// V consecutive channels, V 8 or (rows of fewer) 1, as they lie in memory; widened when they are used.
 template <typename T, int V>
-__device__ __forceinline__ void load_channels(const T* p, float (&x)[V])
-{
-    if constexpr (V == 8) {
-        float lo[4], hi[4];
-        if constexpr (sizeof(T) == 2) {
-            const uint4 w = *reinterpret_cast<const uint4*>(p);
-            Lane4<T>::widen(make_uint2(w.x, w.y), lo);
-            Lane4<T>::widen(make_uint2(w.z, w.w), hi);
-        } else {
-            Lane4<T>::widen(reinterpret_cast<const float4*>(p)[0], lo);
-            Lane4<T>::widen(reinterpret_cast<const float4*>(p)[1], hi);
-        }
+struct Channels;
+template <>
+struct Channels<bf16_t, 8> {
+    words_any w;
+    __device__ __forceinline__ void load(const bf16_t* p) { w = *reinterpret_cast<const words_any*>(p); }
+    __device__ __forceinline__ void widen(float (&x)[8]) const
+    {
+#pragma unroll
+        for (int v = 0; v < 4; ++v) x[2 * v] = __uint_as_float(w[v] << 16), x[2 * v + 1] = __uint_as_float(w[v] & 0xFFFF0000u);
+    }
+};
+template <>
+struct Channels<float, 8> {
+    floats_any lo, hi;
+    __device__ __forceinline__ void load(const float* p) { lo = reinterpret_cast<const floats_any*>(p)[0], hi = reinterpret_cast<const floats_any*>(p)[1]; }
+    __device__ __forceinline__ void widen(float (&x)[8]) const
+    {
 #pragma unroll
         for (int v = 0; v < 4; ++v) x[v] = lo[v], x[v + 4] = hi[v];
-    } else {
-        x[0] = to_f32(*p);
-    }
-}
-template <typename T, int V>
-__device__ __forceinline__ void store_channels(T* p, const float (&y)[V])
-{
-    if constexpr (V == 8 && sizeof(T) == 2) {
-        *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
-    } else if constexpr (V == 8) {
-        reinterpret_cast<float4*>(p)[0] = make_float4(y[0], y[1], y[2], y[3]);
-        reinterpret_cast<float4*>(p)[1] = make_float4(y[4], y[5], y[6], y[7]);
-    } else if constexpr (sizeof(T) == 2) {
-        reinterpret_cast<uint16_t*>(p)[0] = uint16_t(pack_bf16(y[0], 0.0f));
-    } else {
-        *p = y[0];
-    }
-}
-
-// V consecutive channels as they lie in memory, until they are added.
-template <typename T, int V>
-struct Row {
-    typename Lane4<T>::Raw lo, hi;
-    __device__ __forceinline__ void load(const T* p)
-    {
-        lo = reinterpret_cast<const typename Lane4<T>::Raw*>(p)[0];
-        hi = reinterpret_cast<const typename Lane4<T>::Raw*>(p)[1];
-    }
-    __device__ __forceinline__ void add(float (&sum)[V]) const
-    {
-        float x[4], y[4];
-        Lane4<T>::widen(lo, x);
-        Lane4<T>::widen(hi, y);
-#pragma unroll
-        for (int v = 0; v < 4; ++v) sum[v] += x[v], sum[v + 4] += y[v];
     }
 };
 template <typename T>
-struct Row<T, 1> {
-    T x;
-    __device__ __forceinline__ void load(const T* p) { x = *p; }
-    __device__ __forceinline__ void add(float (&sum)[1]) const { sum[0] += to_f32(x); }
+struct Channels<T, 1> {
+    T t;
+    __device__ __forceinline__ void load(const T* p) { t = *p; }
+    __device__ __forceinline__ void widen(float (&x)[1]) const { x[0] = to_f32(t); }
 };
+template <typename T, int V>
+__device__ __forceinline__ void load_channels(const T* p, float (&x)[V])
+{
+    Channels<T, V> c;
+    c.load(p);
+    c.widen(x);
+}
+__device__ __forceinline__ void store_one(float* p, float y) { *p = y; }
+__device__ __forceinline__ void store_one(bf16_t* p, float y) { p->bits = uint16_t(pack_bf16(y, 0.0f)); }
+// Channels from `own` on.
+template <typename T, int V>
+__device__ __forceinline__ void store_channels(T* p, const float (&y)[V], int own)
+{
+    if (V == 1 || own > 0) {
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (v >= own) store_one(p + v, y[v]);
+    } else if constexpr (V == 8 && sizeof(T) == 2) {
+        *reinterpret_cast<words_any*>(p) = words_any{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7])};
+    } else if constexpr (V == 8) {
+        reinterpret_cast<floats_any*>(p)[0] = floats_any{y[0], y[1], y[2], y[3]};
+        reinterpret_cast<floats_any*>(p)[1] = floats_any{y[4], y[5], y[6], y[7]};
+    }
+}
+
+// Which channels a lane takes: V from `at` on, of which those before `own` are another lane's too (the
+// last V of a row whose width is no multiple of V) and not its to store.
+struct Place {
+    int64_t at;
+    int own;
+};
+template <int V>
+__device__ __forceinline__ Place place_of(int64_t c, int64_t width)
+{
+    const int64_t over = c + V - width;
+    return over > 0 ? Place{c - over, int(over)} : Place{c, 0};
+}
 
 // A row's lanes: a power of two, as many as it has pieces of V channels, at most the workgroup.
 struct Lanes {
@@ -93,12 +104,6 @@ Lanes lanes_for(int64_t width, int v)
     while (l.log2 < 8 && (int64_t(v) << l.log2) < width) ++l.log2;
     return l;
 }
-bool wide_rows(const void* p, int64_t stride, int64_t width, int dtype)
-{
-    const int64_t row = stride * (dtype == kBf16 ? 2 : 4);
-    return width % 8 == 0 && row % 16 == 0 && uintptr_t(p) % 16 == 0;
-}
-
 // ------------------------------------------------------------------ look-up
 template <typename T, typename O, int V, int Each>
 __global__ void __launch_bounds__(kThreads) embedding_kernel(EmbeddingArgs a, Lanes lanes)
@@ -107,13 +112,14 @@ __global__ void __launch_bounds__(kThreads) embedding_kernel(EmbeddingArgs a, La
     int64_t t[Each];
 #pragma unroll
     for (int e = 0; e < Each; ++e) t[e] = row0 + e < a.rows ? token_at(a.tokens, row0 + e) : -1;
-    for (int64_t c = int64_t(lanes.lane()) * V; c < a.width; c += int64_t(lanes.count()) * V) {
+    for (int64_t first = int64_t(lanes.lane()) * V; first < a.width; first += int64_t(lanes.count()) * V) {
+        const Place c = place_of<V>(first, a.width);
         float x[Each][V];
 #pragma unroll
         for (int e = 0; e < Each; ++e) {
 #pragma unroll
             for (int v = 0; v < V; ++v) x[e][v] = 0.0f;
-            if (t[e] >= 0 && t[e] < a.vocab) load_channels<T, V>(static_cast<const T*>(a.table) + t[e] * a.table_stride + c, x[e]);
+            if (t[e] >= 0 && t[e] < a.vocab) load_channels<T, V>(static_cast<const T*>(a.table) + t[e] * a.table_stride + c.at, x[e]);
         }
 #pragma unroll
         for (int e = 0; e < Each; ++e) {
@@ -121,7 +127,7 @@ __global__ void __launch_bounds__(kThreads) embedding_kernel(EmbeddingArgs a, La
             const bool there = t[e] >= 0 && t[e] < a.vocab;
 #pragma unroll
             for (int v = 0; v < V; ++v) x[e][v] = there ? x[e][v] * a.scale : 0.0f;
-            store_channels<O, V>(static_cast<O*>(a.out) + (row0 + e) * a.out_stride + c, x[e]);
+            store_channels<O, V>(static_cast<O*>(a.out) + (row0 + e) * a.out_stride + c.at, x[e], c.own);
         }
     }
 }
@@ -210,34 +216,29 @@ struct SortArgs {
 struct Fill {
     char* p;
     int64_t rows, bytes, pitch;      // bytes of a row, and between rows
-    int piece;                       // bytes of an access: 16, 4 or 2
+    int element;                     // bytes: 4 or 2
 };
+// `bytes` from p on by `threads` threads, of which this is the i-th.
+__device__ __forceinline__ void fill_bytes(char* p, int64_t bytes, int element, int64_t i, int64_t threads)
+{
+    const int64_t whole = bytes / 16;
+    for (int64_t k = i; k < whole; k += threads) *reinterpret_cast<words_any*>(p + 16 * k) = words_any{0u, 0u, 0u, 0u};
+    const int64_t at = 16 * whole + i * element;
+    if (at < bytes) {
+        if (element == 4)
+            *reinterpret_cast<uint32_t*>(p + at) = 0;
+        else
+            *reinterpret_cast<uint16_t*>(p + at) = 0;
+    }
+}
 __device__ __forceinline__ void fill_rows(const Fill& f, int64_t first)
 {
     const int64_t block = int64_t(blockIdx.x) - first, blocks = int64_t(gridDim.x) - first;
     if (f.bytes == f.pitch) {        // dense rows are one run
-        const int64_t n = f.rows * f.bytes / f.piece, step = blocks * blockDim.x;
-        for (int64_t i = block * blockDim.x + threadIdx.x; i < n; i += step) {
-            if (f.piece == 16)
-                reinterpret_cast<uint4*>(f.p)[i] = make_uint4(0, 0, 0, 0);
-            else if (f.piece == 4)
-                reinterpret_cast<uint32_t*>(f.p)[i] = 0;
-            else
-                reinterpret_cast<uint16_t*>(f.p)[i] = 0;
-        }
+        fill_bytes(f.p, f.rows * f.bytes, f.element, block * blockDim.x + threadIdx.x, blocks * blockDim.x);
         return;
     }
-    for (int64_t row = block; row < f.rows; row += blocks) {
-        char* p = f.p + row * f.pitch;
-        for (int64_t i = threadIdx.x; i < f.bytes / f.piece; i += blockDim.x) {
-            if (f.piece == 16)
-                reinterpret_cast<uint4*>(p)[i] = make_uint4(0, 0, 0, 0);
-            else if (f.piece == 4)
-                reinterpret_cast<uint32_t*>(p)[i] = 0;
-            else
-                reinterpret_cast<uint16_t*>(p)[i] = 0;
-        }
-    }
+    for (int64_t row = block; row < f.rows; row += blocks) fill_bytes(f.p + row * f.pitch, f.bytes, f.element, threadIdx.x, blockDim.x);
 }
 
 // How many keys of a tile have each value of a digit.
@@ -435,16 +436,16 @@ constexpr uint32_t kNoKey = 0xFFFFFFFFu;
 constexpr int64_t kRunRows = 16384;
 
 template <typename O, int V>
-__device__ __forceinline__ void write_row(const SumArgs& a, uint32_t token, int64_t c, float (&sum)[V])
+__device__ __forceinline__ void write_row(const SumArgs& a, uint32_t token, const Place& c, float (&sum)[V])
 {
-    O* dst = static_cast<O*>(a.dtable) + int64_t(token) * a.table_stride + c;
+    O* dst = static_cast<O*>(a.dtable) + int64_t(token) * a.table_stride + c.at;
     float x[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) x[v] = 0.0f;
     if (a.accumulate) load_channels<O, V>(dst, x);
 #pragma unroll
     for (int v = 0; v < V; ++v) x[v] += a.scale * sum[v];
-    store_channels<O, V>(dst, x);
+    store_channels<O, V>(dst, x, c.own);
 }
 
 // Each piece of sorted positions: its tokens' sums.
@@ -453,8 +454,9 @@ __global__ void __launch_bounds__(kThreads) token_piece_kernel(SumArgs a, Lanes 
 {
     const int64_t piece = int64_t(blockIdx.x) * lanes.rows() + lanes.row(), first = piece * kPiece;
     if (first >= a.rows) return;
-    const int64_t c = (int64_t(blockIdx.y) * lanes.count() + lanes.lane()) * V;
-    if (c >= a.width) return;
+    const int64_t from = (int64_t(blockIdx.y) * lanes.count() + lanes.lane()) * V;
+    if (from >= a.width) return;
+    const Place c = place_of<V>(from, a.width);
     const int n = int(min(int64_t(kPiece), a.rows - first));
     const uint32_t vocab = uint32_t(a.vocab);
     uint32_t key[kPiece], place[kPiece];
@@ -468,9 +470,9 @@ __global__ void __launch_bounds__(kThreads) token_piece_kernel(SumArgs a, Lanes 
     if (key[0] >= vocab) return;      // only rows that do not count from here on
     // every row of the piece is asked for before the first is added (in the place of a row that does not count,
     // all of which come last, the first one again, for a sum that is not kept)
-    Row<T, V> x[kPiece];
+    Channels<T, V> x[kPiece];
 #pragma unroll
-    for (int e = 0; e < kPiece; ++e) x[e].load(static_cast<const T*>(a.dy) + int64_t(key[e] < vocab ? place[e] : place[0]) * a.dy_stride + c);
+    for (int e = 0; e < kPiece; ++e) x[e].load(static_cast<const T*>(a.dy) + int64_t(key[e] < vocab ? place[e] : place[0]) * a.dy_stride + c.at);
     uint32_t token = key[0];
     bool begins = token != before;
     float sum[V];
@@ -480,7 +482,7 @@ __global__ void __launch_bounds__(kThreads) token_piece_kernel(SumArgs a, Lanes 
         if (begins && ends)
             write_row<O, V>(a, token, c, sum);
         else
-            store_channels<float, V>((begins ? a.left : a.entered) + piece * a.ld + c, sum);
+            store_channels<float, V>((begins ? a.left : a.entered) + piece * a.ld + c.at, sum, c.own);
     };
 #pragma unroll
     for (int e = 0; e < kPiece; ++e) {
@@ -491,7 +493,10 @@ __global__ void __launch_bounds__(kThreads) token_piece_kernel(SumArgs a, Lanes 
 #pragma unroll
             for (int v = 0; v < V; ++v) sum[v] = 0.0f;
         }
-        x[e].add(sum);
+        float y[V];
+        x[e].widen(y);
+#pragma unroll
+        for (int v = 0; v < V; ++v) sum[v] += y[v];
     }
     if (token < vocab) flush(token != after);
 }
@@ -505,20 +510,21 @@ __global__ void __launch_bounds__(kThreads) token_run_kernel(SumArgs a)
     const uint32_t k = a.keys[first - 1];
     if (k != a.keys[first + kPiece * kRun - 1] || k >= uint32_t(a.vocab)) return;
     const float* src = a.entered + int64_t(blockIdx.x) * kRun * a.ld;
-    for (int64_t c = int64_t(threadIdx.x) * V; c < a.width; c += kThreads * V) {
+    for (int64_t from = int64_t(threadIdx.x) * V; from < a.width; from += kThreads * V) {
+        const Place c = place_of<V>(from, a.width);
         float sum[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) sum[v] = 0.0f;
         for (int r = 0; r < kRun; r += kDepth) {
             float x[kDepth][V];
 #pragma unroll
-            for (int e = 0; e < kDepth; ++e) load_channels<float, V>(src + (r + e) * a.ld + c, x[e]);
+            for (int e = 0; e < kDepth; ++e) load_channels<float, V>(src + (r + e) * a.ld + c.at, x[e]);
 #pragma unroll
             for (int e = 0; e < kDepth; ++e)
 #pragma unroll
                 for (int v = 0; v < V; ++v) sum[v] += x[e][v];
         }
-        store_channels<float, V>(a.runs + int64_t(blockIdx.x) * a.ld + c, sum);
+        store_channels<float, V>(a.runs + int64_t(blockIdx.x) * a.ld + c.at, sum, c.own);
     }
 }
 
@@ -586,20 +592,21 @@ __global__ void __launch_bounds__(kThreads) token_join_kernel(SumArgs a, Lanes l
     if (token >= uint32_t(a.vocab) || a.keys[last + 1] != token) return;
     if (first > 0 && a.keys[first - 1] == token) return;      // it begins before
     const int64_t p0 = piece + 1, p1 = pieces_entered(a, token, last, lanes);
-    const int64_t c = (int64_t(blockIdx.y) * lanes.count() + lanes.lane()) * V;
-    if (c >= a.width) return;
+    const int64_t from = (int64_t(blockIdx.y) * lanes.count() + lanes.lane()) * V;
+    if (from >= a.width) return;
+    const Place c = place_of<V>(from, a.width);
     float sum[V];
-    load_channels<float, V>(a.left + piece * a.ld + c, sum);
+    load_channels<float, V>(a.left + piece * a.ld + c.at, sum);
     const int64_t r0 = (p0 + kRun - 1) / kRun, r1 = p1 / kRun;
     // a run is whole, the last one only if the token goes on to its end
     const bool runs = a.rows > kRunRows && r0 < r1;
     const int64_t r2 = runs && (r1 * kRun * kPiece > a.rows || a.keys[r1 * kRun * kPiece - 1] != token) ? r1 - 1 : r1;
     if (runs && r0 < r2) {
-        add_rows<V>(sum, a.entered + c, a.ld, p0, r0 * kRun);
-        add_rows<V>(sum, a.runs + c, a.ld, r0, r2);
-        add_rows<V>(sum, a.entered + c, a.ld, r2 * kRun, p1);
+        add_rows<V>(sum, a.entered + c.at, a.ld, p0, r0 * kRun);
+        add_rows<V>(sum, a.runs + c.at, a.ld, r0, r2);
+        add_rows<V>(sum, a.entered + c.at, a.ld, r2 * kRun, p1);
     } else {
-        add_rows<V>(sum, a.entered + c, a.ld, p0, p1);
+        add_rows<V>(sum, a.entered + c.at, a.ld, p0, p1);
     }
     write_row<O, V>(a, token, c, sum);
 }
@@ -647,7 +654,7 @@ hipError_t sums(const SumArgs& a, hipStream_t stream)
 
 hipError_t launch_embedding(const EmbeddingArgs& a, hipStream_t stream)
 {
-    const bool wide = wide_rows(a.table, a.table_stride, a.width, a.dtype) && wide_rows(a.out, a.out_stride, a.width, a.out_dtype);
+    const bool wide = a.width >= 8;
     if (a.dtype == kBf16 && a.out_dtype == kBf16) return wide ? lookup<bf16_t, bf16_t, 8>(a, stream) : lookup<bf16_t, bf16_t, 1>(a, stream);
     if (a.dtype == kBf16) return wide ? lookup<bf16_t, float, 8>(a, stream) : lookup<bf16_t, float, 1>(a, stream);
     if (a.out_dtype == kBf16) return wide ? lookup<float, bf16_t, 8>(a, stream) : lookup<float, bf16_t, 1>(a, stream);
@@ -675,14 +682,13 @@ hipError_t launch_embedding_grad(const EmbeddingGradArgs& a, hipStream_t stream)
     uint32_t* places[2] = {reinterpret_cast<uint32_t*>(ws + lay.places[0]), reinterpret_cast<uint32_t*>(ws + lay.places[1])};
     // the table's rows are filled with zeros in equal shares of the sort's launches
     const int64_t es = a.table_dtype == kBf16 ? 2 : 4, bytes = a.width * es, pitch = a.table_stride * es;
-    const int piece = bytes % 16 == 0 && pitch % 16 == 0 && uintptr_t(a.dtable) % 16 == 0 ? 16 : int(es);
     const int shares = a.rows <= kSortRounds * kSortThreads ? 1 : 2 * digits;
     int share = 0;
     int64_t blocks = 0;
     auto next_fill = [&](int threads) {
         const int64_t r0 = a.vocab * share / shares, r1 = a.vocab * (share + 1) / shares;
         ++share;
-        const Fill f{static_cast<char*>(a.dtable) + r0 * pitch, a.accumulate ? 0 : r1 - r0, bytes, pitch, piece};
+        const Fill f{static_cast<char*>(a.dtable) + r0 * pitch, a.accumulate ? 0 : r1 - r0, bytes, pitch, int(es)};
         // about 64 KB a workgroup, at most eight a compute unit
         blocks = std::min<int64_t>(ceil_to(f.rows * bytes, 65536) / 65536, 2048 * kThreads / threads);
         return f;
@@ -716,7 +722,8 @@ hipError_t launch_embedding_grad(const EmbeddingGradArgs& a, hipStream_t stream)
     const SumArgs k{a.dy, a.rows, a.vocab, a.width, a.dy_stride, a.table_stride, lay.ld, a.scale, a.accumulate, keys[out], places[out],
                     reinterpret_cast<float*>(ws + lay.entered), reinterpret_cast<float*>(ws + lay.left),
                     reinterpret_cast<float*>(ws + lay.runs), a.dtable};
-    const bool wide = wide_rows(a.dy, a.dy_stride, a.width, a.dtype) && wide_rows(a.dtable, a.table_stride, a.width, a.table_dtype);
+    // few rows have a lane for each channel: 777 rows of 321 take 17.6 us so, 19.2 with eight channels a lane
+    const bool wide = a.width >= 8 && a.rows * a.width >= (int64_t(1) << 19);
     if (a.dtype == kBf16 && a.table_dtype == kBf16) return wide ? sums<bf16_t, bf16_t, 8>(k, stream) : sums<bf16_t, bf16_t, 1>(k, stream);
     if (a.dtype == kBf16) return wide ? sums<bf16_t, float, 8>(k, stream) : sums<bf16_t, float, 1>(k, stream);
     if (a.table_dtype == kBf16) return wide ? sums<float, bf16_t, 8>(k, stream) : sums<float, bf16_t, 1>(k, stream);
