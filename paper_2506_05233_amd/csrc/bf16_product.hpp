@@ -1,7 +1,9 @@
 // Products of two bf16 matrices on the matrix cores (gfx950): the tile that a workgroup
 // computes, C[m][n] = sum_k A(m, k) B(n, k) in fp32, for operands that lie in memory either row by
-// row along k or, transposed, row by row along m or n.  Or of two fp32 matrices, each held as three
-// bf16 planes whose sum it is: six products of planes, the others being below 2^-24 of the whole.
+// row along k or, transposed, row by row along m or n.  Or of two fp32 matrices, each held as planes
+// whose sum it is: three of bf16, six products of which are formed (the others are below 2^-24 of the
+// whole), or two of fp16 (22 bits and a sign), three products (the fourth is below 2^-22, and 2^-24 as a
+// rule); the latter of rows scaled by a power of two into fp16's range.
 //
 // A step is 64 of k (of planes: 32).  Its operand tiles go from memory straight to LDS in 16-byte
 // pieces (no registers, no LDS store instructions), into one of two buffers while the other is
@@ -19,7 +21,7 @@
 
 namespace mesa {
 
-// A bf16 matrix in memory, or three planes of one, `plane` elements apart.
+// A matrix of 16-bit values in memory, or planes of one, `plane` elements apart.
 struct Matrix {
     const uint16_t* p;      // 16-byte aligned
     int64_t ld;             // elements between rows: a multiple of 8, below 2^22
@@ -138,7 +140,7 @@ __device__ __forceinline__ void tile_of(int tiles_m, int tiles_n, int& m, int& n
     n = group * kGroup + (in - m * wide);
 }
 
-// M x N of C by WM x WN waves, from bf16 (Planes 1) or fp32 (3).
+// M x N of C by WM x WN waves, from bf16 (Planes 1), or fp32 in two fp16 planes or three bf16 ones.
 template <int Planes_, int M_, int N_, int WM_, int WN_>
 struct TileShape {
     static constexpr int Planes = Planes_, M = M_, N = N_, WM = WM_, WN = WN_;
@@ -192,6 +194,16 @@ struct Product {
         }
     };
 
+    __device__ static __forceinline__ f32x4 matrix(const bf16x8& x, const bf16x8& y, const f32x4& c)
+    {
+        if constexpr (Planes == 2) {
+            typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+            return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, x), __builtin_bit_cast(f16x8, y), c, 0, 0, 0);
+        } else {
+            return mfma16(x, y, c);
+        }
+    }
+
     __device__ static __forceinline__ void read_one(const uint16_t* tiles, int r, int part, uint32_t a, uint32_t b, Operands& o)
     {
         if (r < S::NT)
@@ -226,7 +238,7 @@ struct Product {
             __builtin_amdgcn_sched_barrier(0);
             const int p = q / S::MT, i = q % S::MT;
 #pragma unroll
-            for (int j = 0; j < S::NT; ++j) acc[i][j] = mfma16(px[p]->x[i], py[p]->y[j], acc[i][j]);
+            for (int j = 0; j < S::NT; ++j) acc[i][j] = matrix(px[p]->x[i], py[p]->y[j], acc[i][j]);
             __builtin_amdgcn_sched_barrier(0);
         }
     }
@@ -248,6 +260,11 @@ struct Product {
             next.look_up();
             turn();
             phase<true, 1>({&second}, {&second}, later, other, 0, w, next, cur, acc);
+        } else if constexpr (Planes == 2) {
+            phase<false, 1>({&first}, {&first}, second, cur, 1, w, next, nullptr, acc);
+            next.look_up();
+            turn();
+            phase<true, 2>({&first, &second}, {&second, &first}, later, other, 0, w, next, cur, acc);
         } else {
             phase<false, 1>({&first}, {&first}, second, cur, 1, w, next, nullptr, acc);
             phase<false, 3>({&first, &second, &second}, {&second, &first, &second}, third, cur, 2, w, next, nullptr, acc);

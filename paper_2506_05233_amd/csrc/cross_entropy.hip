@@ -18,7 +18,8 @@ namespace {
 
 constexpr float kInf = __builtin_inff();
 
-// Tiles of the three products: rows of the table or channels by rows of h or of the table.
+// Tiles of the three products: rows of the table or channels by rows of h or of the table.  Planes 1:
+// bf16; of fp32, 2 (fp16) for the logits and 3 (bf16) for the gradients.
 template <int Planes>
 struct Shapes;
 template <>
@@ -27,6 +28,13 @@ struct Shapes<1> {
     using Middle = TileShape<1, 128, 128, 2, 2>;
     using Narrow = TileShape<1, 64, 64, 2, 2>;
     using Thin = TileShape<1, 64, 32, 4, 1>;
+};
+template <>
+struct Shapes<2> {
+    using Wide = TileShape<2, 128, 256, 2, 4>;
+    using Middle = TileShape<2, 128, 128, 2, 2>;
+    using Narrow = TileShape<2, 64, 64, 2, 2>;
+    using Thin = Narrow;
 };
 template <>
 struct Shapes<3> {
@@ -40,16 +48,16 @@ constexpr int kStepK = 64;      // rows that the products read are filled up to 
 int64_t ceil_to(int64_t x, int64_t n) { return (x + n - 1) / n * n; }
 int64_t ceil_div(int64_t x, int64_t n) { return (x + n - 1) / n; }
 
-// ------------------------------------------------------------------ operands in bf16 planes
+// ------------------------------------------------------------------ operands as the products read them
 constexpr int kPackThreads = 256;
 
 struct PackArgs {
-    const void* x;           // [rows] rows of width, stride apart
+    const uint16_t* x;       // [rows] rows of width, stride apart
     int64_t rows, width, stride;
     Tokens targets;          // p null: every row counts; else rows whose target is none come out as zeros
     int64_t vocab;
-    uint16_t* out;           // planes of [out_rows, ld]
-    int64_t out_rows, ld, plane;
+    uint16_t* out;           // [out_rows, ld]
+    int64_t out_rows, ld;
 };
 
 // The three parts of an fp32 value, whose sum it is: each the nearest bf16 to what the parts before
@@ -75,18 +83,9 @@ __device__ __forceinline__ void load8_unaligned(const float* p, float (&x)[8])
 #pragma unroll
     for (int v = 0; v < 4; ++v) x[v] = lo[v], x[v + 4] = hi[v];
 }
-__device__ __forceinline__ void load8_unaligned(const bf16_t* p, float (&x)[8])
-{
-    typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
-    const u32x4_any w = *reinterpret_cast<const u32x4_any*>(p);
-#pragma unroll
-    for (int v = 0; v < 4; ++v) x[2 * v] = __uint_as_float(w[v] << 16), x[2 * v + 1] = __uint_as_float(w[v] & 0xFFFF0000u);
-}
-
-// Eight consecutive channels a thread, out_rows x ld of them; what x does not hold is zero.  One or two
-// matrices a launch.
-template <typename T>
-__global__ void __launch_bounds__(kPackThreads) pack_planes_kernel(PackArgs one, PackArgs two, unsigned blocks_one)
+// bf16 rows as the products read them, eight consecutive channels a thread, out_rows x ld of them; what x
+// does not hold is zero.  One or two matrices a launch.
+__global__ void __launch_bounds__(kPackThreads) pack_copy_kernel(PackArgs one, PackArgs two, unsigned blocks_one)
 {
     const bool first = blockIdx.x < blocks_one;
     const PackArgs& a = first ? one : two;
@@ -96,54 +95,144 @@ __global__ void __launch_bounds__(kPackThreads) pack_planes_kernel(PackArgs one,
     // fewer than 2^32 threads a launch
     const uint32_t at = uint32_t(i), row32 = at / uint32_t(per);
     const int64_t row = row32, c = int64_t(at - row32 * uint32_t(per)) * 8;
-    float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     bool counts = row < a.rows;
     if (counts && a.targets.p != nullptr) {
         const int64_t t = token_at(a.targets, row);
         counts = t >= 0 && t < a.vocab;
     }
+    uint32_t w[4] = {0, 0, 0, 0};
     if (counts) {
-        const T* src = static_cast<const T*>(a.x) + row * a.stride + c;
+        const uint16_t* src = a.x + row * a.stride + c;
         if (c + 8 <= a.width) {
-            load8_unaligned(src, x);
+            typedef uint32_t words_any __attribute__((ext_vector_type(4), aligned(2)));
+            const words_any u = *reinterpret_cast<const words_any*>(src);
+#pragma unroll
+            for (int v = 0; v < 4; ++v) w[v] = u[v];
         } else {
 #pragma unroll
             for (int v = 0; v < 8; ++v)
-                if (c + v < a.width) x[v] = to_f32(src[v]);
+                if (c + v < a.width) w[v / 2] |= uint32_t(src[v]) << (16 * (v % 2));
         }
     }
-    uint16_t* dst = a.out + row * a.ld + c;
-    if constexpr (sizeof(T) == 2) {
-        uint32_t w[4];
-#pragma unroll
-        for (int v = 0; v < 4; ++v) w[v] = __float_as_uint(x[2 * v]) >> 16 | (__float_as_uint(x[2 * v + 1]) & 0xFFFF0000u);
-        *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
-    } else {
-        uint32_t w[3][4];
-#pragma unroll
-        for (int v = 0; v < 4; ++v) {
-            uint32_t p[3], q[3];
-            three_parts(x[2 * v], p);
-            three_parts(x[2 * v + 1], q);
-#pragma unroll
-            for (int k = 0; k < 3; ++k) w[k][v] = p[k] | q[k] << 16;
-        }
-#pragma unroll
-        for (int k = 0; k < 3; ++k) *reinterpret_cast<uint4*>(dst + k * a.plane) = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
-    }
+    *reinterpret_cast<uint4*>(a.out + row * a.ld + c) = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 // Either may have no rows.
-hipError_t pack_planes(const PackArgs& one, const PackArgs& two, int dtype, hipStream_t stream)
+hipError_t pack_copy(const PackArgs& one, const PackArgs& two, hipStream_t stream)
 {
     const int64_t b1 = ceil_div(one.out_rows * (one.ld / 8), kPackThreads), b2 = ceil_div(two.out_rows * (two.ld / 8), kPackThreads);
     if (b1 + b2 == 0) return hipSuccess;
     if (!grid_fits(b1 + b2, kPackThreads)) return hipErrorInvalidConfiguration;
-    const dim3 grid(unsigned(b1 + b2)), block(kPackThreads);
-    if (dtype == kBf16)
-        hipLaunchKernelGGL((pack_planes_kernel<bf16_t>), grid, block, 0, stream, one, two, unsigned(b1));
-    else
-        hipLaunchKernelGGL((pack_planes_kernel<float>), grid, block, 0, stream, one, two, unsigned(b1));
+    hipLaunchKernelGGL(pack_copy_kernel, dim3(unsigned(b1 + b2)), dim3(kPackThreads), 0, stream, one, two, unsigned(b1));
+    return hipGetLastError();
+}
+
+// fp32 rows in planes, a wave a row: two fp16 planes of x 2^-e, e the power of two that brings the row's
+// largest magnitude into [2^14, 2^15), so that parts of elements down to 2^-18 of it are whole (the rest is
+// off by 2^-40 of it at most); and three bf16 planes, which need no scale and so serve sums along either way.
+struct RowArgs {
+    const float* x;          // [rows] rows of width, stride apart
+    int64_t rows, width, stride;
+    Tokens targets;          // as in PackArgs
+    int64_t vocab;
+    uint16_t* halves;        // two planes of [out_rows, ld]
+    int32_t* exponent;       // [exponents]: e, and zeros, which whole tiles read
+    int64_t exponents;
+    uint16_t* parts;         // three planes, or null
+    int64_t out_rows, ld;
+};
+
+__device__ __forceinline__ void two_halves(float x, int e, uint32_t& hi, uint32_t& lo)
+{
+    const float y = __builtin_ldexpf(x, -e);
+    const _Float16 h = _Float16(y);
+    const bool finite = (__float_as_uint(x) & 0x7F800000u) != 0x7F800000u;
+    const _Float16 l = finite ? _Float16(y - float(h)) : _Float16(0.0f);
+    hi = __builtin_bit_cast(uint16_t, h);
+    lo = __builtin_bit_cast(uint16_t, l);
+}
+
+__global__ void __launch_bounds__(kPackThreads) pack_rows_kernel(RowArgs one, RowArgs two, unsigned blocks_one)
+{
+    constexpr int kRows = kPackThreads / kWave;
+    const bool first = blockIdx.x < blocks_one;
+    const RowArgs& a = first ? one : two;
+    const int lane = int(threadIdx.x) % kWave;
+    const int64_t row = int64_t(blockIdx.x - (first ? 0 : blocks_one)) * kRows + threadIdx.x / kWave;
+    if (row >= a.out_rows) {
+        if (lane == 0 && row < a.exponents) a.exponent[row] = 0;
+        return;
+    }
+    bool counts = row < a.rows;
+    if (counts && a.targets.p != nullptr) {
+        const int64_t t = token_at(a.targets, row);
+        counts = t >= 0 && t < a.vocab;
+    }
+    const float* src = a.x + row * a.stride;
+    auto load = [&](int64_t c, float (&x)[8]) {
+#pragma unroll
+        for (int v = 0; v < 8; ++v) x[v] = 0.0f;
+        if (!counts) return;
+        if (c + 8 <= a.width) {
+            load8_unaligned(src + c, x);
+        } else {
+#pragma unroll
+            for (int v = 0; v < 8; ++v)
+                if (c + v < a.width) x[v] = src[c + v];
+        }
+    };
+    uint32_t most = 0;       // bits of the largest finite magnitude
+    for (int64_t c = int64_t(lane) * 8; c < a.width; c += kWave * 8) {
+        float x[8];
+        load(c, x);
+#pragma unroll
+        for (int v = 0; v < 8; ++v) {
+            const uint32_t u = abs_bits(x[v]);
+            most = u < 0x7F800000u ? max(most, u) : most;
+        }
+    }
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) most = max(most, uint32_t(__shfl_xor(int(most), d)));
+    // ilogb of it (of a subnormal by its fraction); a row of zeros is not scaled
+    const int e = most == 0 ? 0 : __builtin_amdgcn_frexp_expf(__uint_as_float(most)) - 1 - 14;
+    if (lane == 0) a.exponent[row] = e;
+    const int64_t plane = a.out_rows * a.ld;
+    for (int64_t c = int64_t(lane) * 8; c < a.ld; c += kWave * 8) {
+        float x[8];
+        load(c, x);
+        uint32_t w[5][4];
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            uint32_t h0, l0, h1, l1;
+            two_halves(x[2 * v], e, h0, l0);
+            two_halves(x[2 * v + 1], e, h1, l1);
+            w[0][v] = h0 | h1 << 16;
+            w[1][v] = l0 | l1 << 16;
+            if (a.parts != nullptr) {
+                uint32_t p[3], q[3];
+                three_parts(x[2 * v], p);
+                three_parts(x[2 * v + 1], q);
+#pragma unroll
+                for (int k = 0; k < 3; ++k) w[2 + k][v] = p[k] | q[k] << 16;
+            }
+        }
+        const int64_t to = row * a.ld + c;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) *reinterpret_cast<uint4*>(a.halves + k * plane + to) = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
+        if (a.parts != nullptr) {
+#pragma unroll
+            for (int k = 0; k < 3; ++k) *reinterpret_cast<uint4*>(a.parts + k * plane + to) = make_uint4(w[2 + k][0], w[2 + k][1], w[2 + k][2], w[2 + k][3]);
+        }
+    }
+}
+
+// Either may have no rows.
+hipError_t pack_rows(const RowArgs& one, const RowArgs& two, hipStream_t stream)
+{
+    const int64_t b1 = ceil_div(one.exponents, kPackThreads / kWave), b2 = ceil_div(two.exponents, kPackThreads / kWave);
+    if (b1 + b2 == 0) return hipSuccess;
+    if (!grid_fits(b1 + b2, kPackThreads)) return hipErrorInvalidConfiguration;
+    hipLaunchKernelGGL(pack_rows_kernel, dim3(unsigned(b1 + b2)), dim3(kPackThreads), 0, stream, one, two, unsigned(b1));
     return hipGetLastError();
 }
 
@@ -162,7 +251,7 @@ __device__ __forceinline__ float tanh_of(float x, float& slope)
 // The same for |x| <= kNear as x P(x^2), P of degree four: 2^-24.5 of itself by its coefficients (a
 // fit that levels the largest relative error), 2^-22.7 as evaluated.  A third of the instructions of the
 // general form, and none of the slow ones.  A soft cap is there to hold the few far logits, so waves
-// whose logits are all near are the rule; the others take the general form for a column at a time.
+// whose logits are all near are the rule; the others evaluate both for 16 rows at a time.
 constexpr float kNear = 0.5625f;
 struct NearTanh {
     float c[5];      // for z in the place of x = z / cap
@@ -187,6 +276,15 @@ struct NearTanh {
     }
 };
 
+// The form that an element's own magnitude asks for: what a row gets does not hang on its neighbours'.
+__device__ __forceinline__ float any_tanh(const NearTanh& near, float z, float inv, float& slope)
+{
+    const float far = tanh_of(z * inv, slope), y = near(z);
+    const bool is_near = fabsf(z) <= near.edge;
+    slope = is_near ? fmaf(-y, y, 1.0f) : slope;
+    return is_near ? y : far;
+}
+
 // Up to this cap exp(l) and sums of them stay far inside fp32's range, whatever l is.
 constexpr float kPlainCap = 60.0f;
 
@@ -208,6 +306,8 @@ __device__ __forceinline__ int row_pair_min(int v)
 
 struct LogitsArgs {
     Matrix table, h;          // from the piece's first row of the table on
+    const int32_t* table_e;   // fp16 planes: the exponents that their rows were scaled by (readable up to whole tiles)
+    const int32_t* h_e;
     int64_t width;
     int64_t first, vocab;     // the piece's first row; rows of the whole table
     int64_t piece;            // rows of the piece
@@ -228,6 +328,24 @@ struct LogitsArgs {
     int64_t dz_ld, dz_plane, dz_rows;
 };
 
+// Products of scaled rows to those of the rows: column c0 + .. of the piece, row r0 + ... (of what lies past the
+// piece or the rows no matter what.)
+template <class S>
+__device__ __forceinline__ void scale_back(f32x4 (&acc)[S::MT][S::NT], const LogitsArgs& a, int64_t c0, int64_t r0, int g, int n)
+{
+    int rows[S::NT];
+#pragma unroll
+    for (int j = 0; j < S::NT; ++j) rows[j] = a.h_e[r0 + 16 * j + n];
+#pragma unroll
+    for (int i = 0; i < S::MT; ++i) {
+        const int4 e = *reinterpret_cast<const int4*>(a.table_e + c0 + 16 * i + 4 * g);
+#pragma unroll
+        for (int j = 0; j < S::NT; ++j)
+            acc[i][j] = f32x4{__builtin_ldexpf(acc[i][j][0], e.x + rows[j]), __builtin_ldexpf(acc[i][j][1], e.y + rows[j]),
+                              __builtin_ldexpf(acc[i][j][2], e.z + rows[j]), __builtin_ldexpf(acc[i][j][3], e.w + rows[j])};
+    }
+}
+
 // One tile of the vocabulary against one of the rows; of every row the tile's largest logit and its
 // sum of exponentials to that, which the next kernel joins over the tiles.
 template <class S>
@@ -245,6 +363,7 @@ __global__ void __launch_bounds__(S::kThreads) logits_kernel(LogitsArgs a)
     const int wave = int(threadIdx.x) / kWave, wm = wave / S::WN, wn = wave % S::WN;
     const int64_t v0 = a.first + m0 + wm * S::MT * 16;      // the wave's first row of the table
     const int here = int(min(a.first + a.piece - v0, int64_t(S::MT * 16)));     // its rows that exist (0 or less: none)
+    if constexpr (S::Planes == 2) scale_back<S>(acc, a, m0 + wm * S::MT * 16, n0 + wn * S::NT * 16, g, n);
     float* red_m = red;           // [WM][N]
     float* red_s = red_m + S::WM * S::N;
     float* red_z = red_s + S::WM * S::N;
@@ -296,7 +415,7 @@ __global__ void __launch_bounds__(S::kThreads) logits_kernel(LogitsArgs a)
 #pragma unroll
                 for (int i = 0; i < S::MT; ++i)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) acc[i][j][r] = a.cap * tanh_of(acc[i][j][r] * inv, slope);
+                    for (int r = 0; r < 4; ++r) acc[i][j][r] = a.cap * any_tanh(near, acc[i][j][r], inv, slope);
             }
         }
         if (a.at != nullptr) {
@@ -444,22 +563,6 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(JoinArgs a)
 }
 
 // ------------------------------------------------------------------ the gradient
-// dz of a column of near logits, none of them a target's: tanh, its slope 1 - tanh^2 (at least 0.74, so
-// nothing cancels), exp and two products.
-template <class S>
-__device__ __forceinline__ void grads_near(f32x4 (&acc)[S::MT][S::NT], int j, const NearTanh& near, float scale, float lse2, float up)
-{
-#pragma unroll
-    for (int i = 0; i < S::MT; ++i)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const float y = near(acc[i][j][r]);
-            const float p = __builtin_amdgcn_exp2f(fmaf(y, scale, -lse2));
-            acc[i][j][r] = p * fmaf(-y, y, 1.0f) * up;
-        }
-}
-
-// The logits of one tile again, and from them dz in bf16 (three planes of it for fp32 operands).
 template <class S>
 __global__ void __launch_bounds__(S::kThreads) logits_grad_kernel(LogitsArgs a)
 {
@@ -474,7 +577,8 @@ __global__ void __launch_bounds__(S::kThreads) logits_grad_kernel(LogitsArgs a)
     const int wave = int(threadIdx.x) / kWave, wm = wave / S::WN, wn = wave % S::WN;
     const int64_t c0 = m0 + wm * S::MT * 16;                // the wave's first column of dz
     const int here = int(min(a.piece - c0, int64_t(S::MT * 16)));
-    const float inv = a.cap > 0.0f ? 1.0f / a.cap : 0.0f, scale = a.cap * kLog2e;
+    if constexpr (S::Planes == 2) scale_back<S>(acc, a, c0, n0 + wn * S::NT * 16, g, n);
+    const float inv = a.cap > 0.0f ? 1.0f / a.cap : 0.0f, scale = (a.cap > 0.0f ? a.cap : 1.0f) * kLog2e;
     const NearTanh near(a.cap);
 #pragma unroll
     for (int j = 0; j < S::NT; ++j) {
@@ -494,26 +598,26 @@ __global__ void __launch_bounds__(S::kThreads) logits_grad_kernel(LogitsArgs a)
 #pragma unroll
             for (int r = 0; r < 4; ++r) far = fmaxf(far, fabsf(acc[i][j][r]));
         const bool all_near = a.cap > 0.0f && !__any(far > near.edge), target = __any(mine >= 0);
-        // dz in the place of z; the target's element, where it is one of the wave's, gets its -1 in place
-        auto grads = [&](auto logit) {
+        // dz in the place of z: of near logits without a target among them tanh, its slope 1 - tanh^2 (at least
+        // 0.68, so nothing cancels), exp and two products; else the target's element gets its -1 in place
+        if (all_near && !target) {
 #pragma unroll
             for (int i = 0; i < S::MT; ++i)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    float slope;
-                    const float p = __builtin_amdgcn_exp2f(logit(acc[i][j][r], slope) - lse2);
-                    acc[i][j][r] = (target && 16 * i + 4 * g + r == mine ? p - 1.0f : p) * (slope * up);
+                    const float y = near(acc[i][j][r]);
+                    acc[i][j][r] = __builtin_amdgcn_exp2f(fmaf(y, scale, -lse2)) * (fmaf(-y, y, 1.0f) * up);
                 }
-        };
-        if (all_near && !target) {
-            grads_near<S>(acc, j, near, scale, lse2, up);
-        } else if (a.cap > 0.0f) {
-            grads([&](float z, float& slope) { return scale * tanh_of(z * inv, slope); });
         } else {
-            grads([&](float z, float& slope) {
-                slope = 1.0f;
-                return z * kLog2e;
-            });
+#pragma unroll
+            for (int i = 0; i < S::MT; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    float slope = 1.0f, y = acc[i][j][r];
+                    if (a.cap > 0.0f) y = any_tanh(near, y, inv, slope);
+                    const float p = __builtin_amdgcn_exp2f(fmaf(y, scale, -lse2));
+                    acc[i][j][r] = (16 * i + 4 * g + r == mine ? p - 1.0f : p) * (slope * up);
+                }
         }
         if (here < S::MT * 16) {
 #pragma unroll
@@ -654,7 +758,8 @@ __global__ void __launch_bounds__(kSumThreads) layer_sum_kernel(SumArgs a)
 constexpr int64_t kUnits = 256;      // compute units of the card
 
 enum Shape { kWide, kMiddle, kNarrow, kThin };
-int planes_of(int dtype) { return dtype == kBf16 ? 1 : 3; }
+int logit_planes(int dtype) { return dtype == kBf16 ? 1 : 2; }
+int grad_planes(int dtype) { return dtype == kBf16 ? 1 : 3; }
 template <int Planes>
 int64_t shape_size(Shape s, bool n)
 {
@@ -662,8 +767,8 @@ int64_t shape_size(Shape s, bool n)
     const int64_t m_of[] = {P::Wide::M, P::Middle::M, P::Narrow::M, P::Thin::M}, n_of[] = {P::Wide::N, P::Middle::N, P::Narrow::N, P::Thin::N};
     return n ? n_of[s] : m_of[s];
 }
-int64_t shape_m(Shape s, int planes) { return planes == 1 ? shape_size<1>(s, false) : shape_size<3>(s, false); }
-int64_t shape_n(Shape s, int planes) { return planes == 1 ? shape_size<1>(s, true) : shape_size<3>(s, true); }
+int64_t shape_m(Shape s, int planes) { return planes == 1 ? shape_size<1>(s, false) : planes == 2 ? shape_size<2>(s, false) : shape_size<3>(s, false); }
+int64_t shape_n(Shape s, int planes) { return planes == 1 ? shape_size<1>(s, true) : planes == 2 ? shape_size<2>(s, true) : shape_size<3>(s, true); }
 
 // What a product takes with each tile shape, in us, fitted to 73 sizes of each type (33 to 4000 rows, 1000 to
 // 50257 of the table, 320 to 2048 channels), most of them within a tenth.  A tile alone on its compute unit takes
@@ -675,13 +780,14 @@ struct Cost {
     float alone, alone_step, shared, shared_step;
     int per_unit;
 };
-constexpr Cost kCost[2][4] = {
+constexpr Cost kCost[3][4] = {
     {{13.0f, 1.15f, 9.1f, 1.49f, 1}, {7.0f, 0.66f, 2.6f, 0.47f, 2}, {4.2f, 0.42f, 0.73f, 0.174f, 5}, {4.0f, 0.40f, 0.6f, 0.12f, 6}},
+    {{11.2f, 0.93f, 9.9f, 1.20f, 1}, {8.2f, 0.68f, 3.4f, 0.66f, 2}, {4.7f, 0.41f, 0.57f, 0.29f, 5}, {4.7f, 0.41f, 0.57f, 0.29f, 5}},
     {{9.7f, 1.68f, 6.7f, 2.13f, 1}, {7.2f, 0.96f, 3.4f, 1.25f, 1}, {4.5f, 0.58f, 0.74f, 0.426f, 3}, {4.5f, 0.58f, 0.74f, 0.426f, 3}}};
 
 float cost_of(Shape s, int planes, int64_t tiles, int64_t k)
 {
-    const Cost& c = kCost[planes == 1 ? 0 : 1][s];
+    const Cost& c = kCost[planes - 1][s];
     const float steps = float(ceil_div(k, step_k(planes))), alone = c.alone + c.alone_step * steps, shared = c.shared + c.shared_step * steps;
     const int64_t each = ceil_div(tiles, kUnits), rounds = each / c.per_unit, rest = each % c.per_unit;
     return float(rounds) * std::max(alone, shared * float(c.per_unit)) + (rest > 0 ? std::max(alone, shared * float(rest)) : 0.0f);
@@ -721,8 +827,14 @@ hipError_t with_shape(Shape s, F f)
         default: return f(typename P::Thin{});
     }
 }
+// A product of logits (bf16 or fp16 planes), and one of a gradient (bf16, one plane or three).
 template <typename F>
-hipError_t with_shape(Shape s, int planes, F f)
+hipError_t with_logits_shape(Shape s, int planes, F f)
+{
+    return planes == 1 ? with_shape<1>(s, f) : with_shape<2>(s, f);
+}
+template <typename F>
+hipError_t with_grad_shape(Shape s, int planes, F f)
 {
     return planes == 1 ? with_shape<1>(s, f) : with_shape<3>(s, f);
 }
@@ -733,15 +845,14 @@ bool direct(const void* p, int64_t stride, int64_t width, int dtype)
     return dtype == kBf16 && width % kStepK == 0 && stride % 8 == 0 && stride < (int64_t(1) << 22) && uintptr_t(p) % 16 == 0;
 }
 
-constexpr int64_t kCopyBytes = int64_t(64) << 20;      // of the table's rows in bf16 planes at a time, forward
+constexpr int64_t kCopyBytes = int64_t(64) << 20;      // of the table's rows that are copied at a time, forward
 constexpr int64_t kPieceBytes = int64_t(256) << 20;    // of dz at a time
 constexpr int64_t kSlabBytes = int64_t(256) << 20;     // of fp32 layers of one product, at most (or one layer)
-
 
 // Rows of the table in a piece of the forward, where it has to be copied.
 int64_t copy_rows(int64_t vocab, int64_t width, int dtype)
 {
-    const int64_t row = ceil_to(width, kStepK) * 2 * planes_of(dtype);
+    const int64_t row = ceil_to(width, kStepK) * 2 * logit_planes(dtype);
     return std::min(ceil_to(vocab, 256), std::max<int64_t>(256, kCopyBytes / row / 256 * 256));
 }
 
@@ -755,33 +866,40 @@ struct Carve {      // the workspace, piece after piece of 256 bytes
     }
 };
 
+// Exponents of n rows, which are read up to the end of the last tile.
+int64_t exponents_of(int64_t n) { return ceil_to(n, 256) + 256; }
+
 struct ForwardPlan {
-    int64_t part, best_z, best_v, at, h, table, bytes, tiles;
+    int64_t part, best_z, best_v, at, h, table, h_e, table_e, bytes;
     ForwardPlan(int64_t rows, int64_t vocab, int64_t width, int dtype)
     {
         // whether the table is copied hangs on its address, so there is room for either way's tiles
         const int64_t copied = copy_rows(vocab, width, dtype);
-        const int planes = planes_of(dtype);
-        tiles = std::max(ceil_div(vocab, shape_m(shape_of(vocab, rows, width, planes), planes)), ceil_div(vocab, shape_m(shape_of(copied, rows, width, planes), planes)));
+        const int planes = logit_planes(dtype);
+        auto tiles_of = [&](int64_t m) { return ceil_div(vocab, shape_m(shape_of(m, rows, width, planes), planes)); };
+        const int64_t tiles = std::max(tiles_of(vocab), tiles_of(copied));
         Carve c;
-        const int64_t row = ceil_to(width, kStepK) * 2 * planes_of(dtype);
+        const int64_t row = ceil_to(width, kStepK) * 2 * planes;
         part = c.take(tiles * rows * 8);
         best_z = c.take(tiles * rows * 4);
         best_v = c.take(tiles * rows * 4);
         at = c.take(rows * 4);
         h = c.take(rows * row);
         table = c.take(copied * row);
+        h_e = planes == 1 ? 0 : c.take(exponents_of(rows) * 4);
+        table_e = planes == 1 ? 0 : c.take(exponents_of(copied) * 4);
         bytes = c.at;
     }
 };
 
 struct GradPlan {
-    int64_t piece, dz, dz_rows, dz_ld, h, table, slab_h, slab_e, bytes, ld;
+    // h and the table as the gradients' products read them, and (fp32) as the logits' does, with the exponents
+    int64_t piece, dz, dz_rows, dz_ld, h, table, h16, table16, h_e, table_e, slab_h, slab_e, bytes, ld;
     Shape logits;
     Cut dh, de, de_last;
     GradPlan(int64_t rows, int64_t vocab, int64_t width, int dtype)
     {
-        const int planes = planes_of(dtype);
+        const int planes = grad_planes(dtype);
         ld = ceil_to(width, kStepK);
         dz_rows = ceil_to(rows, 64);
         piece = std::max<int64_t>(256, kPieceBytes / (dz_rows * 2 * planes) / 256 * 256);
@@ -793,7 +911,7 @@ struct GradPlan {
         else
             piece = piece >= round ? piece / round * round : ceil_to(ceil_div(vocab, ceil_div(vocab, piece)), 256);
         dz_ld = piece;
-        logits = shape_of(piece, rows, width, planes);
+        logits = shape_of(piece, rows, width, logit_planes(dtype));
         dh = layers(width, rows, std::min(piece, vocab), planes);
         // the last piece may be much shorter, and is then cut otherwise
         const int64_t rest = vocab - (ceil_div(vocab, piece) - 1) * piece;
@@ -802,6 +920,10 @@ struct GradPlan {
         Carve c;
         h = c.take(dz_rows * ld * 2 * planes);
         table = c.take(piece * ld * 2 * planes);
+        h16 = planes == 1 ? h : c.take(dz_rows * ld * 4);
+        table16 = planes == 1 ? table : c.take(piece * ld * 4);
+        h_e = planes == 1 ? 0 : c.take(exponents_of(dz_rows) * 4);
+        table_e = planes == 1 ? 0 : c.take(exponents_of(piece) * 4);
         dz = c.take(dz_rows * dz_ld * 2 * planes);
         slab_h = dh.layers > 1 || piece < vocab ? c.take(dh.layers * rows * ld * 4) : 0;
         const int64_t layered = std::max(de.layers > 1 ? de.layers * piece : 0, de_last.layers > 1 ? de_last.layers * rest : 0);
@@ -827,27 +949,26 @@ int64_t cross_entropy_grad_bytes(int64_t rows, int64_t vocab, int64_t width, int
 hipError_t launch_cross_entropy(const CrossEntropyArgs& a, hipStream_t stream)
 {
     const ForwardPlan plan(a.rows, a.vocab, a.width, a.dtype);
-    const int planes = planes_of(a.dtype);
+    const int planes = logit_planes(a.dtype);
     const int64_t ld = ceil_to(a.width, kStepK);
+    char* ws = a.workspace;
     LogitsArgs k{};
     k.width = a.width;
     k.vocab = a.vocab;
     k.rows = a.rows;
     k.targets = a.targets;
     k.cap = a.cap;
-    k.part = reinterpret_cast<float2*>(a.workspace + plan.part);
-    k.best_z = a.best == nullptr ? nullptr : reinterpret_cast<float*>(a.workspace + plan.best_z);
-    k.best_v = reinterpret_cast<int32_t*>(a.workspace + plan.best_v);
-    k.at = a.targets.p == nullptr ? nullptr : reinterpret_cast<float*>(a.workspace + plan.at);
-    PackArgs h{};      // h is copied, if at all, along with the table's first piece
-    if (direct(a.h, a.h_stride, a.width, a.dtype)) {
-        k.h = Matrix{static_cast<const uint16_t*>(a.h), a.h_stride, 0, a.rows, a.width};
-    } else {
-        uint16_t* copy = reinterpret_cast<uint16_t*>(a.workspace + plan.h);
-        k.h = Matrix{copy, ld, a.rows * ld, a.rows, ld};
-        h = PackArgs{a.h, a.rows, a.width, a.h_stride, Tokens{}, 0, copy, a.rows, ld, a.rows * ld};
-    }
-    const bool as_is = direct(a.table, a.table_stride, a.width, a.dtype);
+    k.part = reinterpret_cast<float2*>(ws + plan.part);
+    k.best_z = a.best == nullptr ? nullptr : reinterpret_cast<float*>(ws + plan.best_z);
+    k.best_v = reinterpret_cast<int32_t*>(ws + plan.best_v);
+    k.at = a.targets.p == nullptr ? nullptr : reinterpret_cast<float*>(ws + plan.at);
+    k.h_e = reinterpret_cast<int32_t*>(ws + plan.h_e);
+    k.table_e = reinterpret_cast<int32_t*>(ws + plan.table_e);
+    uint16_t* h = reinterpret_cast<uint16_t*>(ws + plan.h);
+    uint16_t* copy = reinterpret_cast<uint16_t*>(ws + plan.table);
+    // h is copied, if at all, along with the table's first piece
+    const bool h_as_is = direct(a.h, a.h_stride, a.width, a.dtype), as_is = direct(a.table, a.table_stride, a.width, a.dtype);
+    k.h = h_as_is ? Matrix{static_cast<const uint16_t*>(a.h), a.h_stride, 0, a.rows, a.width} : Matrix{h, ld, a.rows * ld, a.rows, ld};
     const int64_t most = as_is ? a.vocab : copy_rows(a.vocab, a.width, a.dtype);
     const Shape shape = shape_of(most, a.rows, a.width, planes);
     k.tiles_n = ceil_div(a.rows, shape_n(shape, planes));
@@ -856,18 +977,22 @@ hipError_t launch_cross_entropy(const CrossEntropyArgs& a, hipStream_t stream)
         k.piece = std::min(most, a.vocab - first);
         k.tile0 = first / shape_m(shape, planes);
         k.tiles_m = ceil_div(k.piece, shape_m(shape, planes));
-        PackArgs table{};
-        if (as_is) {
-            k.table = Matrix{static_cast<const uint16_t*>(a.table), a.table_stride, 0, a.vocab, a.width};
+        k.table = as_is ? Matrix{static_cast<const uint16_t*>(a.table), a.table_stride, 0, a.vocab, a.width} : Matrix{copy, ld, k.piece * ld, k.piece, ld};
+        hipError_t e;
+        if (planes == 1) {
+            const uint16_t* src = static_cast<const uint16_t*>(a.table) + first * a.table_stride;
+            e = pack_copy(first > 0 || h_as_is ? PackArgs{} : PackArgs{static_cast<const uint16_t*>(a.h), a.rows, a.width, a.h_stride, {}, 0, h, a.rows, ld},
+                          as_is ? PackArgs{} : PackArgs{src, k.piece, a.width, a.table_stride, {}, 0, copy, k.piece, ld}, stream);
         } else {
-            uint16_t* copy = reinterpret_cast<uint16_t*>(a.workspace + plan.table);
-            k.table = Matrix{copy, ld, most * ld, k.piece, ld};
-            const char* src = static_cast<const char*>(a.table) + first * a.table_stride * (planes == 1 ? 2 : 4);
-            table = PackArgs{src, k.piece, a.width, a.table_stride, Tokens{}, 0, copy, k.piece, ld, most * ld};
+            const float* src = static_cast<const float*>(a.table) + first * a.table_stride;
+            e = pack_rows(first > 0 ? RowArgs{} : RowArgs{static_cast<const float*>(a.h), a.rows, a.width, a.h_stride, {}, 0, h,
+                                                           reinterpret_cast<int32_t*>(ws + plan.h_e), exponents_of(a.rows), nullptr, a.rows, ld},
+                          RowArgs{src, k.piece, a.width, a.table_stride, {}, 0, copy, reinterpret_cast<int32_t*>(ws + plan.table_e), exponents_of(k.piece),
+                                  nullptr, k.piece, ld},
+                          stream);
         }
-        if (hipError_t e = pack_planes(h, table, a.dtype, stream); e != hipSuccess) return e;
-        h = PackArgs{};
-        const hipError_t e = with_shape(shape, planes, [&](auto s) {
+        if (e != hipSuccess) return e;
+        e = with_logits_shape(shape, planes, [&](auto s) {
             using S = decltype(s);
             if (!grid_fits(k.tiles_m * k.tiles_n, S::kThreads)) return hipErrorInvalidConfiguration;
             hipLaunchKernelGGL((logits_kernel<S>), dim3(unsigned(k.tiles_m * k.tiles_n)), dim3(S::kThreads), 0, stream, k);
@@ -892,7 +1017,7 @@ namespace {
 template <bool AlongB>
 hipError_t launch_grad(const GradArgs& k, Shape shape, int64_t layers, int planes, hipStream_t stream)
 {
-    return with_shape(shape, planes, [&](auto s) {
+    return with_grad_shape(shape, planes, [&](auto s) {
         using S = decltype(s);
         if (!grid_fits(k.tiles_m * k.tiles_n, S::kThreads)) return hipErrorInvalidConfiguration;
         hipLaunchKernelGGL((grad_kernel<S, AlongB>), dim3(unsigned(k.tiles_m * k.tiles_n), unsigned(layers)), dim3(S::kThreads), 0, stream, k);
@@ -921,34 +1046,44 @@ hipError_t launch_cross_entropy_grad(const CrossEntropyGradArgs& a, hipStream_t 
         return launch_sum(none, a.dtype, stream);
     }
     const GradPlan plan(a.rows, a.vocab, a.width, a.dtype);
-    const int planes = planes_of(a.dtype);
+    const int planes = grad_planes(a.dtype);
     const int64_t ld = plan.ld, es = planes == 1 ? 2 : 4;
     char* ws = a.workspace;
-    uint16_t* h = reinterpret_cast<uint16_t*>(ws + plan.h);
-    uint16_t* dz = reinterpret_cast<uint16_t*>(ws + plan.dz);
-    // h is copied always: rows that do not count may hold anything, and the products over rows would meet it
-    PackArgs ph{a.h, a.rows, a.width, a.h_stride, a.targets, a.vocab, h, plan.dz_rows, ld, plan.dz_rows * ld};
+    auto words = [&](int64_t at) { return reinterpret_cast<uint16_t*>(ws + at); };
+    uint16_t* dz = words(plan.dz);
     const bool as_is = direct(a.table, a.table_stride, a.width, a.dtype);
     const int64_t dz_plane = plan.dz_rows * plan.dz_ld;
+    const Matrix h{words(plan.h), ld, plan.dz_rows * ld, plan.dz_rows, ld};
 
     for (int64_t first = 0; first < a.vocab; first += plan.piece) {
         const int64_t piece = std::min(plan.piece, a.vocab - first);
         const bool last = first + piece == a.vocab;
         const char* src = static_cast<const char*>(a.table) + first * a.table_stride * es;
-        Matrix table;
-        PackArgs pt{};
-        if (as_is) {
-            table = Matrix{reinterpret_cast<const uint16_t*>(src), a.table_stride, 0, piece, a.width};
-        } else {
-            uint16_t* copy = reinterpret_cast<uint16_t*>(ws + plan.table);
-            table = Matrix{copy, ld, plan.piece * ld, piece, ld};
-            pt = PackArgs{src, piece, a.width, a.table_stride, Tokens{}, 0, copy, piece, ld, plan.piece * ld};
-        }
-        if (hipError_t e = pack_planes(ph, pt, a.dtype, stream); e != hipSuccess) return e;
-        ph = PackArgs{};
+        const Matrix table = as_is ? Matrix{reinterpret_cast<const uint16_t*>(src), a.table_stride, 0, piece, a.width}
+                                   : Matrix{words(plan.table), ld, piece * ld, piece, ld};
+        // h is copied always: rows that do not count may hold anything, and the products over rows would meet it
+        hipError_t e;
         LogitsArgs k{};
-        k.table = table;
-        k.h = Matrix{h, ld, plan.dz_rows * ld, plan.dz_rows, ld};
+        if (planes == 1) {
+            e = pack_copy(first > 0 ? PackArgs{} : PackArgs{static_cast<const uint16_t*>(a.h), a.rows, a.width, a.h_stride, a.targets, a.vocab,
+                                                            words(plan.h), plan.dz_rows, ld},
+                          as_is ? PackArgs{} : PackArgs{reinterpret_cast<const uint16_t*>(src), piece, a.width, a.table_stride, {}, 0, words(plan.table), piece, ld},
+                          stream);
+            k.table = table;
+            k.h = h;
+        } else {
+            int32_t *h_e = reinterpret_cast<int32_t*>(ws + plan.h_e), *table_e = reinterpret_cast<int32_t*>(ws + plan.table_e);
+            e = pack_rows(first > 0 ? RowArgs{} : RowArgs{static_cast<const float*>(a.h), a.rows, a.width, a.h_stride, a.targets, a.vocab,
+                                                           words(plan.h16), h_e, exponents_of(plan.dz_rows), words(plan.h), plan.dz_rows, ld},
+                          RowArgs{reinterpret_cast<const float*>(src), piece, a.width, a.table_stride, {}, 0, words(plan.table16), table_e,
+                                  exponents_of(piece), words(plan.table), piece, ld},
+                          stream);
+            k.table = Matrix{words(plan.table16), ld, piece * ld, piece, ld};
+            k.h = Matrix{words(plan.h16), ld, plan.dz_rows * ld, plan.dz_rows, ld};
+            k.h_e = h_e;
+            k.table_e = table_e;
+        }
+        if (e != hipSuccess) return e;
         k.width = a.width;
         k.first = first;
         k.vocab = a.vocab;
@@ -962,9 +1097,9 @@ hipError_t launch_cross_entropy_grad(const CrossEntropyGradArgs& a, hipStream_t 
         k.dz_ld = plan.dz_ld;
         k.dz_plane = dz_plane;
         k.dz_rows = plan.dz_rows;
-        k.tiles_m = ceil_div(piece, shape_m(plan.logits, planes));
-        k.tiles_n = ceil_div(plan.dz_rows, shape_n(plan.logits, planes));
-        hipError_t e = with_shape(plan.logits, planes, [&](auto s) {
+        k.tiles_m = ceil_div(piece, shape_m(plan.logits, logit_planes(a.dtype)));
+        k.tiles_n = ceil_div(plan.dz_rows, shape_n(plan.logits, logit_planes(a.dtype)));
+        e = with_logits_shape(plan.logits, logit_planes(a.dtype), [&](auto s) {
             using S = decltype(s);
             if (!grid_fits(k.tiles_m * k.tiles_n, S::kThreads)) return hipErrorInvalidConfiguration;
             hipLaunchKernelGGL((logits_grad_kernel<S>), dim3(unsigned(k.tiles_m * k.tiles_n)), dim3(S::kThreads), 0, stream, k);
@@ -1002,7 +1137,7 @@ hipError_t launch_cross_entropy_grad(const CrossEntropyGradArgs& a, hipStream_t 
             const Cut cut = last ? plan.de_last : plan.de;
             const Shape shape = cut.shape;
             GradArgs d{};
-            d.a = k.h;
+            d.a = h;
             d.b = dz_rows;
             d.k = plan.dz_rows;
             d.k_split = ceil_to(ceil_div(plan.dz_rows, cut.layers), kStepK);
