@@ -65,15 +65,23 @@ def cross_entropy_backward(h, table, targets, dloss, cap=0.0):
 
 def cross_entropy_bounds(h, table, targets, dloss, cap, bf16):
     """Bounds on the errors of lse, loss, dh and dtable.  A product of D terms in fp32 is off by at most D 2^-23 of the sum
-    of its terms' magnitudes (each addition by at most one unit in the last place, whichever way it rounds; the parts of
-    an fp32 factor add 2^-24).  The cap's tanh is good to 2^-20 of itself.  A sum of exponentials is good to 2^-18 (their
+    of its terms' magnitudes (each addition by at most one unit in the last place, whichever way it rounds).  An fp32 factor
+    may be held as two fp16 parts of its row scaled by a power of two to below 2^15.  The first has 11 bits, so what it
+    leaves, a multiple of 2^-23 of the element's power of two, is at most 2^-11 of that: 12 bits, of which the second part
+    keeps 11, off by one of those multiples at most, 2^-23.  Of an element below 2^-16 of the row's largest the second part
+    is a multiple of 2^-24 of the scaled value, off by 2^-25: 2^-39 of the largest, which is 2^14 or more.  The product of
+    two second parts, at most 2^-22, is left out.  Together 2 2^-23 + 2^-22 = 2^-21 of a term, and 2^-39 of the largest
+    magnitude of either row times the other's sum.  The cap's tanh is good to 2^-20 of itself.  A sum of exponentials is good to 2^-18 (their
     arguments, up to about 20 where they weigh, are rounded at 2^-23 of themselves, and at most 128 additions follow each
     other), its logarithm to 2^-22 of itself.  What lies below fp32's smallest normal number, 2^-126, may be lost: a
     probability, and a gradient.  dz is rounded to bf16 (2^-8) for bf16 operands, and so are the gradients."""
     h, table = np.asarray(h, np.float64), np.asarray(table, np.float64)
     D, V, N = h.shape[1], len(table), len(h)
     l, _ = logits(h, table, cap)
-    dl = (D * 2.0 ** -23 + 2.0 ** -23) * (np.abs(h) @ np.abs(table).T) + 2.0 ** -20 * np.abs(l) * (cap > 0)
+    ah, at = np.abs(h), np.abs(table)
+    dl = (D * 2.0 ** -23 + (0.0 if bf16 else 2.0 ** -21)) * (ah @ at.T) + 2.0 ** -20 * np.abs(l) * (cap > 0)
+    if not bf16:
+        dl += 2.0 ** -39 * (ah.max(axis=1)[:, None] * at.sum(axis=1) + ah.sum(axis=1)[:, None] * at.max(axis=1))
     ref = cross_entropy(h, table, targets, cap)
     dlse = dl.max(axis=1) + 2.0 ** -18 + 2.0 ** -22 * np.abs(ref["lse"])
     there = counted(targets, V)

@@ -128,8 +128,10 @@ hipError_t pack_copy(const PackArgs& one, const PackArgs& two, hipStream_t strea
 }
 
 // fp32 rows in planes, a wave a row: two fp16 planes of x 2^-e, e the power of two that brings the row's
-// largest magnitude into [2^14, 2^15), so that parts of elements down to 2^-18 of it are whole (the rest is
-// off by 2^-40 of it at most); and three bf16 planes, which need no scale and so serve sums along either way.
+// largest magnitude into [2^14, 2^15): of 24 bits the first plane takes 11 and a sign, the second 11 of the 12 that
+// are left, so an element down to 2^-16 of the largest is off by 2^-23 of itself at most, a smaller one (whose second
+// part is subnormal) by 2^-39 of the largest.  And three bf16 planes, which need no scale and so serve sums along
+// either way.
 struct RowArgs {
     const float* x;          // [rows] rows of width, stride apart
     int64_t rows, width, stride;
@@ -756,6 +758,7 @@ __global__ void __launch_bounds__(kSumThreads) layer_sum_kernel(SumArgs a)
 
 // ------------------------------------------------------------------ plans
 constexpr int64_t kUnits = 256;      // compute units of the card
+constexpr int64_t kMostTiles = int64_t(UINT32_MAX) / 512;      // of a launch, whose threads are counted in 32 bits
 
 enum Shape { kWide, kMiddle, kNarrow, kThin };
 int logit_planes(int dtype) { return dtype == kBf16 ? 1 : 2; }
@@ -969,25 +972,25 @@ hipError_t launch_cross_entropy(const CrossEntropyArgs& a, hipStream_t stream)
     // h is copied, if at all, along with the table's first piece
     const bool h_as_is = direct(a.h, a.h_stride, a.width, a.dtype), as_is = direct(a.table, a.table_stride, a.width, a.dtype);
     k.h = h_as_is ? Matrix{static_cast<const uint16_t*>(a.h), a.h_stride, 0, a.rows, a.width} : Matrix{h, ld, a.rows * ld, a.rows, ld};
-    const int64_t most = as_is ? a.vocab : copy_rows(a.vocab, a.width, a.dtype);
+    int64_t most = as_is ? a.vocab : copy_rows(a.vocab, a.width, a.dtype);
     const Shape shape = shape_of(most, a.rows, a.width, planes);
     k.tiles_n = ceil_div(a.rows, shape_n(shape, planes));
+    most = std::min(most, kMostTiles / k.tiles_n * shape_m(shape, planes));
     for (int64_t first = 0; first < a.vocab; first += most) {
         k.first = first;
         k.piece = std::min(most, a.vocab - first);
         k.tile0 = first / shape_m(shape, planes);
         k.tiles_m = ceil_div(k.piece, shape_m(shape, planes));
-        k.table = as_is ? Matrix{static_cast<const uint16_t*>(a.table), a.table_stride, 0, a.vocab, a.width} : Matrix{copy, ld, k.piece * ld, k.piece, ld};
+        const uint16_t* src = static_cast<const uint16_t*>(a.table) + first * a.table_stride * planes;      // of fp32, two planes, twice the bytes
+        k.table = as_is ? Matrix{src, a.table_stride, 0, k.piece, a.width} : Matrix{copy, ld, k.piece * ld, k.piece, ld};
         hipError_t e;
         if (planes == 1) {
-            const uint16_t* src = static_cast<const uint16_t*>(a.table) + first * a.table_stride;
             e = pack_copy(first > 0 || h_as_is ? PackArgs{} : PackArgs{static_cast<const uint16_t*>(a.h), a.rows, a.width, a.h_stride, {}, 0, h, a.rows, ld},
                           as_is ? PackArgs{} : PackArgs{src, k.piece, a.width, a.table_stride, {}, 0, copy, k.piece, ld}, stream);
         } else {
-            const float* src = static_cast<const float*>(a.table) + first * a.table_stride;
             e = pack_rows(first > 0 ? RowArgs{} : RowArgs{static_cast<const float*>(a.h), a.rows, a.width, a.h_stride, {}, 0, h,
                                                            reinterpret_cast<int32_t*>(ws + plan.h_e), exponents_of(a.rows), nullptr, a.rows, ld},
-                          RowArgs{src, k.piece, a.width, a.table_stride, {}, 0, copy, reinterpret_cast<int32_t*>(ws + plan.table_e), exponents_of(k.piece),
+                          RowArgs{reinterpret_cast<const float*>(src), k.piece, a.width, a.table_stride, {}, 0, copy, reinterpret_cast<int32_t*>(ws + plan.table_e), exponents_of(k.piece),
                                   nullptr, k.piece, ld},
                           stream);
         }

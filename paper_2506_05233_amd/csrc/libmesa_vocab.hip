@@ -34,8 +34,8 @@ int vocab_sizes(int64_t rows, int64_t vocab, int64_t width)
 
 bool stride_ok(int64_t rows, int64_t width, int64_t stride) { return rows <= 0 || (stride >= width && product_ok({rows, stride})); }
 
-// A factor or cap that a caller can mean
-bool cap_ok(float cap) { return isfinite(cap) && cap >= 0.0f; }
+// A cap that a caller can mean: none, or one whose reciprocal is finite
+bool cap_ok(float cap) { return cap == 0.0f || (isnormal(cap) && cap > 0.0f); }
 
 bool loss_countable(int64_t rows, int64_t vocab, int64_t width, int dtype)
 {

@@ -959,6 +959,15 @@ def output_norm_backward(o, weight, dy, eps=1e-6, workspace=None):
 
 
 # ---------------------------------------------------------------- a language model's two ends
+def _launch(device, entry, *args):
+    """entry(*args) with the device current, which is where a kernel on its default stream starts."""
+    cuda = _torch().cuda
+    if cuda.current_device() == device.index:
+        return entry(*args)
+    with cuda.device(device):
+        return entry(*args)
+
+
 def _token_bytes(t, name, device):
     """Bytes of a token number of t, a dense int32 or int64 tensor on the device."""
     torch = _torch()
@@ -994,7 +1003,7 @@ def embedding(table, tokens, scale=1.0, out_dtype=None, out=None):
     if out is None:
         out = torch.empty(shape, dtype=table.dtype if out_dtype is None else out_dtype, device=dev)
     out_stride = _check_rows(out, "out", shape, out.dtype if out_dtype is None else out_dtype, dev)
-    st = lib.mesa_embedding(_ptr(table), _ptr(tokens), size, float(scale), tokens.numel(), V, W, stride, code,
+    st = _launch(dev, lib.mesa_embedding, _ptr(table), _ptr(tokens), size, float(scale), tokens.numel(), V, W, stride, code,
                             _float_code(out.dtype, "out"), out_stride, _ptr(out), _stream(dev))
     if st != MESA_OK:
         raise MesaError(st, "mesa_embedding")
@@ -1025,7 +1034,7 @@ def embedding_backward(tokens, dy, vocab, scale=1.0, grad_dtype=None, out=None, 
     rows = tokens.numel()
     need = lib.mesa_embedding_backward_workspace_bytes(rows, vocab, W)
     workspace = _workspace(workspace, need, dev)
-    st = lib.mesa_embedding_backward(_ptr(tokens), size, _ptr(dy), float(scale), rows, vocab, W, dy_stride, code,
+    st = _launch(dev, lib.mesa_embedding_backward, _ptr(tokens), size, _ptr(dy), float(scale), rows, vocab, W, dy_stride, code,
                                      _float_code(out.dtype, "out"), out_stride, int(bool(accumulate)), _ptr(out),
                                      _ptr(workspace), need, _stream(dev))
     if st != MESA_OK:
@@ -1061,7 +1070,7 @@ def cross_entropy(h, table, targets=None, cap=0.0, want_best=False, workspace=No
     rows = res["lse"].numel()
     need = lib.mesa_cross_entropy_workspace_bytes(rows, table.shape[0], W, code)
     workspace = _workspace(workspace, need, dev)
-    st = lib.mesa_cross_entropy(_ptr(h), _ptr(table), _ptr(targets), size, float(cap), rows, table.shape[0], W, h_stride,
+    st = _launch(dev, lib.mesa_cross_entropy, _ptr(h), _ptr(table), _ptr(targets), size, float(cap), rows, table.shape[0], W, h_stride,
                                 table_stride, code, _ptr(res.get("loss")), _ptr(res["lse"]), _ptr(res.get("best")),
                                 _ptr(workspace), need, _stream(dev))
     if st != MESA_OK:
@@ -1095,7 +1104,7 @@ def cross_entropy_backward(h, table, targets, lse, dloss, cap=0.0, want_dh=True,
     rows, V = lse.numel(), table.shape[0]
     need = lib.mesa_cross_entropy_backward_workspace_bytes(rows, V, W, code)
     workspace = _workspace(workspace, need, dev)
-    st = lib.mesa_cross_entropy_backward(_ptr(h), _ptr(table), _ptr(targets), size, _ptr(lse), _ptr(dloss), float(cap), rows, V, W,
+    st = _launch(dev, lib.mesa_cross_entropy_backward, _ptr(h), _ptr(table), _ptr(targets), size, _ptr(lse), _ptr(dloss), float(cap), rows, V, W,
                                          h_stride, table_stride, code, W, W, _ptr(res.get("dh")), _ptr(res.get("dtable")),
                                          _ptr(workspace), need, _stream(dev))
     if st != MESA_OK:

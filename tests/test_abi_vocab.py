@@ -68,7 +68,7 @@ def _loss(lib, **kw):
 @pytest.mark.parametrize("kw,status", [
     (dict(rows=-1), L.MESA_ERR_SHAPE), (dict(V=0), L.MESA_ERR_SHAPE), (dict(W=0), L.MESA_ERR_SHAPE), (dict(hs=63), L.MESA_ERR_SHAPE),
     (dict(es=63), L.MESA_ERR_SHAPE), (dict(dt=2), L.MESA_ERR_UNSUPPORTED), (dict(tb=3), L.MESA_ERR_UNSUPPORTED), (dict(cap=-1.0), L.MESA_ERR_ARG),
-    (dict(cap=NAN), L.MESA_ERR_ARG), (dict(cap=INF), L.MESA_ERR_ARG), (dict(h=None), L.MESA_ERR_NULL), (dict(e=None), L.MESA_ERR_NULL),
+    (dict(cap=NAN), L.MESA_ERR_ARG), (dict(cap=INF), L.MESA_ERR_ARG), (dict(cap=1e-40), L.MESA_ERR_ARG), (dict(h=None), L.MESA_ERR_NULL), (dict(e=None), L.MESA_ERR_NULL),
     (dict(lse=None), L.MESA_ERR_NULL), (dict(loss=None), L.MESA_ERR_NULL), (dict(t=None), L.MESA_ERR_NULL), (dict(ws=None), L.MESA_ERR_NULL),
     (dict(wsb=64), L.MESA_ERR_WORKSPACE), (dict(h=A["h"] + 1), L.MESA_ERR_ARG), (dict(lse=A["lse"] + 2), L.MESA_ERR_ARG),
     (dict(best=A["best"] + 2), L.MESA_ERR_ARG), (dict(t=A["t"] + 4), L.MESA_ERR_ARG), (dict(ws=A["ws"] + 4), L.MESA_ERR_ARG),
@@ -89,7 +89,7 @@ def _loss_grad(lib, **kw):
 @pytest.mark.parametrize("kw,status", [
     (dict(rows=-1), L.MESA_ERR_SHAPE), (dict(V=0), L.MESA_ERR_SHAPE), (dict(W=0), L.MESA_ERR_SHAPE), (dict(hs=63), L.MESA_ERR_SHAPE),
     (dict(es=63), L.MESA_ERR_SHAPE), (dict(dhs=63), L.MESA_ERR_SHAPE), (dict(des=63), L.MESA_ERR_SHAPE), (dict(dt=2), L.MESA_ERR_UNSUPPORTED),
-    (dict(tb=0), L.MESA_ERR_UNSUPPORTED), (dict(cap=-1.0), L.MESA_ERR_ARG), (dict(cap=INF), L.MESA_ERR_ARG), (dict(h=None), L.MESA_ERR_NULL),
+    (dict(tb=0), L.MESA_ERR_UNSUPPORTED), (dict(cap=-1.0), L.MESA_ERR_ARG), (dict(cap=INF), L.MESA_ERR_ARG), (dict(cap=1e-40), L.MESA_ERR_ARG), (dict(h=None), L.MESA_ERR_NULL),
     (dict(t=None), L.MESA_ERR_NULL), (dict(lse=None), L.MESA_ERR_NULL), (dict(up=None), L.MESA_ERR_NULL), (dict(ws=None), L.MESA_ERR_NULL),
     (dict(wsb=64), L.MESA_ERR_WORKSPACE), (dict(dh=A["dh"] + 2), L.MESA_ERR_ARG), (dict(de=A["de"] + 2), L.MESA_ERR_ARG),
     (dict(up=A["up"] + 2), L.MESA_ERR_ARG), (dict(ws=A["ws"] + 4), L.MESA_ERR_ARG), (dict(dh=A["h"]), L.MESA_ERR_ARG),
