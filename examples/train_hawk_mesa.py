@@ -2,10 +2,11 @@
 
     python examples/train_hawk_mesa.py [steps]
 
-One block of the paper's Hawk-Mesa hybrid in its smallest form, on one GPU: tokens go through a
-gated linear recurrence and then through a Mesa layer, each with its projections (torch matmuls)
-and a residual connection, over rows that pack several documents (`reset` marks their starts
-for the recurrence).  The task is to name the token seen a few places before.  What the
+One block of the paper's Hawk-Mesa hybrid in its smallest form, on one GPU: tokens are embedded and
+go through a gated linear recurrence and then through a Mesa layer, each with its projections
+(torch matmuls) and a residual connection, over rows that pack several documents (`reset` marks
+their starts for the recurrence); the loss is the cross entropy over the vocabulary, whose
+logits training never holds.  The task is to name the token seen a few places before.  What the
 backward pass needs of the forward is kept in 8 bits (checkpoint_pack, and the recurrence's own
 checkpoints); the Mesa layer's inputs are formed again from its projections' checkpoints.  At
 the end the trained block decodes tokens one at a time from the states that a prefill leaves,
@@ -40,7 +41,7 @@ class Block:
                   "mesa_in": w(DIM, 3 * d + 2 * HEADS, scale=DIM ** -0.5), "conv_q": w(d, 4, scale=0.5),
                   "conv_k": w(d, 4, scale=0.5), "conv_v": w(d, 4, scale=0.5), "lam": w(HEADS, HEAD, scale=0.5),
                   "norm": torch.ones((HEADS, HEAD), device=device), "mesa_out": w(d, DIM, scale=d ** -0.5),
-                  "logits": w(DIM, VOCAB, scale=DIM ** -0.5)}
+                  "logits": w(VOCAB, DIM, scale=DIM ** -0.5)}
 
     def _mesa_inputs(self, proj):
         """The front end's arguments from the projection [B, T, 3 d + 2 H] of a token's features."""
@@ -54,10 +55,10 @@ class Block:
         p = self.p
         return L.frontend(*heads, p["conv_q"], p["conv_k"], p["conv_v"], a_gamma, a_beta, p["lam"])
 
-    def forward(self, tokens, reset, keep=True):
-        """Logits [B, T, VOCAB] and, with keep, what the backward pass needs."""
+    def features(self, tokens, reset, keep=True):
+        """What the logits are formed from, [B, T, DIM], and, with keep, what the backward pass needs."""
         p, B, T = self.p, *tokens.shape
-        e = p["embed"][tokens]
+        e = L.embedding(p["embed"], tokens)
         x, r, i = (e @ p["hawk_in"]).split(WIDTH, dim=-1)
         rec = L.recurrence(x, r, i, p["theta"], reset=reset, want_final=True, want_states=keep, want_checkpoints=keep)
         z = e + rec["y"] @ p["hawk_out"]
@@ -66,18 +67,39 @@ class Block:
         fw = L.forward(f["q"], f["k"], f["v"], f["gamma"], f["beta"], f["lam"], N_CG, want_qstar=True, want_states=True)
         y = L.output_norm(fw["out"], p["norm"], out_dtype=torch.float32).view(B, T, HEADS * HEAD)
         out = z + y @ p["mesa_out"]
-        logits = out @ p["logits"]
         if not keep:
-            return logits, {"h": rec["h"], "H": fw["H"], "G": fw["G"], "heads": heads}
+            return out, {"h": rec["h"], "H": fw["H"], "G": fw["G"], "heads": heads}
         # the projections as the front end's gradients take them: a token's heads in one row
         qp, kp, vp = (t.view(B, T, HEADS * HEAD) for t in heads)
-        kept = {n: L.checkpoint_pack(t) for n, t in (("z", z), ("y", y), ("out", out), ("rec_y", rec["y"]), ("o", fw["out"]),
-                                                    ("qstar", fw["qstar"]), ("qp", qp), ("kp", kp), ("vp", vp))}
+        kept = {n: L.checkpoint_pack(t) for n, t in (("z", z), ("y", y), ("rec_y", rec["y"]), ("o", fw["out"]), ("qstar", fw["qstar"]),
+                                                    ("qp", qp), ("kp", kp), ("vp", vp))}
         kept.update(tokens=tokens, reset=reset, states=rec["states"], x=rec["x"], r=rec["r"], i=rec["i"], a_gamma=a_gamma, a_beta=a_beta)
-        return logits, kept
+        return out, kept
+
+    def forward(self, tokens, reset, keep=True):
+        """Logits [B, T, VOCAB] and, with keep, what `backward` needs."""
+        out, kept = self.features(tokens, reset, keep)
+        if keep:
+            kept["out"] = L.checkpoint_pack(out)
+        return out @ self.p["logits"].T, kept
+
+    def loss(self, out, answers):
+        """The mean cross entropy of the answers [B, T] (-1: none), and its gradients for `out` and the logits' weights."""
+        p, count = self.p, (answers >= 0).sum()
+        f = L.cross_entropy(out, p["logits"], answers)
+        each = (1.0 / count).expand(answers.shape).contiguous()
+        g = L.cross_entropy_backward(out, p["logits"], answers, f["lse"], each)
+        return f["loss"].sum() / count, g["dh"], g["dtable"]
 
     def backward(self, kept, dlogits):
-        """Gradients of every weight, from the checkpoints."""
+        """Gradients of every weight from those of `forward`'s logits, and the checkpoints."""
+        out = L.checkpoint_unpack(kept["out"], torch.float32)
+        g = self.features_backward(kept, dlogits @ self.p["logits"])
+        g["logits"] = dlogits.reshape(-1, VOCAB).T @ out.reshape(-1, DIM)
+        return g
+
+    def features_backward(self, kept, dz):
+        """Gradients of the weights behind `features`, from dz [B, T, DIM] and the checkpoints."""
         p, g = self.p, {}
         B, T = kept["tokens"].shape
 
@@ -87,8 +109,6 @@ class Block:
         def weight(a, da):
             return a.reshape(-1, a.shape[-1]).T @ da.reshape(-1, da.shape[-1])
 
-        g["logits"] = weight(value("out"), dlogits)
-        dz = dlogits @ p["logits"].T                                   # through the residual
         g["mesa_out"] = weight(value("y"), dz)
         dy = (dz @ p["mesa_out"].T).view(B, T, HEADS, HEAD)
         norm = L.output_norm_backward(kept["o"], p["norm"], dy)
@@ -111,16 +131,14 @@ class Block:
         rg = L.recurrence_backward(kept["x"], kept["r"], kept["i"], p["theta"], kept["states"], dz @ p["hawk_out"].T,
                                    reset=kept["reset"], out=dfused.split(WIDTH, dim=-1))
         g["theta"] = rg["dtheta"]
-        e = p["embed"][kept["tokens"]]
-        g["hawk_in"] = weight(e, dfused)
-        de = dz + dfused @ p["hawk_in"].T
-        g["embed"] = torch.zeros_like(p["embed"]).index_add_(0, kept["tokens"].reshape(-1), de.reshape(-1, DIM))
+        g["hawk_in"] = weight(L.embedding(p["embed"], kept["tokens"]), dfused)
+        g["embed"] = L.embedding_backward(kept["tokens"], dz + dfused @ p["hawk_in"].T, VOCAB)
         return g
 
     def decode(self, token, state):
         """Logits [B, VOCAB] of the next token [B], and `state` moved on by it."""
         p, B = self.p, token.shape[0]
-        e = p["embed"][token]
+        e = L.embedding(p["embed"], token)
         x, r, i = (e @ p["hawk_in"]).split(WIDTH, dim=-1)
         z = e + L.recurrence_step(state["h"], x, r, i, p["theta"]) @ p["hawk_out"]
         heads, a_gamma, a_beta = self._mesa_inputs((z @ p["mesa_in"])[:, None])
@@ -132,7 +150,7 @@ class Block:
         o = L.decode_step(state["H"], state["G"], q, k, v, f["gamma"][..., -1].contiguous(), f["beta"][..., -1].contiguous(),
                           f["lam"], N_CG)
         y = L.output_norm(o[:, :, None].contiguous(), p["norm"], out_dtype=torch.float32).view(B, HEADS * HEAD)
-        return (z + y @ p["mesa_out"]) @ p["logits"]
+        return (z + y @ p["mesa_out"]) @ p["logits"].T
 
 
 def batch(gen, device, rows=8, length=200):
@@ -153,14 +171,10 @@ def train(steps=60, device="cuda", say=print):
     moments = {n: (torch.zeros_like(t), torch.zeros_like(t)) for n, t in block.p.items()}
     for step in range(1, steps + 1):
         tokens, reset, answers = batch(gen, device)
-        logits, kept = block.forward(tokens, reset)
-        there = answers >= 0
-        logp = torch.log_softmax(logits, dim=-1)
-        losses.append(float(-logp[there, answers[there]].mean()))
-        dlogits = logp.exp()
-        dlogits[there, answers[there]] -= 1.0
-        dlogits = torch.where(there[..., None], dlogits, 0.0) / there.sum()
-        for n, grad in block.backward(kept, dlogits).items():
+        out, kept = block.features(tokens, reset)
+        loss, dout, dlogits = block.loss(out, answers)
+        losses.append(float(loss))
+        for n, grad in dict(block.features_backward(kept, dout), logits=dlogits).items():
             m, v = moments[n]
             m.mul_(0.9).add_(grad, alpha=0.1)
             v.mul_(0.98).addcmul_(grad, grad, value=0.02)
@@ -179,7 +193,7 @@ def check_decode(block, device="cuda", say=print):
     reset.zero_()
     want, _ = block.forward(tokens, reset, keep=False)
     _, state = block.forward(tokens[:, :70].contiguous(), reset[:, :70].contiguous(), keep=False)
-    worst = max(float((block.decode(tokens[:, t], state) - want[:, t]).abs().max()) for t in range(70, 80))
+    worst = max(float((block.decode(tokens[:, t].contiguous(), state) - want[:, t]).abs().max()) for t in range(70, 80))
     say("decoding a token at a time: largest difference %.1e of %.1f" % (worst, float(want.abs().max())))
     return worst / float(want.abs().max())
 
