@@ -256,16 +256,16 @@ __device__ __forceinline__ float tanh_of(float x, float& slope)
 // whose logits are all near are the rule; the others evaluate both for 16 rows at a time.
 constexpr float kNear = 0.5625f;
 struct NearTanh {
-    float c[5];      // for z in the place of x = z / cap
+    float c[5];      // for z in the place of x = z / cap, and `factor` tanh
     float edge;      // largest |z|
-    __device__ explicit NearTanh(float cap)
+    __device__ NearTanh(float cap, float factor)
     {
-        const float inv = cap > 0.0f ? 1.0f / cap : 0.0f, q = inv * inv;
-        c[0] = 0.99999996002f * inv;
-        c[1] = -0.33332697360f * inv * q;
-        c[2] = 0.13316993368f * inv * q * q;
-        c[3] = -0.05247611788f * inv * q * q * q;
-        c[4] = 0.01610694871f * inv * q * q * q * q;
+        const float inv = cap > 0.0f ? 1.0f / cap : 0.0f, q = inv * inv, f = factor * inv;
+        c[0] = 0.99999996002f * f;
+        c[1] = -0.33332697360f * f * q;
+        c[2] = 0.13316993368f * f * q * q;
+        c[3] = -0.05247611788f * f * q * q * q;
+        c[4] = 0.01610694871f * f * q * q * q * q;
         edge = kNear * cap;
         // powers of a far cap that leave fp32's range, up or down, take the general form
         const float last = inv * q * q * q * q;
@@ -279,9 +279,9 @@ struct NearTanh {
 };
 
 // The form that an element's own magnitude asks for: what a row gets does not hang on its neighbours'.
-__device__ __forceinline__ float any_tanh(const NearTanh& near, float z, float inv, float& slope)
+__device__ __forceinline__ float any_tanh(const NearTanh& near, float factor, float z, float inv, float& slope)
 {
-    const float far = tanh_of(z * inv, slope), y = near(z);
+    const float far = factor * tanh_of(z * inv, slope), y = near(z);
     const bool is_near = fabsf(z) <= near.edge;
     slope = is_near ? fmaf(-y, y, 1.0f) : slope;
     return is_near ? y : far;
@@ -395,9 +395,10 @@ __global__ void __launch_bounds__(S::kThreads) logits_kernel(LogitsArgs a)
             }
         }
     }
-    const NearTanh near(a.cap);
+    const bool plain = a.cap > 0.0f && a.cap <= kPlainCap;      // then nothing has to be taken off the logits,
+    const float factor = plain ? a.cap * kLog2e : a.cap;        // which are held as powers of 2
+    const NearTanh near(a.cap, factor);
     const float inv = a.cap > 0.0f ? 1.0f / a.cap : 0.0f;
-    const bool plain = a.cap > 0.0f && a.cap <= kPlainCap;      // then nothing has to be taken off the logits
 #pragma unroll
     for (int j = 0; j < S::NT; ++j) {
         const int64_t row = n0 + (wn * S::NT + j) * 16 + n;
@@ -411,13 +412,13 @@ __global__ void __launch_bounds__(S::kThreads) logits_kernel(LogitsArgs a)
 #pragma unroll
                 for (int i = 0; i < S::MT; ++i)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) acc[i][j][r] = a.cap * near(acc[i][j][r]);
+                    for (int r = 0; r < 4; ++r) acc[i][j][r] = near(acc[i][j][r]);
             } else {
                 float slope;
 #pragma unroll
                 for (int i = 0; i < S::MT; ++i)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) acc[i][j][r] = a.cap * any_tanh(near, acc[i][j][r], inv, slope);
+                    for (int r = 0; r < 4; ++r) acc[i][j][r] = any_tanh(near, factor, acc[i][j][r], inv, slope);
             }
         }
         if (a.at != nullptr) {
@@ -427,7 +428,7 @@ __global__ void __launch_bounds__(S::kThreads) logits_kernel(LogitsArgs a)
                 for (int i = 0; i < S::MT; ++i)
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
-                        if (16 * i + 4 * g + r == t && t < here) a.at[row] = acc[i][j][r];
+                        if (16 * i + 4 * g + r == t && t < here) a.at[row] = acc[i][j][r] * (plain ? kLn2 : 1.0f);
             }
         }
         if (here < S::MT * 16) {
@@ -442,7 +443,7 @@ __global__ void __launch_bounds__(S::kThreads) logits_kernel(LogitsArgs a)
 #pragma unroll
             for (int i = 0; i < S::MT; ++i)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) sum += __builtin_amdgcn_exp2f(acc[i][j][r] * kLog2e);
+                for (int r = 0; r < 4; ++r) sum += __builtin_amdgcn_exp2f(acc[i][j][r]);
         } else {
             top = -kInf;
 #pragma unroll
@@ -581,7 +582,7 @@ __global__ void __launch_bounds__(S::kThreads) logits_grad_kernel(LogitsArgs a)
     const int here = int(min(a.piece - c0, int64_t(S::MT * 16)));
     if constexpr (S::Planes == 2) scale_back<S>(acc, a, c0, n0 + wn * S::NT * 16, g, n);
     const float inv = a.cap > 0.0f ? 1.0f / a.cap : 0.0f, scale = (a.cap > 0.0f ? a.cap : 1.0f) * kLog2e;
-    const NearTanh near(a.cap);
+    const NearTanh near(a.cap, 1.0f);
 #pragma unroll
     for (int j = 0; j < S::NT; ++j) {
         const int64_t row = n0 + (wn * S::NT + j) * 16 + n;
@@ -616,7 +617,7 @@ __global__ void __launch_bounds__(S::kThreads) logits_grad_kernel(LogitsArgs a)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     float slope = 1.0f, y = acc[i][j][r];
-                    if (a.cap > 0.0f) y = any_tanh(near, y, inv, slope);
+                    if (a.cap > 0.0f) y = any_tanh(near, 1.0f, y, inv, slope);
                     const float p = __builtin_amdgcn_exp2f(fmaf(y, scale, -lse2));
                     acc[i][j][r] = (16 * i + 4 * g + r == mine ? p - 1.0f : p) * (slope * up);
                 }
