@@ -326,6 +326,7 @@ struct LogitsArgs {
     // gradient
     const float* lse;
     const float* dloss;
+    float* rest;              // [rows], of bf16: what rounding takes off the target's dz
     uint16_t* dz;             // planes of [row][piece], dz_ld elements a row
     int64_t dz_ld, dz_plane, dz_rows;
 };
@@ -631,8 +632,16 @@ __global__ void __launch_bounds__(S::kThreads) logits_grad_kernel(LogitsArgs a)
         }
         if (row >= a.dz_rows) continue;
         uint16_t* dst = a.dz + row * a.dz_ld + c0 + 4 * g;
-        // rounded to bf16 once for both products: 2^-8 of an element at most, at random over the sums
+        // Rounded to bf16 once for both products: 2^-8 of an element at most, at random over the sums.  But for the
+        // target's, as large as all others of its row together: what its rounding takes off is kept, and dh gets it back.
         if constexpr (S::Planes == 1) {
+            if (target) {
+#pragma unroll
+                for (int i = 0; i < S::MT; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (16 * i + 4 * g + r == mine) a.rest[row] = acc[i][j][r] - __uint_as_float(pack_bf16(acc[i][j][r], 0.0f) << 16);
+            }
 #pragma unroll
             for (int i = 0; i < S::MT; ++i)
                 *reinterpret_cast<uint2*>(dst + 16 * i) = make_uint2(pack_bf16(acc[i][j][0], acc[i][j][1]), pack_bf16(acc[i][j][2], acc[i][j][3]));
@@ -650,6 +659,47 @@ __global__ void __launch_bounds__(S::kThreads) logits_grad_kernel(LogitsArgs a)
     }
 }
 
+// Rows whose target is none come out as zeros (targets.p null: every row counts), the others with rest times
+// their target's row of the table added (rest null: nothing).
+struct Finish {
+    Tokens targets;
+    int64_t vocab;
+    const float* rest;
+    const uint16_t* table;
+    int64_t table_stride;
+};
+struct RowEnd {
+    bool counts;
+    float rest;
+    const uint16_t* target;      // its row of the table, or null
+    __device__ RowEnd(const Finish& f, int64_t row) : counts(true), rest(0.0f), target(nullptr)
+    {
+        if (f.targets.p == nullptr) return;
+        const int64_t t = token_at(f.targets, row);
+        counts = t >= 0 && t < f.vocab;
+        if (!counts || f.rest == nullptr) return;
+        rest = f.rest[row];
+        target = f.table + t * f.table_stride;
+    }
+    // Its channels m .. m + 3 (n of them exist) as they lie, and added to a sum.
+    __device__ __forceinline__ uint2 load(int64_t m, int n) const
+    {
+        typedef uint32_t words_any __attribute__((ext_vector_type(2), aligned(2)));
+        if (target == nullptr || n <= 0) return make_uint2(0, 0);
+        if (n == 4) {
+            const words_any w = *reinterpret_cast<const words_any*>(target + m);
+            return make_uint2(w[0], w[1]);
+        }
+        return make_uint2(target[m] | (n > 1 ? uint32_t(target[m + 1]) << 16 : 0u), n > 2 ? target[m + 2] : 0u);
+    }
+    __device__ __forceinline__ f32x4 add(const f32x4& y, uint2 w) const
+    {
+        if (!counts) return f32x4{0.f, 0.f, 0.f, 0.f};
+        return f32x4{fmaf(rest, __uint_as_float(w.x << 16), y[0]), fmaf(rest, __uint_as_float(w.x & 0xFFFF0000u), y[1]),
+                     fmaf(rest, __uint_as_float(w.y << 16), y[2]), fmaf(rest, __uint_as_float(w.y & 0xFFFF0000u), y[3])};
+    }
+};
+
 // out[n][m] = sum_k A(m, k) B(n, k): m a channel, n a row of dh or of the table's gradient.
 struct GradArgs {
     Matrix a, b;
@@ -660,12 +710,10 @@ struct GradArgs {
     float* slab;
     int64_t slab_ld, slab_layer;
     bool first;
-    // the result, or null (then the slab is written): rows out_stride apart; rows whose target is
-    // none are 0 (targets.p null: every row counts)
+    // the result, or null (then the slab is written): rows out_stride apart
     void* out;
     int64_t out_stride;
-    Tokens targets;
-    int64_t vocab;
+    Finish finish;
 };
 
 template <typename T>
@@ -699,25 +747,30 @@ __global__ void __launch_bounds__(S::kThreads) grad_kernel(GradArgs a)
     for (int j = 0; j < S::NT; ++j) {
         const int64_t row = n0 + (wn * S::NT + j) * 16 + n;
         if (row >= a.n) continue;
-        bool counts = true;
-        if (a.out != nullptr && a.targets.p != nullptr) {
-            const int64_t t = token_at(a.targets, row);
-            counts = t >= 0 && t < a.vocab;
+        const int64_t first = m0 + wm * S::MT * 16 + 4 * g;
+        if (a.out == nullptr) {
+#pragma unroll
+            for (int i = 0; i < S::MT; ++i) {
+                if (first + 16 * i >= a.width) continue;
+                f32x4* to = reinterpret_cast<f32x4*>(slab + row * a.slab_ld + first + 16 * i);
+                *to = a.first ? acc[i][j] : acc[i][j] + *to;
+            }
+            continue;
+        }
+        const RowEnd end(a.finish, row);
+        uint2 w[S::MT];
+        int left[S::MT];
+#pragma unroll
+        for (int i = 0; i < S::MT; ++i) {
+            left[i] = int(max(min(a.width - first - 16 * i, int64_t(4)), int64_t(0)));
+            w[i] = end.load(first + 16 * i, left[i]);
         }
 #pragma unroll
         for (int i = 0; i < S::MT; ++i) {
-            const int64_t m = m0 + (wm * S::MT + i) * 16 + 4 * g;
-            if (m >= a.width) continue;
+            if (left[i] == 0) continue;
             f32x4 y = acc[i][j];
-            float* s = slab + row * a.slab_ld + m;
-            if (slab != nullptr && !a.first) y += *reinterpret_cast<const f32x4*>(s);
-            if (a.out == nullptr) {
-                *reinterpret_cast<f32x4*>(s) = y;
-            } else {
-                if (!counts) y = f32x4{0.f, 0.f, 0.f, 0.f};
-                const int left = int(min(a.width - m, int64_t(4)));
-                put4(static_cast<T*>(a.out) + row * a.out_stride + m, left, wide && left == 4, y);
-            }
+            if (slab != nullptr && !a.first) y += *reinterpret_cast<const f32x4*>(slab + row * a.slab_ld + first + 16 * i);
+            put4(static_cast<T*>(a.out) + row * a.out_stride + first + 16 * i, left[i], wide && left[i] == 4, end.add(y, w[i]));
         }
     }
 }
@@ -729,8 +782,7 @@ struct SumArgs {
     int64_t n, width;
     void* out;
     int64_t out_stride;
-    Tokens targets;
-    int64_t vocab;
+    Finish finish;
 };
 constexpr int kSumThreads = 256;
 
@@ -742,19 +794,13 @@ __global__ void __launch_bounds__(kSumThreads) layer_sum_kernel(SumArgs a)
     const int64_t row = i / per, m = i % per * 4;
     if (m >= a.width) return;
     f32x4 y = {0.f, 0.f, 0.f, 0.f};
-    bool counts = true;
-    if (a.targets.p != nullptr) {
-        const int64_t t = token_at(a.targets, row);
-        counts = t >= 0 && t < a.vocab;
-    }
-    if (counts) {
-        const float* s = a.slab + row * a.slab_ld + m;
+    const float* src = a.slab + row * a.slab_ld + m;
 #pragma unroll 4
-        for (int64_t l = 0; l < a.layers; ++l) y += *reinterpret_cast<const f32x4*>(s + l * a.slab_layer);
-    }
+    for (int64_t l = 0; l < a.layers; ++l) y += *reinterpret_cast<const f32x4*>(src + l * a.slab_layer);
     T* p = static_cast<T*>(a.out) + row * a.out_stride + m;
     const int left = int(min(a.width - m, int64_t(4)));
-    put4(p, left, left == 4 && uintptr_t(p) % (4 * sizeof(T)) == 0, y);
+    const RowEnd end(a.finish, row);
+    put4(p, left, left == 4 && uintptr_t(p) % (4 * sizeof(T)) == 0, end.add(y, end.load(m, left)));
 }
 
 // ------------------------------------------------------------------ plans
@@ -898,7 +944,7 @@ struct ForwardPlan {
 
 struct GradPlan {
     // h and the table as the gradients' products read them, and (fp32) as the logits' does, with the exponents
-    int64_t piece, dz, dz_rows, dz_ld, h, table, h16, table16, h_e, table_e, slab_h, slab_e, bytes, ld;
+    int64_t piece, dz, dz_rows, dz_ld, h, table, h16, table16, h_e, table_e, rest, slab_h, slab_e, bytes, ld;
     Shape logits;
     Cut dh, de, de_last;
     GradPlan(int64_t rows, int64_t vocab, int64_t width, int dtype)
@@ -918,9 +964,9 @@ struct GradPlan {
         logits = shape_of(piece, rows, width, logit_planes(dtype));
         dh = layers(width, rows, std::min(piece, vocab), planes);
         // the last piece may be much shorter, and is then cut otherwise
-        const int64_t rest = vocab - (ceil_div(vocab, piece) - 1) * piece;
+        const int64_t ending = vocab - (ceil_div(vocab, piece) - 1) * piece;
         de = layers(width, std::min(piece, vocab), rows, planes);
-        de_last = layers(width, rest, rows, planes);
+        de_last = layers(width, ending, rows, planes);
         Carve c;
         h = c.take(dz_rows * ld * 2 * planes);
         table = c.take(piece * ld * 2 * planes);
@@ -928,9 +974,10 @@ struct GradPlan {
         table16 = planes == 1 ? table : c.take(piece * ld * 4);
         h_e = planes == 1 ? 0 : c.take(exponents_of(dz_rows) * 4);
         table_e = planes == 1 ? 0 : c.take(exponents_of(piece) * 4);
+        rest = planes == 1 ? c.take(rows * 4) : 0;
         dz = c.take(dz_rows * dz_ld * 2 * planes);
         slab_h = dh.layers > 1 || piece < vocab ? c.take(dh.layers * rows * ld * 4) : 0;
-        const int64_t layered = std::max(de.layers > 1 ? de.layers * piece : 0, de_last.layers > 1 ? de_last.layers * rest : 0);
+        const int64_t layered = std::max(de.layers > 1 ? de.layers * piece : 0, de_last.layers > 1 ? de_last.layers * ending : 0);
         slab_e = layered > 0 ? c.take(layered * ld * 4) : 0;
         bytes = c.at;
     }
@@ -1046,7 +1093,7 @@ hipError_t launch_cross_entropy_grad(const CrossEntropyGradArgs& a, hipStream_t 
 {
     if (a.rows == 0) {      // the table's gradient is the sum of nothing
         if (a.dtable == nullptr) return hipSuccess;
-        const SumArgs none{nullptr, ceil_to(a.width, 4), 0, 0, a.vocab, a.width, a.dtable, a.dtable_stride, Tokens{}, 0};
+        const SumArgs none{nullptr, ceil_to(a.width, 4), 0, 0, a.vocab, a.width, a.dtable, a.dtable_stride, {}};
         return launch_sum(none, a.dtype, stream);
     }
     const GradPlan plan(a.rows, a.vocab, a.width, a.dtype);
@@ -1055,6 +1102,7 @@ hipError_t launch_cross_entropy_grad(const CrossEntropyGradArgs& a, hipStream_t 
     char* ws = a.workspace;
     auto words = [&](int64_t at) { return reinterpret_cast<uint16_t*>(ws + at); };
     uint16_t* dz = words(plan.dz);
+    float* rest = planes == 1 ? reinterpret_cast<float*>(ws + plan.rest) : nullptr;
     const bool as_is = direct(a.table, a.table_stride, a.width, a.dtype);
     const int64_t dz_plane = plan.dz_rows * plan.dz_ld;
     const Matrix h{words(plan.h), ld, plan.dz_rows * ld, plan.dz_rows, ld};
@@ -1097,6 +1145,7 @@ hipError_t launch_cross_entropy_grad(const CrossEntropyGradArgs& a, hipStream_t 
         k.cap = a.cap;
         k.lse = a.lse;
         k.dloss = a.dloss;
+        k.rest = rest;
         k.dz = dz;
         k.dz_ld = plan.dz_ld;
         k.dz_plane = dz_plane;
@@ -1129,11 +1178,10 @@ hipError_t launch_cross_entropy_grad(const CrossEntropyGradArgs& a, hipStream_t 
             d.first = first == 0;
             d.out = layers == 1 && last ? a.dh : nullptr;
             d.out_stride = a.dh_stride;
-            d.targets = a.targets;
-            d.vocab = a.vocab;
+            d.finish = Finish{a.targets, a.vocab, rest, static_cast<const uint16_t*>(a.table), a.table_stride};
             if (e = launch_grad<true>(d, plan.dh.shape, ceil_div(d.k, d.k_split), planes, stream); e != hipSuccess) return e;
             if (last && layers > 1) {
-                const SumArgs s{d.slab, ld, d.slab_layer, layers, a.rows, a.width, a.dh, a.dh_stride, a.targets, a.vocab};
+                const SumArgs s{d.slab, ld, d.slab_layer, layers, a.rows, a.width, a.dh, a.dh_stride, d.finish};
                 if (e = launch_sum(s, a.dtype, stream); e != hipSuccess) return e;
             }
         }
@@ -1159,7 +1207,7 @@ hipError_t launch_cross_entropy_grad(const CrossEntropyGradArgs& a, hipStream_t 
             d.out_stride = a.dtable_stride;
             if (e = launch_grad<false>(d, shape, layers, planes, stream); e != hipSuccess) return e;
             if (layers > 1) {
-                const SumArgs s{d.slab, ld, d.slab_layer, layers, piece, a.width, out, a.dtable_stride, Tokens{}, 0};
+                const SumArgs s{d.slab, ld, d.slab_layer, layers, piece, a.width, out, a.dtable_stride, {}};
                 if (e = launch_sum(s, a.dtype, stream); e != hipSuccess) return e;
             }
         }
