@@ -895,8 +895,13 @@ bool direct(const void* p, int64_t stride, int64_t width, int dtype)
     return dtype == kBf16 && width % kStepK == 0 && stride % 8 == 0 && stride < (int64_t(1) << 22) && uintptr_t(p) % 16 == 0;
 }
 
-constexpr int64_t kCopyBytes = int64_t(64) << 20;      // of the table's rows that are copied at a time, forward
-constexpr int64_t kPieceBytes = int64_t(256) << 20;    // of dz at a time
+// Of the table's rows that are copied at a time, forward: each time costs two launches whose ends leave the card
+// part empty.  One row by 50257 of 1000 bf16 channels, 103 MB of them: 62 us at 64 MiB, 51 in one; 2000 rows by 50257
+// of 768 fp32 channels 566, 547 (128 MiB), 527 (256), 524 (in one).
+constexpr int64_t kCopyBytes = int64_t(256) << 20;
+// Elements of dz at a time.  16384 rows by 50257 of 2048 bf16 channels: backward 9.41 ms with half as many, 8.60 with
+// these, 8.58 with twice, 9.01 with four times; 4096 rows of 768 fp32 channels 4.88, 4.57, 4.53, 4.47.
+constexpr int64_t kPieceElements = int64_t(1) << 27;
 constexpr int64_t kSlabBytes = int64_t(256) << 20;     // of fp32 layers of one product, at most (or one layer)
 
 // Rows of the table in a piece of the forward, where it has to be copied.
@@ -952,7 +957,7 @@ struct GradPlan {
         const int planes = grad_planes(dtype);
         ld = ceil_to(width, kStepK);
         dz_rows = ceil_to(rows, 64);
-        piece = std::max<int64_t>(256, kPieceBytes / (dz_rows * 2 * planes) / 256 * 256);
+        piece = std::max<int64_t>(256, kPieceElements / dz_rows / 256 * 256);
         // pieces whose part of the table's gradient is whole rounds of wide tiles on all compute units, where they are
         // large enough for that; else pieces of about the same size
         const int64_t round = std::max<int64_t>(1, kUnits / ceil_div(width, shape_m(kWide, planes))) * shape_n(kWide, planes);
@@ -1053,10 +1058,12 @@ hipError_t launch_cross_entropy(const CrossEntropyArgs& a, hipStream_t stream)
     }
     const JoinArgs j{k.part, k.best_z, k.best_v, k.at, a.targets, a.rows, a.vocab,
                      ceil_div(a.vocab, shape_m(shape, planes)), a.targets.p == nullptr ? nullptr : a.loss, a.lse, a.best};
-    // a workgroup for each of few rows; sixteen neighbours, whose sums lie side by side, of many
-    const int64_t blocks = a.rows <= 1024 ? a.rows : ceil_div(a.rows, 16);
+    // a workgroup for each of few rows; sixteen neighbours, whose sums lie side by side, of many (calls by 50257 of 64
+    // channels: 256 rows 19.6 us against 23.6, 512 33.2 and 32.8, 1024 55.2 and 53.0, 2048 104 and 94)
+    const bool few = a.rows < 512;
+    const int64_t blocks = few ? a.rows : ceil_div(a.rows, 16);
     if (!grid_fits(blocks, kJoinThreads)) return hipErrorInvalidConfiguration;
-    if (a.rows <= 1024)
+    if (few)
         hipLaunchKernelGGL((join_kernel<1>), dim3(unsigned(blocks)), dim3(kJoinThreads), 0, stream, j);
     else
         hipLaunchKernelGGL((join_kernel<16>), dim3(unsigned(blocks)), dim3(kJoinThreads), 0, stream, j);

@@ -1,7 +1,7 @@
 // Token embedding, y_n = scale E[t_n], and the gradient of its table, dE_v = scale sum_{n: t_n = v} dy_n.
 //
 // The look-up is a copy.  The gradient sorts the tokens (least significant digits first, stable), so
-// that the rows of one token follow each other in the order in which they came.  Then every piece of 16
+// that the rows of one token follow each other in the order in which they came.  Then every piece of 8 or 16
 // sorted positions is added up by one group of lanes, in order: tokens that begin and end in the piece
 // are written to the table, and the sums of the piece's first and last token, where those go on past it,
 // are kept; a last launch adds those up along each such token (of many rows over whole runs of 32 pieces).
@@ -136,7 +136,8 @@ template <typename T, typename O, int V>
 hipError_t lookup(const EmbeddingArgs& a, hipStream_t stream)
 {
     const Lanes lanes = lanes_for(a.width, V);
-    // two rows a group keep two loads under way behind one look at the tokens; few rows are spread instead
+    // two rows a group keep two loads under way behind one look at the tokens: 65536 rows of 2048 bf16 channels take
+    // 82 us so, 97 one by one, 16384 the same either way; fewer are spread over the card
     const bool many = a.rows >= 2048 * lanes.rows();
     const int64_t at_once = lanes.rows() * (many ? 2 : 1), blocks = (a.rows + at_once - 1) / at_once;
     if (!grid_fits(blocks, kThreads)) return hipErrorInvalidConfiguration;
@@ -152,7 +153,7 @@ constexpr int kTile = 1024;            // tokens a workgroup sorts
 constexpr int kWaves = kThreads / kWave;
 constexpr int kRounds = kTile / kThreads;
 constexpr int kDigitBits = 9, kBins = 1 << kDigitBits;
-constexpr int kPiece = 16, kRun = 32;  // sorted positions of a piece; pieces of a run
+constexpr int kRun = 32;               // pieces of a run
 
 // A token's key: itself, or vocab for one that does not count, which comes last.
 __device__ __forceinline__ uint32_t key_of(const Tokens& t, int64_t i, int64_t vocab)
@@ -429,10 +430,18 @@ struct SumArgs {
     void* dtable;
 };
 
+// Sorted positions of a piece: short ones make more waves of few rows, long ones fewer sums to join.  777 rows of 321
+// fp32 channels take 14.6 us by 8, 17.6 by 16 and 23.7 by 32, 4096 of 1024 bf16 ones 27.9, 30.1 and 35.8, 16384 of
+// 2048 60.0, 55.0 and 57.2 (and all of them one token 204, 126 and 86).
+constexpr int kFewPiece = 8, kManyPiece = 16;
+constexpr int64_t kFewRows = 8192;
+int64_t piece_of(int64_t rows) { return rows <= kFewRows ? kFewPiece : kManyPiece; }
+
 constexpr int kDepth = 16;         // sums asked for together
 constexpr uint32_t kNoKey = 0xFFFFFFFFu;
-// Past so many rows there are runs of pieces.  Up to there a token that is everywhere has 1024 pieces at most,
-// which one group adds in some 100 us; a launch for everyone's runs costs 5.
+// Past so many rows there are runs of pieces.  Up to there a token that is everywhere has 1024 pieces at most: 16384
+// rows of 2048 bf16 channels take 55 us, 126 if they are one token, with runs 60 and 55.  65536 of 512 take 77 and
+// 333 without runs, 69 and 84 with them.
 constexpr int64_t kRunRows = 16384;
 
 template <typename O, int V>
@@ -449,7 +458,7 @@ __device__ __forceinline__ void write_row(const SumArgs& a, uint32_t token, cons
 }
 
 // Each piece of sorted positions: its tokens' sums.
-template <typename T, typename O, int V>
+template <typename T, typename O, int V, int kPiece>
 __global__ void __launch_bounds__(kThreads) token_piece_kernel(SumArgs a, Lanes lanes)
 {
     const int64_t piece = int64_t(blockIdx.x) * lanes.rows() + lanes.row(), first = piece * kPiece;
@@ -502,7 +511,7 @@ __global__ void __launch_bounds__(kThreads) token_piece_kernel(SumArgs a, Lanes 
 }
 
 // Sums of the runs of pieces that lie within one token's rows, the first of which come before them.
-template <int V>
+template <int V, int kPiece>
 __global__ void __launch_bounds__(kThreads) token_run_kernel(SumArgs a)
 {
     const int64_t first = int64_t(blockIdx.x) * kPiece * kRun;
@@ -548,6 +557,7 @@ __device__ __forceinline__ void add_rows(float (&sum)[V], const float* rows, int
 }
 
 // Past the last of the sorted positions from `at` on that have the same key.
+template <int kPiece>
 __device__ __forceinline__ int64_t end_of(const uint32_t* keys, int64_t at, int64_t rows)
 {
     const uint32_t key = keys[at];
@@ -571,9 +581,10 @@ __device__ __forceinline__ int64_t end_of(const uint32_t* keys, int64_t at, int6
 
 // Past the last of the pieces that a token enters which goes on after position `last`, the end of a piece.
 // A piece is entered where it begins with the token; a whole wave of one group looks at 64 of them at once.
+template <int kPiece>
 __device__ __forceinline__ int64_t pieces_entered(const SumArgs& a, uint32_t token, int64_t last, const Lanes& lanes)
 {
-    if (lanes.log2 < 6) return (end_of(a.keys, last, a.rows) + kPiece - 1) / kPiece;
+    if (lanes.log2 < 6) return (end_of<kPiece>(a.keys, last, a.rows) + kPiece - 1) / kPiece;
     const int64_t pieces = (a.rows + kPiece - 1) / kPiece;
     for (int64_t p = last / kPiece + 1;; p += kWave) {
         const int64_t mine = p + int(threadIdx.x) % kWave;
@@ -583,7 +594,7 @@ __device__ __forceinline__ int64_t pieces_entered(const SumArgs& a, uint32_t tok
 }
 
 // The tokens that begin in a piece and go on after it, one a group of lanes.
-template <typename O, int V>
+template <typename O, int V, int kPiece>
 __global__ void __launch_bounds__(kThreads) token_join_kernel(SumArgs a, Lanes lanes)
 {
     const int64_t piece = int64_t(blockIdx.x) * lanes.rows() + lanes.row(), first = piece * kPiece, last = first + kPiece - 1;
@@ -591,7 +602,7 @@ __global__ void __launch_bounds__(kThreads) token_join_kernel(SumArgs a, Lanes l
     const uint32_t token = a.keys[last];
     if (token >= uint32_t(a.vocab) || a.keys[last + 1] != token) return;
     if (first > 0 && a.keys[first - 1] == token) return;      // it begins before
-    const int64_t p0 = piece + 1, p1 = pieces_entered(a, token, last, lanes);
+    const int64_t p0 = piece + 1, p1 = pieces_entered<kPiece>(a, token, last, lanes);
     const int64_t from = (int64_t(blockIdx.y) * lanes.count() + lanes.lane()) * V;
     if (from >= a.width) return;
     const Place c = place_of<V>(from, a.width);
@@ -627,7 +638,8 @@ struct GradLayout {
         };
         hist = take(tiles * kBins * 4);
         for (int k = 0; k < 2; ++k) keys[k] = take(rows * 4), places[k] = take(rows * 4);
-        const int64_t pieces = (rows + kPiece - 1) / kPiece;
+        // no fewer for more rows: a workspace for many serves fewer
+        const int64_t few = std::min(rows, kFewRows), pieces = std::max((rows + piece_of(rows) - 1) / piece_of(rows), (few + kFewPiece - 1) / kFewPiece);
         entered = take(pieces * ld * 4);
         left = take(pieces * ld * 4);
         runs = rows <= kRunRows ? 0 : take(pieces / kRun * ld * 4);
@@ -635,8 +647,8 @@ struct GradLayout {
     }
 };
 
-template <typename T, typename O, int V>
-hipError_t sums(const SumArgs& a, hipStream_t stream)
+template <typename T, typename O, int V, int kPiece>
+hipError_t sums_of(const SumArgs& a, hipStream_t stream)
 {
     const int64_t pieces = (a.rows + kPiece - 1) / kPiece, runs = a.rows <= kRunRows ? 0 : pieces / kRun;
     const Lanes lanes = lanes_for(a.width, V);
@@ -644,10 +656,17 @@ hipError_t sums(const SumArgs& a, hipStream_t stream)
     // a workgroup's lanes side by side, and along the second dimension of the grid
     const unsigned slabs = unsigned((a.width + lanes.count() * V - 1) / (lanes.count() * V));
     if (!grid_fits(blocks, kThreads) || !grid_fits(runs, kThreads)) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL((token_piece_kernel<T, O, V>), dim3(unsigned(blocks), slabs), dim3(kThreads), 0, stream, a, lanes);
-    if (runs > 0) hipLaunchKernelGGL((token_run_kernel<V>), dim3(unsigned(runs)), dim3(kThreads), 0, stream, a);
-    if (pieces > 1) hipLaunchKernelGGL((token_join_kernel<O, V>), dim3(unsigned(blocks), slabs), dim3(kThreads), 0, stream, a, lanes);
+    hipLaunchKernelGGL((token_piece_kernel<T, O, V, kPiece>), dim3(unsigned(blocks), slabs), dim3(kThreads), 0, stream, a, lanes);
+    if constexpr (kPiece == kManyPiece)
+        if (runs > 0) hipLaunchKernelGGL((token_run_kernel<V, kPiece>), dim3(unsigned(runs)), dim3(kThreads), 0, stream, a);
+    if (pieces > 1) hipLaunchKernelGGL((token_join_kernel<O, V, kPiece>), dim3(unsigned(blocks), slabs), dim3(kThreads), 0, stream, a, lanes);
     return hipGetLastError();
+}
+
+template <typename T, typename O, int V>
+hipError_t sums(const SumArgs& a, hipStream_t stream)
+{
+    return piece_of(a.rows) == kFewPiece ? sums_of<T, O, V, kFewPiece>(a, stream) : sums_of<T, O, V, kManyPiece>(a, stream);
 }
 
 }  // namespace
@@ -722,8 +741,10 @@ hipError_t launch_embedding_grad(const EmbeddingGradArgs& a, hipStream_t stream)
     const SumArgs k{a.dy, a.rows, a.vocab, a.width, a.dy_stride, a.table_stride, lay.ld, a.scale, a.accumulate, keys[out], places[out],
                     reinterpret_cast<float*>(ws + lay.entered), reinterpret_cast<float*>(ws + lay.left),
                     reinterpret_cast<float*>(ws + lay.runs), a.dtable};
-    // few rows have a lane for each channel: 777 rows of 321 take 17.6 us so, 19.2 with eight channels a lane
-    const bool wide = a.width >= 8 && a.rows * a.width >= (int64_t(1) << 19);
+    // Few sums have a lane each, so that there are waves enough for the loads' latency: 16384 rows of 64 bf16 channels
+    // take 30.8 us so and 35.8 with eight channels a lane, 1024 of 2048 14.2 and 16.0, 4096 of 1000 29.6 and 29.3,
+    // 16384 of 320 34.7 and 31.6.
+    const bool wide = a.width >= 8 && a.rows * a.width >= (int64_t(1) << 22);
     if (a.dtype == kBf16 && a.table_dtype == kBf16) return wide ? sums<bf16_t, bf16_t, 8>(k, stream) : sums<bf16_t, bf16_t, 1>(k, stream);
     if (a.dtype == kBf16) return wide ? sums<bf16_t, float, 8>(k, stream) : sums<bf16_t, float, 1>(k, stream);
     if (a.table_dtype == kBf16) return wide ? sums<float, bf16_t, 8>(k, stream) : sums<float, bf16_t, 1>(k, stream);

@@ -107,7 +107,7 @@ def test_workspace_bytes():
         assert 0 < f(1, 1, 1, 1) < 1 << 20
     # dz is held a piece at a time, the logits never: 16384 rows of 50257 would be 3.3 GB of them
     assert L.cross_entropy_backward_workspace_bytes(16384, 50257, 2048, 1) < 700 << 20
-    assert L.cross_entropy_workspace_bytes(16384, 50257, 2048, 1) < 200 << 20
+    assert L.cross_entropy_workspace_bytes(16384, 50257, 2048, 1) < 400 << 20
 
 
 def test_binding_checks():

@@ -117,9 +117,9 @@ def test_embedding_backward(rows, vocab, width, pad, dtype, out):
     assert torch.equal(room[quiet], base[quiet]) and torch.equal(room[:, width:], base[:, width:])
 
 
-@pytest.mark.parametrize("rows", [15, 16, 17, 511, 512, 513, 3000, 5000, 16384, 16385, 17000, 33793, 40000])
+@pytest.mark.parametrize("rows", [7, 8, 9, 15, 16, 17, 511, 512, 513, 3000, 5000, 8191, 8192, 8193, 16384, 16385, 17000, 33793, 40000])
 def test_one_token_everywhere(rows):
-    """Every row the same token, at lengths around whole pieces of 16 and runs of 512 sorted positions."""
+    """Every row the same token, at lengths around whole pieces of 8 and 16 and runs of 512 sorted positions."""
     rng = np.random.default_rng(rows)
     dy = _table(rng, rows, 40, F32)
     t = np.full(rows, 2)

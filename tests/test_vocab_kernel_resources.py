@@ -36,8 +36,8 @@ LIMITS = [
     (r"embedding_kernel<(float|bf16_t), (float|bf16_t), (1|8), (1|2)>", 64),
     (r"token_(histogram|scatter)_kernel", 64),
     (r"token_sort_kernel<(1|2)>", 64),
-    (r"token_piece_kernel<float, (float|bf16_t), 8>", 256),
-    (r"token_piece_kernel<bf16_t, (float|bf16_t), 8>", 168),
+    (r"token_piece_kernel<float, (float|bf16_t), 8, (8|16)>", 256),
+    (r"token_piece_kernel<bf16_t, (float|bf16_t), 8, (8|16)>", 168),
     (r"token_run_kernel", 168),
     (r"token_join_kernel", 256),
 ]
