@@ -547,8 +547,8 @@ int mesa_output_norm_backward(const void* o, const float* weight, float eps, con
  * mesa_embedding_backward: dE_v = scale sum over n with token_n = v of dy_n (zeros where there is
  *   none), added in the order of n; with `accumulate` not 0 it is added to what dtable holds
  *   (rows of tokens that do not occur are then not touched).  dy of grad_dtype, dtable of
- *   table_dtype.  Rows of dy that have no token are not read.  Three kernel launches up to 16384
- *   rows, else six or seven (more from a vocabulary of 2^18 on). */
+ *   table_dtype.  Rows of dy that have no token are not read.  Three kernel launches up to 2048
+ *   rows; beyond, two for every nine bits of the vocabulary's size and two or three more. */
 int mesa_embedding(const void* table, const void* token, int token_bytes, float scale, int64_t rows, int64_t vocab,
                    int64_t width, int64_t table_stride, int dtype, int out_dtype, int64_t out_stride, void* out,
                    void* stream);
@@ -562,21 +562,22 @@ int mesa_embedding_backward(const void* token, int token_bytes, const void* dy, 
  *     z_nv = h_n . E_v,  l = cap tanh(z / cap) (cap 0: l = z),  lse_n = log sum_v exp(l_nv)
  *     loss_n = lse_n - l_n,target  (0 where the target does not count)
  *     best_n = the lowest v whose z_nv is the largest (-1 where every one is a NaN)
- *   h, table   dtype (MESA_DTYPE_F32, MESA_DTYPE_BF16): products of bf16 are exact, those of fp32 are formed
- *              from three bf16 parts of each factor (24 bits); both are summed in fp32
+ *   h, table   dtype (MESA_DTYPE_F32, MESA_DTYPE_BF16).  Sums are fp32; products of bf16 are exact.  Those of fp32 are
+ *              formed from parts of 16 bits, the logits' to 2^-21 of each product (and 2^-39 of their rows' largest
+ *              magnitudes), the gradients' to 2^-24; an infinity among fp32 factors makes its sums NaN
  *   target, loss [rows] fp32: both or neither (then only lse and best are computed)
  *   lse [rows] fp32;  best int32 [rows], or NULL
- *   cap        finite and >= 0
+ *   cap        0, or finite, positive and no subnormal number
  * rows 0 is a no-op; vocab and width must be positive.  Two kernel launches, and one or two more for
- * each 64 MiB of a table that has to be copied (fp32, or spaced or aligned otherwise).
+ * each 256 MiB of a table that has to be copied (fp32, or spaced or aligned otherwise).
  *
  * mesa_cross_entropy_backward: gradients for a given dloss [rows] fp32 and the lse of the forward
  *     dz_nv = dloss_n (exp(l_nv - lse_n) - [v = target_n]) (1 - (l_nv / cap)^2), 0 where the target does not count
  *     dh_n = sum_v dz_nv E_v,  dE_v = sum_n dz_nv h_n
  *   dh [rows, width], dtable [vocab, width]: dtype; either may be NULL.  Rows of h, lse and dloss
  *   whose target does not count may hold anything.  dz, formed a piece of the vocabulary at a time
- *   (the workspace holds at most 256 MiB of it, or 256 columns), is rounded to bf16 for bf16 inputs.  With rows 0
- *   dtable is zeros.  Up to five kernel launches a piece, and a few more. */
+ *   (the workspace holds at most 2^27 elements of it, or 256 columns), is rounded to bf16 for bf16 inputs; dh gets
+ *   back what that takes off each target's element.  With rows 0 dtable is zeros.  Up to six kernel launches a piece. */
 size_t mesa_cross_entropy_workspace_bytes(int64_t rows, int64_t vocab, int64_t width, int dtype);
 int mesa_cross_entropy(const void* h, const void* table, const void* target, int token_bytes, float cap, int64_t rows,
                        int64_t vocab, int64_t width, int64_t h_stride, int64_t table_stride, int dtype, float* loss,

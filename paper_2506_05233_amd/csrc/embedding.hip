@@ -6,8 +6,12 @@
 // are written to the table, and the sums of the piece's first and last token, where those go on past it,
 // are kept; a last launch adds those up along each such token (of many rows over whole runs of 32 pieces).
 // No atomics on values, the same bits every time, and no group walks far, however frequent a token is.
-// The sort keeps a few compute units busy for some 30 us; the others fill the gradient with zeros in the
-// same launches, which is most of its traffic.
+//
+// Both are bound by memory: 16384 rows of 2048 bf16 channels are looked up in 18 us (134 MB, 7.2 TB/s, part of it from
+// the last cache).  Their gradient for 50257 tokens takes 81 us, of which 48 are the sort's launches: it keeps 16 of
+// the compute units busy, and the others fill the gradient with zeros in the same launches, which is most of
+// its traffic (206 of 273 MB, 4.3 TB/s).  The pieces take 20 (67 MB read, 30 written), the join 9, which is latency.
+// Few rows are launches and latency: 777 of 321 fp32 channels 15 us.
 #include <algorithm>
 
 #include "mesa_kernels.hpp"
