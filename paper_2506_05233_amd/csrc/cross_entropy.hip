@@ -11,11 +11,11 @@
 // at a time and multiplied from both sides while it lies in the last cache.
 //
 // Training passes over 16384 rows by 50257 of 2048 bf16 channels take 11.2 ms, logits 2.69 (1250 TFLOP/s), dz
-// 3.09, dh 2.83, the table's gradient 2.61; over 777 rows by 5003 of 768 fp32 ones 197 us.  One row by 50257 of 2048
+// 3.09, dh 2.83, the table's gradient 2.61; over 777 rows by 5003 of 768 fp32 ones 188 us.  One row by 50257 of 2048
 // takes 53 us, which reads its 206 MB at 4.4 TB/s, 256 rows 78.
 //
 // fp32 is multiplied as parts of 16 bits: the logits from two fp16 parts of rows scaled by a power of two (three
-// products; the first version took three bf16 parts, six products: 80 us and 43 for 777 rows by 5003 of 768), the
+// products; the first version took three bf16 parts, six products: 80 us and 38 for 777 rows by 5003 of 768), the
 // gradients from three bf16 parts, since a scale of its own for each row stands in the way of sums over rows.
 #include <algorithm>
 #include <type_traits>
@@ -848,20 +848,21 @@ int64_t shape_size(Shape s, bool n)
 int64_t shape_m(Shape s, int planes) { return planes == 1 ? shape_size<1>(s, false) : planes == 2 ? shape_size<2>(s, false) : shape_size<3>(s, false); }
 int64_t shape_n(Shape s, int planes) { return planes == 1 ? shape_size<1>(s, true) : planes == 2 ? shape_size<2>(s, true) : shape_size<3>(s, true); }
 
-// What a product takes with each tile shape, in us, fitted to 73 sizes of each type (33 to 4000 rows, 1000 to
-// 50257 of the table, 320 to 2048 channels), most of them within a tenth.  A tile alone on its compute unit takes
-// `alone` + `alone_step` a step of k; with as many as share a unit it takes `shared` + `shared_step` of the
-// unit's time.  What that decides, by measurement: 16 x 7 tiles of 128 against 8 x 4 of 256 (2000 x 777 by 50257) 195 us
-// against 165, but 4 tiles of 64 against one of 256 (1000 x 64 by 2048) 13 against 45; fp32 280 tiles of 128 on 256
-// units 65, 160 wide ones 55.
+// What a product takes with each tile shape, in us, fitted to 261 sizes of each type (48 to 4000 rows, 1000 to
+// 50257 of the table, 128 to 2048 channels), half of them within 5 to 8 percent.  A tile alone on its compute unit
+// takes `alone` + `alone_step` a step of k; where more share a unit they take `shared` + `shared_step` of
+// its time each.  The shape of the least cost is 0.4 to 1.1 percent slower than the fastest on average, and more than
+// a tenth in 0 to 4 percent of the sizes.  What it decides, in us (256 or 128 x 256, 128, 64 wide): 777 rows by 5003
+// of 768, bf16 27, 19, 22 a call, fp32 47, 49, 54; 2000 by 32003 of 768 bf16 108, 125, 180; 300 by 5003 of 768 fp32
+// 48, 39, 34.
 struct Cost {
     float alone, alone_step, shared, shared_step;
     int per_unit;
 };
 constexpr Cost kCost[3][4] = {
-    {{13.0f, 1.15f, 9.1f, 1.49f, 1}, {7.0f, 0.66f, 2.6f, 0.47f, 2}, {4.2f, 0.42f, 0.73f, 0.174f, 5}, {4.0f, 0.40f, 0.6f, 0.12f, 6}},
-    {{11.2f, 0.93f, 9.9f, 1.20f, 1}, {8.2f, 0.68f, 3.4f, 0.66f, 2}, {4.7f, 0.41f, 0.57f, 0.29f, 5}, {4.7f, 0.41f, 0.57f, 0.29f, 5}},
-    {{9.7f, 1.68f, 6.7f, 2.13f, 1}, {7.2f, 0.96f, 3.4f, 1.25f, 1}, {4.5f, 0.58f, 0.74f, 0.426f, 3}, {4.5f, 0.58f, 0.74f, 0.426f, 3}}};
+    {{11.6f, 1.29f, 11.6f, 1.29f, 1}, {6.5f, 0.69f, 3.35f, 0.47f, 2}, {4.4f, 0.44f, 0.84f, 0.196f, 5}, {4.0f, 0.40f, 0.6f, 0.12f, 6}},
+    {{11.2f, 1.00f, 11.2f, 1.00f, 1}, {9.5f, 0.67f, 4.2f, 0.64f, 2}, {5.8f, 0.375f, 0.92f, 0.307f, 5}, {5.8f, 0.375f, 0.92f, 0.307f, 5}},
+    {{9.2f, 1.91f, 9.2f, 1.91f, 1}, {5.7f, 1.22f, 5.7f, 1.22f, 1}, {4.3f, 0.62f, 0.90f, 0.40f, 3}, {4.3f, 0.62f, 0.90f, 0.40f, 3}}};
 
 float cost_of(Shape s, int planes, int64_t tiles, int64_t k)
 {

@@ -204,6 +204,46 @@ def test_a_row_does_not_hang_on_its_neighbours(dtype):
         assert all(torch.equal(fo[n][~odd], f[n][~odd]) for n in f) and torch.equal(go["dh"][~odd], g["dh"][~odd])
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_two_steps_at_once(dtype):
+    """Steps of two sizes on two streams, over each other several times: each has the bits that it has alone."""
+    inputs = [_inputs(2500, 1000, 64, dtype, 8), _inputs(700, 3001, 200, dtype, 9)]
+    want = [_step(*x) for x in inputs]
+    streams = [torch.cuda.Stream() for _ in inputs]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(5):
+        for k, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[k].append(_step(*inputs[k]))
+    torch.cuda.synchronize()
+    for k in range(2):
+        for out in got[k]:
+            assert all(torch.equal(x, y) for x, y in zip(out, want[k]))
+
+
+@pytest.mark.parametrize("width", [1, 7, 64, 100, 321])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_gaps_are_not_read(dtype, width):
+    """What lies between spaced rows, behind the last one and before the first may be NaN."""
+    table, tokens, targets, up = _inputs(130, 300, width, dtype, 4)
+    h = L.embedding(table, tokens)
+
+    def spaced(x):
+        room = torch.full((x.shape[0] * (width + 3) + 70,), float("nan"), dtype=dtype, device="cuda")
+        rows = room[33:33 + x.shape[0] * (width + 3)].view(x.shape[0], width + 3)[:, :width]
+        rows.copy_(x)
+        return rows
+
+    a, b = (h, table), (spaced(h), spaced(table))
+    f, g = (L.cross_entropy(*x, targets, cap=CAP, want_best=True) for x in (a, b))
+    assert all(torch.equal(f[n], g[n]) for n in f)
+    f, g = (L.cross_entropy_backward(*x, targets, f["lse"], up, cap=CAP) for x in (a, b))
+    assert all(torch.equal(f[n], g[n]) for n in f)
+    assert torch.equal(L.embedding(b[1], tokens), h)
+    assert torch.equal(L.embedding_backward(tokens, b[0], 300), L.embedding_backward(tokens, h, 300))
+
+
 # ------------------------------------------------------------------ far offsets
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_rows_past_32_bits(dtype):
