@@ -273,16 +273,16 @@ __device__ __forceinline__ float tanh_of(float x, float& slope)
 // whose logits are all near are the rule; the others evaluate both for 16 rows at a time.
 constexpr float kNear = 0.5625f;
 struct NearTanh {
-    float c[5];      // for z in the place of x = z / cap, and `factor` tanh
+    float c[5];      // for z in the place of x = z / cap
     float edge;      // largest |z|
-    __device__ NearTanh(float cap, float factor)
+    __device__ explicit NearTanh(float cap)
     {
-        const float inv = cap > 0.0f ? 1.0f / cap : 0.0f, q = inv * inv, f = factor * inv;
-        c[0] = 0.99999996002f * f;
-        c[1] = -0.33332697360f * f * q;
-        c[2] = 0.13316993368f * f * q * q;
-        c[3] = -0.05247611788f * f * q * q * q;
-        c[4] = 0.01610694871f * f * q * q * q * q;
+        const float inv = cap > 0.0f ? 1.0f / cap : 0.0f, q = inv * inv;
+        c[0] = 0.99999996002f * inv;
+        c[1] = -0.33332697360f * inv * q;
+        c[2] = 0.13316993368f * inv * q * q;
+        c[3] = -0.05247611788f * inv * q * q * q;
+        c[4] = 0.01610694871f * inv * q * q * q * q;
         edge = kNear * cap;
         // powers of a far cap that leave fp32's range, up or down, take the general form
         const float last = inv * q * q * q * q;
@@ -296,9 +296,9 @@ struct NearTanh {
 };
 
 // The form that an element's own magnitude asks for: what a row gets does not hang on its neighbours'.
-__device__ __forceinline__ float any_tanh(const NearTanh& near, float factor, float z, float inv, float& slope)
+__device__ __forceinline__ float any_tanh(const NearTanh& near, float z, float inv, float& slope)
 {
-    const float far = factor * tanh_of(z * inv, slope), y = near(z);
+    const float far = tanh_of(z * inv, slope), y = near(z);
     const bool is_near = fabsf(z) <= near.edge;
     slope = is_near ? fmaf(-y, y, 1.0f) : slope;
     return is_near ? y : far;
@@ -306,6 +306,7 @@ __device__ __forceinline__ float any_tanh(const NearTanh& near, float factor, fl
 
 // Up to this cap exp(l) and sums of them stay far inside fp32's range, whatever l is.
 constexpr float kPlainCap = 60.0f;
+__device__ __forceinline__ bool plain_cap(float cap) { return cap > 0.0f && cap <= kPlainCap; }
 
 // max over the four 16-lane rows: every lane receives that of its column position
 __device__ __forceinline__ float row_pair_max(float v)
@@ -339,7 +340,7 @@ struct LogitsArgs {
     float* best_z;            // largest product and the lowest v that has it, or null
     int32_t* best_v;
     int64_t tile0;            // the piece's first tile
-    float* at;                // [rows]: the target's logit
+    float* at;                // [rows]: the target's logit, of capped ones its tanh
     // gradient
     const float* lse;
     const float* dloss;
@@ -416,9 +417,9 @@ __global__ void __launch_bounds__(S::kThreads) logits_kernel(LogitsArgs a)
             }
         }
     }
-    const bool plain = a.cap > 0.0f && a.cap <= kPlainCap;      // then nothing has to be taken off the logits,
-    const float factor = plain ? a.cap * kLog2e : a.cap;        // which are held as powers of 2
-    const NearTanh near(a.cap, factor);
+    const bool plain = plain_cap(a.cap);        // then nothing has to be taken off the logits
+    const float to_power = a.cap * kLog2e;      // tanh to the power of 2
+    const NearTanh near(a.cap);
     const float inv = a.cap > 0.0f ? 1.0f / a.cap : 0.0f;
 #pragma unroll
     for (int j = 0; j < S::NT; ++j) {
@@ -439,7 +440,7 @@ __global__ void __launch_bounds__(S::kThreads) logits_kernel(LogitsArgs a)
 #pragma unroll
                 for (int i = 0; i < S::MT; ++i)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) acc[i][j][r] = any_tanh(near, factor, acc[i][j][r], inv, slope);
+                    for (int r = 0; r < 4; ++r) acc[i][j][r] = any_tanh(near, acc[i][j][r], inv, slope);
             }
         }
         if (a.at != nullptr) {
@@ -449,7 +450,7 @@ __global__ void __launch_bounds__(S::kThreads) logits_kernel(LogitsArgs a)
                 for (int i = 0; i < S::MT; ++i)
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
-                        if (16 * i + 4 * g + r == t && t < here) a.at[row] = acc[i][j][r] * (plain ? kLn2 : 1.0f);
+                        if (16 * i + 4 * g + r == t && t < here) a.at[row] = acc[i][j][r];
             }
         }
         if (here < S::MT * 16) {
@@ -464,8 +465,14 @@ __global__ void __launch_bounds__(S::kThreads) logits_kernel(LogitsArgs a)
 #pragma unroll
             for (int i = 0; i < S::MT; ++i)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) sum += __builtin_amdgcn_exp2f(acc[i][j][r]);
+                for (int r = 0; r < 4; ++r) sum += __builtin_amdgcn_exp2f(acc[i][j][r] * to_power);
         } else {
+            if (a.cap > 0.0f) {
+#pragma unroll
+                for (int i = 0; i < S::MT; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) acc[i][j][r] *= a.cap;
+            }
             top = -kInf;
 #pragma unroll
             for (int i = 0; i < S::MT; ++i)
@@ -522,6 +529,7 @@ struct JoinArgs {
     const int32_t* best_v;
     const float* at;
     Tokens targets;
+    float cap;
     int64_t rows, vocab, tiles;
     float* loss;
     float* lse;
@@ -578,12 +586,25 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(JoinArgs a)
         __syncthreads();
     }
     if (slice != 0 || row >= a.rows) return;
-    const float lse = top + kLn2 * __builtin_amdgcn_logf(sum);
-    a.lse[row] = lse;
+    float lse = top + kLn2 * __builtin_amdgcn_logf(sum), loss = 0.0f;
     if (a.loss != nullptr) {
         const int64_t t = token_at(a.targets, row);
-        a.loss[row] = t >= 0 && t < a.vocab ? lse - a.at[row] : 0.0f;
+        if (t >= 0 && t < a.vocab) {
+            // A small loss is the difference of two numbers that are not: it is formed from the sum in units of the
+            // target's own exponential (to which the sum's element of it is equal), to some 2^-22, and lse from it
+            // with one rounding.  The backward pass takes the same tanh, so its 1 - p is off by lse's rounding only.
+            const float cap = a.cap > 0.0f ? a.cap : 1.0f, l = cap * a.at[row];
+            const float away = plain_cap(a.cap) ? -a.at[row] * (cap * kLog2e) : (top - l) * kLog2e;
+            const float q = sum * __builtin_amdgcn_exp2f(away);
+            loss = lse - l;
+            if (q < 8.0f) {
+                loss = fmaxf(log1pf(q - 1.0f), 0.0f);
+                lse = fmaf(cap, a.at[row], loss);
+            }
+        }
+        a.loss[row] = loss;
     }
+    a.lse[row] = lse;
     if (a.best != nullptr) a.best[row] = v == INT32_MAX ? -1 : v;
 }
 
@@ -605,17 +626,17 @@ __global__ void __launch_bounds__(S::kThreads) logits_grad_kernel(LogitsArgs a)
     const int64_t c0 = m0 + wm * S::MT * 16;                // the wave's first column of dz
     const int here = int(min(a.piece - c0, int64_t(S::MT * 16)));
     if constexpr (S::Planes == 2) scale_back<S>(acc, a, c0, n0 + wn * S::NT * 16, g, n);
-    const float inv = a.cap > 0.0f ? 1.0f / a.cap : 0.0f, scale = (a.cap > 0.0f ? a.cap : 1.0f) * kLog2e;
-    const NearTanh near(a.cap, 1.0f);
+    const float inv = a.cap > 0.0f ? 1.0f / a.cap : 0.0f, cap = a.cap > 0.0f ? a.cap : 1.0f;
+    const NearTanh near(a.cap);
 #pragma unroll
     for (int j = 0; j < S::NT; ++j) {
         const int64_t row = n0 + (wn * S::NT + j) * 16 + n;
         int64_t t = -1;
         // a row that does not count has products of 0 (h is copied so) and takes exp(-far) times 0
-        float lse2 = 1e30f, up = 0.0f;
+        float lse = 1e30f, up = 0.0f;
         if (row < a.rows) {
             t = token_at(a.targets, row);
-            if (t >= 0 && t < a.vocab) lse2 = a.lse[row] * kLog2e, up = a.dloss[row];
+            if (t >= 0 && t < a.vocab) lse = a.lse[row], up = a.dloss[row];
         }
         const int64_t to = t - a.first - c0;
         const int mine = t < a.vocab && to >= 0 && to < here ? int(to) : -1;
@@ -633,7 +654,7 @@ __global__ void __launch_bounds__(S::kThreads) logits_grad_kernel(LogitsArgs a)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const float y = near(acc[i][j][r]);
-                    acc[i][j][r] = __builtin_amdgcn_exp2f(fmaf(y, scale, -lse2)) * (fmaf(-y, y, 1.0f) * up);
+                    acc[i][j][r] = __builtin_amdgcn_exp2f(fmaf(y, cap, -lse) * kLog2e) * (fmaf(-y, y, 1.0f) * up);
                 }
         } else {
 #pragma unroll
@@ -641,8 +662,8 @@ __global__ void __launch_bounds__(S::kThreads) logits_grad_kernel(LogitsArgs a)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     float slope = 1.0f, y = acc[i][j][r];
-                    if (a.cap > 0.0f) y = any_tanh(near, 1.0f, y, inv, slope);
-                    const float p = __builtin_amdgcn_exp2f(fmaf(y, scale, -lse2));
+                    if (a.cap > 0.0f) y = any_tanh(near, y, inv, slope);
+                    const float p = __builtin_amdgcn_exp2f(fmaf(y, cap, -lse) * kLog2e);
                     acc[i][j][r] = (16 * i + 4 * g + r == mine ? p - 1.0f : p) * (slope * up);
                 }
         }
@@ -1085,7 +1106,7 @@ hipError_t launch_cross_entropy(const CrossEntropyArgs& a, hipStream_t stream)
         });
         if (e != hipSuccess) return e;
     }
-    const JoinArgs j{k.part, k.best_z, k.best_v, k.at, a.targets, a.rows, a.vocab,
+    const JoinArgs j{k.part, k.best_z, k.best_v, k.at, a.targets, a.cap, a.rows, a.vocab,
                      ceil_div(a.vocab, shape_m(shape, planes)), a.targets.p == nullptr ? nullptr : a.loss, a.lse, a.best};
     // a workgroup for each of few rows; sixteen neighbours, whose sums lie side by side, of many (calls by 50257 of 64
     // channels: 256 rows 19.6 us against 23.6, 512 33.2 and 32.8, 1024 55.2 and 53.0, 2048 104 and 94)

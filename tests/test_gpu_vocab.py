@@ -305,6 +305,34 @@ def test_leading_dimensions():
     assert g["dh"].shape == (2, 3, 4, 64)
 
 
+@pytest.mark.parametrize("cap", [0.0, 30.0])
+def test_small_losses(cap):
+    """Rows that are sure of their target: the loss, and the target's 1 - p, are the small difference of two numbers near
+    12.  Rows of one 1 make the products exact, and each gradient one element of dz.  The sum over 50 rows of the table in
+    units of the target's exponential takes 8 additions a lane, 2 between lanes and 1 between waves, of 2^-24 each, two
+    exponentials of 2^-23 each: 16 2^-24 in all; the others' part, about the loss, is good to 2^-18 and moves with tanh's
+    2^-20 of two logits.  lse is rounded once, 2^-24 of itself, before the gradient takes it."""
+    rng = np.random.default_rng(12)
+    rows, vocab, width = 40, 50, 64
+    nt = rng.standard_normal((vocab, width)).astype(np.float32)
+    t = rng.integers(0, vocab, rows)
+    nt[t, np.arange(rows)] = 10.0 + 4.0 * rng.random(rows)
+    h, table = torch.eye(rows, width, device="cuda"), torch.from_numpy(nt).cuda()
+    targets, up = torch.from_numpy(t).cuda(), torch.ones(rows, device="cuda")
+    f = L.cross_entropy(h, table, targets, cap=cap)
+    g = L.cross_entropy_backward(h, table, targets, f["lse"], up, cap=cap)
+    nh = np.eye(rows, width)
+    want = E.cross_entropy(nh, nt, t, cap)
+    assert want["loss"].max() < 0.1 and want["loss"].min() > 1e-6
+    top = np.abs(want["lse"]).max()
+    bound = 16 * 2.0 ** -24 + want["loss"] * (2.0 ** -18 + 2.0 ** -19 * top)
+    _within(f["loss"], want["loss"], bound, "loss")
+    assert bool((f["loss"] > 0).all())
+    dz = E.cross_entropy_backward(nh, nt, t, np.ones(rows), cap)["dz"][np.arange(rows), t]
+    got = g["dtable"][targets, torch.arange(rows, device="cuda")]
+    _within(got, dz, bound + 2.0 ** -24 * top + 2.0 ** -22 + 2.0 ** -20 * np.abs(dz), "dz")
+
+
 def test_gradients_against_differences():
     """Central differences of the forward in fp32: a step of 2^-6 leaves the forward's own rounding (about 2e-6 of a loss
     of 5) at 2e-4 of a slope, and the third derivative at less than that."""
