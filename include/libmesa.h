@@ -577,7 +577,8 @@ int mesa_embedding_backward(const void* token, int token_bytes, const void* dy, 
  *   dh [rows, width], dtable [vocab, width]: dtype; either may be NULL.  Rows of h, lse and dloss
  *   whose target does not count may hold anything.  dz, formed a piece of the vocabulary at a time
  *   (the workspace holds at most 2^27 elements of it, or 256 columns), is rounded to bf16 for bf16 inputs; dh gets
- *   back what that takes off each target's element.  With rows 0 dtable is zeros.  Up to six kernel launches a piece. */
+ *   back what that takes off each target's element, dtable of up to 1024 rows what it takes off all.
+ *   With rows 0 dtable is zeros.  Up to six kernel launches a piece. */
 size_t mesa_cross_entropy_workspace_bytes(int64_t rows, int64_t vocab, int64_t width, int dtype);
 int mesa_cross_entropy(const void* h, const void* table, const void* target, int token_bytes, float cap, int64_t rows,
                        int64_t vocab, int64_t width, int64_t h_stride, int64_t table_stride, int dtype, float* loss,

@@ -73,6 +73,7 @@ struct PackArgs {
     int64_t vocab;
     uint16_t* out;           // [out_rows, ld]
     int64_t out_rows, ld;
+    int64_t again;           // from this row on the rows once more; 0: never
 };
 
 // The three parts of an fp32 value, whose sum it is: each the nearest bf16 to what the parts before
@@ -99,8 +100,7 @@ __device__ __forceinline__ void load8_unaligned(const float* p, float (&x)[8])
     for (int v = 0; v < 4; ++v) x[v] = lo[v], x[v + 4] = hi[v];
 }
 // bf16 rows as the products read them, eight consecutive channels a thread, out_rows x ld of them; what x
-// does not hold is zero.  One or two matrices a launch.
-// bf16 rows in rows of whole steps, zeros behind them: a copy (16384 x 2048 in 23 us, 5.8 TB/s; rows of 1000, whose
+// does not hold is zero.  One or two matrices a launch.  A copy (16384 x 2048 in 23 us, 5.8 TB/s; rows of 1000, whose
 // 16-byte pieces are unaligned, 32003 and 3997 of them, 146 MB, in 24).
 __global__ void __launch_bounds__(kPackThreads) pack_copy_kernel(PackArgs one, PackArgs two, unsigned blocks_one)
 {
@@ -111,7 +111,7 @@ __global__ void __launch_bounds__(kPackThreads) pack_copy_kernel(PackArgs one, P
     if (i >= a.out_rows * per) return;
     // fewer than 2^32 threads a launch
     const uint32_t at = uint32_t(i), row32 = at / uint32_t(per);
-    const int64_t row = row32, c = int64_t(at - row32 * uint32_t(per)) * 8;
+    const int64_t to = row32, row = a.again > 0 && to >= a.again ? to - a.again : to, c = int64_t(at - row32 * uint32_t(per)) * 8;
     bool counts = row < a.rows;
     if (counts && a.targets.p != nullptr) {
         const int64_t t = token_at(a.targets, row);
@@ -131,7 +131,7 @@ __global__ void __launch_bounds__(kPackThreads) pack_copy_kernel(PackArgs one, P
                 if (c + v < a.width) w[v / 2] |= uint32_t(src[v]) << (16 * (v % 2));
         }
     }
-    *reinterpret_cast<uint4*>(a.out + row * a.ld + c) = make_uint4(w[0], w[1], w[2], w[3]);
+    *reinterpret_cast<uint4*>(a.out + to * a.ld + c) = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 // Either may have no rows.
@@ -347,6 +347,7 @@ struct LogitsArgs {
     float* rest;              // [rows], of bf16: what rounding takes off the target's dz
     uint16_t* dz;             // planes of [row][piece], dz_ld elements a row
     int64_t dz_ld, dz_plane, dz_rows;
+    bool twice;               // of bf16: what its rounding takes off follows as rows dz_rows ...
 };
 
 // Products of scaled rows to those of the rows: column c0 + .. of the piece, row r0 + ... (of what lies past the
@@ -689,6 +690,13 @@ __global__ void __launch_bounds__(S::kThreads) logits_grad_kernel(LogitsArgs a)
 #pragma unroll
             for (int i = 0; i < S::MT; ++i)
                 *reinterpret_cast<uint2*>(dst + 16 * i) = make_uint2(pack_bf16(acc[i][j][0], acc[i][j][1]), pack_bf16(acc[i][j][2], acc[i][j][3]));
+            if (a.twice) {
+                auto left = [](float x) { return x - __uint_as_float(pack_bf16(x, 0.0f) << 16); };
+#pragma unroll
+                for (int i = 0; i < S::MT; ++i)
+                    *reinterpret_cast<uint2*>(dst + a.dz_rows * a.dz_ld + 16 * i) =
+                        make_uint2(pack_bf16(left(acc[i][j][0]), left(acc[i][j][1])), pack_bf16(left(acc[i][j][2]), left(acc[i][j][3])));
+            }
         } else {
 #pragma unroll
             for (int i = 0; i < S::MT; ++i) {
@@ -952,6 +960,11 @@ constexpr int64_t kCopyBytes = int64_t(256) << 20;
 // Elements of dz at a time.  16384 rows by 50257 of 2048 bf16 channels: backward 9.41 ms with half as many, 8.60 with
 // these, 8.58 with twice, 9.01 with four times; 4096 rows of 768 fp32 channels 4.88, 4.57, 4.53, 4.47.
 constexpr int64_t kPieceElements = int64_t(1) << 27;
+// Up to so many bf16 rows dz has its rounding's rest behind it as rows of their own, and h once more, for the table's
+// gradient: in sums of few rows such roundings do not even out.  Its error, in parts of its norm, is then its own
+// rounding's, 0.0017, for 0.0027 at 3 rows by 20000 of 768 to 1024 channels, 0.0025 at 100, 0.0024 at 1000 (0.0022 at
+// 2048, where it is left); the backward call takes 40 us for 36.5 at 256 rows by 5003 of 768, 368 for 308 by 50257 of 2048.
+constexpr int64_t kTwiceRows = 1024;
 constexpr int64_t kSlabBytes = int64_t(256) << 20;     // of fp32 layers of one product, at most (or one layer)
 
 // Rows of the table in a piece of the forward, where it has to be copied.
@@ -999,7 +1012,7 @@ struct ForwardPlan {
 
 struct GradPlan {
     // h and the table as the gradients' products read them, and (fp32) as the logits' does, with the exponents
-    int64_t piece, dz, dz_rows, dz_ld, h, table, h16, table16, h_e, table_e, rest, slab_h, slab_e, bytes, ld;
+    int64_t piece, dz, dz_rows, deep, dz_ld, h, table, h16, table16, h_e, table_e, rest, slab_h, slab_e, bytes, ld;
     Shape logits;
     Cut dh, de, de_last;
     GradPlan(int64_t rows, int64_t vocab, int64_t width, int dtype)
@@ -1007,7 +1020,8 @@ struct GradPlan {
         const int planes = grad_planes(dtype);
         ld = ceil_to(width, kStepK);
         dz_rows = ceil_to(rows, 64);
-        piece = std::max<int64_t>(256, kPieceElements / dz_rows / 256 * 256);
+        deep = planes == 1 && rows <= kTwiceRows ? 2 * dz_rows : dz_rows;
+        piece = std::max<int64_t>(256, kPieceElements / deep / 256 * 256);
         // pieces whose part of the table's gradient is whole rounds of wide tiles on all compute units, where they are
         // large enough for that; else pieces of about the same size
         const int64_t round = std::max<int64_t>(1, kUnits / ceil_div(width, shape_m(kWide, planes))) * shape_n(kWide, planes);
@@ -1020,17 +1034,17 @@ struct GradPlan {
         dh = layers(width, rows, std::min(piece, vocab), planes);
         // the last piece may be much shorter, and is then cut otherwise
         const int64_t ending = vocab - (ceil_div(vocab, piece) - 1) * piece;
-        de = layers(width, std::min(piece, vocab), rows, planes);
-        de_last = layers(width, ending, rows, planes);
+        de = layers(width, std::min(piece, vocab), deep, planes);
+        de_last = layers(width, ending, deep, planes);
         Carve c;
-        h = c.take(dz_rows * ld * 2 * planes);
+        h = c.take(deep * ld * 2 * planes);
         table = c.take(piece * ld * 2 * planes);
         h16 = planes == 1 ? h : c.take(dz_rows * ld * 4);
         table16 = planes == 1 ? table : c.take(piece * ld * 4);
         h_e = planes == 1 ? 0 : c.take(exponents_of(dz_rows) * 4);
         table_e = planes == 1 ? 0 : c.take(exponents_of(piece) * 4);
         rest = planes == 1 ? c.take(rows * 4) : 0;
-        dz = c.take(dz_rows * dz_ld * 2 * planes);
+        dz = c.take(deep * dz_ld * 2 * planes);
         slab_h = dh.layers > 1 || piece < vocab ? c.take(dh.layers * rows * ld * 4) : 0;
         const int64_t layered = std::max(de.layers > 1 ? de.layers * piece : 0, de_last.layers > 1 ? de_last.layers * ending : 0);
         slab_e = layered > 0 ? c.take(layered * ld * 4) : 0;
@@ -1161,8 +1175,9 @@ hipError_t launch_cross_entropy_grad(const CrossEntropyGradArgs& a, hipStream_t 
     uint16_t* dz = words(plan.dz);
     float* rest = planes == 1 ? reinterpret_cast<float*>(ws + plan.rest) : nullptr;
     const bool as_is = direct(a.table, a.table_stride, a.width, a.dtype);
-    const int64_t dz_plane = plan.dz_rows * plan.dz_ld;
-    const Matrix h{words(plan.h), ld, plan.dz_rows * ld, plan.dz_rows, ld};
+    const int64_t dz_plane = plan.deep * plan.dz_ld;
+    const Matrix h{words(plan.h), ld, plan.deep * ld, plan.deep, ld};
+    const bool twice = plan.deep > plan.dz_rows;
 
     for (int64_t first = 0; first < a.vocab; first += plan.piece) {
         const int64_t piece = std::min(plan.piece, a.vocab - first);
@@ -1175,7 +1190,7 @@ hipError_t launch_cross_entropy_grad(const CrossEntropyGradArgs& a, hipStream_t 
         LogitsArgs k{};
         if (planes == 1) {
             e = pack_copy(first > 0 ? PackArgs{} : PackArgs{static_cast<const uint16_t*>(a.h), a.rows, a.width, a.h_stride, a.targets, a.vocab,
-                                                            words(plan.h), plan.dz_rows, ld},
+                                                            words(plan.h), plan.deep, ld, twice ? plan.dz_rows : 0},
                           as_is ? PackArgs{} : PackArgs{reinterpret_cast<const uint16_t*>(src), piece, a.width, a.table_stride, {}, 0, words(plan.table), piece, ld},
                           stream);
             k.table = table;
@@ -1207,6 +1222,7 @@ hipError_t launch_cross_entropy_grad(const CrossEntropyGradArgs& a, hipStream_t 
         k.dz_ld = plan.dz_ld;
         k.dz_plane = dz_plane;
         k.dz_rows = plan.dz_rows;
+        k.twice = twice;
         k.tiles_m = ceil_div(piece, shape_m(plan.logits, logit_planes(a.dtype)));
         k.tiles_n = ceil_div(plan.dz_rows, shape_n(plan.logits, logit_planes(a.dtype)));
         e = with_logits_shape(plan.logits, logit_planes(a.dtype), [&](auto s) {
@@ -1216,7 +1232,7 @@ hipError_t launch_cross_entropy_grad(const CrossEntropyGradArgs& a, hipStream_t 
             return hipGetLastError();
         });
         if (e != hipSuccess) return e;
-        const Matrix dz_rows{dz, plan.dz_ld, dz_plane, plan.dz_rows, plan.dz_ld};
+        const Matrix dz_rows{dz, plan.dz_ld, dz_plane, plan.deep, plan.dz_ld};
         if (a.dh != nullptr) {
             const bool slab = plan.dh.layers > 1 || plan.piece < a.vocab;
             GradArgs d{};
@@ -1248,8 +1264,8 @@ hipError_t launch_cross_entropy_grad(const CrossEntropyGradArgs& a, hipStream_t 
             GradArgs d{};
             d.a = h;
             d.b = dz_rows;
-            d.k = plan.dz_rows;
-            d.k_split = ceil_to(ceil_div(plan.dz_rows, cut.layers), kStepK);
+            d.k = plan.deep;
+            d.k_split = ceil_to(ceil_div(plan.deep, cut.layers), kStepK);
             const int64_t layers = ceil_div(d.k, d.k_split);
             d.tiles_m = ceil_div(a.width, shape_m(shape, planes));
             d.tiles_n = ceil_div(piece, shape_n(shape, planes));

@@ -200,7 +200,8 @@ def test_cross_entropy_of_spaced_and_unaligned_rows(pad, shift, dtype):
     (2048, 2000, 1900, BF16),      # and the gradients', ragged
     (16384, 8500, 24, BF16),       # two pieces of the vocabulary
     (6000, 8200, 16, F32),         # the same with three planes
-    (3000, 200, 40, F32), (40, 9000, 40, BF16), (700, 90, 30, BF16)])   # few tiles: the sums are cut into layers
+    (3000, 200, 40, F32), (40, 9000, 40, BF16), (700, 90, 30, BF16),    # few tiles: the sums are cut into layers
+    (1024, 301, 72, BF16), (1025, 301, 72, BF16)])      # the most rows whose dz has its rounding's rest behind it, and one more
 def test_cross_entropy_of_larger_sizes(rows, vocab, width, dtype):
     _check_all(*_problem(rows, vocab, width, dtype, seed=rows), 30.0)
 
