@@ -568,8 +568,9 @@ int mesa_embedding_backward(const void* token, int token_bytes, const void* dy, 
  *   target, loss [rows] fp32: both or neither (then only lse and best are computed)
  *   lse [rows] fp32;  best int32 [rows], or NULL
  *   cap        0, or finite, positive and no subnormal number
- * rows 0 is a no-op; vocab and width must be positive.  Two kernel launches, and one or two more for
- * each 256 MiB of a table that has to be copied (fp32, or spaced or aligned otherwise).
+ * rows 0 is a no-op; vocab and width must be positive.  Two or three kernel launches, and up to two more
+ * for each 256 MiB of a table that has to be copied (fp32 for more than 32 rows, or bf16 rows that are
+ * spaced or aligned otherwise).
  *
  * mesa_cross_entropy_backward: gradients for a given dloss [rows] fp32 and the lse of the forward
  *     dz_nv = dloss_n (exp(l_nv - lse_n) - [v = target_n]) (1 - (l_nv / cap)^2), 0 where the target does not count

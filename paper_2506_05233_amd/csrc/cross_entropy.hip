@@ -14,7 +14,7 @@
 // 3.09, dh 2.83, the table's gradient 2.61; over 777 rows by 5003 of 768 fp32 ones 188 us.  One row by 50257 of 2048
 // takes 53 us, which reads its 206 MB at 4.4 TB/s, 256 rows 78.
 //
-// fp32 is multiplied as parts of 16 bits: the logits from two fp16 parts of rows scaled by a power of two (three
+// fp32 is multiplied as parts of 16 bits: the logits of more than 32 rows from two fp16 parts of rows scaled by a power of two (three
 // products; the first version took three bf16 parts, six products: 80 us and 38 for 777 rows by 5003 of 768), the
 // gradients from three bf16 parts, since a scale of its own for each row stands in the way of sums over rows.
 #include <algorithm>
@@ -49,7 +49,7 @@ struct Shapes<2> {
     using Wide = TileShape<2, 128, 256, 2, 4>;
     using Middle = TileShape<2, 128, 128, 2, 2>;
     using Narrow = TileShape<2, 64, 64, 2, 2>;
-    using Thin = Narrow;
+    using Thin = TileShape<2, 64, 32, 4, 1>;      // by Stream
 };
 template <>
 struct Shapes<3> {
@@ -154,7 +154,7 @@ struct RowArgs {
     int64_t rows, width, stride;
     Tokens targets;          // as in PackArgs
     int64_t vocab;
-    uint16_t* halves;        // two planes of [out_rows, ld]
+    uint16_t* halves;        // two planes of [out_rows, ld], or null
     int32_t* exponent;       // [exponents]: e, and zeros, which whole tiles read
     int64_t exponents;
     uint16_t* parts;         // three planes, or null
@@ -236,8 +236,9 @@ __global__ void __launch_bounds__(kPackThreads) pack_rows_kernel(RowArgs one, Ro
             }
         }
         const int64_t to = row * a.ld + c;
+        if (a.halves != nullptr)
 #pragma unroll
-        for (int k = 0; k < 2; ++k) *reinterpret_cast<uint4*>(a.halves + k * plane + to) = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
+            for (int k = 0; k < 2; ++k) *reinterpret_cast<uint4*>(a.halves + k * plane + to) = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
         if (a.parts != nullptr) {
 #pragma unroll
             for (int k = 0; k < 3; ++k) *reinterpret_cast<uint4*>(a.parts + k * plane + to) = make_uint4(w[2 + k][0], w[2 + k][1], w[2 + k][2], w[2 + k][3]);
@@ -326,6 +327,8 @@ __device__ __forceinline__ int row_pair_min(int v)
 
 struct LogitsArgs {
     Matrix table, h;          // from the piece's first row of the table on
+    const float* whole;       // of Stream: the table's rows in fp32, and h is three bf16 planes
+    int64_t whole_stride;
     const int32_t* table_e;   // fp16 planes: the exponents that their rows were scaled by (readable up to whole tiles)
     const int32_t* h_e;
     int64_t width;
@@ -368,6 +371,131 @@ __device__ __forceinline__ void scale_back(f32x4 (&acc)[S::MT][S::NT], const Log
     }
 }
 
+// The fp32 product of the thin tile: few rows of h against a table that is read once, as it lies, which bounds it.  A wave
+// holds 16 rows of the table; a lane (g, n) loads the pieces of 8 channels of row n that it multiplies itself, 128
+// channels ahead, and parts them into three bf16 in registers (six products).  h's parts come through LDS, 128
+// channels at a time; they are asked for before the table's, so that waiting for them leaves those under way, and so
+// does the barrier, which waits for LDS only.  One row by 50257 of 2048 channels takes 119 us (412 MB, 3.5 TB/s), where
+// a copy of the table in fp16 parts ahead of the tiled product took 318: three times the bytes.  (Few bf16 rows keep
+// the tiled product: loads to registers like these took 53.4 us there for 52.6.)
+struct Stream {
+    static constexpr int K = 128, kRows = 32, kPieces = K / 8, kSteps = K / 32, kEach = kRows * kPieces / 256;
+    static constexpr int kBuffer = 3 * kRows * K;
+    typedef float floats_any __attribute__((ext_vector_type(4), aligned(4)));
+    struct Piece {
+        floats_any lo, hi;
+    };
+    __device__ static __forceinline__ void barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+    // h: three planes, zeros past the width up to a multiple of 64
+    __device__ static __forceinline__ void run(const float* table, int64_t stride, int64_t rows, int64_t width, const Matrix& h, int64_t m0,
+                                               uint16_t* even, uint16_t* odd, f32x4 (&acc)[1][2])
+    {
+        const int t = int(threadIdx.x), lane = t % kWave, g = lane / 16, n = lane % 16;
+        const float* row = table + min(m0 + t / kWave * 16 + n, rows - 1) * stride + 8 * g;      // rows past the end read the last
+        const int column = t % kPieces * 8;
+        const uint16_t* from[kEach];
+        int to[kEach];
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            const int r = (j * 256 + t) / kPieces;
+            from[j] = h.p + min(int64_t(r), h.rows - 1) * h.ld + column;
+            to[j] = r * K + 8 * ((t % kPieces) ^ (r & 15));      // sixteen rows' pieces stand in different banks
+        }
+        // past the end the last piece, in whose place zeros are put
+        auto load_h = [&](int64_t k, uint4 (&x)[3][kEach]) {
+            const int64_t at = min(k, h.cols - 8 - column);
+#pragma unroll
+            for (int p = 0; p < 3; ++p)
+#pragma unroll
+                for (int j = 0; j < kEach; ++j) x[p][j] = *reinterpret_cast<const uint4*>(from[j] + p * h.plane + at);
+        };
+        auto put = [&](int64_t k, const uint4 (&x)[3][kEach], uint16_t* lds) {
+            const bool there = k + column < h.cols;
+#pragma unroll
+            for (int p = 0; p < 3; ++p)
+#pragma unroll
+                for (int j = 0; j < kEach; ++j)
+                    *reinterpret_cast<uint4*>(lds + p * kRows * K + to[j]) =
+                        make_uint4(there ? x[p][j].x : 0, there ? x[p][j].y : 0, there ? x[p][j].z : 0, there ? x[p][j].w : 0);
+        };
+        auto load_table = [&](int64_t k, Piece (&x)[kSteps]) {
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s) x[s] = *reinterpret_cast<const Piece*>(row + k + 32 * s);
+        };
+        f32x4 low[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+        auto multiply = [&](const Piece (&x)[kSteps], const uint16_t* lds) {
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s) {
+                uint32_t w[3][4];
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    uint32_t p[3], q[3];
+                    three_parts(v < 2 ? x[s].lo[2 * v] : x[s].hi[2 * v - 4], p);
+                    three_parts(v < 2 ? x[s].lo[2 * v + 1] : x[s].hi[2 * v - 3], q);
+#pragma unroll
+                    for (int k = 0; k < 3; ++k) w[k][v] = p[k] | q[k] << 16;
+                }
+                bf16x8 a[3];
+#pragma unroll
+                for (int k = 0; k < 3; ++k) a[k] = __builtin_bit_cast(bf16x8, make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]));
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const uint16_t* src = lds + (16 * j + n) * K + 8 * ((4 * s + g) ^ n);
+                    bf16x8 b[3];
+#pragma unroll
+                    for (int k = 0; k < 3; ++k) b[k] = *reinterpret_cast<const bf16x8*>(src + k * kRows * K);
+                    // the small products apart: what is added to the large sum is rounded at its size each time
+                    f32x4& c = low[j];
+                    c = mfma16(a[0], b[2], c);
+                    c = mfma16(a[2], b[0], c);
+                    c = mfma16(a[1], b[1], c);
+                    c = mfma16(a[0], b[1], c);
+                    c = mfma16(a[1], b[0], c);
+                    acc[0][j] = mfma16(a[0], b[0], acc[0][j]);
+                }
+            }
+        };
+        acc[0][0] = acc[0][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+        const int64_t whole = width / K * K;
+        uint4 parts[3][kEach];
+        Piece one[kSteps], two[kSteps];
+        uint16_t *now = even, *then = odd;
+        load_h(0, parts);
+        if (whole > 0) load_table(0, one);
+        put(0, parts, now);
+        barrier();
+        for (int64_t k = 0; k < whole; k += K) {
+            // past the last whole step: h's rest, and the first step again, which nobody uses
+            load_h(k + K, parts);
+            load_table(k + K < whole ? k + K : 0, two);
+            multiply(one, now);
+            put(k + K, parts, then);
+            barrier();
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s) one[s] = two[s];
+            uint16_t* x = now;
+            now = then, then = x;
+        }
+        if (whole < width) {
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+                for (int v = 0; v < 8; ++v) {
+                    const int64_t c = whole + 32 * s + v;
+                    const float y = c + 8 * g < width ? row[c] : 0.0f;
+                    if (v < 4)
+                        one[s].lo[v] = y;
+                    else
+                        one[s].hi[v - 4] = y;
+                }
+            multiply(one, now);
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) acc[0][j] += low[j];
+        barrier();
+    }
+};
+
 // One tile of the vocabulary against one of the rows; of every row the tile's largest logit and its
 // sum of exponentials to that, which the next kernel joins over the tiles.  A cap of up to 60 bounds the logits, and
 // exp(l) is summed as it is.  The products are 48 of a wide tile's 57 us at 2048 channels; the other 9, its first loads
@@ -376,11 +504,16 @@ __device__ __forceinline__ void scale_back(f32x4 (&acc)[S::MT][S::NT], const Log
 template <class S>
 __global__ void __launch_bounds__(S::kThreads) logits_kernel(LogitsArgs a)
 {
-    __shared__ __attribute__((aligned(16))) uint16_t even[S::kBuffer], odd[S::kBuffer];
+    constexpr bool kStream = std::is_same_v<S, Shapes<2>::Thin>;
+    constexpr int kBuffer = kStream ? Stream::kBuffer : S::kBuffer;
+    __shared__ __attribute__((aligned(16))) uint16_t even[kBuffer], odd[kBuffer];
     int tm, tn;
     tile_of(int(a.tiles_m), int(a.tiles_n), tm, tn);
     f32x4 acc[S::MT][S::NT];
-    Product<S, true, true>::run(a.table, a.h, tm, tn, 0, a.width, even, odd, acc);
+    if constexpr (kStream)
+        Stream::run(a.whole, a.whole_stride, a.piece, a.width, a.h, int64_t(tm) * S::M, even, odd, acc);
+    else
+        Product<S, true, true>::run(a.table, a.h, tm, tn, 0, a.width, even, odd, acc);
 
     float* red = reinterpret_cast<float*>(even);
     const int64_t m0 = int64_t(tm) * S::M, n0 = int64_t(tn) * S::N;
@@ -388,7 +521,7 @@ __global__ void __launch_bounds__(S::kThreads) logits_kernel(LogitsArgs a)
     const int wave = int(threadIdx.x) / kWave, wm = wave / S::WN, wn = wave % S::WN;
     const int64_t v0 = a.first + m0 + wm * S::MT * 16;      // the wave's first row of the table
     const int here = int(min(a.first + a.piece - v0, int64_t(S::MT * 16)));     // its rows that exist (0 or less: none)
-    if constexpr (S::Planes == 2) scale_back<S>(acc, a, m0 + wm * S::MT * 16, n0 + wn * S::NT * 16, g, n);
+    if constexpr (S::Planes == 2 && !kStream) scale_back<S>(acc, a, m0 + wm * S::MT * 16, n0 + wn * S::NT * 16, g, n);
     float* red_m = red;           // [WM][N]
     float* red_s = red_m + S::WM * S::N;
     float* red_z = red_s + S::WM * S::N;
@@ -615,18 +748,23 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(JoinArgs a)
 template <class S>
 __global__ void __launch_bounds__(S::kThreads) logits_grad_kernel(LogitsArgs a)
 {
-    __shared__ __attribute__((aligned(16))) uint16_t even[S::kBuffer], odd[S::kBuffer];
+    constexpr bool kStream = std::is_same_v<S, Shapes<2>::Thin>;
+    constexpr int kBuffer = kStream ? Stream::kBuffer : S::kBuffer;
+    __shared__ __attribute__((aligned(16))) uint16_t even[kBuffer], odd[kBuffer];
     int tm, tn;
     tile_of(int(a.tiles_m), int(a.tiles_n), tm, tn);
     f32x4 acc[S::MT][S::NT];
-    Product<S, true, true>::run(a.table, a.h, tm, tn, 0, a.width, even, odd, acc);
+    if constexpr (kStream)
+        Stream::run(a.whole, a.whole_stride, a.piece, a.width, a.h, int64_t(tm) * S::M, even, odd, acc);
+    else
+        Product<S, true, true>::run(a.table, a.h, tm, tn, 0, a.width, even, odd, acc);
 
     const int64_t m0 = int64_t(tm) * S::M, n0 = int64_t(tn) * S::N;
     const int lane = int(threadIdx.x) % kWave, g = lane / 16, n = lane % 16;
     const int wave = int(threadIdx.x) / kWave, wm = wave / S::WN, wn = wave % S::WN;
     const int64_t c0 = m0 + wm * S::MT * 16;                // the wave's first column of dz
     const int here = int(min(a.piece - c0, int64_t(S::MT * 16)));
-    if constexpr (S::Planes == 2) scale_back<S>(acc, a, c0, n0 + wn * S::NT * 16, g, n);
+    if constexpr (S::Planes == 2 && !kStream) scale_back<S>(acc, a, c0, n0 + wn * S::NT * 16, g, n);
     const float inv = a.cap > 0.0f ? 1.0f / a.cap : 0.0f, cap = a.cap > 0.0f ? a.cap : 1.0f;
     const NearTanh near(a.cap);
 #pragma unroll
@@ -704,8 +842,11 @@ __global__ void __launch_bounds__(S::kThreads) logits_grad_kernel(LogitsArgs a)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) three_parts(acc[i][j][r], p[r]);
 #pragma unroll
-                for (int k = 0; k < 3; ++k)
+                for (int k = 0; k < 3; ++k) {
                     *reinterpret_cast<uint2*>(dst + k * a.dz_plane + 16 * i) = make_uint2(p[0][k] | p[1][k] << 16, p[2][k] | p[3][k] << 16);
+                    // the other rows of the step of 64 that the table's gradient takes
+                    if constexpr (kStream) *reinterpret_cast<uint2*>(dst + k * a.dz_plane + 32 * a.dz_ld + 16 * i) = make_uint2(0, 0);
+                }
             }
         }
     }
@@ -907,12 +1048,15 @@ struct Cut {
     Shape shape;
     int64_t layers;
 };
+// Whether a product of fp32 logits, of n rows, is Stream's.
+bool streams(int64_t n, int planes) { return planes == 2 && n <= Stream::kRows; }
 Cut cut_of(int64_t m, int64_t n, int64_t k, int planes, int64_t most)
 {
     Cut best{kThin, 1};
     float least = 0.0f;
     for (Shape s : {kWide, kMiddle, kNarrow, kThin}) {
         if (s == kThin && n > 32) continue;      // it reads the table's rows once for 32 of the others
+        if (s != kThin && streams(n, planes)) continue;
         const int64_t tiles = ceil_div(m, shape_m(s, planes)) * ceil_div(n, shape_n(s, planes));
         for (int64_t l = 1; l <= most; l += l < 4 ? 1 : l / 2) {
             const float sum = l > 1 ? 5.0f + float(l) * float(m) * float(n) * 1e-6f : 0.0f;
@@ -988,12 +1132,12 @@ struct Carve {      // the workspace, piece after piece of 256 bytes
 int64_t exponents_of(int64_t n) { return ceil_to(n, 256) + 256; }
 
 struct ForwardPlan {
-    int64_t part, best_z, best_v, at, h, table, h_e, table_e, bytes;
+    int64_t part, best_z, best_v, at, h, h_parts, table, h_e, table_e, bytes;
     ForwardPlan(int64_t rows, int64_t vocab, int64_t width, int dtype)
     {
         // whether the table is copied hangs on its address, so there is room for either way's tiles
-        const int64_t copied = copy_rows(vocab, width, dtype);
         const int planes = logit_planes(dtype);
+        const int64_t copied = streams(rows, planes) ? 0 : copy_rows(vocab, width, dtype);
         auto tiles_of = [&](int64_t m) { return ceil_div(vocab, shape_m(shape_of(m, rows, width, planes), planes)); };
         const int64_t tiles = std::max(tiles_of(vocab), tiles_of(copied));
         Carve c;
@@ -1003,6 +1147,7 @@ struct ForwardPlan {
         best_v = c.take(tiles * rows * 4);
         at = c.take(rows * 4);
         h = c.take(rows * row);
+        h_parts = streams(rows, planes) ? c.take(rows * ceil_to(width, kStepK) * 6) : 0;
         table = c.take(copied * row);
         h_e = planes == 1 ? 0 : c.take(exponents_of(rows) * 4);
         table_e = planes == 1 ? 0 : c.take(exponents_of(copied) * 4);
@@ -1089,7 +1234,10 @@ hipError_t launch_cross_entropy(const CrossEntropyArgs& a, hipStream_t stream)
     // h is copied, if at all, along with the table's first piece
     const bool h_as_is = direct(a.h, a.h_stride, a.width, a.dtype), as_is = direct(a.table, a.table_stride, a.width, a.dtype);
     k.h = h_as_is ? Matrix{static_cast<const uint16_t*>(a.h), a.h_stride, 0, a.rows, a.width} : Matrix{h, ld, a.rows * ld, a.rows, ld};
-    int64_t most = as_is ? a.vocab : copy_rows(a.vocab, a.width, a.dtype);
+    const bool stream_table = streams(a.rows, planes);
+    uint16_t* parts = stream_table ? reinterpret_cast<uint16_t*>(ws + plan.h_parts) : nullptr;
+    if (stream_table) k.h = Matrix{parts, ld, a.rows * ld, a.rows, ld};
+    int64_t most = as_is || stream_table ? a.vocab : copy_rows(a.vocab, a.width, a.dtype);
     const Shape shape = shape_of(most, a.rows, a.width, planes);
     k.tiles_n = ceil_div(a.rows, shape_n(shape, planes));
     most = std::min(most, kMostTiles / k.tiles_n * shape_m(shape, planes));
@@ -1100,14 +1248,16 @@ hipError_t launch_cross_entropy(const CrossEntropyArgs& a, hipStream_t stream)
         k.tiles_m = ceil_div(k.piece, shape_m(shape, planes));
         const uint16_t* src = static_cast<const uint16_t*>(a.table) + first * a.table_stride * planes;      // of fp32, two planes, twice the bytes
         k.table = as_is ? Matrix{src, a.table_stride, 0, k.piece, a.width} : Matrix{copy, ld, k.piece * ld, k.piece, ld};
+        k.whole = reinterpret_cast<const float*>(src);
+        k.whole_stride = a.table_stride;
         hipError_t e;
         if (planes == 1) {
             e = pack_copy(first > 0 || h_as_is ? PackArgs{} : PackArgs{static_cast<const uint16_t*>(a.h), a.rows, a.width, a.h_stride, {}, 0, h, a.rows, ld},
                           as_is ? PackArgs{} : PackArgs{src, k.piece, a.width, a.table_stride, {}, 0, copy, k.piece, ld}, stream);
         } else {
             e = pack_rows(first > 0 ? RowArgs{} : RowArgs{static_cast<const float*>(a.h), a.rows, a.width, a.h_stride, {}, 0, h,
-                                                           reinterpret_cast<int32_t*>(ws + plan.h_e), exponents_of(a.rows), nullptr, a.rows, ld},
-                          RowArgs{reinterpret_cast<const float*>(src), k.piece, a.width, a.table_stride, {}, 0, copy, reinterpret_cast<int32_t*>(ws + plan.table_e), exponents_of(k.piece),
+                                                           reinterpret_cast<int32_t*>(ws + plan.h_e), exponents_of(a.rows), parts, a.rows, ld},
+                          stream_table ? RowArgs{} : RowArgs{reinterpret_cast<const float*>(src), k.piece, a.width, a.table_stride, {}, 0, copy, reinterpret_cast<int32_t*>(ws + plan.table_e), exponents_of(k.piece),
                                   nullptr, k.piece, ld},
                           stream);
         }
@@ -1196,14 +1346,17 @@ hipError_t launch_cross_entropy_grad(const CrossEntropyGradArgs& a, hipStream_t 
             k.table = table;
             k.h = h;
         } else {
+            const bool streamed = streams(a.rows, logit_planes(a.dtype));
             int32_t *h_e = reinterpret_cast<int32_t*>(ws + plan.h_e), *table_e = reinterpret_cast<int32_t*>(ws + plan.table_e);
             e = pack_rows(first > 0 ? RowArgs{} : RowArgs{static_cast<const float*>(a.h), a.rows, a.width, a.h_stride, a.targets, a.vocab,
                                                            words(plan.h16), h_e, exponents_of(plan.dz_rows), words(plan.h), plan.dz_rows, ld},
-                          RowArgs{reinterpret_cast<const float*>(src), piece, a.width, a.table_stride, {}, 0, words(plan.table16), table_e,
+                          RowArgs{reinterpret_cast<const float*>(src), piece, a.width, a.table_stride, {}, 0, streamed ? nullptr : words(plan.table16), table_e,
                                   exponents_of(piece), words(plan.table), piece, ld},
                           stream);
             k.table = Matrix{words(plan.table16), ld, piece * ld, piece, ld};
-            k.h = Matrix{words(plan.h16), ld, plan.dz_rows * ld, plan.dz_rows, ld};
+            k.h = streamed ? h : Matrix{words(plan.h16), ld, plan.dz_rows * ld, plan.dz_rows, ld};
+            k.whole = reinterpret_cast<const float*>(src);
+            k.whole_stride = a.table_stride;
             k.h_e = h_e;
             k.table_e = table_e;
         }
@@ -1224,7 +1377,7 @@ hipError_t launch_cross_entropy_grad(const CrossEntropyGradArgs& a, hipStream_t 
         k.dz_rows = plan.dz_rows;
         k.twice = twice;
         k.tiles_m = ceil_div(piece, shape_m(plan.logits, logit_planes(a.dtype)));
-        k.tiles_n = ceil_div(plan.dz_rows, shape_n(plan.logits, logit_planes(a.dtype)));
+        k.tiles_n = streams(a.rows, logit_planes(a.dtype)) ? 1 : ceil_div(plan.dz_rows, shape_n(plan.logits, logit_planes(a.dtype)));
         e = with_logits_shape(plan.logits, logit_planes(a.dtype), [&](auto s) {
             using S = decltype(s);
             if (!grid_fits(k.tiles_m * k.tiles_n, S::kThreads)) return hipErrorInvalidConfiguration;

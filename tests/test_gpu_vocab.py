@@ -175,7 +175,7 @@ def _check_all(h, table, t, targets, up, cap):
     return f, g
 
 
-SIZES = [(1, 1, 1), (1, 5003, 64), (2, 50, 2048), (5, 64, 8), (16, 63, 65), (31, 65, 100), (33, 129, 64), (64, 300, 200), (65, 257, 321),
+SIZES = [(1, 1, 1), (1, 5003, 64), (32, 300, 128), (3, 200, 129), (20, 130, 383), (2, 50, 2048), (5, 64, 8), (16, 63, 65), (31, 65, 100), (33, 129, 64), (64, 300, 200), (65, 257, 321),
          (100, 5003, 321), (130, 1000, 128), (300, 777, 72), (513, 513, 64)]
 
 

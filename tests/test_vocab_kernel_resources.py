@@ -27,7 +27,9 @@ def reports():
 LIMITS = [
     (r"logits(_grad)?_kernel<TileShape<1, 256, 256, 2, 4>", 256),
     (r"(logits|logits_grad|grad)_kernel<TileShape<1, 128, 128, 2, 2>", 256),
-    (r"(logits|logits_grad|grad)_kernel<TileShape<(1|2|3), 64, (32|64), ", 128),
+    (r"(logits|logits_grad|grad)_kernel<TileShape<(1|2|3), 64, 64, ", 128),
+    (r"(logits|logits_grad|grad)_kernel<TileShape<1, 64, 32, ", 128),
+    (r"(logits|logits_grad)_kernel<TileShape<2, 64, 32, ", 168),
     (r"grad_kernel<TileShape<1, 256, 256, 2, 4>", 256),
     (r"(logits|logits_grad)_kernel<TileShape<2, ", 256),
     (r"grad_kernel<TileShape<3, ", 256),
