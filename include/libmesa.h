@@ -577,9 +577,10 @@ int mesa_embedding_backward(const void* token, int token_bytes, const void* dy, 
  *     dh_n = sum_v dz_nv E_v,  dE_v = sum_n dz_nv h_n
  *   dh [rows, width], dtable [vocab, width]: dtype; either may be NULL.  Rows of h, lse and dloss
  *   whose target does not count may hold anything.  dz, formed a piece of the vocabulary at a time
- *   (the workspace holds at most 2^27 elements of it, or 256 columns), is rounded to bf16 for bf16 inputs; dh gets
- *   back what that takes off each target's element, dtable of up to 1024 rows what it takes off all.
- *   With rows 0 dtable is zeros.  Up to six kernel launches a piece. */
+ *   (the workspace holds at most 2^27 elements of it, or 256 columns), is rounded to bf16 for bf16 inputs (2^-8 of an
+ *   element).  dh and dtable get back what that takes off each target's element, which is as large as the others of its row
+ *   together; dtable of up to 1024 rows, or rows vocab width up to 4.3e9, what it takes off all.
+ *   With rows 0 dtable is zeros.  Up to nine kernel launches a piece, and up to eight before the first. */
 size_t mesa_cross_entropy_workspace_bytes(int64_t rows, int64_t vocab, int64_t width, int dtype);
 int mesa_cross_entropy(const void* h, const void* table, const void* target, int token_bytes, float cap, int64_t rows,
                        int64_t vocab, int64_t width, int64_t h_stride, int64_t table_stride, int dtype, float* loss,

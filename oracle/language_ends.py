@@ -74,8 +74,8 @@ def cross_entropy_bounds(h, table, targets, dloss, cap, bf16):
     magnitude of either row times the other's sum.  The cap's tanh is good to 2^-20 of itself.  A sum of exponentials is good to 2^-18 (their
     arguments, up to about 20 where they weigh, are rounded at 2^-23 of themselves, and at most 128 additions follow each
     other), its logarithm to 2^-22 of itself.  What lies below fp32's smallest normal number, 2^-126, may be lost: a
-    probability, and a gradient.  dz is rounded to bf16 (2^-8) for bf16 operands, and so are the gradients; but for
-    dh what rounding takes off the target's dz is added again (to 2^-23: an fp32 difference, and its product), and for
+    probability, and a gradient.  dz is rounded to bf16 (2^-8) for bf16 operands, and so are the gradients; but
+    what rounding takes off the target's dz is added again (to 2^-23: an fp32 difference, and its product), and in
     the table's gradient of up to 1024 rows what it takes off any, itself rounded (2^-16)."""
     h, table = np.asarray(h, np.float64), np.asarray(table, np.float64)
     D, V, N = h.shape[1], len(table), len(h)
@@ -100,11 +100,10 @@ def cross_entropy_bounds(h, table, targets, dloss, cap, bf16):
     half = 2.0 ** -8 if bf16 else 2.0 ** -24
     ddz += half * np.abs(g["dz"]) + 2.0 ** -126 * (up + 1.0 * there[:, None])
     size_h, size_e = np.abs(g["dz"]) @ np.abs(table), np.abs(g["dz"])[there].T @ np.abs(h[there])
-    exact, few = ddz.copy(), ddz
+    exact = ddz.copy()
     if bf16:
         exact[y == 1.0] -= (half - 2.0 ** -23) * np.abs(g["dz"][y == 1.0])
-        if N <= 1024:
-            few = ddz - (half - 2.0 ** -16) * np.abs(g["dz"])
+    few = ddz - (half - 2.0 ** -16) * np.abs(g["dz"]) if bf16 and N <= 1024 else exact
     out["dh"] = exact @ np.abs(table) + (V + 1) * 2.0 ** -23 * size_h + half * np.abs(g["dh"]) * 1.01 + 2.0 ** -126
     out["dtable"] = few[there].T @ np.abs(h[there]) + (2 * N + 1) * 2.0 ** -23 * size_e + half * np.abs(g["dtable"]) * 1.01 + 2.0 ** -126
     return out

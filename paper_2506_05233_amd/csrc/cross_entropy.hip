@@ -816,7 +816,7 @@ __global__ void __launch_bounds__(S::kThreads) logits_grad_kernel(LogitsArgs a)
         if (row >= a.dz_rows) continue;
         uint16_t* dst = a.dz + row * a.dz_ld + c0 + 4 * g;
         // Rounded to bf16 once for both products: 2^-8 of an element at most, at random over the sums.  But for the
-        // target's, as large as all others of its row together: what its rounding takes off is kept, and dh gets it back.
+        // target's, as large as all others of its row together: what its rounding takes off is kept, and both get it back.
         if constexpr (S::Planes == 1) {
             if (target) {
 #pragma unroll
@@ -852,15 +852,23 @@ __global__ void __launch_bounds__(S::kThreads) logits_grad_kernel(LogitsArgs a)
     }
 }
 
-// Rows whose target is none come out as zeros (targets.p null: every row counts), the others with rest times
-// their target's row of the table added (rest null: nothing).
+// What a gradient's rows get at the end.  Of dh (targets.p not null), zeros where the target is none, else rest times
+// their target's row of the table added (rest null: nothing).  Of the table (at not null), row at[row] - 1 of
+// `sums` added, where at[row] is not 0: the sum of rest_n h_n over the rows n whose target it is.
 struct Finish {
     Tokens targets;
     int64_t vocab;
     const float* rest;
     const uint16_t* table;
     int64_t table_stride;
+    const float* sums;
+    int64_t sums_ld;
+    const int32_t* at;
 };
+__device__ __forceinline__ const float* sums_of(const Finish& f, int32_t at)
+{
+    return at > 0 ? f.sums + int64_t(at - 1) * f.sums_ld : nullptr;
+}
 struct RowEnd {
     bool counts;
     float rest;
@@ -941,6 +949,15 @@ __global__ void __launch_bounds__(S::kThreads) grad_kernel(GradArgs a)
     // four channels in one access: the rows' pitch and the base allow it (the slab's always do)
     const bool wide = a.out != nullptr && (a.out_stride * int64_t(sizeof(T))) % (4 * sizeof(T)) == 0 && uintptr_t(a.out) % (4 * sizeof(T)) == 0;
     float* slab = a.slab == nullptr ? nullptr : a.slab + int64_t(blockIdx.y) * a.slab_layer;
+    int32_t at[S::NT];      // of all rows together, ahead of what hangs on them: row by row their latency was 4 us of a wide tile
+#pragma unroll
+    for (int j = 0; j < S::NT; ++j) {
+        at[j] = 0;
+        if constexpr (!AlongB) {
+            const int64_t row = n0 + (wn * S::NT + j) * 16 + n;
+            if (a.out != nullptr && a.finish.at != nullptr && row < a.n) at[j] = a.finish.at[row];
+        }
+    }
 #pragma unroll
     for (int j = 0; j < S::NT; ++j) {
         const int64_t row = n0 + (wn * S::NT + j) * 16 + n;
@@ -952,6 +969,22 @@ __global__ void __launch_bounds__(S::kThreads) grad_kernel(GradArgs a)
                 if (first + 16 * i >= a.width) continue;
                 f32x4* to = reinterpret_cast<f32x4*>(slab + row * a.slab_ld + first + 16 * i);
                 *to = a.first ? acc[i][j] : acc[i][j] + *to;
+            }
+            continue;
+        }
+        if constexpr (!AlongB) {
+            const float* more = sums_of(a.finish, at[j]);
+            if (more != nullptr) {
+                f32x4 x[S::MT];      // asked for together
+#pragma unroll
+                for (int i = 0; i < S::MT; ++i) x[i] = first + 16 * i < a.width ? *reinterpret_cast<const f32x4*>(more + first + 16 * i) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int i = 0; i < S::MT; ++i) acc[i][j] += x[i];
+            }
+#pragma unroll
+            for (int i = 0; i < S::MT; ++i) {
+                const int left = int(max(min(a.width - first - 16 * i, int64_t(4)), int64_t(0)));
+                if (left > 0) put4(static_cast<T*>(a.out) + row * a.out_stride + first + 16 * i, left, wide && left == 4, acc[i][j]);
             }
             continue;
         }
@@ -995,6 +1028,7 @@ __global__ void __launch_bounds__(kSumThreads) layer_sum_kernel(SumArgs a)
     const float* src = a.slab + row * a.slab_ld + m;
 #pragma unroll 4
     for (int64_t l = 0; l < a.layers; ++l) y += *reinterpret_cast<const f32x4*>(src + l * a.slab_layer);
+    if (const float* more = sums_of(a.finish, a.finish.at == nullptr ? 0 : a.finish.at[row]); more != nullptr) y += *reinterpret_cast<const f32x4*>(more + m);
     T* p = static_cast<T*>(a.out) + row * a.out_stride + m;
     const int left = int(min(a.width - m, int64_t(4)));
     const RowEnd end(a.finish, row);
@@ -1104,11 +1138,21 @@ constexpr int64_t kCopyBytes = int64_t(256) << 20;
 // Elements of dz at a time.  16384 rows by 50257 of 2048 bf16 channels: backward 9.41 ms with half as many, 8.60 with
 // these, 8.58 with twice, 9.01 with four times; 4096 rows of 768 fp32 channels 4.88, 4.57, 4.53, 4.47.
 constexpr int64_t kPieceElements = int64_t(1) << 27;
-// Up to so many bf16 rows dz has its rounding's rest behind it as rows of their own, and h once more, for the table's
-// gradient: in sums of few rows such roundings do not even out.  Its error, in parts of its norm, is then its own
-// rounding's, 0.0017, for 0.0027 at 3 rows by 20000 of 768 to 1024 channels, 0.0025 at 100, 0.0024 at 1000 (0.0022 at
-// 2048, where it is left); the backward call takes 40 us for 36.5 at 256 rows by 5003 of 768, 368 for 308 by 50257 of 2048.
+// What rounding takes off bf16 rows' dz does not even out in sums of few rows.  Up to so many rows, or products, dz has its
+// rounding's rest behind it as rows of their own, and h once more, for the table's gradient: its error is its own
+// rounding's, 0.0017 of its norm, for 0.0027 at 3 rows by 20000 of 768 to 1024 channels, 0.0025 at 100, 0.0024 at 1000.  That
+// doubles the product: the backward call takes 40 us for 36.5 at 256 rows by 5003 of 768, 368 for 308 by 50257 of 2048.
+// Of more the target's element alone, which is most of it, gets its rest back, summed over the sorted rows of each target:
+// 0.0017 as well where the probabilities are spread (0.0020 without at 3997 rows by 32003 of 1000), at most 0.0024 where other
+// elements of dz are as large.  Sorting and summing are launches: a training pass over 1500 rows by 1000 of 128
+// takes 47 us with all of the rest, 60 with the target's, over 1100 by 5003 of 768 106 and 110, 2048 by 5003 of 768 161
+// and 159, backward over 2000 by 32003 of 1000 609 and 475, 2048 by 50257 of 2048 1742 and 1285.
 constexpr int64_t kTwiceRows = 1024;
+constexpr float kTwiceProducts = 4.3e9f;
+bool keeps_all_rest(int64_t rows, int64_t vocab, int64_t width)
+{
+    return rows <= kTwiceRows || float(rows) * float(vocab) * float(width) <= kTwiceProducts;
+}
 constexpr int64_t kSlabBytes = int64_t(256) << 20;     // of fp32 layers of one product, at most (or one layer)
 
 // Rows of the table in a piece of the forward, where it has to be copied.
@@ -1157,15 +1201,17 @@ struct ForwardPlan {
 
 struct GradPlan {
     // h and the table as the gradients' products read them, and (fp32) as the logits' does, with the exponents
-    int64_t piece, dz, dz_rows, deep, dz_ld, h, table, h16, table16, h_e, table_e, rest, slab_h, slab_e, bytes, ld;
+    int64_t piece, dz, dz_rows, deep, dz_ld, h, table, h16, table16, h_e, table_e, rest, slab_h, slab_e, order, sums, at, bytes, ld;
     Shape logits;
     Cut dh, de, de_last;
+    bool sorts;      // the table's gradient gets the targets' rests, from sorted targets
     GradPlan(int64_t rows, int64_t vocab, int64_t width, int dtype)
     {
         const int planes = grad_planes(dtype);
         ld = ceil_to(width, kStepK);
         dz_rows = ceil_to(rows, 64);
-        deep = planes == 1 && rows <= kTwiceRows ? 2 * dz_rows : dz_rows;
+        const bool all_rest = keeps_all_rest(rows, vocab, width);
+        deep = planes == 1 && all_rest ? 2 * dz_rows : dz_rows;
         piece = std::max<int64_t>(256, kPieceElements / deep / 256 * 256);
         // pieces whose part of the table's gradient is whole rounds of wide tiles on all compute units, where they are
         // large enough for that; else pieces of about the same size
@@ -1193,6 +1239,10 @@ struct GradPlan {
         slab_h = dh.layers > 1 || piece < vocab ? c.take(dh.layers * rows * ld * 4) : 0;
         const int64_t layered = std::max(de.layers > 1 ? de.layers * piece : 0, de_last.layers > 1 ? de_last.layers * ending : 0);
         slab_e = layered > 0 ? c.take(layered * ld * 4) : 0;
+        sorts = planes == 1 && !all_rest;
+        order = sorts ? c.take(embedding_grad_bytes(rows, width)) : 0;
+        sums = sorts ? c.take(rows * ld * 4) : 0;
+        at = sorts ? c.take(vocab * 4) : 0;
         bytes = c.at;
     }
     // Layers have at least eight steps of 64, and there is room for their sums.
@@ -1328,6 +1378,23 @@ hipError_t launch_cross_entropy_grad(const CrossEntropyGradArgs& a, hipStream_t 
     const int64_t dz_plane = plan.deep * plan.dz_ld;
     const Matrix h{words(plan.h), ld, plan.deep * ld, plan.deep, ld};
     const bool twice = plan.deep > plan.dz_rows;
+    Finish more{};
+    TokenSumArgs sums{};
+    const bool sorts = plan.sorts && a.dtable != nullptr;
+    if (sorts) {
+        more.sums = sums.sums = reinterpret_cast<float*>(ws + plan.sums);
+        more.sums_ld = sums.ld = ld;
+        sums.at = reinterpret_cast<int32_t*>(ws + plan.at);
+        sums.rows = a.rows;
+        sums.width = a.width;
+        sums.x = words(plan.h);
+        sums.stride = ld;
+        sums.weight = rest;
+        sums.workspace = ws + plan.order;
+        if (hipError_t e = launch_token_sort(a.targets, a.rows, a.vocab, a.width, Zeros{sums.at, a.vocab, 4, 4, 4}, sums.workspace, &sums.sorted, stream);
+            e != hipSuccess)
+            return e;
+    }
 
     for (int64_t first = 0; first < a.vocab; first += plan.piece) {
         const int64_t piece = std::min(plan.piece, a.vocab - first);
@@ -1428,12 +1495,19 @@ hipError_t launch_cross_entropy_grad(const CrossEntropyGradArgs& a, hipStream_t 
             d.slab_ld = ld;
             d.slab_layer = piece * ld;
             d.first = true;
+            if (sorts) {
+                sums.first = uint32_t(first);
+                sums.count = uint32_t(piece);
+                if (e = launch_token_sums(sums, stream); e != hipSuccess) return e;
+                more.at = sums.at + first;
+            }
+            d.finish = more;
             void* out = static_cast<char*>(a.dtable) + first * a.dtable_stride * es;
             d.out = layers == 1 ? out : nullptr;
             d.out_stride = a.dtable_stride;
             if (e = launch_grad<false>(d, shape, layers, planes, stream); e != hipSuccess) return e;
             if (layers > 1) {
-                const SumArgs s{d.slab, ld, d.slab_layer, layers, piece, a.width, out, a.dtable_stride, {}};
+                const SumArgs s{d.slab, ld, d.slab_layer, layers, piece, a.width, out, a.dtable_stride, more};
                 if (e = launch_sum(s, a.dtype, stream); e != hipSuccess) return e;
             }
         }

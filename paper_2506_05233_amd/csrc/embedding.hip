@@ -12,6 +12,8 @@
 // the compute units busy, and the others fill the gradient with zeros in the same launches, which is most of
 // its traffic (206 of 273 MB, 4.3 TB/s).  The pieces take 20 (67 MB read, 30 written), the join 9, which is latency.
 // Few rows are launches and latency: 777 of 321 fp32 channels 15 us.
+//
+// The loss's gradient adds up weighted rows of sorted targets by the same kernels, a part of the vocabulary at a time.
 #include <algorithm>
 
 #include "mesa_kernels.hpp"
@@ -217,12 +219,6 @@ struct SortArgs {
     int digits;                    // of a whole key (a single workgroup sorts by all of them)
 };
 
-// Zeros for rows of the table's gradient, in a launch's workgroups from `first` on.
-struct Fill {
-    char* p;
-    int64_t rows, bytes, pitch;      // bytes of a row, and between rows
-    int element;                     // bytes: 4 or 2
-};
 // `bytes` from p on by `threads` threads, of which this is the i-th.
 __device__ __forceinline__ void fill_bytes(char* p, int64_t bytes, int element, int64_t i, int64_t threads)
 {
@@ -236,18 +232,20 @@ __device__ __forceinline__ void fill_bytes(char* p, int64_t bytes, int element, 
             *reinterpret_cast<uint16_t*>(p + at) = 0;
     }
 }
-__device__ __forceinline__ void fill_rows(const Fill& f, int64_t first)
+// Rows of zeros, in a launch's workgroups from `first` on.
+__device__ __forceinline__ void fill_rows(const Zeros& f, int64_t first)
 {
+    char* to = static_cast<char*>(f.p);
     const int64_t block = int64_t(blockIdx.x) - first, blocks = int64_t(gridDim.x) - first;
     if (f.bytes == f.pitch) {        // dense rows are one run
-        fill_bytes(f.p, f.rows * f.bytes, f.element, block * blockDim.x + threadIdx.x, blocks * blockDim.x);
+        fill_bytes(to, f.rows * f.bytes, f.element, block * blockDim.x + threadIdx.x, blocks * blockDim.x);
         return;
     }
-    for (int64_t row = block; row < f.rows; row += blocks) fill_bytes(f.p + row * f.pitch, f.bytes, f.element, threadIdx.x, blockDim.x);
+    for (int64_t row = block; row < f.rows; row += blocks) fill_bytes(to + row * f.pitch, f.bytes, f.element, threadIdx.x, blockDim.x);
 }
 
 // How many keys of a tile have each value of a digit.
-__global__ void __launch_bounds__(kThreads) token_histogram_kernel(SortArgs a, Fill fill)
+__global__ void __launch_bounds__(kThreads) token_histogram_kernel(SortArgs a, Zeros fill)
 {
     if (int64_t(blockIdx.x) >= a.tiles) {
         fill_rows(fill, a.tiles);
@@ -286,7 +284,7 @@ __device__ __forceinline__ void scan_bins(uint32_t* x, uint32_t* wave_total)
 static_assert(kBins == 2 * kThreads, "two bins a thread");
 
 // A tile's keys to their places by one digit.
-__global__ void __launch_bounds__(kThreads) token_scatter_kernel(SortArgs a, Fill fill)
+__global__ void __launch_bounds__(kThreads) token_scatter_kernel(SortArgs a, Zeros fill)
 {
     if (int64_t(blockIdx.x) >= a.tiles) {
         fill_rows(fill, a.tiles);
@@ -345,7 +343,7 @@ __global__ void __launch_bounds__(kThreads) token_scatter_kernel(SortArgs a, Fil
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / kWave, kSortRounds = 2;
 
 template <int Rounds>
-__global__ void __launch_bounds__(kSortThreads) token_sort_kernel(SortArgs a, Fill fill)
+__global__ void __launch_bounds__(kSortThreads) token_sort_kernel(SortArgs a, Zeros fill)
 {
     if (blockIdx.x > 0) {
         fill_rows(fill, 1);
@@ -423,9 +421,12 @@ __global__ void __launch_bounds__(kSortThreads) token_sort_kernel(SortArgs a, Fi
 // ------------------------------------------------------------------ the sums
 struct SumArgs {
     const void* dy;
-    int64_t rows, vocab, width, dy_stride, table_stride, ld;     // ld: of the pieces' sums
+    int64_t rows, width, dy_stride, table_stride, ld;     // ld: of the pieces' sums
+    uint32_t first, count;         // tokens whose sums are wanted (first 0 but for weighted rows)
     float scale;
     bool accumulate;
+    const float* weight;           // of weighted rows: their weights,
+    int32_t* at;                   // and where a token's sum is, plus one, in dtable, here a list of sums
     const uint32_t* keys;          // sorted, with the rows that they came from
     const uint32_t* places;
     float* entered;                // [pieces][ld]: of each piece its part of a token that begins before it
@@ -448,10 +449,13 @@ constexpr uint32_t kNoKey = 0xFFFFFFFFu;
 // 333 without runs, 69 and 84 with them.
 constexpr int64_t kRunRows = 16384;
 
+__device__ __forceinline__ bool wanted(const SumArgs& a, uint32_t key) { return key - a.first < a.count; }
+
+// A token's sum to its row: the token's own, or of weighted rows that of its first sorted position.
 template <typename O, int V>
-__device__ __forceinline__ void write_row(const SumArgs& a, uint32_t token, const Place& c, float (&sum)[V])
+__device__ __forceinline__ void write_row(const SumArgs& a, int64_t row, const Place& c, float (&sum)[V])
 {
-    O* dst = static_cast<O*>(a.dtable) + int64_t(token) * a.table_stride + c.at;
+    O* dst = static_cast<O*>(a.dtable) + row * a.table_stride + c.at;
     float x[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) x[v] = 0.0f;
@@ -462,8 +466,8 @@ __device__ __forceinline__ void write_row(const SumArgs& a, uint32_t token, cons
 }
 
 // Each piece of sorted positions: its tokens' sums.
-template <typename T, typename O, int V, int kPiece>
-__global__ void __launch_bounds__(kThreads) token_piece_kernel(SumArgs a, Lanes lanes)
+template <typename T, typename O, int V, int kPiece, bool Weighted>
+__device__ __forceinline__ void add_piece(const SumArgs& a, const Lanes& lanes)
 {
     const int64_t piece = int64_t(blockIdx.x) * lanes.rows() + lanes.row(), first = piece * kPiece;
     if (first >= a.rows) return;
@@ -471,7 +475,7 @@ __global__ void __launch_bounds__(kThreads) token_piece_kernel(SumArgs a, Lanes 
     if (from >= a.width) return;
     const Place c = place_of<V>(from, a.width);
     const int n = int(min(int64_t(kPiece), a.rows - first));
-    const uint32_t vocab = uint32_t(a.vocab);
+    if (Weighted && a.keys[first + n - 1] < a.first) return;
     uint32_t key[kPiece], place[kPiece];
 #pragma unroll
     for (int e = 0; e < kPiece; ++e) {
@@ -480,28 +484,41 @@ __global__ void __launch_bounds__(kThreads) token_piece_kernel(SumArgs a, Lanes 
         place[e] = a.places[i];
     }
     const uint32_t before = first > 0 ? a.keys[first - 1] : kNoKey, after = first + n < a.rows ? a.keys[first + n] : kNoKey;
-    if (key[0] >= vocab) return;      // only rows that do not count from here on
-    // every row of the piece is asked for before the first is added (in the place of a row that does not count,
-    // all of which come last, the first one again, for a sum that is not kept)
-    Channels<T, V> x[kPiece];
+    if (key[0] >= a.first + a.count) return;      // only rows that do not count from here on
+    // every row of the piece is asked for before the first is added (in the place of a row that does not count
+    // one that does, for a sum that is not kept: those come last, and of weighted rows first, too)
+    uint32_t some = place[0];
+    if constexpr (Weighted) {
 #pragma unroll
-    for (int e = 0; e < kPiece; ++e) x[e].load(static_cast<const T*>(a.dy) + int64_t(key[e] < vocab ? place[e] : place[0]) * a.dy_stride + c.at);
+        for (int e = 0; e < kPiece; ++e) some = wanted(a, key[e]) ? place[e] : some;
+    }
+    Channels<T, V> x[kPiece];
+    float weight[kPiece];
+#pragma unroll
+    for (int e = 0; e < kPiece; ++e) {
+        const uint32_t row = wanted(a, key[e]) ? place[e] : some;
+        x[e].load(static_cast<const T*>(a.dy) + int64_t(row) * a.dy_stride + c.at);
+        if constexpr (Weighted) weight[e] = a.weight[row];
+    }
     uint32_t token = key[0];
+    int64_t begin = first;
     bool begins = token != before;
     float sum[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) sum[v] = 0.0f;
     auto flush = [&](bool ends) {
+        if (Weighted && begins && from == 0) a.at[token] = int32_t(begin) + 1;
         if (begins && ends)
-            write_row<O, V>(a, token, c, sum);
+            write_row<O, V>(a, Weighted ? begin : int64_t(token), c, sum);
         else
             store_channels<float, V>((begins ? a.left : a.entered) + piece * a.ld + c.at, sum, c.own);
     };
 #pragma unroll
     for (int e = 0; e < kPiece; ++e) {
         if (key[e] != token) {
-            if (token < vocab) flush(true);
+            if (wanted(a, token)) flush(true);
             token = key[e];
+            begin = first + e;
             begins = true;
 #pragma unroll
             for (int v = 0; v < V; ++v) sum[v] = 0.0f;
@@ -509,9 +526,19 @@ __global__ void __launch_bounds__(kThreads) token_piece_kernel(SumArgs a, Lanes 
         float y[V];
         x[e].widen(y);
 #pragma unroll
-        for (int v = 0; v < V; ++v) sum[v] += y[v];
+        for (int v = 0; v < V; ++v) sum[v] = Weighted ? fmaf(weight[e], y[v], sum[v]) : sum[v] + y[v];
     }
-    if (token < vocab) flush(token != after);
+    if (wanted(a, token)) flush(token != after);
+}
+template <typename T, typename O, int V, int kPiece>
+__global__ void __launch_bounds__(kThreads) token_piece_kernel(SumArgs a, Lanes lanes)
+{
+    add_piece<T, O, V, kPiece, false>(a, lanes);
+}
+template <int V, int kPiece>
+__global__ void __launch_bounds__(kThreads) weighted_piece_kernel(SumArgs a, Lanes lanes)
+{
+    add_piece<bf16_t, float, V, kPiece, true>(a, lanes);
 }
 
 // Sums of the runs of pieces that lie within one token's rows, the first of which come before them.
@@ -521,7 +548,7 @@ __global__ void __launch_bounds__(kThreads) token_run_kernel(SumArgs a)
     const int64_t first = int64_t(blockIdx.x) * kPiece * kRun;
     if (first == 0 || first + kPiece * kRun > a.rows) return;
     const uint32_t k = a.keys[first - 1];
-    if (k != a.keys[first + kPiece * kRun - 1] || k >= uint32_t(a.vocab)) return;
+    if (k != a.keys[first + kPiece * kRun - 1] || !wanted(a, k)) return;
     const float* src = a.entered + int64_t(blockIdx.x) * kRun * a.ld;
     for (int64_t from = int64_t(threadIdx.x) * V; from < a.width; from += kThreads * V) {
         const Place c = place_of<V>(from, a.width);
@@ -598,13 +625,13 @@ __device__ __forceinline__ int64_t pieces_entered(const SumArgs& a, uint32_t tok
 }
 
 // The tokens that begin in a piece and go on after it, one a group of lanes.
-template <typename O, int V, int kPiece>
-__global__ void __launch_bounds__(kThreads) token_join_kernel(SumArgs a, Lanes lanes)
+template <typename O, int V, int kPiece, bool Weighted>
+__device__ __forceinline__ void join_pieces(const SumArgs& a, const Lanes& lanes)
 {
     const int64_t piece = int64_t(blockIdx.x) * lanes.rows() + lanes.row(), first = piece * kPiece, last = first + kPiece - 1;
     if (last + 1 >= a.rows) return;
     const uint32_t token = a.keys[last];
-    if (token >= uint32_t(a.vocab) || a.keys[last + 1] != token) return;
+    if (!wanted(a, token) || a.keys[last + 1] != token) return;
     if (first > 0 && a.keys[first - 1] == token) return;      // it begins before
     const int64_t p0 = piece + 1, p1 = pieces_entered<kPiece>(a, token, last, lanes);
     const int64_t from = (int64_t(blockIdx.y) * lanes.count() + lanes.lane()) * V;
@@ -623,7 +650,17 @@ __global__ void __launch_bounds__(kThreads) token_join_kernel(SumArgs a, Lanes l
     } else {
         add_rows<V>(sum, a.entered + c.at, a.ld, p0, p1);
     }
-    write_row<O, V>(a, token, c, sum);
+    write_row<O, V>(a, Weighted ? int64_t(a.at[token]) - 1 : int64_t(token), c, sum);
+}
+template <typename O, int V, int kPiece>
+__global__ void __launch_bounds__(kThreads) token_join_kernel(SumArgs a, Lanes lanes)
+{
+    join_pieces<O, V, kPiece, false>(a, lanes);
+}
+template <int V, int kPiece>
+__global__ void __launch_bounds__(kThreads) weighted_join_kernel(SumArgs a, Lanes lanes)
+{
+    join_pieces<float, V, kPiece, true>(a, lanes);
 }
 
 int64_t ceil_to(int64_t x, int64_t n) { return (x + n - 1) / n * n; }
@@ -651,7 +688,7 @@ struct GradLayout {
     }
 };
 
-template <typename T, typename O, int V, int kPiece>
+template <typename T, typename O, int V, int kPiece, bool Weighted>
 hipError_t sums_of(const SumArgs& a, hipStream_t stream)
 {
     const int64_t pieces = (a.rows + kPiece - 1) / kPiece, runs = a.rows <= kRunRows ? 0 : pieces / kRun;
@@ -660,18 +697,32 @@ hipError_t sums_of(const SumArgs& a, hipStream_t stream)
     // a workgroup's lanes side by side, and along the second dimension of the grid
     const unsigned slabs = unsigned((a.width + lanes.count() * V - 1) / (lanes.count() * V));
     if (!grid_fits(blocks, kThreads) || !grid_fits(runs, kThreads)) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL((token_piece_kernel<T, O, V, kPiece>), dim3(unsigned(blocks), slabs), dim3(kThreads), 0, stream, a, lanes);
+    const dim3 grid(unsigned(blocks), slabs);
+    if constexpr (Weighted)
+        hipLaunchKernelGGL((weighted_piece_kernel<V, kPiece>), grid, dim3(kThreads), 0, stream, a, lanes);
+    else
+        hipLaunchKernelGGL((token_piece_kernel<T, O, V, kPiece>), grid, dim3(kThreads), 0, stream, a, lanes);
     if constexpr (kPiece == kManyPiece)
         if (runs > 0) hipLaunchKernelGGL((token_run_kernel<V, kPiece>), dim3(unsigned(runs)), dim3(kThreads), 0, stream, a);
-    if (pieces > 1) hipLaunchKernelGGL((token_join_kernel<O, V, kPiece>), dim3(unsigned(blocks), slabs), dim3(kThreads), 0, stream, a, lanes);
+    if (pieces > 1) {
+        if constexpr (Weighted)
+            hipLaunchKernelGGL((weighted_join_kernel<V, kPiece>), grid, dim3(kThreads), 0, stream, a, lanes);
+        else
+            hipLaunchKernelGGL((token_join_kernel<O, V, kPiece>), grid, dim3(kThreads), 0, stream, a, lanes);
+    }
     return hipGetLastError();
 }
 
-template <typename T, typename O, int V>
+template <typename T, typename O, int V, bool Weighted = false>
 hipError_t sums(const SumArgs& a, hipStream_t stream)
 {
-    return piece_of(a.rows) == kFewPiece ? sums_of<T, O, V, kFewPiece>(a, stream) : sums_of<T, O, V, kManyPiece>(a, stream);
+    return piece_of(a.rows) == kFewPiece ? sums_of<T, O, V, kFewPiece, Weighted>(a, stream) : sums_of<T, O, V, kManyPiece, Weighted>(a, stream);
 }
+
+// Few sums have a lane each, so that there are waves enough for the loads' latency: 16384 rows of 64 bf16 channels
+// take 30.8 us so and 35.8 with eight channels a lane, 1024 of 2048 14.2 and 16.0, 4096 of 1000 29.6 and 29.3,
+// 16384 of 320 34.7 and 31.6.
+bool eight_channels(int64_t rows, int64_t width) { return width >= 8 && rows * width >= (int64_t(1) << 22); }
 
 }  // namespace
 
@@ -686,34 +737,33 @@ hipError_t launch_embedding(const EmbeddingArgs& a, hipStream_t stream)
 
 int64_t embedding_grad_bytes(int64_t rows, int64_t width) { return GradLayout(rows, width).bytes; }
 
-hipError_t launch_embedding_grad(const EmbeddingGradArgs& a, hipStream_t stream)
+hipError_t launch_token_sort(const Tokens& tokens, int64_t rows, int64_t vocab, int64_t width, const Zeros& zeros, char* ws, Sorted* sorted,
+                             hipStream_t stream)
 {
-    const GradLayout lay(a.rows, a.width);
-    char* ws = a.workspace;
+    const GradLayout lay(rows, width);
     int key_bits = 1;
-    while (key_bits < 32 && (int64_t(1) << key_bits) <= a.vocab) ++key_bits;
+    while (key_bits < 32 && (int64_t(1) << key_bits) <= vocab) ++key_bits;
     const int digits = (key_bits + kDigitBits - 1) / kDigitBits;
     SortArgs s{};
-    s.tokens = a.tokens;
-    s.rows = a.rows;
-    s.vocab = a.vocab;
+    s.tokens = tokens;
+    s.rows = rows;
+    s.vocab = vocab;
     s.hist = reinterpret_cast<uint32_t*>(ws + lay.hist);
     s.tiles = lay.tiles;
     s.bits = (key_bits + digits - 1) / digits;
     s.digits = digits;
     uint32_t* keys[2] = {reinterpret_cast<uint32_t*>(ws + lay.keys[0]), reinterpret_cast<uint32_t*>(ws + lay.keys[1])};
     uint32_t* places[2] = {reinterpret_cast<uint32_t*>(ws + lay.places[0]), reinterpret_cast<uint32_t*>(ws + lay.places[1])};
-    // the table's rows are filled with zeros in equal shares of the sort's launches
-    const int64_t es = a.table_dtype == kBf16 ? 2 : 4, bytes = a.width * es, pitch = a.table_stride * es;
-    const int shares = a.rows <= kSortRounds * kSortThreads ? 1 : 2 * digits;
+    // the rows of zeros are written in equal shares of the sort's launches
+    const int shares = rows <= kSortRounds * kSortThreads ? 1 : 2 * digits;
     int share = 0;
     int64_t blocks = 0;
     auto next_fill = [&](int threads) {
-        const int64_t r0 = a.vocab * share / shares, r1 = a.vocab * (share + 1) / shares;
+        const int64_t r0 = zeros.rows * share / shares, r1 = zeros.rows * (share + 1) / shares;
         ++share;
-        const Fill f{static_cast<char*>(a.dtable) + r0 * pitch, a.accumulate ? 0 : r1 - r0, bytes, pitch, int(es)};
+        const Zeros f{static_cast<char*>(zeros.p) + r0 * zeros.pitch, r1 - r0, zeros.bytes, zeros.pitch, zeros.element};
         // about 64 KB a workgroup, at most eight a compute unit
-        blocks = std::min<int64_t>(ceil_to(f.rows * bytes, 65536) / 65536, 2048 * kThreads / threads);
+        blocks = std::min<int64_t>(ceil_to(f.rows * f.bytes, 65536) / 65536, 2048 * kThreads / threads);
         return f;
     };
     int out = 0;
@@ -721,9 +771,9 @@ hipError_t launch_embedding_grad(const EmbeddingGradArgs& a, hipStream_t stream)
     if (shares == 1) {
         s.keys_out = keys[0];
         s.places_out = places[0];
-        const Fill fill = next_fill(kSortThreads);
+        const Zeros fill = next_fill(kSortThreads);
         const dim3 grid(unsigned(1 + blocks)), block(kSortThreads);
-        if (a.rows <= kSortThreads)
+        if (rows <= kSortThreads)
             hipLaunchKernelGGL(token_sort_kernel<1>, grid, block, 0, stream, s, fill);
         else
             hipLaunchKernelGGL(token_sort_kernel<kSortRounds>, grid, block, 0, stream, s, fill);
@@ -735,24 +785,42 @@ hipError_t launch_embedding_grad(const EmbeddingGradArgs& a, hipStream_t stream)
             out = d == 0 ? 0 : 1 - out;
             s.keys_out = keys[out];
             s.places_out = places[out];
-            const Fill one = next_fill(kThreads);
+            const Zeros one = next_fill(kThreads);
             hipLaunchKernelGGL(token_histogram_kernel, dim3(unsigned(lay.tiles + blocks)), dim3(kThreads), 0, stream, s, one);
-            const Fill two = next_fill(kThreads);
+            const Zeros two = next_fill(kThreads);
             hipLaunchKernelGGL(token_scatter_kernel, dim3(unsigned(lay.tiles + blocks)), dim3(kThreads), 0, stream, s, two);
         }
     }
-    if (hipError_t e = hipGetLastError(); e != hipSuccess || a.rows == 0) return e;
-    const SumArgs k{a.dy, a.rows, a.vocab, a.width, a.dy_stride, a.table_stride, lay.ld, a.scale, a.accumulate, keys[out], places[out],
-                    reinterpret_cast<float*>(ws + lay.entered), reinterpret_cast<float*>(ws + lay.left),
+    *sorted = Sorted{keys[out], places[out]};
+    return hipGetLastError();
+}
+
+hipError_t launch_embedding_grad(const EmbeddingGradArgs& a, hipStream_t stream)
+{
+    const GradLayout lay(a.rows, a.width);
+    char* ws = a.workspace;
+    const int64_t es = a.table_dtype == kBf16 ? 2 : 4;
+    Sorted sorted;
+    const Zeros zeros{a.dtable, a.accumulate ? 0 : a.vocab, a.width * es, a.table_stride * es, int(es)};
+    if (hipError_t e = launch_token_sort(a.tokens, a.rows, a.vocab, a.width, zeros, ws, &sorted, stream); e != hipSuccess || a.rows == 0) return e;
+    const SumArgs k{a.dy, a.rows, a.width, a.dy_stride, a.table_stride, lay.ld, 0, uint32_t(a.vocab), a.scale, a.accumulate, nullptr, nullptr,
+                    sorted.keys, sorted.places, reinterpret_cast<float*>(ws + lay.entered), reinterpret_cast<float*>(ws + lay.left),
                     reinterpret_cast<float*>(ws + lay.runs), a.dtable};
-    // Few sums have a lane each, so that there are waves enough for the loads' latency: 16384 rows of 64 bf16 channels
-    // take 30.8 us so and 35.8 with eight channels a lane, 1024 of 2048 14.2 and 16.0, 4096 of 1000 29.6 and 29.3,
-    // 16384 of 320 34.7 and 31.6.
-    const bool wide = a.width >= 8 && a.rows * a.width >= (int64_t(1) << 22);
+    const bool wide = eight_channels(a.rows, a.width);
     if (a.dtype == kBf16 && a.table_dtype == kBf16) return wide ? sums<bf16_t, bf16_t, 8>(k, stream) : sums<bf16_t, bf16_t, 1>(k, stream);
     if (a.dtype == kBf16) return wide ? sums<bf16_t, float, 8>(k, stream) : sums<bf16_t, float, 1>(k, stream);
     if (a.table_dtype == kBf16) return wide ? sums<float, bf16_t, 8>(k, stream) : sums<float, bf16_t, 1>(k, stream);
     return wide ? sums<float, float, 8>(k, stream) : sums<float, float, 1>(k, stream);
+}
+
+hipError_t launch_token_sums(const TokenSumArgs& a, hipStream_t stream)
+{
+    const GradLayout lay(a.rows, a.width);
+    char* ws = a.workspace;
+    const SumArgs k{a.x, a.rows, a.width, a.stride, a.ld, lay.ld, a.first, a.count, 1.0f, false, a.weight, a.at,
+                    a.sorted.keys, a.sorted.places, reinterpret_cast<float*>(ws + lay.entered), reinterpret_cast<float*>(ws + lay.left),
+                    reinterpret_cast<float*>(ws + lay.runs), a.sums};
+    return eight_channels(a.rows, a.width) ? sums<bf16_t, float, 8, true>(k, stream) : sums<bf16_t, float, 1, true>(k, stream);
 }
 
 }  // namespace mesa

@@ -36,6 +36,36 @@ struct EmbeddingGradArgs {
 int64_t embedding_grad_bytes(int64_t rows, int64_t width);
 hipError_t launch_embedding_grad(const EmbeddingGradArgs& a, hipStream_t stream);
 
+// Its two stages apart, for sums that are wanted a part of the vocabulary at a time and of weighted rows.
+struct Sorted {
+    const uint32_t* keys;     // [rows] tokens in order (vocab for one that does not count)
+    const uint32_t* places;   // and the rows that they came from
+};
+// Zeros for `rows` rows of `bytes`, `pitch` apart, of elements of 4 or 2 bytes.
+struct Zeros {
+    void* p;
+    int64_t rows, bytes, pitch;
+    int element;
+};
+// Sorts the tokens and writes the zeros.  The workspace, of embedding_grad_bytes(rows, width), holds what is sorted.
+hipError_t launch_token_sort(const Tokens& tokens, int64_t rows, int64_t vocab, int64_t width, const Zeros& zeros, char* workspace, Sorted* sorted,
+                             hipStream_t stream);
+struct TokenSumArgs {
+    Sorted sorted;
+    int64_t rows, width;
+    uint32_t first, count;    // the tokens [first, first + count)
+    const uint16_t* x;        // [rows] bf16 rows, stride apart
+    int64_t stride;
+    const float* weight;      // [rows]
+    // of each of those tokens that occurs sum weight_n x_n over its rows in their order, fp32, at row at[token] - 1 of `sums`
+    // (where the first of its rows was sorted to), ld a multiple of 4; at[] of the others is left as it is
+    float* sums;
+    int64_t ld;
+    int32_t* at;
+    char* workspace;          // the sort's
+};
+hipError_t launch_token_sums(const TokenSumArgs& a, hipStream_t stream);
+
 struct CrossEntropyArgs {
     const void* h;            // [rows] rows of width, h_stride apart
     const void* table;        // [vocab] rows of width, table_stride apart
