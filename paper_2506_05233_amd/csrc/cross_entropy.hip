@@ -771,11 +771,12 @@ __global__ void __launch_bounds__(S::kThreads) logits_grad_kernel(LogitsArgs a)
     for (int j = 0; j < S::NT; ++j) {
         const int64_t row = n0 + (wn * S::NT + j) * 16 + n;
         int64_t t = -1;
-        // a row that does not count has products of 0 (h is copied so) and takes exp(-far) times 0
-        float lse = 1e30f, up = 0.0f;
+        bool counts = false;
+        float lse = 0.0f, up = 0.0f;
         if (row < a.rows) {
             t = token_at(a.targets, row);
-            if (t >= 0 && t < a.vocab) lse = a.lse[row], up = a.dloss[row];
+            counts = t >= 0 && t < a.vocab;
+            if (counts) lse = a.lse[row], up = a.dloss[row];
         }
         const int64_t to = t - a.first - c0;
         const int mine = t < a.vocab && to >= 0 && to < here ? int(to) : -1;
@@ -812,6 +813,14 @@ __global__ void __launch_bounds__(S::kThreads) logits_grad_kernel(LogitsArgs a)
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
                     if (16 * i + 4 * g + r >= here) acc[i][j][r] = 0.0f;
+        }
+        // rows that do not count, and those that fill up the last step of 64: h is copied as zeros there, but the products
+        // of those with an infinity or a NaN of the table are not 0
+        if (!__all(counts)) {
+#pragma unroll
+            for (int i = 0; i < S::MT; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) acc[i][j][r] = counts ? acc[i][j][r] : 0.0f;
         }
         if (row >= a.dz_rows) continue;
         uint16_t* dst = a.dz + row * a.dz_ld + c0 + 4 * g;
