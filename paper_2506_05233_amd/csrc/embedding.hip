@@ -19,9 +19,12 @@
 #include "mesa_kernels.hpp"
 #include "mesa_lanes.hpp"
 #include "vocab.hpp"
+#include "vocab_plan.hpp"
 
 namespace mesa {
 namespace {
+
+using namespace vocab;
 
 constexpr int kThreads = 256;
 
@@ -155,11 +158,8 @@ hipError_t lookup(const EmbeddingArgs& a, hipStream_t stream)
 }
 
 // ------------------------------------------------------------------ the tokens in order
-constexpr int kTile = 1024;            // tokens a workgroup sorts
 constexpr int kWaves = kThreads / kWave;
 constexpr int kRounds = kTile / kThreads;
-constexpr int kDigitBits = 9, kBins = 1 << kDigitBits;
-constexpr int kRun = 32;               // pieces of a run
 
 // A token's key: itself, or vocab for one that does not count, which comes last.
 __device__ __forceinline__ uint32_t key_of(const Tokens& t, int64_t i, int64_t vocab)
@@ -435,19 +435,8 @@ struct SumArgs {
     void* dtable;
 };
 
-// Sorted positions of a piece: short ones make more waves of few rows, long ones fewer sums to join.  777 rows of 321
-// fp32 channels take 14.6 us by 8, 17.6 by 16 and 23.7 by 32, 4096 of 1024 bf16 ones 27.9, 30.1 and 35.8, 16384 of
-// 2048 60.0, 55.0 and 57.2 (and all of them one token 204, 126 and 86).
-constexpr int kFewPiece = 8, kManyPiece = 16;
-constexpr int64_t kFewRows = 8192;
-int64_t piece_of(int64_t rows) { return rows <= kFewRows ? kFewPiece : kManyPiece; }
-
 constexpr int kDepth = 16;         // sums asked for together
 constexpr uint32_t kNoKey = 0xFFFFFFFFu;
-// Past so many rows there are runs of pieces.  Up to there a token that is everywhere has 1024 pieces at most: 16384
-// rows of 2048 bf16 channels take 55 us, 126 if they are one token, with runs 60 and 55.  65536 of 512 take 77 and
-// 333 without runs, 69 and 84 with them.
-constexpr int64_t kRunRows = 16384;
 
 __device__ __forceinline__ bool wanted(const SumArgs& a, uint32_t key) { return key - a.first < a.count; }
 
@@ -663,31 +652,6 @@ __global__ void __launch_bounds__(kThreads) weighted_join_kernel(SumArgs a, Lane
     join_pieces<float, V, kPiece, true>(a, lanes);
 }
 
-int64_t ceil_to(int64_t x, int64_t n) { return (x + n - 1) / n * n; }
-
-struct GradLayout {
-    int64_t tiles, ld, hist, keys[2], places[2], entered, left, runs, bytes;
-    GradLayout(int64_t rows, int64_t width)
-    {
-        tiles = (rows + kTile - 1) / kTile;
-        ld = ceil_to(width, 8);
-        int64_t at = 0;
-        auto take = [&](int64_t n) {
-            const int64_t p = at;
-            at += ceil_to(n, 256);
-            return p;
-        };
-        hist = take(tiles * kBins * 4);
-        for (int k = 0; k < 2; ++k) keys[k] = take(rows * 4), places[k] = take(rows * 4);
-        // no fewer for more rows: a workspace for many serves fewer
-        const int64_t few = std::min(rows, kFewRows), pieces = std::max((rows + piece_of(rows) - 1) / piece_of(rows), (few + kFewPiece - 1) / kFewPiece);
-        entered = take(pieces * ld * 4);
-        left = take(pieces * ld * 4);
-        runs = rows <= kRunRows ? 0 : take(pieces / kRun * ld * 4);
-        bytes = at;
-    }
-};
-
 template <typename T, typename O, int V, int kPiece, bool Weighted>
 hipError_t sums_of(const SumArgs& a, hipStream_t stream)
 {
@@ -735,12 +699,12 @@ hipError_t launch_embedding(const EmbeddingArgs& a, hipStream_t stream)
     return wide ? lookup<float, float, 8>(a, stream) : lookup<float, float, 1>(a, stream);
 }
 
-int64_t embedding_grad_bytes(int64_t rows, int64_t width) { return GradLayout(rows, width).bytes; }
+int64_t embedding_grad_bytes(int64_t rows, int64_t width) { return TokenSumLayout(rows, width).bytes; }
 
 hipError_t launch_token_sort(const Tokens& tokens, int64_t rows, int64_t vocab, int64_t width, const Zeros& zeros, char* ws, Sorted* sorted,
                              hipStream_t stream)
 {
-    const GradLayout lay(rows, width);
+    const TokenSumLayout lay(rows, width);
     int key_bits = 1;
     while (key_bits < 32 && (int64_t(1) << key_bits) <= vocab) ++key_bits;
     const int digits = (key_bits + kDigitBits - 1) / kDigitBits;
@@ -797,7 +761,7 @@ hipError_t launch_token_sort(const Tokens& tokens, int64_t rows, int64_t vocab, 
 
 hipError_t launch_embedding_grad(const EmbeddingGradArgs& a, hipStream_t stream)
 {
-    const GradLayout lay(a.rows, a.width);
+    const TokenSumLayout lay(a.rows, a.width);
     char* ws = a.workspace;
     const int64_t es = a.table_dtype == kBf16 ? 2 : 4;
     Sorted sorted;
@@ -815,7 +779,7 @@ hipError_t launch_embedding_grad(const EmbeddingGradArgs& a, hipStream_t stream)
 
 hipError_t launch_token_sums(const TokenSumArgs& a, hipStream_t stream)
 {
-    const GradLayout lay(a.rows, a.width);
+    const TokenSumLayout lay(a.rows, a.width);
     char* ws = a.workspace;
     const SumArgs k{a.x, a.rows, a.width, a.stride, a.ld, lay.ld, a.first, a.count, 1.0f, false, a.weight, a.at,
                     a.sorted.keys, a.sorted.places, reinterpret_cast<float*>(ws + lay.entered), reinterpret_cast<float*>(ws + lay.left),

@@ -6,6 +6,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "mesa_dtypes.hpp"
+
 namespace mesa {
 
 // Shapes of one forward call.  Token (b, h, t) lives at row (b*heads + h)*seq_len + t.
@@ -185,9 +187,6 @@ struct NormArgs {
     void* y;
 };
 hipError_t launch_output_norm(const NormArgs& a, hipStream_t stream);
-
-// Element types of the calls below (MESA_DTYPE_*).
-constexpr int kF32 = 0, kBf16 = 1, kQ8 = 2;
 
 // An 8-bit checkpoint of rows x width values: the int8 codes [rows, width], then, from the
 // next multiple of 16 bytes, the exponent bytes [rows, ceil(width / 32)].

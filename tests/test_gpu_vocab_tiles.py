@@ -1,0 +1,49 @@
+"""Every tile of the cross entropy's products over several steps, with remainders, in layers and not: the sizes of
+tests/vocab_cases.py, element by element within the oracle's bounds."""
+import pytest
+
+import vocab_cases as C
+from paper_2506_05233_amd import libmesa as L
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    L.load()
+    yield
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+
+
+def within(got, want, bound, name):
+    worst = (got.double() - want).abs() / bound.clamp(min=1e-300)
+    assert bool((worst <= 1.0).all()), (name, float(worst.max()), int(worst.argmax()))
+
+
+@pytest.mark.parametrize("cap", [0.0, 30.0])
+@pytest.mark.parametrize("rows,vocab,width,dtype", [c[:4] for c in C.TILES])
+def test_tiles(rows, vocab, width, dtype, cap):
+    h, table, targets, up = C.problem(rows, vocab, width, dtype, rows + vocab)
+    want, bound = C.reference(h, table, targets, up, cap, rows <= 1024)
+    need = L.cross_entropy_workspace_bytes(rows, vocab, width, dtype)
+    f = L.cross_entropy(h, table, targets, cap=cap, want_best=True, workspace=torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda"))
+    for n in ("lse", "loss"):
+        within(f[n], want[n], bound[n], n)
+    # the largest product, within what its terms' rounding may hide
+    slack = 2.0 * (width + 4) * 2.0 ** -23
+    z = (h.double() * table.double()[f["best"].long()]).sum(dim=1)
+    top = (h.double() * table.double()[want["best"]]).sum(dim=1)
+    size = h.double().abs().sum(dim=1) * table.double().abs().amax()
+    assert bool((z >= top - slack * size).all())
+    need = L.cross_entropy_backward_workspace_bytes(rows, vocab, width, dtype)
+    g = L.cross_entropy_backward(h, table, targets, f["lse"], up, cap=cap, workspace=torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda"))
+    for n in ("dh", "dtable"):
+        within(g[n], want[n], bound[n], n)
+    for _ in range(3):      # over what the last call left, and over itself: the same bits
+        again = dict(L.cross_entropy(h, table, targets, cap=cap, want_best=True), **L.cross_entropy_backward(h, table, targets, f["lse"], up, cap=cap))
+        assert all(torch.equal(again[n], v) for n, v in list(f.items()) + list(g.items()))
