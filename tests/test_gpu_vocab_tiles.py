@@ -1,5 +1,5 @@
-"""Every tile of the cross entropy's products over several steps, with remainders, in layers and not: the sizes of
-tests/vocab_cases.py, element by element within the oracle's bounds."""
+"""Every tile of the cross entropy's products over several steps, with remainders, in layers and not, and tables in
+several pieces: the sizes of tests/vocab_cases.py, element by element within the oracle's bounds."""
 import pytest
 
 import vocab_cases as C
@@ -28,6 +28,15 @@ def within(got, want, bound, name):
 @pytest.mark.parametrize("cap", [0.0, 30.0])
 @pytest.mark.parametrize("rows,vocab,width,dtype", [c[:4] for c in C.TILES])
 def test_tiles(rows, vocab, width, dtype, cap):
+    _check(rows, vocab, width, dtype, cap)
+
+
+@pytest.mark.parametrize("rows,vocab,width,dtype", [c[:4] for c in C.PIECES])
+def test_pieces(rows, vocab, width, dtype):
+    _check(rows, vocab, width, dtype, 30.0)
+
+
+def _check(rows, vocab, width, dtype, cap):
     h, table, targets, up = C.problem(rows, vocab, width, dtype, rows + vocab)
     want, bound = C.reference(h, table, targets, up, cap, rows <= 1024)
     need = L.cross_entropy_workspace_bytes(rows, vocab, width, dtype)

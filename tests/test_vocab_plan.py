@@ -54,6 +54,13 @@ def test_tiles(plan, case):
     assert (p["forward"], p["logits"], "%s%d" % (p["dh"], p["dh_layers"]), "%s%d" % (p["de"], p["de_layers"])) == case[4:]
 
 
+@pytest.mark.parametrize("case", C.PIECES)
+def test_pieces(plan, case):
+    p = plan(*case[:4])
+    assert (p["copies"], p["pieces"]) == case[4:]
+    assert p["pieces"] == 1 or 0 < case[1] - (p["pieces"] - 1) * p["piece"] < p["piece"]
+
+
 def _taken(p, dtype):
     return {(dtype, "forward", p["forward"], False), (dtype, "logits", p["logits"], False), (dtype, "dh", p["dh"], p["dh_layers"] > 1),
             (dtype, "de", p["de"], p["de_layers"] > 1)}

@@ -37,6 +37,19 @@ TILES = [
     (3001, 2003, 520, F32, "W", "W", "W4", "M3"),
 ]
 
+# rows, vocabulary, width, type; the parts of the table that the forward copies one after the other, and the pieces of
+# the vocabulary that the gradients take: both of the last kind shorter than the others
+PIECES = [
+    (3, 140001, 1000, BF16, 2, 1),       # a copied table, rows of 1000 channels
+    (1000, 70000, 64, BF16, 1, 2),       # dz with all of its rounding's rest behind it
+    (9000, 16000, 40, BF16, 1, 2),       # the targets' rests, from sorted targets
+    (17000, 9001, 32, BF16, 1, 2),       # the same over runs of sorted rows
+    (16384, 9000, 2048, BF16, 1, 2),     # wide tiles, no layers
+    (40, 70000, 2048, F32, 3, 1),        # planes and exponents of a table that is copied
+    (16384, 8500, 24, F32, 1, 2),        # layers of dh, added to by the second piece
+    (4100, 40001, 300, F32, 1, 2),       # wide tiles
+]
+
 
 def reference(h, table, targets, up, cap, keeps_all):
     """lse, loss, best, dh and dtable in 64 bits and, as oracle.language_ends.cross_entropy_bounds has them, their bounds
