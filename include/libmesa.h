@@ -576,11 +576,15 @@ int mesa_embedding_backward(const void* token, int token_bytes, const void* dy, 
  *     dz_nv = dloss_n (exp(l_nv - lse_n) - [v = target_n]) (1 - (l_nv / cap)^2), 0 where the target does not count
  *     dh_n = sum_v dz_nv E_v,  dE_v = sum_n dz_nv h_n
  *   dh [rows, width], dtable [vocab, width]: dtype; either may be NULL.  Rows of h, lse and dloss
- *   whose target does not count may hold anything.  dz, formed a piece of the vocabulary at a time
- *   (the workspace holds at most 2^27 elements of it, or 256 columns), is rounded to bf16 for bf16 inputs (2^-8 of an
- *   element).  dh and dtable get back what that takes off each target's element, which is as large as the others of its row
- *   together; dtable of up to 1024 rows, or rows vocab width up to 4.3e9, what it takes off all.
- *   With rows 0 dtable is zeros.  Up to nine kernel launches a piece, and up to eight before the first. */
+ *   whose target does not count may hold anything.  dz, formed a piece of the vocabulary at a time, is
+ *   rounded to bf16 for bf16 inputs (2^-8 of an element).  dh and dtable get back what that takes off each
+ *   target's element, which is as large as the others of its row together; dtable of up to 1024 rows, or
+ *   rows vocab width up to 4.3e9, what it takes off all.
+ *   With rows 0 dtable is zeros.  Up to nine kernel launches a piece, and up to eight before the first.
+ *   The workspace holds of a piece dz, at most 2^27 elements or 256 columns, of 2 bytes (fp32: 6), and a
+ *   copy of its part of the table, at most 1 GiB or 256 rows (2 bytes an element, of fp32 10, 6 for up to
+ *   32 rows; the query counts it also where the table turns out to need none); copies and sums of the
+ *   rows, at most 10 bytes an element; and sums of layers, at most 512 MiB or 4 bytes an element. */
 size_t mesa_cross_entropy_workspace_bytes(int64_t rows, int64_t vocab, int64_t width, int dtype);
 int mesa_cross_entropy(const void* h, const void* table, const void* target, int token_bytes, float cap, int64_t rows,
                        int64_t vocab, int64_t width, int64_t h_stride, int64_t table_stride, int dtype, float* loss,

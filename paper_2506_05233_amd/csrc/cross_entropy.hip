@@ -1081,7 +1081,7 @@ hipError_t with_grad_shape(Shape s, int planes, F f)
 // A table or h that the products read where it lies: bf16 rows of whole steps in 16-byte pieces.
 bool direct(const void* p, int64_t stride, int64_t width, int dtype)
 {
-    return dtype == kBf16 && width % kStepK == 0 && stride % 8 == 0 && stride < (int64_t(1) << 22) && uintptr_t(p) % 16 == 0;
+    return may_lie(width, dtype) && stride % 8 == 0 && stride < (int64_t(1) << 22) && uintptr_t(p) % 16 == 0;
 }
 
 }  // namespace
@@ -1090,7 +1090,7 @@ int64_t cross_entropy_bytes(int64_t rows, int64_t vocab, int64_t width, int dtyp
 
 int64_t cross_entropy_grad_bytes(int64_t rows, int64_t vocab, int64_t width, int dtype)
 {
-    return GradPlan(rows, vocab, width, dtype).bytes;
+    return grad_bytes(rows, vocab, width, dtype);
 }
 
 hipError_t launch_cross_entropy(const CrossEntropyArgs& a, hipStream_t stream)
@@ -1199,14 +1199,14 @@ hipError_t launch_cross_entropy_grad(const CrossEntropyGradArgs& a, hipStream_t 
         const SumArgs none{nullptr, ceil_to(a.width, 4), 0, 0, a.vocab, a.width, a.dtable, a.dtable_stride, {}};
         return launch_sum(none, a.dtype, stream);
     }
-    const GradPlan plan(a.rows, a.vocab, a.width, a.dtype);
+    const bool as_is = direct(a.table, a.table_stride, a.width, a.dtype);
+    const GradPlan plan(a.rows, a.vocab, a.width, a.dtype, !as_is);
     const int planes = grad_planes(a.dtype);
     const int64_t ld = plan.ld, es = planes == 1 ? 2 : 4;
     char* ws = a.workspace;
     auto words = [&](int64_t at) { return reinterpret_cast<uint16_t*>(ws + at); };
     uint16_t* dz = words(plan.dz);
     float* rest = planes == 1 ? reinterpret_cast<float*>(ws + plan.rest) : nullptr;
-    const bool as_is = direct(a.table, a.table_stride, a.width, a.dtype);
     const int64_t dz_plane = plan.deep * plan.dz_ld;
     const Matrix h{words(plan.h), ld, plan.deep * ld, plan.deep, ld};
     const bool twice = plan.deep > plan.dz_rows;

@@ -131,6 +131,10 @@ inline Shape shape_of(int64_t m, int64_t n, int64_t k, int planes) { return cut_
 // part empty.  One row by 50257 of 1000 bf16 channels, 103 MB of them: 62 us at 64 MiB, 51 in one; 2000 rows by 50257
 // of 768 fp32 channels 566, 547 (128 MiB), 527 (256), 524 (in one).
 constexpr int64_t kCopyBytes = int64_t(256) << 20;
+// And for the gradients, which take a piece of the vocabulary at a time for that too: 64 rows by 128000 of 4096 fp32
+// channels, 5.2 GB of planes, 3.65 ms in one piece, 4.16 by 1 GiB, 5.65 by 256 MiB; 256 rows by 50257 of 2048, 1.03 GB, 1.20
+// and (256 MiB) 1.48.
+constexpr int64_t kGradCopyBytes = int64_t(1) << 30;
 // Elements of dz at a time.  16384 rows by 50257 of 2048 bf16 channels: backward 9.41 ms with half as many, 8.60 with
 // these, 8.58 with twice, 9.01 with four times; 4096 rows of 768 fp32 channels 4.88, 4.57, 4.53, 4.47.
 constexpr int64_t kPieceElements = int64_t(1) << 27;
@@ -185,27 +189,35 @@ struct ForwardPlan {
     }
 };
 
+// Whether the products may read a table where it lies; whether they do hangs on its address and stride.
+inline bool may_lie(int64_t width, int dtype) { return dtype == kBf16 && width % kStepK == 0; }
+
 struct GradPlan {
     // h and the table as the gradients' products read them, and (fp32) as the logits' does, with the exponents
     int64_t piece, dz, dz_rows, deep, dz_ld, h, table, h16, table16, h_e, table_e, rest, slab_h, slab_e, order, sums, at, bytes, ld;
     Shape logits;
     Cut dh, de, de_last;
     bool sorts;      // the table's gradient gets the targets' rests, from sorted targets
-    GradPlan(int64_t rows, int64_t vocab, int64_t width, int dtype)
+    // copied: of a table that the products cannot read where it lies
+    GradPlan(int64_t rows, int64_t vocab, int64_t width, int dtype, bool copied)
     {
         const int planes = grad_planes(dtype);
+        const bool halves = planes > 1 && !streams(rows, logit_planes(dtype));      // of the table, for the logits
         ld = ceil_to(width, kStepK);
         dz_rows = ceil_to(rows, 64);
         const bool all_rest = keeps_all_rest(rows, vocab, width);
         deep = planes == 1 && all_rest ? 2 * dz_rows : dz_rows;
         piece = std::max<int64_t>(256, kPieceElements / deep / 256 * 256);
-        // pieces whose part of the table's gradient is whole rounds of wide tiles on all compute units, where they are
-        // large enough for that; else pieces of about the same size
+        const int64_t row = ld * (2 * planes + (halves ? 4 : 0));
+        if (copied) piece = std::min(piece, std::max<int64_t>(256, kGradCopyBytes / row / 256 * 256));
+        // pieces of about the same size, and whose part of the table's gradient is whole rounds of wide tiles on all
+        // compute units, where they are large enough for that
         const int64_t round = std::max<int64_t>(1, kUnits / ceil_div(width, shape_m(kWide, planes))) * shape_n(kWide, planes);
         if (vocab <= piece)
             piece = ceil_to(vocab, 256);
         else
-            piece = piece >= round ? piece / round * round : ceil_to(ceil_div(vocab, ceil_div(vocab, piece)), 256);
+            piece = piece >= round ? ceil_to(ceil_div(vocab, ceil_div(vocab, piece / round * round)), round)
+                                   : ceil_to(ceil_div(vocab, ceil_div(vocab, piece)), 256);
         dz_ld = piece;
         logits = shape_of(piece, rows, width, logit_planes(dtype));
         dh = layers(width, rows, std::min(piece, vocab), planes);
@@ -215,15 +227,15 @@ struct GradPlan {
         de_last = layers(width, ending, deep, planes);
         Carve c;
         h = c.take(deep * ld * 2 * planes);
-        table = c.take(piece * ld * 2 * planes);
+        table = copied ? c.take(piece * ld * 2 * planes) : 0;
         h16 = planes == 1 ? h : c.take(dz_rows * ld * 4);
-        table16 = planes == 1 ? table : c.take(piece * ld * 4);
+        table16 = halves ? c.take(piece * ld * 4) : table;
         h_e = planes == 1 ? 0 : c.take(exponents_of(dz_rows) * 4);
         table_e = planes == 1 ? 0 : c.take(exponents_of(piece) * 4);
         rest = planes == 1 ? c.take(rows * 4) : 0;
         dz = c.take(deep * dz_ld * 2 * planes);
         slab_h = dh.layers > 1 || piece < vocab ? c.take(dh.layers * rows * ld * 4) : 0;
-        const int64_t layered = std::max(de.layers > 1 ? de.layers * piece : 0, de_last.layers > 1 ? de_last.layers * ending : 0);
+        const int64_t layered = std::max(de.layers > 1 ? de.layers * std::min(piece, vocab) : 0, de_last.layers > 1 ? de_last.layers * ending : 0);
         slab_e = layered > 0 ? c.take(layered * ld * 4) : 0;
         sorts = planes == 1 && !all_rest;
         order = sorts ? c.take(TokenSumLayout(rows, width).bytes) : 0;
@@ -237,6 +249,11 @@ struct GradPlan {
         return cut_of(m, n, k, planes, std::max<int64_t>(1, std::min(ceil_div(k, kStepK) / 8, kSlabBytes / (ceil_to(m, kStepK) * n * 4))));
     }
 };
+inline int64_t grad_bytes(int64_t rows, int64_t vocab, int64_t width, int dtype)
+{
+    const int64_t copied = GradPlan(rows, vocab, width, dtype, true).bytes;
+    return may_lie(width, dtype) ? std::max(copied, GradPlan(rows, vocab, width, dtype, false).bytes) : copied;
+}
 
 }  // namespace vocab
 }  // namespace mesa

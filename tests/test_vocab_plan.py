@@ -13,12 +13,12 @@ WRAPPER = """
 #include "vocab_plan.hpp"
 using namespace mesa::vocab;
 extern "C" void plan(int64_t rows, int64_t vocab, int64_t width, int dtype, int64_t* out) {
-  const GradPlan g(rows, vocab, width, dtype);
+  const GradPlan g(rows, vocab, width, dtype, !may_lie(width, dtype));
   const ForwardPlan f(rows, vocab, width, dtype);
   const int planes = logit_planes(dtype);
   const int64_t at_once = streams(rows, planes) ? vocab : copy_rows(vocab, width, dtype);
   const int64_t x[] = {shape_of(at_once, rows, width, planes), ceil_div(vocab, at_once), g.logits, g.dh.shape, g.dh.layers,
-                       g.de.shape, g.de.layers, g.de_last.shape, g.de_last.layers, ceil_div(vocab, g.piece), g.piece, g.sorts, f.bytes, g.bytes};
+                       g.de.shape, g.de.layers, g.de_last.shape, g.de_last.layers, ceil_div(vocab, g.piece), g.piece, g.sorts, f.bytes, grad_bytes(rows, vocab, width, dtype)};
   for (int i = 0; i < 14; ++i) out[i] = x[i];
 }
 """

@@ -45,7 +45,8 @@ PIECES = [
     (9000, 16000, 40, BF16, 1, 2),       # the targets' rests, from sorted targets
     (17000, 9001, 32, BF16, 1, 2),       # the same over runs of sorted rows
     (16384, 9000, 2048, BF16, 1, 2),     # wide tiles, no layers
-    (40, 70000, 2048, F32, 3, 1),        # planes and exponents of a table that is copied
+    (40, 70000, 2048, F32, 3, 2),        # planes and exponents of a table that is copied
+    (20, 100000, 2048, F32, 1, 2),       # few rows, which read it as it lies for the logits
     (16384, 8500, 24, F32, 1, 2),        # layers of dh, added to by the second piece
     (4100, 40001, 300, F32, 1, 2),       # wide tiles
 ]
