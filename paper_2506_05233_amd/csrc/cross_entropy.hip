@@ -1207,9 +1207,11 @@ hipError_t launch_cross_entropy_grad(const CrossEntropyGradArgs& a, hipStream_t 
     auto words = [&](int64_t at) { return reinterpret_cast<uint16_t*>(ws + at); };
     uint16_t* dz = words(plan.dz);
     float* rest = planes == 1 ? reinterpret_cast<float*>(ws + plan.rest) : nullptr;
-    const int64_t dz_plane = plan.deep * plan.dz_ld;
-    const Matrix h{words(plan.h), ld, plan.deep * ld, plan.deep, ld};
-    const bool twice = plan.deep > plan.dz_rows;
+    const int64_t dz_plane = plan.dz_rows * plan.dz_ld;      // of fp32
+    // dz's rest and h once more are for the table's gradient
+    const bool twice = plan.deep > plan.dz_rows && a.dtable != nullptr;
+    const int64_t deep = twice ? plan.deep : plan.dz_rows;
+    const Matrix h{words(plan.h), ld, deep * ld, deep, ld};
     Finish more{};
     TokenSumArgs sums{};
     const bool sorts = plan.sorts && a.dtable != nullptr;
@@ -1239,7 +1241,7 @@ hipError_t launch_cross_entropy_grad(const CrossEntropyGradArgs& a, hipStream_t 
         LogitsArgs k{};
         if (planes == 1) {
             e = pack_copy(first > 0 ? PackArgs{} : PackArgs{static_cast<const uint16_t*>(a.h), a.rows, a.width, a.h_stride, a.targets, a.vocab,
-                                                            words(plan.h), plan.deep, ld, twice ? plan.dz_rows : 0},
+                                                            words(plan.h), deep, ld, twice ? plan.dz_rows : 0},
                           as_is ? PackArgs{} : PackArgs{reinterpret_cast<const uint16_t*>(src), piece, a.width, a.table_stride, {}, 0, words(plan.table), piece, ld},
                           stream);
             k.table = table;
@@ -1284,7 +1286,7 @@ hipError_t launch_cross_entropy_grad(const CrossEntropyGradArgs& a, hipStream_t 
             return hipGetLastError();
         });
         if (e != hipSuccess) return e;
-        const Matrix dz_rows{dz, plan.dz_ld, dz_plane, plan.deep, plan.dz_ld};
+        const Matrix dz_rows{dz, plan.dz_ld, dz_plane, deep, plan.dz_ld};
         if (a.dh != nullptr) {
             const bool slab = plan.dh.layers > 1 || plan.piece < a.vocab;
             GradArgs d{};
@@ -1316,8 +1318,8 @@ hipError_t launch_cross_entropy_grad(const CrossEntropyGradArgs& a, hipStream_t 
             GradArgs d{};
             d.a = h;
             d.b = dz_rows;
-            d.k = plan.deep;
-            d.k_split = ceil_to(ceil_div(plan.deep, cut.layers), kStepK);
+            d.k = deep;
+            d.k_split = ceil_to(ceil_div(deep, cut.layers), kStepK);
             const int64_t layers = ceil_div(d.k, d.k_split);
             d.tiles_m = ceil_div(a.width, shape_m(shape, planes));
             d.tiles_n = ceil_div(piece, shape_n(shape, planes));
