@@ -154,10 +154,12 @@ struct RowArgs {
     Tokens targets;          // as in PackArgs
     int64_t vocab;
     uint16_t* halves;        // two planes of [out_rows, ld], or null
-    int32_t* exponent;       // [exponents]: e, and zeros, which whole tiles read
+    int32_t* exponent;       // of halves, [exponents]: e, and zeros, which whole tiles read
     int64_t exponents;
     uint16_t* parts;         // three planes, or null
     int64_t out_rows, ld;
+    // a wave each; neither planes: nothing to do
+    int64_t waves() const { return halves != nullptr ? exponents : parts != nullptr ? out_rows : 0; }
 };
 
 __device__ __forceinline__ void two_halves(float x, int e, uint32_t& hi, uint32_t& lo)
@@ -178,7 +180,7 @@ __global__ void __launch_bounds__(kPackThreads) pack_rows_kernel(RowArgs one, Ro
     const int lane = int(threadIdx.x) % kWave;
     const int64_t row = int64_t(blockIdx.x - (first ? 0 : blocks_one)) * kRows + threadIdx.x / kWave;
     if (row >= a.out_rows) {
-        if (lane == 0 && row < a.exponents) a.exponent[row] = 0;
+        if (lane == 0 && a.halves != nullptr && row < a.exponents) a.exponent[row] = 0;
         return;
     }
     bool counts = row < a.rows;
@@ -199,21 +201,24 @@ __global__ void __launch_bounds__(kPackThreads) pack_rows_kernel(RowArgs one, Ro
                 if (c + v < a.width) x[v] = src[c + v];
         }
     };
-    uint32_t most = 0;       // bits of the largest finite magnitude
-    for (int64_t c = int64_t(lane) * 8; c < a.width; c += kWave * 8) {
-        float x[8];
-        load(c, x);
+    int e = 0;
+    if (a.halves != nullptr) {
+        uint32_t most = 0;       // bits of the largest finite magnitude
+        for (int64_t c = int64_t(lane) * 8; c < a.width; c += kWave * 8) {
+            float x[8];
+            load(c, x);
 #pragma unroll
-        for (int v = 0; v < 8; ++v) {
-            const uint32_t u = abs_bits(x[v]);
-            most = u < 0x7F800000u ? max(most, u) : most;
+            for (int v = 0; v < 8; ++v) {
+                const uint32_t u = abs_bits(x[v]);
+                most = u < 0x7F800000u ? max(most, u) : most;
+            }
         }
-    }
 #pragma unroll
-    for (int d = 1; d < kWave; d *= 2) most = max(most, uint32_t(__shfl_xor(int(most), d)));
-    // ilogb of it (of a subnormal by its fraction); a row of zeros is not scaled
-    const int e = most == 0 ? 0 : __builtin_amdgcn_frexp_expf(__uint_as_float(most)) - 1 - 14;
-    if (lane == 0) a.exponent[row] = e;
+        for (int d = 1; d < kWave; d *= 2) most = max(most, uint32_t(__shfl_xor(int(most), d)));
+        // ilogb of it (of a subnormal by its fraction); a row of zeros is not scaled
+        e = most == 0 ? 0 : __builtin_amdgcn_frexp_expf(__uint_as_float(most)) - 1 - 14;
+        if (lane == 0) a.exponent[row] = e;
+    }
     const int64_t plane = a.out_rows * a.ld;
     for (int64_t c = int64_t(lane) * 8; c < a.ld; c += kWave * 8) {
         float x[8];
@@ -248,7 +253,7 @@ __global__ void __launch_bounds__(kPackThreads) pack_rows_kernel(RowArgs one, Ro
 // Either may have no rows.
 hipError_t pack_rows(const RowArgs& one, const RowArgs& two, hipStream_t stream)
 {
-    const int64_t b1 = ceil_div(one.exponents, kPackThreads / kWave), b2 = ceil_div(two.exponents, kPackThreads / kWave);
+    const int64_t b1 = ceil_div(one.waves(), kPackThreads / kWave), b2 = ceil_div(two.waves(), kPackThreads / kWave);
     if (b1 + b2 == 0) return hipSuccess;
     if (!grid_fits(b1 + b2, kPackThreads)) return hipErrorInvalidConfiguration;
     hipLaunchKernelGGL(pack_rows_kernel, dim3(unsigned(b1 + b2)), dim3(kPackThreads), 0, stream, one, two, unsigned(b1));
@@ -1137,10 +1142,10 @@ hipError_t launch_cross_entropy(const CrossEntropyArgs& a, hipStream_t stream)
             e = pack_copy(first > 0 || h_as_is ? PackArgs{} : PackArgs{static_cast<const uint16_t*>(a.h), a.rows, a.width, a.h_stride, {}, 0, h, a.rows, ld},
                           as_is ? PackArgs{} : PackArgs{src, k.piece, a.width, a.table_stride, {}, 0, copy, k.piece, ld}, stream);
         } else {
-            e = pack_rows(first > 0 ? RowArgs{} : RowArgs{static_cast<const float*>(a.h), a.rows, a.width, a.h_stride, {}, 0, h,
+            e = pack_rows(first > 0 ? RowArgs{} : RowArgs{static_cast<const float*>(a.h), a.rows, a.width, a.h_stride, {}, 0, stream_table ? nullptr : h,
                                                            reinterpret_cast<int32_t*>(ws + plan.h_e), exponents_of(a.rows), parts, a.rows, ld},
-                          stream_table ? RowArgs{} : RowArgs{reinterpret_cast<const float*>(src), k.piece, a.width, a.table_stride, {}, 0, copy, reinterpret_cast<int32_t*>(ws + plan.table_e), exponents_of(k.piece),
-                                  nullptr, k.piece, ld},
+                          stream_table ? RowArgs{} : RowArgs{reinterpret_cast<const float*>(src), k.piece, a.width, a.table_stride, {}, 0, copy,
+                                                             reinterpret_cast<int32_t*>(ws + plan.table_e), exponents_of(k.piece), nullptr, k.piece, ld},
                           stream);
         }
         if (e != hipSuccess) return e;
@@ -1249,10 +1254,12 @@ hipError_t launch_cross_entropy_grad(const CrossEntropyGradArgs& a, hipStream_t 
         } else {
             const bool streamed = streams(a.rows, logit_planes(a.dtype));
             int32_t *h_e = reinterpret_cast<int32_t*>(ws + plan.h_e), *table_e = reinterpret_cast<int32_t*>(ws + plan.table_e);
+            // parts of h for the table's gradient, of the table for dh, and of few rows of h for the logits
             e = pack_rows(first > 0 ? RowArgs{} : RowArgs{static_cast<const float*>(a.h), a.rows, a.width, a.h_stride, a.targets, a.vocab,
-                                                           words(plan.h16), h_e, exponents_of(plan.dz_rows), words(plan.h), plan.dz_rows, ld},
+                                                           streamed ? nullptr : words(plan.h16), h_e, exponents_of(plan.dz_rows),
+                                                           streamed || a.dtable != nullptr ? words(plan.h) : nullptr, plan.dz_rows, ld},
                           RowArgs{reinterpret_cast<const float*>(src), piece, a.width, a.table_stride, {}, 0, streamed ? nullptr : words(plan.table16), table_e,
-                                  exponents_of(piece), words(plan.table), piece, ld},
+                                  exponents_of(piece), a.dh != nullptr ? words(plan.table) : nullptr, piece, ld},
                           stream);
             k.table = Matrix{words(plan.table16), ld, piece * ld, piece, ld};
             k.h = streamed ? h : Matrix{words(plan.h16), ld, plan.dz_rows * ld, plan.dz_rows, ld};

@@ -180,11 +180,12 @@ struct ForwardPlan {
         best_z = c.take(tiles * rows * 4);
         best_v = c.take(tiles * rows * 4);
         at = c.take(rows * 4);
-        h = c.take(rows * row);
+        const bool halves = planes > 1 && !streams(rows, planes);
+        h = planes == 1 || halves ? c.take(rows * row) : 0;
         h_parts = streams(rows, planes) ? c.take(rows * ceil_to(width, kStepK) * 6) : 0;
         table = c.take(copied * row);
-        h_e = planes == 1 ? 0 : c.take(exponents_of(rows) * 4);
-        table_e = planes == 1 ? 0 : c.take(exponents_of(copied) * 4);
+        h_e = halves ? c.take(exponents_of(rows) * 4) : 0;
+        table_e = halves ? c.take(exponents_of(copied) * 4) : 0;
         bytes = c.at;
     }
 };
@@ -228,10 +229,10 @@ struct GradPlan {
         Carve c;
         h = c.take(deep * ld * 2 * planes);
         table = copied ? c.take(piece * ld * 2 * planes) : 0;
-        h16 = planes == 1 ? h : c.take(dz_rows * ld * 4);
+        h16 = halves ? c.take(dz_rows * ld * 4) : h;
         table16 = halves ? c.take(piece * ld * 4) : table;
-        h_e = planes == 1 ? 0 : c.take(exponents_of(dz_rows) * 4);
-        table_e = planes == 1 ? 0 : c.take(exponents_of(piece) * 4);
+        h_e = halves ? c.take(exponents_of(dz_rows) * 4) : 0;
+        table_e = halves ? c.take(exponents_of(piece) * 4) : 0;
         rest = planes == 1 ? c.take(rows * 4) : 0;
         dz = c.take(deep * dz_ld * 2 * planes);
         slab_h = dh.layers > 1 || piece < vocab ? c.take(dh.layers * rows * ld * 4) : 0;

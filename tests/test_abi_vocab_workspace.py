@@ -40,3 +40,10 @@ def test_bound(dtype):
 def test_few_rows(rows, vocab, width, dtype, most):
     """Of fp32 no more of the table than its three planes, and no more than 1 GiB of it."""
     assert L.cross_entropy_backward_workspace_bytes(rows, vocab, width, dtype) <= most * MIB
+
+
+def test_few_fp32_rows_forward():
+    """Three planes of h, the tiles' sums, and nothing of the two planes that more rows take."""
+    for rows, vocab in ((1, 50), (32, 50), (32, 50257)):
+        tiles = -(-vocab // 64)
+        assert L.cross_entropy_workspace_bytes(rows, vocab, 65536, F32) <= rows * 65536 * 6 + 16 * rows * tiles + 4 * rows + 2048

@@ -44,3 +44,17 @@ def test_sums_of_targets_without_the_tables_gradient():
     """The targets' rests, [rows, width] fp32, and what sorts them."""
     rows, vocab, width = 4100, 2003, 1024
     assert _untouched(rows, vocab, width, C.BF16, want_dtable=False) >= rows * width * 4 + vocab * 4
+
+
+def test_without_the_rows_gradient():
+    """fp32: three planes of the table are for dh alone.  (Up to 32 rows nothing else of it is laid out, past them two planes.)"""
+    vocab, width = 20000, 512
+    planes = vocab * width * 6
+    for rows in (20, 70):
+        assert _untouched(rows, vocab, width, C.F32) < planes <= _untouched(rows, vocab, width, C.F32, want_dh=False)
+
+
+def test_fp32_without_the_tables_gradient():
+    """The three planes of h are for the table's gradient alone, past 32 rows."""
+    rows, width = 2000, 1024
+    assert _untouched(rows, 70, width, C.F32) < rows * width * 6 <= _untouched(rows, 70, width, C.F32, want_dtable=False)
