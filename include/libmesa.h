@@ -563,8 +563,10 @@ int mesa_embedding_backward(const void* token, int token_bytes, const void* dy, 
  *     loss_n = lse_n - l_n,target  (0 where the target does not count)
  *     best_n = the lowest v whose z_nv is the largest (-1 where every one is a NaN)
  *   h, table   dtype (MESA_DTYPE_F32, MESA_DTYPE_BF16).  Sums are fp32; products of bf16 are exact.  Those of fp32 are
- *              formed from parts of 16 bits, the logits' to 2^-21 of each product (and 2^-39 of their rows' largest
- *              magnitudes), the gradients' to 2^-24; an infinity among fp32 factors makes its sums NaN
+ *              formed from parts of 16 bits: of up to 32 rows, and the gradients', from three to 2^-24 of each product,
+ *              the logits of more from two, for speed, to 2^-21 of each (and 2^-39 of their rows' largest magnitudes: a
+ *              row with a channel more than 2^16 times the others holds those in fewer bits beside 32 other rows
+ *              than among fewer); an infinity among fp32 factors makes its sums NaN
  *   target, loss [rows] fp32: both or neither (then only lse and best are computed)
  *   lse [rows] fp32;  best int32 [rows], or NULL
  *   cap        0, or finite, positive and no subnormal number

@@ -81,3 +81,29 @@ def test_a_nan_in_the_table_of_rows_that_count(dtype):
     f = L.cross_entropy(h, table, targets, cap=30.0)
     g = L.cross_entropy_backward(h, table, targets, f["lse"], up, cap=30.0)
     assert bool(f["lse"].isnan().all()) and bool(g["dh"].isnan().all()) and bool(g["dtable"].isnan().all())
+
+
+@pytest.mark.parametrize("rows", [1, 32, 33, 64, 200])
+@pytest.mark.parametrize("cap", [0.0, 30.0])
+def test_one_channel_far_above_the_others(rows, cap):
+    """fp32 rows with a channel 2^30 times the others, which the table does not take.  Up to 32 rows, of three parts each, every
+    product is good to 2^-23 of itself; more are held in two parts of 11 bits below their row's largest magnitude, so the
+    others may be off by 2^-39 of that: 2^-9 of themselves here."""
+    h, table, t, up = _problem(rows, 300, 96, F32, rows)
+    h[:, 5], table[:, 5] = 2.0 ** 30, 0.0
+    f = L.cross_entropy(h, table, torch.from_numpy(t).cuda(), cap=cap)
+    g = L.cross_entropy_backward(h, table, torch.from_numpy(t).cuda(), f["lse"], up, cap=cap)
+    held = _np(h)
+    if rows <= 32:
+        held[:, 5] = 0.0      # it takes no part in the bounds
+    want, grads = E.cross_entropy(_np(h), _np(table), t, cap), E.cross_entropy_backward(_np(h), _np(table), t, _np(up), cap)
+    bound = E.cross_entropy_bounds(held, _np(table), t, _np(up), cap, False)
+    for n, got, ref in (("lse", f["lse"], want["lse"]), ("loss", f["loss"], want["loss"]), ("dh", g["dh"], grads["dh"])):
+        assert (np.abs(_np(got) - ref) <= bound[n]).all(), n
+    keep = np.arange(96) != 5
+    assert (np.abs(_np(g["dtable"]) - grads["dtable"]) <= bound["dtable"])[:, keep].all()
+    # and the same rows among more: to the sum of both bounds
+    if rows == 32:
+        more = L.cross_entropy(torch.cat([h, h]), table, torch.from_numpy(np.concatenate([t, t])).cuda(), cap=cap)
+        wide = E.cross_entropy_bounds(_np(h), _np(table), t, _np(up), cap, False)
+        assert (np.abs(_np(more["lse"][:32]) - _np(f["lse"])) <= wide["lse"] + bound["lse"]).all()
