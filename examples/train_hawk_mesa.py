@@ -58,6 +58,7 @@ class Block:
     def features(self, tokens, reset, keep=True):
         """What the logits are formed from, [B, T, DIM], and, with keep, what the backward pass needs."""
         p, B, T = self.p, *tokens.shape
+        tokens = tokens.contiguous()
         e = L.embedding(p["embed"], tokens)
         x, r, i = (e @ p["hawk_in"]).split(WIDTH, dim=-1)
         rec = L.recurrence(x, r, i, p["theta"], reset=reset, want_final=True, want_states=keep, want_checkpoints=keep)
@@ -85,7 +86,7 @@ class Block:
 
     def loss(self, out, answers):
         """The mean cross entropy of the answers [B, T] (-1: none), and its gradients for `out` and the logits' weights."""
-        p, count = self.p, (answers >= 0).sum()
+        p, count, answers = self.p, (answers >= 0).sum(), answers.contiguous()
         f = L.cross_entropy(out, p["logits"], answers)
         each = (1.0 / count).expand(answers.shape).contiguous()
         g = L.cross_entropy_backward(out, p["logits"], answers, f["lse"], each)
@@ -138,7 +139,7 @@ class Block:
     def decode(self, token, state):
         """Logits [B, VOCAB] of the next token [B], and `state` moved on by it."""
         p, B = self.p, token.shape[0]
-        e = L.embedding(p["embed"], token)
+        e = L.embedding(p["embed"], token.contiguous())
         x, r, i = (e @ p["hawk_in"]).split(WIDTH, dim=-1)
         z = e + L.recurrence_step(state["h"], x, r, i, p["theta"]) @ p["hawk_out"]
         heads, a_gamma, a_beta = self._mesa_inputs((z @ p["mesa_in"])[:, None])
@@ -193,7 +194,7 @@ def check_decode(block, device="cuda", say=print):
     reset.zero_()
     want, _ = block.forward(tokens, reset, keep=False)
     _, state = block.forward(tokens[:, :70].contiguous(), reset[:, :70].contiguous(), keep=False)
-    worst = max(float((block.decode(tokens[:, t].contiguous(), state) - want[:, t]).abs().max()) for t in range(70, 80))
+    worst = max(float((block.decode(tokens[:, t], state) - want[:, t]).abs().max()) for t in range(70, 80))
     say("decoding a token at a time: largest difference %.1e of %.1f" % (worst, float(want.abs().max())))
     return worst / float(want.abs().max())
 
