@@ -59,7 +59,6 @@ struct Shapes<3> {
     using Wide = TileShape<3, 128, 256, 2, 4>;
     using Middle = TileShape<3, 128, 128, 2, 4>;
     using Narrow = TileShape<3, 64, 64, 2, 2>;
-    using Thin = Narrow;
 };
 
 // ------------------------------------------------------------------ operands as the products read them
@@ -1049,14 +1048,18 @@ __global__ void __launch_bounds__(kSumThreads) layer_sum_kernel(SumArgs a)
 }
 
 // ------------------------------------------------------------------ the tiles' launches
+template <int Planes, class S>
+constexpr bool planned(Shape s)
+{
+    return S::M == kTileRows[Planes - 1][s] && S::N == kTileColumns[Planes - 1][s] && S::K == step_of(Planes);
+}
 template <int Planes>
 constexpr bool planned()
 {
     using P = Shapes<Planes>;
-    constexpr int m[] = {P::Wide::M, P::Middle::M, P::Narrow::M, P::Thin::M}, n[] = {P::Wide::N, P::Middle::N, P::Narrow::N, P::Thin::N};
-    for (int s = 0; s < 4; ++s)
-        if (m[s] != kTileRows[Planes - 1][s] || n[s] != kTileColumns[Planes - 1][s]) return false;
-    return step_k(Planes) == step_of(Planes);
+    bool all = planned<Planes, typename P::Wide>(kWide) && planned<Planes, typename P::Middle>(kMiddle) && planned<Planes, typename P::Narrow>(kNarrow);
+    if constexpr (Planes < 3) all = all && planned<Planes, typename P::Thin>(kThin);
+    return all;
 }
 static_assert(planned<1>() && planned<2>() && planned<3>() && Stream::kRows == kStreamRows, "the tiles that the plans are made for");
 
@@ -1067,8 +1070,10 @@ hipError_t with_shape(Shape s, F f)
     switch (s) {
         case kWide: return f(typename P::Wide{});
         case kMiddle: return f(typename P::Middle{});
-        case kNarrow: return f(typename P::Narrow{});
-        default: return f(typename P::Thin{});
+        case kThin:
+            if constexpr (Planes < 3) return f(typename P::Thin{});
+            [[fallthrough]];
+        default: return f(typename P::Narrow{});
     }
 }
 // A product of logits (bf16 or fp16 planes), and one of a gradient (bf16, one plane or three).

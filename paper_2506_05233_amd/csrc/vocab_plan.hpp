@@ -69,9 +69,10 @@ constexpr int64_t kMostTiles = int64_t(UINT32_MAX) / 512;      // of a launch, w
 enum Shape { kWide, kMiddle, kNarrow, kThin };
 inline int logit_planes(int dtype) { return dtype == kBf16 ? 1 : 2; }
 inline int grad_planes(int dtype) { return dtype == kBf16 ? 1 : 3; }
-// Rows of the tile (of the table, or channels) and columns (of h, or of the table).
-constexpr int kTileRows[3][4] = {{256, 128, 64, 64}, {128, 128, 64, 64}, {128, 128, 64, 64}};
-constexpr int kTileColumns[3][4] = {{256, 128, 64, 32}, {256, 128, 64, 32}, {256, 128, 64, 64}};
+// Rows of the tile (of the table, or channels) and columns (of h, or of the table).  There is a thin one of bf16 and of
+// fp32 logits.
+constexpr int kTileRows[3][4] = {{256, 128, 64, 64}, {128, 128, 64, 64}, {128, 128, 64, 0}};
+constexpr int kTileColumns[3][4] = {{256, 128, 64, 32}, {256, 128, 64, 32}, {256, 128, 64, 0}};
 inline int64_t shape_m(Shape s, int planes) { return kTileRows[planes - 1][s]; }
 inline int64_t shape_n(Shape s, int planes) { return kTileColumns[planes - 1][s]; }
 constexpr int step_of(int planes) { return planes == 1 ? 64 : 32; }      // of k
@@ -87,14 +88,15 @@ struct Cost {
     float alone, alone_step, shared, shared_step;
     int per_unit;
 };
-constexpr Cost kCost[3][4] = {
-    {{11.6f, 1.29f, 11.6f, 1.29f, 1}, {6.5f, 0.69f, 3.35f, 0.47f, 2}, {4.4f, 0.44f, 0.84f, 0.196f, 5}, {4.0f, 0.40f, 0.6f, 0.12f, 6}},
-    {{11.2f, 1.00f, 11.2f, 1.00f, 1}, {9.5f, 0.67f, 4.2f, 0.64f, 2}, {5.8f, 0.375f, 0.92f, 0.307f, 5}, {5.8f, 0.375f, 0.92f, 0.307f, 5}},
-    {{9.2f, 1.91f, 9.2f, 1.91f, 1}, {5.7f, 1.22f, 5.7f, 1.22f, 1}, {4.3f, 0.62f, 0.90f, 0.40f, 3}, {4.3f, 0.62f, 0.90f, 0.40f, 3}}};
+constexpr Cost kCost[3][3] = {
+    {{11.6f, 1.29f, 11.6f, 1.29f, 1}, {6.5f, 0.69f, 3.35f, 0.47f, 2}, {4.4f, 0.44f, 0.84f, 0.196f, 5}},
+    {{11.2f, 1.00f, 11.2f, 1.00f, 1}, {9.5f, 0.67f, 4.2f, 0.64f, 2}, {5.8f, 0.375f, 0.92f, 0.307f, 5}},
+    {{9.2f, 1.91f, 9.2f, 1.91f, 1}, {5.7f, 1.22f, 5.7f, 1.22f, 1}, {4.3f, 0.62f, 0.90f, 0.40f, 3}}};
+constexpr Cost kThinCost = {4.0f, 0.40f, 0.6f, 0.12f, 6};      // of bf16
 
 inline float cost_of(Shape s, int planes, int64_t tiles, int64_t k)
 {
-    const Cost& c = kCost[planes - 1][s];
+    const Cost& c = s == kThin ? kThinCost : kCost[planes - 1][s];
     const float steps = float(ceil_div(k, step_of(planes))), alone = c.alone + c.alone_step * steps, shared = c.shared + c.shared_step * steps;
     const int64_t each = ceil_div(tiles, kUnits), rounds = each / c.per_unit, rest = each % c.per_unit;
     return float(rounds) * std::max(alone, shared * float(c.per_unit)) + (rest > 0 ? std::max(alone, shared * float(rest)) : 0.0f);
@@ -112,10 +114,10 @@ inline bool streams(int64_t n, int planes) { return planes == 2 && n <= kStreamR
 inline Cut cut_of(int64_t m, int64_t n, int64_t k, int planes, int64_t most)
 {
     Cut best{kThin, 1};
+    if (streams(n, planes)) return best;
     float least = 0.0f;
     for (Shape s : {kWide, kMiddle, kNarrow, kThin}) {
-        if (s == kThin && n > 32) continue;      // it reads the table's rows once for 32 of the others
-        if (s != kThin && streams(n, planes)) continue;
+        if (s == kThin && (planes != 1 || n > 32)) continue;      // it reads the table's rows once for 32 of the others
         const int64_t tiles = ceil_div(m, shape_m(s, planes)) * ceil_div(n, shape_n(s, planes));
         for (int64_t l = 1; l <= most; l += l < 4 ? 1 : l / 2) {
             const float sum = l > 1 ? 5.0f + float(l) * float(m) * float(n) * 1e-6f : 0.0f;
