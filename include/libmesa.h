@@ -583,10 +583,11 @@ int mesa_embedding_backward(const void* token, int token_bytes, const void* dy, 
  *   target's element, which is as large as the others of its row together; dtable of up to 1024 rows, or
  *   rows vocab width up to 4.3e9, what it takes off all.
  *   With rows 0 dtable is zeros.  Up to nine kernel launches a piece, and up to eight before the first.
- *   The workspace holds of a piece dz, at most 2^27 elements or 256 columns, of 2 bytes (fp32: 6), and a
- *   copy of its part of the table, at most 1 GiB or 256 rows (2 bytes an element, of fp32 10, 6 for up to
- *   32 rows; the query counts it also where the table turns out to need none); copies and sums of the
- *   rows, at most 10 bytes an element; and sums of layers, at most 512 MiB or 4 bytes an element. */
+ *   The workspace holds of a piece dz, with its rest at most 2^27 elements or 256 columns (of each), of 2 bytes
+ *   (fp32: 6), and a copy of its part of the table, at most 1 GiB or 256 rows (2 bytes an element, of fp32
+ *   10, 6 for up to 32 rows; the query counts it also where the table turns out to need none); copies and
+ *   sums of the rows, at most 10 bytes an element; sums of layers, at most 512 MiB or 4 bytes an element; and
+ *   some 32 bytes a row and 4 a row of the table. */
 size_t mesa_cross_entropy_workspace_bytes(int64_t rows, int64_t vocab, int64_t width, int dtype);
 int mesa_cross_entropy(const void* h, const void* table, const void* target, int token_bytes, float cap, int64_t rows,
                        int64_t vocab, int64_t width, int64_t h_stride, int64_t table_stride, int dtype, float* loss,

@@ -10,9 +10,9 @@
 // sum of exponentials to it, and a small launch joins them.  Backward, dz is formed a piece of the vocabulary
 // at a time and multiplied from both sides while it lies in the last cache.
 //
-// Training passes over 16384 rows by 50257 of 2048 bf16 channels take 11.2 ms, logits 2.69 (1250 TFLOP/s), dz
-// 3.09, dh 2.83, the table's gradient 2.61; over 777 rows by 5003 of 768 fp32 ones 188 us.  One row by 50257 of 2048
-// takes 53 us, which reads its 206 MB at 4.4 TB/s, 256 rows 78.
+// Training passes over 16384 rows by 50257 of 2048 bf16 channels take 11.3 to 11.8 ms by the clock that the card holds, logits
+// 2.74 (1231 TFLOP/s), dz 3.13, dh 2.99, the table's gradient 2.75 and the targets' rests 0.17; over 777 rows by 5003 of
+// 768 fp32 ones 186 us.  One row by 50257 of 2048 takes 54 us, which reads its 206 MB at 4.4 TB/s, 256 rows 76.
 //
 // fp32 is multiplied as parts of 16 bits: the logits of more than 32 rows from two fp16 parts of rows scaled by a power of two (three
 // products; the first version took three bf16 parts, six products: 80 us and 38 for 777 rows by 5003 of 768), the
@@ -746,8 +746,8 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(JoinArgs a)
 }
 
 // ------------------------------------------------------------------ the gradient
-// dz of one tile, from the same product: 492 us for 16384 rows by 8192 of 2048 channels (1117 TFLOP/s), of which the
-// product alone is some 430; the rest are its exponentials and 268 MB written.
+// dz of one tile, from the same product: 503 us for 16384 rows by 8192 of 2048 channels (1093 TFLOP/s), of which the
+// product alone is some 440; the rest are its exponentials and 268 MB written.
 template <class S>
 __global__ void __launch_bounds__(S::kThreads) logits_grad_kernel(LogitsArgs a)
 {
@@ -940,8 +940,8 @@ __device__ __forceinline__ void put4(T* p, int n, bool wide, const f32x4& y)
 }
 
 // AlongB: dh, whose k is the vocabulary, else the table's gradient, whose k are the rows; k lies across the
-// memory's rows of A, and there of B too, and is read transposed from LDS.  16384 rows by 8192 of 2048 channels 451
-// and 421 us (1219 and 1306 TFLOP/s).  Few tiles are cut into layers of k, added up by the next launch: dh of 3997 rows
+// memory's rows of A, and there of B too, and is read transposed from LDS.  16384 rows by 8192 of 2048 channels 470
+// and 439 us (1170 and 1252 TFLOP/s).  Few tiles are cut into layers of k, added up by the next launch: dh of 3997 rows
 // of 1000 by 32003 are 64 tiles, in four layers 250 us.  Both in one launch, so that the one's last tiles run
 // beside the other's first, was slower (211 us for 204 of a pass over 777 rows, 11.8 ms for 11.5 over 16384).
 template <class S, bool AlongB>
