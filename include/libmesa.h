@@ -539,7 +539,8 @@ int mesa_output_norm_backward(const void* o, const float* weight, float eps, con
  *     (MESA_ERR_SHAPE otherwise, as for a launch of 2^32 threads or more);
  *   - outputs and workspaces must overlap neither an input nor each other (MESA_ERR_ARG; slices of
  *     one array with the same stride may interleave); workspaces are 16-byte aligned and hold at
- *     least what the call's *_workspace_bytes says;
+ *     least what the call's *_workspace_bytes says (of the cross entropy's more rows may ask for less:
+ *     a workspace for several sizes takes the largest of their queries);
  *   - sums are fp32 and in a fixed order: the same inputs give the same bits.
  *
  * mesa_embedding: out_n = scale E[token_n], a row of zeros where there is no token; dtype is the
